@@ -323,6 +323,77 @@ int gem_nlr_run_host_timed(const gem_nlr_params *params, const float *X_host, fl
 int gem_nlr_column_sums_static(const float *U_dev, int64_t n, int32_t r, float *p_dev,
                                void *cuda_stream);
 
+/* ---- Training an encoder on the cluster labels -----------------------------------------------------------
+ * Features that are clustered come from an encoder, and the labels that come back are what the next round of
+ * its training aims at.  These calls are the parts of such a training step that are not matrix products: layer
+ * norm and its gradient, softmax cross entropy against the int32 labels of gem_nlr_labels with its gradient, and
+ * the norm of all gradients with clipping.  They need no handle.
+ *
+ * All matrices are row-major with rows `ld` elements apart (ld >= columns for outputs; inputs take any ld >= 0,
+ * 0 meaning that every row is the same one).  Pointers need only their element type's alignment; 16-byte aligned
+ * rows are fastest.  Elements are GEM_NLR_F32, GEM_NLR_F16 or GEM_NLR_BF16; sums, statistics and everything in
+ * between is held in FP32 or FP64 and rounded once when stored.  Outputs overlap neither each other nor an input,
+ * except where a call says so.  Results are the same bits on every call (no floating-point atomics).
+ * Work is enqueued on cuda_stream, whose device must be current; nothing is allocated and no call synchronizes,
+ * so all of them can be captured into a graph.  scratch_dev (256-byte aligned, at least the bytes that the
+ * matching *_scratch_bytes call names; contents never matter) is used until the work has run.
+ * They return GEM_NLR_OK, GEM_NLR_E_INVALID, GEM_NLR_E_WORKSPACE (scratch missing, misaligned or too small) or
+ * GEM_NLR_E_CUDA (a launch failed).  The paper has no counterpart of this section.                            */
+#define GEM_NLR_F32  0
+#define GEM_NLR_F16  1
+#define GEM_NLR_BF16 2
+
+/* y_ij = (x_ij - mean_i) rstd_i w_j + b_j with mean_i = (1/d) sum_j x_ij, rstd_i = 1 / sqrt((1/d) sum_j (x_ij -
+ * mean_i)^2 + eps).  x, y: n x d of `type`; weight, bias: d values of `wtype` (FP32, or the same as `type`), NULL
+ * for ones and zeros; mean, rstd: n floats, may be NULL.  n >= 0, d >= 1, eps >= 0.  A row that holds an infinity
+ * or a NaN gives NaN; no other row sees it.                                                                    */
+int gem_nlr_layer_norm(const void *x_dev, int32_t type, int64_t ld_x, const void *weight_dev, const void *bias_dev,
+                       int32_t wtype, int64_t n, int32_t d, float eps, void *y_dev, int64_t ld_y, float *mean_dev,
+                       float *rstd_dev, void *cuda_stream);
+
+/* The gradient: with h_ij = (x_ij - mean_i) rstd_i and g_ij = dy_ij w_j,
+ *   dx_ij = rstd_i (g_ij - (1/d) sum_j g_ij - h_ij (1/d) sum_j g_ij h_ij),  dw_j = sum_i dy_ij h_ij,  db_j = sum_i dy_ij.
+ * dy, x, dx: n x d of `type`; mean, rstd: as the forward pass wrote them; weight: d of `wtype` or NULL (ones).
+ * dx, dweight and dbias (d of `wtype`) may each be NULL when not wanted, not all three.  n == 0 gives zero sums.  */
+size_t gem_nlr_layer_norm_backward_scratch_bytes(int64_t n, int32_t d);
+int gem_nlr_layer_norm_backward(const void *dy_dev, int64_t ld_dy, const void *x_dev, int64_t ld_x, int32_t type,
+                                const float *mean_dev, const float *rstd_dev, const void *weight_dev, int32_t wtype,
+                                int64_t n, int32_t d, void *dx_dev, int64_t ld_dx, void *dweight_dev,
+                                void *dbias_dev, void *scratch_dev, size_t scratch_bytes, void *cuda_stream);
+
+/* row_loss_i = log sum_j exp z_ij - z_i,label(i);  loss = s sum_i row_loss_i;  dz_ij = s (softmax(z_i)_j - [j = label(i)])
+ * with s = 1 (mean == 0) or 1 / (number of rows that count) (mean == 1).  logits: n x k of `type`; labels: n int32;
+ * loss: one float; row_loss: n floats; dlogits: n x k of `type`, NULL for the loss alone; it may be the logits
+ * themselves (same pointer and ld).
+ * A row with a negative label does not count: its loss and gradient are 0 whatever its logits hold; when no row
+ * counts the loss is 0.  A label >= k is a mistake of the caller that shows: the row's loss and gradient are NaN.
+ * Logits of -inf have probability 0 (with the label on one of them the row's loss is +inf, the gradient finite); a
+ * row of nothing but -inf has loss +inf and gradient 0.  A NaN or +inf in a row that counts makes the row's loss
+ * and gradient NaN.                                                                                            */
+size_t gem_nlr_label_cross_entropy_scratch_bytes(int64_t n, int32_t k);
+int gem_nlr_label_cross_entropy(const void *logits_dev, int32_t type, int64_t ld, const int32_t *labels_dev,
+                                int64_t n, int32_t k, int32_t mean, float *loss_dev, float *row_loss_dev,
+                                void *dlogits_dev, int64_t ld_d, void *scratch_dev, size_t scratch_bytes,
+                                void *cuda_stream);
+
+/* norm = sqrt(sum over all tensors and elements of g^2);  c = min(1, max_norm / (norm + eps));  out = c g.
+ * tensors_host: `count` records (host memory, read before the call returns).  in: numel elements of `type`; out:
+ * numel elements of out_type, which is `type` or FP32.  out may be in itself (same type); then nothing is written
+ * when c == 1.  out NULL in every record: the norm alone (max_norm is not looked at).  norm: one float.  The squares
+ * are summed in FP64 over the whole range of the types (no overflow or underflow inside); the stored norm is +inf
+ * when it passes FP32.  A NaN anywhere makes norm and every output NaN; an infinite norm gives c = 0, a norm of 0 c = 1.
+ * count >= 0, max_norm >= 0, eps >= 0.                                                                         */
+typedef struct {
+    const void *in_dev;
+    void       *out_dev;
+    int64_t     numel;
+    int32_t     type;
+    int32_t     out_type;
+} gem_nlr_tensor;
+size_t gem_nlr_clip_grad_norm_scratch_bytes(int32_t count);
+int gem_nlr_clip_grad_norm(const gem_nlr_tensor *tensors_host, int32_t count, float max_norm, float eps,
+                           float *norm_dev, void *scratch_dev, size_t scratch_bytes, void *cuda_stream);
+
 #ifdef __cplusplus
 }
 #endif

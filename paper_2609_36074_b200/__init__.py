@@ -18,3 +18,10 @@ from .binding import (  # noqa: F401
     E_TIMEOUT, E_TOO_LARGE, STATIC_MAX_R,
     OK, CONVERGED, ITER_CAP, E_INVALID, E_CUDA, E_WORKSPACE, E_BREAKDOWN, E_NONFINITE, E_NOT_READY,
 )
+from .training import (  # noqa: F401
+    layer_norm,
+    layer_norm_backward,
+    label_cross_entropy,
+    clip_grad_norm,
+    grad_norm,
+)

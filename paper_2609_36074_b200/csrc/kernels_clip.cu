@@ -1,0 +1,214 @@
+// The norm of many gradient tensors, and clipping.
+//
+//   norm = sqrt(sum g^2),  c = min(1, max_norm / (norm + eps)),  out = c g
+//
+// The tensors' records travel in the kernel's parameters (up to kMaxRecords a launch), so a call needs no table on the
+// device, no copy to it and no synchronization.  Every tensor is cut into chunks of kChunk elements; a block takes a
+// contiguous range of the chunks of all tensors of its launch.
+#include "train_common.cuh"
+
+namespace gemnlr {
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kChunk = 8192;
+constexpr int kBlocks = 148 * 2;
+constexpr int kMaxRecords = 1000;      // 32 bytes a record: within the 32764 bytes of a kernel's parameters
+
+struct Record {
+    const void* in;
+    void*       out;
+    int64_t     numel;
+    uint32_t    first;                 // its first chunk's number
+    uint16_t    type, out_type;
+};
+
+template <int CAP>
+struct Table {
+    int32_t  count;
+    uint32_t chunks;
+    Record   r[CAP];
+};
+
+// Sum of squares of `m` values: FP32 where nothing can have been lost at either end of its range, else FP64.
+template <int M>
+__device__ __forceinline__ double sum_squares(const float (&v)[M])
+{
+    float s = 0.0f;
+#pragma unroll
+    for (int i = 0; i < M; ++i) s = fmaf(v[i], v[i], s);
+    if (s >= 1e-28f && s <= 1e37f) return (double)s;
+    double t = 0.0;
+#pragma unroll
+    for (int i = 0; i < M; ++i) t = fma((double)v[i], (double)v[i], t);
+    return t;
+}
+
+template <typename T>
+__device__ __forceinline__ double chunk_squares(const T* __restrict__ p, int m)
+{
+    double acc = 0.0;
+    for (int e = threadIdx.x; e < m; e += kThreads) {
+        const float v[1] = {to_f(p[e])};
+        acc += sum_squares(v);
+    }
+    return acc;
+}
+
+template <typename T, typename O>
+__device__ __forceinline__ void chunk_scale(const T* p, O* o, int m, float c)
+{
+    for (int e = threadIdx.x; e < m; e += kThreads) o[e] = from_f<O>(to_f(p[e]) * c);
+}
+
+// The record that holds chunk number q: the last one with first <= q (records without elements hold none).
+template <int CAP>
+__device__ __forceinline__ int find_record(const Table<CAP>& tb, uint32_t q)
+{
+    int lo = 0, hi = tb.count - 1;
+    while (lo < hi) {
+        const int mid = (lo + hi + 1) >> 1;
+        if (tb.r[mid].first <= q) lo = mid; else hi = mid - 1;
+    }
+    return lo;
+}
+
+template <int CAP>
+__global__ void __launch_bounds__(kThreads)
+k_clip_squares(const __grid_constant__ Table<CAP> tb, double* __restrict__ part)
+{
+    __shared__ double sred[kThreads / 32];
+    const uint32_t q0 = (uint32_t)((uint64_t)tb.chunks * blockIdx.x / gridDim.x);
+    const uint32_t q1 = (uint32_t)((uint64_t)tb.chunks * (blockIdx.x + 1) / gridDim.x);
+    double acc = 0.0;
+    int t = q0 < q1 ? find_record(tb, q0) : 0;
+    for (uint32_t q = q0; q < q1; ++q) {
+        while (t + 1 < tb.count && tb.r[t + 1].first <= q) ++t;
+        const int64_t e0 = (int64_t)(q - tb.r[t].first) * kChunk;
+        const int64_t left = tb.r[t].numel - e0;
+        const int m = (int)(left < kChunk ? left : kChunk);
+        if (tb.r[t].type == GEM_NLR_F32) acc += chunk_squares((const float*)tb.r[t].in + e0, m);
+        else if (tb.r[t].type == GEM_NLR_F16) acc += chunk_squares((const __half*)tb.r[t].in + e0, m);
+        else acc += chunk_squares((const __nv_bfloat16*)tb.r[t].in + e0, m);
+    }
+    acc = block_sum<kThreads>(acc, sred);
+    if (threadIdx.x == 0) part[blockIdx.x] = acc;
+}
+
+__device__ __forceinline__ double norm_of(const double* __restrict__ part, int parts, double* sred)
+{
+    double v = 0.0;
+    for (int i = threadIdx.x; i < parts; i += kThreads) v += part[i];
+    return sqrt(block_sum<kThreads>(v, sred));
+}
+
+__global__ void __launch_bounds__(kThreads)
+k_clip_norm(const double* __restrict__ part, int parts, float* __restrict__ norm)
+{
+    __shared__ double sred[kThreads / 32];
+    const double v = norm_of(part, parts, sred);
+    if (threadIdx.x == 0) *norm = (float)v;
+}
+
+template <int CAP>
+__global__ void __launch_bounds__(kThreads)
+k_clip_scale(const __grid_constant__ Table<CAP> tb, const double* __restrict__ part, int parts, float max_norm, float eps)
+{
+    __shared__ double sred[kThreads / 32];
+    const double norm = norm_of(part, parts, sred), ratio = (double)max_norm / (norm + (double)eps);
+    const float c = ratio >= 1.0 || norm == 0.0 ? 1.0f : (float)ratio;          // a NaN stays one
+    const uint32_t q0 = (uint32_t)((uint64_t)tb.chunks * blockIdx.x / gridDim.x);
+    const uint32_t q1 = (uint32_t)((uint64_t)tb.chunks * (blockIdx.x + 1) / gridDim.x);
+    int t = q0 < q1 ? find_record(tb, q0) : 0;
+    for (uint32_t q = q0; q < q1; ++q) {
+        while (t + 1 < tb.count && tb.r[t + 1].first <= q) ++t;
+        if (tb.r[t].in == tb.r[t].out && c == 1.0f) continue;
+        const int64_t e0 = (int64_t)(q - tb.r[t].first) * kChunk;
+        const int64_t left = tb.r[t].numel - e0;
+        const int m = (int)(left < kChunk ? left : kChunk);
+        const int type = tb.r[t].type, out = tb.r[t].out_type;
+        const void* in = tb.r[t].in;
+        if (type == GEM_NLR_F32) chunk_scale((const float*)in + e0, (float*)tb.r[t].out + e0, m, c);
+        else if (type == GEM_NLR_F16) {
+            if (out == GEM_NLR_F32) chunk_scale((const __half*)in + e0, (float*)tb.r[t].out + e0, m, c);
+            else chunk_scale((const __half*)in + e0, (__half*)tb.r[t].out + e0, m, c);
+        } else {
+            if (out == GEM_NLR_F32) chunk_scale((const __nv_bfloat16*)in + e0, (float*)tb.r[t].out + e0, m, c);
+            else chunk_scale((const __nv_bfloat16*)in + e0, (__nv_bfloat16*)tb.r[t].out + e0, m, c);
+        }
+    }
+}
+
+int clip_launches(int32_t count) { return (count + kMaxRecords - 1) / kMaxRecords; }
+
+// One launch's records; the number of chunks, or -1 if it does not fit 32 bits.
+template <int CAP>
+bool fill(Table<CAP>& tb, const gem_nlr_tensor* ts, int count)
+{
+    uint64_t chunks = 0;
+    tb.count = count;
+    for (int i = 0; i < count; ++i) {
+        tb.r[i] = Record{ts[i].in_dev, ts[i].out_dev, ts[i].numel, (uint32_t)chunks, (uint16_t)ts[i].type, (uint16_t)ts[i].out_type};
+        chunks += (uint64_t)(ts[i].numel / kChunk) + (ts[i].numel % kChunk != 0);
+        if (chunks > 0xffffffffull) return false;
+    }
+    tb.chunks = (uint32_t)chunks;
+    return true;
+}
+
+template <int CAP>
+int clip_all(const gem_nlr_tensor* ts, int32_t count, bool scale, float max_norm, float eps, float* norm, double* part, cudaStream_t st)
+{
+    static thread_local Table<CAP> tb;               // 32 KB: not on the caller's stack
+    const int launches = clip_launches(count);
+    const int parts = launches * kBlocks;
+    for (int l = 0; l < launches; ++l) {
+        const int first = l * kMaxRecords, m = count - first < kMaxRecords ? count - first : kMaxRecords;
+        if (!fill(tb, ts + first, m)) return GEM_NLR_E_INVALID;
+        k_clip_squares<CAP><<<kBlocks, kThreads, 0, st>>>(tb, part + (size_t)l * kBlocks);
+    }
+    k_clip_norm<<<1, kThreads, 0, st>>>(part, parts, norm);
+    for (int l = launches - 1; scale && l >= 0; --l) {
+        const int first = l * kMaxRecords, m = count - first < kMaxRecords ? count - first : kMaxRecords;
+        fill(tb, ts + first, m);
+        k_clip_scale<CAP><<<kBlocks, kThreads, 0, st>>>(tb, part, parts, max_norm, eps);
+    }
+    return launched();
+}
+
+}  // namespace
+}  // namespace gemnlr
+
+using namespace gemnlr;
+
+extern "C" size_t gem_nlr_clip_grad_norm_scratch_bytes(int32_t count)
+{
+    if (count < 0) return 0;
+    const int l = clip_launches(count);
+    return sizeof(double) * (size_t)kBlocks * (l < 1 ? 1 : l);
+}
+
+extern "C" int gem_nlr_clip_grad_norm(const gem_nlr_tensor* tensors_host, int32_t count, float max_norm, float eps, float* norm_dev,
+                                      void* scratch_dev, size_t scratch_bytes, void* cuda_stream)
+{
+    if (count < 0 || (count > 0 && !tensors_host) || !norm_dev || !aligned_to(norm_dev, 4)) return GEM_NLR_E_INVALID;
+    bool scale = false;                              // an empty tensor may have no address
+    for (int i = 0; i < count; ++i) scale |= tensors_host[i].out_dev != nullptr;
+    if (scale && (!(max_norm >= 0.0f) || !(eps >= 0.0f))) return GEM_NLR_E_INVALID;
+    for (int i = 0; i < count; ++i) {
+        const gem_nlr_tensor& t = tensors_host[i];
+        const int tb = type_bytes(t.type);
+        if (!tb || t.numel < 0 || (t.numel > 0 && !t.in_dev) || !aligned_to(t.in_dev, tb)) return GEM_NLR_E_INVALID;
+        if (scale) {
+            if ((t.out_type != t.type && t.out_type != GEM_NLR_F32) || (t.numel > 0 && !t.out_dev) ||
+                !aligned_to(t.out_dev, type_bytes(t.out_type)) || (t.out_dev == t.in_dev && t.out_type != t.type && t.numel > 0))
+                return GEM_NLR_E_INVALID;
+        }
+    }
+    if (!scratch_dev || !aligned_to(scratch_dev, 256) || scratch_bytes < gem_nlr_clip_grad_norm_scratch_bytes(count))
+        return GEM_NLR_E_WORKSPACE;
+    cudaStream_t st = (cudaStream_t)cuda_stream;
+    double* part = (double*)scratch_dev;
+    if (count <= 64) return clip_all<64>(tensors_host, count, scale, max_norm, eps, norm_dev, part, st);
+    return clip_all<kMaxRecords>(tensors_host, count, scale, max_norm, eps, norm_dev, part, st);
+}

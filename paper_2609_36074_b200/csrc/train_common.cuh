@@ -1,0 +1,65 @@
+// Shared by the training operators (layer norm, cross entropy, clipping): element types and argument checks.
+#pragma once
+#include <cuda_runtime.h>
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <math.h>
+#include <stddef.h>
+#include <stdint.h>
+#include "../../include/gem_nlr.h"
+#include "device_utils.cuh"
+
+namespace gemnlr {
+
+template <typename T> __device__ __forceinline__ float to_f(T v);
+template <> __device__ __forceinline__ float to_f<float>(float v) { return v; }
+template <> __device__ __forceinline__ float to_f<__half>(__half v) { return __half2float(v); }
+template <> __device__ __forceinline__ float to_f<__nv_bfloat16>(__nv_bfloat16 v) { return __bfloat162float(v); }
+
+template <typename T> __device__ __forceinline__ T from_f(float v);
+template <> __device__ __forceinline__ float from_f<float>(float v) { return v; }
+template <> __device__ __forceinline__ __half from_f<__half>(float v) { return __float2half_rn(v); }
+template <> __device__ __forceinline__ __nv_bfloat16 from_f<__nv_bfloat16>(float v) { return __float2bfloat16_rn(v); }
+
+inline int type_bytes(int32_t type) { return type == GEM_NLR_F32 ? 4 : (type == GEM_NLR_F16 || type == GEM_NLR_BF16) ? 2 : 0; }
+inline bool aligned_to(const void* p, size_t bytes) { return (reinterpret_cast<uintptr_t>(p) & (bytes - 1)) == 0; }
+
+// Sum over the block (fixed order), the same value in every thread; sred: NT / 32 floats, reusable at once.
+template <int NT>
+__device__ __forceinline__ float block_sum_f(float v, float* sred)
+{
+    v = warp_sum(v);
+    __syncthreads();
+    if ((threadIdx.x & 31) == 0) sred[threadIdx.x >> 5] = v;
+    __syncthreads();
+    float t = 0.0f;
+#pragma unroll
+    for (int w = 0; w < NT / 32; ++w) t += sred[w];
+    return t;
+}
+
+template <int NT>
+__device__ __forceinline__ float block_max_f(float v, float* sred)
+{
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, o));
+    __syncthreads();
+    if ((threadIdx.x & 31) == 0) sred[threadIdx.x >> 5] = v;
+    __syncthreads();
+    float t = sred[0];
+#pragma unroll
+    for (int w = 1; w < NT / 32; ++w) t = fmaxf(t, sred[w]);
+    return t;
+}
+
+// Calls f with a value of the element type that `type` names (one of the three; checked before).
+template <typename F> inline int by_type(int32_t type, F f)
+{
+    if (type == GEM_NLR_F32) return f(float{});
+    if (type == GEM_NLR_F16) return f(__half{});
+    return f(__nv_bfloat16{});
+}
+
+inline int launched() { return cudaGetLastError() == cudaSuccess ? GEM_NLR_OK : GEM_NLR_E_CUDA; }
+
+}  // namespace gemnlr

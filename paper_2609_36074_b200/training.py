@@ -1,0 +1,293 @@
+"""Training an encoder on the cluster labels: layer norm and its gradient, cross entropy against the labels, gradient
+clipping.  Argument marshalling only, like binding.py; the functions have the C entry points' names and return torch
+tensors.  None of them synchronizes.
+
+`stream`: the torch stream to work on; None is the current one.  With a stream of its own, a call allocates there and
+tells the allocator that the inputs are in use there; ordering it after the work that wrote the inputs (and the outputs'
+readers after it) stays with the caller, as for any torch operation."""
+from __future__ import annotations
+
+import ctypes as C
+
+from .binding import OK, lib
+
+F32, F16, BF16 = 0, 1, 2
+
+
+class Tensor(C.Structure):
+    """Mirror of gem_nlr_tensor."""
+    _fields_ = [("in_dev", C.c_void_p), ("out_dev", C.c_void_p), ("numel", C.c_int64), ("type", C.c_int32),
+                ("out_type", C.c_int32)]
+
+
+_types = None
+_fn = None
+_torch = None
+
+
+def _load():
+    """The entry points with their argument types, and torch, on the first call."""
+    global _types, _fn, _torch
+    import torch
+    L = lib()
+    vp, i32, i64, f32, size = C.c_void_p, C.c_int32, C.c_int64, C.c_float, C.c_size_t
+    sig = {
+        "layer_norm": [vp, i32, i64, vp, vp, i32, i64, i32, f32, vp, i64, vp, vp, vp],
+        "layer_norm_backward": [vp, i64, vp, i64, i32, vp, vp, vp, i32, i64, i32, vp, i64, vp, vp, vp, size, vp],
+        "layer_norm_backward_scratch_bytes": [i64, i32],
+        "label_cross_entropy": [vp, i32, i64, vp, i64, i32, i32, vp, vp, vp, i64, vp, size, vp],
+        "label_cross_entropy_scratch_bytes": [i64, i32],
+        "clip_grad_norm": [vp, i32, f32, f32, vp, vp, size, vp],
+        "clip_grad_norm_scratch_bytes": [i32],
+    }
+    fn = {}
+    for name, args in sig.items():
+        f = getattr(L, "gem_nlr_" + name)
+        f.argtypes = args
+        f.restype = size if name.endswith("_bytes") else C.c_int
+        fn[name] = f
+    _torch, _types, _fn = torch, {torch.float32: F32, torch.float16: F16, torch.bfloat16: BF16}, fn
+    return fn
+
+
+def _check(rc, name):
+    if rc != OK:
+        raise RuntimeError(f"gem_nlr_{name} failed: {rc}")
+
+
+def _type(t, name):
+    try:
+        return _types[t.dtype]
+    except KeyError:
+        raise ValueError(f"{name} is {t.dtype}: float32, float16 or bfloat16 is needed") from None
+
+
+def _rows(t, name):
+    """(rows, columns, elements from one row to the next) of a matrix, or of a batch of them that is one."""
+    if not t.is_cuda:
+        raise ValueError(f"{name} is not on a GPU")
+    if t.dim() != 2:
+        if t.dim() == 0:
+            raise ValueError(f"{name} has no columns")
+        try:
+            t = t.view(-1, t.shape[-1]) if t.numel() else t.reshape(t.shape[:-1].numel(), t.shape[-1])
+        except RuntimeError:
+            raise ValueError(f"the rows of {name} are not evenly spaced: make it contiguous") from None
+    n, d = t.shape
+    ld, one = t.stride()
+    if d < 1:
+        raise ValueError(f"{name} has no columns")
+    if one != 1 and d > 1 and n > 0:
+        raise ValueError(f"the columns of {name} are not contiguous")
+    return n, d, ld if n > 1 else max(ld, d)
+
+
+def _vector(t, d, like, name):
+    if t.shape != (d,) or not t.is_contiguous() or t.device != like.device:
+        raise ValueError(f"{name} has to be a contiguous vector of {d} on {like.device}")
+    return t.data_ptr()
+
+
+def _elsewhere(stream, device):
+    """Whether a call has to move to another stream or device first."""
+    return stream is not None or device.index != _torch.cuda.current_device()
+
+
+def _there(fn, stream, device, inputs, *args, **kw):
+    torch = _torch
+    if stream is None:
+        with torch.cuda.device(device):
+            return fn(*args, **kw)
+    if stream.device != device:
+        raise ValueError(f"the stream is on {stream.device}, the data on {device}")
+    with torch.cuda.stream(stream):
+        got = fn(*args, **kw)
+    for t in inputs:
+        if t is not None:
+            t.record_stream(stream)
+    return got
+
+
+def _out(out, like, shape, name):
+    if out is None:
+        return _torch.empty(shape, dtype=like.dtype, device=like.device)
+    if out.shape != shape or out.dtype != like.dtype or out.device != like.device:
+        raise ValueError(f"{name} has to be {tuple(shape)} {like.dtype} on {like.device}")
+    return out
+
+
+def layer_norm(x, weight=None, bias=None, eps=1e-5, out=None, stream=None):
+    """gem_nlr_layer_norm over the last dimension: (y, mean, rstd), y of x's type and shape, mean and rstd float32 of
+    x's leading dimensions.  weight, bias: float32 or x's type, None for ones and zeros."""
+    fn = _fn or _load()
+    dev = x.device
+    n, d, ld = _rows(x, "x")
+    if _elsewhere(stream, dev):
+        return _there(layer_norm, stream, dev, (x, weight, bias, out), x, weight, bias, eps, out)
+    torch = _torch
+    t = wt = _type(x, "x")
+    wp = bp = None
+    if weight is not None:
+        wt, wp = _type(weight, "weight"), _vector(weight, d, x, "weight")
+    if bias is not None:
+        bt, bp = _type(bias, "bias"), _vector(bias, d, x, "bias")
+        if weight is None:
+            wt = bt
+        elif bt != wt:
+            raise ValueError(f"weight is {weight.dtype} and bias {bias.dtype}")
+    if wt != t and wt != F32:
+        raise ValueError("weight and bias have to be float32 or of x's type")
+    if not eps >= 0 or eps == float("inf"):
+        raise ValueError(f"eps is {eps}")
+    y = _out(out, x, x.shape, "out")
+    ldy = d if out is None else _rows(out, "out")[2]
+    lead = x.shape[:-1]
+    mean = torch.empty(lead, dtype=torch.float32, device=dev)
+    rstd = torch.empty(lead, dtype=torch.float32, device=dev)
+    _check(fn["layer_norm"](x.data_ptr(), t, ld, wp, bp, wt, n, d, eps, y.data_ptr(), ldy, mean.data_ptr(), rstd.data_ptr(),
+                            torch.cuda.current_stream(dev).cuda_stream), "layer_norm")
+    return y, mean, rstd
+
+
+def layer_norm_backward(dy, x, mean, rstd, weight=None, need_dx=True, need_dweight=None, need_dbias=None, stream=None):
+    """gem_nlr_layer_norm_backward: (dx, dweight, dbias), None for each that is not needed.  dx has x's type and shape,
+    dweight and dbias the weight's type (float32 without a weight).  By default the gradients of weight and bias are
+    taken where there is a weight."""
+    fn = _fn or _load()
+    dev = x.device
+    n, d, ld = _rows(x, "x")
+    if _elsewhere(stream, dev):
+        return _there(layer_norm_backward, stream, dev, (dy, x, mean, rstd, weight), dy, x, mean, rstd, weight, need_dx,
+                      need_dweight, need_dbias)
+    torch = _torch
+    if dy.shape != x.shape or dy.dtype != x.dtype or dy.device != dev:
+        raise ValueError(f"dy has to be {tuple(x.shape)} {x.dtype} on {dev}, as x")
+    ldg = _rows(dy, "dy")[2]
+    for s, name in ((mean, "mean"), (rstd, "rstd")):
+        if s.dtype != torch.float32 or s.numel() != n or not s.is_contiguous() or s.device != dev:
+            raise ValueError(f"{name} has to be {n} contiguous float32 on {dev}")
+    t = _type(x, "x")
+    wt, wp, wdt = F32, None, torch.float32
+    if weight is not None:
+        wt, wp, wdt = _type(weight, "weight"), _vector(weight, d, x, "weight"), weight.dtype
+        if wt != t and wt != F32:
+            raise ValueError("weight has to be float32 or of x's type")
+    if need_dweight is None:
+        need_dweight = weight is not None
+    if need_dbias is None:
+        need_dbias = weight is not None
+    if not (need_dx or need_dweight or need_dbias):
+        return None, None, None
+    dx = torch.empty(x.shape, dtype=x.dtype, device=dev) if need_dx else None
+    dw = torch.empty(d, dtype=wdt, device=dev) if need_dweight else None
+    db = torch.empty(d, dtype=wdt, device=dev) if need_dbias else None
+    size = fn["layer_norm_backward_scratch_bytes"](n, d)
+    scratch = torch.empty(size, dtype=torch.uint8, device=dev)
+    _check(fn["layer_norm_backward"](
+        dy.data_ptr(), ldg, x.data_ptr(), ld, t, mean.data_ptr(), rstd.data_ptr(), wp, wt, n, d,
+        None if dx is None else dx.data_ptr(), d, None if dw is None else dw.data_ptr(), None if db is None else db.data_ptr(),
+        scratch.data_ptr(), size, torch.cuda.current_stream(dev).cuda_stream), "layer_norm_backward")
+    return dx, dw, db
+
+
+def label_cross_entropy(logits, labels, mean=True, dlogits=None, need_grad=True, stream=None):
+    """gem_nlr_label_cross_entropy: (loss, row_loss, dlogits).  logits: (n, k); labels: n int32 as GemNlr.labels gives
+    them, negative ones left out.  loss: a float32 scalar, the mean over the rows that count (mean=False: the sum);
+    row_loss: n float32; dlogits: the loss's gradient in logits' type, written to the tensor given (the logits themselves
+    are fine) or a new one; need_grad=False: None."""
+    fn = _fn or _load()
+    dev = logits.device
+    n, k, ld = _rows(logits, "logits")
+    if _elsewhere(stream, dev):
+        return _there(label_cross_entropy, stream, dev, (logits, labels, dlogits), logits, labels, mean, dlogits, need_grad)
+    torch = _torch
+    t = _type(logits, "logits")
+    if labels.dtype != torch.int32 or labels.shape != logits.shape[:-1] or not labels.is_contiguous() or labels.device != dev:
+        raise ValueError(f"labels have to be {n} contiguous int32 on {dev}")
+    ldd = k
+    dp = None
+    if need_grad:
+        given = dlogits is not None
+        dlogits = _out(dlogits, logits, logits.shape, "dlogits")
+        dp = dlogits.data_ptr()
+        if given:
+            ldd = _rows(dlogits, "dlogits")[2]
+    else:
+        dlogits = None
+    loss = torch.empty((), dtype=torch.float32, device=dev)
+    row = torch.empty(logits.shape[:-1], dtype=torch.float32, device=dev)
+    size = fn["label_cross_entropy_scratch_bytes"](n, k)
+    scratch = torch.empty(size, dtype=torch.uint8, device=dev)
+    _check(fn["label_cross_entropy"](logits.data_ptr(), t, ld, labels.data_ptr(), n, k, int(bool(mean)), loss.data_ptr(),
+                                     row.data_ptr(), dp, ldd, scratch.data_ptr(), size,
+                                     torch.cuda.current_stream(dev).cuda_stream), "label_cross_entropy")
+    return loss, row, dlogits
+
+
+def _norm_and_clip(grads, max_norm, out, eps, stream):
+    fn = _fn or _load()
+    torch = _torch
+    grads = list(grads)
+    if not grads:
+        raise ValueError("no tensors")
+    dev = grads[0].device
+    if dev.type != "cuda":
+        raise ValueError("the first tensor is not on a GPU")
+    if _elsewhere(stream, dev):
+        out = out if out is None or out is grads else list(out)
+        return _there(_norm_and_clip, stream, dev, grads + (list(out) if out else []), grads, max_norm, out, eps, None)
+    count, at = len(grads), dev.index
+    table = (Tensor * count)()
+    types = _types
+    if out is not None:
+        out = list(out)
+        if len(out) != count:
+            raise ValueError(f"{count} tensors and {len(out)} outputs")
+        if not max_norm >= 0:
+            raise ValueError(f"max_norm is {max_norm}")
+        if not eps >= 0:
+            raise ValueError(f"eps is {eps}")
+    for i, g in enumerate(grads):
+        t = types.get(g.dtype)
+        if t is None or g.get_device() != at or not _dense(g):
+            raise ValueError(f"tensor {i} has to be float32, float16 or bfloat16, without gaps, on {dev}")
+        if out is None:
+            table[i] = (g.data_ptr(), None, g.numel(), t, t)
+        else:
+            o = out[i]
+            ot = types.get(o.dtype)
+            if (ot != t and ot != F32) or o.shape != g.shape or o.get_device() != at or \
+                    not (o is g or (o.is_contiguous() and g.is_contiguous()) or o.stride() == g.stride() and _dense(o)):
+                raise ValueError(f"output {i} has to be like its tensor, or float32 of its shape and order")
+            table[i] = (g.data_ptr(), o.data_ptr(), g.numel(), t, ot)
+    norm = torch.empty((), dtype=torch.float32, device=dev)
+    size = fn["clip_grad_norm_scratch_bytes"](count)
+    scratch = torch.empty(size, dtype=torch.uint8, device=dev)
+    _check(fn["clip_grad_norm"](table, count, max_norm, eps, norm.data_ptr(), scratch.data_ptr(), size,
+                                torch.cuda.current_stream(dev).cuda_stream), "clip_grad_norm")
+    return norm
+
+
+def _dense(t):
+    """Whether the tensor's elements fill its memory, in any order of its dimensions."""
+    if t.is_contiguous():
+        return True
+    need = 1
+    for stride, size in sorted(zip(t.stride(), t.shape)):
+        if size != 1:
+            if stride != need:
+                return False
+            need *= size
+    return True
+
+
+def clip_grad_norm(grads, max_norm, out=None, eps=1e-6, stream=None):
+    """gem_nlr_clip_grad_norm: scales all tensors by min(1, max_norm / (norm + eps)), in place or into `out` (tensors of
+    the same shapes, of the same types or float32), and returns the norm before it, a float32 scalar on the GPU."""
+    grads = list(grads)
+    return _norm_and_clip(grads, max_norm, grads if out is None else out, eps, stream)
+
+
+def grad_norm(grads, stream=None):
+    """The same norm alone; nothing else is written."""
+    return _norm_and_clip(grads, 0.0, None, 0.0, stream)
