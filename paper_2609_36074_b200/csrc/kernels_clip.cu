@@ -3,16 +3,18 @@
 //   norm = sqrt(sum g^2),  c = min(1, max_norm / (norm + eps)),  out = c g
 //
 // The tensors' records travel in the kernel's parameters (up to kMaxRecords a launch), so a call needs no table on the
-// device, no copy to it and no synchronization.  Every tensor is cut into chunks of kChunk elements; a block takes a
-// contiguous range of the chunks of all tensors of its launch.
-#include "train_common.cuh"
+// device, no copy to it and no synchronization.  Every tensor is cut into chunks; a block takes a contiguous range of the
+// chunks of all tensors of its launch, and goes through it backwards when it scales: what the first pass read last is
+// still in L2 then.
+#include "train_rows.cuh"
 
 namespace gemnlr {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kChunk = 8192;
-constexpr int kBlocks = 148 * 2;
+constexpr int kBlocks = kTrainSMs * 4;
+constexpr int kChunk = 8192;           // elements; kSmallChunk where those would leave blocks without one
+constexpr int kSmallChunk = 2048;
 constexpr int kMaxRecords = 1000;      // 32 bytes a record: within the 32764 bytes of a kernel's parameters
 
 struct Record {
@@ -25,7 +27,7 @@ struct Record {
 
 template <int CAP>
 struct Table {
-    int32_t  count;
+    int32_t  count, chunk;             // records, elements of a chunk
     uint32_t chunks;
     Record   r[CAP];
 };
@@ -44,21 +46,65 @@ __device__ __forceinline__ double sum_squares(const float (&v)[M])
     return t;
 }
 
+constexpr int kAhead = 4;              // vectors that a thread loads before it uses the first
+
+// Sum of squares of the thread's share of m elements; vectors where the chunk begins at a multiple of 16 bytes.
 template <typename T>
-__device__ __forceinline__ double chunk_squares(const T* __restrict__ p, int m)
+__device__ __forceinline__ double chunk_squares(const T* p, int m)
 {
+    constexpr int N = 16 / (int)sizeof(T);
     double acc = 0.0;
-    for (int e = threadIdx.x; e < m; e += kThreads) {
-        const float v[1] = {to_f(p[e])};
-        acc += sum_squares(v);
+    int e = 0;
+    if ((reinterpret_cast<uintptr_t>(p) & 15) == 0) {
+        const int whole = m / N;
+        for (int v0 = threadIdx.x; v0 < whole; v0 += kThreads * kAhead) {
+            Vec<T, 16> x[kAhead];
+#pragma unroll
+            for (int u = 0; u < kAhead; ++u)
+                if (v0 + u * kThreads < whole) x[u].load(p + (size_t)(v0 + u * kThreads) * N); else x[u].zero();
+#pragma unroll
+            for (int u = 0; u < kAhead; ++u) {
+                float f[N];
+#pragma unroll
+                for (int i = 0; i < N; ++i) f[i] = x[u].get(i);
+                acc += sum_squares(f);
+            }
+        }
+        e = whole * N;
+    }
+    for (e += threadIdx.x; e < m; e += kThreads) {
+        const float f[1] = {to_f(p[e])};
+        acc += sum_squares(f);
     }
     return acc;
 }
 
+// o = c p; four elements at a time where both begin at a multiple of four of theirs, 16-byte stores of FP32
 template <typename T, typename O>
 __device__ __forceinline__ void chunk_scale(const T* p, O* o, int m, float c)
 {
-    for (int e = threadIdx.x; e < m; e += kThreads) o[e] = from_f<O>(to_f(p[e]) * c);
+    constexpr int N = sizeof(O) == 4 ? 4 : 8;
+    constexpr int AHEAD = 2 * kAhead * 4 / N;
+    int e = 0;
+    if ((reinterpret_cast<uintptr_t>(p) & (N * sizeof(T) - 1)) == 0 && (reinterpret_cast<uintptr_t>(o) & 15) == 0) {
+        const int whole = m / N;
+        for (int v0 = threadIdx.x; v0 < whole; v0 += kThreads * AHEAD) {
+            Vec<T, N * (int)sizeof(T)> x[AHEAD];
+#pragma unroll
+            for (int u = 0; u < AHEAD; ++u)
+                if (v0 + u * kThreads < whole) x[u].load(p + (size_t)(v0 + u * kThreads) * N);
+#pragma unroll
+            for (int u = 0; u < AHEAD; ++u)
+                if (v0 + u * kThreads < whole) {
+                    Vec<O, 16> y;
+#pragma unroll
+                    for (int i = 0; i < N; ++i) y.set(i, x[u].get(i) * c);
+                    y.store_streaming(o + (size_t)(v0 + u * kThreads) * N);
+                }
+        }
+        e = whole * N;
+    }
+    for (e += threadIdx.x; e < m; e += kThreads) o[e] = from_f<O>(to_f(p[e]) * c);
 }
 
 // The record that holds chunk number q: the last one with first <= q (records without elements hold none).
@@ -84,15 +130,16 @@ k_clip_squares(const __grid_constant__ Table<CAP> tb, double* __restrict__ part)
     int t = q0 < q1 ? find_record(tb, q0) : 0;
     for (uint32_t q = q0; q < q1; ++q) {
         while (t + 1 < tb.count && tb.r[t + 1].first <= q) ++t;
-        const int64_t e0 = (int64_t)(q - tb.r[t].first) * kChunk;
+        const int64_t e0 = (int64_t)(q - tb.r[t].first) * tb.chunk;
         const int64_t left = tb.r[t].numel - e0;
-        const int m = (int)(left < kChunk ? left : kChunk);
+        const int m = (int)(left < tb.chunk ? left : tb.chunk);
         if (tb.r[t].type == GEM_NLR_F32) acc += chunk_squares((const float*)tb.r[t].in + e0, m);
         else if (tb.r[t].type == GEM_NLR_F16) acc += chunk_squares((const __half*)tb.r[t].in + e0, m);
         else acc += chunk_squares((const __nv_bfloat16*)tb.r[t].in + e0, m);
     }
     acc = block_sum<kThreads>(acc, sred);
     if (threadIdx.x == 0) part[blockIdx.x] = acc;
+    next_may_start();
 }
 
 __device__ __forceinline__ double norm_of(const double* __restrict__ part, int parts, double* sred)
@@ -106,26 +153,30 @@ __global__ void __launch_bounds__(kThreads)
 k_clip_norm(const double* __restrict__ part, int parts, float* __restrict__ norm)
 {
     __shared__ double sred[kThreads / 32];
+    grid_ready();
     const double v = norm_of(part, parts, sred);
     if (threadIdx.x == 0) *norm = (float)v;
 }
 
 template <int CAP>
 __global__ void __launch_bounds__(kThreads)
-k_clip_scale(const __grid_constant__ Table<CAP> tb, const double* __restrict__ part, int parts, float max_norm, float eps)
+k_clip_scale(const __grid_constant__ Table<CAP> tb, const double* __restrict__ part, int parts, float max_norm, float eps,
+             float* __restrict__ norm_out)
 {
     __shared__ double sred[kThreads / 32];
+    grid_ready();
     const double norm = norm_of(part, parts, sred), ratio = (double)max_norm / (norm + (double)eps);
     const float c = ratio >= 1.0 || norm == 0.0 ? 1.0f : (float)ratio;          // a NaN stays one
+    if (norm_out && blockIdx.x == 0 && threadIdx.x == 0) *norm_out = (float)norm;
     const uint32_t q0 = (uint32_t)((uint64_t)tb.chunks * blockIdx.x / gridDim.x);
     const uint32_t q1 = (uint32_t)((uint64_t)tb.chunks * (blockIdx.x + 1) / gridDim.x);
-    int t = q0 < q1 ? find_record(tb, q0) : 0;
-    for (uint32_t q = q0; q < q1; ++q) {
-        while (t + 1 < tb.count && tb.r[t + 1].first <= q) ++t;
+    int t = q0 < q1 ? find_record(tb, q1 - 1) : 0;
+    for (uint32_t q = q1; q-- > q0;) {
+        while (tb.r[t].first > q) --t;
         if (tb.r[t].in == tb.r[t].out && c == 1.0f) continue;
-        const int64_t e0 = (int64_t)(q - tb.r[t].first) * kChunk;
+        const int64_t e0 = (int64_t)(q - tb.r[t].first) * tb.chunk;
         const int64_t left = tb.r[t].numel - e0;
-        const int m = (int)(left < kChunk ? left : kChunk);
+        const int m = (int)(left < tb.chunk ? left : tb.chunk);
         const int type = tb.r[t].type, out = tb.r[t].out_type;
         const void* in = tb.r[t].in;
         if (type == GEM_NLR_F32) chunk_scale((const float*)in + e0, (float*)tb.r[t].out + e0, m, c);
@@ -141,15 +192,18 @@ k_clip_scale(const __grid_constant__ Table<CAP> tb, const double* __restrict__ p
 
 int clip_launches(int32_t count) { return (count + kMaxRecords - 1) / kMaxRecords; }
 
-// One launch's records; the number of chunks, or -1 if it does not fit 32 bits.
+// One launch's records; false if their chunks' number passes 32 bits.
 template <int CAP>
 bool fill(Table<CAP>& tb, const gem_nlr_tensor* ts, int count)
 {
+    int64_t all = 0;
+    for (int i = 0; i < count; ++i) all += ts[i].numel / kChunk;
+    tb.chunk = all >= kBlocks ? kChunk : kSmallChunk;
     uint64_t chunks = 0;
     tb.count = count;
     for (int i = 0; i < count; ++i) {
         tb.r[i] = Record{ts[i].in_dev, ts[i].out_dev, ts[i].numel, (uint32_t)chunks, (uint16_t)ts[i].type, (uint16_t)ts[i].out_type};
-        chunks += (uint64_t)(ts[i].numel / kChunk) + (ts[i].numel % kChunk != 0);
+        chunks += (uint64_t)(ts[i].numel / tb.chunk) + (ts[i].numel % tb.chunk != 0);
         if (chunks > 0xffffffffull) return false;
     }
     tb.chunks = (uint32_t)chunks;
@@ -160,18 +214,29 @@ template <int CAP>
 int clip_all(const gem_nlr_tensor* ts, int32_t count, bool scale, float max_norm, float eps, float* norm, double* part, cudaStream_t st)
 {
     static thread_local Table<CAP> tb;               // 32 KB: not on the caller's stack
-    const int launches = clip_launches(count);
-    const int parts = launches * kBlocks;
+    const int launches = clip_launches(count) < 1 ? 1 : clip_launches(count);
+    int parts = 0;
     for (int l = 0; l < launches; ++l) {
         const int first = l * kMaxRecords, m = count - first < kMaxRecords ? count - first : kMaxRecords;
         if (!fill(tb, ts + first, m)) return GEM_NLR_E_INVALID;
-        k_clip_squares<CAP><<<kBlocks, kThreads, 0, st>>>(tb, part + (size_t)l * kBlocks);
+        const int blocks = tb.chunks < 1 ? 1 : tb.chunks < (uint32_t)kBlocks ? (int)tb.chunks : kBlocks;
+        k_clip_squares<CAP><<<blocks, kThreads, 0, st>>>(tb, part + parts);
+        parts += blocks;
     }
-    k_clip_norm<<<1, kThreads, 0, st>>>(part, parts, norm);
-    for (int l = launches - 1; scale && l >= 0; --l) {
+    if (launched() != GEM_NLR_OK) return GEM_NLR_E_CUDA;
+    if (!scale)
+        return launch_early(k_clip_norm, dim3(1), kThreads, st, (const double*)part, parts, norm) == cudaSuccess ? GEM_NLR_OK : GEM_NLR_E_CUDA;
+    for (int l = launches - 1; l >= 0; --l) {
         const int first = l * kMaxRecords, m = count - first < kMaxRecords ? count - first : kMaxRecords;
-        fill(tb, ts + first, m);
-        k_clip_scale<CAP><<<kBlocks, kThreads, 0, st>>>(tb, part, parts, max_norm, eps);
+        if (launches > 1) fill(tb, ts + first, m);
+        const int blocks = tb.chunks < 1 ? 1 : tb.chunks < (uint32_t)kBlocks ? (int)tb.chunks : kBlocks;
+        // only the first one may begin early: it waits for the squares, the others for it
+        if (l == launches - 1) {
+            if (launch_early(k_clip_scale<CAP>, dim3((unsigned)blocks), kThreads, st, tb, (const double*)part, parts, max_norm, eps, norm) != cudaSuccess)
+                return GEM_NLR_E_CUDA;
+        } else {
+            k_clip_scale<CAP><<<blocks, kThreads, 0, st>>>(tb, part, parts, max_norm, eps, nullptr);
+        }
     }
     return launched();
 }

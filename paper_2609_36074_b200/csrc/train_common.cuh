@@ -60,6 +60,13 @@ template <typename F> inline int by_type(int32_t type, F f)
     return f(__nv_bfloat16{});
 }
 
+constexpr int kTrainSMs = 148;
+
+// Programmatic launches: the kernel before says that the next one may begin; that one waits for the kernel before to be
+// complete (every block of it has to, or the kernel after it might begin before the first one is done).
+__device__ __forceinline__ void next_may_start() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+__device__ __forceinline__ void grid_ready() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+
 inline int launched() { return cudaGetLastError() == cudaSuccess ? GEM_NLR_OK : GEM_NLR_E_CUDA; }
 
 }  // namespace gemnlr
