@@ -8,6 +8,7 @@ readers after it) stays with the caller, as for any torch operation."""
 from __future__ import annotations
 
 import ctypes as C
+from array import array
 
 from .binding import OK, lib
 
@@ -20,14 +21,16 @@ class Tensor(C.Structure):
                 ("out_type", C.c_int32)]
 
 
-_types = None
-_fn = None
+_fn = None          # the entry points, by name
+_types = None       # torch dtype -> GEM_NLR_F32, ...
 _torch = None
+_device = None      # the current device's number, and the current stream of a device as a pointer: torch's own
+_stream = None      # accessors without the objects that torch.cuda.current_stream() builds (2 us of a 15 us call)
 
 
 def _load():
     """The entry points with their argument types, and torch, on the first call."""
-    global _types, _fn, _torch
+    global _fn, _types, _torch, _device, _stream
     import torch
     L = lib()
     vp, i32, i64, f32, size = C.c_void_p, C.c_int32, C.c_int64, C.c_float, C.c_size_t
@@ -46,6 +49,7 @@ def _load():
         f.argtypes = args
         f.restype = size if name.endswith("_bytes") else C.c_int
         fn[name] = f
+    _device, _stream = torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream
     _torch, _types, _fn = torch, {torch.float32: F32, torch.float16: F16, torch.bfloat16: BF16}, fn
     return fn
 
@@ -56,96 +60,96 @@ def _check(rc, name):
 
 
 def _type(t, name):
-    try:
-        return _types[t.dtype]
-    except KeyError:
-        raise ValueError(f"{name} is {t.dtype}: float32, float16 or bfloat16 is needed") from None
+    k = _types.get(t.dtype)
+    if k is None:
+        raise ValueError(f"{name} is {t.dtype}: float32, float16 or bfloat16 is needed")
+    return k
 
 
 def _rows(t, name):
     """(rows, columns, elements from one row to the next) of a matrix, or of a batch of them that is one."""
     if not t.is_cuda:
         raise ValueError(f"{name} is not on a GPU")
-    if t.dim() != 2:
-        if t.dim() == 0:
+    shape = t.shape
+    if len(shape) != 2:
+        if not shape:
             raise ValueError(f"{name} has no columns")
         try:
-            t = t.view(-1, t.shape[-1]) if t.numel() else t.reshape(t.shape[:-1].numel(), t.shape[-1])
+            t = t.view(-1, shape[-1]) if t.numel() else t.reshape(shape[:-1].numel(), shape[-1])
         except RuntimeError:
             raise ValueError(f"the rows of {name} are not evenly spaced: make it contiguous") from None
-    n, d = t.shape
+        shape = t.shape
+    n, d = shape
     ld, one = t.stride()
     if d < 1:
         raise ValueError(f"{name} has no columns")
     if one != 1 and d > 1 and n > 0:
         raise ValueError(f"the columns of {name} are not contiguous")
-    return n, d, ld if n > 1 else max(ld, d)
+    return n, d, ld if n > 1 or ld > d else d
 
 
-def _vector(t, d, like, name):
-    if t.shape != (d,) or not t.is_contiguous() or t.device != like.device:
-        raise ValueError(f"{name} has to be a contiguous vector of {d} on {like.device}")
+def _vector(t, d, at, name):
+    if t.shape != (d,) or not t.is_contiguous() or t.get_device() != at:
+        raise ValueError(f"{name} has to be a contiguous vector of {d} on GPU {at}")
     return t.data_ptr()
 
 
-def _elsewhere(stream, device):
-    """Whether a call has to move to another stream or device first."""
-    return stream is not None or device.index != _torch.cuda.current_device()
-
-
-def _there(fn, stream, device, inputs, *args, **kw):
+def _there(fn, stream, inputs, *args):
+    """The call on another stream than the current one, or on a device that is not current."""
     torch = _torch
+    device = inputs[0].device
     if stream is None:
         with torch.cuda.device(device):
-            return fn(*args, **kw)
+            return fn(*args)
     if stream.device != device:
         raise ValueError(f"the stream is on {stream.device}, the data on {device}")
     with torch.cuda.stream(stream):
-        got = fn(*args, **kw)
+        got = fn(*args)
     for t in inputs:
-        if t is not None:
+        if t is not None and t.is_cuda:
             t.record_stream(stream)
     return got
 
 
-def _out(out, like, shape, name):
-    if out is None:
-        return _torch.empty(shape, dtype=like.dtype, device=like.device)
-    if out.shape != shape or out.dtype != like.dtype or out.device != like.device:
-        raise ValueError(f"{name} has to be {tuple(shape)} {like.dtype} on {like.device}")
-    return out
+def _given(out, like, name):
+    """The row distance of an output that the caller gave."""
+    if out.shape != like.shape or out.dtype != like.dtype or out.device != like.device:
+        raise ValueError(f"{name} has to be {tuple(like.shape)} {like.dtype} on {like.device}")
+    return _rows(out, name)[2]
 
 
 def layer_norm(x, weight=None, bias=None, eps=1e-5, out=None, stream=None):
     """gem_nlr_layer_norm over the last dimension: (y, mean, rstd), y of x's type and shape, mean and rstd float32 of
     x's leading dimensions.  weight, bias: float32 or x's type, None for ones and zeros."""
     fn = _fn or _load()
-    dev = x.device
     n, d, ld = _rows(x, "x")
-    if _elsewhere(stream, dev):
-        return _there(layer_norm, stream, dev, (x, weight, bias, out), x, weight, bias, eps, out)
+    at = x.get_device()
+    if stream is not None or at != _device():
+        return _there(layer_norm, stream, (x, weight, bias, out), x, weight, bias, eps, out)
     torch = _torch
     t = wt = _type(x, "x")
     wp = bp = None
     if weight is not None:
-        wt, wp = _type(weight, "weight"), _vector(weight, d, x, "weight")
+        wt, wp = _type(weight, "weight"), _vector(weight, d, at, "weight")
     if bias is not None:
-        bt, bp = _type(bias, "bias"), _vector(bias, d, x, "bias")
+        bt, bp = _type(bias, "bias"), _vector(bias, d, at, "bias")
         if weight is None:
             wt = bt
         elif bt != wt:
             raise ValueError(f"weight is {weight.dtype} and bias {bias.dtype}")
     if wt != t and wt != F32:
         raise ValueError("weight and bias have to be float32 or of x's type")
-    if not eps >= 0 or eps == float("inf"):
+    if not 0 <= eps < float("inf"):
         raise ValueError(f"eps is {eps}")
-    y = _out(out, x, x.shape, "out")
-    ldy = d if out is None else _rows(out, "out")[2]
-    lead = x.shape[:-1]
-    mean = torch.empty(lead, dtype=torch.float32, device=dev)
-    rstd = torch.empty(lead, dtype=torch.float32, device=dev)
+    shape = x.shape
+    if out is None:
+        y, ldy = torch.empty_like(x) if x.is_contiguous() else x.new_empty(shape), d
+    else:
+        y, ldy = out, _given(out, x, "out")
+    mean = x.new_empty(shape[:-1], dtype=torch.float32)
+    rstd = torch.empty_like(mean)
     _check(fn["layer_norm"](x.data_ptr(), t, ld, wp, bp, wt, n, d, eps, y.data_ptr(), ldy, mean.data_ptr(), rstd.data_ptr(),
-                            torch.cuda.current_stream(dev).cuda_stream), "layer_norm")
+                            _stream(at)), "layer_norm")
     return y, mean, rstd
 
 
@@ -154,22 +158,22 @@ def layer_norm_backward(dy, x, mean, rstd, weight=None, need_dx=True, need_dweig
     dweight and dbias the weight's type (float32 without a weight).  By default the gradients of weight and bias are
     taken where there is a weight."""
     fn = _fn or _load()
-    dev = x.device
     n, d, ld = _rows(x, "x")
-    if _elsewhere(stream, dev):
-        return _there(layer_norm_backward, stream, dev, (dy, x, mean, rstd, weight), dy, x, mean, rstd, weight, need_dx,
-                      need_dweight, need_dbias)
+    at = x.get_device()
+    if stream is not None or at != _device():
+        return _there(layer_norm_backward, stream, (x, dy, mean, rstd, weight), dy, x, mean, rstd, weight, need_dx, need_dweight,
+                      need_dbias)
     torch = _torch
-    if dy.shape != x.shape or dy.dtype != x.dtype or dy.device != dev:
-        raise ValueError(f"dy has to be {tuple(x.shape)} {x.dtype} on {dev}, as x")
+    if dy.shape != x.shape or dy.dtype != x.dtype or dy.get_device() != at:
+        raise ValueError(f"dy has to be {tuple(x.shape)} {x.dtype} on GPU {at}, as x")
     ldg = _rows(dy, "dy")[2]
     for s, name in ((mean, "mean"), (rstd, "rstd")):
-        if s.dtype != torch.float32 or s.numel() != n or not s.is_contiguous() or s.device != dev:
-            raise ValueError(f"{name} has to be {n} contiguous float32 on {dev}")
+        if s.dtype != torch.float32 or s.numel() != n or not s.is_contiguous() or s.get_device() != at:
+            raise ValueError(f"{name} has to be {n} contiguous float32 on GPU {at}")
     t = _type(x, "x")
     wt, wp, wdt = F32, None, torch.float32
     if weight is not None:
-        wt, wp, wdt = _type(weight, "weight"), _vector(weight, d, x, "weight"), weight.dtype
+        wt, wp, wdt = _type(weight, "weight"), _vector(weight, d, at, "weight"), weight.dtype
         if wt != t and wt != F32:
             raise ValueError("weight has to be float32 or of x's type")
     if need_dweight is None:
@@ -178,15 +182,19 @@ def layer_norm_backward(dy, x, mean, rstd, weight=None, need_dx=True, need_dweig
         need_dbias = weight is not None
     if not (need_dx or need_dweight or need_dbias):
         return None, None, None
-    dx = torch.empty(x.shape, dtype=x.dtype, device=dev) if need_dx else None
-    dw = torch.empty(d, dtype=wdt, device=dev) if need_dweight else None
-    db = torch.empty(d, dtype=wdt, device=dev) if need_dbias else None
+    dx = dw = db = None
+    if need_dx:
+        dx = torch.empty_like(x) if x.is_contiguous() else x.new_empty(x.shape)
+    if need_dweight:
+        dw = mean.new_empty(d, dtype=wdt)
+    if need_dbias:
+        db = mean.new_empty(d, dtype=wdt) if dw is None else torch.empty_like(dw)
     size = fn["layer_norm_backward_scratch_bytes"](n, d)
-    scratch = torch.empty(size, dtype=torch.uint8, device=dev)
+    scratch = mean.new_empty(size, dtype=torch.uint8)
     _check(fn["layer_norm_backward"](
         dy.data_ptr(), ldg, x.data_ptr(), ld, t, mean.data_ptr(), rstd.data_ptr(), wp, wt, n, d,
         None if dx is None else dx.data_ptr(), d, None if dw is None else dw.data_ptr(), None if db is None else db.data_ptr(),
-        scratch.data_ptr(), size, torch.cuda.current_stream(dev).cuda_stream), "layer_norm_backward")
+        scratch.data_ptr(), size, _stream(at)), "layer_norm_backward")
     return dx, dw, db
 
 
@@ -196,82 +204,79 @@ def label_cross_entropy(logits, labels, mean=True, dlogits=None, need_grad=True,
     row_loss: n float32; dlogits: the loss's gradient in logits' type, written to the tensor given (the logits themselves
     are fine) or a new one; need_grad=False: None."""
     fn = _fn or _load()
-    dev = logits.device
     n, k, ld = _rows(logits, "logits")
-    if _elsewhere(stream, dev):
-        return _there(label_cross_entropy, stream, dev, (logits, labels, dlogits), logits, labels, mean, dlogits, need_grad)
+    at = logits.get_device()
+    if stream is not None or at != _device():
+        return _there(label_cross_entropy, stream, (logits, labels, dlogits), logits, labels, mean, dlogits, need_grad)
     torch = _torch
     t = _type(logits, "logits")
-    if labels.dtype != torch.int32 or labels.shape != logits.shape[:-1] or not labels.is_contiguous() or labels.device != dev:
-        raise ValueError(f"labels have to be {n} contiguous int32 on {dev}")
-    ldd = k
-    dp = None
-    if need_grad:
-        given = dlogits is not None
-        dlogits = _out(dlogits, logits, logits.shape, "dlogits")
-        dp = dlogits.data_ptr()
-        if given:
-            ldd = _rows(dlogits, "dlogits")[2]
-    else:
+    lead = logits.shape[:-1]
+    if labels.dtype != torch.int32 or labels.shape != lead or not labels.is_contiguous() or labels.get_device() != at:
+        raise ValueError(f"labels have to be {tuple(lead)} contiguous int32 on GPU {at}")
+    ldd, dp = k, None
+    if not need_grad:
         dlogits = None
-    loss = torch.empty((), dtype=torch.float32, device=dev)
-    row = torch.empty(logits.shape[:-1], dtype=torch.float32, device=dev)
+    else:
+        if dlogits is None:
+            dlogits = torch.empty_like(logits) if logits.is_contiguous() else logits.new_empty(logits.shape)
+        else:
+            ldd = _given(dlogits, logits, "dlogits")
+        dp = dlogits.data_ptr()
+    row = logits.new_empty(lead, dtype=torch.float32)
+    loss = row.new_empty(())
     size = fn["label_cross_entropy_scratch_bytes"](n, k)
-    scratch = torch.empty(size, dtype=torch.uint8, device=dev)
-    _check(fn["label_cross_entropy"](logits.data_ptr(), t, ld, labels.data_ptr(), n, k, int(bool(mean)), loss.data_ptr(),
-                                     row.data_ptr(), dp, ldd, scratch.data_ptr(), size,
-                                     torch.cuda.current_stream(dev).cuda_stream), "label_cross_entropy")
+    scratch = labels.new_empty(size, dtype=torch.uint8)
+    _check(fn["label_cross_entropy"](logits.data_ptr(), t, ld, labels.data_ptr(), n, k, 1 if mean else 0, loss.data_ptr(), row.data_ptr(),
+                                     dp, ldd, scratch.data_ptr(), size, _stream(at)), "label_cross_entropy")
     return loss, row, dlogits
 
 
 def _norm_and_clip(grads, max_norm, out, eps, stream):
     fn = _fn or _load()
     torch = _torch
-    grads = list(grads)
     if not grads:
         raise ValueError("no tensors")
-    dev = grads[0].device
-    if dev.type != "cuda":
+    if not grads[0].is_cuda:
         raise ValueError("the first tensor is not on a GPU")
-    if _elsewhere(stream, dev):
-        out = out if out is None or out is grads else list(out)
-        return _there(_norm_and_clip, stream, dev, grads + (list(out) if out else []), grads, max_norm, out, eps, None)
-    count, at = len(grads), dev.index
-    table = (Tensor * count)()
-    types = _types
+    at = grads[0].get_device()
+    if stream is not None or at != _device():
+        return _there(_norm_and_clip, stream, grads if out is None or out is grads else grads + out, grads, max_norm, out, eps, None)
+    count, types = len(grads), _types
     if out is not None:
-        out = list(out)
         if len(out) != count:
             raise ValueError(f"{count} tensors and {len(out)} outputs")
         if not max_norm >= 0:
             raise ValueError(f"max_norm is {max_norm}")
         if not eps >= 0:
             raise ValueError(f"eps is {eps}")
+    flat = []                                        # gem_nlr_tensor as four 64-bit words
     for i, g in enumerate(grads):
         t = types.get(g.dtype)
-        if t is None or g.get_device() != at or not _dense(g):
-            raise ValueError(f"tensor {i} has to be float32, float16 or bfloat16, without gaps, on {dev}")
+        if t is None or g.get_device() != at or not (g.is_contiguous() or _dense(g)):
+            raise ValueError(f"tensor {i} has to be float32, float16 or bfloat16, without gaps, on GPU {at}")
+        p = g.data_ptr()
         if out is None:
-            table[i] = (g.data_ptr(), None, g.numel(), t, t)
-        else:
-            o = out[i]
-            ot = types.get(o.dtype)
-            if (ot != t and ot != F32) or o.shape != g.shape or o.get_device() != at or \
-                    not (o is g or (o.is_contiguous() and g.is_contiguous()) or o.stride() == g.stride() and _dense(o)):
-                raise ValueError(f"output {i} has to be like its tensor, or float32 of its shape and order")
-            table[i] = (g.data_ptr(), o.data_ptr(), g.numel(), t, ot)
-    norm = torch.empty((), dtype=torch.float32, device=dev)
+            flat += (p, 0, g.numel(), t | t << 32)
+            continue
+        o = out[i]
+        if o is g:
+            flat += (p, p, g.numel(), t | t << 32)
+            continue
+        ot = types.get(o.dtype)
+        if (ot != t and ot != F32) or o.shape != g.shape or o.get_device() != at or \
+                not (o.is_contiguous() and g.is_contiguous() or o.stride() == g.stride() and _dense(o)):
+            raise ValueError(f"output {i} has to be like its tensor, or float32 of its shape and order")
+        flat += (p, o.data_ptr(), g.numel(), t | ot << 32)
+    table = array("Q", flat)
+    norm = grads[0].new_empty((), dtype=torch.float32)
     size = fn["clip_grad_norm_scratch_bytes"](count)
-    scratch = torch.empty(size, dtype=torch.uint8, device=dev)
-    _check(fn["clip_grad_norm"](table, count, max_norm, eps, norm.data_ptr(), scratch.data_ptr(), size,
-                                torch.cuda.current_stream(dev).cuda_stream), "clip_grad_norm")
+    scratch = norm.new_empty(size, dtype=torch.uint8)
+    _check(fn["clip_grad_norm"](table.buffer_info()[0], count, max_norm, eps, norm.data_ptr(), scratch.data_ptr(), size, _stream(at)), "clip_grad_norm")
     return norm
 
 
 def _dense(t):
     """Whether the tensor's elements fill its memory, in any order of its dimensions."""
-    if t.is_contiguous():
-        return True
     need = 1
     for stride, size in sorted(zip(t.stride(), t.shape)):
         if size != 1:
@@ -285,9 +290,9 @@ def clip_grad_norm(grads, max_norm, out=None, eps=1e-6, stream=None):
     """gem_nlr_clip_grad_norm: scales all tensors by min(1, max_norm / (norm + eps)), in place or into `out` (tensors of
     the same shapes, of the same types or float32), and returns the norm before it, a float32 scalar on the GPU."""
     grads = list(grads)
-    return _norm_and_clip(grads, max_norm, grads if out is None else out, eps, stream)
+    return _norm_and_clip(grads, max_norm, grads if out is None else list(out), eps, stream)
 
 
 def grad_norm(grads, stream=None):
     """The same norm alone; nothing else is written."""
-    return _norm_and_clip(grads, 0.0, None, 0.0, stream)
+    return _norm_and_clip(list(grads), 0.0, None, 0.0, stream)
