@@ -61,12 +61,12 @@ __device__ __forceinline__ double chunk_squares(const T* p, int m)
             Vec<T, 16> x[kAhead];
 #pragma unroll
             for (int u = 0; u < kAhead; ++u)
-                if (v0 + u * kThreads < whole) x[u].load(p + (size_t)(v0 + u * kThreads) * N); else x[u].zero();
+                if (v0 + u * kThreads < whole) x[u].load(p + (size_t)(v0 + u * kThreads) * N); else x[u].fill(0);
 #pragma unroll
             for (int u = 0; u < kAhead; ++u) {
                 float f[N];
 #pragma unroll
-                for (int i = 0; i < N; ++i) f[i] = x[u].get(i);
+                for (int i = 0; i < N; i += 2) { const float2 p = x[u].pair(i / 2); f[i] = p.x; f[i + 1] = p.y; }
                 acc += sum_squares(f);
             }
         }
@@ -98,7 +98,7 @@ __device__ __forceinline__ void chunk_scale(const T* p, O* o, int m, float c)
                 if (v0 + u * kThreads < whole) {
                     Vec<O, 16> y;
 #pragma unroll
-                    for (int i = 0; i < N; ++i) y.set(i, x[u].get(i) * c);
+                    for (int i = 0; i < N / 2; ++i) y.set_pair(i, __fmul2_rn(x[u].pair(i), f2(c)));
                     y.store_streaming(o + (size_t)(v0 + u * kThreads) * N);
                 }
         }

@@ -105,206 +105,169 @@ k_norm_dw_sum(const float* __restrict__ part, int records, int d, W* __restrict_
 
 // ---- rows in registers -------------------------------------------------------------------------------------------
 
-template <typename T, int N>
-__device__ __forceinline__ void load_weights(const void* w, int wtype_f32, int e, float (&out)[N], float none)
-{
-#pragma unroll
-    for (int i = 0; i < N; ++i)
-        out[i] = !w ? none : wtype_f32 ? ((const float*)w)[e + i] : to_f(((const T*)w)[e + i]);
-}
+// Rows that a group has in flight: enough loads to hide HBM's latency at two blocks an SM, within 128 registers.
+template <typename T> __host__ __device__ constexpr int fwd_rows(int epl) { return epl <= 8 ? 4 : epl <= 16 && sizeof(T) == 2 ? 4 : 2; }
 
-// rows in flight per group: about 48 registers of row, next to the weights
-template <typename T> __host__ __device__ constexpr int fwd_rows(int tpr, int epl)
-{
-    return tpr >= 512 ? 1 : epl <= 16 && tpr <= 32 ? 4 : 2;
-}
-
-template <typename T, int VB, int TPR, int EPL>
-__global__ void __launch_bounds__(block_of(TPR), TPR <= 256 ? 2 : 1)
-k_norm_rows(const T* __restrict__ x, int64_t ldx, const void* __restrict__ w, const void* __restrict__ b, int w32, int64_t n, int d,
+template <typename T, int MODE, int TPR, int EPL, int C>
+__global__ void __launch_bounds__(kRowBlock, 2)
+k_norm_rows(const T* __restrict__ x, int64_t ldx, const void* __restrict__ w, const void* __restrict__ b, int wtype, int64_t n, int d,
             float eps, T* __restrict__ y, int64_t ldy, float* __restrict__ mean, float* __restrict__ rstd)
 {
-    using V = Vec<T, VB>;
-    constexpr int N = V::N, NV = EPL / N, R = fwd_rows<T>(TPR, EPL), NT = block_of(TPR), GROUPS = NT / TPR;
-    constexpr bool KEEP = TPR <= 256;                 // the weights stay in registers; wider blocks have no room
-    __shared__ float sred[group_floats(TPR, R)];
+    using L = Lane<T, MODE, TPR, EPL, C>;
+    constexpr int R = fwd_rows<T>(EPL), N = L::N;
+    __shared__ float sred[group_floats(TPR, C, R)];
     int turn = 0;
-    const int l = threadIdx.x % TPR, g = threadIdx.x / TPR;
+    L ln(d);
+    ln.lie(x, ldx);
     const float inv_d = 1.0f / (float)d;
-    float wr[KEEP ? NV : 1][N], br[KEEP ? NV : 1][N];
-    if constexpr (KEEP) {
-#pragma unroll
-        for (int v = 0; v < NV; ++v) {
-            const int e = (v * TPR + l) * N;
-            if (e < d) { load_weights<T, N>(w, w32, e, wr[v], 1.0f); load_weights<T, N>(b, w32, e, br[v], 0.0f); }
-        }
-    }
-    for (int64_t base = (int64_t)blockIdx.x * GROUPS * R; base < n; base += (int64_t)gridDim.x * GROUPS * R) {
-        V xv[R][NV];
-        float s[R];
+    const int64_t span = (n - 1) * ldx + d, step = ln.groups();
+    float2 w2[L::PAIRS], b2[L::PAIRS];
+    load_weights<T>(ln, w, wtype, 1.0f, w2);
+    load_weights<T>(ln, b, wtype, 0.0f, b2);
+    for (int64_t base = ln.first_group(); base < n; base += R * step) {
+        Row<T, MODE, EPL> xv[R];
+        float s[R], mu[R];
 #pragma unroll
         for (int r = 0; r < R; ++r) {
-            const int64_t row = base + r * GROUPS + g;
-            const T* xr = x + row * ldx;
-#pragma unroll
-            for (int v = 0; v < NV; ++v) {
-                const int e = (v * TPR + l) * N;
-                if (row < n && e < d) xv[r][v].load(xr + e); else xv[r][v].zero();
-            }
+            const int64_t row = base + r * step + ln.g;
+            xv[r].load(ln, x, row, ldx, row < n, span, 0u);
         }
 #pragma unroll
         for (int r = 0; r < R; ++r) {
-            s[r] = 0.0f;
+            float2 a = f2(0.0f);
 #pragma unroll
-            for (int v = 0; v < NV; ++v)
-#pragma unroll
-                for (int i = 0; i < N; ++i) s[r] += xv[r][v].get(i);
+            for (int q = 0; q < L::PAIRS; ++q) a = __fadd2_rn(a, xv[r].pair(q));
+            s[r] = a.x + a.y;
         }
-        group_all<SumOp, TPR>(s, sred, turn);
-        float mu[R];
+        group_all<SumOp, TPR, C>(s, sred, turn);
 #pragma unroll
         for (int r = 0; r < R; ++r) {
             mu[r] = s[r] * inv_d;
-            s[r] = 0.0f;
+            const float2 m2 = f2(-mu[r]);
+            float2 a = f2(0.0f);
 #pragma unroll
-            for (int v = 0; v < NV; ++v)
-                if ((v * TPR + l) * N < d) {
-#pragma unroll
-                    for (int i = 0; i < N; ++i) { const float c = xv[r][v].get(i) - mu[r]; s[r] += c * c; }
+            for (int q = 0; q < L::PAIRS; ++q) {
+                const int k = 2 * q / N, i = 2 * q % N, k1 = (2 * q + 1) / N, i1 = (2 * q + 1) % N;
+                if (MODE == 2 || ln.any(k)) {
+                    float2 c = __fadd2_rn(xv[r].pair(q), m2);
+                    if (MODE == 2 || !ln.full(k)) {
+                        if (!ln.holds(k, i)) c.x = 0.0f;
+                        if (!ln.holds(k1, i1)) c.y = 0.0f;
+                    }
+                    a = __ffma2_rn(c, c, a);
                 }
+            }
+            s[r] = a.x + a.y;
         }
-        group_all<SumOp, TPR>(s, sred, turn);
+        group_all<SumOp, TPR, C>(s, sred, turn);
 #pragma unroll
         for (int r = 0; r < R; ++r) {
-            const int64_t row = base + r * GROUPS + g;
+            const int64_t row = base + r * step + ln.g;
             const float rs = 1.0f / sqrtf(s[r] * inv_d + eps);
             if (row < n) {
-                T* yr = y + row * ldy;
+                const float2 m2 = f2(-mu[r]), r2 = f2(rs);
 #pragma unroll
-                for (int v = 0; v < NV; ++v) {
-                    const int e = (v * TPR + l) * N;
-                    if (e < d) {
-                        float ww[N], bb[N];
-                        if constexpr (!KEEP) { load_weights<T, N>(w, w32, e, ww, 1.0f); load_weights<T, N>(b, w32, e, bb, 0.0f); }
-                        V o;
-#pragma unroll
-                        for (int i = 0; i < N; ++i) {
-                            const float h = (xv[r][v].get(i) - mu[r]) * rs;
-                            o.set(i, KEEP ? h * wr[KEEP ? v : 0][i] + br[KEEP ? v : 0][i] : h * ww[i] + bb[i]);
-                        }
-                        o.store(yr + e);
-                    }
-                }
-                if (l == 0) {
+                for (int q = 0; q < L::PAIRS; ++q)
+                    xv[r].set_pair(q, __ffma2_rn(__fmul2_rn(__fadd2_rn(xv[r].pair(q), m2), r2), w2[q], b2[q]));
+                xv[r].store(ln, y, row, ldy);
+                if (ln.l == 0) {
                     if (mean) mean[row] = mu[r];
                     if (rstd) rstd[row] = rs;
                 }
             }
         }
     }
+    leave_cluster<C>();
 }
 
 // The gradient.  Every thread keeps its columns' sums of dy h and dy over the rows that it sees (FP32), the block joins its
-// groups' sums and writes one record; k_norm_dw_join adds the records.
-template <typename T, int VB, int TPR, int EPL>
-__global__ void __launch_bounds__(block_of(TPR), TPR <= 256 ? 2 : 1)
+// groups' sums and writes one record; k_norm_dw_join adds the records.  While a row is worked on, the next one is already
+// on its way where the registers allow it.
+template <typename T, int MODE, int TPR, int EPL, int C>
+__global__ void __launch_bounds__(kRowBlock, 2)
 k_norm_grad_rows(const T* __restrict__ dy, int64_t lddy, const T* __restrict__ x, int64_t ldx, const float* __restrict__ mean,
-                 const float* __restrict__ rstd, const void* __restrict__ w, int w32, int64_t n, int d, T* __restrict__ dx, int64_t lddx,
+                 const float* __restrict__ rstd, const void* __restrict__ w, int wtype, int64_t n, int d, T* __restrict__ dx, int64_t lddx,
                  float* __restrict__ part)
 {
-    using V = Vec<T, VB>;
-    constexpr int N = V::N, NV = EPL / N, NT = block_of(TPR), GROUPS = NT / TPR;
-    __shared__ float sred[group_floats(TPR, 2)];
-    __shared__ float sums[GROUPS > 1 ? NT * EPL : 1];          // first the weights (one row), then the groups' sums
+    using L = Lane<T, MODE, TPR, EPL, C>;
+    constexpr int N = L::N;
+    constexpr bool AHEAD = sizeof(T) == 2 && MODE != 2 && EPL <= 16;
+    __shared__ float sred[group_floats(TPR, C, 2)];
+    __shared__ float sums[L::GROUPS > 1 ? kRowBlock * EPL : 1];
     int turn = 0;
-    const int l = threadIdx.x % TPR, g = threadIdx.x / TPR;
+    L ln(d);
+    ln.lie(x, ldx);
     const float inv_d = 1.0f / (float)d;
-    float aw[NV][N], ab[NV][N];
+    const int64_t span_x = (n - 1) * ldx + d, span_g = (n - 1) * lddy + d, step = ln.groups();
+    float2 w2[L::PAIRS], aw[L::PAIRS], ab[L::PAIRS];
+    load_weights<T>(ln, w, wtype, 1.0f, w2);
 #pragma unroll
-    for (int v = 0; v < NV; ++v)
-#pragma unroll
-        for (int i = 0; i < N; ++i) aw[v][i] = ab[v][i] = 0.0f;
-    const int64_t step = (int64_t)gridDim.x * GROUPS;
-    V xv[NV], gv[NV];
-    float mu = 0.0f, rs = 0.0f;
-    const auto fetch = [&](int64_t row) {
+    for (int q = 0; q < L::PAIRS; ++q) aw[q] = ab[q] = f2(0.0f);
+    Row<T, MODE, EPL> xv, gv, xn, gn;
+    float mu = 0.0f, rs = 0.0f, mun = 0.0f, rsn = 0.0f;
+    const auto fetch = [&](int64_t row, Row<T, MODE, EPL>& xr, Row<T, MODE, EPL>& gr, float& m, float& r) {
         const bool ok = row < n;
-        const T *xr = x + row * ldx, *gr = dy + row * lddy;
-#pragma unroll
-        for (int v = 0; v < NV; ++v) {
-            const int e = (v * TPR + l) * N;
-            if (ok && e < d) { xv[v].load(xr + e); gv[v].load(gr + e); } else { xv[v].zero(); gv[v].zero(); }
-        }
-        mu = ok ? mean[row] : 0.0f;
-        rs = ok ? rstd[row] : 0.0f;
+        xr.load(ln, x, row, ldx, ok, span_x, 0u);
+        gr.load(ln, dy, row, lddy, ok, span_g, 0u);
+        m = ok ? mean[row] : 0.0f;
+        r = ok ? rstd[row] : 0.0f;
     };
-    for (int64_t base = (int64_t)blockIdx.x * GROUPS; base < n; base += step) {
-        const int64_t row = base + g;
-        fetch(row);
-        float s[2] = {0.0f, 0.0f};
+    if (AHEAD) fetch(ln.group(), xn, gn, mun, rsn);
+    for (int64_t base = ln.first_group(); base < n; base += step) {
+        const int64_t row = base + ln.g;
+        if (AHEAD) {
+            xv = xn; gv = gn; mu = mun; rs = rsn;
+            fetch(row + step, xn, gn, mun, rsn);
+        } else {
+            fetch(row, xv, gv, mu, rs);
+        }
+        const float2 m2 = f2(-mu), r2 = f2(rs);
+        float2 s0 = f2(0.0f), s1 = f2(0.0f);
 #pragma unroll
-        for (int v = 0; v < NV; ++v) {
-            const int e = (v * TPR + l) * N;
-            if (e < d) {
-                float ww[N];
-                load_weights<T, N>(w, w32, e, ww, 1.0f);
-#pragma unroll
-                for (int i = 0; i < N; ++i) {
-                    const float gd = gv[v].get(i), h = (xv[v].get(i) - mu) * rs;
-                    aw[v][i] += gd * h;
-                    ab[v][i] += gd;
-                    s[0] += gd * ww[i];
-                    s[1] += gd * ww[i] * h;
-                }
-            }
+        for (int q = 0; q < L::PAIRS; ++q) {
+            const float2 g = gv.pair(q), h = __fmul2_rn(__fadd2_rn(xv.pair(q), m2), r2), gw = __fmul2_rn(g, w2[q]);
+            aw[q] = __ffma2_rn(g, h, aw[q]);
+            ab[q] = __fadd2_rn(ab[q], g);
+            s0 = __fadd2_rn(s0, gw);
+            s1 = __ffma2_rn(gw, h, s1);
         }
         if (!dx) continue;
-        group_all<SumOp, TPR>(s, sred, turn);
+        float s[2] = {s0.x + s0.y, s1.x + s1.y};
+        group_all<SumOp, TPR, C>(s, sred, turn);
         if (row < n) {
-            const float c1 = s[0] * inv_d, c2 = s[1] * inv_d;
+            const float2 c1 = f2(-s[0] * inv_d), c2 = f2(-s[1] * inv_d);
 #pragma unroll
-            for (int v = 0; v < NV; ++v) {
-                const int e = (v * TPR + l) * N;
-                if (e < d) {
-                    float ww[N];
-                    load_weights<T, N>(w, w32, e, ww, 1.0f);
-                    V o;
-#pragma unroll
-                    for (int i = 0; i < N; ++i) {
-                        const float h = (xv[v].get(i) - mu) * rs;
-                        o.set(i, rs * (gv[v].get(i) * ww[i] - c1 - h * c2));
-                    }
-                    o.store(dx + row * lddx + e);
-                }
+            for (int q = 0; q < L::PAIRS; ++q) {
+                const float2 h = __fmul2_rn(__fadd2_rn(xv.pair(q), m2), r2), gw = __fmul2_rn(gv.pair(q), w2[q]);
+                xv.set_pair(q, __fmul2_rn(r2, __ffma2_rn(h, c2, __fadd2_rn(gw, c1))));
             }
+            xv.store(ln, dx, row, lddx);
         }
     }
+    leave_cluster<C>();
     if (!part) return;
     next_may_start();
-    float* rec = part + (size_t)blockIdx.x * 2 * d;
+    float* rec = part + (size_t)(blockIdx.x / C) * 2 * d;
 #pragma unroll
     for (int which = 0; which < 2; ++which) {
-        if constexpr (GROUPS > 1) {
-            __syncthreads();
+        if constexpr (L::GROUPS > 1) __syncthreads();
 #pragma unroll
-            for (int v = 0; v < NV; ++v)
+        for (int q = 0; q < L::PAIRS; ++q)
 #pragma unroll
-                for (int i = 0; i < N; ++i) sums[g * (TPR * EPL) + (v * TPR + l) * N + i] = which ? ab[v][i] : aw[v][i];
+            for (int h = 0; h < 2; ++h) {
+                const int k = (2 * q + h) / N, i = (2 * q + h) % N;
+                if (ln.holds(k, i)) {
+                    const float2 a = which ? ab[q] : aw[q];
+                    (L::GROUPS > 1 ? sums + ln.g * (TPR * EPL) : rec + which * d)[ln.first(k) + i] = h ? a.y : a.x;
+                }
+            }
+        if constexpr (L::GROUPS > 1) {
             __syncthreads();
-            for (int e = threadIdx.x; e < d; e += NT) {
+            for (int e = threadIdx.x; e < d; e += kRowBlock) {
                 float t = 0.0f;
 #pragma unroll
-                for (int q = 0; q < GROUPS; ++q) t += sums[q * (TPR * EPL) + e];
+                for (int q = 0; q < L::GROUPS; ++q) t += sums[q * (TPR * EPL) + e];
                 rec[which * d + e] = t;
-            }
-        } else {
-#pragma unroll
-            for (int v = 0; v < NV; ++v) {
-                const int e = (v * TPR + l) * N;
-                if (e < d) {
-#pragma unroll
-                    for (int i = 0; i < N; ++i) rec[which * d + e + i] = which ? ab[v][i] : aw[v][i];
-                }
             }
         }
     }
@@ -332,9 +295,13 @@ k_norm_dw_join(const float* __restrict__ part, int records, int d, W* __restrict
     }
 }
 
-constexpr int kMaxRecords = 296;
-
-int norm_records(int64_t n) { const int64_t r = n; return (int)(r < 1 ? 1 : r > kMaxRecords ? kMaxRecords : r); }
+// Records of partial sums: at most one a block (or cluster) of the widest grid for the width, at least the eight that spread()
+// may round up to.
+int norm_records(int64_t n, int32_t d)
+{
+    const int most = d <= 6144 ? 2 * kTrainSMs : d <= 12288 ? kTrainSMs : kTrainSMs / 2;
+    return n > most ? most : n < 8 ? 8 : (int)n;
+}
 
 bool bad_rows(const void* p, int32_t type, int64_t ld) { return !p || !aligned_to(p, type_bytes(type)) || ld < 0; }
 
@@ -355,21 +322,21 @@ extern "C" int gem_nlr_layer_norm(const void* x_dev, int32_t type, int64_t ld_x,
         !aligned_to(rstd_dev, 4))
         return GEM_NLR_E_INVALID;
     cudaStream_t st = (cudaStream_t)cuda_stream;
-    const int tb = type_bytes(type), vx = vector_bytes(x_dev, ld_x, d, tb), vy = vector_bytes(y_dev, ld_y, d, tb);
-    const int w32 = wtype == GEM_NLR_F32;
+    const int tb = type_bytes(type);
+    const Matrix ms[2] = {{x_dev, ld_x}, {y_dev, ld_y}};
+    const Lying lie = lying(ms, 2, n, d, tb);
     bool held = false;
-    by_vector(type, vx < vy ? vx : vy, [&](auto t, auto vb) {
+    cudaError_t rc = cudaSuccess;
+    by_mode(type, lie.mode, [&](auto t, auto mode) {
         using T = decltype(t);
-        held = by_width<1024>(d, [&](auto tpr, auto epl) {
-            constexpr auto k = k_norm_rows<T, vb.value, tpr.value, epl.value>;
-            constexpr int nt = block_of(tpr.value);
-            constexpr int64_t rows = (int64_t)(nt / tpr.value) * fwd_rows<T>(tpr.value, epl.value);
-            const int64_t all = resident_blocks<k>(nt), need = (n + rows - 1) / rows;
-            k<<<(int)(need < all ? need : all), nt, 0, st>>>((const T*)x_dev, ld_x, weight_dev, bias_dev, w32, n, d, eps, (T*)y_dev, ld_y,
-                                                             mean_dev, rstd_dev);
+        held = by_width<sizeof(T)>(lie.mode == 1 ? (int64_t)d + 16 / tb - 1 : d, [&](auto tpr, auto epl, auto c) {
+            constexpr auto k = k_norm_rows<T, mode.value, tpr.value, epl.value, c.value>;
+            const int cl = spread(n, kRowBlock / tpr.value, fwd_rows<T>(epl.value), lie.period, resident_clusters<k, c.value>());
+            rc = launch_rows(k, cl * c.value, c.value, false, st, (const T*)x_dev, ld_x, weight_dev, bias_dev, (int)wtype, n, (int)d, eps,
+                             (T*)y_dev, ld_y, mean_dev, rstd_dev);
         });
     });
-    if (held) return launched();
+    if (held) return rc == cudaSuccess ? GEM_NLR_OK : GEM_NLR_E_CUDA;
     const int blocks = (int)(n < 148 * 8 ? n : 148 * 8);
     return by_type(type, [&](auto t) {
         using T = decltype(t);
@@ -386,7 +353,7 @@ extern "C" int gem_nlr_layer_norm(const void* x_dev, int32_t type, int64_t ld_x,
 extern "C" size_t gem_nlr_layer_norm_backward_scratch_bytes(int64_t n, int32_t d)
 {
     if (n < 0 || d < 1) return 0;
-    return (size_t)norm_records(n) * 2 * (size_t)d * sizeof(float);
+    return (size_t)norm_records(n, d) * 2 * (size_t)d * sizeof(float);
 }
 
 extern "C" int gem_nlr_layer_norm_backward(const void* dy_dev, int64_t ld_dy, const void* x_dev, int64_t ld_x, int32_t type,
@@ -407,28 +374,25 @@ extern "C" int gem_nlr_layer_norm_backward(const void* dy_dev, int64_t ld_dy, co
         return GEM_NLR_E_WORKSPACE;
     cudaStream_t st = (cudaStream_t)cuda_stream;
     float* part = (float*)scratch_dev;
-    const int tb = type_bytes(type), w32 = wtype == GEM_NLR_F32;
-    int vb_all = vector_bytes(dy_dev, ld_dy, d, tb);
-    const int vx = vector_bytes(x_dev, ld_x, d, tb), vdx = dx_dev ? vector_bytes(dx_dev, ld_dx, d, tb) : 16;
-    if (vx < vb_all) vb_all = vx;
-    if (vdx < vb_all) vb_all = vdx;
+    const int tb = type_bytes(type);
+    const Matrix ms[3] = {{dy_dev, ld_dy}, {x_dev, ld_x}, {dx_dev, ld_dx}};
+    const Lying lie = lying(ms, dx_dev ? 3 : 2, n, d, tb);
     bool held = false;
     int rec = 0;
+    cudaError_t err = cudaSuccess;
     if (n > 0)
-        by_vector(type, vb_all, [&](auto t, auto vb) {
+        by_mode(type, lie.mode, [&](auto t, auto mode) {
             using T = decltype(t);
-            held = by_width<512>(d, [&](auto tpr, auto epl) {
-                constexpr auto k = k_norm_grad_rows<T, vb.value, tpr.value, epl.value>;
-                constexpr int nt = block_of(tpr.value), groups = nt / tpr.value;
-                int64_t all = resident_blocks<k>(nt), need = (n + groups - 1) / groups;
-                if (all > kMaxRecords) all = kMaxRecords;
-                rec = (int)(need < all ? need : all);
-                k<<<rec, nt, 0, st>>>((const T*)dy_dev, ld_dy, (const T*)x_dev, ld_x, mean_dev, rstd_dev, weight_dev, w32, n, d,
-                                      (T*)dx_dev, ld_dx, dweight_dev || dbias_dev ? part : nullptr);
+            held = by_width<sizeof(T)>(lie.mode == 1 ? (int64_t)d + 16 / tb - 1 : d, [&](auto tpr, auto epl, auto c) {
+                constexpr auto k = k_norm_grad_rows<T, mode.value, tpr.value, epl.value, c.value>;
+                const int most = resident_clusters<k, c.value>(), room = norm_records(n, d);
+                rec = spread(n, kRowBlock / tpr.value, 1, lie.period, most < room ? most : room);
+                err = launch_rows(k, rec * c.value, c.value, false, st, (const T*)dy_dev, ld_dy, (const T*)x_dev, ld_x, mean_dev, rstd_dev,
+                                  weight_dev, (int)wtype, n, (int)d, (T*)dx_dev, ld_dx, dweight_dev || dbias_dev ? part : nullptr);
             });
         });
     if (held) {
-        int rc = launched();
+        int rc = err == cudaSuccess ? GEM_NLR_OK : GEM_NLR_E_CUDA;
         if (rc == GEM_NLR_OK && (dweight_dev || dbias_dev))
             rc = by_type(wtype, [&](auto t) {
                 using W = decltype(t);
@@ -437,7 +401,7 @@ extern "C" int gem_nlr_layer_norm_backward(const void* dy_dev, int64_t ld_dy, co
             });
         return rc;
     }
-    const int blocks = (int)(n < 148 * 8 ? n : 148 * 8), records = norm_records(n);
+    const int blocks = (int)(n < 148 * 8 ? n : 148 * 8), records = norm_records(n, d);
     return by_type(type, [&](auto t) {
         using T = decltype(t);
         const T *dy = (const T*)dy_dev, *x = (const T*)x_dev;

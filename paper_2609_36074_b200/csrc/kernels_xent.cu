@@ -125,64 +125,89 @@ k_xent_any(const T* z, int64_t ld, const int32_t* __restrict__ labels, int64_t n
 
 // ---- rows in registers -------------------------------------------------------------------------------------------
 
-// Rows at a time per group: the exponentials (FP32) and the logits of all of them stay in registers.
-__host__ __device__ constexpr int xent_rows(int tpr, int epl) { return tpr >= 512 ? 1 : epl <= 8 ? 4 : epl <= 16 ? 2 : 1; }
+// Rows that a group has in flight: their logits (own type) and exponentials (FP32) stay in registers.
+__host__ __device__ constexpr int xent_rows(int epl) { return epl <= 8 ? 4 : 2; }
 
-template <typename T, int VB, int TPR, int EPL>
-__global__ void __launch_bounds__(block_of(TPR), TPR <= 256 ? 3 : TPR <= 512 ? 2 : 1)
+// -inf in every element of a word
+template <typename T> __device__ __forceinline__ uint32_t minus_infinity();
+template <> __device__ __forceinline__ uint32_t minus_infinity<float>() { return 0xff800000u; }
+template <> __device__ __forceinline__ uint32_t minus_infinity<__half>() { return 0xfc00fc00u; }
+template <> __device__ __forceinline__ uint32_t minus_infinity<__nv_bfloat16>() { return 0xff80ff80u; }
+
+// 2^x to 2 ulp, 0 below FP32's normal range: the exponentials are weights beside a largest one of 1
+__device__ __forceinline__ float exp2_fast(float x) { float y; asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x)); return y; }
+
+// Largest element of a thread's part of a row (NaNs are passed over: they show in the sum); two at a time in 16-bit types.
+template <typename T, int MODE, int EPL>
+__device__ __forceinline__ float row_max(const Row<T, MODE, EPL>& z)
+{
+    using R = Row<T, MODE, EPL>;
+    if constexpr (sizeof(T) == 2 && MODE != 2) {
+        using T2 = typename std::conditional<std::is_same<T, __half>::value, __half2, __nv_bfloat162>::type;
+        T2 m = *reinterpret_cast<const T2*>(&z.v[0].w[0]);
+#pragma unroll
+        for (int k = 0; k < R::NV; ++k)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) m = __hmax2(m, *reinterpret_cast<const T2*>(&z.v[k].w[i]));
+        return fmaxf(to_f(m.x), to_f(m.y));
+    } else {
+        float m = -INFINITY;
+#pragma unroll
+        for (int q = 0; q < EPL / 2; ++q) { const float2 p = z.pair(q); m = fmaxf(fmaxf(m, p.x), p.y); }
+        return m;
+    }
+}
+
+template <typename T, int MODE, int TPR, int EPL, int C>
+__global__ void __launch_bounds__(kRowBlock, 2)
 k_xent_rows(const T* z, int64_t ld, const int32_t* __restrict__ labels, int64_t n, int k, int mean, Scratch* sc, float* __restrict__ loss,
             float* __restrict__ row_loss, T* dz, int64_t ldd)
 {
-    using V = Vec<T, VB>;
-    constexpr int N = V::N, NV = EPL / N, R = xent_rows(TPR, EPL), NT = block_of(TPR), GROUPS = NT / TPR;
+    using L = Lane<T, MODE, TPR, EPL, C>;
+    constexpr int N = L::N, R = xent_rows(EPL);
     constexpr float kLog2e = 1.4426950408889634f;
-    __shared__ float sred[group_floats(TPR, R)];
+    __shared__ float sred[group_floats(TPR, C, R)];
     int turn = 0;
-    const int l = threadIdx.x % TPR, g = threadIdx.x / TPR;
+    L ln(k);
+    ln.lie(z, ld);
     const float nan = __int_as_float(0x7fffffff);
+    const int64_t span = (n - 1) * ld + k, step = ln.groups();
     float scale = 0.0f;
     bool scaled = false;
     double sum = 0.0;
-    for (int64_t base = (int64_t)blockIdx.x * GROUPS * R; base < n; base += (int64_t)gridDim.x * GROUPS * R) {
-        V zv[R][NV];
+    for (int64_t base = ln.first_group(); base < n; base += R * step) {
+        Row<T, MODE, EPL> zv[R];
         float m[R], s[R], zl[R];
         int lab[R];
 #pragma unroll
         for (int r = 0; r < R; ++r) {
-            const int64_t row = base + r * GROUPS + g;
+            const int64_t row = base + r * step + ln.g;
             lab[r] = row < n ? labels[row] : -1;
-            const T* zr = z + row * ld;
-#pragma unroll
-            for (int v = 0; v < NV; ++v) {
-                const int e = (v * TPR + l) * N;
-                if (row < n && e < k) zv[r][v].load(zr + e);
-            }
-            zl[r] = lab[r] >= 0 && lab[r] < k ? to_f(zr[lab[r]]) : nan;
+            zv[r].load(ln, z, row, ld, row < n, span, minus_infinity<T>());
         }
 #pragma unroll
         for (int r = 0; r < R; ++r) {
-            m[r] = -INFINITY;
-#pragma unroll
-            for (int v = 0; v < NV; ++v)
-                if ((v * TPR + l) * N < k) {
-#pragma unroll
-                    for (int i = 0; i < N; ++i) m[r] = fmaxf(m[r], zv[r][v].get(i));
-                }
+            const int64_t row = base + r * step + ln.g;
+            zl[r] = lab[r] >= 0 && lab[r] < k ? to_f(z[row * ld + lab[r]]) : nan;
         }
-        group_all<MaxOp, TPR>(m, sred, turn);
-        float e_[R][NV][N];
+#pragma unroll
+        for (int r = 0; r < R; ++r) m[r] = row_max<T, MODE, EPL>(zv[r]);
+        group_all<MaxOp, TPR, C>(m, sred, turn);
+        float2 e2[R][L::PAIRS];
 #pragma unroll
         for (int r = 0; r < R; ++r) {
             if (m[r] == -INFINITY) m[r] = 0.0f;              // nothing but -inf (or NaN): no -inf - -inf below
-            s[r] = 0.0f;
+            const float2 m2 = f2(-m[r]);
+            float2 a = f2(0.0f);
 #pragma unroll
-            for (int v = 0; v < NV; ++v)
-                if ((v * TPR + l) * N < k) {
-#pragma unroll
-                    for (int i = 0; i < N; ++i) { e_[r][v][i] = exp2f((zv[r][v].get(i) - m[r]) * kLog2e); s[r] += e_[r][v][i]; }
-                }
+            for (int q = 0; q < L::PAIRS; ++q) {
+                const float2 t = __fmul2_rn(__fadd2_rn(zv[r].pair(q), m2), f2(kLog2e));
+                e2[r][q] = make_float2(exp2_fast(t.x), exp2_fast(t.y));
+                a = __fadd2_rn(a, e2[r][q]);
+            }
+            s[r] = a.x + a.y;
         }
-        group_all<SumOp, TPR>(s, sred, turn);
+        group_all<SumOp, TPR, C>(s, sred, turn);
         if (!scaled) {                                        // the first rows are read while the labels are counted
             grid_ready();
             scale = loss_scale(sc, mean);
@@ -190,35 +215,44 @@ k_xent_rows(const T* z, int64_t ld, const int32_t* __restrict__ labels, int64_t 
         }
 #pragma unroll
         for (int r = 0; r < R; ++r) {
-            const int64_t row = base + r * GROUPS + g;
+            const int64_t row = base + r * step + ln.g;
             if (row >= n) continue;
-            const bool counts = lab[r] >= 0, known = lab[r] < k, empty = s[r] == 0.0f;
-            if (l == 0) {
-                const float v = !counts ? 0.0f : !known ? nan : empty ? INFINITY : logf(s[r]) - (zl[r] - m[r]);
+            const bool known = lab[r] < k, empty = s[r] == 0.0f;
+            if (ln.l == 0) {
+                const float v = lab[r] < 0 ? 0.0f : !known ? nan : empty ? INFINITY : logf(s[r]) - (zl[r] - m[r]);
                 row_loss[row] = v;
                 sum += (double)v;
             }
             if (!dz) continue;
-            const float q = !known ? nan : empty ? 0.0f : 1.0f / s[r];
-            const int hot = empty ? -1 : lab[r];
-            T* dr = dz + row * ldd;
+            Row<T, MODE, EPL> o;
+            if (lab[r] < 0) o.zero();
+            else {
+                const float q = !known ? nan : empty ? 0.0f : 1.0f / s[r];
+                const float2 q2 = f2(q * scale);
+                const int hot = empty ? -N : lab[r];
 #pragma unroll
-            for (int v = 0; v < NV; ++v) {
-                const int e = (v * TPR + l) * N;
-                if (e < k) {
-                    V o;
+                for (int p = 0; p < L::PAIRS; ++p) o.set_pair(p, __fmul2_rn(e2[r][p], q2));
+                // the label's element: (p - 1) s
 #pragma unroll
-                    for (int i = 0; i < N; ++i) {
-                        const float p = e_[r][v][i] * q - (e + i == hot ? 1.0f : 0.0f);
-                        o.set(i, counts ? p * scale : 0.0f);
+                for (int v = 0; v < L::NV; ++v) {
+                    const int at = hot - ln.first(v);
+                    if (at >= 0 && at < N) {
+#pragma unroll
+                        for (int i = 0; i < N; ++i)
+                            if (i == at) {
+                                const int j = v * N + i;
+                                const float one = ((j & 1 ? e2[r][j / 2].y : e2[r][j / 2].x) * q - 1.0f) * scale;
+                                if constexpr (MODE == 2) o.v[v].e = from_f<T>(one); else o.v[v].set(i, from_f<T>(one));
+                            }
                     }
-                    o.store(dr + e);
                 }
             }
+            o.store(ln, dz, row, ldd);
         }
     }
     if (!scaled) grid_ready();
-    finish_loss<NT>(sum, mean, sc, loss);
+    leave_cluster<C>();
+    finish_loss<kRowBlock>(sum, mean, sc, loss);
 }
 
 }  // namespace
@@ -246,26 +280,22 @@ extern "C" int gem_nlr_label_cross_entropy(const void* logits_dev, int32_t type,
     Scratch* sc = (Scratch*)scratch_dev;
     k_count_labels<<<kCountBlocks, 256, 0, st>>>(labels_dev, n, sc);
     if (launched() != GEM_NLR_OK) return GEM_NLR_E_CUDA;
-    int vb_all = vector_bytes(logits_dev, ld, k, tb);
-    const int vd = dlogits_dev ? vector_bytes(dlogits_dev, ld_d, k, tb) : 16;
-    if (vd < vb_all) vb_all = vd;
+    const Matrix ms[2] = {{logits_dev, ld}, {dlogits_dev, ld_d}};
+    const Lying lie = lying(ms, dlogits_dev ? 2 : 1, n, k, tb);
     cudaError_t rc = cudaSuccess;
-    by_vector(type, vb_all, [&](auto t, auto vb) {
+    by_mode(type, lie.mode, [&](auto t, auto mode) {
         using T = decltype(t);
-        const bool held = by_width<1024>(k, [&](auto tpr, auto epl) {
-            constexpr auto kern = k_xent_rows<T, vb.value, tpr.value, epl.value>;
-            constexpr int nt = block_of(tpr.value);
-            constexpr int64_t rows = (int64_t)(nt / tpr.value) * xent_rows(tpr.value, epl.value);
-            int64_t blocks = resident_blocks<kern>(nt);
-            if (blocks > kMaxBlocks) blocks = kMaxBlocks;
-            if (blocks > (n + rows - 1) / rows) blocks = (n + rows - 1) / rows;
-            rc = launch_early(kern, dim3((unsigned)(blocks < 1 ? 1 : blocks)), nt, st, (const T*)logits_dev, ld, labels_dev, n, k, mean, sc,
-                              loss_dev, row_loss_dev, (T*)dlogits_dev, ld_d);
+        const bool held = by_width<sizeof(T)>(lie.mode == 1 ? (int64_t)k + 16 / tb - 1 : k, [&](auto tpr, auto epl, auto c) {
+            constexpr auto kern = k_xent_rows<T, mode.value, tpr.value, epl.value, c.value>;
+            const int most = resident_clusters<kern, c.value>();
+            const int cl = spread(n, kRowBlock / tpr.value, xent_rows(epl.value), lie.period, most < kMaxBlocks / c.value ? most : kMaxBlocks / c.value);
+            rc = launch_rows(kern, cl * c.value, c.value, true, st, (const T*)logits_dev, ld, labels_dev, n, (int)k, (int)mean, sc, loss_dev,
+                             row_loss_dev, (T*)dlogits_dev, ld_d);
         });
         if (!held) {
             const int64_t blocks = n < kTrainSMs * 8 ? n : kTrainSMs * 8;
             rc = launch_early(k_xent_any<T>, dim3((unsigned)(blocks < 1 ? 1 : blocks)), kRowThreads, st, (const T*)logits_dev, ld, labels_dev, n,
-                              k, mean, sc, loss_dev, row_loss_dev, (T*)dlogits_dev, ld_d);
+                              (int)k, (int)mean, sc, loss_dev, row_loss_dev, (T*)dlogits_dev, ld_d);
         }
     });
     return rc == cudaSuccess ? GEM_NLR_OK : GEM_NLR_E_CUDA;

@@ -6,6 +6,7 @@
 #include <math.h>
 #include <stddef.h>
 #include <stdint.h>
+#include <type_traits>
 #include "../../include/gem_nlr.h"
 #include "device_utils.cuh"
 

@@ -1,47 +1,251 @@
 // Rows of a matrix in registers: the layout that the layer norm and cross entropy kernels share.
 //
-// A row of `d` elements belongs to a group of TPR threads (8 or 16 of a warp, a warp, or several), EPL elements to a thread, taken as vectors of VB bytes: vector v of thread l holds elements (v TPR + l) N ... + N - 1, N = VB /
-// sizeof(T), so that a group's loads are contiguous.  The row is read once and stays in registers, still in its own type.
+// A row of d elements belongs to a group of TPR threads of a block (part of a warp, a warp, or several), or of C whole
+// blocks in a cluster; EPL elements to a thread, in vectors of N: vector v of lane l of the group's TPR C lanes holds
+// elements (v TPR C + l) N - s ... + N - 1, so that a group's loads are contiguous.  The row is read once and stays in
+// registers, in its own type, between the passes over it.
+//
+// Three ways of reading a matrix (MODE):
+//   0  every row begins and ends at a multiple of 16 bytes: vectors of 16 bytes, s = 0
+//   1  rows begin anywhere: still vectors of 16 bytes at multiples of 16, beginning s elements before the row.  s depends on
+//      the row's number modulo 16 bytes / element only, and a group's rows are that far apart (see Spread), so a thread's
+//      columns are the same in all its rows.  The first and last vector hold elements of the neighbouring rows (or of the
+//      padding), which are replaced after loading and left alone in storing
+//   2  element by element, where the matrices of one call lie differently to 16 bytes
+
 #pragma once
 #include "train_common.cuh"
 
 namespace gemnlr {
 
+// ---- a vector of elements ----------------------------------------------------------------------------------------
+
+__device__ __forceinline__ float2 f2(float a) { return make_float2(a, a); }
+
+template <typename T> __device__ __forceinline__ float2 unpack2(uint32_t w);
+template <> __device__ __forceinline__ float2 unpack2<__nv_bfloat16>(uint32_t w)
+{
+    return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u));
+}
+template <> __device__ __forceinline__ float2 unpack2<__half>(uint32_t w) { return __half22float2(*reinterpret_cast<__half2*>(&w)); }
+template <typename T> __device__ __forceinline__ uint32_t pack2(float2 v);
+template <> __device__ __forceinline__ uint32_t pack2<__nv_bfloat16>(float2 v)
+{
+    const __nv_bfloat162 t = __float22bfloat162_rn(v);
+    return *reinterpret_cast<const uint32_t*>(&t);
+}
+template <> __device__ __forceinline__ uint32_t pack2<__half>(float2 v)
+{
+    const __half2 t = __float22half2_rn(v);
+    return *reinterpret_cast<const uint32_t*>(&t);
+}
+
 template <int VB> struct RawOf;
-template <> struct RawOf<2> { using type = uint16_t; };
-template <> struct RawOf<4> { using type = uint32_t; };
 template <> struct RawOf<8> { using type = uint2; };
 template <> struct RawOf<16> { using type = uint4; };
 
+// VB = 8 or 16 bytes of elements
 template <typename T, int VB>
 struct Vec {
-    static constexpr int N = VB / (int)sizeof(T);
+    static constexpr int N = VB / (int)sizeof(T), P = N / 2;
     union {
         typename RawOf<VB>::type raw;
-        T e[N];
+        uint32_t w[VB / 4];
     };
     __device__ __forceinline__ Vec() {}
     __device__ __forceinline__ void load(const T* p) { raw = *reinterpret_cast<const typename RawOf<VB>::type*>(p); }
-    __device__ __forceinline__ void zero() { raw = typename RawOf<VB>::type{}; }
     __device__ __forceinline__ void store(T* p) const { *reinterpret_cast<typename RawOf<VB>::type*>(p) = raw; }
     __device__ __forceinline__ void store_streaming(T* p) const { __stcs(reinterpret_cast<typename RawOf<VB>::type*>(p), raw); }
-    __device__ __forceinline__ float get(int i) const { return to_f(e[i]); }
-    __device__ __forceinline__ void set(int i, float v) { e[i] = from_f<T>(v); }
+    __device__ __forceinline__ void fill(uint32_t x)
+    {
+#pragma unroll
+        for (int i = 0; i < VB / 4; ++i) w[i] = x;
+    }
+    __device__ __forceinline__ float2 pair(int p) const
+    {
+        if constexpr (sizeof(T) == 4) return make_float2(__uint_as_float(w[2 * p]), __uint_as_float(w[2 * p + 1]));
+        else return unpack2<T>(w[p]);
+    }
+    __device__ __forceinline__ void set_pair(int p, float2 v)
+    {
+        if constexpr (sizeof(T) == 4) { w[2 * p] = __float_as_uint(v.x); w[2 * p + 1] = __float_as_uint(v.y); }
+        else w[p] = pack2<T>(v);
+    }
+    __device__ __forceinline__ T at(int i) const
+    {
+        if constexpr (sizeof(T) == 4) return *reinterpret_cast<const T*>(&w[i]);
+        else {
+            const uint16_t h = (uint16_t)(w[i >> 1] >> ((i & 1) * 16));
+            return *reinterpret_cast<const T*>(&h);
+        }
+    }
+    __device__ __forceinline__ void set(int i, T v)
+    {
+        if constexpr (sizeof(T) == 4) w[i] = *reinterpret_cast<uint32_t*>(&v);
+        else {
+            const uint32_t h = *reinterpret_cast<uint16_t*>(&v);
+            w[i >> 1] = (i & 1) ? (w[i >> 1] & 0xffffu) | (h << 16) : (w[i >> 1] & 0xffff0000u) | h;
+        }
+    }
+    // elements outside [lo, hi) become those of the word x
+    __device__ __forceinline__ void keep(int lo, int hi, uint32_t x)
+    {
+        constexpr int E = 4 / (int)sizeof(T);
+#pragma unroll
+        for (int i = 0; i < VB / 4; ++i) {
+            uint32_t m = 0;
+#pragma unroll
+            for (int j = 0; j < E; ++j)
+                if (i * E + j >= lo && i * E + j < hi) m |= E == 1 ? 0xffffffffu : (0xffffu << (16 * j));
+            w[i] = (w[i] & m) | (x & ~m);
+        }
+    }
 };
 
-__host__ __device__ constexpr int block_of(int tpr) { return tpr <= 256 ? 256 : tpr; }
+// ---- a thread's part of a row ------------------------------------------------------------------------------------
 
-// Floats of shared memory that group_all needs for R values at a time.
-__host__ __device__ constexpr int group_floats(int tpr, int r) { return tpr <= 32 ? 1 : 2 * r * block_of(tpr) / 32; }
+constexpr int kRowBlock = 256;                       // threads of a block, whatever the shape
 
-// Sums (or maxima) of R values over the TPR threads of a group; every thread gets the same bits.  Where a group is more than
-// a warp, its warps meet at a barrier of their own (number 1 + group); `turn` alternates between the halves of the group's
-// part of `buf`, so that one barrier a call is enough: a thread that writes a half has passed the barrier that followed
-// every thread's last reads of it.
+__device__ __forceinline__ uint32_t cluster_rank() { uint32_t r; asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r)); return r; }
+__device__ __forceinline__ void cluster_barrier()
+{
+    asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+
+template <typename T, int MODE, int TPR, int EPL, int C>
+struct Lane {
+    static constexpr int N = MODE == 2 ? 1 : 16 / (int)sizeof(T);
+    static constexpr int NV = EPL / N, LANES = TPR * C, GROUPS = kRowBlock / TPR;
+    static constexpr int PAIRS = EPL / 2;            // pair q holds the thread's elements 2 q and 2 q + 1
+    static_assert(C == 1 || TPR == kRowBlock, "");
+    static_assert(EPL % N == 0 && EPL % 2 == 0, "");
+
+    int l, g, s, d;
+    __device__ __forceinline__ Lane(int d_) : g((int)threadIdx.x / TPR), s(0), d(d_)
+    {
+        l = (int)threadIdx.x % TPR;
+        if constexpr (C > 1) l += (int)cluster_rank() * TPR;
+    }
+    // number of the group among all groups of the grid, and their count
+    __device__ __forceinline__ int64_t group() const { return (int64_t)(blockIdx.x / C) * GROUPS + g; }
+    __device__ __forceinline__ int64_t first_group() const { return (int64_t)(blockIdx.x / C) * GROUPS; }
+    __device__ __forceinline__ int64_t groups() const { return (int64_t)(gridDim.x / C) * GROUPS; }
+    // s of the group's rows
+    __device__ __forceinline__ void lie(const T* base, int64_t ld)
+    {
+        if constexpr (MODE == 1) s = (int)((reinterpret_cast<uintptr_t>(base + group() * ld) & 15) / sizeof(T));
+    }
+    __device__ __forceinline__ int first(int v) const { return (v * LANES + l) * N - (MODE == 1 ? s : 0); }
+    __device__ __forceinline__ bool any(int v) const { return first(v) < d; }
+    __device__ __forceinline__ bool full(int v) const { return MODE == 1 ? first(v) >= 0 && first(v) + N <= d : any(v); }
+    __device__ __forceinline__ bool holds(int v, int i) const { return MODE == 1 ? first(v) + i >= 0 && first(v) + i < d : any(v); }
+};
+
+
+// The thread's elements of one row.
+template <typename T, int MODE, int EPL>
+struct Row {
+    static constexpr int N = MODE == 2 ? 1 : 16 / (int)sizeof(T), NV = EPL / N;
+    using V = Vec<T, 16>;
+    struct One { T e; };
+    typename std::conditional<MODE == 2, One, V>::type v[NV];
+
+    // span: elements from the matrix's first to its last; what lies between them may be read.  `none` fills what is no
+    // element of the row.
+    template <typename LN>
+    __device__ __forceinline__ void load(const LN& ln, const T* base, int64_t row, int64_t ld, bool ok, int64_t span, uint32_t none)
+    {
+        const int64_t at = row * ld;
+#pragma unroll
+        for (int k = 0; k < NV; ++k) {
+            const int e = ln.first(k);
+            if constexpr (MODE == 2) {
+                const uint32_t n = none;
+                if (ok && ln.any(k)) v[k].e = base[at + e]; else v[k].e = *reinterpret_cast<const T*>(&n);
+            } else {
+                if (ok && ln.full(k)) v[k].load(base + at + e);
+                else {
+                    v[k].fill(none);
+                    if (MODE == 1 && ok && ln.any(k)) {
+                        if (at + e >= 0 && at + e + N <= span) {
+                            v[k].load(base + at + e);
+                            v[k].keep(-e, ln.d - e, none);
+                        } else {
+#pragma unroll
+                            for (int i = 0; i < N; ++i)
+                                if (ln.holds(k, i)) v[k].set(i, base[at + e + i]);
+                        }
+                    }
+                }
+            }
+        }
+    }
+    template <typename LN>
+    __device__ __forceinline__ void store(const LN& ln, T* base, int64_t row, int64_t ld) const
+    {
+        T* p = base + row * ld;
+#pragma unroll
+        for (int k = 0; k < NV; ++k) {
+            const int e = ln.first(k);
+            if constexpr (MODE == 2) {
+                if (ln.any(k)) p[e] = v[k].e;
+            } else {
+                if (ln.full(k)) v[k].store(p + e);
+                else if (MODE == 1 && ln.any(k)) {
+#pragma unroll
+                    for (int i = 0; i < N; ++i)
+                        if (ln.holds(k, i)) p[e + i] = v[k].at(i);
+                }
+            }
+        }
+    }
+    __device__ __forceinline__ float2 pair(int q) const
+    {
+        if constexpr (MODE == 2) return make_float2(to_f(v[2 * q].e), to_f(v[2 * q + 1].e));
+        else return v[2 * q / N].pair(2 * q % N / 2);
+    }
+    __device__ __forceinline__ void set_pair(int q, float2 x)
+    {
+        if constexpr (MODE == 2) { v[2 * q].e = from_f<T>(x.x); v[2 * q + 1].e = from_f<T>(x.y); }
+        else v[2 * q / N].set_pair(2 * q % N / 2, x);
+    }
+    __device__ __forceinline__ void zero()
+    {
+#pragma unroll
+        for (int k = 0; k < NV; ++k)
+            if constexpr (MODE == 2) v[k].e = from_f<T>(0.0f); else v[k].fill(0);
+    }
+};
+
+// A thread's elements of a vector of d values (weights), as FP32 pairs; `none` where there is no vector, 0 outside the row.
+template <typename T, typename LN>
+__device__ __forceinline__ void load_weights(const LN& ln, const void* w, int wtype, float none, float2 (&out)[LN::PAIRS])
+{
+#pragma unroll
+    for (int q = 0; q < LN::PAIRS; ++q) {
+        float x[2];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const int k = (2 * q + h) / LN::N, i = (2 * q + h) % LN::N, e = ln.first(k) + i;
+            x[h] = !ln.holds(k, i) ? 0.0f : !w ? none : wtype == GEM_NLR_F32 ? ((const float*)w)[e] : to_f(((const T*)w)[e]);
+        }
+        out[q] = make_float2(x[0], x[1]);
+    }
+}
+
+// ---- sums over a group -------------------------------------------------------------------------------------------
+
 struct SumOp { __device__ __forceinline__ static float of(float a, float b) { return a + b; } };
 struct MaxOp { __device__ __forceinline__ static float of(float a, float b) { return fmaxf(a, b); } };
 
-template <typename Op, int TPR, int R>
+// Floats of shared memory that group_all needs for R values at a time.
+__host__ __device__ constexpr int group_floats(int tpr, int c, int r) { return tpr <= 32 ? 1 : 2 * r * c * kRowBlock / 32; }
+
+// Sums (or maxima) of R values over a group; every thread gets the same bits.  Where a group is more than a warp, its warps
+// write theirs to shared memory (of every block of the cluster) and meet at the group's barrier; `turn` alternates between
+// the halves of `buf`, so that one barrier a call is enough: a thread that writes a half has passed the barrier that
+// followed every thread's last reads of it.
+template <typename Op, int TPR, int C, int R>
 __device__ __forceinline__ void group_all(float (&v)[R], float* buf, int& turn)
 {
 #pragma unroll
@@ -49,85 +253,178 @@ __device__ __forceinline__ void group_all(float (&v)[R], float* buf, int& turn)
 #pragma unroll
         for (int r = 0; r < R; ++r) v[r] = Op::of(v[r], __shfl_xor_sync(0xffffffffu, v[r], o));
     if constexpr (TPR > 32) {
-        constexpr int W = TPR / 32, NT = block_of(TPR);
+        constexpr int W = TPR / 32 * C;              // values to join: one a warp
         const int g = threadIdx.x / TPR, warp = (threadIdx.x % TPR) >> 5, l = threadIdx.x & 31;
         float* b = buf + (g * 2 + turn) * R * W;
         turn ^= 1;
-        if (l == 0)
+        if constexpr (C > 1) {
+            if (l < C) {
+                const uint32_t here = (uint32_t)__cvta_generic_to_shared(b + cluster_rank() * (TPR / 32) + warp);
+                uint32_t there;
+                asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(there) : "r"(here), "r"(l));
 #pragma unroll
-            for (int r = 0; r < R; ++r) b[r * W + warp] = v[r];
-        if constexpr (TPR == NT) __syncthreads();
-        else asm volatile("bar.sync %0, %1;" ::"r"(g + 1), "n"(TPR) : "memory");
+                for (int r = 0; r < R; ++r)
+                    asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(there + (uint32_t)(r * W * sizeof(float))), "f"(v[r]) : "memory");
+            }
+            __syncwarp();
+            cluster_barrier();
+        } else {
+            if (l == 0)
+#pragma unroll
+                for (int r = 0; r < R; ++r) b[r * W + warp] = v[r];
+            if constexpr (TPR == kRowBlock) __syncthreads();
+            else asm volatile("bar.sync %0, %1;" ::"r"(g + 1), "n"(TPR) : "memory");
+        }
         // a warp's lanes take the warps' values and join them, instead of every thread reading all of them
 #pragma unroll
         for (int r = 0; r < R; ++r) {
             float t = b[r * W + (l & (W - 1))];
+            if constexpr (W == 64) t = Op::of(t, b[r * W + 32 + l]);
 #pragma unroll
-            for (int o = W / 2; o > 0; o >>= 1) t = Op::of(t, __shfl_xor_sync(0xffffffffu, t, o));
+            for (int o = (W < 32 ? W : 32) / 2; o > 0; o >>= 1) t = Op::of(t, __shfl_xor_sync(0xffffffffu, t, o));
             v[r] = t;
         }
     }
 }
 
-// How a row of d elements is spread: f(TPR, EPL) as constants, with TPR EPL >= d and no more than 24 elements (32 where a
-// full block is all there is) to a thread, which is what 128 registers hold next to weights or sums.  Returns false for a row wider than TMAX threads can hold.
+// A block of a cluster may not end while another one still writes to its shared memory.
+template <int C> __device__ __forceinline__ void leave_cluster() { if constexpr (C > 1) cluster_barrier(); }
+
+// ---- host: which shape, how many blocks ----------------------------------------------------------------------------
+
 template <int V> struct Const { static constexpr int value = V; };
-template <int TMAX, typename F>
-bool by_width(int64_t d, F f)
+
+// f(TPR, EPL, C) as constants for rows of `width` elements of `bytes` bytes (the window's s included), false if it is wider
+// than eight blocks hold.  EPL is what 128 registers hold next to weights or sums: 24 elements of 2 bytes, 16 of 4.  Rows of
+// more than 4096 (6144) elements go to clusters of blocks, so that every SM still has two blocks, one of which loads
+// while the other adds.
+template <int BYTES, typename F>
+bool by_width(int64_t width, F f)
 {
-    if (d <= 64) f(Const<8>{}, Const<8>{});
-    else if (d <= 128) f(Const<8>{}, Const<16>{});
-    else if (d <= 256) f(Const<16>{}, Const<16>{});
-    else if (d <= 512) f(Const<32>{}, Const<16>{});
-    else if (d <= 768) f(Const<32>{}, Const<24>{});
-    else if (d <= 1024) f(Const<64>{}, Const<16>{});
-    else if (d <= 1536) f(Const<64>{}, Const<24>{});
-    else if (d <= 2048) f(Const<128>{}, Const<16>{});
-    else if (d <= 4096) f(Const<256>{}, Const<16>{});
-    else if (d <= 8192) f(Const<512>{}, Const<16>{});
-    else {
-        if constexpr (TMAX >= 1024) {
-            if (d <= 16384) { f(Const<1024>{}, Const<16>{}); return true; }
-            if (d <= 32768) { f(Const<1024>{}, Const<32>{}); return true; }
-        }
-        return false;
-    }
+    constexpr int A = BYTES == 2 ? 16 : 12, B = BYTES == 2 ? 24 : 16;
+    if (width <= 64) f(Const<8>{}, Const<8>{}, Const<1>{});
+    else if (width <= 128) f(Const<8>{}, Const<16>{}, Const<1>{});
+    else if (width <= 256) f(Const<16>{}, Const<16>{}, Const<1>{});
+    else if (width <= 512) f(Const<32>{}, Const<16>{}, Const<1>{});
+    else if (BYTES == 2 && width <= 768) f(Const<BYTES == 2 ? 32 : 64>{}, Const<BYTES == 2 ? 24 : A>{}, Const<1>{});
+    else if (width <= 64 * A) f(Const<64>{}, Const<A>{}, Const<1>{});
+    else if (width <= 64 * B) f(Const<64>{}, Const<B>{}, Const<1>{});
+    else if (width <= 128 * A) f(Const<128>{}, Const<A>{}, Const<1>{});
+    else if (width <= 128 * B) f(Const<128>{}, Const<B>{}, Const<1>{});
+    else if (width <= 256 * A) f(Const<256>{}, Const<A>{}, Const<1>{});
+    else if (width <= 256 * B) f(Const<256>{}, Const<B>{}, Const<1>{});
+    else if (width <= 512 * A) f(Const<256>{}, Const<A>{}, Const<2>{});
+    else if (width <= 512 * B) f(Const<256>{}, Const<B>{}, Const<2>{});
+    else if (width <= 1024 * A) f(Const<256>{}, Const<A>{}, Const<4>{});
+    else if (width <= 1024 * B) f(Const<256>{}, Const<B>{}, Const<4>{});
+    else if (width <= 2048 * A) f(Const<256>{}, Const<A>{}, Const<8>{});
+    else if (width <= 2048 * B) f(Const<256>{}, Const<B>{}, Const<8>{});
+    else return false;
     return true;
 }
 
-// f(T, VB) for an element type and a vector width (as vector_bytes gives it)
+// One matrix operand of a call.
+struct Matrix {
+    const void* p;
+    int64_t     ld;
+};
+
+// How the matrices of a call can be read together, and the period of s in rows.
+struct Lying {
+    int mode;
+    int period;
+};
+inline Lying lying(const Matrix* ms, int count, int64_t n, int64_t d, int tb)
+{
+    const auto begin = [&](const Matrix& m) { return (int)(reinterpret_cast<uintptr_t>(m.p) & 15); };
+    const auto step = [&](const Matrix& m) { return n > 1 ? (int)((uint64_t)(m.ld * tb) & 15) : 0; };
+    for (int i = 1; i < count; ++i)
+        if (begin(ms[i]) != begin(ms[0]) || step(ms[i]) != step(ms[0])) return {2, 1};
+    const int st = step(ms[0]);
+    if (begin(ms[0]) == 0 && st == 0 && d * tb % 16 == 0) return {0, 1};
+    int period = 1;
+    while (st * period % 16 != 0) period *= 2;
+    return {1, period};
+}
+
+// f(T, MODE) as a value and a constant
 template <typename F>
-void by_vector(int32_t type, int vb, F f)
+void by_mode(int32_t type, int mode, F f)
 {
     by_type(type, [&](auto t) {
-        using T = decltype(t);
-        if (vb == 16) f(t, Const<16>{});
-        else if (vb == 4 || sizeof(T) == 4) f(t, Const<4>{});
-        else if constexpr (sizeof(T) == 2) f(t, Const<2>{});
+        if (mode == 0) f(t, Const<0>{});
+        else if (mode == 1) f(t, Const<1>{});
+        else f(t, Const<2>{});
         return 0;
     });
 }
 
-// Blocks of kernel K that fit the GPU at once (looked up once).
-template <auto K>
-int resident_blocks(int threads)
+// Groups of C blocks of kernel K that fit the GPU at once (looked up once).
+template <auto K, int C>
+int resident_clusters()
 {
-    static const int blocks = [&] {
-        int per_sm = 0;
-        if (cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, K, threads, 0) != cudaSuccess || per_sm < 1) per_sm = 1;
-        return per_sm * kTrainSMs;
+    static const int found = [] {
+        int per = 0;
+        if constexpr (C == 1) {
+            if (cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per, K, kRowBlock, 0) != cudaSuccess || per < 1) per = 1;
+            return per * kTrainSMs;
+        } else {
+            cudaLaunchConfig_t cfg = {};
+            cfg.gridDim = dim3(C);
+            cfg.blockDim = dim3(kRowBlock);
+            cudaLaunchAttribute at = {};
+            at.id = cudaLaunchAttributeClusterDimension;
+            at.val.clusterDim.x = C;
+            at.val.clusterDim.y = at.val.clusterDim.z = 1;
+            cfg.attrs = &at;
+            cfg.numAttrs = 1;
+            if (cudaOccupancyMaxActiveClusters(&per, K, &cfg) != cudaSuccess || per < 1) { cudaGetLastError(); per = 1; }
+            return per;
+        }
     }();
-    return blocks;
+    return found;
 }
 
-// The widest vector that every row of a matrix can be read in: its address, its row distance and its width are multiples.
-inline int vector_bytes(const void* p, int64_t ld, int64_t d, int tb)
+// Clusters (or blocks) to launch for n rows, `at_once` of them handled by one at a time: no more than `most`, and a multiple
+// of the period of s over the groups of one when rows come round again.
+inline int spread(int64_t n, int groups, int at_once, int period, int64_t most)
 {
-    const uintptr_t all = reinterpret_cast<uintptr_t>(p) | (uintptr_t)(ld * tb) | (uintptr_t)(d * tb);
-    return (all & 15) == 0 ? 16 : (all & 3) == 0 ? 4 : 2;
+    const int64_t need = (n + (int64_t)groups * at_once - 1) / ((int64_t)groups * at_once);
+    if (need <= most && at_once == 1) return (int)(need < 1 ? 1 : need);
+    int64_t c = need < most ? need : most;
+    const int per = period > groups ? period / groups : 1;
+    if (c > per) c -= c % per;
+    else c = per;                                    // (a few more than there are rows for: they find none)
+    return (int)c;
 }
 
-// Launch behind `st`'s last kernel that may begin while it ends (it waits for its results with grid_ready()).
+// Launch of `blocks` blocks of kRowBlock threads in clusters of c; `early`: it may begin while the stream's last kernel ends
+// (and waits for its results with grid_ready()).
+template <typename... P, typename... A>
+cudaError_t launch_rows(void (*k)(P...), int blocks, int c, bool early, cudaStream_t st, A... args)
+{
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)blocks);
+    cfg.blockDim = dim3(kRowBlock);
+    cfg.stream = st;
+    cudaLaunchAttribute at[2] = {};
+    int m = 0;
+    if (early) {
+        at[m].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+        at[m++].val.programmaticStreamSerializationAllowed = 1;
+    }
+    if (c > 1) {
+        at[m].id = cudaLaunchAttributeClusterDimension;
+        at[m].val.clusterDim.x = (unsigned)c;
+        at[m].val.clusterDim.y = at[m].val.clusterDim.z = 1;
+        ++m;
+    }
+    cfg.attrs = at;
+    cfg.numAttrs = (unsigned)m;
+    return cudaLaunchKernelEx(&cfg, k, (P)args...);
+}
+
+// Launch behind `st`'s last kernel that may begin while it ends.
 template <typename... P, typename... A>
 cudaError_t launch_early(void (*k)(P...), dim3 grid, int threads, cudaStream_t st, A... args)
 {
