@@ -103,10 +103,16 @@ k_norm_dw_sum(const float* __restrict__ part, int records, int d, W* __restrict_
     out[e < d ? e : e - d] = from_f<W>((float)v);
 }
 
-// ---- rows in registers -------------------------------------------------------------------------------------------
+// ---- streamed rows -----------------------------------------------------------------------------------------------
 
-// Rows that a group has in flight: enough loads to hide HBM's latency at two blocks an SM, within 128 registers.
-template <typename T> __host__ __device__ constexpr int fwd_rows(int epl) { return epl <= 8 ? 4 : epl <= 16 && sizeof(T) == 2 ? 4 : 2; }
+// Rows that a group works on at a time: two of a few vectors, so that their sums over the group run side by side.
+__host__ __device__ constexpr int fwd_rows(int epl) { return epl <= 16 ? 2 : 1; }
+
+template <typename T, int MODE, int TPR, int EPL, int C>
+struct NormShape {
+    using S0 = Source<T, MODE, TPR, EPL, C>;
+    static constexpr int ROWS = fwd_rows(EPL), STAGE = ROWS * S0::stage_bytes(), STAGES = ring_stages(STAGE), SHARED = STAGE * STAGES;
+};
 
 template <typename T, int MODE, int TPR, int EPL, int C>
 __global__ void __launch_bounds__(kRowBlock, 2)
@@ -114,24 +120,36 @@ k_norm_rows(const T* __restrict__ x, int64_t ldx, const void* __restrict__ w, co
             float eps, T* __restrict__ y, int64_t ldy, float* __restrict__ mean, float* __restrict__ rstd)
 {
     using L = Lane<T, MODE, TPR, EPL, C>;
-    constexpr int R = fwd_rows<T>(EPL), N = L::N;
+    using H = NormShape<T, MODE, TPR, EPL, C>;
+    constexpr int R = H::ROWS, N = L::N, S = H::STAGES;
+    extern __shared__ __align__(16) unsigned char ring[];
     __shared__ float sred[group_floats(TPR, C, R)];
-    int turn = 0;
-    L ln(d);
-    ln.lie(x, ldx);
+    int turn = 0, at = 0;
+    const L ln(d, x, ldx);
+    const Source<T, MODE, TPR, EPL, C> xs(x, ldx, n, d);
+    const uint32_t slot = (uint32_t)__cvta_generic_to_shared(ring) + threadIdx.x * 16;
     const float inv_d = 1.0f / (float)d;
-    const int64_t span = (n - 1) * ldx + d, step = ln.groups();
+    const int64_t step = ln.groups();
+    const auto send = [&](int64_t base, int stage) {
+        if (base < n)
+#pragma unroll
+            for (int r = 0; r < R; ++r) xs.send(ln, base + r * step + ln.g, slot + (uint32_t)(stage * H::STAGE + r * H::S0::stage_bytes()));
+        copies_end();
+    };
+#pragma unroll
+    for (int i = 0; i < S - 1; ++i) send(ln.first_group() + i * R * step, i);
     float2 w2[L::PAIRS], b2[L::PAIRS];
     load_weights<T>(ln, w, wtype, 1.0f, w2);
     load_weights<T>(ln, b, wtype, 0.0f, b2);
     for (int64_t base = ln.first_group(); base < n; base += R * step) {
+        send(base + (S - 1) * R * step, at == 0 ? S - 1 : at - 1);
+        copies_wait<S - 1>();
         Row<T, MODE, EPL> xv[R];
         float s[R], mu[R];
 #pragma unroll
-        for (int r = 0; r < R; ++r) {
-            const int64_t row = base + r * step + ln.g;
-            xv[r].load(ln, x, row, ldx, row < n, span, 0u);
-        }
+        for (int r = 0; r < R; ++r)
+            xs.take(ln, base + r * step + ln.g, slot + (uint32_t)(at * H::STAGE + r * H::S0::stage_bytes()), 0u, xv[r]);
+        at = at + 1 == S ? 0 : at + 1;
 #pragma unroll
         for (int r = 0; r < R; ++r) {
             float2 a = f2(0.0f);
@@ -146,15 +164,19 @@ k_norm_rows(const T* __restrict__ x, int64_t ldx, const void* __restrict__ w, co
             const float2 m2 = f2(-mu[r]);
             float2 a = f2(0.0f);
 #pragma unroll
-            for (int q = 0; q < L::PAIRS; ++q) {
-                const int k = 2 * q / N, i = 2 * q % N, k1 = (2 * q + 1) / N, i1 = (2 * q + 1) % N;
-                if (MODE == 2 || ln.any(k)) {
-                    float2 c = __fadd2_rn(xv[r].pair(q), m2);
-                    if (MODE == 2 || !ln.full(k)) {
-                        if (!ln.holds(k, i)) c.x = 0.0f;
-                        if (!ln.holds(k1, i1)) c.y = 0.0f;
+            for (int k = 0; k < (MODE == 2 ? L::PAIRS : L::NV); ++k) {
+                const bool cut = MODE == 2 || ln.end(k);
+                if (cut || ln.any(k)) {
+#pragma unroll
+                    for (int i = 0; i < (MODE == 2 ? 1 : N / 2); ++i) {
+                        const int q = MODE == 2 ? k : k * (N / 2) + i;
+                        float2 c = __fadd2_rn(xv[r].pair(q), m2);
+                        if (cut) {
+                            if (!ln.holds(2 * q / N, 2 * q % N)) c.x = 0.0f;
+                            if (!ln.holds((2 * q + 1) / N, (2 * q + 1) % N)) c.y = 0.0f;
+                        }
+                        a = __ffma2_rn(c, c, a);
                     }
-                    a = __ffma2_rn(c, c, a);
                 }
             }
             s[r] = a.x + a.y;
@@ -181,8 +203,15 @@ k_norm_rows(const T* __restrict__ x, int64_t ldx, const void* __restrict__ w, co
 }
 
 // The gradient.  Every thread keeps its columns' sums of dy h and dy over the rows that it sees (FP32), the block joins its
-// groups' sums and writes one record; k_norm_dw_join adds the records.  While a row is worked on, the next one is already
-// on its way where the registers allow it.
+// groups' sums and writes one record; k_norm_dw_join adds the records.  A row's mean and rstd come through the ring too.
+template <typename T, int MODE, int TPR, int EPL, int C>
+struct GradShape {
+    using S0 = Source<T, MODE, TPR, EPL, C>;
+    static constexpr int ROW = S0::stage_bytes(), STAGE = 2 * ROW + (MODE == 2 ? 0 : 2 * 4 * kRowBlock), STAGES = ring_stages(STAGE);
+    static constexpr int SUMS = kRowBlock / TPR > 1 ? kRowBlock * EPL * 4 : 0;       // the groups' sums, after the ring's last use
+    static constexpr int SHARED = STAGE * STAGES > SUMS ? STAGE * STAGES : SUMS;
+};
+
 template <typename T, int MODE, int TPR, int EPL, int C>
 __global__ void __launch_bounds__(kRowBlock, 2)
 k_norm_grad_rows(const T* __restrict__ dy, int64_t lddy, const T* __restrict__ x, int64_t ldx, const float* __restrict__ mean,
@@ -190,37 +219,53 @@ k_norm_grad_rows(const T* __restrict__ dy, int64_t lddy, const T* __restrict__ x
                  float* __restrict__ part)
 {
     using L = Lane<T, MODE, TPR, EPL, C>;
-    constexpr int N = L::N;
-    constexpr bool AHEAD = sizeof(T) == 2 && MODE != 2 && EPL <= 16;
+    using H = GradShape<T, MODE, TPR, EPL, C>;
+    constexpr int N = L::N, S = H::STAGES;
+    constexpr bool AGAIN = MODE != 2 && EPL > 16;    // the row is read from the ring a second time: its registers hold sums
+    extern __shared__ __align__(16) unsigned char ring[];
     __shared__ float sred[group_floats(TPR, C, 2)];
-    __shared__ float sums[L::GROUPS > 1 ? kRowBlock * EPL : 1];
-    int turn = 0;
-    L ln(d);
-    ln.lie(x, ldx);
+    int turn = 0, at = 0;
+    const L ln(d, x, ldx);
+    const Source<T, MODE, TPR, EPL, C> xs(x, ldx, n, d), gs(dy, lddy, n, d);
+    const uint32_t ring0 = (uint32_t)__cvta_generic_to_shared(ring), slot = ring0 + threadIdx.x * 16, slot4 = ring0 + 2 * H::ROW + threadIdx.x * 4;
     const float inv_d = 1.0f / (float)d;
-    const int64_t span_x = (n - 1) * ldx + d, span_g = (n - 1) * lddy + d, step = ln.groups();
+    const int64_t step = ln.groups();
+    const auto send = [&](int64_t base, int stage) {
+        if constexpr (MODE != 2) {
+            if (base < n) {
+                const int64_t row = base + ln.g;
+                const uint32_t o = (uint32_t)(stage * H::STAGE);
+                xs.send(ln, row, slot + o);
+                gs.send(ln, row, slot + o + H::ROW);
+                copy4_ahead(slot4 + o, row < n ? mean + row : mean, row < n);
+                copy4_ahead(slot4 + o + 4 * kRowBlock, row < n ? rstd + row : rstd, row < n);
+            }
+            copies_end();
+        }
+    };
+#pragma unroll
+    for (int i = 0; i < S - 1; ++i) send(ln.first_group() + i * step, i);
     float2 w2[L::PAIRS], aw[L::PAIRS], ab[L::PAIRS];
     load_weights<T>(ln, w, wtype, 1.0f, w2);
 #pragma unroll
     for (int q = 0; q < L::PAIRS; ++q) aw[q] = ab[q] = f2(0.0f);
-    Row<T, MODE, EPL> xv, gv, xn, gn;
-    float mu = 0.0f, rs = 0.0f, mun = 0.0f, rsn = 0.0f;
-    const auto fetch = [&](int64_t row, Row<T, MODE, EPL>& xr, Row<T, MODE, EPL>& gr, float& m, float& r) {
-        const bool ok = row < n;
-        xr.load(ln, x, row, ldx, ok, span_x, 0u);
-        gr.load(ln, dy, row, lddy, ok, span_g, 0u);
-        m = ok ? mean[row] : 0.0f;
-        r = ok ? rstd[row] : 0.0f;
-    };
-    if (AHEAD) fetch(ln.group(), xn, gn, mun, rsn);
     for (int64_t base = ln.first_group(); base < n; base += step) {
         const int64_t row = base + ln.g;
-        if (AHEAD) {
-            xv = xn; gv = gn; mu = mun; rs = rsn;
-            fetch(row + step, xn, gn, mun, rsn);
+        const uint32_t o = (uint32_t)(at * H::STAGE);
+        Row<T, MODE, EPL> xv, gv;
+        float mu, rs;
+        if constexpr (MODE != 2) {
+            send(base + (S - 1) * step, at == 0 ? S - 1 : at - 1);
+            copies_wait<S - 1>();
+            mu = __uint_as_float(read4(slot4 + o));
+            rs = __uint_as_float(read4(slot4 + o + 4 * kRowBlock));
         } else {
-            fetch(row, xv, gv, mu, rs);
+            mu = row < n ? mean[row] : 0.0f;
+            rs = row < n ? rstd[row] : 0.0f;
         }
+        xs.take(ln, row, slot + o, 0u, xv);
+        gs.take(ln, row, slot + o + H::ROW, 0u, gv);
+        at = at + 1 == S ? 0 : at + 1;
         const float2 m2 = f2(-mu), r2 = f2(rs);
         float2 s0 = f2(0.0f), s1 = f2(0.0f);
 #pragma unroll
@@ -236,6 +281,10 @@ k_norm_grad_rows(const T* __restrict__ dy, int64_t lddy, const T* __restrict__ x
         group_all<SumOp, TPR, C>(s, sred, turn);
         if (row < n) {
             const float2 c1 = f2(-s[0] * inv_d), c2 = f2(-s[1] * inv_d);
+            if (AGAIN) {
+                xs.take(ln, row, slot + o, 0u, xv);
+                gs.take(ln, row, slot + o + H::ROW, 0u, gv);
+            }
 #pragma unroll
             for (int q = 0; q < L::PAIRS; ++q) {
                 const float2 h = __fmul2_rn(__fadd2_rn(xv.pair(q), m2), r2), gw = __fmul2_rn(gv.pair(q), w2[q]);
@@ -247,7 +296,10 @@ k_norm_grad_rows(const T* __restrict__ dy, int64_t lddy, const T* __restrict__ x
     leave_cluster<C>();
     if (!part) return;
     next_may_start();
+    copies_wait<0>();
     float* rec = part + (size_t)(blockIdx.x / C) * 2 * d;
+    float* sums = reinterpret_cast<float*>(ring);
+    constexpr int W = TPR * EPL;                     // places of a group in `sums`
 #pragma unroll
     for (int which = 0; which < 2; ++which) {
         if constexpr (L::GROUPS > 1) __syncthreads();
@@ -258,16 +310,30 @@ k_norm_grad_rows(const T* __restrict__ dy, int64_t lddy, const T* __restrict__ x
                 const int k = (2 * q + h) / N, i = (2 * q + h) % N;
                 if (ln.holds(k, i)) {
                     const float2 a = which ? ab[q] : aw[q];
-                    (L::GROUPS > 1 ? sums + ln.g * (TPR * EPL) : rec + which * d)[ln.first(k) + i] = h ? a.y : a.x;
+                    (L::GROUPS > 1 ? sums + ln.g * W : rec + which * d)[ln.first(k) + i] = h ? a.y : a.x;
                 }
             }
         if constexpr (L::GROUPS > 1) {
+            // in two steps where a row is narrower than the block: its threads share a column's groups
+            constexpr int SPLIT = W < kRowBlock ? kRowBlock / W : 1, EACH = L::GROUPS / SPLIT;
             __syncthreads();
-            for (int e = threadIdx.x; e < d; e += kRowBlock) {
+            for (int e = threadIdx.x % W; e < W; e += kRowBlock) {
+                const int q0 = SPLIT > 1 ? (int)threadIdx.x / W * EACH : 0;
                 float t = 0.0f;
+                if (e < d)
 #pragma unroll
-                for (int q = 0; q < L::GROUPS; ++q) t += sums[q * (TPR * EPL) + e];
-                rec[which * d + e] = t;
+                    for (int q = 0; q < EACH; ++q) t += sums[(q0 + q) * W + e];
+                if constexpr (SPLIT > 1) sums[q0 * W + e] = t;           // (only this thread reads that place)
+                else if (e < d) rec[which * d + e] = t;
+            }
+            if constexpr (SPLIT > 1) {
+                __syncthreads();
+                if ((int)threadIdx.x < d) {
+                    float t = 0.0f;
+#pragma unroll
+                    for (int q = 0; q < SPLIT; ++q) t += sums[q * EACH * W + threadIdx.x];
+                    rec[which * d + threadIdx.x] = t;
+                }
             }
         }
     }
@@ -329,10 +395,11 @@ extern "C" int gem_nlr_layer_norm(const void* x_dev, int32_t type, int64_t ld_x,
     cudaError_t rc = cudaSuccess;
     by_mode(type, lie.mode, [&](auto t, auto mode) {
         using T = decltype(t);
-        held = by_width<sizeof(T)>(lie.mode == 1 ? (int64_t)d + 16 / tb - 1 : d, [&](auto tpr, auto epl, auto c) {
+        held = by_width<mode.value == 2 ? 4 : (int)sizeof(T), mode.value != 2 && sizeof(T) == 2 ? 32 : 16>(lie.mode == 1 ? (int64_t)d + 16 / tb - 1 : d, [&](auto tpr, auto epl, auto c) {
             constexpr auto k = k_norm_rows<T, mode.value, tpr.value, epl.value, c.value>;
-            const int cl = spread(n, kRowBlock / tpr.value, fwd_rows<T>(epl.value), lie.period, resident_clusters<k, c.value>());
-            rc = launch_rows(k, cl * c.value, c.value, false, st, (const T*)x_dev, ld_x, weight_dev, bias_dev, (int)wtype, n, (int)d, eps,
+            constexpr int shared = NormShape<T, mode.value, tpr.value, epl.value, c.value>::SHARED;
+            const int cl = spread(n, kRowBlock / tpr.value, fwd_rows(epl.value), lie.period, resident_clusters<k, c.value>(shared));
+            rc = launch_rows(k, cl * c.value, c.value, shared, false, st, (const T*)x_dev, ld_x, weight_dev, bias_dev, (int)wtype, n, (int)d, eps,
                              (T*)y_dev, ld_y, mean_dev, rstd_dev);
         });
     });
@@ -383,11 +450,12 @@ extern "C" int gem_nlr_layer_norm_backward(const void* dy_dev, int64_t ld_dy, co
     if (n > 0)
         by_mode(type, lie.mode, [&](auto t, auto mode) {
             using T = decltype(t);
-            held = by_width<sizeof(T)>(lie.mode == 1 ? (int64_t)d + 16 / tb - 1 : d, [&](auto tpr, auto epl, auto c) {
+            held = by_width<mode.value == 2 ? 4 : (int)sizeof(T), mode.value != 2 && sizeof(T) == 2 ? 24 : 16>(lie.mode == 1 ? (int64_t)d + 16 / tb - 1 : d, [&](auto tpr, auto epl, auto c) {
                 constexpr auto k = k_norm_grad_rows<T, mode.value, tpr.value, epl.value, c.value>;
-                const int most = resident_clusters<k, c.value>(), room = norm_records(n, d);
+                constexpr int shared = GradShape<T, mode.value, tpr.value, epl.value, c.value>::SHARED;
+                const int most = resident_clusters<k, c.value>(shared), room = norm_records(n, d);
                 rec = spread(n, kRowBlock / tpr.value, 1, lie.period, most < room ? most : room);
-                err = launch_rows(k, rec * c.value, c.value, false, st, (const T*)dy_dev, ld_dy, (const T*)x_dev, ld_x, mean_dev, rstd_dev,
+                err = launch_rows(k, rec * c.value, c.value, shared, false, st, (const T*)dy_dev, ld_dy, (const T*)x_dev, ld_x, mean_dev, rstd_dev,
                                   weight_dev, (int)wtype, n, (int)d, (T*)dx_dev, ld_dx, dweight_dev || dbias_dev ? part : nullptr);
             });
         });

@@ -125,8 +125,15 @@ k_xent_any(const T* z, int64_t ld, const int32_t* __restrict__ labels, int64_t n
 
 // ---- rows in registers -------------------------------------------------------------------------------------------
 
-// Rows that a group has in flight: their logits (own type) and exponentials (FP32) stay in registers.
-__host__ __device__ constexpr int xent_rows(int epl) { return epl <= 8 ? 4 : 2; }
+// Rows that a group works on at a time (their exponentials stay in registers, FP32).
+__host__ __device__ constexpr int xent_rows(int epl) { return epl <= 16 ? 2 : 1; }
+
+template <typename T, int MODE, int TPR, int EPL, int C>
+struct XentShape {
+    using S0 = Source<T, MODE, TPR, EPL, C>;
+    static constexpr int ROWS = xent_rows(EPL), ROW = S0::stage_bytes() + (MODE == 2 ? 0 : 4 * kRowBlock);       // a row and its label
+    static constexpr int STAGE = ROWS * ROW, STAGES = ring_stages(STAGE), SHARED = STAGE * STAGES;
+};
 
 // -inf in every element of a word
 template <typename T> __device__ __forceinline__ uint32_t minus_infinity();
@@ -164,32 +171,53 @@ k_xent_rows(const T* z, int64_t ld, const int32_t* __restrict__ labels, int64_t 
             float* __restrict__ row_loss, T* dz, int64_t ldd)
 {
     using L = Lane<T, MODE, TPR, EPL, C>;
-    constexpr int N = L::N, R = xent_rows(EPL);
+    using H = XentShape<T, MODE, TPR, EPL, C>;
+    constexpr int N = L::N, R = H::ROWS, S = H::STAGES;
     constexpr float kLog2e = 1.4426950408889634f;
+    extern __shared__ __align__(16) unsigned char ring[];
     __shared__ float sred[group_floats(TPR, C, R)];
-    int turn = 0;
-    L ln(k);
-    ln.lie(z, ld);
+    int turn = 0, at = 0;
+    const L ln(k, z, ld);
+    const Source<T, MODE, TPR, EPL, C> zs(z, ld, n, k);
+    const uint32_t ring0 = (uint32_t)__cvta_generic_to_shared(ring), slot = ring0 + threadIdx.x * 16,
+                   slot4 = ring0 + H::S0::stage_bytes() + threadIdx.x * 4;
     const float nan = __int_as_float(0x7fffffff);
-    const int64_t span = (n - 1) * ld + k, step = ln.groups();
+    const int64_t step = ln.groups();
+    const auto send = [&](int64_t base, int stage) {
+        if constexpr (MODE != 2) {
+            if (base < n)
+#pragma unroll
+                for (int r = 0; r < R; ++r) {
+                    const int64_t row = base + r * step + ln.g;
+                    const uint32_t o = (uint32_t)(stage * H::STAGE + r * H::ROW);
+                    zs.send(ln, row, slot + o);
+                    copy4_ahead(slot4 + o, row < n ? labels + row : labels, row < n);
+                }
+            copies_end();
+        }
+    };
+#pragma unroll
+    for (int i = 0; i < S - 1; ++i) send(ln.first_group() + i * R * step, i);
     float scale = 0.0f;
     bool scaled = false;
     double sum = 0.0;
     for (int64_t base = ln.first_group(); base < n; base += R * step) {
         Row<T, MODE, EPL> zv[R];
-        float m[R], s[R], zl[R];
+        float m[R], s[R];
         int lab[R];
-#pragma unroll
-        for (int r = 0; r < R; ++r) {
-            const int64_t row = base + r * step + ln.g;
-            lab[r] = row < n ? labels[row] : -1;
-            zv[r].load(ln, z, row, ld, row < n, span, minus_infinity<T>());
+        if constexpr (MODE != 2) {
+            send(base + (S - 1) * R * step, at == 0 ? S - 1 : at - 1);
+            copies_wait<S - 1>();
         }
 #pragma unroll
         for (int r = 0; r < R; ++r) {
             const int64_t row = base + r * step + ln.g;
-            zl[r] = lab[r] >= 0 && lab[r] < k ? to_f(z[row * ld + lab[r]]) : nan;
+            const uint32_t o = (uint32_t)(at * H::STAGE + r * H::ROW);
+            if constexpr (MODE != 2) lab[r] = (int)read4(slot4 + o);
+            else lab[r] = row < n ? labels[row] : -1;
+            zs.take(ln, row, slot + o, minus_infinity<T>(), zv[r]);
         }
+        at = at + 1 == S ? 0 : at + 1;
 #pragma unroll
         for (int r = 0; r < R; ++r) m[r] = row_max<T, MODE, EPL>(zv[r]);
         group_all<MaxOp, TPR, C>(m, sred, turn);
@@ -208,7 +236,7 @@ k_xent_rows(const T* z, int64_t ld, const int32_t* __restrict__ labels, int64_t 
             s[r] = a.x + a.y;
         }
         group_all<SumOp, TPR, C>(s, sred, turn);
-        if (!scaled) {                                        // the first rows are read while the labels are counted
+        if (!scaled) {                                        // the first rows are worked on while the labels are counted
             grid_ready();
             scale = loss_scale(sc, mean);
             scaled = true;
@@ -217,37 +245,45 @@ k_xent_rows(const T* z, int64_t ld, const int32_t* __restrict__ labels, int64_t 
         for (int r = 0; r < R; ++r) {
             const int64_t row = base + r * step + ln.g;
             if (row >= n) continue;
-            const bool known = lab[r] < k, empty = s[r] == 0.0f;
-            if (ln.l == 0) {
-                const float v = lab[r] < 0 ? 0.0f : !known ? nan : empty ? INFINITY : logf(s[r]) - (zl[r] - m[r]);
-                row_loss[row] = v;
-                sum += (double)v;
+            const bool counts = lab[r] >= 0, known = lab[r] < k, empty = s[r] == 0.0f;
+            const float q = !known ? nan : empty ? 0.0f : 1.0f / s[r];
+            // the label's element: its lane has the row's loss; lane 0 where there is no such element
+            const int v_hot = (lab[r] + (MODE == 1 ? ln.s : 0)) / N;
+            if (counts && known) {
+                if (v_hot % L::LANES == ln.l) {
+                    const int i_hot = (lab[r] + (MODE == 1 ? ln.s : 0)) % N, k_hot = v_hot / L::LANES;
+                    float z_hot = 0.0f;
+#pragma unroll
+                    for (int j = 0; j < EPL; ++j)
+                        if (j / N == k_hot && j % N == i_hot) {
+                            const float2 p = zv[r].pair(j / 2);
+                            z_hot = j & 1 ? p.y : p.x;
+                        }
+                    const float v = empty ? INFINITY : logf(s[r]) - (z_hot - m[r]);
+                    row_loss[row] = v;
+                    sum += (double)v;
+                }
+            } else if (ln.l == 0) {
+                row_loss[row] = counts ? nan : 0.0f;
+                if (counts) sum += (double)nan;
             }
             if (!dz) continue;
-            Row<T, MODE, EPL> o;
-            if (lab[r] < 0) o.zero();
+            if (!counts) zv[r].zero();
             else {
-                const float q = !known ? nan : empty ? 0.0f : 1.0f / s[r];
                 const float2 q2 = f2(q * scale);
-                const int hot = empty ? -N : lab[r];
 #pragma unroll
-                for (int p = 0; p < L::PAIRS; ++p) o.set_pair(p, __fmul2_rn(e2[r][p], q2));
-                // the label's element: (p - 1) s
+                for (int p = 0; p < L::PAIRS; ++p) zv[r].set_pair(p, __fmul2_rn(e2[r][p], q2));
+                if (known && !empty && v_hot % L::LANES == ln.l) {              // (p - 1) s
+                    const int i_hot = (lab[r] + (MODE == 1 ? ln.s : 0)) % N, k_hot = v_hot / L::LANES;
 #pragma unroll
-                for (int v = 0; v < L::NV; ++v) {
-                    const int at = hot - ln.first(v);
-                    if (at >= 0 && at < N) {
-#pragma unroll
-                        for (int i = 0; i < N; ++i)
-                            if (i == at) {
-                                const int j = v * N + i;
-                                const float one = ((j & 1 ? e2[r][j / 2].y : e2[r][j / 2].x) * q - 1.0f) * scale;
-                                if constexpr (MODE == 2) o.v[v].e = from_f<T>(one); else o.v[v].set(i, from_f<T>(one));
-                            }
-                    }
+                    for (int j = 0; j < EPL; ++j)
+                        if (j / N == k_hot && j % N == i_hot) {
+                            const T one = from_f<T>(((j & 1 ? e2[r][j / 2].y : e2[r][j / 2].x) * q - 1.0f) * scale);
+                            if constexpr (MODE == 2) zv[r].v[j].e = one; else zv[r].v[j / N].set(j % N, one);
+                        }
                 }
             }
-            o.store(ln, dz, row, ldd);
+            zv[r].store(ln, dz, row, ldd);
         }
     }
     if (!scaled) grid_ready();
@@ -285,11 +321,12 @@ extern "C" int gem_nlr_label_cross_entropy(const void* logits_dev, int32_t type,
     cudaError_t rc = cudaSuccess;
     by_mode(type, lie.mode, [&](auto t, auto mode) {
         using T = decltype(t);
-        const bool held = by_width<sizeof(T)>(lie.mode == 1 ? (int64_t)k + 16 / tb - 1 : k, [&](auto tpr, auto epl, auto c) {
+        const bool held = by_width<mode.value == 2 ? 4 : (int)sizeof(T), mode.value != 2 && sizeof(T) == 2 ? 32 : 16>(lie.mode == 1 ? (int64_t)k + 16 / tb - 1 : k, [&](auto tpr, auto epl, auto c) {
             constexpr auto kern = k_xent_rows<T, mode.value, tpr.value, epl.value, c.value>;
-            const int most = resident_clusters<kern, c.value>();
+            constexpr int shared = XentShape<T, mode.value, tpr.value, epl.value, c.value>::SHARED;
+            const int most = resident_clusters<kern, c.value>(shared);
             const int cl = spread(n, kRowBlock / tpr.value, xent_rows(epl.value), lie.period, most < kMaxBlocks / c.value ? most : kMaxBlocks / c.value);
-            rc = launch_rows(kern, cl * c.value, c.value, true, st, (const T*)logits_dev, ld, labels_dev, n, (int)k, (int)mean, sc, loss_dev,
+            rc = launch_rows(kern, cl * c.value, c.value, shared, true, st, (const T*)logits_dev, ld, labels_dev, n, (int)k, (int)mean, sc, loss_dev,
                              row_loss_dev, (T*)dlogits_dev, ld_d);
         });
         if (!held) {

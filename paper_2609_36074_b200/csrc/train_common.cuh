@@ -6,6 +6,7 @@
 #include <math.h>
 #include <stddef.h>
 #include <stdint.h>
+#include <atomic>
 #include <type_traits>
 #include "../../include/gem_nlr.h"
 #include "device_utils.cuh"
@@ -61,7 +62,7 @@ template <typename F> inline int by_type(int32_t type, F f)
     return f(__nv_bfloat16{});
 }
 
-constexpr int kTrainSMs = 148;
+constexpr int kTrainSMs = 148, kTrainDevices = 64;
 
 // Programmatic launches: the kernel before says that the next one may begin; that one waits for the kernel before to be
 // complete (every block of it has to, or the kernel after it might begin before the first one is done).

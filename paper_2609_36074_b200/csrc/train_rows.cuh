@@ -1,18 +1,20 @@
-// Rows of a matrix in registers: the layout that the layer norm and cross entropy kernels share.
+// Rows of a matrix, streamed: the layout that the layer norm and cross entropy kernels share.
 //
 // A row of d elements belongs to a group of TPR threads of a block (part of a warp, a warp, or several), or of C whole
-// blocks in a cluster; EPL elements to a thread, in vectors of N: vector v of lane l of the group's TPR C lanes holds
-// elements (v TPR C + l) N - s ... + N - 1, so that a group's loads are contiguous.  The row is read once and stays in
-// registers, in its own type, between the passes over it.
+// blocks in a cluster; EPL elements to a thread, in vectors of N: vector k of lane l of the group's LANES = TPR C lanes holds
+// elements (k LANES + l) N - s ... + N - 1, so that a group's loads are contiguous.  The row is read from HBM once.
 //
 // Three ways of reading a matrix (MODE):
 //   0  every row begins and ends at a multiple of 16 bytes: vectors of 16 bytes, s = 0
 //   1  rows begin anywhere: still vectors of 16 bytes at multiples of 16, beginning s elements before the row.  s depends on
-//      the row's number modulo 16 bytes / element only, and a group's rows are that far apart (see Spread), so a thread's
-//      columns are the same in all its rows.  The first and last vector hold elements of the neighbouring rows (or of the
-//      padding), which are replaced after loading and left alone in storing
+//      the row's number modulo 16 bytes / element only, and a group's rows are that far apart (see spread()), so a thread's
+//      columns are the same in all its rows.  The first and the last vector hold elements of the neighbouring rows (or of
+//      the padding), which are replaced after loading and left alone in storing
 //   2  element by element, where the matrices of one call lie differently to 16 bytes
-
+//
+// In modes 0 and 1 a thread's vectors come through a ring of stages in shared memory (asynchronous copies, S rows ahead):
+// registers alone hold too few bytes in flight for HBM.  Each thread copies the very vectors that it reads, so the ring
+// needs no barrier: its own copies' completion is all that a thread waits for.
 #pragma once
 #include "train_common.cuh"
 
@@ -87,19 +89,6 @@ struct Vec {
             w[i >> 1] = (i & 1) ? (w[i >> 1] & 0xffffu) | (h << 16) : (w[i >> 1] & 0xffff0000u) | h;
         }
     }
-    // elements outside [lo, hi) become those of the word x
-    __device__ __forceinline__ void keep(int lo, int hi, uint32_t x)
-    {
-        constexpr int E = 4 / (int)sizeof(T);
-#pragma unroll
-        for (int i = 0; i < VB / 4; ++i) {
-            uint32_t m = 0;
-#pragma unroll
-            for (int j = 0; j < E; ++j)
-                if (i * E + j >= lo && i * E + j < hi) m |= E == 1 ? 0xffffffffu : (0xffffu << (16 * j));
-            w[i] = (w[i] & m) | (x & ~m);
-        }
-    }
 };
 
 // ---- a thread's part of a row ------------------------------------------------------------------------------------
@@ -112,6 +101,25 @@ __device__ __forceinline__ void cluster_barrier()
     asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
 
+// 16 bytes from global to shared memory, asynchronously: the first `bytes` of them, zeros behind
+__device__ __forceinline__ void copy_ahead(uint32_t to, const void* from, int bytes)
+{
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(from), "r"(bytes) : "memory");
+}
+// 4 bytes, or a zero
+__device__ __forceinline__ void copy4_ahead(uint32_t to, const void* from, bool ok)
+{
+    asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(to), "l"(from), "r"(ok ? 4 : 0) : "memory");
+}
+__device__ __forceinline__ uint32_t read4(uint32_t at)
+{
+    uint32_t v;
+    asm volatile("ld.shared.b32 %0, [%1];" : "=r"(v) : "r"(at) : "memory");
+    return v;
+}
+__device__ __forceinline__ void copies_end() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int LEFT> __device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(LEFT) : "memory"); }
+
 template <typename T, int MODE, int TPR, int EPL, int C>
 struct Lane {
     static constexpr int N = MODE == 2 ? 1 : 16 / (int)sizeof(T);
@@ -121,26 +129,39 @@ struct Lane {
     static_assert(EPL % N == 0 && EPL % 2 == 0, "");
 
     int l, g, s, d;
-    __device__ __forceinline__ Lane(int d_) : g((int)threadIdx.x / TPR), s(0), d(d_)
+    int last;                                        // k of the row's last vector (of whichever lane)
+    uint32_t head[MODE == 1 ? 4 : 1], tail[MODE == 1 ? 4 : 1];   // the row's part of vector 0 and of vector `last`, as bits
+    __device__ __forceinline__ Lane(int d_, const T* base, int64_t ld) : g((int)threadIdx.x / TPR), s(0), d(d_)
     {
         l = (int)threadIdx.x % TPR;
         if constexpr (C > 1) l += (int)cluster_rank() * TPR;
+        if constexpr (MODE == 1) {
+            s = (int)((reinterpret_cast<uintptr_t>(base + group() * ld) & 15) / sizeof(T));
+            last = (s + d - 1) / N / LANES;
+#pragma unroll
+            for (int w = 0; w < 4; ++w) {
+                constexpr int E = 4 / (int)sizeof(T);
+                constexpr uint32_t ONE = E == 1 ? 0xffffffffu : 0xffffu;
+                head[w] = tail[w] = 0;
+#pragma unroll
+                for (int j = 0; j < E; ++j) {
+                    if (first(0) + w * E + j >= 0) head[w] |= ONE << (16 * j);
+                    if (first(last) + w * E + j < d) tail[w] |= ONE << (16 * j);
+                }
+            }
+        }
     }
     // number of the group among all groups of the grid, and their count
     __device__ __forceinline__ int64_t group() const { return (int64_t)(blockIdx.x / C) * GROUPS + g; }
     __device__ __forceinline__ int64_t first_group() const { return (int64_t)(blockIdx.x / C) * GROUPS; }
     __device__ __forceinline__ int64_t groups() const { return (int64_t)(gridDim.x / C) * GROUPS; }
-    // s of the group's rows
-    __device__ __forceinline__ void lie(const T* base, int64_t ld)
-    {
-        if constexpr (MODE == 1) s = (int)((reinterpret_cast<uintptr_t>(base + group() * ld) & 15) / sizeof(T));
-    }
-    __device__ __forceinline__ int first(int v) const { return (v * LANES + l) * N - (MODE == 1 ? s : 0); }
-    __device__ __forceinline__ bool any(int v) const { return first(v) < d; }
-    __device__ __forceinline__ bool full(int v) const { return MODE == 1 ? first(v) >= 0 && first(v) + N <= d : any(v); }
-    __device__ __forceinline__ bool holds(int v, int i) const { return MODE == 1 ? first(v) + i >= 0 && first(v) + i < d : any(v); }
+    __device__ __forceinline__ int first(int k) const { return (k * LANES + l) * N - (MODE == 1 ? s : 0); }
+    __device__ __forceinline__ bool any(int k) const { return first(k) < d; }
+    // whether vector k may be cut by an end of the row (the same for all lanes)
+    __device__ __forceinline__ bool end(int k) const { return MODE == 1 && (k == 0 || k == last); }
+    __device__ __forceinline__ bool full(int k) const { return MODE == 1 ? first(k) >= 0 && first(k) + N <= d : any(k); }
+    __device__ __forceinline__ bool holds(int k, int i) const { return MODE == 1 ? first(k) + i >= 0 && first(k) + i < d : any(k); }
 };
-
 
 // The thread's elements of one row.
 template <typename T, int MODE, int EPL>
@@ -150,36 +171,6 @@ struct Row {
     struct One { T e; };
     typename std::conditional<MODE == 2, One, V>::type v[NV];
 
-    // span: elements from the matrix's first to its last; what lies between them may be read.  `none` fills what is no
-    // element of the row.
-    template <typename LN>
-    __device__ __forceinline__ void load(const LN& ln, const T* base, int64_t row, int64_t ld, bool ok, int64_t span, uint32_t none)
-    {
-        const int64_t at = row * ld;
-#pragma unroll
-        for (int k = 0; k < NV; ++k) {
-            const int e = ln.first(k);
-            if constexpr (MODE == 2) {
-                const uint32_t n = none;
-                if (ok && ln.any(k)) v[k].e = base[at + e]; else v[k].e = *reinterpret_cast<const T*>(&n);
-            } else {
-                if (ok && ln.full(k)) v[k].load(base + at + e);
-                else {
-                    v[k].fill(none);
-                    if (MODE == 1 && ok && ln.any(k)) {
-                        if (at + e >= 0 && at + e + N <= span) {
-                            v[k].load(base + at + e);
-                            v[k].keep(-e, ln.d - e, none);
-                        } else {
-#pragma unroll
-                            for (int i = 0; i < N; ++i)
-                                if (ln.holds(k, i)) v[k].set(i, base[at + e + i]);
-                        }
-                    }
-                }
-            }
-        }
-    }
     template <typename LN>
     __device__ __forceinline__ void store(const LN& ln, T* base, int64_t row, int64_t ld) const
     {
@@ -189,9 +180,11 @@ struct Row {
             const int e = ln.first(k);
             if constexpr (MODE == 2) {
                 if (ln.any(k)) p[e] = v[k].e;
+            } else if (!ln.end(k)) {
+                if (ln.any(k)) v[k].store(p + e);
             } else {
                 if (ln.full(k)) v[k].store(p + e);
-                else if (MODE == 1 && ln.any(k)) {
+                else if (ln.any(k)) {
 #pragma unroll
                     for (int i = 0; i < N; ++i)
                         if (ln.holds(k, i)) p[e + i] = v[k].at(i);
@@ -214,6 +207,67 @@ struct Row {
 #pragma unroll
         for (int k = 0; k < NV; ++k)
             if constexpr (MODE == 2) v[k].e = from_f<T>(0.0f); else v[k].fill(0);
+    }
+};
+
+// A matrix that is read row by row.  `none`: what stands for elements outside the row (its bits in every element of a word).
+template <typename T, int MODE, int TPR, int EPL, int C>
+struct Source {
+    using L = Lane<T, MODE, TPR, EPL, C>;
+    static constexpr int N = L::N, NV = L::NV;
+    // bytes of a block's stage for one row
+    __host__ __device__ static constexpr int stage_bytes() { return MODE == 2 ? 0 : NV * 16 * kRowBlock; }
+    const T* base;
+    int64_t  ld, n, span;                            // span: elements from the matrix's first to its last
+    __device__ __forceinline__ Source(const T* p, int64_t ld_, int64_t n_, int d) : base(p), ld(ld_), n(n_), span((n_ - 1) * ld_ + d) {}
+
+    // Sends for the row; `slot` is the thread's place in the stage (vectors are kRowBlock places apart).
+    __device__ __forceinline__ void send(const L& ln, int64_t row, uint32_t slot) const
+    {
+        if constexpr (MODE != 2) {
+            const int64_t at = row * ld;
+#pragma unroll
+            for (int k = 0; k < NV; ++k) {
+                const int e = ln.first(k);
+                int bytes = row < n && ln.any(k) ? 16 : 0;
+                if (ln.end(k) && bytes) {            // what is not between the matrix's ends is not touched
+                    if (at + e < 0) bytes = 0;
+                    else if (at + e + N > span) bytes = (int)(span - (at + e)) * (int)sizeof(T);
+                }
+                copy_ahead(slot + (uint32_t)k * 16 * kRowBlock, bytes ? base + at + e : base - (MODE == 1 ? (int)((reinterpret_cast<uintptr_t>(base) & 15) / sizeof(T)) : 0), bytes);
+            }
+        }
+    }
+    // The row that was sent for, once its copies are complete.
+    __device__ __forceinline__ void take(const L& ln, int64_t row, uint32_t slot, uint32_t none, Row<T, MODE, EPL>& r) const
+    {
+        const int64_t at = row * ld;
+#pragma unroll
+        for (int k = 0; k < NV; ++k) {
+            const int e = ln.first(k);
+            if constexpr (MODE == 2) {
+                const uint32_t x = none;
+                if (row < n && ln.any(k)) r.v[k].e = base[at + e]; else r.v[k].e = *reinterpret_cast<const T*>(&x);
+            } else {
+                asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];"
+                             : "=r"(r.v[k].w[0]), "=r"(r.v[k].w[1]), "=r"(r.v[k].w[2]), "=r"(r.v[k].w[3])
+                             : "r"(slot + (uint32_t)k * 16 * kRowBlock) : "memory");
+                if (ln.end(k)) {
+                    if (at + e < 0 && row < n) {     // only where the matrix itself begins inside a vector
+#pragma unroll
+                        for (int i = 0; i < N; ++i)
+                            if (ln.holds(k, i)) r.v[k].set(i, base[at + e + i]);
+                    }
+#pragma unroll
+                    for (int w = 0; w < 4; ++w) {
+                        const uint32_t m = (k == 0 ? ln.head[w] : ~0u) & (k == ln.last ? ln.tail[w] : ~0u);
+                        r.v[k].w[w] = (r.v[k].w[w] & m) | (none & ~m);
+                    }
+                } else if (none != 0 && !ln.any(k)) {
+                    r.v[k].fill(none);
+                }
+            }
+        }
     }
 };
 
@@ -295,18 +349,22 @@ template <int C> __device__ __forceinline__ void leave_cluster() { if constexpr 
 template <int V> struct Const { static constexpr int value = V; };
 
 // f(TPR, EPL, C) as constants for rows of `width` elements of `bytes` bytes (the window's s included), false if it is wider
-// than eight blocks hold.  EPL is what 128 registers hold next to weights or sums: 24 elements of 2 bytes, 16 of 4.  Rows of
+// than eight blocks hold.  Few threads a row and many elements a thread keep the work per row (sums over the group, labels,
+// statistics) small; what bounds EPL are 128 registers next to weights and sums: 16 elements, 24 or WIDEST of 2 bytes.  Rows of
 // more than 4096 (6144) elements go to clusters of blocks, so that every SM still has two blocks, one of which loads
 // while the other adds.
-template <int BYTES, typename F>
+template <int BYTES, int WIDEST, typename F>
 bool by_width(int64_t width, F f)
 {
     constexpr int A = BYTES == 2 ? 16 : 12, B = BYTES == 2 ? 24 : 16;
-    if (width <= 64) f(Const<8>{}, Const<8>{}, Const<1>{});
+    if (width <= 16) f(Const<1>{}, Const<16>{}, Const<1>{});
+    else if (width <= 32) f(Const<2>{}, Const<16>{}, Const<1>{});
+    else if (width <= 64) f(Const<4>{}, Const<16>{}, Const<1>{});
     else if (width <= 128) f(Const<8>{}, Const<16>{}, Const<1>{});
     else if (width <= 256) f(Const<16>{}, Const<16>{}, Const<1>{});
     else if (width <= 512) f(Const<32>{}, Const<16>{}, Const<1>{});
-    else if (BYTES == 2 && width <= 768) f(Const<BYTES == 2 ? 32 : 64>{}, Const<BYTES == 2 ? 24 : A>{}, Const<1>{});
+    else if (WIDEST >= 24 && width <= 768) f(Const<32>{}, Const<WIDEST >= 24 ? 24 : 16>{}, Const<1>{});
+    else if (WIDEST >= 32 && width <= 1024) f(Const<32>{}, Const<WIDEST >= 32 ? 32 : 16>{}, Const<1>{});
     else if (width <= 64 * A) f(Const<64>{}, Const<A>{}, Const<1>{});
     else if (width <= 64 * B) f(Const<64>{}, Const<B>{}, Const<1>{});
     else if (width <= 128 * A) f(Const<128>{}, Const<A>{}, Const<1>{});
@@ -322,6 +380,9 @@ bool by_width(int64_t width, F f)
     else return false;
     return true;
 }
+
+// Stages of a ring whose stage takes `bytes`: up to four, within a half of an SM's shared memory (two blocks an SM).
+__host__ __device__ constexpr int ring_stages(int bytes) { return bytes == 0 ? 1 : 98304 / bytes < 2 ? 2 : 98304 / bytes > 4 ? 4 : 98304 / bytes; }
 
 // One matrix operand of a call.
 struct Matrix {
@@ -359,30 +420,35 @@ void by_mode(int32_t type, int mode, F f)
     });
 }
 
-// Groups of C blocks of kernel K that fit the GPU at once (looked up once).
+// Groups of C blocks of kernel K, with `shared` bytes of dynamic shared memory, that fit the current device at once (looked up
+// once a device, where the kernel is also allowed that much).
 template <auto K, int C>
-int resident_clusters()
+int resident_clusters(int shared)
 {
-    static const int found = [] {
-        int per = 0;
-        if constexpr (C == 1) {
-            if (cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per, K, kRowBlock, 0) != cudaSuccess || per < 1) per = 1;
-            return per * kTrainSMs;
-        } else {
-            cudaLaunchConfig_t cfg = {};
-            cfg.gridDim = dim3(C);
-            cfg.blockDim = dim3(kRowBlock);
-            cudaLaunchAttribute at = {};
-            at.id = cudaLaunchAttributeClusterDimension;
-            at.val.clusterDim.x = C;
-            at.val.clusterDim.y = at.val.clusterDim.z = 1;
-            cfg.attrs = &at;
-            cfg.numAttrs = 1;
-            if (cudaOccupancyMaxActiveClusters(&per, K, &cfg) != cudaSuccess || per < 1) { cudaGetLastError(); per = 1; }
-            return per;
-        }
-    }();
-    return found;
+    static std::atomic<int> found[kTrainDevices];
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= kTrainDevices) return 1;
+    int per = found[dev].load(std::memory_order_acquire);
+    if (per) return per;
+    if (shared > 0) cudaFuncSetAttribute(K, cudaFuncAttributeMaxDynamicSharedMemorySize, shared);
+    if constexpr (C == 1) {
+        if (cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per, K, kRowBlock, (size_t)shared) != cudaSuccess || per < 1) per = 1;
+        per *= kTrainSMs;
+    } else {
+        cudaLaunchConfig_t cfg = {};
+        cfg.gridDim = dim3(C);
+        cfg.blockDim = dim3(kRowBlock);
+        cfg.dynamicSmemBytes = (size_t)shared;
+        cudaLaunchAttribute at = {};
+        at.id = cudaLaunchAttributeClusterDimension;
+        at.val.clusterDim.x = C;
+        at.val.clusterDim.y = at.val.clusterDim.z = 1;
+        cfg.attrs = &at;
+        cfg.numAttrs = 1;
+        if (cudaOccupancyMaxActiveClusters(&per, K, &cfg) != cudaSuccess || per < 1) per = 1;
+    }
+    found[dev].store(per, std::memory_order_release);
+    return per;
 }
 
 // Clusters (or blocks) to launch for n rows, `at_once` of them handled by one at a time: no more than `most`, and a multiple
@@ -398,14 +464,15 @@ inline int spread(int64_t n, int groups, int at_once, int period, int64_t most)
     return (int)c;
 }
 
-// Launch of `blocks` blocks of kRowBlock threads in clusters of c; `early`: it may begin while the stream's last kernel ends
+// Launch of `blocks` blocks of kRowBlock threads with `shared` bytes of dynamic shared memory in clusters of c; `early`: it may begin while the stream's last kernel ends
 // (and waits for its results with grid_ready()).
 template <typename... P, typename... A>
-cudaError_t launch_rows(void (*k)(P...), int blocks, int c, bool early, cudaStream_t st, A... args)
+cudaError_t launch_rows(void (*k)(P...), int blocks, int c, int shared, bool early, cudaStream_t st, A... args)
 {
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)blocks);
     cfg.blockDim = dim3(kRowBlock);
+    cfg.dynamicSmemBytes = (size_t)shared;
     cfg.stream = st;
     cudaLaunchAttribute at[2] = {};
     int m = 0;
