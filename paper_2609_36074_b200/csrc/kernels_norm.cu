@@ -123,8 +123,10 @@ k_norm_rows(const T* __restrict__ x, int64_t ldx, const void* __restrict__ w, co
     using H = NormShape<T, MODE, TPR, EPL, C>;
     constexpr int R = H::ROWS, N = L::N, S = H::STAGES;
     extern __shared__ __align__(16) unsigned char ring[];
-    __shared__ float sred[group_floats(TPR, C, R)];
-    int turn = 0, at = 0;
+    __shared__ Join<TPR, C, R> jn;
+    uint32_t turn = 0;
+    int at = 0;
+    jn.begin();
     const L ln(d, x, ldx);
     const Source<T, MODE, TPR, EPL, C> xs(x, ldx, n, d);
     const uint32_t slot = (uint32_t)__cvta_generic_to_shared(ring) + threadIdx.x * 16;
@@ -157,7 +159,7 @@ k_norm_rows(const T* __restrict__ x, int64_t ldx, const void* __restrict__ w, co
             for (int q = 0; q < L::PAIRS; ++q) a = __fadd2_rn(a, xv[r].pair(q));
             s[r] = a.x + a.y;
         }
-        group_all<SumOp, TPR, C>(s, sred, turn);
+        group_all<SumOp, TPR, C>(s, jn, turn);
 #pragma unroll
         for (int r = 0; r < R; ++r) {
             mu[r] = s[r] * inv_d;
@@ -171,9 +173,12 @@ k_norm_rows(const T* __restrict__ x, int64_t ldx, const void* __restrict__ w, co
                     for (int i = 0; i < (MODE == 2 ? 1 : N / 2); ++i) {
                         const int q = MODE == 2 ? k : k * (N / 2) + i;
                         float2 c = __fadd2_rn(xv[r].pair(q), m2);
-                        if (cut) {
-                            if (!ln.holds(2 * q / N, 2 * q % N)) c.x = 0.0f;
-                            if (!ln.holds((2 * q + 1) / N, (2 * q + 1) % N)) c.y = 0.0f;
+                        if (MODE == 2) {
+                            if (!ln.any(2 * q)) c.x = 0.0f;
+                            if (!ln.any(2 * q + 1)) c.y = 0.0f;
+                        } else if (cut) {
+                            if (!(ln.bits(k) & (1u << 2 * i))) c.x = 0.0f;
+                            if (!(ln.bits(k) & (2u << 2 * i))) c.y = 0.0f;
                         }
                         a = __ffma2_rn(c, c, a);
                     }
@@ -181,7 +186,7 @@ k_norm_rows(const T* __restrict__ x, int64_t ldx, const void* __restrict__ w, co
             }
             s[r] = a.x + a.y;
         }
-        group_all<SumOp, TPR, C>(s, sred, turn);
+        group_all<SumOp, TPR, C>(s, jn, turn);
 #pragma unroll
         for (int r = 0; r < R; ++r) {
             const int64_t row = base + r * step + ln.g;
@@ -208,7 +213,7 @@ template <typename T, int MODE, int TPR, int EPL, int C>
 struct GradShape {
     using S0 = Source<T, MODE, TPR, EPL, C>;
     static constexpr int ROW = S0::stage_bytes(), STAGE = 2 * ROW + (MODE == 2 ? 0 : 2 * 4 * kRowBlock), STAGES = ring_stages(STAGE);
-    static constexpr int SUMS = kRowBlock / TPR > 1 ? kRowBlock * EPL * 4 : 0;       // the groups' sums, after the ring's last use
+    static constexpr int SUMS = kRowBlock * EPL * 4;                                 // the columns' sums, after the ring's last use
     static constexpr int SHARED = STAGE * STAGES > SUMS ? STAGE * STAGES : SUMS;
 };
 
@@ -223,8 +228,10 @@ k_norm_grad_rows(const T* __restrict__ dy, int64_t lddy, const T* __restrict__ x
     constexpr int N = L::N, S = H::STAGES;
     constexpr bool AGAIN = MODE != 2 && EPL > 16;    // the row is read from the ring a second time: its registers hold sums
     extern __shared__ __align__(16) unsigned char ring[];
-    __shared__ float sred[group_floats(TPR, C, 2)];
-    int turn = 0, at = 0;
+    __shared__ Join<TPR, C, 2> jn;
+    uint32_t turn = 0;
+    int at = 0;
+    jn.begin();
     const L ln(d, x, ldx);
     const Source<T, MODE, TPR, EPL, C> xs(x, ldx, n, d), gs(dy, lddy, n, d);
     const uint32_t ring0 = (uint32_t)__cvta_generic_to_shared(ring), slot = ring0 + threadIdx.x * 16, slot4 = ring0 + 2 * H::ROW + threadIdx.x * 4;
@@ -278,7 +285,7 @@ k_norm_grad_rows(const T* __restrict__ dy, int64_t lddy, const T* __restrict__ x
         }
         if (!dx) continue;
         float s[2] = {s0.x + s0.y, s1.x + s1.y};
-        group_all<SumOp, TPR, C>(s, sred, turn);
+        group_all<SumOp, TPR, C>(s, jn, turn);
         if (row < n) {
             const float2 c1 = f2(-s[0] * inv_d), c2 = f2(-s[1] * inv_d);
             if (AGAIN) {
@@ -299,41 +306,58 @@ k_norm_grad_rows(const T* __restrict__ dy, int64_t lddy, const T* __restrict__ x
     copies_wait<0>();
     float* rec = part + (size_t)(blockIdx.x / C) * 2 * d;
     float* sums = reinterpret_cast<float*>(ring);
+    if constexpr (L::GROUPS == 1) {
+        // one group: through shared memory only to store neighbouring columns together
+        const int s0 = MODE == 1 ? ln.s : 0, rank = C > 1 ? (int)cluster_rank() : 0;
+#pragma unroll
+        for (int which = 0; which < 2; ++which) {
+            __syncthreads();
+#pragma unroll
+            for (int q = 0; q < L::PAIRS; ++q) {
+                const int p = 2 * q / N * (kRowBlock * N) + (int)threadIdx.x * N + 2 * q % N;
+                const float2 a = which ? ab[q] : aw[q];
+                if constexpr (N > 1) *reinterpret_cast<float2*>(sums + p) = a;
+                else { sums[p] = a.x; sums[p + kRowBlock] = a.y; }
+            }
+            __syncthreads();
+            for (int p = threadIdx.x; p < kRowBlock * EPL; p += kRowBlock) {
+                const int e = (p / (kRowBlock * N) * C + rank) * (kRowBlock * N) + p % (kRowBlock * N) - s0;
+                if (e >= 0 && e < d) rec[which * d + e] = sums[p];
+            }
+        }
+        return;
+    }
     constexpr int W = TPR * EPL;                     // places of a group in `sums`
 #pragma unroll
     for (int which = 0; which < 2; ++which) {
-        if constexpr (L::GROUPS > 1) __syncthreads();
+        __syncthreads();
 #pragma unroll
         for (int q = 0; q < L::PAIRS; ++q)
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
                 const int k = (2 * q + h) / N, i = (2 * q + h) % N;
-                if (ln.holds(k, i)) {
-                    const float2 a = which ? ab[q] : aw[q];
-                    (L::GROUPS > 1 ? sums + ln.g * W : rec + which * d)[ln.first(k) + i] = h ? a.y : a.x;
-                }
+                const float2 a = which ? ab[q] : aw[q];
+                if (ln.holds(k, i)) sums[ln.g * W + ln.first(k) + i] = h ? a.y : a.x;
             }
-        if constexpr (L::GROUPS > 1) {
-            // in two steps where a row is narrower than the block: its threads share a column's groups
-            constexpr int SPLIT = W < kRowBlock ? kRowBlock / W : 1, EACH = L::GROUPS / SPLIT;
+        // in two steps where a row is narrower than the block: its threads share a column's groups
+        constexpr int SPLIT = W < kRowBlock ? kRowBlock / W : 1, EACH = L::GROUPS / SPLIT;
+        __syncthreads();
+        for (int e = threadIdx.x % W; e < W; e += kRowBlock) {
+            const int q0 = SPLIT > 1 ? (int)threadIdx.x / W * EACH : 0;
+            float t = 0.0f;
+            if (e < d)
+#pragma unroll
+                for (int q = 0; q < EACH; ++q) t += sums[(q0 + q) * W + e];
+            if constexpr (SPLIT > 1) sums[q0 * W + e] = t;               // (only this thread reads that place)
+            else if (e < d) rec[which * d + e] = t;
+        }
+        if constexpr (SPLIT > 1) {
             __syncthreads();
-            for (int e = threadIdx.x % W; e < W; e += kRowBlock) {
-                const int q0 = SPLIT > 1 ? (int)threadIdx.x / W * EACH : 0;
+            if ((int)threadIdx.x < d) {
                 float t = 0.0f;
-                if (e < d)
 #pragma unroll
-                    for (int q = 0; q < EACH; ++q) t += sums[(q0 + q) * W + e];
-                if constexpr (SPLIT > 1) sums[q0 * W + e] = t;           // (only this thread reads that place)
-                else if (e < d) rec[which * d + e] = t;
-            }
-            if constexpr (SPLIT > 1) {
-                __syncthreads();
-                if ((int)threadIdx.x < d) {
-                    float t = 0.0f;
-#pragma unroll
-                    for (int q = 0; q < SPLIT; ++q) t += sums[q * EACH * W + threadIdx.x];
-                    rec[which * d + threadIdx.x] = t;
-                }
+                for (int q = 0; q < SPLIT; ++q) t += sums[q * EACH * W + threadIdx.x];
+                rec[which * d + threadIdx.x] = t;
             }
         }
     }
@@ -450,7 +474,7 @@ extern "C" int gem_nlr_layer_norm_backward(const void* dy_dev, int64_t ld_dy, co
     if (n > 0)
         by_mode(type, lie.mode, [&](auto t, auto mode) {
             using T = decltype(t);
-            held = by_width<mode.value == 2 ? 4 : (int)sizeof(T), mode.value != 2 && sizeof(T) == 2 ? 24 : 16>(lie.mode == 1 ? (int64_t)d + 16 / tb - 1 : d, [&](auto tpr, auto epl, auto c) {
+            held = by_width<mode.value == 2 ? 4 : (int)sizeof(T), mode.value == 0 && sizeof(T) == 2 ? 24 : 16>(lie.mode == 1 ? (int64_t)d + 16 / tb - 1 : d, [&](auto tpr, auto epl, auto c) {
                 constexpr auto k = k_norm_grad_rows<T, mode.value, tpr.value, epl.value, c.value>;
                 constexpr int shared = GradShape<T, mode.value, tpr.value, epl.value, c.value>::SHARED;
                 const int most = resident_clusters<k, c.value>(shared), room = norm_records(n, d);

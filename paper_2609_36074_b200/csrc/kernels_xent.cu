@@ -175,8 +175,10 @@ k_xent_rows(const T* z, int64_t ld, const int32_t* __restrict__ labels, int64_t 
     constexpr int N = L::N, R = H::ROWS, S = H::STAGES;
     constexpr float kLog2e = 1.4426950408889634f;
     extern __shared__ __align__(16) unsigned char ring[];
-    __shared__ float sred[group_floats(TPR, C, R)];
-    int turn = 0, at = 0;
+    __shared__ Join<TPR, C, R> jn;
+    uint32_t turn = 0;
+    int at = 0;
+    jn.begin();
     const L ln(k, z, ld);
     const Source<T, MODE, TPR, EPL, C> zs(z, ld, n, k);
     const uint32_t ring0 = (uint32_t)__cvta_generic_to_shared(ring), slot = ring0 + threadIdx.x * 16,
@@ -217,10 +219,9 @@ k_xent_rows(const T* z, int64_t ld, const int32_t* __restrict__ labels, int64_t 
             else lab[r] = row < n ? labels[row] : -1;
             zs.take(ln, row, slot + o, minus_infinity<T>(), zv[r]);
         }
-        at = at + 1 == S ? 0 : at + 1;
 #pragma unroll
         for (int r = 0; r < R; ++r) m[r] = row_max<T, MODE, EPL>(zv[r]);
-        group_all<MaxOp, TPR, C>(m, sred, turn);
+        group_all<MaxOp, TPR, C>(m, jn, turn);
         float2 e2[R][L::PAIRS];
 #pragma unroll
         for (int r = 0; r < R; ++r) {
@@ -235,7 +236,7 @@ k_xent_rows(const T* z, int64_t ld, const int32_t* __restrict__ labels, int64_t 
             }
             s[r] = a.x + a.y;
         }
-        group_all<SumOp, TPR, C>(s, sred, turn);
+        group_all<SumOp, TPR, C>(s, jn, turn);
         if (!scaled) {                                        // the first rows are worked on while the labels are counted
             grid_ready();
             scale = loss_scale(sc, mean);
@@ -247,25 +248,26 @@ k_xent_rows(const T* z, int64_t ld, const int32_t* __restrict__ labels, int64_t 
             if (row >= n) continue;
             const bool counts = lab[r] >= 0, known = lab[r] < k, empty = s[r] == 0.0f;
             const float q = !known ? nan : empty ? 0.0f : 1.0f / s[r];
-            // the label's element: its lane has the row's loss; lane 0 where there is no such element
-            const int v_hot = (lab[r] + (MODE == 1 ? ln.s : 0)) / N;
-            if (counts && known) {
-                if (v_hot % L::LANES == ln.l) {
-                    const int i_hot = (lab[r] + (MODE == 1 ? ln.s : 0)) % N, k_hot = v_hot / L::LANES;
-                    float z_hot = 0.0f;
-#pragma unroll
-                    for (int j = 0; j < EPL; ++j)
-                        if (j / N == k_hot && j % N == i_hot) {
-                            const float2 p = zv[r].pair(j / 2);
-                            z_hot = j & 1 ? p.y : p.x;
-                        }
-                    const float v = empty ? INFINITY : logf(s[r]) - (z_hot - m[r]);
-                    row_loss[row] = v;
-                    sum += (double)v;
+            // the label's element: its thread has the row's loss and its gradient (p - 1) s; lane 0 where there is none
+            const int hot = lab[r] + (MODE == 1 ? ln.s : 0), v_hot = hot / N;
+            const bool mine = counts && known ? v_hot % L::LANES == ln.l : ln.l == 0;
+            T one;
+            if (mine) {
+                float v = counts ? nan : 0.0f;
+                if (counts && known) {
+                    float z_hot;
+                    if constexpr (MODE == 2) z_hot = to_f(z[row * ld + lab[r]]);
+                    else {
+                        // (the matrix's own first and last vectors may not have come through the ring whole)
+                        const uint32_t o = (uint32_t)(at * H::STAGE + r * H::ROW + v_hot / L::LANES * 16 * kRowBlock) + threadIdx.x * 16;
+                        z_hot = MODE == 1 && row == 0 ? to_f(z[lab[r]]) : to_f(reinterpret_cast<const T*>(ring + o)[hot % N]);
+                    }
+                    const float t = z_hot - m[r];
+                    v = empty ? INFINITY : logf(s[r]) - t;
+                    one = from_f<T>(empty ? 0.0f : (exp2_fast(t * kLog2e) * q - 1.0f) * scale);
                 }
-            } else if (ln.l == 0) {
-                row_loss[row] = counts ? nan : 0.0f;
-                if (counts) sum += (double)nan;
+                row_loss[row] = v;
+                sum += (double)v;
             }
             if (!dz) continue;
             if (!counts) zv[r].zero();
@@ -273,18 +275,11 @@ k_xent_rows(const T* z, int64_t ld, const int32_t* __restrict__ labels, int64_t 
                 const float2 q2 = f2(q * scale);
 #pragma unroll
                 for (int p = 0; p < L::PAIRS; ++p) zv[r].set_pair(p, __fmul2_rn(e2[r][p], q2));
-                if (known && !empty && v_hot % L::LANES == ln.l) {              // (p - 1) s
-                    const int i_hot = (lab[r] + (MODE == 1 ? ln.s : 0)) % N, k_hot = v_hot / L::LANES;
-#pragma unroll
-                    for (int j = 0; j < EPL; ++j)
-                        if (j / N == k_hot && j % N == i_hot) {
-                            const T one = from_f<T>(((j & 1 ? e2[r][j / 2].y : e2[r][j / 2].x) * q - 1.0f) * scale);
-                            if constexpr (MODE == 2) zv[r].v[j].e = one; else zv[r].v[j / N].set(j % N, one);
-                        }
-                }
             }
             zv[r].store(ln, dz, row, ldd);
+            if (mine && counts && known) dz[row * ldd + lab[r]] = one;
         }
+        at = at + 1 == S ? 0 : at + 1;
     }
     if (!scaled) grid_ready();
     leave_cluster<C>();

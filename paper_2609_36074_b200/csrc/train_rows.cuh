@@ -130,7 +130,8 @@ struct Lane {
 
     int l, g, s, d;
     int last;                                        // k of the row's last vector (of whichever lane)
-    uint32_t head[MODE == 1 ? 4 : 1], tail[MODE == 1 ? 4 : 1];   // the row's part of vector 0 and of vector `last`, as bits
+    uint32_t head[MODE == 1 ? 4 : 1], tail[MODE == 1 ? 4 : 1];   // the row's part of vector 0 and of vector `last`, as words
+    uint32_t head_bits, tail_bits;                               // and as a bit an element
     __device__ __forceinline__ Lane(int d_, const T* base, int64_t ld) : g((int)threadIdx.x / TPR), s(0), d(d_)
     {
         l = (int)threadIdx.x % TPR;
@@ -138,6 +139,13 @@ struct Lane {
         if constexpr (MODE == 1) {
             s = (int)((reinterpret_cast<uintptr_t>(base + group() * ld) & 15) / sizeof(T));
             last = (s + d - 1) / N / LANES;
+            head_bits = tail_bits = 0;
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                if (first(0) + i >= 0) head_bits |= 1u << i;
+                if (first(last) + i < d) tail_bits |= 1u << i;
+            }
+            if (last == 0) head_bits = tail_bits = head_bits & tail_bits;
 #pragma unroll
             for (int w = 0; w < 4; ++w) {
                 constexpr int E = 4 / (int)sizeof(T);
@@ -159,7 +167,7 @@ struct Lane {
     __device__ __forceinline__ bool any(int k) const { return first(k) < d; }
     // whether vector k may be cut by an end of the row (the same for all lanes)
     __device__ __forceinline__ bool end(int k) const { return MODE == 1 && (k == 0 || k == last); }
-    __device__ __forceinline__ bool full(int k) const { return MODE == 1 ? first(k) >= 0 && first(k) + N <= d : any(k); }
+    __device__ __forceinline__ uint32_t bits(int k) const { return k == 0 ? head_bits : tail_bits; }      // where end(k)
     __device__ __forceinline__ bool holds(int k, int i) const { return MODE == 1 ? first(k) + i >= 0 && first(k) + i < d : any(k); }
 };
 
@@ -183,11 +191,12 @@ struct Row {
             } else if (!ln.end(k)) {
                 if (ln.any(k)) v[k].store(p + e);
             } else {
-                if (ln.full(k)) v[k].store(p + e);
-                else if (ln.any(k)) {
+                const uint32_t b = ln.bits(k);
+                if (b == (1u << N) - 1) v[k].store(p + e);
+                else if (b) {
 #pragma unroll
                     for (int i = 0; i < N; ++i)
-                        if (ln.holds(k, i)) p[e + i] = v[k].at(i);
+                        if (b & (1u << i)) p[e + i] = v[k].at(i);
                 }
             }
         }
@@ -292,36 +301,87 @@ __device__ __forceinline__ void load_weights(const LN& ln, const void* w, int wt
 struct SumOp { __device__ __forceinline__ static float of(float a, float b) { return a + b; } };
 struct MaxOp { __device__ __forceinline__ static float of(float a, float b) { return fmaxf(a, b); } };
 
-// Floats of shared memory that group_all needs for R values at a time.
-__host__ __device__ constexpr int group_floats(int tpr, int c, int r) { return tpr <= 32 ? 1 : 2 * r * c * kRowBlock / 32; }
+// Shared memory of group_all for R values at a time: two halves of a value for every warp of a group (or cluster).
+template <int TPR, int C, int R>
+struct Join {
+    static constexpr int W = TPR > 32 ? TPR / 32 * C : 1;        // values to join: one a warp
+    float    v[TPR <= 32 ? 1 : 2 * R * C * kRowBlock / 32];
+    uint64_t bar[C > 1 ? 2 : 1];                                 // the halves' arrivals from the cluster's blocks
+    uint32_t late;                                               // a wait has run out: no wait after it, sums are NaN
+    __device__ __forceinline__ void arm(int half)
+    {
+        asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"((uint32_t)__cvta_generic_to_shared(&bar[half])),
+                     "r"((uint32_t)(W * R * sizeof(float))) : "memory");
+    }
+    // before the first group_all, by all threads
+    __device__ __forceinline__ void begin()
+    {
+        if constexpr (C > 1) {
+            if (threadIdx.x == 0) {
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+                    asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" ::"r"((uint32_t)__cvta_generic_to_shared(&bar[h])) : "memory");
+                asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+                late = 0;
+                arm(0);
+                arm(1);
+            }
+            __syncwarp();
+            cluster_barrier();
+        }
+    }
+};
 
-// Sums (or maxima) of R values over a group; every thread gets the same bits.  Where a group is more than a warp, its warps
-// write theirs to shared memory (of every block of the cluster) and meet at the group's barrier; `turn` alternates between
-// the halves of `buf`, so that one barrier a call is enough: a thread that writes a half has passed the barrier that
-// followed every thread's last reads of it.
+// Polls of one wait.  A healthy one ends within microseconds; one that runs out leaves NaN in its row's results and every
+// later wait of the block returns at once, so that the kernel ends whatever has happened.
+constexpr uint32_t kJoinPolls = 1u << 20;
+
+__device__ __forceinline__ bool join_wait(uint64_t* bar, uint32_t parity, volatile uint32_t* late)
+{
+    const uint32_t b = (uint32_t)__cvta_generic_to_shared(bar);
+    for (uint32_t i = 0; i < kJoinPolls; ++i) {
+        uint32_t ok;
+        asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+                     : "=r"(ok) : "r"(b), "r"(parity) : "memory");
+        if (ok) return true;
+        if ((i & 63u) == 63u && *late) return false;
+    }
+    *late = 1;
+    return false;
+}
+
+// Sums (or maxima) of R values over a group; every thread gets the same bits.  `turn` counts the calls.
+// Where a group is more than a warp, its warps write their values to shared memory and meet at the group's barrier.  In a
+// cluster every warp sends its values to every block, and a thread waits until its block has all of them; no block waits for
+// a barrier of the cluster, whose release would wait for the rows' stores too.  Both use the halves of the buffer in turn:
+// whoever writes a half has seen, in the call between, values that every warp sent after its last reads of that half.
 template <typename Op, int TPR, int C, int R>
-__device__ __forceinline__ void group_all(float (&v)[R], float* buf, int& turn)
+__device__ __forceinline__ void group_all(float (&v)[R], Join<TPR, C, R>& jn, uint32_t& turn)
 {
 #pragma unroll
     for (int o = (TPR < 32 ? TPR : 32) / 2; o > 0; o >>= 1)
 #pragma unroll
         for (int r = 0; r < R; ++r) v[r] = Op::of(v[r], __shfl_xor_sync(0xffffffffu, v[r], o));
     if constexpr (TPR > 32) {
-        constexpr int W = TPR / 32 * C;              // values to join: one a warp
-        const int g = threadIdx.x / TPR, warp = (threadIdx.x % TPR) >> 5, l = threadIdx.x & 31;
-        float* b = buf + (g * 2 + turn) * R * W;
-        turn ^= 1;
+        constexpr int W = Join<TPR, C, R>::W;
+        const int g = threadIdx.x / TPR, warp = (threadIdx.x % TPR) >> 5, l = threadIdx.x & 31, half = turn & 1;
+        float* b = jn.v + (g * 2 + half) * R * W;
+        bool here = true;
         if constexpr (C > 1) {
             if (l < C) {
-                const uint32_t here = (uint32_t)__cvta_generic_to_shared(b + cluster_rank() * (TPR / 32) + warp);
-                uint32_t there;
-                asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(there) : "r"(here), "r"(l));
+                const uint32_t mine = (uint32_t)__cvta_generic_to_shared(b + cluster_rank() * (TPR / 32) + warp);
+                const uint32_t bar = (uint32_t)__cvta_generic_to_shared(&jn.bar[half]);
+                uint32_t there, there_bar;
+                asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(there) : "r"(mine), "r"(l));
+                asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(there_bar) : "r"(bar), "r"(l));
 #pragma unroll
                 for (int r = 0; r < R; ++r)
-                    asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(there + (uint32_t)(r * W * sizeof(float))), "f"(v[r]) : "memory");
+                    asm volatile("st.async.shared::cluster.mbarrier::complete_tx::bytes.b32 [%0], %1, [%2];"
+                                 ::"r"(there + (uint32_t)(r * W * sizeof(float))), "r"(__float_as_uint(v[r])), "r"(there_bar) : "memory");
             }
             __syncwarp();
-            cluster_barrier();
+            here = join_wait(&jn.bar[half], (turn >> 1) & 1, &jn.late);
+            if (threadIdx.x == 0) jn.arm(half);      // for the call after the next
         } else {
             if (l == 0)
 #pragma unroll
@@ -329,6 +389,7 @@ __device__ __forceinline__ void group_all(float (&v)[R], float* buf, int& turn)
             if constexpr (TPR == kRowBlock) __syncthreads();
             else asm volatile("bar.sync %0, %1;" ::"r"(g + 1), "n"(TPR) : "memory");
         }
+        ++turn;
         // a warp's lanes take the warps' values and join them, instead of every thread reading all of them
 #pragma unroll
         for (int r = 0; r < R; ++r) {
@@ -336,7 +397,7 @@ __device__ __forceinline__ void group_all(float (&v)[R], float* buf, int& turn)
             if constexpr (W == 64) t = Op::of(t, b[r * W + 32 + l]);
 #pragma unroll
             for (int o = (W < 32 ? W : 32) / 2; o > 0; o >>= 1) t = Op::of(t, __shfl_xor_sync(0xffffffffu, t, o));
-            v[r] = t;
+            v[r] = here ? t : __int_as_float(0x7fffffff);
         }
     }
 }
@@ -356,7 +417,7 @@ template <int V> struct Const { static constexpr int value = V; };
 template <int BYTES, int WIDEST, typename F>
 bool by_width(int64_t width, F f)
 {
-    constexpr int A = BYTES == 2 ? 16 : 12, B = BYTES == 2 ? 24 : 16;
+    constexpr int A = BYTES == 2 ? 16 : 12, B = BYTES == 2 && WIDEST >= 24 ? 24 : 16;
     if (width <= 16) f(Const<1>{}, Const<16>{}, Const<1>{});
     else if (width <= 32) f(Const<2>{}, Const<16>{}, Const<1>{});
     else if (width <= 64) f(Const<4>{}, Const<16>{}, Const<1>{});
