@@ -105,13 +105,13 @@ k_norm_dw_sum(const float* __restrict__ part, int records, int d, W* __restrict_
 
 // ---- streamed rows -----------------------------------------------------------------------------------------------
 
-// Rows that a group works on at a time: two of a few vectors, so that their sums over the group run side by side.
-__host__ __device__ constexpr int fwd_rows(int epl) { return epl <= 16 ? 2 : 1; }
+// Rows that a group works on at a time: two of the narrow ones, so that their sums over the group run side by side.
+__host__ __device__ constexpr int fwd_rows(int tpr) { return tpr < 32 ? 2 : 1; }
 
 template <typename T, int MODE, int TPR, int EPL, int C>
 struct NormShape {
     using S0 = Source<T, MODE, TPR, EPL, C>;
-    static constexpr int ROWS = fwd_rows(EPL), STAGE = ROWS * S0::stage_bytes(), STAGES = ring_stages(STAGE), SHARED = STAGE * STAGES;
+    static constexpr int ROWS = fwd_rows(TPR), ROW = S0::stage_bytes(), STAGE = ROWS * ROW, STAGES = ring_stages(STAGE), SHARED = STAGE * STAGES;
 };
 
 template <typename T, int MODE, int TPR, int EPL, int C>
@@ -122,44 +122,64 @@ k_norm_rows(const T* __restrict__ x, int64_t ldx, const void* __restrict__ w, co
     using L = Lane<T, MODE, TPR, EPL, C>;
     using H = NormShape<T, MODE, TPR, EPL, C>;
     constexpr int R = H::ROWS, N = L::N, S = H::STAGES;
-    extern __shared__ __align__(16) unsigned char ring[];
-    __shared__ Join<TPR, C, R> jn;
-    uint32_t turn = 0;
+    extern __shared__ __align__(128) unsigned char ring[];
+    __shared__ Join<L, TPR, C, R, S> jn;
+    __shared__ Edges<L> ed;
+    uint32_t turn = 0, phase = 0;
     int at = 0;
     jn.begin();
-    const L ln(d, x, ldx);
+    const L ln(d, x, ldx, ldy);
     const Source<T, MODE, TPR, EPL, C> xs(x, ldx, n, d);
-    const uint32_t slot = (uint32_t)__cvta_generic_to_shared(ring) + threadIdx.x * 16;
+    const uint32_t ring0 = (uint32_t)__cvta_generic_to_shared(ring);
+    const bool lead = L::BULK && (int)threadIdx.x % TPR == 0;
     const float inv_d = 1.0f / (float)d;
     const int64_t step = ln.groups();
+    // the rows of the iteration that begins at `base`
     const auto send = [&](int64_t base, int stage) {
-        if (base < n)
+        if constexpr (L::BULK) {
+            const int64_t row = base + ln.g;
+            if (lead && row < n) {
+                int64_t from;
+                const uint32_t bytes = xs.window(ln, row, from), bar = jn.stage(ln, stage);
+                expect_bytes(bar, bytes);
+                xs.send_bulk(ln, row, from, bytes, ring0 + (uint32_t)(stage * H::STAGE), bar);
+            }
+        } else if constexpr (MODE != 2) {
+            if (base < n)
 #pragma unroll
-            for (int r = 0; r < R; ++r) xs.send(ln, base + r * step + ln.g, slot + (uint32_t)(stage * H::STAGE + r * H::S0::stage_bytes()));
-        copies_end();
+                for (int r = 0; r < R; ++r) xs.send_own(ln, base + r * step + ln.g, ring0 + (uint32_t)(stage * H::STAGE + r * H::ROW));
+            copies_end();
+        }
     };
+    for (int i = 0; i < S; ++i) {
 #pragma unroll
-    for (int i = 0; i < S - 1; ++i) send(ln.first_group() + i * R * step, i);
+        for (int r = 0; r < R; ++r) xs.prepare(ln, ring0 + (uint32_t)(i * H::STAGE + r * H::ROW), 0u);
+        if (L::BULK || i < S - 1) send(ln.first_group() + i * R * step, i);
+    }
     float2 w2[L::PAIRS], b2[L::PAIRS];
     load_weights<T>(ln, w, wtype, 1.0f, w2);
     load_weights<T>(ln, b, wtype, 0.0f, b2);
     for (int64_t base = ln.first_group(); base < n; base += R * step) {
-        send(base + (S - 1) * R * step, at == 0 ? S - 1 : at - 1);
-        copies_wait<S - 1>();
         Row<T, MODE, EPL> xv[R];
         float s[R], mu[R];
-#pragma unroll
-        for (int r = 0; r < R; ++r)
-            xs.take(ln, base + r * step + ln.g, slot + (uint32_t)(at * H::STAGE + r * H::S0::stage_bytes()), 0u, xv[r]);
-        at = at + 1 == S ? 0 : at + 1;
+        bool here = true;
+        if constexpr (L::BULK) {
+            if (base + ln.g < n) here = wait_for(jn.stage(ln, at), phase, &jn.late);
+        } else if constexpr (MODE != 2) {
+            send(base + (S - 1) * R * step, at == 0 ? S - 1 : at - 1);
+            copies_wait<S - 1>();
+        }
 #pragma unroll
         for (int r = 0; r < R; ++r) {
-            float2 a = f2(0.0f);
+            xs.take(ln, base + r * step + ln.g, ring0 + (uint32_t)(at * H::STAGE + r * H::ROW), 0u, xv[r]);
+            float2 a = f2(here ? 0.0f : __int_as_float(0x7fffffff));
 #pragma unroll
             for (int q = 0; q < L::PAIRS; ++q) a = __fadd2_rn(a, xv[r].pair(q));
             s[r] = a.x + a.y;
         }
         group_all<SumOp, TPR, C>(s, jn, turn);
+        if constexpr (L::BULK) send(base + S * step, at);        // every thread of the group has its part of the row
+        if (++at == S) { at = 0; phase ^= 1; }
 #pragma unroll
         for (int r = 0; r < R; ++r) {
             mu[r] = s[r] * inv_d;
@@ -191,16 +211,14 @@ k_norm_rows(const T* __restrict__ x, int64_t ldx, const void* __restrict__ w, co
         for (int r = 0; r < R; ++r) {
             const int64_t row = base + r * step + ln.g;
             const float rs = 1.0f / sqrtf(s[r] * inv_d + eps);
-            if (row < n) {
-                const float2 m2 = f2(-mu[r]), r2 = f2(rs);
+            const float2 m2 = f2(-mu[r]), r2 = f2(rs);
 #pragma unroll
-                for (int q = 0; q < L::PAIRS; ++q)
-                    xv[r].set_pair(q, __ffma2_rn(__fmul2_rn(__fadd2_rn(xv[r].pair(q), m2), r2), w2[q], b2[q]));
-                xv[r].store(ln, y, row, ldy);
-                if (ln.l == 0) {
-                    if (mean) mean[row] = mu[r];
-                    if (rstd) rstd[row] = rs;
-                }
+            for (int q = 0; q < L::PAIRS; ++q)
+                xv[r].set_pair(q, __ffma2_rn(__fmul2_rn(__fadd2_rn(xv[r].pair(q), m2), r2), w2[q], b2[q]));
+            xv[r].store(ln, y, row, ldy, row < n, n, ed);
+            if (ln.l == 0 && ln.rank == 0 && row < n) {
+                if (mean) mean[row] = mu[r];
+                if (rstd) rstd[row] = rs;
             }
         }
     }
@@ -208,11 +226,12 @@ k_norm_rows(const T* __restrict__ x, int64_t ldx, const void* __restrict__ w, co
 }
 
 // The gradient.  Every thread keeps its columns' sums of dy h and dy over the rows that it sees (FP32), the block joins its
-// groups' sums and writes one record; k_norm_dw_join adds the records.  A row's mean and rstd come through the ring too.
+// groups' sums and writes one record; k_norm_dw_join adds the records.  A row's mean and rstd are read a row ahead.
 template <typename T, int MODE, int TPR, int EPL, int C>
 struct GradShape {
     using S0 = Source<T, MODE, TPR, EPL, C>;
-    static constexpr int ROW = S0::stage_bytes(), STAGE = 2 * ROW + (MODE == 2 ? 0 : 2 * 4 * kRowBlock), STAGES = ring_stages(STAGE);
+    static constexpr bool OWN = MODE != 2 && TPR < 32;
+    static constexpr int ROW = S0::stage_bytes(), STAGE = 2 * ROW + (OWN ? 2 * 4 * kRowBlock : 0), STAGES = ring_stages(STAGE);
     static constexpr int SUMS = kRowBlock * EPL * 4;                                 // the columns' sums, after the ring's last use
     static constexpr int SHARED = STAGE * STAGES > SUMS ? STAGE * STAGES : SUMS;
 };
@@ -226,55 +245,70 @@ k_norm_grad_rows(const T* __restrict__ dy, int64_t lddy, const T* __restrict__ x
     using L = Lane<T, MODE, TPR, EPL, C>;
     using H = GradShape<T, MODE, TPR, EPL, C>;
     constexpr int N = L::N, S = H::STAGES;
-    constexpr bool AGAIN = MODE != 2 && EPL > 16;    // the row is read from the ring a second time: its registers hold sums
-    extern __shared__ __align__(16) unsigned char ring[];
-    __shared__ Join<TPR, C, 2> jn;
-    uint32_t turn = 0;
+    constexpr bool AGAIN = L::BULK && EPL > 16;      // the row is read from the ring a second time: its registers hold sums
+    extern __shared__ __align__(128) unsigned char ring[];
+    __shared__ Join<L, TPR, C, 2, S> jn;
+    __shared__ Edges<L> ed;
+    uint32_t turn = 0, phase = 0;
     int at = 0;
     jn.begin();
-    const L ln(d, x, ldx);
+    const L ln(d, x, ldx, lddx);
     const Source<T, MODE, TPR, EPL, C> xs(x, ldx, n, d), gs(dy, lddy, n, d);
-    const uint32_t ring0 = (uint32_t)__cvta_generic_to_shared(ring), slot = ring0 + threadIdx.x * 16, slot4 = ring0 + 2 * H::ROW + threadIdx.x * 4;
+    const uint32_t ring0 = (uint32_t)__cvta_generic_to_shared(ring), slot4 = ring0 + 2 * H::ROW + threadIdx.x * 4;
+    const bool lead = L::BULK && (int)threadIdx.x % TPR == 0;
     const float inv_d = 1.0f / (float)d;
     const int64_t step = ln.groups();
-    const auto send = [&](int64_t base, int stage) {
-        if constexpr (MODE != 2) {
-            if (base < n) {
-                const int64_t row = base + ln.g;
-                const uint32_t o = (uint32_t)(stage * H::STAGE);
-                xs.send(ln, row, slot + o);
-                gs.send(ln, row, slot + o + H::ROW);
-                copy4_ahead(slot4 + o, row < n ? mean + row : mean, row < n);
-                copy4_ahead(slot4 + o + 4 * kRowBlock, row < n ? rstd + row : rstd, row < n);
+    const auto send = [&](int64_t row, int stage) {
+        const uint32_t o = ring0 + (uint32_t)(stage * H::STAGE);
+        if constexpr (L::BULK) {
+            if (lead && row < n) {
+                int64_t fx, fg;
+                const uint32_t bx = xs.window(ln, row, fx), bg = gs.window(ln, row, fg), bar = jn.stage(ln, stage);
+                expect_bytes(bar, bx + bg);
+                xs.send_bulk(ln, row, fx, bx, o, bar);
+                gs.send_bulk(ln, row, fg, bg, o + H::ROW, bar);
+            }
+        } else if constexpr (MODE != 2) {
+            if (row - ln.g < n) {
+                xs.send_own(ln, row, o);
+                gs.send_own(ln, row, o + H::ROW);
+                copy4_ahead(slot4 + (uint32_t)(stage * H::STAGE), row < n ? mean + row : mean, row < n);
+                copy4_ahead(slot4 + (uint32_t)(stage * H::STAGE) + 4 * kRowBlock, row < n ? rstd + row : rstd, row < n);
             }
             copies_end();
         }
     };
-#pragma unroll
-    for (int i = 0; i < S - 1; ++i) send(ln.first_group() + i * step, i);
+    for (int i = 0; i < S; ++i) {
+        xs.prepare(ln, ring0 + (uint32_t)(i * H::STAGE), 0u);
+        gs.prepare(ln, ring0 + (uint32_t)(i * H::STAGE + H::ROW), 0u);
+        if (L::BULK || i < S - 1) send(ln.group() + i * step, i);
+    }
     float2 w2[L::PAIRS], aw[L::PAIRS], ab[L::PAIRS];
     load_weights<T>(ln, w, wtype, 1.0f, w2);
 #pragma unroll
     for (int q = 0; q < L::PAIRS; ++q) aw[q] = ab[q] = f2(0.0f);
+    float mu_next = 0.0f, rs_next = 0.0f;
+    if (!H::OWN && ln.group() < n) { mu_next = mean[ln.group()]; rs_next = rstd[ln.group()]; }
     for (int64_t base = ln.first_group(); base < n; base += step) {
         const int64_t row = base + ln.g;
         const uint32_t o = (uint32_t)(at * H::STAGE);
         Row<T, MODE, EPL> xv, gv;
-        float mu, rs;
-        if constexpr (MODE != 2) {
-            send(base + (S - 1) * step, at == 0 ? S - 1 : at - 1);
+        float mu = mu_next, rs = rs_next;
+        bool here = true;
+        if constexpr (L::BULK) {
+            if (row < n) here = wait_for(jn.stage(ln, at), phase, &jn.late);
+        } else if constexpr (MODE != 2) {
+            send(row + (S - 1) * step, at == 0 ? S - 1 : at - 1);
             copies_wait<S - 1>();
             mu = __uint_as_float(read4(slot4 + o));
             rs = __uint_as_float(read4(slot4 + o + 4 * kRowBlock));
-        } else {
-            mu = row < n ? mean[row] : 0.0f;
-            rs = row < n ? rstd[row] : 0.0f;
         }
-        xs.take(ln, row, slot + o, 0u, xv);
-        gs.take(ln, row, slot + o + H::ROW, 0u, gv);
-        at = at + 1 == S ? 0 : at + 1;
+        if (!H::OWN && row + step < n) { mu_next = mean[row + step]; rs_next = rstd[row + step]; }
+        xs.take(ln, row, ring0 + o, 0u, xv);
+        gs.take(ln, row, ring0 + o + H::ROW, 0u, gv);
+        if (row >= n) { xv.zero(); gv.zero(); mu = rs = 0.0f; }
         const float2 m2 = f2(-mu), r2 = f2(rs);
-        float2 s0 = f2(0.0f), s1 = f2(0.0f);
+        float2 s0 = f2(here ? 0.0f : __int_as_float(0x7fffffff)), s1 = f2(0.0f);
 #pragma unroll
         for (int q = 0; q < L::PAIRS; ++q) {
             const float2 g = gv.pair(q), h = __fmul2_rn(__fadd2_rn(xv.pair(q), m2), r2), gw = __fmul2_rn(g, w2[q]);
@@ -283,22 +317,27 @@ k_norm_grad_rows(const T* __restrict__ dy, int64_t lddy, const T* __restrict__ x
             s0 = __fadd2_rn(s0, gw);
             s1 = __ffma2_rn(gw, h, s1);
         }
-        if (!dx) continue;
         float s[2] = {s0.x + s0.y, s1.x + s1.y};
         group_all<SumOp, TPR, C>(s, jn, turn);
-        if (row < n) {
+        // every thread of the group is done with this row's stage, or (where it reads it again) with the one before
+        if constexpr (L::BULK && !AGAIN) send(row + S * step, at);
+        if constexpr (AGAIN) {
+            if (base != ln.first_group()) send(row + (S - 1) * step, at == 0 ? S - 1 : at - 1);
+        }
+        if (dx) {
             const float2 c1 = f2(-s[0] * inv_d), c2 = f2(-s[1] * inv_d);
-            if (AGAIN) {
-                xs.take(ln, row, slot + o, 0u, xv);
-                gs.take(ln, row, slot + o + H::ROW, 0u, gv);
+            if constexpr (AGAIN) {
+                xs.take(ln, row, ring0 + o, 0u, xv);
+                gs.take(ln, row, ring0 + o + H::ROW, 0u, gv);
             }
 #pragma unroll
             for (int q = 0; q < L::PAIRS; ++q) {
                 const float2 h = __fmul2_rn(__fadd2_rn(xv.pair(q), m2), r2), gw = __fmul2_rn(gv.pair(q), w2[q]);
                 xv.set_pair(q, __fmul2_rn(r2, __ffma2_rn(h, c2, __fadd2_rn(gw, c1))));
             }
-            xv.store(ln, dx, row, lddx);
+            xv.store(ln, dx, row, lddx, row < n, n, ed);
         }
+        if (++at == S) { at = 0; phase ^= 1; }
     }
     leave_cluster<C>();
     if (!part) return;
@@ -308,7 +347,7 @@ k_norm_grad_rows(const T* __restrict__ dy, int64_t lddy, const T* __restrict__ x
     float* sums = reinterpret_cast<float*>(ring);
     if constexpr (L::GROUPS == 1) {
         // one group: through shared memory only to store neighbouring columns together
-        const int s0 = MODE == 1 ? ln.s : 0, rank = C > 1 ? (int)cluster_rank() : 0;
+        const int from = ln.rank * (kRowBlock * EPL) - ln.s;
 #pragma unroll
         for (int which = 0; which < 2; ++which) {
             __syncthreads();
@@ -321,7 +360,7 @@ k_norm_grad_rows(const T* __restrict__ dy, int64_t lddy, const T* __restrict__ x
             }
             __syncthreads();
             for (int p = threadIdx.x; p < kRowBlock * EPL; p += kRowBlock) {
-                const int e = (p / (kRowBlock * N) * C + rank) * (kRowBlock * N) + p % (kRowBlock * N) - s0;
+                const int e = from + p;
                 if (e >= 0 && e < d) rec[which * d + e] = sums[p];
             }
         }
@@ -419,10 +458,10 @@ extern "C" int gem_nlr_layer_norm(const void* x_dev, int32_t type, int64_t ld_x,
     cudaError_t rc = cudaSuccess;
     by_mode(type, lie.mode, [&](auto t, auto mode) {
         using T = decltype(t);
-        held = by_width<mode.value == 2 ? 4 : (int)sizeof(T), mode.value != 2 && sizeof(T) == 2 ? 32 : 16>(lie.mode == 1 ? (int64_t)d + 16 / tb - 1 : d, [&](auto tpr, auto epl, auto c) {
+        held = by_width<mode.value != 2 && sizeof(T) == 2 ? 24 : 16, mode.value != 2 && sizeof(T) == 2 ? 32 : 24>(lie.mode == 1 ? (int64_t)d + 16 / tb - 1 : d, [&](auto tpr, auto epl, auto c) {
             constexpr auto k = k_norm_rows<T, mode.value, tpr.value, epl.value, c.value>;
             constexpr int shared = NormShape<T, mode.value, tpr.value, epl.value, c.value>::SHARED;
-            const int cl = spread(n, kRowBlock / tpr.value, fwd_rows(epl.value), lie.period, resident_clusters<k, c.value>(shared));
+            const int cl = spread(n, kRowBlock / tpr.value, fwd_rows(tpr.value), lie.period, resident_clusters<k, c.value>(shared));
             rc = launch_rows(k, cl * c.value, c.value, shared, false, st, (const T*)x_dev, ld_x, weight_dev, bias_dev, (int)wtype, n, (int)d, eps,
                              (T*)y_dev, ld_y, mean_dev, rstd_dev);
         });
@@ -474,7 +513,7 @@ extern "C" int gem_nlr_layer_norm_backward(const void* dy_dev, int64_t ld_dy, co
     if (n > 0)
         by_mode(type, lie.mode, [&](auto t, auto mode) {
             using T = decltype(t);
-            held = by_width<mode.value == 2 ? 4 : (int)sizeof(T), mode.value == 0 && sizeof(T) == 2 ? 24 : 16>(lie.mode == 1 ? (int64_t)d + 16 / tb - 1 : d, [&](auto tpr, auto epl, auto c) {
+            held = by_width<mode.value != 2 && sizeof(T) == 2 ? 16 : 12, mode.value == 0 && sizeof(T) == 2 ? 24 : 16>(lie.mode == 1 ? (int64_t)d + 16 / tb - 1 : d, [&](auto tpr, auto epl, auto c) {
                 constexpr auto k = k_norm_grad_rows<T, mode.value, tpr.value, epl.value, c.value>;
                 constexpr int shared = GradShape<T, mode.value, tpr.value, epl.value, c.value>::SHARED;
                 const int most = resident_clusters<k, c.value>(shared), room = norm_records(n, d);

@@ -125,13 +125,14 @@ k_xent_any(const T* z, int64_t ld, const int32_t* __restrict__ labels, int64_t n
 
 // ---- rows in registers -------------------------------------------------------------------------------------------
 
-// Rows that a group works on at a time (their exponentials stay in registers, FP32).
-__host__ __device__ constexpr int xent_rows(int epl) { return epl <= 16 ? 2 : 1; }
+// Rows that a group works on at a time: two of the narrow ones.
+__host__ __device__ constexpr int xent_rows(int tpr) { return tpr < 32 ? 2 : 1; }
 
 template <typename T, int MODE, int TPR, int EPL, int C>
 struct XentShape {
     using S0 = Source<T, MODE, TPR, EPL, C>;
-    static constexpr int ROWS = xent_rows(EPL), ROW = S0::stage_bytes() + (MODE == 2 ? 0 : 4 * kRowBlock);       // a row and its label
+    static constexpr bool OWN = MODE != 2 && TPR < 32;
+    static constexpr int ROWS = xent_rows(TPR), ROW = S0::stage_bytes() + (OWN ? 4 * kRowBlock : 0);       // rows and, if OWN, labels
     static constexpr int STAGE = ROWS * ROW, STAGES = ring_stages(STAGE), SHARED = STAGE * STAGES;
 };
 
@@ -174,40 +175,59 @@ k_xent_rows(const T* z, int64_t ld, const int32_t* __restrict__ labels, int64_t 
     using H = XentShape<T, MODE, TPR, EPL, C>;
     constexpr int N = L::N, R = H::ROWS, S = H::STAGES;
     constexpr float kLog2e = 1.4426950408889634f;
-    extern __shared__ __align__(16) unsigned char ring[];
-    __shared__ Join<TPR, C, R> jn;
-    uint32_t turn = 0;
+    extern __shared__ __align__(128) unsigned char ring[];
+    __shared__ Join<L, TPR, C, R, S> jn;
+    __shared__ Edges<L> ed;
+    uint32_t turn = 0, phase = 0;
     int at = 0;
     jn.begin();
-    const L ln(k, z, ld);
+    const L ln(k, z, ld, ldd);
     const Source<T, MODE, TPR, EPL, C> zs(z, ld, n, k);
-    const uint32_t ring0 = (uint32_t)__cvta_generic_to_shared(ring), slot = ring0 + threadIdx.x * 16,
-                   slot4 = ring0 + H::S0::stage_bytes() + threadIdx.x * 4;
+    const uint32_t ring0 = (uint32_t)__cvta_generic_to_shared(ring), slot4 = ring0 + H::S0::stage_bytes() + threadIdx.x * 4;
+    const bool lead = L::BULK && (int)threadIdx.x % TPR == 0;
     const float nan = __int_as_float(0x7fffffff);
     const int64_t step = ln.groups();
     const auto send = [&](int64_t base, int stage) {
-        if constexpr (MODE != 2) {
+        if constexpr (L::BULK) {
+            const int64_t row = base + ln.g;
+            if (lead && row < n) {
+                int64_t from;
+                const uint32_t bytes = zs.window(ln, row, from), bar = jn.stage(ln, stage);
+                expect_bytes(bar, bytes);
+                zs.send_bulk(ln, row, from, bytes, ring0 + (uint32_t)(stage * H::STAGE), bar);
+            }
+        } else if constexpr (MODE != 2) {
             if (base < n)
 #pragma unroll
                 for (int r = 0; r < R; ++r) {
                     const int64_t row = base + r * step + ln.g;
                     const uint32_t o = (uint32_t)(stage * H::STAGE + r * H::ROW);
-                    zs.send(ln, row, slot + o);
+                    zs.send_own(ln, row, ring0 + o);
                     copy4_ahead(slot4 + o, row < n ? labels + row : labels, row < n);
                 }
             copies_end();
         }
     };
+    for (int i = 0; i < S; ++i) {
 #pragma unroll
-    for (int i = 0; i < S - 1; ++i) send(ln.first_group() + i * R * step, i);
+        for (int r = 0; r < R; ++r) zs.prepare(ln, ring0 + (uint32_t)(i * H::STAGE + r * H::ROW), minus_infinity<T>());
+        if (L::BULK || i < S - 1) send(ln.first_group() + i * R * step, i);
+    }
     float scale = 0.0f;
     bool scaled = false;
     double sum = 0.0;
+    int next = -1;
+    if (L::BULK && ln.group() < n) next = labels[ln.group()];
     for (int64_t base = ln.first_group(); base < n; base += R * step) {
         Row<T, MODE, EPL> zv[R];
-        float m[R], s[R];
+        float m[R], s[R], z_hot[R];
         int lab[R];
-        if constexpr (MODE != 2) {
+        bool here = true;
+        if constexpr (L::BULK) {
+            lab[0] = base + ln.g < n ? next : -1;
+            if (base + step + ln.g < n) next = labels[base + step + ln.g];
+            if (base + ln.g < n) here = wait_for(jn.stage(ln, at), phase, &jn.late);
+        } else if constexpr (MODE != 2) {
             send(base + (S - 1) * R * step, at == 0 ? S - 1 : at - 1);
             copies_wait<S - 1>();
         }
@@ -215,19 +235,28 @@ k_xent_rows(const T* z, int64_t ld, const int32_t* __restrict__ labels, int64_t 
         for (int r = 0; r < R; ++r) {
             const int64_t row = base + r * step + ln.g;
             const uint32_t o = (uint32_t)(at * H::STAGE + r * H::ROW);
-            if constexpr (MODE != 2) lab[r] = (int)read4(slot4 + o);
-            else lab[r] = row < n ? labels[row] : -1;
-            zs.take(ln, row, slot + o, minus_infinity<T>(), zv[r]);
+            if constexpr (H::OWN) lab[r] = row < n ? (int)read4(slot4 + o) : -1;
+            if constexpr (MODE == 2) lab[r] = row < n ? labels[row] : -1;
+            zs.take(ln, row, ring0 + o, minus_infinity<T>(), zv[r]);
+            // the label's logit, by the thread that has it
+            const int hot = lab[r] + ln.s - ln.rank * (L::NV * TPR * N), v_hot = hot / N;
+            z_hot[r] = nan;
+            if (lab[r] >= 0 && lab[r] < k && hot >= 0 && v_hot < L::NV * TPR && v_hot % TPR == ln.l) {
+                if (MODE == 2 || (MODE == 1 && (row == 0 || row == n - 1))) z_hot[r] = to_f(z[row * ld + lab[r]]);
+                else z_hot[r] = to_f(reinterpret_cast<const T*>(ring + o + ln.place(v_hot / TPR) * 16)[hot % N]);
+            }
         }
 #pragma unroll
         for (int r = 0; r < R; ++r) m[r] = row_max<T, MODE, EPL>(zv[r]);
         group_all<MaxOp, TPR, C>(m, jn, turn);
+        if constexpr (L::BULK) send(base + S * step, at);        // every thread of the group has its part of the row
+        if (++at == S) { at = 0; phase ^= 1; }
         float2 e2[R][L::PAIRS];
 #pragma unroll
         for (int r = 0; r < R; ++r) {
             if (m[r] == -INFINITY) m[r] = 0.0f;              // nothing but -inf (or NaN): no -inf - -inf below
             const float2 m2 = f2(-m[r]);
-            float2 a = f2(0.0f);
+            float2 a = f2(here ? 0.0f : nan);
 #pragma unroll
             for (int q = 0; q < L::PAIRS; ++q) {
                 const float2 t = __fmul2_rn(__fadd2_rn(zv[r].pair(q), m2), f2(kLog2e));
@@ -245,24 +274,16 @@ k_xent_rows(const T* z, int64_t ld, const int32_t* __restrict__ labels, int64_t 
 #pragma unroll
         for (int r = 0; r < R; ++r) {
             const int64_t row = base + r * step + ln.g;
-            if (row >= n) continue;
             const bool counts = lab[r] >= 0, known = lab[r] < k, empty = s[r] == 0.0f;
             const float q = !known ? nan : empty ? 0.0f : 1.0f / s[r];
-            // the label's element: its thread has the row's loss and its gradient (p - 1) s; lane 0 where there is none
-            const int hot = lab[r] + (MODE == 1 ? ln.s : 0), v_hot = hot / N;
-            const bool mine = counts && known ? v_hot % L::LANES == ln.l : ln.l == 0;
+            // the label's element: its thread has the row's loss and its gradient (p - 1) s; the first thread where there is none
+            const int hot = lab[r] + ln.s - ln.rank * (L::NV * TPR * N), v_hot = hot / N;
+            const bool mine = row < n && (counts && known ? hot >= 0 && v_hot < L::NV * TPR && v_hot % TPR == ln.l : ln.l == 0 && ln.rank == 0);
             T one;
             if (mine) {
                 float v = counts ? nan : 0.0f;
                 if (counts && known) {
-                    float z_hot;
-                    if constexpr (MODE == 2) z_hot = to_f(z[row * ld + lab[r]]);
-                    else {
-                        // (the matrix's own first and last vectors may not have come through the ring whole)
-                        const uint32_t o = (uint32_t)(at * H::STAGE + r * H::ROW + v_hot / L::LANES * 16 * kRowBlock) + threadIdx.x * 16;
-                        z_hot = MODE == 1 && row == 0 ? to_f(z[lab[r]]) : to_f(reinterpret_cast<const T*>(ring + o)[hot % N]);
-                    }
-                    const float t = z_hot - m[r];
+                    const float t = z_hot[r] - m[r];
                     v = empty ? INFINITY : logf(s[r]) - t;
                     one = from_f<T>(empty ? 0.0f : (exp2_fast(t * kLog2e) * q - 1.0f) * scale);
                 }
@@ -276,10 +297,9 @@ k_xent_rows(const T* z, int64_t ld, const int32_t* __restrict__ labels, int64_t 
 #pragma unroll
                 for (int p = 0; p < L::PAIRS; ++p) zv[r].set_pair(p, __fmul2_rn(e2[r][p], q2));
             }
-            zv[r].store(ln, dz, row, ldd);
+            zv[r].store(ln, dz, row, ldd, row < n, n, ed);   // (ends with the warp's lanes in step: no store of theirs comes after)
             if (mine && counts && known) dz[row * ldd + lab[r]] = one;
         }
-        at = at + 1 == S ? 0 : at + 1;
     }
     if (!scaled) grid_ready();
     leave_cluster<C>();
@@ -316,11 +336,11 @@ extern "C" int gem_nlr_label_cross_entropy(const void* logits_dev, int32_t type,
     cudaError_t rc = cudaSuccess;
     by_mode(type, lie.mode, [&](auto t, auto mode) {
         using T = decltype(t);
-        const bool held = by_width<mode.value == 2 ? 4 : (int)sizeof(T), mode.value != 2 && sizeof(T) == 2 ? 32 : 16>(lie.mode == 1 ? (int64_t)k + 16 / tb - 1 : k, [&](auto tpr, auto epl, auto c) {
+        const bool held = by_width<mode.value != 2 && sizeof(T) == 2 ? 24 : 16, mode.value != 2 && sizeof(T) == 2 ? 32 : 24>(lie.mode == 1 ? (int64_t)k + 16 / tb - 1 : k, [&](auto tpr, auto epl, auto c) {
             constexpr auto kern = k_xent_rows<T, mode.value, tpr.value, epl.value, c.value>;
             constexpr int shared = XentShape<T, mode.value, tpr.value, epl.value, c.value>::SHARED;
             const int most = resident_clusters<kern, c.value>(shared);
-            const int cl = spread(n, kRowBlock / tpr.value, xent_rows(epl.value), lie.period, most < kMaxBlocks / c.value ? most : kMaxBlocks / c.value);
+            const int cl = spread(n, kRowBlock / tpr.value, xent_rows(tpr.value), lie.period, most < kMaxBlocks / c.value ? most : kMaxBlocks / c.value);
             rc = launch_rows(kern, cl * c.value, c.value, shared, true, st, (const T*)logits_dev, ld, labels_dev, n, (int)k, (int)mean, sc, loss_dev,
                              row_loss_dev, (T*)dlogits_dev, ld_d);
         });

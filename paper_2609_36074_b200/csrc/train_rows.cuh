@@ -1,8 +1,8 @@
 // Rows of a matrix, streamed: the layout that the layer norm and cross entropy kernels share.
 //
 // A row of d elements belongs to a group of TPR threads of a block (part of a warp, a warp, or several), or of C whole
-// blocks in a cluster; EPL elements to a thread, in vectors of N: vector k of lane l of the group's LANES = TPR C lanes holds
-// elements (k LANES + l) N - s ... + N - 1, so that a group's loads are contiguous.  The row is read from HBM once.
+// blocks in a cluster; EPL elements to a thread, in NV vectors of N: vector k of thread l of block r of the group holds
+// elements ((r NV + k) TPR + l) N - s ... + N - 1, so that a group's accesses are contiguous.  The row is read from HBM once.
 //
 // Three ways of reading a matrix (MODE):
 //   0  every row begins and ends at a multiple of 16 bytes: vectors of 16 bytes, s = 0
@@ -12,9 +12,10 @@
 //      the padding), which are replaced after loading and left alone in storing
 //   2  element by element, where the matrices of one call lie differently to 16 bytes
 //
-// In modes 0 and 1 a thread's vectors come through a ring of stages in shared memory (asynchronous copies, S rows ahead):
-// registers alone hold too few bytes in flight for HBM.  Each thread copies the very vectors that it reads, so the ring
-// needs no barrier: its own copies' completion is all that a thread waits for.
+// In modes 0 and 1 rows come through a ring of stages in shared memory, S rows ahead: registers alone hold too few bytes in
+// flight for HBM.  From a warp a row on (BULK), one thread sends for the whole row by one bulk copy, which arrives at a
+// barrier in shared memory; the threads of narrower rows copy 16 bytes each, the very vectors that they read themselves, and
+// need no barrier.
 #pragma once
 #include "train_common.cuh"
 
@@ -120,32 +121,73 @@ __device__ __forceinline__ uint32_t read4(uint32_t at)
 __device__ __forceinline__ void copies_end() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int LEFT> __device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(LEFT) : "memory"); }
 
+// One contiguous piece from global to shared memory; arrives at the barrier.  16-byte aligned, a multiple of 16 bytes.
+__device__ __forceinline__ void bulk_ahead(uint32_t to, const void* from, uint32_t bytes, uint32_t bar)
+{
+    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
+                 ::"r"(to), "l"(from), "r"(bytes), "r"(bar) : "memory");
+}
+__device__ __forceinline__ void expect_bytes(uint32_t bar, uint32_t bytes)
+{
+    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void barrier_init(uint32_t bar, uint32_t count)
+{
+    asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count) : "memory");
+}
+
+// Polls of one wait.  A healthy one ends within microseconds.  One that runs out raises the block's `late` flag: its row's
+// results become NaN, and later waits poll a little only (their copies still have to land), so that the kernel ends whatever
+// has happened.
+constexpr uint32_t kPolls = 1u << 20, kLatePolls = 1u << 12;
+
+__device__ __forceinline__ bool wait_for(uint32_t bar, uint32_t parity, volatile uint32_t* late)
+{
+    uint32_t limit = kPolls;
+    for (uint32_t i = 0; i < limit; ++i) {
+        uint32_t ok;
+        asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+                     : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
+        if (ok) return true;
+        if ((i & 63u) == 63u && *late) limit = kLatePolls;
+    }
+    *late = 1;
+    return false;
+}
+
 template <typename T, int MODE, int TPR, int EPL, int C>
 struct Lane {
     static constexpr int N = MODE == 2 ? 1 : 16 / (int)sizeof(T);
-    static constexpr int NV = EPL / N, LANES = TPR * C, GROUPS = kRowBlock / TPR;
+    static constexpr int NV = EPL / N, GROUPS = kRowBlock / TPR;
     static constexpr int PAIRS = EPL / 2;            // pair q holds the thread's elements 2 q and 2 q + 1
+    static constexpr bool BULK = MODE != 2 && TPR >= 32;
+    // Elements of cut vectors are stored one each by other lanes of the warp, through EDGES places of 16 bytes a warp; rows
+    // of less than 8 threads have more ends than that pays for.
+    static constexpr bool EDGED = MODE == 1 && TPR >= 8;
+    static constexpr int ENDS = TPR >= 32 ? 2 : 2 * 32 / TPR, TURNS = EDGED ? (ENDS * N + 31) / 32 : 1;
     static_assert(C == 1 || TPR == kRowBlock, "");
     static_assert(EPL % N == 0 && EPL % 2 == 0, "");
 
-    int l, g, s, d;
-    int last;                                        // k of the row's last vector (of whichever lane)
+    int l, g, s, d, rank;
+    int last;                                        // k of the row's last vector, in the block that has it; else never reached
     uint32_t head[MODE == 1 ? 4 : 1], tail[MODE == 1 ? 4 : 1];   // the row's part of vector 0 and of vector `last`, as words
     uint32_t head_bits, tail_bits;                               // and as a bit an element
-    __device__ __forceinline__ Lane(int d_, const T* base, int64_t ld) : g((int)threadIdx.x / TPR), s(0), d(d_)
+    int64_t edge[TURNS];                                         // elements that this lane stores for cut vectors: from its own row's
+    int edge_group[TURNS];                                       // beginning, and of which group; -1: none
+
+    __device__ __forceinline__ Lane(int d_, const T* base, int64_t ld, int64_t ld_out)
+        : l((int)threadIdx.x % TPR), g((int)threadIdx.x / TPR), s(0), d(d_), rank(C > 1 ? (int)cluster_rank() : 0)
     {
-        l = (int)threadIdx.x % TPR;
-        if constexpr (C > 1) l += (int)cluster_rank() * TPR;
         if constexpr (MODE == 1) {
-            s = (int)((reinterpret_cast<uintptr_t>(base + group() * ld) & 15) / sizeof(T));
-            last = (s + d - 1) / N / LANES;
+            s = lies(base, ld, group());
+            const int v_last = (s + d - 1) / N - rank * NV * TPR;
+            last = v_last < 0 ? -1 : v_last / TPR;   // (NV and more: another block's)
             head_bits = tail_bits = 0;
 #pragma unroll
             for (int i = 0; i < N; ++i) {
-                if (first(0) + i >= 0) head_bits |= 1u << i;
+                if (first(0) + i >= 0 && (last != 0 || first(0) + i < d)) head_bits |= 1u << i;
                 if (first(last) + i < d) tail_bits |= 1u << i;
             }
-            if (last == 0) head_bits = tail_bits = head_bits & tail_bits;
 #pragma unroll
             for (int w = 0; w < 4; ++w) {
                 constexpr int E = 4 / (int)sizeof(T);
@@ -153,23 +195,51 @@ struct Lane {
                 head[w] = tail[w] = 0;
 #pragma unroll
                 for (int j = 0; j < E; ++j) {
-                    if (first(0) + w * E + j >= 0) head[w] |= ONE << (16 * j);
-                    if (first(last) + w * E + j < d) tail[w] |= ONE << (16 * j);
+                    if (head_bits >> (w * E + j) & 1) head[w] |= ONE << (16 * j);
+                    if (tail_bits >> (w * E + j) & 1) tail[w] |= ONE << (16 * j);
+                }
+            }
+            if constexpr (EDGED) {
+                const int lane = threadIdx.x & 31;
+#pragma unroll
+                for (int t = 0; t < TURNS; ++t) {
+                    const int x = lane + 32 * t, end = x / N, i = x % N;        // element i of one of the warp's ends
+                    edge[t] = 0;
+                    edge_group[t] = -1;
+                    if (end >= ENDS) continue;
+                    const int first_group = (int)(threadIdx.x & ~31u) / TPR, gg = first_group + end / 2;
+                    const int ss = lies(base, ld, group() + (gg - g));
+                    const int v = end % 2 == 0 ? 0 : (ss + d - 1) / N, owner = v % TPR, e = v * N - ss + i;
+                    const bool here = (v / TPR) / NV == rank && (TPR < 32 || owner / 32 == l / 32);
+                    const bool cut = v * N - ss < 0 || v * N - ss + N > d;
+                    if (here && cut && (end % 2 == 0 || v != 0) && e >= 0 && e < d) {
+                        edge[t] = (gg - g) * ld_out + e;
+                        edge_group[t] = gg;
+                    }
                 }
             }
         }
+    }
+    static __device__ __forceinline__ int lies(const T* base, int64_t ld, int64_t row)
+    {
+        return (int)((reinterpret_cast<uintptr_t>(base + row * ld) & 15) / sizeof(T));
     }
     // number of the group among all groups of the grid, and their count
     __device__ __forceinline__ int64_t group() const { return (int64_t)(blockIdx.x / C) * GROUPS + g; }
     __device__ __forceinline__ int64_t first_group() const { return (int64_t)(blockIdx.x / C) * GROUPS; }
     __device__ __forceinline__ int64_t groups() const { return (int64_t)(gridDim.x / C) * GROUPS; }
-    __device__ __forceinline__ int first(int k) const { return (k * LANES + l) * N - (MODE == 1 ? s : 0); }
+    __device__ __forceinline__ int first(int k) const { return ((rank * NV + k) * TPR + l) * N - (MODE == 1 ? s : 0); }
     __device__ __forceinline__ bool any(int k) const { return first(k) < d; }
-    // whether vector k may be cut by an end of the row (the same for all lanes)
-    __device__ __forceinline__ bool end(int k) const { return MODE == 1 && (k == 0 || k == last); }
-    __device__ __forceinline__ uint32_t bits(int k) const { return k == 0 ? head_bits : tail_bits; }      // where end(k)
+    // whether vector k may be cut by an end of the row (the same for all lanes of the group)
+    __device__ __forceinline__ bool end(int k) const { return MODE == 1 && ((k == 0 && rank == 0) || k == last); }
+    __device__ __forceinline__ uint32_t bits(int k) const { return k == 0 && rank == 0 ? head_bits : tail_bits; }      // where end(k)
     __device__ __forceinline__ bool holds(int k, int i) const { return MODE == 1 ? first(k) + i >= 0 && first(k) + i < d : any(k); }
+    // place of the thread's vector k in a stage, in vectors
+    __device__ __forceinline__ int place(int k) const { return BULK ? (g * NV + k) * TPR + l : k * kRowBlock + (int)threadIdx.x; }
 };
+
+// Shared memory of cut vectors on their way out.
+template <typename LN> struct Edges { uint4 v[LN::EDGED ? kRowBlock / 32 * LN::ENDS : 1]; };
 
 // The thread's elements of one row.
 template <typename T, int MODE, int EPL>
@@ -179,26 +249,40 @@ struct Row {
     struct One { T e; };
     typename std::conditional<MODE == 2, One, V>::type v[NV];
 
+    // By all lanes of the warp, `ok` or not.  (A lane's row is at most 31 rows from another's in its warp.)
     template <typename LN>
-    __device__ __forceinline__ void store(const LN& ln, T* base, int64_t row, int64_t ld) const
+    __device__ __forceinline__ void store(const LN& ln, T* base, int64_t row, int64_t ld, bool ok, int64_t n, Edges<LN>& ed) const
     {
         T* p = base + row * ld;
+        if (ok) {
 #pragma unroll
-        for (int k = 0; k < NV; ++k) {
-            const int e = ln.first(k);
-            if constexpr (MODE == 2) {
-                if (ln.any(k)) p[e] = v[k].e;
-            } else if (!ln.end(k)) {
-                if (ln.any(k)) v[k].store(p + e);
-            } else {
-                const uint32_t b = ln.bits(k);
-                if (b == (1u << N) - 1) v[k].store(p + e);
-                else if (b) {
+            for (int k = 0; k < NV; ++k) {
+                const int e = ln.first(k);
+                if constexpr (MODE == 2) {
+                    if (ln.any(k)) p[e] = v[k].e;
+                } else if (!ln.end(k)) {
+                    if (ln.any(k)) v[k].store(p + e);
+                } else {
+                    const uint32_t b = ln.bits(k);
+                    if (b == (1u << N) - 1) v[k].store(p + e);
+                    else if constexpr (LN::EDGED) {
+                        const int at = (int)threadIdx.x / 32 * LN::ENDS + (LN::ENDS > 2 ? ln.g % (LN::ENDS / 2) * 2 : 0) + (k == 0 && ln.rank == 0 && ln.l == 0 ? 0 : 1);
+                        if (b) ed.v[at] = v[k].raw;
+                    } else if (b) {
 #pragma unroll
-                    for (int i = 0; i < N; ++i)
-                        if (b & (1u << i)) p[e + i] = v[k].at(i);
+                        for (int i = 0; i < N; ++i)
+                            if (b & (1u << i)) p[e + i] = v[k].at(i);
+                    }
                 }
             }
+        }
+        if constexpr (LN::EDGED) {
+            __syncwarp();
+            const T* places = reinterpret_cast<const T*>(ed.v + threadIdx.x / 32 * LN::ENDS);
+#pragma unroll
+            for (int t = 0; t < LN::TURNS; ++t)
+                if (ln.edge_group[t] >= 0 && row + (ln.edge_group[t] - ln.g) < n) p[ln.edge[t]] = places[(threadIdx.x & 31) + 32 * t];
+            __syncwarp();
         }
     }
     __device__ __forceinline__ float2 pair(int q) const
@@ -224,56 +308,75 @@ template <typename T, int MODE, int TPR, int EPL, int C>
 struct Source {
     using L = Lane<T, MODE, TPR, EPL, C>;
     static constexpr int N = L::N, NV = L::NV;
-    // bytes of a block's stage for one row
+    // bytes of a block's stage for one row of every group
     __host__ __device__ static constexpr int stage_bytes() { return MODE == 2 ? 0 : NV * 16 * kRowBlock; }
     const T* base;
     int64_t  ld, n, span;                            // span: elements from the matrix's first to its last
     __device__ __forceinline__ Source(const T* p, int64_t ld_, int64_t n_, int d) : base(p), ld(ld_), n(n_), span((n_ - 1) * ld_ + d) {}
 
-    // Sends for the row; `slot` is the thread's place in the stage (vectors are kRowBlock places apart).
-    __device__ __forceinline__ void send(const L& ln, int64_t row, uint32_t slot) const
+    // Before the first send: what no copy will write reads as `none` (the vectors beyond the row).
+    __device__ __forceinline__ void prepare(const L& ln, uint32_t stage, uint32_t none) const
     {
         if constexpr (MODE != 2) {
-            const int64_t at = row * ld;
 #pragma unroll
-            for (int k = 0; k < NV; ++k) {
-                const int e = ln.first(k);
-                int bytes = row < n && ln.any(k) ? 16 : 0;
-                if (ln.end(k) && bytes) {            // what is not between the matrix's ends is not touched
-                    if (at + e < 0) bytes = 0;
-                    else if (at + e + N > span) bytes = (int)(span - (at + e)) * (int)sizeof(T);
-                }
-                copy_ahead(slot + (uint32_t)k * 16 * kRowBlock, bytes ? base + at + e : base - (MODE == 1 ? (int)((reinterpret_cast<uintptr_t>(base) & 15) / sizeof(T)) : 0), bytes);
-            }
+            for (int k = 0; k < NV; ++k)
+                if (!ln.any(k))
+                    asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(stage + (uint32_t)ln.place(k) * 16), "r"(none) : "memory");
         }
     }
-    // The row that was sent for, once its copies are complete.
-    __device__ __forceinline__ void take(const L& ln, int64_t row, uint32_t slot, uint32_t none, Row<T, MODE, EPL>& r) const
+    // What one thread of a group (BULK) sends for: the bytes of the group's window that lie between the matrix's ends.
+    __device__ __forceinline__ uint32_t window(const L& ln, int64_t row, int64_t& from) const
+    {
+        const int64_t begin = row * ld - ln.s + ln.rank * (NV * TPR * N);
+        int64_t stop = row * ld - ln.s + (ln.s + ln.d + N - 1) / N * N;
+        if (C > 1 && stop > begin + NV * TPR * N) stop = begin + NV * TPR * N;
+        from = begin < 0 ? begin + N : begin;        // (only vectors that are whole: the rest is picked up by take())
+        if (MODE == 1 && stop > span) stop -= N;
+        return stop > from ? (uint32_t)(stop - from) * (uint32_t)sizeof(T) : 0u;
+    }
+    __device__ __forceinline__ void send_bulk(const L& ln, int64_t row, int64_t from, uint32_t bytes, uint32_t stage, uint32_t bar) const
+    {
+        const int64_t begin = row * ld - ln.s + ln.rank * (NV * TPR * N);
+        if (bytes) bulk_ahead(stage + (uint32_t)(ln.g * NV * TPR * 16) + (uint32_t)(from - begin) * (uint32_t)sizeof(T), base + from, bytes, bar);
+    }
+    // What every thread of a narrower group sends for.
+    __device__ __forceinline__ void send_own(const L& ln, int64_t row, uint32_t stage) const
     {
         const int64_t at = row * ld;
 #pragma unroll
         for (int k = 0; k < NV; ++k) {
             const int e = ln.first(k);
+            if (row < n && ln.any(k)) {
+                if (!ln.end(k) || (at + e >= 0 && at + e + N <= span)) copy_ahead(stage + (uint32_t)ln.place(k) * 16, base + at + e, 16);
+            }
+        }
+    }
+    // The row that was sent for, once its copies are complete.
+    __device__ __forceinline__ void take(const L& ln, int64_t row, uint32_t stage, uint32_t none, Row<T, MODE, EPL>& r) const
+    {
+#pragma unroll
+        for (int k = 0; k < NV; ++k) {
+            const int e = ln.first(k);
             if constexpr (MODE == 2) {
                 const uint32_t x = none;
-                if (row < n && ln.any(k)) r.v[k].e = base[at + e]; else r.v[k].e = *reinterpret_cast<const T*>(&x);
+                if (row < n && ln.any(k)) r.v[k].e = base[row * ld + e]; else r.v[k].e = *reinterpret_cast<const T*>(&x);
             } else {
                 asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];"
                              : "=r"(r.v[k].w[0]), "=r"(r.v[k].w[1]), "=r"(r.v[k].w[2]), "=r"(r.v[k].w[3])
-                             : "r"(slot + (uint32_t)k * 16 * kRowBlock) : "memory");
+                             : "r"(stage + (uint32_t)ln.place(k) * 16) : "memory");
                 if (ln.end(k)) {
-                    if (at + e < 0 && row < n) {     // only where the matrix itself begins inside a vector
+                    const int64_t at = row * ld + e;
+                    if ((at < 0 || at + N > span) && row < n) {      // a vector that reaches over the matrix's own end
 #pragma unroll
                         for (int i = 0; i < N; ++i)
-                            if (ln.holds(k, i)) r.v[k].set(i, base[at + e + i]);
+                            if (ln.holds(k, i)) r.v[k].set(i, base[at + i]);
                     }
+                    const bool h = k == 0 && ln.rank == 0;
 #pragma unroll
                     for (int w = 0; w < 4; ++w) {
-                        const uint32_t m = (k == 0 ? ln.head[w] : ~0u) & (k == ln.last ? ln.tail[w] : ~0u);
+                        const uint32_t m = h ? ln.head[w] : ln.tail[w];
                         r.v[k].w[w] = (r.v[k].w[w] & m) | (none & ~m);
                     }
-                } else if (none != 0 && !ln.any(k)) {
-                    r.v[k].fill(none);
                 }
             }
         }
@@ -301,76 +404,59 @@ __device__ __forceinline__ void load_weights(const LN& ln, const void* w, int wt
 struct SumOp { __device__ __forceinline__ static float of(float a, float b) { return a + b; } };
 struct MaxOp { __device__ __forceinline__ static float of(float a, float b) { return fmaxf(a, b); } };
 
-// Shared memory of group_all for R values at a time: two halves of a value for every warp of a group (or cluster).
-template <int TPR, int C, int R>
+// Shared memory of group_all for R values at a time: two halves of a value for every warp of a group (or cluster); and the
+// barriers of a ring of S stages, one a stage and group.
+template <typename LN, int TPR, int C, int R, int S>
 struct Join {
     static constexpr int W = TPR > 32 ? TPR / 32 * C : 1;        // values to join: one a warp
+    static constexpr int FULLS = LN::BULK ? S * LN::GROUPS : 1;
     float    v[TPR <= 32 ? 1 : 2 * R * C * kRowBlock / 32];
     uint64_t bar[C > 1 ? 2 : 1];                                 // the halves' arrivals from the cluster's blocks
-    uint32_t late;                                               // a wait has run out: no wait after it, sums are NaN
-    __device__ __forceinline__ void arm(int half)
-    {
-        asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"((uint32_t)__cvta_generic_to_shared(&bar[half])),
-                     "r"((uint32_t)(W * R * sizeof(float))) : "memory");
-    }
-    // before the first group_all, by all threads
+    uint64_t full[FULLS];                                        // the ring's stages
+    uint32_t late;                                               // a wait has run out
+    __device__ __forceinline__ uint32_t half(int h) { return (uint32_t)__cvta_generic_to_shared(&bar[h]); }
+    __device__ __forceinline__ uint32_t stage(const LN& ln, int at) { return (uint32_t)__cvta_generic_to_shared(&full[at * LN::GROUPS + ln.g]); }
+    // before the first use, by all threads
     __device__ __forceinline__ void begin()
     {
-        if constexpr (C > 1) {
+        if constexpr (LN::BULK || C > 1) {
             if (threadIdx.x == 0) {
-#pragma unroll
-                for (int h = 0; h < 2; ++h)
-                    asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" ::"r"((uint32_t)__cvta_generic_to_shared(&bar[h])) : "memory");
+                if constexpr (LN::BULK)
+                    for (int i = 0; i < FULLS; ++i) barrier_init((uint32_t)__cvta_generic_to_shared(&full[i]), 1);
+                if constexpr (C > 1) { barrier_init(half(0), 1); barrier_init(half(1), 1); }
                 asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
                 late = 0;
-                arm(0);
-                arm(1);
+                if constexpr (C > 1)
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) expect_bytes(half(h), W * R * (uint32_t)sizeof(float));
             }
             __syncwarp();
-            cluster_barrier();
+            if constexpr (C > 1) cluster_barrier(); else __syncthreads();
         }
     }
 };
-
-// Polls of one wait.  A healthy one ends within microseconds; one that runs out leaves NaN in its row's results and every
-// later wait of the block returns at once, so that the kernel ends whatever has happened.
-constexpr uint32_t kJoinPolls = 1u << 20;
-
-__device__ __forceinline__ bool join_wait(uint64_t* bar, uint32_t parity, volatile uint32_t* late)
-{
-    const uint32_t b = (uint32_t)__cvta_generic_to_shared(bar);
-    for (uint32_t i = 0; i < kJoinPolls; ++i) {
-        uint32_t ok;
-        asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
-                     : "=r"(ok) : "r"(b), "r"(parity) : "memory");
-        if (ok) return true;
-        if ((i & 63u) == 63u && *late) return false;
-    }
-    *late = 1;
-    return false;
-}
 
 // Sums (or maxima) of R values over a group; every thread gets the same bits.  `turn` counts the calls.
 // Where a group is more than a warp, its warps write their values to shared memory and meet at the group's barrier.  In a
 // cluster every warp sends its values to every block, and a thread waits until its block has all of them; no block waits for
 // a barrier of the cluster, whose release would wait for the rows' stores too.  Both use the halves of the buffer in turn:
 // whoever writes a half has seen, in the call between, values that every warp sent after its last reads of that half.
-template <typename Op, int TPR, int C, int R>
-__device__ __forceinline__ void group_all(float (&v)[R], Join<TPR, C, R>& jn, uint32_t& turn)
+template <typename Op, int TPR, int C, int R, typename J>
+__device__ __forceinline__ void group_all(float (&v)[R], J& jn, uint32_t& turn)
 {
 #pragma unroll
     for (int o = (TPR < 32 ? TPR : 32) / 2; o > 0; o >>= 1)
 #pragma unroll
         for (int r = 0; r < R; ++r) v[r] = Op::of(v[r], __shfl_xor_sync(0xffffffffu, v[r], o));
     if constexpr (TPR > 32) {
-        constexpr int W = Join<TPR, C, R>::W;
+        constexpr int W = J::W;
         const int g = threadIdx.x / TPR, warp = (threadIdx.x % TPR) >> 5, l = threadIdx.x & 31, half = turn & 1;
         float* b = jn.v + (g * 2 + half) * R * W;
         bool here = true;
         if constexpr (C > 1) {
             if (l < C) {
                 const uint32_t mine = (uint32_t)__cvta_generic_to_shared(b + cluster_rank() * (TPR / 32) + warp);
-                const uint32_t bar = (uint32_t)__cvta_generic_to_shared(&jn.bar[half]);
+                const uint32_t bar = jn.half(half);
                 uint32_t there, there_bar;
                 asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(there) : "r"(mine), "r"(l));
                 asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(there_bar) : "r"(bar), "r"(l));
@@ -380,8 +466,8 @@ __device__ __forceinline__ void group_all(float (&v)[R], Join<TPR, C, R>& jn, ui
                                  ::"r"(there + (uint32_t)(r * W * sizeof(float))), "r"(__float_as_uint(v[r])), "r"(there_bar) : "memory");
             }
             __syncwarp();
-            here = join_wait(&jn.bar[half], (turn >> 1) & 1, &jn.late);
-            if (threadIdx.x == 0) jn.arm(half);      // for the call after the next
+            here = wait_for(jn.half(half), (turn >> 1) & 1, &jn.late);
+            if (threadIdx.x == 0) expect_bytes(jn.half(half), W * R * (uint32_t)sizeof(float));      // for the call after the next
         } else {
             if (l == 0)
 #pragma unroll
@@ -409,35 +495,34 @@ template <int C> __device__ __forceinline__ void leave_cluster() { if constexpr 
 
 template <int V> struct Const { static constexpr int value = V; };
 
-// f(TPR, EPL, C) as constants for rows of `width` elements of `bytes` bytes (the window's s included), false if it is wider
-// than eight blocks hold.  Few threads a row and many elements a thread keep the work per row (sums over the group, labels,
-// statistics) small; what bounds EPL are 128 registers next to weights and sums: 16 elements, 24 or WIDEST of 2 bytes.  Rows of
-// more than 4096 (6144) elements go to clusters of blocks, so that every SM still has two blocks, one of which loads
-// while the other adds.
-template <int BYTES, int WIDEST, typename F>
+// f(TPR, EPL, C) as constants for rows of `width` elements (the window's s included), false if it is wider than eight blocks
+// hold.  Few threads a row and many elements a thread keep the work per row (sums over the group, labels, statistics) small;
+// what bounds EPL are 128 registers next to weights and sums: E1 or E2 elements from a warp a row on (E1 TPR > E2 TPR / 2).
+// Rows wider than 256 E2 go to clusters of blocks, so that every SM still has two blocks, one of which loads while the
+// other adds.
+template <int E1, int E2, typename F>
 bool by_width(int64_t width, F f)
 {
-    constexpr int A = BYTES == 2 ? 16 : 12, B = BYTES == 2 && WIDEST >= 24 ? 24 : 16;
     if (width <= 16) f(Const<1>{}, Const<16>{}, Const<1>{});
     else if (width <= 32) f(Const<2>{}, Const<16>{}, Const<1>{});
     else if (width <= 64) f(Const<4>{}, Const<16>{}, Const<1>{});
     else if (width <= 128) f(Const<8>{}, Const<16>{}, Const<1>{});
     else if (width <= 256) f(Const<16>{}, Const<16>{}, Const<1>{});
     else if (width <= 512) f(Const<32>{}, Const<16>{}, Const<1>{});
-    else if (WIDEST >= 24 && width <= 768) f(Const<32>{}, Const<WIDEST >= 24 ? 24 : 16>{}, Const<1>{});
-    else if (WIDEST >= 32 && width <= 1024) f(Const<32>{}, Const<WIDEST >= 32 ? 32 : 16>{}, Const<1>{});
-    else if (width <= 64 * A) f(Const<64>{}, Const<A>{}, Const<1>{});
-    else if (width <= 64 * B) f(Const<64>{}, Const<B>{}, Const<1>{});
-    else if (width <= 128 * A) f(Const<128>{}, Const<A>{}, Const<1>{});
-    else if (width <= 128 * B) f(Const<128>{}, Const<B>{}, Const<1>{});
-    else if (width <= 256 * A) f(Const<256>{}, Const<A>{}, Const<1>{});
-    else if (width <= 256 * B) f(Const<256>{}, Const<B>{}, Const<1>{});
-    else if (width <= 512 * A) f(Const<256>{}, Const<A>{}, Const<2>{});
-    else if (width <= 512 * B) f(Const<256>{}, Const<B>{}, Const<2>{});
-    else if (width <= 1024 * A) f(Const<256>{}, Const<A>{}, Const<4>{});
-    else if (width <= 1024 * B) f(Const<256>{}, Const<B>{}, Const<4>{});
-    else if (width <= 2048 * A) f(Const<256>{}, Const<A>{}, Const<8>{});
-    else if (width <= 2048 * B) f(Const<256>{}, Const<B>{}, Const<8>{});
+    else if (E2 > 16 && width <= 32 * E1) f(Const<32>{}, Const<(E2 > 16 ? E1 : 16)>{}, Const<1>{});
+    else if (E2 > 16 && width <= 32 * E2) f(Const<32>{}, Const<(E2 > 16 ? E2 : 16)>{}, Const<1>{});
+    else if (width <= 64 * E1) f(Const<64>{}, Const<E1>{}, Const<1>{});
+    else if (width <= 64 * E2) f(Const<64>{}, Const<E2>{}, Const<1>{});
+    else if (width <= 128 * E1) f(Const<128>{}, Const<E1>{}, Const<1>{});
+    else if (width <= 128 * E2) f(Const<128>{}, Const<E2>{}, Const<1>{});
+    else if (width <= 256 * E1) f(Const<256>{}, Const<E1>{}, Const<1>{});
+    else if (width <= 256 * E2) f(Const<256>{}, Const<E2>{}, Const<1>{});
+    else if (width <= 512 * E1) f(Const<256>{}, Const<E1>{}, Const<2>{});
+    else if (width <= 512 * E2) f(Const<256>{}, Const<E2>{}, Const<2>{});
+    else if (width <= 1024 * E1) f(Const<256>{}, Const<E1>{}, Const<4>{});
+    else if (width <= 1024 * E2) f(Const<256>{}, Const<E2>{}, Const<4>{});
+    else if (width <= 2048 * E1) f(Const<256>{}, Const<E1>{}, Const<8>{});
+    else if (width <= 2048 * E2) f(Const<256>{}, Const<E2>{}, Const<8>{});
     else return false;
     return true;
 }
