@@ -105,13 +105,14 @@ k_norm_dw_sum(const float* __restrict__ part, int records, int d, W* __restrict_
 
 // ---- streamed rows -----------------------------------------------------------------------------------------------
 
-// Rows that a group works on at a time: two of the narrow ones, so that their sums over the group run side by side.
-__host__ __device__ constexpr int fwd_rows(int tpr) { return tpr < 32 ? 2 : 1; }
+// Rows that a group works on at a time: two or four of the narrow ones, so that their sums over the group run side by side.
+__host__ __device__ constexpr int fwd_rows(int tpr, int epl) { return tpr >= 32 ? 1 : epl <= 8 ? 4 : 2; }
 
 template <typename T, int MODE, int TPR, int EPL, int C>
 struct NormShape {
     using S0 = Source<T, MODE, TPR, EPL, C>;
-    static constexpr int ROWS = fwd_rows(TPR), ROW = S0::stage_bytes(), STAGE = ROWS * ROW, STAGES = ring_stages(STAGE), SHARED = STAGE * STAGES;
+    static constexpr int ROWS = fwd_rows(TPR, EPL), ROW = S0::stage_bytes(), STAGE = ROWS * ROW;
+    static constexpr int MASKS = S0::L::mask_bytes(), STAGES = ring_stages(STAGE, MASKS), SHARED = STAGE * STAGES + MASKS;
 };
 
 template <typename T, int MODE, int TPR, int EPL, int C>
@@ -128,9 +129,9 @@ k_norm_rows(const T* __restrict__ x, int64_t ldx, const void* __restrict__ w, co
     uint32_t turn = 0, phase = 0;
     int at = 0;
     jn.begin();
-    const L ln(d, x, ldx, ldy);
-    const Source<T, MODE, TPR, EPL, C> xs(x, ldx, n, d);
     const uint32_t ring0 = (uint32_t)__cvta_generic_to_shared(ring);
+    const L ln(d, x, ldx, ldy, ring0 + H::STAGE * S);
+    const Source<T, MODE, TPR, EPL, C> xs(x, ldx, n, d);
     const bool lead = L::BULK && (int)threadIdx.x % TPR == 0;
     const float inv_d = 1.0f / (float)d;
     const int64_t step = ln.groups();
@@ -172,10 +173,15 @@ k_norm_rows(const T* __restrict__ x, int64_t ldx, const void* __restrict__ w, co
 #pragma unroll
         for (int r = 0; r < R; ++r) {
             xs.take(ln, base + r * step + ln.g, ring0 + (uint32_t)(at * H::STAGE + r * H::ROW), 0u, xv[r]);
+            xv[r].mend_own(ln);
             float2 a = f2(here ? 0.0f : __int_as_float(0x7fffffff));
 #pragma unroll
             for (int q = 0; q < L::PAIRS; ++q) a = __fadd2_rn(a, xv[r].pair(q));
             s[r] = a.x + a.y;
+            if constexpr (MODE == 1)
+#pragma unroll
+                for (int k = 0; k < L::NV; ++k)
+                    if (L::may_cut(k)) s[r] -= ln.spare(k) * to_f(xv[r].own(ln, k));
         }
         group_all<SumOp, TPR, C>(s, jn, turn);
         if constexpr (L::BULK) send(base + S * step, at);        // every thread of the group has its part of the row
@@ -187,22 +193,23 @@ k_norm_rows(const T* __restrict__ x, int64_t ldx, const void* __restrict__ w, co
             float2 a = f2(0.0f);
 #pragma unroll
             for (int k = 0; k < (MODE == 2 ? L::PAIRS : L::NV); ++k) {
-                const bool cut = MODE == 2 || ln.end(k);
-                if (cut || ln.any(k)) {
+                float2 b = f2(0.0f);
 #pragma unroll
-                    for (int i = 0; i < (MODE == 2 ? 1 : N / 2); ++i) {
-                        const int q = MODE == 2 ? k : k * (N / 2) + i;
-                        float2 c = __fadd2_rn(xv[r].pair(q), m2);
-                        if (MODE == 2) {
-                            if (!ln.any(2 * q)) c.x = 0.0f;
-                            if (!ln.any(2 * q + 1)) c.y = 0.0f;
-                        } else if (cut) {
-                            if (!(ln.bits(k) & (1u << 2 * i))) c.x = 0.0f;
-                            if (!(ln.bits(k) & (2u << 2 * i))) c.y = 0.0f;
-                        }
-                        a = __ffma2_rn(c, c, a);
+                for (int i = 0; i < (MODE == 2 ? 1 : N / 2); ++i) {
+                    const int q = MODE == 2 ? k : k * (N / 2) + i;
+                    float2 c = __fadd2_rn(xv[r].pair(q), m2);
+                    if (MODE == 2) {
+                        if (!ln.any(2 * q)) c.x = 0.0f;
+                        if (!ln.any(2 * q + 1)) c.y = 0.0f;
                     }
+                    b = __ffma2_rn(c, c, b);
                 }
+                if (MODE != 2 && !ln.any(k)) b = f2(0.0f);
+                if (L::may_cut(k)) {
+                    const float c = to_f(xv[r].own(ln, k)) - mu[r];
+                    b.x -= ln.spare(k) * (c * c);
+                }
+                a = __fadd2_rn(a, b);
             }
             s[r] = a.x + a.y;
         }
@@ -231,9 +238,10 @@ template <typename T, int MODE, int TPR, int EPL, int C>
 struct GradShape {
     using S0 = Source<T, MODE, TPR, EPL, C>;
     static constexpr bool OWN = MODE != 2 && TPR < 32;
-    static constexpr int ROW = S0::stage_bytes(), STAGE = 2 * ROW + (OWN ? 2 * 4 * kRowBlock : 0), STAGES = ring_stages(STAGE);
+    static constexpr int ROW = S0::stage_bytes(), STAGE = 2 * ROW + (OWN ? 2 * 4 * kRowBlock : 0), MASKS = S0::L::mask_bytes();
+    static constexpr int STAGES = ring_stages(STAGE, MASKS);
     static constexpr int SUMS = kRowBlock * EPL * 4;                                 // the columns' sums, after the ring's last use
-    static constexpr int SHARED = STAGE * STAGES > SUMS ? STAGE * STAGES : SUMS;
+    static constexpr int SHARED = STAGE * STAGES + MASKS > SUMS ? STAGE * STAGES + MASKS : SUMS;
 };
 
 template <typename T, int MODE, int TPR, int EPL, int C>
@@ -252,9 +260,10 @@ k_norm_grad_rows(const T* __restrict__ dy, int64_t lddy, const T* __restrict__ x
     uint32_t turn = 0, phase = 0;
     int at = 0;
     jn.begin();
-    const L ln(d, x, ldx, lddx);
+    const uint32_t ring0 = (uint32_t)__cvta_generic_to_shared(ring);
+    const L ln(d, x, ldx, lddx, ring0 + H::STAGE * S);
     const Source<T, MODE, TPR, EPL, C> xs(x, ldx, n, d), gs(dy, lddy, n, d);
-    const uint32_t ring0 = (uint32_t)__cvta_generic_to_shared(ring), slot4 = ring0 + 2 * H::ROW + threadIdx.x * 4;
+    const uint32_t slot4 = ring0 + 2 * H::ROW + threadIdx.x * 4;
     const bool lead = L::BULK && (int)threadIdx.x % TPR == 0;
     const float inv_d = 1.0f / (float)d;
     const int64_t step = ln.groups();
@@ -306,6 +315,8 @@ k_norm_grad_rows(const T* __restrict__ dy, int64_t lddy, const T* __restrict__ x
         if (!H::OWN && row + step < n) { mu_next = mean[row + step]; rs_next = rstd[row + step]; }
         xs.take(ln, row, ring0 + o, 0u, xv);
         gs.take(ln, row, ring0 + o + H::ROW, 0u, gv);
+        xv.mend(ln, 0u);
+        gv.mend(ln, 0u);
         if (row >= n) { xv.zero(); gv.zero(); mu = rs = 0.0f; }
         const float2 m2 = f2(-mu), r2 = f2(rs);
         float2 s0 = f2(here ? 0.0f : __int_as_float(0x7fffffff)), s1 = f2(0.0f);
@@ -328,7 +339,7 @@ k_norm_grad_rows(const T* __restrict__ dy, int64_t lddy, const T* __restrict__ x
             const float2 c1 = f2(-s[0] * inv_d), c2 = f2(-s[1] * inv_d);
             if constexpr (AGAIN) {
                 xs.take(ln, row, ring0 + o, 0u, xv);
-                gs.take(ln, row, ring0 + o + H::ROW, 0u, gv);
+                gs.take(ln, row, ring0 + o + H::ROW, 0u, gv);        // (what lies outside the row is not stored)
             }
 #pragma unroll
             for (int q = 0; q < L::PAIRS; ++q) {
@@ -458,10 +469,10 @@ extern "C" int gem_nlr_layer_norm(const void* x_dev, int32_t type, int64_t ld_x,
     cudaError_t rc = cudaSuccess;
     by_mode(type, lie.mode, [&](auto t, auto mode) {
         using T = decltype(t);
-        held = by_width<mode.value != 2 && sizeof(T) == 2 ? 24 : 16, mode.value != 2 && sizeof(T) == 2 ? 32 : 24>(lie.mode == 1 ? (int64_t)d + 16 / tb - 1 : d, [&](auto tpr, auto epl, auto c) {
+        held = by_width<mode.value != 2 && sizeof(T) == 2 ? 16 : 8, mode.value != 2 && sizeof(T) == 2 ? 24 : 16, mode.value != 2 && sizeof(T) == 2 ? 32 : 24>(lie.mode == 1 ? (int64_t)d + 16 / tb - 1 : d, [&](auto tpr, auto epl, auto c) {
             constexpr auto k = k_norm_rows<T, mode.value, tpr.value, epl.value, c.value>;
             constexpr int shared = NormShape<T, mode.value, tpr.value, epl.value, c.value>::SHARED;
-            const int cl = spread(n, kRowBlock / tpr.value, fwd_rows(tpr.value), lie.period, resident_clusters<k, c.value>(shared));
+            const int cl = spread(n, kRowBlock / tpr.value, fwd_rows(tpr.value, epl.value), lie.period, resident_clusters<k, c.value>(shared));
             rc = launch_rows(k, cl * c.value, c.value, shared, false, st, (const T*)x_dev, ld_x, weight_dev, bias_dev, (int)wtype, n, (int)d, eps,
                              (T*)y_dev, ld_y, mean_dev, rstd_dev);
         });
@@ -513,7 +524,7 @@ extern "C" int gem_nlr_layer_norm_backward(const void* dy_dev, int64_t ld_dy, co
     if (n > 0)
         by_mode(type, lie.mode, [&](auto t, auto mode) {
             using T = decltype(t);
-            held = by_width<mode.value != 2 && sizeof(T) == 2 ? 16 : 12, mode.value == 0 && sizeof(T) == 2 ? 24 : 16>(lie.mode == 1 ? (int64_t)d + 16 / tb - 1 : d, [&](auto tpr, auto epl, auto c) {
+            held = by_width<mode.value != 2 && sizeof(T) == 2 ? 16 : 8, mode.value != 2 && sizeof(T) == 2 ? 16 : 12, mode.value == 0 && sizeof(T) == 2 ? 24 : 16>(lie.mode == 1 ? (int64_t)d + 16 / tb - 1 : d, [&](auto tpr, auto epl, auto c) {
                 constexpr auto k = k_norm_grad_rows<T, mode.value, tpr.value, epl.value, c.value>;
                 constexpr int shared = GradShape<T, mode.value, tpr.value, epl.value, c.value>::SHARED;
                 const int most = resident_clusters<k, c.value>(shared), room = norm_records(n, d);

@@ -125,15 +125,15 @@ k_xent_any(const T* z, int64_t ld, const int32_t* __restrict__ labels, int64_t n
 
 // ---- rows in registers -------------------------------------------------------------------------------------------
 
-// Rows that a group works on at a time: two of the narrow ones.
-__host__ __device__ constexpr int xent_rows(int tpr) { return tpr < 32 ? 2 : 1; }
+// Rows that a group works on at a time: two or four of the narrow ones.
+__host__ __device__ constexpr int xent_rows(int tpr, int epl) { return tpr >= 32 ? 1 : epl <= 8 ? 4 : 2; }
 
 template <typename T, int MODE, int TPR, int EPL, int C>
 struct XentShape {
     using S0 = Source<T, MODE, TPR, EPL, C>;
     static constexpr bool OWN = MODE != 2 && TPR < 32;
-    static constexpr int ROWS = xent_rows(TPR), ROW = S0::stage_bytes() + (OWN ? 4 * kRowBlock : 0);       // rows and, if OWN, labels
-    static constexpr int STAGE = ROWS * ROW, STAGES = ring_stages(STAGE), SHARED = STAGE * STAGES;
+    static constexpr int ROWS = xent_rows(TPR, EPL), ROW = S0::stage_bytes() + (OWN ? 4 * kRowBlock : 0);       // rows and, if OWN, labels
+    static constexpr int STAGE = ROWS * ROW, MASKS = S0::L::mask_bytes(), STAGES = ring_stages(STAGE, MASKS), SHARED = STAGE * STAGES + MASKS;
 };
 
 // -inf in every element of a word
@@ -181,9 +181,10 @@ k_xent_rows(const T* z, int64_t ld, const int32_t* __restrict__ labels, int64_t 
     uint32_t turn = 0, phase = 0;
     int at = 0;
     jn.begin();
-    const L ln(k, z, ld, ldd);
+    const uint32_t ring0 = (uint32_t)__cvta_generic_to_shared(ring);
+    const L ln(k, z, ld, ldd, ring0 + H::STAGE * S);
     const Source<T, MODE, TPR, EPL, C> zs(z, ld, n, k);
-    const uint32_t ring0 = (uint32_t)__cvta_generic_to_shared(ring), slot4 = ring0 + H::S0::stage_bytes() + threadIdx.x * 4;
+    const uint32_t slot4 = ring0 + H::S0::stage_bytes() + threadIdx.x * 4;
     const bool lead = L::BULK && (int)threadIdx.x % TPR == 0;
     const float nan = __int_as_float(0x7fffffff);
     const int64_t step = ln.groups();
@@ -222,7 +223,7 @@ k_xent_rows(const T* z, int64_t ld, const int32_t* __restrict__ labels, int64_t 
         Row<T, MODE, EPL> zv[R];
         float m[R], s[R], z_hot[R];
         int lab[R];
-        bool here = true;
+        bool owner[R], here = true;
         if constexpr (L::BULK) {
             lab[0] = base + ln.g < n ? next : -1;
             if (base + step + ln.g < n) next = labels[base + step + ln.g];
@@ -238,12 +239,15 @@ k_xent_rows(const T* z, int64_t ld, const int32_t* __restrict__ labels, int64_t 
             if constexpr (H::OWN) lab[r] = row < n ? (int)read4(slot4 + o) : -1;
             if constexpr (MODE == 2) lab[r] = row < n ? labels[row] : -1;
             zs.take(ln, row, ring0 + o, minus_infinity<T>(), zv[r]);
-            // the label's logit, by the thread that has it
-            const int hot = lab[r] + ln.s - ln.rank * (L::NV * TPR * N), v_hot = hot / N;
-            z_hot[r] = nan;
-            if (lab[r] >= 0 && lab[r] < k && hot >= 0 && v_hot < L::NV * TPR && v_hot % TPR == ln.l) {
-                if (MODE == 2 || (MODE == 1 && (row == 0 || row == n - 1))) z_hot[r] = to_f(z[row * ld + lab[r]]);
-                else z_hot[r] = to_f(reinterpret_cast<const T*>(ring + o + ln.place(v_hot / TPR) * 16)[hot % N]);
+            zv[r].mend(ln, minus_infinity<T>());
+            // the label's logit, right in the thread that has it (and anything elsewhere)
+            const int hot = lab[r] + ln.s - ln.rank * (L::NV * TPR * N);
+            owner[r] = row < n && lab[r] >= 0 && lab[r] < k && hot >= 0 && hot < L::NV * TPR * N && hot / N % TPR == ln.l;
+            if constexpr (MODE == 2) z_hot[r] = owner[r] ? to_f(z[row * ld + lab[r]]) : nan;
+            else {
+                const int v = owner[r] ? hot / N / TPR : 0;
+                z_hot[r] = to_f(reinterpret_cast<const T*>(ring + o + ln.place(v) * 16)[hot & (N - 1)]);
+                if (MODE == 1 && zs.near_end(row) && owner[r]) z_hot[r] = to_f(z[row * ld + lab[r]]);
             }
         }
 #pragma unroll
@@ -276,29 +280,22 @@ k_xent_rows(const T* z, int64_t ld, const int32_t* __restrict__ labels, int64_t 
             const int64_t row = base + r * step + ln.g;
             const bool counts = lab[r] >= 0, known = lab[r] < k, empty = s[r] == 0.0f;
             const float q = !known ? nan : empty ? 0.0f : 1.0f / s[r];
-            // the label's element: its thread has the row's loss and its gradient (p - 1) s; the first thread where there is none
-            const int hot = lab[r] + ln.s - ln.rank * (L::NV * TPR * N), v_hot = hot / N;
-            const bool mine = row < n && (counts && known ? hot >= 0 && v_hot < L::NV * TPR && v_hot % TPR == ln.l : ln.l == 0 && ln.rank == 0);
-            T one;
-            if (mine) {
-                float v = counts ? nan : 0.0f;
-                if (counts && known) {
-                    const float t = z_hot[r] - m[r];
-                    v = empty ? INFINITY : logf(s[r]) - t;
-                    one = from_f<T>(empty ? 0.0f : (exp2_fast(t * kLog2e) * q - 1.0f) * scale);
-                }
+            // the label's thread has the row's loss and its element's gradient (p - 1) s; the first thread where there is none
+            const bool teller = counts && known ? owner[r] : row < n && ln.l == 0 && ln.rank == 0;
+            const float t = z_hot[r] - m[r];
+            const float v = !counts ? 0.0f : !known ? nan : empty ? INFINITY : logf(s[r]) - t;
+            const T one = from_f<T>(empty ? 0.0f : (exp2_fast(t * kLog2e) * q - 1.0f) * scale);
+            if (teller) {
                 row_loss[row] = v;
                 sum += (double)v;
             }
             if (!dz) continue;
-            if (!counts) zv[r].zero();
-            else {
-                const float2 q2 = f2(q * scale);
+            const float2 q2 = f2(q * scale);
 #pragma unroll
-                for (int p = 0; p < L::PAIRS; ++p) zv[r].set_pair(p, __fmul2_rn(e2[r][p], q2));
-            }
+            for (int p = 0; p < L::PAIRS; ++p) zv[r].set_pair(p, __fmul2_rn(e2[r][p], q2));
+            if (!counts) zv[r].zero();
             zv[r].store(ln, dz, row, ldd, row < n, n, ed);   // (ends with the warp's lanes in step: no store of theirs comes after)
-            if (mine && counts && known) dz[row * ldd + lab[r]] = one;
+            if (owner[r]) dz[row * ldd + lab[r]] = one;
         }
     }
     if (!scaled) grid_ready();
@@ -336,11 +333,11 @@ extern "C" int gem_nlr_label_cross_entropy(const void* logits_dev, int32_t type,
     cudaError_t rc = cudaSuccess;
     by_mode(type, lie.mode, [&](auto t, auto mode) {
         using T = decltype(t);
-        const bool held = by_width<mode.value != 2 && sizeof(T) == 2 ? 24 : 16, mode.value != 2 && sizeof(T) == 2 ? 32 : 24>(lie.mode == 1 ? (int64_t)k + 16 / tb - 1 : k, [&](auto tpr, auto epl, auto c) {
+        const bool held = by_width<mode.value != 2 && sizeof(T) == 2 ? 16 : 8, mode.value != 2 && sizeof(T) == 2 ? 24 : 16, mode.value != 2 && sizeof(T) == 2 ? 32 : 24>(lie.mode == 1 ? (int64_t)k + 16 / tb - 1 : k, [&](auto tpr, auto epl, auto c) {
             constexpr auto kern = k_xent_rows<T, mode.value, tpr.value, epl.value, c.value>;
             constexpr int shared = XentShape<T, mode.value, tpr.value, epl.value, c.value>::SHARED;
             const int most = resident_clusters<kern, c.value>(shared);
-            const int cl = spread(n, kRowBlock / tpr.value, xent_rows(tpr.value), lie.period, most < kMaxBlocks / c.value ? most : kMaxBlocks / c.value);
+            const int cl = spread(n, kRowBlock / tpr.value, xent_rows(tpr.value, epl.value), lie.period, most < kMaxBlocks / c.value ? most : kMaxBlocks / c.value);
             rc = launch_rows(kern, cl * c.value, c.value, shared, true, st, (const T*)logits_dev, ld, labels_dev, n, (int)k, (int)mean, sc, loss_dev,
                              row_loss_dev, (T*)dlogits_dev, ld_d);
         });

@@ -8,8 +8,8 @@
 //   0  every row begins and ends at a multiple of 16 bytes: vectors of 16 bytes, s = 0
 //   1  rows begin anywhere: still vectors of 16 bytes at multiples of 16, beginning s elements before the row.  s depends on
 //      the row's number modulo 16 bytes / element only, and a group's rows are that far apart (see spread()), so a thread's
-//      columns are the same in all its rows.  The first and the last vector hold elements of the neighbouring rows (or of
-//      the padding), which are replaced after loading and left alone in storing
+//      columns are the same in all its rows.  The first and the last vector may be cut: they hold elements of the
+//      neighbouring rows (or of the padding) too, which are replaced after loading and left alone in storing
 //   2  element by element, where the matrices of one call lie differently to 16 bytes
 //
 // In modes 0 and 1 rows come through a ring of stages in shared memory, S rows ahead: registers alone hold too few bytes in
@@ -160,6 +160,7 @@ struct Lane {
     static constexpr int N = MODE == 2 ? 1 : 16 / (int)sizeof(T);
     static constexpr int NV = EPL / N, GROUPS = kRowBlock / TPR;
     static constexpr int PAIRS = EPL / 2;            // pair q holds the thread's elements 2 q and 2 q + 1
+    static constexpr int LANES = TPR * C, STRIDE = TPR * N;           // elements from a thread's vector to its next
     static constexpr bool BULK = MODE != 2 && TPR >= 32;
     // Elements of cut vectors are stored one each by other lanes of the warp, through EDGES places of 16 bytes a warp; rows
     // of less than 8 threads have more ends than that pays for.
@@ -169,35 +170,34 @@ struct Lane {
     static_assert(EPL % N == 0 && EPL % 2 == 0, "");
 
     int l, g, s, d, rank;
-    int last;                                        // k of the row's last vector, in the block that has it; else never reached
-    uint32_t head[MODE == 1 ? 4 : 1], tail[MODE == 1 ? 4 : 1];   // the row's part of vector 0 and of vector `last`, as words
-    uint32_t head_bits, tail_bits;                               // and as a bit an element
-    int64_t edge[TURNS];                                         // elements that this lane stores for cut vectors: from its own row's
-    int edge_group[TURNS];                                       // beginning, and of which group; -1: none
+    uint32_t wholes;                                 // bit k: vector k lies within the row (MODE 1)
+    bool head;                                       // the thread's vector 0 is the row's first, and cut
+    int tail;                                        // the thread's vector that is the row's last, and cut; -1: none
+    int64_t edge[TURNS];                             // elements that this lane stores for cut vectors: from its own row's
+    int edge_group[TURNS];                           // beginning, and of which group; -1: none
 
-    __device__ __forceinline__ Lane(int d_, const T* base, int64_t ld, int64_t ld_out)
-        : l((int)threadIdx.x % TPR), g((int)threadIdx.x / TPR), s(0), d(d_), rank(C > 1 ? (int)cluster_rank() : 0)
+    // Vectors that a cut can be in: the first, and from LATEST / 2 - 1 on (a row fills more than half of its shape's places,
+    // less a vector; in clusters the last block may have a few only, and the narrowest shape takes every row there is).
+    static constexpr int CUTS_FROM = C > 1 || TPR == 2 ? 0 : (NV + 1) / 2 - 1;
+    __host__ __device__ static constexpr bool may_cut(int k) { return MODE == 1 && (k == 0 || k >= CUTS_FROM); }
+    __host__ __device__ static constexpr int mask_bytes() { return MODE == 1 ? NV * 16 * kRowBlock : 0; }
+    uint32_t masks;                                  // shared memory: the row's part of the thread's vectors, as bits
+
+    // `masks_`: mask_bytes() of the block's shared memory; each thread reads what it has written there itself
+    __device__ __forceinline__ Lane(int d_, const T* base, int64_t ld, int64_t ld_out, uint32_t masks_)
+        : l((int)threadIdx.x % TPR), g((int)threadIdx.x / TPR), s(0), d(d_), rank(C > 1 ? (int)cluster_rank() : 0), wholes(0), head(false), tail(-1), masks(masks_ + threadIdx.x * 16)
     {
         if constexpr (MODE == 1) {
             s = lies(base, ld, group());
-            const int v_last = (s + d - 1) / N - rank * NV * TPR;
-            last = v_last < 0 ? -1 : v_last / TPR;   // (NV and more: another block's)
-            head_bits = tail_bits = 0;
 #pragma unroll
-            for (int i = 0; i < N; ++i) {
-                if (first(0) + i >= 0 && (last != 0 || first(0) + i < d)) head_bits |= 1u << i;
-                if (first(last) + i < d) tail_bits |= 1u << i;
-            }
-#pragma unroll
-            for (int w = 0; w < 4; ++w) {
-                constexpr int E = 4 / (int)sizeof(T);
-                constexpr uint32_t ONE = E == 1 ? 0xffffffffu : 0xffffu;
-                head[w] = tail[w] = 0;
-#pragma unroll
-                for (int j = 0; j < E; ++j) {
-                    if (head_bits >> (w * E + j) & 1) head[w] |= ONE << (16 * j);
-                    if (tail_bits >> (w * E + j) & 1) tail[w] |= ONE << (16 * j);
-                }
+            for (int k = 0; k < NV; ++k) {
+                const int lo = first(k), hi = lo + N;
+                if (lo >= 0 && hi <= d) wholes |= 1u << k;
+                else if (lo < 0) head = true;
+                else if (lo < d && (k | rank | l) == 0) head = true;     // a row within one vector
+                else if (lo < d) tail = k;
+                const uint4 m = words_of(lo);
+                asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(masks + k * 16 * kRowBlock), "r"(m.x), "r"(m.y), "r"(m.z), "r"(m.w) : "memory");
             }
             if constexpr (EDGED) {
                 const int lane = threadIdx.x & 31;
@@ -220,6 +220,35 @@ struct Lane {
             }
         }
     }
+    // the row's part of the vector whose first element is e, as bits
+    __device__ __forceinline__ uint4 words_of(int e) const
+    {
+        uint32_t m[4];
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+            constexpr int E = 4 / (int)sizeof(T);
+            constexpr uint32_t ONE = E == 1 ? 0xffffffffu : 0xffffu;
+            m[w] = 0;
+#pragma unroll
+            for (int j = 0; j < E; ++j)
+                if (e + w * E + j >= 0 && e + w * E + j < d) m[w] |= ONE << (16 * j);
+        }
+        return make_uint4(m[0], m[1], m[2], m[3]);
+    }
+    // elements of vector k that are not the row's, where it has any of the row's
+    __device__ __forceinline__ float spare(int k) const
+    {
+        const int lo = first(k);
+        return any(k) ? (float)(max(-lo, 0) + max(lo + N - d, 0)) : 0.0f;
+    }
+    __device__ __forceinline__ uint4 mask(int k) const
+    {
+        uint4 m;
+        asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(m.x), "=r"(m.y), "=r"(m.z), "=r"(m.w) : "r"(masks + k * 16 * kRowBlock) : "memory");
+        return m;
+    }
+    // place of the group's ends (a first and a last vector) among the block's; with more than a warp to a group, of the warp's
+    __device__ __forceinline__ int place_of_ends() const { return TPR >= 32 ? (int)threadIdx.x / 32 : g; }
     static __device__ __forceinline__ int lies(const T* base, int64_t ld, int64_t row)
     {
         return (int)((reinterpret_cast<uintptr_t>(base + row * ld) & 15) / sizeof(T));
@@ -230,16 +259,18 @@ struct Lane {
     __device__ __forceinline__ int64_t groups() const { return (int64_t)(gridDim.x / C) * GROUPS; }
     __device__ __forceinline__ int first(int k) const { return ((rank * NV + k) * TPR + l) * N - (MODE == 1 ? s : 0); }
     __device__ __forceinline__ bool any(int k) const { return first(k) < d; }
-    // whether vector k may be cut by an end of the row (the same for all lanes of the group)
-    __device__ __forceinline__ bool end(int k) const { return MODE == 1 && ((k == 0 && rank == 0) || k == last); }
-    __device__ __forceinline__ uint32_t bits(int k) const { return k == 0 && rank == 0 ? head_bits : tail_bits; }      // where end(k)
+    __device__ __forceinline__ bool whole(int k) const { return MODE == 1 ? (wholes >> k & 1) != 0 : any(k); }
     __device__ __forceinline__ bool holds(int k, int i) const { return MODE == 1 ? first(k) + i >= 0 && first(k) + i < d : any(k); }
     // place of the thread's vector k in a stage, in vectors
     __device__ __forceinline__ int place(int k) const { return BULK ? (g * NV + k) * TPR + l : k * kRowBlock + (int)threadIdx.x; }
 };
 
-// Shared memory of cut vectors on their way out.
-template <typename LN> struct Edges { uint4 v[LN::EDGED ? kRowBlock / 32 * LN::ENDS : 1]; };
+// Shared memory for the ends of rows: cut vectors on their way out.
+template <typename LN>
+struct Edges {
+    static constexpr int PLACES = LN::GROUPS < kRowBlock / 32 ? 2 * (kRowBlock / 32) : 2 * LN::GROUPS;
+    uint4 v[LN::EDGED ? PLACES : 1];
+};
 
 // The thread's elements of one row.
 template <typename T, int MODE, int EPL>
@@ -255,25 +286,28 @@ struct Row {
     {
         T* p = base + row * ld;
         if (ok) {
+            T* mine = p + ln.first(0);
 #pragma unroll
             for (int k = 0; k < NV; ++k) {
-                const int e = ln.first(k);
                 if constexpr (MODE == 2) {
-                    if (ln.any(k)) p[e] = v[k].e;
-                } else if (!ln.end(k)) {
-                    if (ln.any(k)) v[k].store(p + e);
+                    if (ln.any(k)) mine[k * LN::STRIDE] = v[k].e;
                 } else {
-                    const uint32_t b = ln.bits(k);
-                    if (b == (1u << N) - 1) v[k].store(p + e);
-                    else if constexpr (LN::EDGED) {
-                        const int at = (int)threadIdx.x / 32 * LN::ENDS + (LN::ENDS > 2 ? ln.g % (LN::ENDS / 2) * 2 : 0) + (k == 0 && ln.rank == 0 && ln.l == 0 ? 0 : 1);
-                        if (b) ed.v[at] = v[k].raw;
-                    } else if (b) {
+                    if (ln.whole(k)) v[k].store(mine + k * LN::STRIDE);
+                }
+            }
+            if constexpr (LN::EDGED) {
+                if (ln.head) ed.v[2 * ln.place_of_ends()] = v[0].raw;
+#pragma unroll
+                for (int k = 0; k < NV; ++k)
+                    if (k == ln.tail) ed.v[2 * ln.place_of_ends() + 1] = v[k].raw;
+            } else if constexpr (MODE == 1) {
+#pragma unroll
+                for (int k = 0; k < NV; ++k)
+                    if ((k == 0 && ln.head) || k == ln.tail) {
 #pragma unroll
                         for (int i = 0; i < N; ++i)
-                            if (b & (1u << i)) p[e + i] = v[k].at(i);
+                            if (ln.holds(k, i)) mine[k * LN::STRIDE + i] = v[k].at(i);
                     }
-                }
             }
         }
         if constexpr (LN::EDGED) {
@@ -284,6 +318,58 @@ struct Row {
                 if (ln.edge_group[t] >= 0 && row + (ln.edge_group[t] - ln.g) < n) p[ln.edge[t]] = places[(threadIdx.x & 31) + 32 * t];
             __syncwarp();
         }
+    }
+    // What stands in cut vectors for elements that are not the row's: the bits of a word.  (No branches here and below: a
+    // divergent one costs more than masking every vector that could be cut.)
+    template <typename LN>
+    __device__ __forceinline__ void mend(const LN& ln, uint32_t none)
+    {
+        if constexpr (MODE == 1) {
+#pragma unroll
+            for (int k = 0; k < NV; ++k)
+                if (LN::may_cut(k)) blend(v[k], none, ln.mask(k));
+        }
+    }
+    // The same with copies of one of the row's elements in each cut vector (its last in the row's first vector, its first in
+    // the others); it is what stands there afterwards that the sums are corrected by, which loses no more than as many
+    // roundings as there are copies, wherever zero lies.
+    template <typename LN>
+    __device__ __forceinline__ void mend_own(const LN& ln)
+    {
+        if constexpr (MODE == 1) {
+#pragma unroll
+            for (int k = 0; k < NV; ++k)
+                if (LN::may_cut(k)) blend(v[k], twice(own(ln, k)), ln.mask(k));
+        }
+    }
+    template <typename LN>
+    __device__ __forceinline__ T own(const LN& ln, int k) const
+    {
+        if constexpr (MODE == 2) return v[k].e;
+        else return own_of(ln, k);
+    }
+    template <typename LN>
+    __device__ __forceinline__ T own_of(const LN& ln, int k) const
+    {
+        T one = ln.first(k) < 0 ? v[k].at(N - 1) : v[k].at(0);
+        if (LN::NV * LN::LANES * N <= 16 && ln.first(k) < 0 && ln.d < N - ln.s) {        // the whole row within one vector
+#pragma unroll
+            for (int i = 0; i < N; ++i)
+                if (i == ln.s) one = v[k].at(i);
+        }
+        return one;
+    }
+    static __device__ __forceinline__ uint32_t twice(T x)
+    {
+        if constexpr (sizeof(T) == 4) return *reinterpret_cast<uint32_t*>(&x);
+        else return *reinterpret_cast<uint16_t*>(&x) * 0x10001u;
+    }
+    static __device__ __forceinline__ void blend(V& x, uint32_t none, uint4 m)
+    {
+        x.w[0] = (x.w[0] & m.x) | (none & ~m.x);
+        x.w[1] = (x.w[1] & m.y) | (none & ~m.y);
+        x.w[2] = (x.w[2] & m.z) | (none & ~m.z);
+        x.w[3] = (x.w[3] & m.w) | (none & ~m.w);
     }
     __device__ __forceinline__ float2 pair(int q) const
     {
@@ -312,7 +398,9 @@ struct Source {
     __host__ __device__ static constexpr int stage_bytes() { return MODE == 2 ? 0 : NV * 16 * kRowBlock; }
     const T* base;
     int64_t  ld, n, span;                            // span: elements from the matrix's first to its last
-    __device__ __forceinline__ Source(const T* p, int64_t ld_, int64_t n_, int d) : base(p), ld(ld_), n(n_), span((n_ - 1) * ld_ + d) {}
+    int64_t  near;                                   // rows that begin within N elements of the matrix's first
+    __device__ __forceinline__ Source(const T* p, int64_t ld_, int64_t n_, int d)
+        : base(p), ld(ld_), n(n_), span((n_ - 1) * ld_ + d), near(ld_ >= N ? 1 : ld_ > 0 ? (N - 1) / ld_ + 1 : n_) {}
 
     // Before the first send: what no copy will write reads as `none` (the vectors beyond the row).
     __device__ __forceinline__ void prepare(const L& ln, uint32_t stage, uint32_t none) const
@@ -342,42 +430,44 @@ struct Source {
     // What every thread of a narrower group sends for.
     __device__ __forceinline__ void send_own(const L& ln, int64_t row, uint32_t stage) const
     {
-        const int64_t at = row * ld;
+        const T* mine = base + row * ld + ln.first(0);
 #pragma unroll
-        for (int k = 0; k < NV; ++k) {
-            const int e = ln.first(k);
-            if (row < n && ln.any(k)) {
-                if (!ln.end(k) || (at + e >= 0 && at + e + N <= span)) copy_ahead(stage + (uint32_t)ln.place(k) * 16, base + at + e, 16);
-            }
-        }
+        for (int k = 0; k < NV; ++k)
+            if (row < n && ln.any(k) && (MODE == 0 || ln.whole(k) || within(ln, row, k)))
+                copy_ahead(stage + (uint32_t)ln.place(k) * 16, mine + k * L::STRIDE, 16);
     }
-    // The row that was sent for, once its copies are complete.
+    // whether a vector of the row may reach over one of the matrix's ends
+    __device__ __forceinline__ bool near_end(int64_t row) const { return row < near || row >= n - near; }
+    // whether the thread's vector k of the row lies between the matrix's ends
+    __device__ __forceinline__ bool within(const L& ln, int64_t row, int k) const
+    {
+        const int64_t at = row * ld + ln.first(k);
+        return at >= 0 && at + N <= span;
+    }
+    // The row that was sent for, once its copies are complete; cut vectors are not mended yet.
     __device__ __forceinline__ void take(const L& ln, int64_t row, uint32_t stage, uint32_t none, Row<T, MODE, EPL>& r) const
     {
 #pragma unroll
         for (int k = 0; k < NV; ++k) {
-            const int e = ln.first(k);
             if constexpr (MODE == 2) {
                 const uint32_t x = none;
-                if (row < n && ln.any(k)) r.v[k].e = base[row * ld + e]; else r.v[k].e = *reinterpret_cast<const T*>(&x);
+                if (row < n && ln.any(k)) r.v[k].e = base[row * ld + ln.first(k)]; else r.v[k].e = *reinterpret_cast<const T*>(&x);
             } else {
                 asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];"
                              : "=r"(r.v[k].w[0]), "=r"(r.v[k].w[1]), "=r"(r.v[k].w[2]), "=r"(r.v[k].w[3])
                              : "r"(stage + (uint32_t)ln.place(k) * 16) : "memory");
-                if (ln.end(k)) {
-                    const int64_t at = row * ld + e;
-                    if ((at < 0 || at + N > span) && row < n) {      // a vector that reaches over the matrix's own end
+            }
+        }
+        if constexpr (MODE == 1) {
+            if (row < n && near_end(row)) {          // vectors that reach over the matrix's own ends came through no copy
+
+#pragma unroll
+                for (int k = 0; k < NV; ++k)
+                    if (((k == 0 && ln.head) || k == ln.tail) && !within(ln, row, k)) {
 #pragma unroll
                         for (int i = 0; i < N; ++i)
-                            if (ln.holds(k, i)) r.v[k].set(i, base[at + i]);
+                            if (ln.holds(k, i)) r.v[k].set(i, base[row * ld + ln.first(k) + i]);
                     }
-                    const bool h = k == 0 && ln.rank == 0;
-#pragma unroll
-                    for (int w = 0; w < 4; ++w) {
-                        const uint32_t m = h ? ln.head[w] : ln.tail[w];
-                        r.v[k].w[w] = (r.v[k].w[w] & m) | (none & ~m);
-                    }
-                }
             }
         }
     }
@@ -498,16 +588,17 @@ template <int V> struct Const { static constexpr int value = V; };
 // f(TPR, EPL, C) as constants for rows of `width` elements (the window's s included), false if it is wider than eight blocks
 // hold.  Few threads a row and many elements a thread keep the work per row (sums over the group, labels, statistics) small;
 // what bounds EPL are 128 registers next to weights and sums: E1 or E2 elements from a warp a row on (E1 TPR > E2 TPR / 2).
+// Narrower rows: E0, two vectors to a thread, so that neighbouring threads read whole sectors of 32 bytes.
 // Rows wider than 256 E2 go to clusters of blocks, so that every SM still has two blocks, one of which loads while the
 // other adds.
-template <int E1, int E2, typename F>
+template <int E0, int E1, int E2, typename F>
 bool by_width(int64_t width, F f)
 {
-    if (width <= 16) f(Const<1>{}, Const<16>{}, Const<1>{});
-    else if (width <= 32) f(Const<2>{}, Const<16>{}, Const<1>{});
-    else if (width <= 64) f(Const<4>{}, Const<16>{}, Const<1>{});
-    else if (width <= 128) f(Const<8>{}, Const<16>{}, Const<1>{});
-    else if (width <= 256) f(Const<16>{}, Const<16>{}, Const<1>{});
+    if (width <= 16) f(Const<2>{}, Const<8>{}, Const<1>{});
+    else if (width <= 32) f(Const<32 / E0>{}, Const<E0>{}, Const<1>{});
+    else if (width <= 64) f(Const<64 / E0>{}, Const<E0>{}, Const<1>{});
+    else if (width <= 128) f(Const<128 / E0>{}, Const<E0>{}, Const<1>{});
+    else if (width <= 256) f(Const<256 / E0>{}, Const<E0>{}, Const<1>{});
     else if (width <= 512) f(Const<32>{}, Const<16>{}, Const<1>{});
     else if (E2 > 16 && width <= 32 * E1) f(Const<32>{}, Const<(E2 > 16 ? E1 : 16)>{}, Const<1>{});
     else if (E2 > 16 && width <= 32 * E2) f(Const<32>{}, Const<(E2 > 16 ? E2 : 16)>{}, Const<1>{});
@@ -527,8 +618,12 @@ bool by_width(int64_t width, F f)
     return true;
 }
 
-// Stages of a ring whose stage takes `bytes`: up to four, within a half of an SM's shared memory (two blocks an SM).
-__host__ __device__ constexpr int ring_stages(int bytes) { return bytes == 0 ? 1 : 98304 / bytes < 2 ? 2 : 98304 / bytes > 4 ? 4 : 98304 / bytes; }
+// Stages of a ring whose stage takes `bytes`: two to four, within a half of an SM's shared memory (two blocks an SM) less
+// `others`.
+__host__ __device__ constexpr int ring_stages(int bytes, int others)
+{
+    return bytes == 0 ? 1 : (104448 - others) / bytes < 2 ? 2 : (104448 - others) / bytes > 4 ? 4 : (104448 - others) / bytes;
+}
 
 // One matrix operand of a call.
 struct Matrix {
