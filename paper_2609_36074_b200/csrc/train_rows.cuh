@@ -172,7 +172,8 @@ struct Lane {
     int l, g, s, d, rank;
     uint32_t wholes;                                 // bit k: vector k lies within the row (MODE 1)
     bool head;                                       // the thread's vector 0 is the row's first, and cut
-    int tail;                                        // the thread's vector that is the row's last, and cut; -1: none
+    uint32_t tail;                                   // bit k: vector k is the row's last, not its first, and cut.  (A number to compare
+                                                     // k with would make the compiler index the row, and so hold it in local memory.)
     int64_t edge[TURNS];                             // elements that this lane stores for cut vectors: from its own row's
     int edge_group[TURNS];                           // beginning, and of which group; -1: none
 
@@ -185,7 +186,7 @@ struct Lane {
 
     // `masks_`: mask_bytes() of the block's shared memory; each thread reads what it has written there itself
     __device__ __forceinline__ Lane(int d_, const T* base, int64_t ld, int64_t ld_out, uint32_t masks_)
-        : l((int)threadIdx.x % TPR), g((int)threadIdx.x / TPR), s(0), d(d_), rank(C > 1 ? (int)cluster_rank() : 0), wholes(0), head(false), tail(-1), masks(masks_ + threadIdx.x * 16)
+        : l((int)threadIdx.x % TPR), g((int)threadIdx.x / TPR), s(0), d(d_), rank(C > 1 ? (int)cluster_rank() : 0), wholes(0), head(false), tail(0), masks(masks_ + threadIdx.x * 16)
     {
         if constexpr (MODE == 1) {
             s = lies(base, ld, group());
@@ -195,7 +196,7 @@ struct Lane {
                 if (lo >= 0 && hi <= d) wholes |= 1u << k;
                 else if (lo < 0) head = true;
                 else if (lo < d && (k | rank | l) == 0) head = true;     // a row within one vector
-                else if (lo < d) tail = k;
+                else if (lo < d) tail |= 1u << k;
                 const uint4 m = words_of(lo);
                 asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(masks + k * 16 * kRowBlock), "r"(m.x), "r"(m.y), "r"(m.z), "r"(m.w) : "memory");
             }
@@ -299,11 +300,11 @@ struct Row {
                 if (ln.head) ed.v[2 * ln.place_of_ends()] = v[0].raw;
 #pragma unroll
                 for (int k = 0; k < NV; ++k)
-                    if (k == ln.tail) ed.v[2 * ln.place_of_ends() + 1] = v[k].raw;
+                    if (ln.tail >> k & 1) ed.v[2 * ln.place_of_ends() + 1] = v[k].raw;
             } else if constexpr (MODE == 1) {
 #pragma unroll
                 for (int k = 0; k < NV; ++k)
-                    if ((k == 0 && ln.head) || k == ln.tail) {
+                    if ((k == 0 && ln.head) || (ln.tail >> k & 1)) {
 #pragma unroll
                         for (int i = 0; i < N; ++i)
                             if (ln.holds(k, i)) mine[k * LN::STRIDE + i] = v[k].at(i);
@@ -463,7 +464,7 @@ struct Source {
 
 #pragma unroll
                 for (int k = 0; k < NV; ++k)
-                    if (((k == 0 && ln.head) || k == ln.tail) && !within(ln, row, k)) {
+                    if (((k == 0 && ln.head) || (ln.tail >> k & 1)) && !within(ln, row, k)) {
 #pragma unroll
                         for (int i = 0; i < N; ++i)
                             if (ln.holds(k, i)) r.v[k].set(i, base[row * ld + ln.first(k) + i]);
