@@ -124,7 +124,7 @@ k_norm_rows(const T* __restrict__ x, int64_t ldx, const void* __restrict__ w, co
     using H = NormShape<T, MODE, TPR, EPL, C>;
     constexpr int R = H::ROWS, N = L::N, S = H::STAGES;
     extern __shared__ __align__(128) unsigned char ring[];
-    __shared__ Join<L, TPR, C, R, S> jn;
+    __shared__ Join<L, TPR, C, (TPR > 32 ? 3 : R), S> jn;
     __shared__ Edges<L> ed;
     uint32_t turn = 0, phase = 0;
     int at = 0;
@@ -134,6 +134,16 @@ k_norm_rows(const T* __restrict__ x, int64_t ldx, const void* __restrict__ w, co
     const Source<T, MODE, TPR, EPL, C> xs(x, ldx, n, d);
     const bool lead = L::BULK && (int)threadIdx.x % TPR == 0;
     const float inv_d = 1.0f / (float)d;
+    const float head_spares = ln.head_spares(), tail_spares = ln.tail_spares();
+    float warp_n = (float)d;                         // the row's elements that this warp has, where it has not all of them
+    if constexpr (TPR > 32) {
+        float c[1] = {0.0f};
+        for (int k = 0; k < L::NV; ++k)
+            for (int i = 0; i < N; ++i) c[0] += ln.holds(k, i);
+        warp_all<SumOp, TPR>(c);
+        warp_n = c[0];
+    }
+    const float inv_n = warp_n > 0.0f ? 1.0f / warp_n : 0.0f;
     const int64_t step = ln.groups();
     // the rows of the iteration that begins at `base`
     const auto send = [&](int64_t base, int stage) {
@@ -162,6 +172,7 @@ k_norm_rows(const T* __restrict__ x, int64_t ldx, const void* __restrict__ w, co
     load_weights<T>(ln, b, wtype, 0.0f, b2);
     for (int64_t base = ln.first_group(); base < n; base += R * step) {
         Row<T, MODE, EPL> xv[R];
+        float2 sp[R];
         float s[R], mu[R];
         bool here = true;
         if constexpr (L::BULK) {
@@ -178,17 +189,15 @@ k_norm_rows(const T* __restrict__ x, int64_t ldx, const void* __restrict__ w, co
 #pragma unroll
             for (int q = 0; q < L::PAIRS; ++q) a = __fadd2_rn(a, xv[r].pair(q));
             s[r] = a.x + a.y;
-            if constexpr (MODE == 1)
-#pragma unroll
-                for (int k = 0; k < L::NV; ++k)
-                    if (L::may_cut(k)) s[r] -= ln.spare(k) * to_f(xv[r].own(ln, k));
+            if constexpr (MODE == 1) {
+                sp[r] = xv[r].spares(ln);
+                s[r] -= head_spares * sp[r].x + tail_spares * sp[r].y;
+            }
         }
-        group_all<SumOp, TPR, C>(s, jn, turn);
-        if constexpr (L::BULK) send(base + S * step, at);        // every thread of the group has its part of the row
-        if (++at == S) { at = 0; phase ^= 1; }
+        warp_all<SumOp, TPR>(s);
 #pragma unroll
         for (int r = 0; r < R; ++r) {
-            mu[r] = s[r] * inv_d;
+            mu[r] = s[r] * inv_n;                    // of the group's, or the warp's, elements
             const float2 m2 = f2(-mu[r]);
             float2 a = f2(0.0f);
 #pragma unroll
@@ -205,15 +214,31 @@ k_norm_rows(const T* __restrict__ x, int64_t ldx, const void* __restrict__ w, co
                     b = __ffma2_rn(c, c, b);
                 }
                 if (MODE != 2 && !ln.any(k)) b = f2(0.0f);
-                if (L::may_cut(k)) {
-                    const float c = to_f(xv[r].own(ln, k)) - mu[r];
-                    b.x -= ln.spare(k) * (c * c);
-                }
                 a = __fadd2_rn(a, b);
             }
             s[r] = a.x + a.y;
+            if constexpr (MODE == 1) {
+                const float ch = sp[r].x - mu[r], ct = sp[r].y - mu[r];
+                s[r] -= head_spares * (ch * ch) + tail_spares * (ct * ct);
+            }
         }
-        group_all<SumOp, TPR, C>(s, jn, turn);
+        warp_all<SumOp, TPR>(s);
+        if constexpr (TPR > 32) {
+            // each warp's count, mean and sum of squares about it, to the row's: the squares about the row's mean are the
+            // warp's own and count (warp's mean - mean)^2.  One meeting of the group a row, and no cancellation.
+            float v[3][2];
+            const float mine[3] = {warp_n, mu[0], s[0]};
+            group_join<TPR, C>(mine, v, jn, turn);
+            float t = v[0][0] * v[1][0] + v[0][1] * v[1][1];
+            join_all<SumOp, TPR, C>(t);
+            mu[0] = t * inv_d;
+            const float c0 = v[1][0] - mu[0], c1 = v[1][1] - mu[0];
+            t = v[2][0] + v[0][0] * (c0 * c0) + (v[2][1] + v[0][1] * (c1 * c1));
+            join_all<SumOp, TPR, C>(t);
+            s[0] = t;
+        }
+        if constexpr (L::BULK) send(base + S * step, at);        // every thread of the group has its part of the row
+        if (++at == S) { at = 0; phase ^= 1; }
 #pragma unroll
         for (int r = 0; r < R; ++r) {
             const int64_t row = base + r * step + ln.g;
@@ -329,7 +354,7 @@ k_norm_grad_rows(const T* __restrict__ dy, int64_t lddy, const T* __restrict__ x
             s1 = __ffma2_rn(gw, h, s1);
         }
         float s[2] = {s0.x + s0.y, s1.x + s1.y};
-        group_all<SumOp, TPR, C>(s, jn, turn);
+        group_sum<TPR, C>(s, jn, turn);
         // every thread of the group is done with this row's stage, or (where it reads it again) with the one before
         if constexpr (L::BULK && !AGAIN) send(row + S * step, at);
         if constexpr (AGAIN) {

@@ -176,7 +176,7 @@ k_xent_rows(const T* z, int64_t ld, const int32_t* __restrict__ labels, int64_t 
     constexpr int N = L::N, R = H::ROWS, S = H::STAGES;
     constexpr float kLog2e = 1.4426950408889634f;
     extern __shared__ __align__(128) unsigned char ring[];
-    __shared__ Join<L, TPR, C, R, S> jn;
+    __shared__ Join<L, TPR, C, (TPR > 32 ? 2 : R), S> jn;
     __shared__ Edges<L> ed;
     uint32_t turn = 0, phase = 0;
     int at = 0;
@@ -252,13 +252,13 @@ k_xent_rows(const T* z, int64_t ld, const int32_t* __restrict__ labels, int64_t 
         }
 #pragma unroll
         for (int r = 0; r < R; ++r) m[r] = row_max<T, MODE, EPL>(zv[r]);
-        group_all<MaxOp, TPR, C>(m, jn, turn);
-        if constexpr (L::BULK) send(base + S * step, at);        // every thread of the group has its part of the row
-        if (++at == S) { at = 0; phase ^= 1; }
+        warp_all<MaxOp, TPR>(m);                     // of the group's, or the warp's, elements
         float2 e2[R][L::PAIRS];
+        bool bare = false;
 #pragma unroll
         for (int r = 0; r < R; ++r) {
-            if (m[r] == -INFINITY) m[r] = 0.0f;              // nothing but -inf (or NaN): no -inf - -inf below
+            bare = m[r] == -INFINITY;                // nothing but -inf (or NaN): no -inf - -inf below
+            if (bare) m[r] = 0.0f;
             const float2 m2 = f2(-m[r]);
             float2 a = f2(here ? 0.0f : nan);
 #pragma unroll
@@ -269,7 +269,27 @@ k_xent_rows(const T* z, int64_t ld, const int32_t* __restrict__ labels, int64_t 
             }
             s[r] = a.x + a.y;
         }
-        group_all<SumOp, TPR, C>(s, jn, turn);
+        warp_all<SumOp, TPR>(s);
+        float down[R];                               // to the row's maximum from the warp's
+#pragma unroll
+        for (int r = 0; r < R; ++r) down[r] = 1.0f;
+        if constexpr (TPR > 32) {
+            // each warp's maximum and sum to the row's, at one meeting of the group a row
+            float v[2][2];
+            const float mine[2] = {bare ? -INFINITY : m[0], s[0]}, m_warp = m[0];
+            group_join<TPR, C>(mine, v, jn, turn);
+            constexpr bool MANY = TPR / 32 * C == 64;
+            float t = MANY ? fmaxf(v[0][0], v[0][1]) : v[0][0];
+            join_all<MaxOp, TPR, C>(t);
+            m[0] = t == -INFINITY ? 0.0f : t;
+            t = v[1][0] * exp2_fast((v[0][0] - m[0]) * kLog2e);
+            if (MANY) t += v[1][1] * exp2_fast((v[0][1] - m[0]) * kLog2e);
+            join_all<SumOp, TPR, C>(t);
+            s[0] = t;
+            down[0] = exp2_fast((bare ? -INFINITY : m_warp - m[0]) * kLog2e);
+        }
+        if constexpr (L::BULK) send(base + S * step, at);        // every thread of the group has its part of the row
+        if (++at == S) { at = 0; phase ^= 1; }
         if (!scaled) {                                        // the first rows are worked on while the labels are counted
             grid_ready();
             scale = loss_scale(sc, mean);
@@ -290,7 +310,7 @@ k_xent_rows(const T* z, int64_t ld, const int32_t* __restrict__ labels, int64_t 
                 sum += (double)v;
             }
             if (!dz) continue;
-            const float2 q2 = f2(q * scale);
+            const float2 q2 = f2(q * down[r] * scale);
 #pragma unroll
             for (int p = 0; p < L::PAIRS; ++p) zv[r].set_pair(p, __fmul2_rn(e2[r][p], q2));
             if (!counts) zv[r].zero();

@@ -236,12 +236,9 @@ struct Lane {
         }
         return make_uint4(m[0], m[1], m[2], m[3]);
     }
-    // elements of vector k that are not the row's, where it has any of the row's
-    __device__ __forceinline__ float spare(int k) const
-    {
-        const int lo = first(k);
-        return any(k) ? (float)(max(-lo, 0) + max(lo + N - d, 0)) : 0.0f;
-    }
+    // elements of the thread's cut vectors that are not the row's
+    __device__ __forceinline__ float head_spares() const { return MODE == 1 && head ? (float)(max(s, 0) + max(N - s - d, 0)) : 0.0f; }
+    __device__ __forceinline__ float tail_spares() const { return MODE == 1 && tail ? (float)((N - (s + d) % N) % N) : 0.0f; }
     __device__ __forceinline__ uint4 mask(int k) const
     {
         uint4 m;
@@ -293,7 +290,7 @@ struct Row {
                 if constexpr (MODE == 2) {
                     if (ln.any(k)) mine[k * LN::STRIDE] = v[k].e;
                 } else {
-                    if (ln.whole(k)) v[k].store(mine + k * LN::STRIDE);
+                    if (ln.whole(k)) v[k].store_streaming(mine + k * LN::STRIDE);
                 }
             }
             if constexpr (LN::EDGED) {
@@ -346,19 +343,23 @@ struct Row {
     template <typename LN>
     __device__ __forceinline__ T own(const LN& ln, int k) const
     {
-        if constexpr (MODE == 2) return v[k].e;
-        else return own_of(ln, k);
-    }
-    template <typename LN>
-    __device__ __forceinline__ T own_of(const LN& ln, int k) const
-    {
-        T one = ln.first(k) < 0 ? v[k].at(N - 1) : v[k].at(0);
-        if (LN::NV * LN::LANES * N <= 16 && ln.first(k) < 0 && ln.d < N - ln.s) {        // the whole row within one vector
+        T one = k == 0 && ln.head ? v[0].at(N - 1) : v[k].at(0);
+        if (LN::NV * LN::LANES * N <= 16 && k == 0 && ln.d < N - ln.s) {         // the whole row within one vector
 #pragma unroll
             for (int i = 0; i < N; ++i)
                 if (i == ln.s) one = v[k].at(i);
         }
         return one;
+    }
+    // those elements of the thread's cut vectors: the row's first, the row's last (anything where it has none)
+    template <typename LN>
+    __device__ __forceinline__ float2 spares(const LN& ln) const
+    {
+        float t = 0.0f;
+#pragma unroll
+        for (int k = 0; k < NV; ++k)
+            if (LN::may_cut(k) && (ln.tail >> k & 1)) t = to_f(v[k].at(0));
+        return make_float2(to_f(own(ln, 0)), t);
     }
     static __device__ __forceinline__ uint32_t twice(T x)
     {
@@ -495,7 +496,7 @@ __device__ __forceinline__ void load_weights(const LN& ln, const void* w, int wt
 struct SumOp { __device__ __forceinline__ static float of(float a, float b) { return a + b; } };
 struct MaxOp { __device__ __forceinline__ static float of(float a, float b) { return fmaxf(a, b); } };
 
-// Shared memory of group_all for R values at a time: two halves of a value for every warp of a group (or cluster); and the
+// Shared memory of group_join for R values at a time: two halves of a value for every warp of a group (or cluster); and the
 // barriers of a ring of S stages, one a stage and group.
 template <typename LN, int TPR, int C, int R, int S>
 struct Join {
@@ -527,54 +528,80 @@ struct Join {
     }
 };
 
-// Sums (or maxima) of R values over a group; every thread gets the same bits.  `turn` counts the calls.
-// Where a group is more than a warp, its warps write their values to shared memory and meet at the group's barrier.  In a
-// cluster every warp sends its values to every block, and a thread waits until its block has all of them; no block waits for
-// a barrier of the cluster, whose release would wait for the rows' stores too.  Both use the halves of the buffer in turn:
-// whoever writes a half has seen, in the call between, values that every warp sent after its last reads of that half.
-template <typename Op, int TPR, int C, int R, typename J>
-__device__ __forceinline__ void group_all(float (&v)[R], J& jn, uint32_t& turn)
+// Sums (or maxima) of R values over the group's threads in a warp; every thread gets the same bits.
+template <typename Op, int TPR, int R>
+__device__ __forceinline__ void warp_all(float (&v)[R])
 {
 #pragma unroll
     for (int o = (TPR < 32 ? TPR : 32) / 2; o > 0; o >>= 1)
 #pragma unroll
         for (int r = 0; r < R; ++r) v[r] = Op::of(v[r], __shfl_xor_sync(0xffffffffu, v[r], o));
-    if constexpr (TPR > 32) {
-        constexpr int W = J::W;
-        const int g = threadIdx.x / TPR, warp = (threadIdx.x % TPR) >> 5, l = threadIdx.x & 31, half = turn & 1;
-        float* b = jn.v + (g * 2 + half) * R * W;
-        bool here = true;
-        if constexpr (C > 1) {
-            if (l < C) {
-                const uint32_t mine = (uint32_t)__cvta_generic_to_shared(b + cluster_rank() * (TPR / 32) + warp);
-                const uint32_t bar = jn.half(half);
-                uint32_t there, there_bar;
-                asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(there) : "r"(mine), "r"(l));
-                asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(there_bar) : "r"(bar), "r"(l));
+}
+
+// Groups of more than a warp: R values of every warp to every warp; lane l gets those of warp l modulo their number W (and, of
+// 64, of warp 32 + l too; zeros otherwise).  `turn` counts the calls.
+// The warps write to shared memory and meet at the group's barrier.  In a cluster every warp sends its values to every block,
+// and a thread waits until its block has all of them; no block waits for a barrier of the cluster, whose release would wait
+// for the rows' stores too.  Both use the halves of the buffer in turn: whoever writes a half has seen, in the call between,
+// values that every warp sent after its last reads of that half.
+template <int TPR, int C, int R, typename J>
+__device__ __forceinline__ void group_join(const float (&v)[R], float (&out)[R][2], J& jn, uint32_t& turn)
+{
+    constexpr int W = J::W;
+    const int g = threadIdx.x / TPR, warp = (threadIdx.x % TPR) >> 5, l = threadIdx.x & 31, half = turn & 1;
+    float* b = jn.v + (g * 2 + half) * R * W;
+    bool here = true;
+    if constexpr (C > 1) {
+        if (l < C) {
+            const uint32_t mine = (uint32_t)__cvta_generic_to_shared(b + cluster_rank() * (TPR / 32) + warp);
+            const uint32_t bar = jn.half(half);
+            uint32_t there, there_bar;
+            asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(there) : "r"(mine), "r"(l));
+            asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(there_bar) : "r"(bar), "r"(l));
 #pragma unroll
-                for (int r = 0; r < R; ++r)
-                    asm volatile("st.async.shared::cluster.mbarrier::complete_tx::bytes.b32 [%0], %1, [%2];"
-                                 ::"r"(there + (uint32_t)(r * W * sizeof(float))), "r"(__float_as_uint(v[r])), "r"(there_bar) : "memory");
-            }
-            __syncwarp();
-            here = wait_for(jn.half(half), (turn >> 1) & 1, &jn.late);
-            if (threadIdx.x == 0) expect_bytes(jn.half(half), W * R * (uint32_t)sizeof(float));      // for the call after the next
-        } else {
-            if (l == 0)
-#pragma unroll
-                for (int r = 0; r < R; ++r) b[r * W + warp] = v[r];
-            if constexpr (TPR == kRowBlock) __syncthreads();
-            else asm volatile("bar.sync %0, %1;" ::"r"(g + 1), "n"(TPR) : "memory");
+            for (int r = 0; r < R; ++r)
+                asm volatile("st.async.shared::cluster.mbarrier::complete_tx::bytes.b32 [%0], %1, [%2];"
+                             ::"r"(there + (uint32_t)(r * W * sizeof(float))), "r"(__float_as_uint(v[r])), "r"(there_bar) : "memory");
         }
-        ++turn;
-        // a warp's lanes take the warps' values and join them, instead of every thread reading all of them
+        __syncwarp();
+        here = wait_for(jn.half(half), (turn >> 1) & 1, &jn.late);
+        if (threadIdx.x == 0) expect_bytes(jn.half(half), W * R * (uint32_t)sizeof(float));      // for the call after the next
+    } else {
+        if (l == 0)
+#pragma unroll
+            for (int r = 0; r < R; ++r) b[r * W + warp] = v[r];
+        if constexpr (TPR == kRowBlock) __syncthreads();
+        else asm volatile("bar.sync %0, %1;" ::"r"(g + 1), "n"(TPR) : "memory");
+    }
+    ++turn;
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+        out[r][0] = here ? b[r * W + (l & (W - 1))] : __int_as_float(0x7fffffff);
+        out[r][1] = W == 64 ? b[r * W + (W == 64 ? 32 + l : 0)] : 0.0f;
+    }
+}
+
+// Sum (or maximum) of what group_join left in the lanes.
+template <typename Op, int TPR, int C>
+__device__ __forceinline__ void join_all(float& t)
+{
+    constexpr int W = TPR / 32 * C;
+#pragma unroll
+    for (int o = (W < 32 ? W : 32) / 2; o > 0; o >>= 1) t = Op::of(t, __shfl_xor_sync(0xffffffffu, t, o));
+}
+
+// Sums of R values over a group.
+template <int TPR, int C, int R, typename J>
+__device__ __forceinline__ void group_sum(float (&v)[R], J& jn, uint32_t& turn)
+{
+    warp_all<SumOp, TPR>(v);
+    if constexpr (TPR > 32) {
+        float o[R][2];
+        group_join<TPR, C>(v, o, jn, turn);
 #pragma unroll
         for (int r = 0; r < R; ++r) {
-            float t = b[r * W + (l & (W - 1))];
-            if constexpr (W == 64) t = Op::of(t, b[r * W + 32 + l]);
-#pragma unroll
-            for (int o = (W < 32 ? W : 32) / 2; o > 0; o >>= 1) t = Op::of(t, __shfl_xor_sync(0xffffffffu, t, o));
-            v[r] = here ? t : __int_as_float(0x7fffffff);
+            v[r] = o[r][0] + o[r][1];
+            join_all<SumOp, TPR, C>(v[r]);
         }
     }
 }
