@@ -13,8 +13,7 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kBlocks = kTrainSMs * 4;
-constexpr int kChunk = 8192;           // elements; kSmallChunk where those would leave blocks without one
-constexpr int kSmallChunk = 2048;
+constexpr int kChunk = 2048;           // elements: the grain in which tensors are dealt out
 constexpr int kMaxRecords = 1000;      // 32 bytes a record: within the 32764 bytes of a kernel's parameters
 
 struct Record {
@@ -27,7 +26,7 @@ struct Record {
 
 template <int CAP>
 struct Table {
-    int32_t  count, chunk;             // records, elements of a chunk
+    int32_t  count;
     uint32_t chunks;
     Record   r[CAP];
 };
@@ -46,31 +45,38 @@ __device__ __forceinline__ double sum_squares(const float (&v)[M])
     return t;
 }
 
-constexpr int kAhead = 4;              // vectors that a thread loads before it uses the first
+constexpr int kAhead = 8;              // vectors that a thread loads before it uses the first: 128 KB an SM on their way
 
-// Sum of squares of the thread's share of m elements; vectors where the chunk begins at a multiple of 16 bytes.
+// Sum of squares of the thread's share of a span of m elements; vectors where it begins at a multiple of 16 bytes.
 template <typename T>
-__device__ __forceinline__ double chunk_squares(const T* p, int m)
+__device__ __forceinline__ double span_squares(const T* p, int64_t m)
 {
     constexpr int N = 16 / (int)sizeof(T);
     double acc = 0.0;
-    int e = 0;
+    int64_t e = 0;
     if ((reinterpret_cast<uintptr_t>(p) & 15) == 0) {
-        const int whole = m / N;
-        for (int v0 = threadIdx.x; v0 < whole; v0 += kThreads * kAhead) {
+        const auto add = [&](const Vec<T, 16>& x) {
+            float f[N];
+#pragma unroll
+            for (int i = 0; i < N; i += 2) { const float2 q = x.pair(i / 2); f[i] = q.x; f[i + 1] = q.y; }
+            acc += sum_squares(f);
+        };
+        constexpr int STRIP = kThreads * kAhead * N;
+        const T* mine = p + threadIdx.x * N;
+        for (; e + STRIP <= m; e += STRIP) {
             Vec<T, 16> x[kAhead];
 #pragma unroll
-            for (int u = 0; u < kAhead; ++u)
-                if (v0 + u * kThreads < whole) x[u].load(p + (size_t)(v0 + u * kThreads) * N); else x[u].fill(0);
+            for (int u = 0; u < kAhead; ++u) x[u].load(mine + e + u * (kThreads * N));
 #pragma unroll
-            for (int u = 0; u < kAhead; ++u) {
-                float f[N];
-#pragma unroll
-                for (int i = 0; i < N; i += 2) { const float2 p = x[u].pair(i / 2); f[i] = p.x; f[i + 1] = p.y; }
-                acc += sum_squares(f);
-            }
+            for (int u = 0; u < kAhead; ++u) add(x[u]);
         }
-        e = whole * N;
+#pragma unroll 4
+        for (; e + (int)(threadIdx.x + 1) * N <= m; e += kThreads * N) {
+            Vec<T, 16> x;
+            x.load(mine + e);
+            add(x);
+        }
+        e = m / N * N;
     }
     for (e += threadIdx.x; e < m; e += kThreads) {
         const float f[1] = {to_f(p[e])};
@@ -79,32 +85,37 @@ __device__ __forceinline__ double chunk_squares(const T* p, int m)
     return acc;
 }
 
-// o = c p; four elements at a time where both begin at a multiple of four of theirs, 16-byte stores of FP32
+// o = c p over a span, from its end to its beginning; vectors where both begin at a multiple of their bytes, 16-byte stores
 template <typename T, typename O>
-__device__ __forceinline__ void chunk_scale(const T* p, O* o, int m, float c)
+__device__ __forceinline__ void span_scale(const T* p, O* o, int64_t m, float c)
 {
     constexpr int N = sizeof(O) == 4 ? 4 : 8;
-    constexpr int AHEAD = 2 * kAhead * 4 / N;
-    int e = 0;
-    if ((reinterpret_cast<uintptr_t>(p) & (N * sizeof(T) - 1)) == 0 && (reinterpret_cast<uintptr_t>(o) & 15) == 0) {
-        const int whole = m / N;
-        for (int v0 = threadIdx.x; v0 < whole; v0 += kThreads * AHEAD) {
-            Vec<T, N * (int)sizeof(T)> x[AHEAD];
+    int64_t whole = 0;                               // elements in vectors
+    if ((reinterpret_cast<uintptr_t>(p) & (N * sizeof(T) - 1)) == 0 && (reinterpret_cast<uintptr_t>(o) & 15) == 0) whole = m / N * N;
+    for (int64_t e = whole + threadIdx.x; e < m; e += kThreads) o[e] = from_f<O>(to_f(p[e]) * c);
+    using In = Vec<T, N * (int)sizeof(T)>;
+    const auto put = [&](const In& x, int64_t e) {
+        Vec<O, 16> y;
 #pragma unroll
-            for (int u = 0; u < AHEAD; ++u)
-                if (v0 + u * kThreads < whole) x[u].load(p + (size_t)(v0 + u * kThreads) * N);
-#pragma unroll
-            for (int u = 0; u < AHEAD; ++u)
-                if (v0 + u * kThreads < whole) {
-                    Vec<O, 16> y;
-#pragma unroll
-                    for (int i = 0; i < N / 2; ++i) y.set_pair(i, __fmul2_rn(x[u].pair(i), f2(c)));
-                    y.store_streaming(o + (size_t)(v0 + u * kThreads) * N);
-                }
-        }
-        e = whole * N;
+        for (int i = 0; i < N / 2; ++i) y.set_pair(i, __fmul2_rn(x.pair(i), f2(c)));
+        y.store_streaming(o + e + threadIdx.x * N);
+    };
+    constexpr int STRIP = kThreads * kAhead * N;
+    const T* mine = p + threadIdx.x * N;
+    const int64_t strips = whole / STRIP;
+#pragma unroll 4
+    for (int64_t e = strips * STRIP; e + (int)(threadIdx.x + 1) * N <= whole; e += kThreads * N) {
+        In x;
+        x.load(mine + e);
+        put(x, e);
     }
-    for (e += threadIdx.x; e < m; e += kThreads) o[e] = from_f<O>(to_f(p[e]) * c);
+    for (int64_t e = (strips - 1) * STRIP; e >= 0; e -= STRIP) {
+        In x[kAhead];
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) x[u].load(mine + e + u * (kThreads * N));
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) put(x[u], e + u * (kThreads * N));
+    }
 }
 
 // The record that holds chunk number q: the last one with first <= q (records without elements hold none).
@@ -120,7 +131,7 @@ __device__ __forceinline__ int find_record(const Table<CAP>& tb, uint32_t q)
 }
 
 template <int CAP>
-__global__ void __launch_bounds__(kThreads)
+__global__ void __launch_bounds__(kThreads, 4)
 k_clip_squares(const __grid_constant__ Table<CAP> tb, double* __restrict__ part)
 {
     __shared__ double sred[kThreads / 32];
@@ -128,14 +139,15 @@ k_clip_squares(const __grid_constant__ Table<CAP> tb, double* __restrict__ part)
     const uint32_t q1 = (uint32_t)((uint64_t)tb.chunks * (blockIdx.x + 1) / gridDim.x);
     double acc = 0.0;
     int t = q0 < q1 ? find_record(tb, q0) : 0;
-    for (uint32_t q = q0; q < q1; ++q) {
+    for (uint32_t q = q0; q < q1;) {                 // a span: the block's chunks of one tensor
         while (t + 1 < tb.count && tb.r[t + 1].first <= q) ++t;
-        const int64_t e0 = (int64_t)(q - tb.r[t].first) * tb.chunk;
-        const int64_t left = tb.r[t].numel - e0;
-        const int m = (int)(left < tb.chunk ? left : tb.chunk);
-        if (tb.r[t].type == GEM_NLR_F32) acc += chunk_squares((const float*)tb.r[t].in + e0, m);
-        else if (tb.r[t].type == GEM_NLR_F16) acc += chunk_squares((const __half*)tb.r[t].in + e0, m);
-        else acc += chunk_squares((const __nv_bfloat16*)tb.r[t].in + e0, m);
+        const uint32_t end = t + 1 < tb.count && tb.r[t + 1].first < q1 ? tb.r[t + 1].first : q1;
+        const int64_t e0 = (int64_t)(q - tb.r[t].first) * kChunk, e1 = (int64_t)(end - tb.r[t].first) * kChunk;
+        const int64_t m = (e1 < tb.r[t].numel ? e1 : tb.r[t].numel) - e0;
+        if (tb.r[t].type == GEM_NLR_F32) acc += span_squares((const float*)tb.r[t].in + e0, m);
+        else if (tb.r[t].type == GEM_NLR_F16) acc += span_squares((const __half*)tb.r[t].in + e0, m);
+        else acc += span_squares((const __nv_bfloat16*)tb.r[t].in + e0, m);
+        q = end;
     }
     acc = block_sum<kThreads>(acc, sred);
     if (threadIdx.x == 0) part[blockIdx.x] = acc;
@@ -159,7 +171,7 @@ k_clip_norm(const double* __restrict__ part, int parts, float* __restrict__ norm
 }
 
 template <int CAP>
-__global__ void __launch_bounds__(kThreads)
+__global__ void __launch_bounds__(kThreads, 4)
 k_clip_scale(const __grid_constant__ Table<CAP> tb, const double* __restrict__ part, int parts, float max_norm, float eps,
              float* __restrict__ norm_out)
 {
@@ -171,21 +183,23 @@ k_clip_scale(const __grid_constant__ Table<CAP> tb, const double* __restrict__ p
     const uint32_t q0 = (uint32_t)((uint64_t)tb.chunks * blockIdx.x / gridDim.x);
     const uint32_t q1 = (uint32_t)((uint64_t)tb.chunks * (blockIdx.x + 1) / gridDim.x);
     int t = q0 < q1 ? find_record(tb, q1 - 1) : 0;
-    for (uint32_t q = q1; q-- > q0;) {
-        while (tb.r[t].first > q) --t;
-        if (tb.r[t].in == tb.r[t].out && c == 1.0f) continue;
-        const int64_t e0 = (int64_t)(q - tb.r[t].first) * tb.chunk;
-        const int64_t left = tb.r[t].numel - e0;
-        const int m = (int)(left < tb.chunk ? left : tb.chunk);
+    for (uint32_t q = q1; q > q0;) {
+        while (tb.r[t].first >= q) --t;
+        const uint32_t begin = tb.r[t].first > q0 ? tb.r[t].first : q0;
+        const int64_t e0 = (int64_t)(begin - tb.r[t].first) * kChunk, e1 = (int64_t)(q - tb.r[t].first) * kChunk;
+        const int64_t m = (e1 < tb.r[t].numel ? e1 : tb.r[t].numel) - e0;
         const int type = tb.r[t].type, out = tb.r[t].out_type;
         const void* in = tb.r[t].in;
-        if (type == GEM_NLR_F32) chunk_scale((const float*)in + e0, (float*)tb.r[t].out + e0, m, c);
+        void* to = tb.r[t].out;
+        q = begin;
+        if (in == to && c == 1.0f) continue;
+        if (type == GEM_NLR_F32) span_scale((const float*)in + e0, (float*)to + e0, m, c);
         else if (type == GEM_NLR_F16) {
-            if (out == GEM_NLR_F32) chunk_scale((const __half*)in + e0, (float*)tb.r[t].out + e0, m, c);
-            else chunk_scale((const __half*)in + e0, (__half*)tb.r[t].out + e0, m, c);
+            if (out == GEM_NLR_F32) span_scale((const __half*)in + e0, (float*)to + e0, m, c);
+            else span_scale((const __half*)in + e0, (__half*)to + e0, m, c);
         } else {
-            if (out == GEM_NLR_F32) chunk_scale((const __nv_bfloat16*)in + e0, (float*)tb.r[t].out + e0, m, c);
-            else chunk_scale((const __nv_bfloat16*)in + e0, (__nv_bfloat16*)tb.r[t].out + e0, m, c);
+            if (out == GEM_NLR_F32) span_scale((const __nv_bfloat16*)in + e0, (float*)to + e0, m, c);
+            else span_scale((const __nv_bfloat16*)in + e0, (__nv_bfloat16*)to + e0, m, c);
         }
     }
 }
@@ -196,14 +210,11 @@ int clip_launches(int32_t count) { return (count + kMaxRecords - 1) / kMaxRecord
 template <int CAP>
 bool fill(Table<CAP>& tb, const gem_nlr_tensor* ts, int count)
 {
-    int64_t all = 0;
-    for (int i = 0; i < count; ++i) all += ts[i].numel / kChunk;
-    tb.chunk = all >= kBlocks ? kChunk : kSmallChunk;
     uint64_t chunks = 0;
     tb.count = count;
     for (int i = 0; i < count; ++i) {
         tb.r[i] = Record{ts[i].in_dev, ts[i].out_dev, ts[i].numel, (uint32_t)chunks, (uint16_t)ts[i].type, (uint16_t)ts[i].out_type};
-        chunks += (uint64_t)(ts[i].numel / tb.chunk) + (ts[i].numel % tb.chunk != 0);
+        chunks += (uint64_t)(ts[i].numel / kChunk) + (ts[i].numel % kChunk != 0);
         if (chunks > 0xffffffffull) return false;
     }
     tb.chunks = (uint32_t)chunks;
