@@ -336,7 +336,7 @@ int gem_nlr_column_sums_static(const float *U_dev, int64_t n, int32_t r, float *
  * except where a call says so.  Results are the same bits on every call (no floating-point atomics).
  * Work is enqueued on cuda_stream, whose device must be current; nothing is allocated and no call synchronizes,
  * so all of them can be captured into a graph.  scratch_dev (256-byte aligned, at least the bytes that the
- * matching *_scratch_bytes call names; contents never matter) is used until the work has run.
+ * matching *_scratch_bytes call names, which is 0 for small calls; contents never matter) is used until the work has run.
  * They return GEM_NLR_OK, GEM_NLR_E_INVALID, GEM_NLR_E_WORKSPACE (scratch missing, misaligned or too small) or
  * GEM_NLR_E_CUDA (a launch failed).  The paper has no counterpart of this section.                            */
 #define GEM_NLR_F32  0
@@ -382,7 +382,7 @@ int gem_nlr_label_cross_entropy(const void *logits_dev, int32_t type, int64_t ld
  * when c == 1.  out NULL in every record: the norm alone (max_norm is not looked at).  norm: one float.  The squares
  * are summed in FP64 over the whole range of the types (no overflow or underflow inside); the stored norm is +inf
  * when it passes FP32.  A NaN anywhere makes norm and every output NaN; an infinite norm gives c = 0, a norm of 0 c = 1.
- * count >= 0, max_norm >= 0, eps >= 0.                                                                         */
+ * count >= 0, max_norm >= 0, eps >= 0; no two records' outputs overlap.                                         */
 typedef struct {
     const void *in_dev;
     void       *out_dev;

@@ -14,6 +14,7 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kBlocks = kTrainSMs * 4;
 constexpr int kChunk = 2048;           // elements: the grain in which tensors are dealt out
+constexpr int kOneChunks = 64;         // a call of no more is one launch of one cluster: 16384 elements a block
 constexpr int kMaxRecords = 1000;      // 32 bytes a record: within the 32764 bytes of a kernel's parameters
 
 struct Record {
@@ -130,16 +131,13 @@ __device__ __forceinline__ int find_record(const Table<CAP>& tb, uint32_t q)
     return lo;
 }
 
+// the thread's share of the squares of the chunks q0 ... q1 - 1
 template <int CAP>
-__global__ void __launch_bounds__(kThreads, 4)
-k_clip_squares(const __grid_constant__ Table<CAP> tb, double* __restrict__ part)
+__device__ __forceinline__ double all_squares(const Table<CAP>& tb, uint32_t q0, uint32_t q1)
 {
-    __shared__ double sred[kThreads / 32];
-    const uint32_t q0 = (uint32_t)((uint64_t)tb.chunks * blockIdx.x / gridDim.x);
-    const uint32_t q1 = (uint32_t)((uint64_t)tb.chunks * (blockIdx.x + 1) / gridDim.x);
     double acc = 0.0;
     int t = q0 < q1 ? find_record(tb, q0) : 0;
-    for (uint32_t q = q0; q < q1;) {                 // a span: the block's chunks of one tensor
+    for (uint32_t q = q0; q < q1;) {                 // a span: the chunks of one tensor
         while (t + 1 < tb.count && tb.r[t + 1].first <= q) ++t;
         const uint32_t end = t + 1 < tb.count && tb.r[t + 1].first < q1 ? tb.r[t + 1].first : q1;
         const int64_t e0 = (int64_t)(q - tb.r[t].first) * kChunk, e1 = (int64_t)(end - tb.r[t].first) * kChunk;
@@ -149,9 +147,74 @@ k_clip_squares(const __grid_constant__ Table<CAP> tb, double* __restrict__ part)
         else acc += span_squares((const __nv_bfloat16*)tb.r[t].in + e0, m);
         q = end;
     }
-    acc = block_sum<kThreads>(acc, sred);
+    return acc;
+}
+
+// the scaled outputs of the chunks q0 ... q1 - 1, from the last to the first
+template <int CAP>
+__device__ __forceinline__ void all_scaled(const Table<CAP>& tb, uint32_t q0, uint32_t q1, float c)
+{
+    int t = q0 < q1 ? find_record(tb, q1 - 1) : 0;
+    for (uint32_t q = q1; q > q0;) {
+        while (tb.r[t].first >= q) --t;
+        const uint32_t begin = tb.r[t].first > q0 ? tb.r[t].first : q0;
+        const int64_t e0 = (int64_t)(begin - tb.r[t].first) * kChunk, e1 = (int64_t)(q - tb.r[t].first) * kChunk;
+        const int64_t m = (e1 < tb.r[t].numel ? e1 : tb.r[t].numel) - e0;
+        const int type = tb.r[t].type, out = tb.r[t].out_type;
+        const void* in = tb.r[t].in;
+        void* to = tb.r[t].out;
+        q = begin;
+        if (in == to && c == 1.0f) continue;
+        if (type == GEM_NLR_F32) span_scale((const float*)in + e0, (float*)to + e0, m, c);
+        else if (type == GEM_NLR_F16) {
+            if (out == GEM_NLR_F32) span_scale((const __half*)in + e0, (float*)to + e0, m, c);
+            else span_scale((const __half*)in + e0, (__half*)to + e0, m, c);
+        } else {
+            if (out == GEM_NLR_F32) span_scale((const __nv_bfloat16*)in + e0, (float*)to + e0, m, c);
+            else span_scale((const __nv_bfloat16*)in + e0, (__nv_bfloat16*)to + e0, m, c);
+        }
+    }
+}
+
+template <int CAP>
+__device__ __forceinline__ uint32_t first_chunk(const Table<CAP>& tb, unsigned block) { return (uint32_t)((uint64_t)tb.chunks * block / gridDim.x); }
+
+__device__ __forceinline__ float clip_factor(double norm, float max_norm, float eps)
+{
+    const double ratio = (double)max_norm / (norm + (double)eps);
+    return ratio >= 1.0 || norm == 0.0 ? 1.0f : (float)ratio;            // a NaN stays one
+}
+
+template <int CAP>
+__global__ void __launch_bounds__(kThreads, 4)
+k_clip_squares(const __grid_constant__ Table<CAP> tb, double* __restrict__ part)
+{
+    __shared__ double sred[kThreads / 32];
+    const double acc = block_sum<kThreads>(all_squares(tb, first_chunk(tb, blockIdx.x), first_chunk(tb, blockIdx.x + 1)), sred);
     if (threadIdx.x == 0) part[blockIdx.x] = acc;
     next_may_start();
+}
+
+// A small call in one launch: the grid is one cluster, its blocks read each other's sums.
+template <int CAP>
+__global__ void __launch_bounds__(kThreads, 4)
+k_clip_one(const __grid_constant__ Table<CAP> tb, int scale, float max_norm, float eps, float* __restrict__ norm_out)
+{
+    __shared__ double sred[kThreads / 32], slot, norm;
+    const uint32_t q0 = first_chunk(tb, blockIdx.x), q1 = first_chunk(tb, blockIdx.x + 1);
+    const double acc = block_sum<kThreads>(all_squares(tb, q0, q1), sred);
+    if (threadIdx.x == 0) slot = acc;
+    __syncwarp();
+    cluster_barrier();
+    if (threadIdx.x == 0) {
+        double t = 0.0;
+        for (int b = 0; b < (int)gridDim.x; ++b) t += from_block(&slot, b);
+        norm = sqrt(t);
+        if (blockIdx.x == 0) *norm_out = (float)norm;
+    }
+    __syncthreads();
+    cluster_barrier();                               // (no block ends while another one reads its sum)
+    if (scale) all_scaled(tb, q0, q1, clip_factor(norm, max_norm, eps));
 }
 
 __device__ __forceinline__ double norm_of(const double* __restrict__ part, int parts, double* sred)
@@ -177,31 +240,9 @@ k_clip_scale(const __grid_constant__ Table<CAP> tb, const double* __restrict__ p
 {
     __shared__ double sred[kThreads / 32];
     grid_ready();
-    const double norm = norm_of(part, parts, sred), ratio = (double)max_norm / (norm + (double)eps);
-    const float c = ratio >= 1.0 || norm == 0.0 ? 1.0f : (float)ratio;          // a NaN stays one
+    const double norm = norm_of(part, parts, sred);
     if (norm_out && blockIdx.x == 0 && threadIdx.x == 0) *norm_out = (float)norm;
-    const uint32_t q0 = (uint32_t)((uint64_t)tb.chunks * blockIdx.x / gridDim.x);
-    const uint32_t q1 = (uint32_t)((uint64_t)tb.chunks * (blockIdx.x + 1) / gridDim.x);
-    int t = q0 < q1 ? find_record(tb, q1 - 1) : 0;
-    for (uint32_t q = q1; q > q0;) {
-        while (tb.r[t].first >= q) --t;
-        const uint32_t begin = tb.r[t].first > q0 ? tb.r[t].first : q0;
-        const int64_t e0 = (int64_t)(begin - tb.r[t].first) * kChunk, e1 = (int64_t)(q - tb.r[t].first) * kChunk;
-        const int64_t m = (e1 < tb.r[t].numel ? e1 : tb.r[t].numel) - e0;
-        const int type = tb.r[t].type, out = tb.r[t].out_type;
-        const void* in = tb.r[t].in;
-        void* to = tb.r[t].out;
-        q = begin;
-        if (in == to && c == 1.0f) continue;
-        if (type == GEM_NLR_F32) span_scale((const float*)in + e0, (float*)to + e0, m, c);
-        else if (type == GEM_NLR_F16) {
-            if (out == GEM_NLR_F32) span_scale((const __half*)in + e0, (float*)to + e0, m, c);
-            else span_scale((const __half*)in + e0, (__half*)to + e0, m, c);
-        } else {
-            if (out == GEM_NLR_F32) span_scale((const __nv_bfloat16*)in + e0, (float*)to + e0, m, c);
-            else span_scale((const __nv_bfloat16*)in + e0, (__nv_bfloat16*)to + e0, m, c);
-        }
-    }
+    all_scaled(tb, first_chunk(tb, blockIdx.x), first_chunk(tb, blockIdx.x + 1), clip_factor(norm, max_norm, eps));
 }
 
 int clip_launches(int32_t count) { return (count + kMaxRecords - 1) / kMaxRecords; }
@@ -227,6 +268,14 @@ int clip_all(const gem_nlr_tensor* ts, int32_t count, bool scale, float max_norm
     static thread_local Table<CAP> tb;               // 32 KB: not on the caller's stack
     const int launches = clip_launches(count) < 1 ? 1 : clip_launches(count);
     int parts = 0;
+    if (launches == 1) {
+        if (!fill(tb, ts, count)) return GEM_NLR_E_INVALID;
+        if (tb.chunks <= (uint32_t)kOneChunks) {
+            const int blocks = tb.chunks < 1 ? 1 : tb.chunks < (uint32_t)kOneBlocks ? (int)tb.chunks : kOneBlocks;
+            return launch_rows(k_clip_one<CAP>, blocks, blocks, 0, false, st, tb, (int)scale, max_norm, eps, norm) == cudaSuccess ? GEM_NLR_OK
+                                                                                                                            : GEM_NLR_E_CUDA;
+        }
+    }
     for (int l = 0; l < launches; ++l) {
         const int first = l * kMaxRecords, m = count - first < kMaxRecords ? count - first : kMaxRecords;
         if (!fill(tb, ts + first, m)) return GEM_NLR_E_INVALID;

@@ -266,14 +266,15 @@ struct GradShape {
     static constexpr int ROW = S0::stage_bytes(), STAGE = 2 * ROW + (OWN ? 2 * 4 * kRowBlock : 0), MASKS = S0::L::mask_bytes();
     static constexpr int STAGES = ring_stages(STAGE, MASKS);
     static constexpr int SUMS = kRowBlock * EPL * 4;                                 // the columns' sums, after the ring's last use
-    static constexpr int SHARED = STAGE * STAGES + MASKS > SUMS ? STAGE * STAGES + MASKS : SUMS;
+    static constexpr int OWN_SUMS = C == 1 ? 2 * TPR * EPL * 4 : 0;                  // a block's record, where blocks read each other's
+    static constexpr int SHARED = STAGE * STAGES + MASKS > SUMS + OWN_SUMS ? STAGE * STAGES + MASKS : SUMS + OWN_SUMS;
 };
 
 template <typename T, int MODE, int TPR, int EPL, int C>
 __global__ void __launch_bounds__(kRowBlock, 2)
 k_norm_grad_rows(const T* __restrict__ dy, int64_t lddy, const T* __restrict__ x, int64_t ldx, const float* __restrict__ mean,
                  const float* __restrict__ rstd, const void* __restrict__ w, int wtype, int64_t n, int d, T* __restrict__ dx, int64_t lddx,
-                 float* __restrict__ part)
+                 float* __restrict__ part, int one, void* __restrict__ dw, void* __restrict__ db)
 {
     using L = Lane<T, MODE, TPR, EPL, C>;
     using H = GradShape<T, MODE, TPR, EPL, C>;
@@ -376,11 +377,30 @@ k_norm_grad_rows(const T* __restrict__ dy, int64_t lddy, const T* __restrict__ x
         if (++at == S) { at = 0; phase ^= 1; }
     }
     leave_cluster<C>();
-    if (!part) return;
+    if (!part && !one) return;
     next_may_start();
     copies_wait<0>();
-    float* rec = part + (size_t)(blockIdx.x / C) * 2 * d;
     float* sums = reinterpret_cast<float*>(ring);
+    float* rec = one ? sums + kRowBlock * EPL : part + (size_t)(blockIdx.x / C) * 2 * d;
+    // the records of a grid that is one cluster, joined by its blocks (in block order, FP64)
+    const auto join_one = [&] {
+        if constexpr (C == 1) {
+            cluster_barrier();
+            const int blocks = (int)gridDim.x;
+            for (int e = (int)(blockIdx.x * kRowBlock + threadIdx.x); e < 2 * d; e += blocks * kRowBlock) {
+                double v = 0.0;
+                for (int b = 0; b < blocks; ++b) v += (double)from_block(rec + e, b);
+                void* out = e < d ? dw : db;
+                const int j = e < d ? e : e - d;
+                if (out) {
+                    if (wtype == GEM_NLR_F32) ((float*)out)[j] = (float)v;
+                    else ((T*)out)[j] = from_f<T>((float)v);
+                }
+            }
+            __syncwarp();
+            cluster_barrier();
+        }
+    };
     if constexpr (L::GROUPS == 1) {
         // one group: through shared memory only to store neighbouring columns together
         const int from = ln.rank * (kRowBlock * EPL) - ln.s;
@@ -400,6 +420,7 @@ k_norm_grad_rows(const T* __restrict__ dy, int64_t lddy, const T* __restrict__ x
                 if (e >= 0 && e < d) rec[which * d + e] = sums[p];
             }
         }
+        if (one) join_one();
         return;
     }
     constexpr int W = TPR * EPL;                     // places of a group in `sums`
@@ -436,6 +457,7 @@ k_norm_grad_rows(const T* __restrict__ dy, int64_t lddy, const T* __restrict__ x
             }
         }
     }
+    if (one) join_one();
 }
 
 // dw, db: 32 columns a block, the records split over its 32 warps' lanes' rows, joined in a fixed order in FP64.
@@ -518,7 +540,7 @@ extern "C" int gem_nlr_layer_norm(const void* x_dev, int32_t type, int64_t ld_x,
 
 extern "C" size_t gem_nlr_layer_norm_backward_scratch_bytes(int64_t n, int32_t d)
 {
-    if (n < 0 || d < 1) return 0;
+    if (n < 0 || d < 1 || (n > 0 && one_cluster(n, d))) return 0;
     return (size_t)norm_records(n, d) * 2 * (size_t)d * sizeof(float);
 }
 
@@ -536,13 +558,15 @@ extern "C" int gem_nlr_layer_norm_backward(const void* dy_dev, int64_t ld_dy, co
     if (!aligned_to(weight_dev, type_bytes(wtype)) || !aligned_to(dweight_dev, type_bytes(wtype)) ||
         !aligned_to(dbias_dev, type_bytes(wtype)))
         return GEM_NLR_E_INVALID;
-    if (!scratch_dev || !aligned_to(scratch_dev, 256) || scratch_bytes < gem_nlr_layer_norm_backward_scratch_bytes(n, d))
+    const size_t need = gem_nlr_layer_norm_backward_scratch_bytes(n, d);
+    if (need > 0 && (!scratch_dev || !aligned_to(scratch_dev, 256) || scratch_bytes < need))
         return GEM_NLR_E_WORKSPACE;
     cudaStream_t st = (cudaStream_t)cuda_stream;
     float* part = (float*)scratch_dev;
     const int tb = type_bytes(type);
     const Matrix ms[3] = {{dy_dev, ld_dy}, {x_dev, ld_x}, {dx_dev, ld_dx}};
     const Lying lie = lying(ms, dx_dev ? 3 : 2, n, d, tb);
+    const bool one = n > 0 && one_cluster(n, d) && (dweight_dev || dbias_dev);
     bool held = false;
     int rec = 0;
     cudaError_t err = cudaSuccess;
@@ -553,14 +577,14 @@ extern "C" int gem_nlr_layer_norm_backward(const void* dy_dev, int64_t ld_dy, co
                 constexpr auto k = k_norm_grad_rows<T, mode.value, tpr.value, epl.value, c.value>;
                 constexpr int shared = GradShape<T, mode.value, tpr.value, epl.value, c.value>::SHARED;
                 const int most = resident_clusters<k, c.value>(shared), room = norm_records(n, d);
-                rec = spread(n, kRowBlock / tpr.value, 1, lie.period, most < room ? most : room);
-                err = launch_rows(k, rec * c.value, c.value, shared, false, st, (const T*)dy_dev, ld_dy, (const T*)x_dev, ld_x, mean_dev, rstd_dev,
-                                  weight_dev, (int)wtype, n, (int)d, (T*)dx_dev, ld_dx, dweight_dev || dbias_dev ? part : nullptr);
+                rec = spread(n, kRowBlock / tpr.value, 1, lie.period, one ? kOneBlocks : most < room ? most : room);
+                err = launch_rows(k, rec * c.value, one ? rec : c.value, shared, false, st, (const T*)dy_dev, ld_dy, (const T*)x_dev, ld_x, mean_dev, rstd_dev,
+                                  weight_dev, (int)wtype, n, (int)d, (T*)dx_dev, ld_dx, (dweight_dev || dbias_dev) && !one ? part : nullptr, (int)one, dweight_dev, dbias_dev);
             });
         });
     if (held) {
         int rc = err == cudaSuccess ? GEM_NLR_OK : GEM_NLR_E_CUDA;
-        if (rc == GEM_NLR_OK && (dweight_dev || dbias_dev))
+        if (rc == GEM_NLR_OK && (dweight_dev || dbias_dev) && !one)
             rc = by_type(wtype, [&](auto t) {
                 using W = decltype(t);
                 return launch_early(k_norm_dw_join<W>, dim3((unsigned)((2 * (int64_t)d + 31) / 32)), 1024, st, (const float*)part, rec, (int)d,

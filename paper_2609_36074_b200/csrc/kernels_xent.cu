@@ -61,6 +61,23 @@ __device__ __forceinline__ void finish_loss(double mine, int mean, Scratch* sc, 
     }
 }
 
+// The same in a grid that is one cluster; `slot`: the block's shared memory.
+__device__ __forceinline__ void finish_loss_one(double mine, int mean, int64_t counted, double* slot, float* loss)
+{
+    __shared__ double sred[kRowBlock / 32];
+    const double v = block_sum<kRowBlock>(mine, sred);
+    if (threadIdx.x == 0) *slot = v;
+    __syncwarp();
+    cluster_barrier();
+    if (blockIdx.x == 0 && threadIdx.x == 0) {
+        double t = 0.0;
+        for (int b = 0; b < (int)gridDim.x; ++b) t += from_block(slot, b);
+        *loss = (float)(!mean ? t : counted > 0 ? t / (double)counted : 0.0);
+    }
+    __syncwarp();
+    cluster_barrier();
+}
+
 // s of the loss: 1, or 1 / (rows that count).  One thread reads the counts for the block.
 __device__ __forceinline__ float loss_scale(const Scratch* sc, int mean)
 {
@@ -169,7 +186,7 @@ __device__ __forceinline__ float row_max(const Row<T, MODE, EPL>& z)
 template <typename T, int MODE, int TPR, int EPL, int C>
 __global__ void __launch_bounds__(kRowBlock, 2)
 k_xent_rows(const T* z, int64_t ld, const int32_t* __restrict__ labels, int64_t n, int k, int mean, Scratch* sc, float* __restrict__ loss,
-            float* __restrict__ row_loss, T* dz, int64_t ldd)
+            float* __restrict__ row_loss, T* dz, int64_t ldd, int one)
 {
     using L = Lane<T, MODE, TPR, EPL, C>;
     using H = XentShape<T, MODE, TPR, EPL, C>;
@@ -214,9 +231,20 @@ k_xent_rows(const T* z, int64_t ld, const int32_t* __restrict__ labels, int64_t 
         for (int r = 0; r < R; ++r) zs.prepare(ln, ring0 + (uint32_t)(i * H::STAGE + r * H::ROW), minus_infinity<T>());
         if (L::BULK || i < S - 1) send(ln.first_group() + i * R * step, i);
     }
-    float scale = 0.0f;
+    float scale = 1.0f;
     bool scaled = false;
     double sum = 0.0;
+    int64_t counted = 0;
+    __shared__ double slot, cred[kRowBlock / 32];
+    if (C == 1 && one) {                             // a small call's blocks count the labels themselves
+        scaled = true;
+        if (mean) {
+            double c = 0.0;
+            for (int64_t i = threadIdx.x; i < n; i += kRowBlock) c += labels[i] >= 0;
+            counted = (int64_t)block_sum<kRowBlock>(c, cred);
+            scale = counted > 0 ? (float)(1.0 / (double)counted) : 0.0f;
+        }
+    }
     int next = -1;
     if (L::BULK && ln.group() < n) next = labels[ln.group()];
     for (int64_t base = ln.first_group(); base < n; base += R * step) {
@@ -320,7 +348,8 @@ k_xent_rows(const T* z, int64_t ld, const int32_t* __restrict__ labels, int64_t 
     }
     if (!scaled) grid_ready();
     leave_cluster<C>();
-    finish_loss<kRowBlock>(sum, mean, sc, loss);
+    if (C == 1 && one) finish_loss_one(sum, mean, counted, &slot, loss);
+    else finish_loss<kRowBlock>(sum, mean, sc, loss);
 }
 
 }  // namespace
@@ -330,7 +359,7 @@ using namespace gemnlr;
 
 extern "C" size_t gem_nlr_label_cross_entropy_scratch_bytes(int64_t n, int32_t k)
 {
-    return n < 0 || k < 1 ? 0 : sizeof(Scratch);
+    return n < 0 || k < 1 || (n > 0 && one_cluster(n, k)) ? 0 : sizeof(Scratch);
 }
 
 extern "C" int gem_nlr_label_cross_entropy(const void* logits_dev, int32_t type, int64_t ld, const int32_t* labels_dev, int64_t n,
@@ -343,11 +372,14 @@ extern "C" int gem_nlr_label_cross_entropy(const void* logits_dev, int32_t type,
                   !row_loss_dev || !aligned_to(row_loss_dev, 4) || !aligned_to(dlogits_dev, tb) || (dlogits_dev && ld_d < k) ||
                   (dlogits_dev == logits_dev && ld != ld_d)))
         return GEM_NLR_E_INVALID;
-    if (!scratch_dev || !aligned_to(scratch_dev, 256) || scratch_bytes < sizeof(Scratch)) return GEM_NLR_E_WORKSPACE;
+    const bool one = n > 0 && one_cluster(n, k);
+    if (!one && (!scratch_dev || !aligned_to(scratch_dev, 256) || scratch_bytes < sizeof(Scratch))) return GEM_NLR_E_WORKSPACE;
     cudaStream_t st = (cudaStream_t)cuda_stream;
     Scratch* sc = (Scratch*)scratch_dev;
-    k_count_labels<<<kCountBlocks, 256, 0, st>>>(labels_dev, n, sc);
-    if (launched() != GEM_NLR_OK) return GEM_NLR_E_CUDA;
+    if (!one) {
+        k_count_labels<<<kCountBlocks, 256, 0, st>>>(labels_dev, n, sc);
+        if (launched() != GEM_NLR_OK) return GEM_NLR_E_CUDA;
+    }
     const Matrix ms[2] = {{logits_dev, ld}, {dlogits_dev, ld_d}};
     const Lying lie = lying(ms, dlogits_dev ? 2 : 1, n, k, tb);
     cudaError_t rc = cudaSuccess;
@@ -357,9 +389,10 @@ extern "C" int gem_nlr_label_cross_entropy(const void* logits_dev, int32_t type,
             constexpr auto kern = k_xent_rows<T, mode.value, tpr.value, epl.value, c.value>;
             constexpr int shared = XentShape<T, mode.value, tpr.value, epl.value, c.value>::SHARED;
             const int most = resident_clusters<kern, c.value>(shared);
-            const int cl = spread(n, kRowBlock / tpr.value, xent_rows(tpr.value, epl.value), lie.period, most < kMaxBlocks / c.value ? most : kMaxBlocks / c.value);
-            rc = launch_rows(kern, cl * c.value, c.value, shared, true, st, (const T*)logits_dev, ld, labels_dev, n, (int)k, (int)mean, sc, loss_dev,
-                             row_loss_dev, (T*)dlogits_dev, ld_d);
+            const int room = kMaxBlocks / c.value;
+            const int cl = spread(n, kRowBlock / tpr.value, one ? 1 : xent_rows(tpr.value, epl.value), lie.period, one ? kOneBlocks : most < room ? most : room);
+            rc = launch_rows(kern, cl * c.value, one ? cl : c.value, shared, !one, st, (const T*)logits_dev, ld, labels_dev, n, (int)k, (int)mean, sc, loss_dev,
+                             row_loss_dev, (T*)dlogits_dev, ld_d, (int)one);
         });
         if (!held) {
             const int64_t blocks = n < kTrainSMs * 8 ? n : kTrainSMs * 8;

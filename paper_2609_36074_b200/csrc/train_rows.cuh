@@ -733,6 +733,33 @@ inline int spread(int64_t n, int groups, int at_once, int period, int64_t most)
     return (int)c;
 }
 
+// Whether a call is small enough for one launch of one cluster of up to kOneBlocks blocks that join their sums themselves: at
+// most two rows a group, by the shape with the fewest groups that any layout of rows of d elements gets.
+constexpr int kOneBlocks = 8;
+inline bool one_cluster(int64_t n, int64_t d)
+{
+    int tpr = 2;
+    while (tpr < kRowBlock && (int64_t)tpr * 12 < d + 7) tpr *= 2;
+    return (int64_t)tpr * 12 >= d + 7 && n <= 2 * kOneBlocks * (kRowBlock / tpr);
+}
+
+// A value in another block's shared memory, at the place that `p` has in this one's.
+template <typename V>
+__device__ __forceinline__ V from_block(const V* p, int block)
+{
+    uint32_t at = (uint32_t)__cvta_generic_to_shared(p);
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(at), "r"(block));
+    if constexpr (sizeof(V) == 8) {
+        double v;
+        asm volatile("ld.shared::cluster.f64 %0, [%1];" : "=d"(v) : "r"(at) : "memory");
+        return v;
+    } else {
+        float v;
+        asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(at) : "memory");
+        return v;
+    }
+}
+
 // Launch of `blocks` blocks of kRowBlock threads with `shared` bytes of dynamic shared memory in clusters of c; `early`: it may begin while the stream's last kernel ends
 // (and waits for its results with grid_ready()).
 template <typename... P, typename... A>

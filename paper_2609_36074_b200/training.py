@@ -190,7 +190,7 @@ def layer_norm_backward(dy, x, mean, rstd, weight=None, need_dx=True, need_dweig
     if need_dbias:
         db = mean.new_empty(d, dtype=wdt) if dw is None else torch.empty_like(dw)
     size = fn["layer_norm_backward_scratch_bytes"](n, d)
-    scratch = mean.new_empty(size, dtype=torch.uint8)
+    scratch = mean.new_empty(size, dtype=torch.uint8) if size else mean
     _check(fn["layer_norm_backward"](
         dy.data_ptr(), ldg, x.data_ptr(), ld, t, mean.data_ptr(), rstd.data_ptr(), wp, wt, n, d,
         None if dx is None else dx.data_ptr(), d, None if dw is None else dw.data_ptr(), None if db is None else db.data_ptr(),
@@ -225,7 +225,7 @@ def label_cross_entropy(logits, labels, mean=True, dlogits=None, need_grad=True,
     row = logits.new_empty(lead, dtype=torch.float32)
     loss = row.new_empty(())
     size = fn["label_cross_entropy_scratch_bytes"](n, k)
-    scratch = labels.new_empty(size, dtype=torch.uint8)
+    scratch = labels.new_empty(size, dtype=torch.uint8) if size else labels          # (none is needed then)
     _check(fn["label_cross_entropy"](logits.data_ptr(), t, ld, labels.data_ptr(), n, k, 1 if mean else 0, loss.data_ptr(), row.data_ptr(),
                                      dp, ldd, scratch.data_ptr(), size, _stream(at)), "label_cross_entropy")
     return loss, row, dlogits
@@ -249,24 +249,28 @@ def _norm_and_clip(grads, max_norm, out, eps, stream):
             raise ValueError(f"max_norm is {max_norm}")
         if not eps >= 0:
             raise ValueError(f"eps is {eps}")
-    flat = []                                        # gem_nlr_tensor as four 64-bit words
-    for i, g in enumerate(grads):
-        t = types.get(g.dtype)
-        if t is None or g.get_device() != at or not (g.is_contiguous() or _dense(g)):
-            raise ValueError(f"tensor {i} has to be float32, float16 or bfloat16, without gaps, on GPU {at}")
-        p = g.data_ptr()
-        if out is None:
-            flat += (p, 0, g.numel(), t | t << 32)
-            continue
-        o = out[i]
-        if o is g:
-            flat += (p, p, g.numel(), t | t << 32)
-            continue
-        ot = types.get(o.dtype)
-        if (ot != t and ot != F32) or o.shape != g.shape or o.get_device() != at or \
-                not (o.is_contiguous() and g.is_contiguous() or o.stride() == g.stride() and _dense(o)):
-            raise ValueError(f"output {i} has to be like its tensor, or float32 of its shape and order")
-        flat += (p, o.data_ptr(), g.numel(), t | ot << 32)
+    kinds, sizes, ptrs = [types.get(g.dtype) for g in grads], [g.numel() for g in grads], [g.data_ptr() for g in grads]
+    if None in kinds or [g.get_device() for g in grads].count(at) != count:
+        raise ValueError(f"every tensor has to be float32, float16 or bfloat16 on GPU {at}")
+    whole = [g.is_contiguous() for g in grads]
+    for i in (i for i, w in enumerate(whole) if not w):
+        if not _dense(grads[i]):
+            raise ValueError(f"tensor {i} has gaps between its elements")
+    to, to_kinds = ptrs, kinds
+    if out is None:
+        to = [0] * count
+    elif out is not grads:
+        to, to_kinds = [o.data_ptr() for o in out], [types.get(o.dtype) for o in out]
+        if [o.numel() for o in out] != sizes or [o.get_device() for o in out].count(at) != count or \
+                (to_kinds != kinds and any(o != k and o != F32 for o, k in zip(to_kinds, kinds))):
+            raise ValueError(f"every output has to have its tensor's size and type, or float32, on GPU {at}")
+        if False in whole or False in [o.is_contiguous() for o in out]:
+            for i, (g, o) in enumerate(zip(grads, out)):
+                if not (g.is_contiguous() and o.is_contiguous()) and (o.shape != g.shape or o.stride() != g.stride() or not _dense(o)):
+                    raise ValueError(f"the elements of output {i} are in another order than its tensor's")
+    flat = [0] * (4 * count)                         # gem_nlr_tensor as four 64-bit words
+    flat[0::4], flat[1::4], flat[2::4] = ptrs, to, sizes
+    flat[3::4] = [k | o << 32 for k, o in zip(kinds, to_kinds)]
     table = array("Q", flat)
     norm = grads[0].new_empty((), dtype=torch.float32)
     size = fn["clip_grad_norm_scratch_bytes"](count)
@@ -288,7 +292,7 @@ def _dense(t):
 
 def clip_grad_norm(grads, max_norm, out=None, eps=1e-6, stream=None):
     """gem_nlr_clip_grad_norm: scales all tensors by min(1, max_norm / (norm + eps)), in place or into `out` (tensors of
-    the same shapes, of the same types or float32), and returns the norm before it, a float32 scalar on the GPU."""
+    the same sizes, in the same order of elements, of the same types or float32), and returns the norm before it, a float32 scalar on the GPU."""
     grads = list(grads)
     return _norm_and_clip(grads, max_norm, grads if out is None else list(out), eps, stream)
 
