@@ -13,6 +13,7 @@ from array import array
 from .binding import OK, lib
 
 F32, F16, BF16 = 0, 1, 2
+_INF = float("inf")
 
 
 class Tensor(C.Structure):
@@ -88,6 +89,13 @@ def _rows(t, name):
     return n, d, ld if n > 1 or ld > d else d
 
 
+def _floats(like, n):
+    """float32 of like's leading dimensions, n elements.  (empty_strided is torch's shortest way to one: 1.5 us, empty() 2.4.)"""
+    if like.dim() == 2:
+        return _torch.empty_strided((n,), (1,), dtype=_torch.float32, device=like.device)
+    return like.new_empty(like.shape[:-1], dtype=_torch.float32)
+
+
 def _vector(t, d, at, name):
     if t.shape != (d,) or not t.is_contiguous() or t.get_device() != at:
         raise ValueError(f"{name} has to be a contiguous vector of {d} on GPU {at}")
@@ -139,14 +147,13 @@ def layer_norm(x, weight=None, bias=None, eps=1e-5, out=None, stream=None):
             raise ValueError(f"weight is {weight.dtype} and bias {bias.dtype}")
     if wt != t and wt != F32:
         raise ValueError("weight and bias have to be float32 or of x's type")
-    if not 0 <= eps < float("inf"):
+    if not 0 <= eps < _INF:
         raise ValueError(f"eps is {eps}")
-    shape = x.shape
     if out is None:
-        y, ldy = torch.empty_like(x) if x.is_contiguous() else x.new_empty(shape), d
+        y, ldy = torch.empty_like(x) if x.is_contiguous() else x.new_empty(x.shape), d
     else:
         y, ldy = out, _given(out, x, "out")
-    mean = x.new_empty(shape[:-1], dtype=torch.float32)
+    mean = _floats(x, n)
     rstd = torch.empty_like(mean)
     _check(fn["layer_norm"](x.data_ptr(), t, ld, wp, bp, wt, n, d, eps, y.data_ptr(), ldy, mean.data_ptr(), rstd.data_ptr(),
                             _stream(at)), "layer_norm")
@@ -171,9 +178,9 @@ def layer_norm_backward(dy, x, mean, rstd, weight=None, need_dx=True, need_dweig
         if s.dtype != torch.float32 or s.numel() != n or not s.is_contiguous() or s.get_device() != at:
             raise ValueError(f"{name} has to be {n} contiguous float32 on GPU {at}")
     t = _type(x, "x")
-    wt, wp, wdt = F32, None, torch.float32
+    wt, wp = F32, None
     if weight is not None:
-        wt, wp, wdt = _type(weight, "weight"), _vector(weight, d, at, "weight"), weight.dtype
+        wt, wp = _type(weight, "weight"), _vector(weight, d, at, "weight")
         if wt != t and wt != F32:
             raise ValueError("weight has to be float32 or of x's type")
     if need_dweight is None:
@@ -186,9 +193,9 @@ def layer_norm_backward(dy, x, mean, rstd, weight=None, need_dx=True, need_dweig
     if need_dx:
         dx = torch.empty_like(x) if x.is_contiguous() else x.new_empty(x.shape)
     if need_dweight:
-        dw = mean.new_empty(d, dtype=wdt)
+        dw = mean.new_empty(d) if weight is None else torch.empty_like(weight)
     if need_dbias:
-        db = mean.new_empty(d, dtype=wdt) if dw is None else torch.empty_like(dw)
+        db = mean.new_empty(d) if weight is None else torch.empty_like(weight)
     size = fn["layer_norm_backward_scratch_bytes"](n, d)
     scratch = mean.new_empty(size, dtype=torch.uint8) if size else mean
     _check(fn["layer_norm_backward"](
@@ -222,8 +229,8 @@ def label_cross_entropy(logits, labels, mean=True, dlogits=None, need_grad=True,
         else:
             ldd = _given(dlogits, logits, "dlogits")
         dp = dlogits.data_ptr()
-    row = logits.new_empty(lead, dtype=torch.float32)
-    loss = row.new_empty(())
+    row = _floats(logits, n)
+    loss = torch.empty_strided((), (), dtype=torch.float32, device=logits.device)
     size = fn["label_cross_entropy_scratch_bytes"](n, k)
     scratch = labels.new_empty(size, dtype=torch.uint8) if size else labels          # (none is needed then)
     _check(fn["label_cross_entropy"](logits.data_ptr(), t, ld, labels.data_ptr(), n, k, 1 if mean else 0, loss.data_ptr(), row.data_ptr(),
@@ -272,9 +279,9 @@ def _norm_and_clip(grads, max_norm, out, eps, stream):
     flat[0::4], flat[1::4], flat[2::4] = ptrs, to, sizes
     flat[3::4] = [k | o << 32 for k, o in zip(kinds, to_kinds)]
     table = array("Q", flat)
-    norm = grads[0].new_empty((), dtype=torch.float32)
+    norm = torch.empty_strided((), (), dtype=torch.float32, device=grads[0].device)
     size = fn["clip_grad_norm_scratch_bytes"](count)
-    scratch = norm.new_empty(size, dtype=torch.uint8)
+    scratch = norm.new_empty(size // 4)
     _check(fn["clip_grad_norm"](table.buffer_info()[0], count, max_norm, eps, norm.data_ptr(), scratch.data_ptr(), size, _stream(at)), "clip_grad_norm")
     return norm
 
