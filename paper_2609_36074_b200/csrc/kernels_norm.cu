@@ -348,13 +348,13 @@ k_norm_grad_rows(const T* __restrict__ dy, int64_t lddy, const T* __restrict__ x
         float2 s0 = f2(here ? 0.0f : __int_as_float(0x7fffffff)), s1 = f2(0.0f);
 #pragma unroll
         for (int q = 0; q < L::PAIRS; ++q) {
-            const float2 g = gv.pair(q), h = __fmul2_rn(__fadd2_rn(xv.pair(q), m2), r2), gw = __fmul2_rn(g, w2[q]);
-            aw[q] = __ffma2_rn(g, h, aw[q]);
+            const float2 g = gv.pair(q), t = __fmul2_rn(g, __fadd2_rn(xv.pair(q), m2));          // dy (x - mu)
+            aw[q] = __ffma2_rn(t, r2, aw[q]);
             ab[q] = __fadd2_rn(ab[q], g);
-            s0 = __fadd2_rn(s0, gw);
-            s1 = __ffma2_rn(gw, h, s1);
+            s0 = __ffma2_rn(g, w2[q], s0);
+            s1 = __ffma2_rn(t, w2[q], s1);
         }
-        float s[2] = {s0.x + s0.y, s1.x + s1.y};
+        float s[2] = {s0.x + s0.y, (s1.x + s1.y) * rs};
         group_sum<TPR, C>(s, jn, turn);
         // every thread of the group is done with this row's stage, or (where it reads it again) with the one before
         if constexpr (L::BULK && !AGAIN) send(row + S * step, at);
@@ -362,15 +362,16 @@ k_norm_grad_rows(const T* __restrict__ dy, int64_t lddy, const T* __restrict__ x
             if (base != ln.first_group()) send(row + (S - 1) * step, at == 0 ? S - 1 : at - 1);
         }
         if (dx) {
-            const float2 c1 = f2(-s[0] * inv_d), c2 = f2(-s[1] * inv_d);
+            // dx = r dy w - r c1 - (x - mu) r^2 c2
+            const float2 c1 = f2(-rs * (s[0] * inv_d)), c2 = f2(-rs * rs * (s[1] * inv_d));
             if constexpr (AGAIN) {
                 xs.take(ln, row, ring0 + o, 0u, xv);
                 gs.take(ln, row, ring0 + o + H::ROW, 0u, gv);        // (what lies outside the row is not stored)
             }
 #pragma unroll
             for (int q = 0; q < L::PAIRS; ++q) {
-                const float2 h = __fmul2_rn(__fadd2_rn(xv.pair(q), m2), r2), gw = __fmul2_rn(gv.pair(q), w2[q]);
-                xv.set_pair(q, __fmul2_rn(r2, __ffma2_rn(h, c2, __fadd2_rn(gw, c1))));
+                const float2 gw = __fmul2_rn(gv.pair(q), w2[q]);
+                xv.set_pair(q, __ffma2_rn(__fadd2_rn(xv.pair(q), m2), c2, __ffma2_rn(gw, r2, c1)));
             }
             xv.store(ln, dx, row, lddx, row < n, n, ed);
         }
