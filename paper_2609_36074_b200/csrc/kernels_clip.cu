@@ -207,9 +207,7 @@ k_clip_one(const __grid_constant__ Table<CAP> tb, int scale, float max_norm, flo
     __syncwarp();
     cluster_barrier();
     if (threadIdx.x == 0) {
-        double t = 0.0;
-        for (int b = 0; b < (int)gridDim.x; ++b) t += from_block(&slot, b);
-        norm = sqrt(t);
+        norm = sqrt(from_all_blocks(&slot, (int)gridDim.x));
         if (blockIdx.x == 0) *norm_out = (float)norm;
     }
     __syncthreads();

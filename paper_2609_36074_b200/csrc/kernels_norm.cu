@@ -389,8 +389,7 @@ k_norm_grad_rows(const T* __restrict__ dy, int64_t lddy, const T* __restrict__ x
             cluster_barrier();
             const int blocks = (int)gridDim.x;
             for (int e = (int)(blockIdx.x * kRowBlock + threadIdx.x); e < 2 * d; e += blocks * kRowBlock) {
-                double v = 0.0;
-                for (int b = 0; b < blocks; ++b) v += (double)from_block(rec + e, b);
+                const double v = from_all_blocks(rec + e, blocks);
                 void* out = e < d ? dw : db;
                 const int j = e < d ? e : e - d;
                 if (out) {

@@ -70,8 +70,7 @@ __device__ __forceinline__ void finish_loss_one(double mine, int mean, int64_t c
     __syncwarp();
     cluster_barrier();
     if (blockIdx.x == 0 && threadIdx.x == 0) {
-        double t = 0.0;
-        for (int b = 0; b < (int)gridDim.x; ++b) t += from_block(slot, b);
+        const double t = from_all_blocks(slot, (int)gridDim.x);
         *loss = (float)(!mean ? t : counted > 0 ? t / (double)counted : 0.0);
     }
     __syncwarp();

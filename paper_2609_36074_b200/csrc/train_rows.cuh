@@ -734,13 +734,14 @@ inline int spread(int64_t n, int groups, int at_once, int period, int64_t most)
 }
 
 // Whether a call is small enough for one launch of one cluster of up to kOneBlocks blocks that join their sums themselves: at
-// most two rows a group, by the shape with the fewest groups that any layout of rows of d elements gets.
-constexpr int kOneBlocks = 8;
+// most kOneRows rows a group, by the shape with the fewest groups that any layout of rows of d elements gets.
+constexpr int kOneBlocks = 8, kOneRows = 4;
 inline bool one_cluster(int64_t n, int64_t d)
 {
     int tpr = 2;
-    while (tpr < kRowBlock && (int64_t)tpr * 12 < d + 7) tpr *= 2;
-    return (int64_t)tpr * 12 >= d + 7 && n <= 2 * kOneBlocks * (kRowBlock / tpr);
+    const auto holds = [&] { return (int64_t)tpr * (tpr < 32 ? 8 : 16) >= d + 7; };
+    while (tpr < kRowBlock && !holds()) tpr *= 2;
+    return holds() && n <= kOneRows * kOneBlocks * (kRowBlock / tpr);
 }
 
 // A value in another block's shared memory, at the place that `p` has in this one's.
@@ -758,6 +759,19 @@ __device__ __forceinline__ V from_block(const V* p, int block)
         asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(at) : "memory");
         return v;
     }
+}
+
+// Sum of that value over the `blocks` blocks of the cluster, in block order (the reads do not wait for one another).
+template <typename V>
+__device__ __forceinline__ double from_all_blocks(const V* p, int blocks)
+{
+    V v[kOneBlocks];
+#pragma unroll
+    for (int b = 0; b < kOneBlocks; ++b) v[b] = from_block(p, b < blocks ? b : 0);
+    double t = 0.0;
+#pragma unroll
+    for (int b = 0; b < kOneBlocks; ++b) t += b < blocks ? (double)v[b] : 0.0;
+    return t;
 }
 
 // Launch of `blocks` blocks of kRowBlock threads with `shared` bytes of dynamic shared memory in clusters of c; `early`: it may begin while the stream's last kernel ends

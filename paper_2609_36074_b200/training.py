@@ -9,6 +9,7 @@ from __future__ import annotations
 
 import ctypes as C
 from array import array
+from functools import lru_cache
 
 from .binding import OK, lib
 
@@ -53,6 +54,12 @@ def _load():
     _device, _stream = torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream
     _torch, _types, _fn = torch, {torch.float32: F32, torch.float16: F16, torch.bfloat16: BF16}, fn
     return fn
+
+
+@lru_cache(maxsize=1024)
+def _scratch(name, *sizes):
+    """Bytes of scratch for a call of these sizes."""
+    return _fn[name](*sizes)
 
 
 def _check(rc, name):
@@ -196,7 +203,7 @@ def layer_norm_backward(dy, x, mean, rstd, weight=None, need_dx=True, need_dweig
         dw = mean.new_empty(d) if weight is None else torch.empty_like(weight)
     if need_dbias:
         db = mean.new_empty(d) if weight is None else torch.empty_like(weight)
-    size = fn["layer_norm_backward_scratch_bytes"](n, d)
+    size = _scratch("layer_norm_backward_scratch_bytes", n, d)
     scratch = mean.new_empty(size, dtype=torch.uint8) if size else mean
     _check(fn["layer_norm_backward"](
         dy.data_ptr(), ldg, x.data_ptr(), ld, t, mean.data_ptr(), rstd.data_ptr(), wp, wt, n, d,
@@ -231,7 +238,7 @@ def label_cross_entropy(logits, labels, mean=True, dlogits=None, need_grad=True,
         dp = dlogits.data_ptr()
     row = _floats(logits, n)
     loss = torch.empty_strided((), (), dtype=torch.float32, device=logits.device)
-    size = fn["label_cross_entropy_scratch_bytes"](n, k)
+    size = _scratch("label_cross_entropy_scratch_bytes", n, k)
     scratch = labels.new_empty(size, dtype=torch.uint8) if size else labels          # (none is needed then)
     _check(fn["label_cross_entropy"](logits.data_ptr(), t, ld, labels.data_ptr(), n, k, 1 if mean else 0, loss.data_ptr(), row.data_ptr(),
                                      dp, ldd, scratch.data_ptr(), size, _stream(at)), "label_cross_entropy")
@@ -280,7 +287,7 @@ def _norm_and_clip(grads, max_norm, out, eps, stream):
     flat[3::4] = [k | o << 32 for k, o in zip(kinds, to_kinds)]
     table = array("Q", flat)
     norm = torch.empty_strided((), (), dtype=torch.float32, device=grads[0].device)
-    size = fn["clip_grad_norm_scratch_bytes"](count)
+    size = _scratch("clip_grad_norm_scratch_bytes", count)
     scratch = norm.new_empty(size // 4)
     _check(fn["clip_grad_norm"](table.buffer_info()[0], count, max_norm, eps, norm.data_ptr(), scratch.data_ptr(), size, _stream(at)), "clip_grad_norm")
     return norm
