@@ -133,6 +133,7 @@ k_norm_rows(const T* __restrict__ x, int64_t ldx, const void* __restrict__ w, co
     const L ln(d, x, ldx, ldy, ring0 + H::STAGE * S);
     const Source<T, MODE, TPR, EPL, C> xs(x, ldx, n, d);
     const bool lead = L::BULK && (int)threadIdx.x % TPR == 0;
+    const uint32_t usual = xs.window_bytes(ln);
     const float inv_d = 1.0f / (float)d;
     const float head_spares = ln.head_spares(), tail_spares = ln.tail_spares();
     float warp_n = (float)d;                         // the row's elements that this warp has, where it has not all of them
@@ -150,10 +151,10 @@ k_norm_rows(const T* __restrict__ x, int64_t ldx, const void* __restrict__ w, co
         if constexpr (L::BULK) {
             const int64_t row = base + ln.g;
             if (lead && row < n) {
-                int64_t from;
-                const uint32_t bytes = xs.window(ln, row, from), bar = jn.stage(ln, stage);
+                int skip;
+                const uint32_t bytes = xs.window(ln, row, usual, skip), bar = jn.stage(ln, stage);
                 expect_bytes(bar, bytes);
-                xs.send_bulk(ln, row, from, bytes, ring0 + (uint32_t)(stage * H::STAGE), bar);
+                xs.send_bulk(ln, row, skip, bytes, ring0 + (uint32_t)(stage * H::STAGE), bar);
             }
         } else if constexpr (MODE != 2) {
             if (base < n)
@@ -242,7 +243,7 @@ k_norm_rows(const T* __restrict__ x, int64_t ldx, const void* __restrict__ w, co
 #pragma unroll
         for (int r = 0; r < R; ++r) {
             const int64_t row = base + r * step + ln.g;
-            const float rs = 1.0f / sqrtf(s[r] * inv_d + eps);
+            const float rs = rsqrtf(s[r] * inv_d + eps);
             const float2 m2 = f2(-mu[r]), r2 = f2(rs);
 #pragma unroll
             for (int q = 0; q < L::PAIRS; ++q)
@@ -256,6 +257,9 @@ k_norm_rows(const T* __restrict__ x, int64_t ldx, const void* __restrict__ w, co
     }
     leave_cluster<C>();
 }
+
+// Floats from one record to the next: 2 d, rounded up so that every record begins at a multiple of 16 bytes.
+__host__ __device__ inline int64_t record_stride(int d) { return (2 * (int64_t)d + 3) & ~(int64_t)3; }
 
 // The gradient.  Every thread keeps its columns' sums of dy h and dy over the rows that it sees (FP32), the block joins its
 // groups' sums and writes one record; k_norm_dw_join adds the records.  A row's mean and rstd are read a row ahead.
@@ -291,17 +295,18 @@ k_norm_grad_rows(const T* __restrict__ dy, int64_t lddy, const T* __restrict__ x
     const Source<T, MODE, TPR, EPL, C> xs(x, ldx, n, d), gs(dy, lddy, n, d);
     const uint32_t slot4 = ring0 + 2 * H::ROW + threadIdx.x * 4;
     const bool lead = L::BULK && (int)threadIdx.x % TPR == 0;
+    const uint32_t usual = xs.window_bytes(ln);
     const float inv_d = 1.0f / (float)d;
     const int64_t step = ln.groups();
     const auto send = [&](int64_t row, int stage) {
         const uint32_t o = ring0 + (uint32_t)(stage * H::STAGE);
         if constexpr (L::BULK) {
             if (lead && row < n) {
-                int64_t fx, fg;
-                const uint32_t bx = xs.window(ln, row, fx), bg = gs.window(ln, row, fg), bar = jn.stage(ln, stage);
+                int sx, sg;
+                const uint32_t bx = xs.window(ln, row, usual, sx), bg = gs.window(ln, row, usual, sg), bar = jn.stage(ln, stage);
                 expect_bytes(bar, bx + bg);
-                xs.send_bulk(ln, row, fx, bx, o, bar);
-                gs.send_bulk(ln, row, fg, bg, o + H::ROW, bar);
+                xs.send_bulk(ln, row, sx, bx, o, bar);
+                gs.send_bulk(ln, row, sg, bg, o + H::ROW, bar);
             }
         } else if constexpr (MODE != 2) {
             if (row - ln.g < n) {
@@ -382,7 +387,7 @@ k_norm_grad_rows(const T* __restrict__ dy, int64_t lddy, const T* __restrict__ x
     next_may_start();
     copies_wait<0>();
     float* sums = reinterpret_cast<float*>(ring);
-    float* rec = one ? sums + kRowBlock * EPL : part + (size_t)(blockIdx.x / C) * 2 * d;
+    float* rec = one ? sums + kRowBlock * EPL : part + (int64_t)(blockIdx.x / C) * record_stride(d);
     // the records of a grid that is one cluster, joined by its blocks (in block order, FP64)
     const auto join_one = [&] {
         if constexpr (C == 1) {
@@ -460,25 +465,41 @@ k_norm_grad_rows(const T* __restrict__ dy, int64_t lddy, const T* __restrict__ x
     if (one) join_one();
 }
 
-// dw, db: 32 columns a block, the records split over its 32 warps' lanes' rows, joined in a fixed order in FP64.
+// dw, db: 128 columns a block, four to a lane; the block's 32 warps share the records out.  Fixed order, FP64.
 template <typename W>
 __global__ void __launch_bounds__(1024)
 k_norm_dw_join(const float* __restrict__ part, int records, int d, W* __restrict__ dw, W* __restrict__ db)
 {
-    __shared__ double s[32][33];
-    const int tx = threadIdx.x & 31, ty = threadIdx.x >> 5, e = blockIdx.x * 32 + tx;
+    __shared__ double s[32][128];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, e = blockIdx.x * 128 + lane * 4;
+    const int64_t stride = record_stride(d);
     grid_ready();
-    double v = 0.0;
-    if (e < 2 * d)
-        for (int c = ty; c < records; c += 32) v += (double)part[(size_t)c * 2 * d + e];
-    s[ty][tx] = v;
+    double v[4] = {0.0, 0.0, 0.0, 0.0};
+    if (e < stride) {
+#pragma unroll 4
+        for (int c = warp; c < records; c += 32) {
+            const float4 x = *reinterpret_cast<const float4*>(part + c * stride + e);
+            v[0] += (double)x.x;
+            v[1] += (double)x.y;
+            v[2] += (double)x.z;
+            v[3] += (double)x.w;
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) s[warp][lane * 4 + i] = v[i];
     __syncthreads();
-    // warp ty adds column ty's 32 partial sums
-    v = warp_sum(s[tx][ty]);
-    const int o = blockIdx.x * 32 + ty;
-    if (tx == 0 && o < 2 * d) {
+    // thread (j, p): rows 4 p ... of column j; then the eight parts
+    const int j = threadIdx.x & 127, p = threadIdx.x >> 7, o = blockIdx.x * 128 + j;
+    double t = s[4 * p][j] + s[4 * p + 1][j] + s[4 * p + 2][j] + s[4 * p + 3][j];
+    __syncthreads();
+    s[p][j] = t;
+    __syncthreads();
+    if (p == 0 && o < 2 * d) {
+        t = 0.0;
+#pragma unroll
+        for (int q = 0; q < 8; ++q) t += s[q][j];
         W* out = o < d ? dw : db;
-        if (out) out[o < d ? o : o - d] = from_f<W>((float)v);
+        if (out) out[o < d ? o : o - d] = from_f<W>((float)t);
     }
 }
 
@@ -541,7 +562,7 @@ extern "C" int gem_nlr_layer_norm(const void* x_dev, int32_t type, int64_t ld_x,
 extern "C" size_t gem_nlr_layer_norm_backward_scratch_bytes(int64_t n, int32_t d)
 {
     if (n < 0 || d < 1 || (n > 0 && one_cluster(n, d))) return 0;
-    return (size_t)norm_records(n, d) * 2 * (size_t)d * sizeof(float);
+    return (size_t)norm_records(n, d) * (size_t)record_stride(d) * sizeof(float);
 }
 
 extern "C" int gem_nlr_layer_norm_backward(const void* dy_dev, int64_t ld_dy, const void* x_dev, int64_t ld_x, int32_t type,
@@ -587,7 +608,7 @@ extern "C" int gem_nlr_layer_norm_backward(const void* dy_dev, int64_t ld_dy, co
         if (rc == GEM_NLR_OK && (dweight_dev || dbias_dev) && !one)
             rc = by_type(wtype, [&](auto t) {
                 using W = decltype(t);
-                return launch_early(k_norm_dw_join<W>, dim3((unsigned)((2 * (int64_t)d + 31) / 32)), 1024, st, (const float*)part, rec, (int)d,
+                return launch_early(k_norm_dw_join<W>, dim3((unsigned)((2 * (int64_t)d + 127) / 128)), 1024, st, (const float*)part, rec, (int)d,
                                     (W*)dweight_dev, (W*)dbias_dev) == cudaSuccess ? GEM_NLR_OK : GEM_NLR_E_CUDA;
             });
         return rc;

@@ -202,16 +202,17 @@ k_xent_rows(const T* z, int64_t ld, const int32_t* __restrict__ labels, int64_t 
     const Source<T, MODE, TPR, EPL, C> zs(z, ld, n, k);
     const uint32_t slot4 = ring0 + H::S0::stage_bytes() + threadIdx.x * 4;
     const bool lead = L::BULK && (int)threadIdx.x % TPR == 0;
+    const uint32_t usual = zs.window_bytes(ln);
     const float nan = __int_as_float(0x7fffffff);
     const int64_t step = ln.groups();
     const auto send = [&](int64_t base, int stage) {
         if constexpr (L::BULK) {
             const int64_t row = base + ln.g;
             if (lead && row < n) {
-                int64_t from;
-                const uint32_t bytes = zs.window(ln, row, from), bar = jn.stage(ln, stage);
+                int skip;
+                const uint32_t bytes = zs.window(ln, row, usual, skip), bar = jn.stage(ln, stage);
                 expect_bytes(bar, bytes);
-                zs.send_bulk(ln, row, from, bytes, ring0 + (uint32_t)(stage * H::STAGE), bar);
+                zs.send_bulk(ln, row, skip, bytes, ring0 + (uint32_t)(stage * H::STAGE), bar);
             }
         } else if constexpr (MODE != 2) {
             if (base < n)
@@ -326,7 +327,7 @@ k_xent_rows(const T* z, int64_t ld, const int32_t* __restrict__ labels, int64_t 
         for (int r = 0; r < R; ++r) {
             const int64_t row = base + r * step + ln.g;
             const bool counts = lab[r] >= 0, known = lab[r] < k, empty = s[r] == 0.0f;
-            const float q = !known ? nan : empty ? 0.0f : 1.0f / s[r];
+            const float q = !known ? nan : empty ? 0.0f : __fdividef(1.0f, s[r]);         // (1 <= s <= k, or NaN)
             // the label's thread has the row's loss and its element's gradient (p - 1) s; the first thread where there is none
             const bool teller = counts && known ? owner[r] : row < n && ln.l == 0 && ln.rank == 0;
             const float t = z_hot[r] - m[r];

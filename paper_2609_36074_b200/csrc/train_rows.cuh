@@ -415,19 +415,29 @@ struct Source {
         }
     }
     // What one thread of a group (BULK) sends for: the bytes of the group's window that lie between the matrix's ends.
-    __device__ __forceinline__ uint32_t window(const L& ln, int64_t row, int64_t& from) const
+    __device__ __forceinline__ uint32_t window_bytes(const L& ln) const
     {
-        const int64_t begin = row * ld - ln.s + ln.rank * (NV * TPR * N);
-        int64_t stop = row * ld - ln.s + (ln.s + ln.d + N - 1) / N * N;
-        if (C > 1 && stop > begin + NV * TPR * N) stop = begin + NV * TPR * N;
-        from = begin < 0 ? begin + N : begin;        // (only vectors that are whole: the rest is picked up by take())
-        if (MODE == 1 && stop > span) stop -= N;
-        return stop > from ? (uint32_t)(stop - from) * (uint32_t)sizeof(T) : 0u;
+        int stop = (ln.s + ln.d + N - 1) / N * N - ln.rank * (NV * TPR * N);
+        if (C > 1 && stop > NV * TPR * N) stop = NV * TPR * N;
+        return stop > 0 ? (uint32_t)stop * (uint32_t)sizeof(T) : 0u;
     }
-    __device__ __forceinline__ void send_bulk(const L& ln, int64_t row, int64_t from, uint32_t bytes, uint32_t stage, uint32_t bar) const
+    // usual: window_bytes(), which all rows share but those near the matrix's ends.  Returns the bytes, and adds the vectors
+    // to leave out at the beginning to `skip` (what is left out is picked up by take()).
+    __device__ __forceinline__ uint32_t window(const L& ln, int64_t row, uint32_t usual, int& skip) const
     {
-        const int64_t begin = row * ld - ln.s + ln.rank * (NV * TPR * N);
-        if (bytes) bulk_ahead(stage + (uint32_t)(ln.g * NV * TPR * 16) + (uint32_t)(from - begin) * (uint32_t)sizeof(T), base + from, bytes, bar);
+        skip = 0;
+        if (MODE == 1 && near_end(row)) {
+            const int64_t begin = row * ld - ln.s + ln.rank * (NV * TPR * N), stop = begin + usual / (uint32_t)sizeof(T);
+            const int64_t from = begin < 0 ? begin + N : begin, to = stop > span ? stop - N : stop;
+            skip = begin < 0 ? N : 0;
+            return to > from ? (uint32_t)(to - from) * (uint32_t)sizeof(T) : 0u;
+        }
+        return usual;
+    }
+    __device__ __forceinline__ void send_bulk(const L& ln, int64_t row, int skip, uint32_t bytes, uint32_t stage, uint32_t bar) const
+    {
+        const T* from = base + (row * ld - ln.s + ln.rank * (NV * TPR * N) + skip);
+        if (bytes) bulk_ahead(stage + (uint32_t)(ln.g * NV * TPR * 16 + skip * (int)sizeof(T)), from, bytes, bar);
     }
     // What every thread of a narrower group sends for.
     __device__ __forceinline__ void send_own(const L& ln, int64_t row, uint32_t stage) const
