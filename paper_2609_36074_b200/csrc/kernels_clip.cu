@@ -270,8 +270,7 @@ int clip_all(const gem_nlr_tensor* ts, int32_t count, bool scale, float max_norm
         if (!fill(tb, ts, count)) return GEM_NLR_E_INVALID;
         if (tb.chunks <= (uint32_t)kOneChunks) {
             const int blocks = tb.chunks < 1 ? 1 : tb.chunks < (uint32_t)kOneBlocks ? (int)tb.chunks : kOneBlocks;
-            return launch_rows(k_clip_one<CAP>, blocks, blocks, 0, false, st, tb, (int)scale, max_norm, eps, norm) == cudaSuccess ? GEM_NLR_OK
-                                                                                                                            : GEM_NLR_E_CUDA;
+            return told(launch_rows(k_clip_one<CAP>, blocks, blocks, 0, false, st, tb, (int)scale, max_norm, eps, norm));
         }
     }
     for (int l = 0; l < launches; ++l) {
@@ -283,15 +282,15 @@ int clip_all(const gem_nlr_tensor* ts, int32_t count, bool scale, float max_norm
     }
     if (launched() != GEM_NLR_OK) return GEM_NLR_E_CUDA;
     if (!scale)
-        return launch_early(k_clip_norm, dim3(1), kThreads, st, (const double*)part, parts, norm) == cudaSuccess ? GEM_NLR_OK : GEM_NLR_E_CUDA;
+        return told(launch_early(k_clip_norm, dim3(1), kThreads, st, (const double*)part, parts, norm));
     for (int l = launches - 1; l >= 0; --l) {
         const int first = l * kMaxRecords, m = count - first < kMaxRecords ? count - first : kMaxRecords;
         if (launches > 1) fill(tb, ts + first, m);
         const int blocks = tb.chunks < 1 ? 1 : tb.chunks < (uint32_t)kBlocks ? (int)tb.chunks : kBlocks;
         // only the first one may begin early: it waits for the squares, the others for it
         if (l == launches - 1) {
-            if (launch_early(k_clip_scale<CAP>, dim3((unsigned)blocks), kThreads, st, tb, (const double*)part, parts, max_norm, eps, norm) != cudaSuccess)
-                return GEM_NLR_E_CUDA;
+            const int rc = told(launch_early(k_clip_scale<CAP>, dim3((unsigned)blocks), kThreads, st, tb, (const double*)part, parts, max_norm, eps, norm));
+            if (rc != GEM_NLR_OK) return rc;
         } else {
             k_clip_scale<CAP><<<blocks, kThreads, 0, st>>>(tb, part, parts, max_norm, eps, nullptr);
         }

@@ -94,8 +94,8 @@ template <typename W>
 __global__ void __launch_bounds__(256)
 k_norm_dw_sum(const float* __restrict__ part, int records, int d, W* __restrict__ dw, W* __restrict__ db)
 {
-    const int e = blockIdx.x * 256 + threadIdx.x;
-    if (e >= 2 * d) return;
+    const int64_t e = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (e >= 2 * (int64_t)d) return;
     W* out = e < d ? dw : db;
     if (!out) return;
     double v = 0.0;
@@ -522,7 +522,8 @@ extern "C" int gem_nlr_layer_norm(const void* x_dev, int32_t type, int64_t ld_x,
                                   int32_t wtype, int64_t n, int32_t d, float eps, void* y_dev, int64_t ld_y, float* mean_dev,
                                   float* rstd_dev, void* cuda_stream)
 {
-    if (!type_bytes(type) || (wtype != type && wtype != GEM_NLR_F32) || n < 0 || d < 1 || !(eps >= 0.0f) || isinf(eps))
+    if (!type_bytes(type) || (wtype != type && wtype != GEM_NLR_F32) || n < 0 || d < 1 || d > kMaxColumns || !(eps >= 0.0f) ||
+        isinf(eps))
         return GEM_NLR_E_INVALID;
     if (n == 0) return GEM_NLR_OK;
     if (bad_rows(x_dev, type, ld_x) || bad_rows(y_dev, type, ld_y) || ld_y < d || x_dev == y_dev ||
@@ -545,7 +546,7 @@ extern "C" int gem_nlr_layer_norm(const void* x_dev, int32_t type, int64_t ld_x,
                              (T*)y_dev, ld_y, mean_dev, rstd_dev);
         });
     });
-    if (held) return rc == cudaSuccess ? GEM_NLR_OK : GEM_NLR_E_CUDA;
+    if (held) return told(rc);
     const int blocks = (int)(n < 148 * 8 ? n : 148 * 8);
     return by_type(type, [&](auto t) {
         using T = decltype(t);
@@ -561,7 +562,7 @@ extern "C" int gem_nlr_layer_norm(const void* x_dev, int32_t type, int64_t ld_x,
 
 extern "C" size_t gem_nlr_layer_norm_backward_scratch_bytes(int64_t n, int32_t d)
 {
-    if (n < 0 || d < 1 || (n > 0 && one_cluster(n, d))) return 0;
+    if (n < 0 || d < 1 || d > kMaxColumns || (n > 0 && one_cluster(n, d))) return 0;
     return (size_t)norm_records(n, d) * (size_t)record_stride(d) * sizeof(float);
 }
 
@@ -570,7 +571,8 @@ extern "C" int gem_nlr_layer_norm_backward(const void* dy_dev, int64_t ld_dy, co
                                            int64_t n, int32_t d, void* dx_dev, int64_t ld_dx, void* dweight_dev, void* dbias_dev,
                                            void* scratch_dev, size_t scratch_bytes, void* cuda_stream)
 {
-    if (!type_bytes(type) || (wtype != type && wtype != GEM_NLR_F32) || n < 0 || d < 1 || (!dx_dev && !dweight_dev && !dbias_dev))
+    if (!type_bytes(type) || (wtype != type && wtype != GEM_NLR_F32) || n < 0 || d < 1 || d > kMaxColumns ||
+        (!dx_dev && !dweight_dev && !dbias_dev))
         return GEM_NLR_E_INVALID;
     if (n > 0 && (bad_rows(dy_dev, type, ld_dy) || bad_rows(x_dev, type, ld_x) || !mean_dev || !rstd_dev ||
                   !aligned_to(mean_dev, 4) || !aligned_to(rstd_dev, 4) || (dx_dev && ld_dx < d) ||
@@ -604,12 +606,12 @@ extern "C" int gem_nlr_layer_norm_backward(const void* dy_dev, int64_t ld_dy, co
             });
         });
     if (held) {
-        int rc = err == cudaSuccess ? GEM_NLR_OK : GEM_NLR_E_CUDA;
+        int rc = told(err);
         if (rc == GEM_NLR_OK && (dweight_dev || dbias_dev) && !one)
             rc = by_type(wtype, [&](auto t) {
                 using W = decltype(t);
-                return launch_early(k_norm_dw_join<W>, dim3((unsigned)((2 * (int64_t)d + 127) / 128)), 1024, st, (const float*)part, rec, (int)d,
-                                    (W*)dweight_dev, (W*)dbias_dev) == cudaSuccess ? GEM_NLR_OK : GEM_NLR_E_CUDA;
+                return told(launch_early(k_norm_dw_join<W>, dim3((unsigned)((2 * (int64_t)d + 127) / 128)), 1024, st, (const float*)part, rec,
+                                         (int)d, (W*)dweight_dev, (W*)dbias_dev));
             });
         return rc;
     }

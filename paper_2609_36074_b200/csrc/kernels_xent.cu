@@ -359,7 +359,7 @@ using namespace gemnlr;
 
 extern "C" size_t gem_nlr_label_cross_entropy_scratch_bytes(int64_t n, int32_t k)
 {
-    return n < 0 || k < 1 || (n > 0 && one_cluster(n, k)) ? 0 : sizeof(Scratch);
+    return n < 0 || k < 1 || k > kMaxColumns || (n > 0 && one_cluster(n, k)) ? 0 : sizeof(Scratch);
 }
 
 extern "C" int gem_nlr_label_cross_entropy(const void* logits_dev, int32_t type, int64_t ld, const int32_t* labels_dev, int64_t n,
@@ -367,7 +367,7 @@ extern "C" int gem_nlr_label_cross_entropy(const void* logits_dev, int32_t type,
                                            int64_t ld_d, void* scratch_dev, size_t scratch_bytes, void* cuda_stream)
 {
     const int tb = type_bytes(type);
-    if (!tb || n < 0 || k < 1 || (mean != 0 && mean != 1) || !loss_dev || !aligned_to(loss_dev, 4)) return GEM_NLR_E_INVALID;
+    if (!tb || n < 0 || k < 1 || k > kMaxColumns || (mean != 0 && mean != 1) || !loss_dev || !aligned_to(loss_dev, 4)) return GEM_NLR_E_INVALID;
     if (n > 0 && (!logits_dev || !aligned_to(logits_dev, tb) || ld < 0 || !labels_dev || !aligned_to(labels_dev, 4) ||
                   !row_loss_dev || !aligned_to(row_loss_dev, 4) || !aligned_to(dlogits_dev, tb) || (dlogits_dev && ld_d < k) ||
                   (dlogits_dev == logits_dev && ld != ld_d)))
@@ -400,5 +400,5 @@ extern "C" int gem_nlr_label_cross_entropy(const void* logits_dev, int32_t type,
                               (int)k, (int)mean, sc, loss_dev, row_loss_dev, (T*)dlogits_dev, ld_d);
         }
     });
-    return rc == cudaSuccess ? GEM_NLR_OK : GEM_NLR_E_CUDA;
+    return told(rc);
 }

@@ -69,6 +69,9 @@ constexpr int kTrainSMs = 148, kTrainDevices = 64;
 __device__ __forceinline__ void next_may_start() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 __device__ __forceinline__ void grid_ready() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 
+// Columns of a row at most: int arithmetic on columns, steps included, stays far from its end.
+constexpr int32_t kMaxColumns = 1 << 30;
+
 inline int launched() { return cudaGetLastError() == cudaSuccess ? GEM_NLR_OK : GEM_NLR_E_CUDA; }
 
 }  // namespace gemnlr

@@ -102,10 +102,10 @@ __device__ __forceinline__ void cluster_barrier()
     asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
 
-// 16 bytes from global to shared memory, asynchronously: the first `bytes` of them, zeros behind
-__device__ __forceinline__ void copy_ahead(uint32_t to, const void* from, int bytes)
+// 16 bytes from global to shared memory, asynchronously
+__device__ __forceinline__ void copy_ahead(uint32_t to, const void* from)
 {
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(from), "r"(bytes) : "memory");
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(from) : "memory");
 }
 // 4 bytes, or a zero
 __device__ __forceinline__ void copy4_ahead(uint32_t to, const void* from, bool ok)
@@ -177,8 +177,8 @@ struct Lane {
     int64_t edge[TURNS];                             // elements that this lane stores for cut vectors: from its own row's
     int edge_group[TURNS];                           // beginning, and of which group; -1: none
 
-    // Vectors that a cut can be in: the first, and from LATEST / 2 - 1 on (a row fills more than half of its shape's places,
-    // less a vector; in clusters the last block may have a few only, and the narrowest shape takes every row there is).
+    // Vectors that a cut can be in: the first, and from the middle on (a row fills more than half of its shape's places, less
+    // a vector; in clusters the last block may have a few only, and the narrowest shape takes every row there is).
     static constexpr int CUTS_FROM = C > 1 || TPR == 2 ? 0 : (NV + 1) / 2 - 1;
     __host__ __device__ static constexpr bool may_cut(int k) { return MODE == 1 && (k == 0 || k >= CUTS_FROM); }
     __host__ __device__ static constexpr int mask_bytes() { return MODE == 1 ? NV * 16 * kRowBlock : 0; }
@@ -446,7 +446,7 @@ struct Source {
 #pragma unroll
         for (int k = 0; k < NV; ++k)
             if (row < n && ln.any(k) && (MODE == 0 || ln.whole(k) || within(ln, row, k)))
-                copy_ahead(stage + (uint32_t)ln.place(k) * 16, mine + k * L::STRIDE, 16);
+                copy_ahead(stage + (uint32_t)ln.place(k) * 16, mine + k * L::STRIDE);
     }
     // whether a vector of the row may reach over one of the matrix's ends
     __device__ __forceinline__ bool near_end(int64_t row) const { return row < near || row >= n - near; }
@@ -782,6 +782,14 @@ __device__ __forceinline__ double from_all_blocks(const V* p, int blocks)
 #pragma unroll
     for (int b = 0; b < kOneBlocks; ++b) t += b < blocks ? (double)v[b] : 0.0;
     return t;
+}
+
+// What a launch's error becomes at the C boundary (the error itself is not left behind for the next call).
+inline int told(cudaError_t e)
+{
+    if (e == cudaSuccess) return GEM_NLR_OK;
+    cudaGetLastError();
+    return GEM_NLR_E_CUDA;
 }
 
 // Launch of `blocks` blocks of kRowBlock threads with `shared` bytes of dynamic shared memory in clusters of c; `early`: it may begin while the stream's last kernel ends

@@ -33,7 +33,7 @@ def test_layer_norm_refuses():
         return fn(*{**good, **kw}.values(), None)
 
     for kw in (dict(x=None), dict(x=P + 1), dict(type=3), dict(type=-1), dict(ld=-1), dict(wtype=2), dict(wtype=7), dict(n=-1),
-               dict(d=0), dict(d=-4), dict(eps=-1.0), dict(eps=float("nan")), dict(eps=float("inf")), dict(y=None), dict(y=P),
+               dict(d=0), dict(d=-4), dict(d=2 ** 31 - 1, ld=2 ** 31, ldy=2 ** 31), dict(eps=-1.0), dict(eps=float("nan")), dict(eps=float("inf")), dict(y=None), dict(y=P),
                dict(ldy=7), dict(w=P + 2), dict(b=P + 1), dict(mean=P + 2), dict(rstd=P + 1), dict(type=2, wtype=1)):
         assert call(**kw) == gem.E_INVALID, kw
     assert call(n=0, x=None, y=None) == gem.OK
@@ -48,7 +48,7 @@ def test_layer_norm_backward_refuses():
     def call(**kw):
         return fns["layer_norm_backward"](*{**good, **kw}.values(), None)
 
-    for kw in (dict(dy=None), dict(x=None), dict(mean=None), dict(rstd=None), dict(type=4), dict(wtype=1), dict(n=-1), dict(d=0),
+    for kw in (dict(dy=None), dict(x=None), dict(mean=None), dict(rstd=None), dict(type=4), dict(wtype=1), dict(n=-1), dict(d=0), dict(d=2 ** 30 + 1, lddx=2 ** 31),
                dict(lddx=7), dict(dx=P), dict(dx=None, dw=None, db=None), dict(dy=P + 2), dict(x=P + 3), dict(dw=P + 1),
                dict(db=P + 2), dict(w=P + 1), dict(lddy=-8), dict(ld=-1), dict(mean=P + 1), dict(dx=2 * P + 2)):
         assert call(**kw) == gem.E_INVALID, kw
@@ -64,7 +64,7 @@ def test_cross_entropy_refuses():
     def call(**kw):
         return fns["label_cross_entropy"](*{**good, **kw}.values(), None)
 
-    for kw in (dict(z=None), dict(z=P + 2), dict(type=5), dict(ld=-1), dict(labels=None), dict(labels=P + 2), dict(n=-1), dict(k=0),
+    for kw in (dict(z=None), dict(z=P + 2), dict(type=5), dict(ld=-1), dict(labels=None), dict(labels=P + 2), dict(n=-1), dict(k=0), dict(k=2 ** 30 + 1, ldd=2 ** 31),
                dict(mean=2), dict(loss=None), dict(loss=P + 1), dict(row=None), dict(row=P + 2), dict(dz=P + 1), dict(ldd=7),
                dict(dz=P, ld=9)):
         assert call(**kw) == gem.E_INVALID, kw
