@@ -192,9 +192,9 @@ k_xent_rows(const T* z, int64_t ld, const int32_t* __restrict__ labels, int64_t 
     constexpr int N = L::N, R = H::ROWS, S = H::STAGES;
     constexpr float kLog2e = 1.4426950408889634f;
     extern __shared__ __align__(128) unsigned char ring[];
-    __shared__ Join<L, TPR, C, (TPR > 32 ? 2 : R), S> jn;
+    __shared__ Join<L, TPR, C, (TPR > 32 ? 2 : R), S, (C > 1 ? 4 : 2)> jn;
     __shared__ Edges<L> ed;
-    uint32_t turn = 0, phase = 0;
+    uint32_t turn = 0, sent = 0, phase = 0;
     int at = 0;
     jn.begin();
     const uint32_t ring0 = (uint32_t)__cvta_generic_to_shared(ring);
@@ -247,13 +247,23 @@ k_xent_rows(const T* z, int64_t ld, const int32_t* __restrict__ labels, int64_t 
     }
     int next = -1;
     if (L::BULK && ln.group() < n) next = labels[ln.group()];
-    for (int64_t base = ln.first_group(); base < n; base += R * step) {
+    // Rows between their two halves: begun when the warp's maximum and sum are known (and, in a cluster, sent to the other
+    // blocks), ended when the row's are.
+    struct Rows {
+        float2  e[R][L::PAIRS];
+        float   m[R], s[R], z_hot[R];
+        int     lab[R];
+        bool    owner[R], bare;
+        int64_t base;
+        int     at;
+    };
+    const auto begin = [&](Rows& w, int64_t base) {
         Row<T, MODE, EPL> zv[R];
-        float m[R], s[R], z_hot[R];
-        int lab[R];
-        bool owner[R], here = true;
+        bool here = true;
+        w.base = base;
+        w.at = at;
         if constexpr (L::BULK) {
-            lab[0] = base + ln.g < n ? next : -1;
+            w.lab[0] = base + ln.g < n ? next : -1;
             if (base + step + ln.g < n) next = labels[base + step + ln.g];
             if (base + ln.g < n) here = wait_for(jn.stage(ln, at), phase, &jn.late);
         } else if constexpr (MODE != 2) {
@@ -264,60 +274,65 @@ k_xent_rows(const T* z, int64_t ld, const int32_t* __restrict__ labels, int64_t 
         for (int r = 0; r < R; ++r) {
             const int64_t row = base + r * step + ln.g;
             const uint32_t o = (uint32_t)(at * H::STAGE + r * H::ROW);
-            if constexpr (H::OWN) lab[r] = row < n ? (int)read4(slot4 + o) : -1;
-            if constexpr (MODE == 2) lab[r] = row < n ? labels[row] : -1;
+            if constexpr (H::OWN) w.lab[r] = row < n ? (int)read4(slot4 + o) : -1;
+            if constexpr (MODE == 2) w.lab[r] = row < n ? labels[row] : -1;
             zs.take(ln, row, ring0 + o, minus_infinity<T>(), zv[r]);
             zv[r].mend(ln, minus_infinity<T>());
             // the label's logit, right in the thread that has it (and anything elsewhere)
-            const int hot = lab[r] + ln.s - ln.rank * (L::NV * TPR * N);
-            owner[r] = row < n && lab[r] >= 0 && lab[r] < k && hot >= 0 && hot < L::NV * TPR * N && hot / N % TPR == ln.l;
-            if constexpr (MODE == 2) z_hot[r] = owner[r] ? to_f(z[row * ld + lab[r]]) : nan;
+            const int lab = w.lab[r], hot = lab + ln.s - ln.rank * (L::NV * TPR * N);
+            w.owner[r] = row < n && lab >= 0 && lab < k && hot >= 0 && hot < L::NV * TPR * N && hot / N % TPR == ln.l;
+            if constexpr (MODE == 2) w.z_hot[r] = w.owner[r] ? to_f(z[row * ld + lab]) : nan;
             else {
-                const int v = owner[r] ? hot / N / TPR : 0;
-                z_hot[r] = to_f(reinterpret_cast<const T*>(ring + o + ln.place(v) * 16)[hot & (N - 1)]);
-                if (MODE == 1 && zs.near_end(row) && owner[r]) z_hot[r] = to_f(z[row * ld + lab[r]]);
+                const int v = w.owner[r] ? hot / N / TPR : 0;
+                w.z_hot[r] = to_f(reinterpret_cast<const T*>(ring + o + ln.place(v) * 16)[hot & (N - 1)]);
+                if (MODE == 1 && zs.near_end(row) && w.owner[r]) w.z_hot[r] = to_f(z[row * ld + lab]);
             }
         }
 #pragma unroll
-        for (int r = 0; r < R; ++r) m[r] = row_max<T, MODE, EPL>(zv[r]);
-        warp_all<MaxOp, TPR>(m);                     // of the group's, or the warp's, elements
-        float2 e2[R][L::PAIRS];
-        bool bare = false;
+        for (int r = 0; r < R; ++r) w.m[r] = row_max<T, MODE, EPL>(zv[r]);
+        warp_all<MaxOp, TPR>(w.m);                   // of the group's, or the warp's, elements
 #pragma unroll
         for (int r = 0; r < R; ++r) {
-            bare = m[r] == -INFINITY;                // nothing but -inf (or NaN): no -inf - -inf below
-            if (bare) m[r] = 0.0f;
-            const float2 m2 = f2(-m[r]);
+            w.bare = w.m[r] == -INFINITY;            // nothing but -inf (or NaN): no -inf - -inf below
+            if (w.bare) w.m[r] = 0.0f;
+            const float2 m2 = f2(-w.m[r]);
             float2 a = f2(here ? 0.0f : nan);
 #pragma unroll
             for (int q = 0; q < L::PAIRS; ++q) {
                 const float2 t = __fmul2_rn(__fadd2_rn(zv[r].pair(q), m2), f2(kLog2e));
-                e2[r][q] = make_float2(exp2_fast(t.x), exp2_fast(t.y));
-                a = __fadd2_rn(a, e2[r][q]);
+                w.e[r][q] = make_float2(exp2_fast(t.x), exp2_fast(t.y));
+                a = __fadd2_rn(a, w.e[r][q]);
             }
-            s[r] = a.x + a.y;
+            w.s[r] = a.x + a.y;
         }
-        warp_all<SumOp, TPR>(s);
+        warp_all<SumOp, TPR>(w.s);
+        if constexpr (C > 1) {
+            const float mine[2] = {w.bare ? -INFINITY : w.m[0], w.s[0]};
+            join_send<TPR, C>(mine, jn, sent++);
+        }
+        if (++at == S) { at = 0; phase ^= 1; }
+    };
+    const auto end = [&](Rows& w) {
         float down[R];                               // to the row's maximum from the warp's
 #pragma unroll
         for (int r = 0; r < R; ++r) down[r] = 1.0f;
         if constexpr (TPR > 32) {
             // each warp's maximum and sum to the row's, at one meeting of the group a row
             float v[2][2];
-            const float mine[2] = {bare ? -INFINITY : m[0], s[0]}, m_warp = m[0];
-            group_join<TPR, C>(mine, v, jn, turn);
+            const float mine[2] = {w.bare ? -INFINITY : w.m[0], w.s[0]}, m_warp = w.m[0];
+            if constexpr (C > 1) join_wait(v, jn, turn++);
+            else group_join<TPR, C>(mine, v, jn, turn);
             constexpr bool MANY = TPR / 32 * C == 64;
             float t = MANY ? fmaxf(v[0][0], v[0][1]) : v[0][0];
             join_all<MaxOp, TPR, C>(t);
-            m[0] = t == -INFINITY ? 0.0f : t;
-            t = v[1][0] * exp2_fast((v[0][0] - m[0]) * kLog2e);
-            if (MANY) t += v[1][1] * exp2_fast((v[0][1] - m[0]) * kLog2e);
+            w.m[0] = t == -INFINITY ? 0.0f : t;
+            t = v[1][0] * exp2_fast((v[0][0] - w.m[0]) * kLog2e);
+            if (MANY) t += v[1][1] * exp2_fast((v[0][1] - w.m[0]) * kLog2e);
             join_all<SumOp, TPR, C>(t);
-            s[0] = t;
-            down[0] = exp2_fast((bare ? -INFINITY : m_warp - m[0]) * kLog2e);
+            w.s[0] = t;
+            down[0] = exp2_fast((w.bare ? -INFINITY : m_warp - w.m[0]) * kLog2e);
         }
-        if constexpr (L::BULK) send(base + S * step, at);        // every thread of the group has its part of the row
-        if (++at == S) { at = 0; phase ^= 1; }
+        if constexpr (L::BULK) send(w.base + S * step, w.at);    // every thread of the group has its part of the row
         if (!scaled) {                                        // the first rows are worked on while the labels are counted
             grid_ready();
             scale = loss_scale(sc, mean);
@@ -325,25 +340,46 @@ k_xent_rows(const T* z, int64_t ld, const int32_t* __restrict__ labels, int64_t 
         }
 #pragma unroll
         for (int r = 0; r < R; ++r) {
-            const int64_t row = base + r * step + ln.g;
-            const bool counts = lab[r] >= 0, known = lab[r] < k, empty = s[r] == 0.0f;
-            const float q = !known ? nan : empty ? 0.0f : __fdividef(1.0f, s[r]);         // (1 <= s <= k, or NaN)
+            const int64_t row = w.base + r * step + ln.g;
+            const float s = w.s[r];
+            const bool counts = w.lab[r] >= 0, known = w.lab[r] < k, empty = s == 0.0f;
+            const float q = !known ? nan : empty ? 0.0f : __fdividef(1.0f, s);       // (1 <= s <= k, or NaN)
             // the label's thread has the row's loss and its element's gradient (p - 1) s; the first thread where there is none
-            const bool teller = counts && known ? owner[r] : row < n && ln.l == 0 && ln.rank == 0;
-            const float t = z_hot[r] - m[r];
-            const float v = !counts ? 0.0f : !known ? nan : empty ? INFINITY : logf(s[r]) - t;
-            const T one = from_f<T>(empty ? 0.0f : (exp2_fast(t * kLog2e) * q - 1.0f) * scale);
+            const bool teller = counts && known ? w.owner[r] : row < n && ln.l == 0 && ln.rank == 0;
+            const float t = w.z_hot[r] - w.m[r];
+            const float v = !counts ? 0.0f : !known ? nan : empty ? INFINITY : logf(s) - t;
+            const T one_hot = from_f<T>(empty ? 0.0f : (exp2_fast(t * kLog2e) * q - 1.0f) * scale);
             if (teller) {
                 row_loss[row] = v;
                 sum += (double)v;
             }
             if (!dz) continue;
+            Row<T, MODE, EPL> o;
             const float2 q2 = f2(q * down[r] * scale);
 #pragma unroll
-            for (int p = 0; p < L::PAIRS; ++p) zv[r].set_pair(p, __fmul2_rn(e2[r][p], q2));
-            if (!counts) zv[r].zero();
-            zv[r].store(ln, dz, row, ldd, row < n, n, ed);   // (ends with the warp's lanes in step: no store of theirs comes after)
-            if (owner[r]) dz[row * ldd + lab[r]] = one;
+            for (int p = 0; p < L::PAIRS; ++p) o.set_pair(p, __fmul2_rn(w.e[r][p], q2));
+            if (!counts) o.zero();
+            o.store(ln, dz, row, ldd, row < n, n, ed);       // (ends with the warp's lanes in step: no store of theirs comes after)
+            if (w.owner[r]) dz[row * ldd + w.lab[r]] = one_hot;
+        }
+    };
+    if constexpr (C > 1) {
+        // the next row is begun before this one is ended: the messages of one travel while the other is worked on
+        Rows a, b;
+        int64_t base = ln.first_group();
+        if (base < n) begin(a, base);
+        for (; base < n; base += 2 * step) {
+            const bool more = base + step < n;
+            if (more) begin(b, base + step);
+            end(a);
+            if (base + 2 * step < n) begin(a, base + 2 * step);
+            if (more) end(b);
+        }
+    } else {
+        Rows a;
+        for (int64_t base = ln.first_group(); base < n; base += R * step) {
+            begin(a, base);
+            end(a);
         }
     }
     if (!scaled) grid_ready();

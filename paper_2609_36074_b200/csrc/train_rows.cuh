@@ -506,17 +506,18 @@ __device__ __forceinline__ void load_weights(const LN& ln, const void* w, int wt
 struct SumOp { __device__ __forceinline__ static float of(float a, float b) { return a + b; } };
 struct MaxOp { __device__ __forceinline__ static float of(float a, float b) { return fmaxf(a, b); } };
 
-// Shared memory of group_join for R values at a time: two halves of a value for every warp of a group (or cluster); and the
+// Shared memory of group_join for R values at a time: PARTS times a value for every warp of a group (or cluster); and the
 // barriers of a ring of S stages, one a stage and group.
-template <typename LN, int TPR, int C, int R, int S>
+template <typename LN, int TPR, int C, int R, int S, int PARTS_ = 2>
 struct Join {
+    static constexpr int PARTS = PARTS_;
     static constexpr int W = TPR > 32 ? TPR / 32 * C : 1;        // values to join: one a warp
     static constexpr int FULLS = LN::BULK ? S * LN::GROUPS : 1;
-    float    v[TPR <= 32 ? 1 : 2 * R * C * kRowBlock / 32];
-    uint64_t bar[C > 1 ? 2 : 1];                                 // the halves' arrivals from the cluster's blocks
+    float    v[TPR <= 32 ? 1 : PARTS * R * C * kRowBlock / 32];
+    uint64_t bar[C > 1 ? PARTS : 1];                             // the parts' arrivals from the cluster's blocks
     uint64_t full[FULLS];                                        // the ring's stages
     uint32_t late;                                               // a wait has run out
-    __device__ __forceinline__ uint32_t half(int h) { return (uint32_t)__cvta_generic_to_shared(&bar[h]); }
+    __device__ __forceinline__ uint32_t part(int h) { return (uint32_t)__cvta_generic_to_shared(&bar[h]); }
     __device__ __forceinline__ uint32_t stage(const LN& ln, int at) { return (uint32_t)__cvta_generic_to_shared(&full[at * LN::GROUPS + ln.g]); }
     // before the first use, by all threads
     __device__ __forceinline__ void begin()
@@ -525,12 +526,13 @@ struct Join {
             if (threadIdx.x == 0) {
                 if constexpr (LN::BULK)
                     for (int i = 0; i < FULLS; ++i) barrier_init((uint32_t)__cvta_generic_to_shared(&full[i]), 1);
-                if constexpr (C > 1) { barrier_init(half(0), 1); barrier_init(half(1), 1); }
+                if constexpr (C > 1)
+                    for (int h = 0; h < PARTS; ++h) barrier_init(part(h), 1);
                 asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
                 late = 0;
                 if constexpr (C > 1)
 #pragma unroll
-                    for (int h = 0; h < 2; ++h) expect_bytes(half(h), W * R * (uint32_t)sizeof(float));
+                    for (int h = 0; h < PARTS; ++h) expect_bytes(part(h), W * R * (uint32_t)sizeof(float));
             }
             __syncwarp();
             if constexpr (C > 1) cluster_barrier(); else __syncthreads();
@@ -550,45 +552,70 @@ __device__ __forceinline__ void warp_all(float (&v)[R])
 
 // Groups of more than a warp: R values of every warp to every warp; lane l gets those of warp l modulo their number W (and, of
 // 64, of warp 32 + l too; zeros otherwise).  `turn` counts the calls.
-// The warps write to shared memory and meet at the group's barrier.  In a cluster every warp sends its values to every block,
-// and a thread waits until its block has all of them; no block waits for a barrier of the cluster, whose release would wait
-// for the rows' stores too.  Both use the halves of the buffer in turn: whoever writes a half has seen, in the call between,
-// values that every warp sent after its last reads of that half.
+// The warps write to shared memory and meet at the group's barrier.  In a cluster every warp sends its values to every block
+// (join_send), and a thread waits until its block has all of them (join_wait); no block waits for a barrier of the cluster,
+// whose release would wait for the rows' stores too.  The parts of the buffer are used in turn, two where a warp waits
+// before it sends again: whoever writes a part has seen, in the call between, values that every warp sent after its last reads
+// of that part.  A warp that sends once more before it waits needs four: it has then seen values of two calls before, sent
+// after the reads of four calls before.
 template <int TPR, int C, int R, typename J>
-__device__ __forceinline__ void group_join(const float (&v)[R], float (&out)[R][2], J& jn, uint32_t& turn)
+__device__ __forceinline__ void join_send(const float (&v)[R], J& jn, uint32_t turn)
 {
     constexpr int W = J::W;
-    const int g = threadIdx.x / TPR, warp = (threadIdx.x % TPR) >> 5, l = threadIdx.x & 31, half = turn & 1;
-    float* b = jn.v + (g * 2 + half) * R * W;
-    bool here = true;
-    if constexpr (C > 1) {
-        if (l < C) {
-            const uint32_t mine = (uint32_t)__cvta_generic_to_shared(b + cluster_rank() * (TPR / 32) + warp);
-            const uint32_t bar = jn.half(half);
-            uint32_t there, there_bar;
-            asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(there) : "r"(mine), "r"(l));
-            asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(there_bar) : "r"(bar), "r"(l));
+    const int warp = threadIdx.x >> 5, l = threadIdx.x & 31, p = turn % J::PARTS;
+    if (l < C) {
+        const uint32_t mine = (uint32_t)__cvta_generic_to_shared(jn.v + p * R * W + cluster_rank() * (TPR / 32) + warp);
+        const uint32_t bar = jn.part(p);
+        uint32_t there, there_bar;
+        asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(there) : "r"(mine), "r"(l));
+        asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(there_bar) : "r"(bar), "r"(l));
 #pragma unroll
-            for (int r = 0; r < R; ++r)
-                asm volatile("st.async.shared::cluster.mbarrier::complete_tx::bytes.b32 [%0], %1, [%2];"
-                             ::"r"(there + (uint32_t)(r * W * sizeof(float))), "r"(__float_as_uint(v[r])), "r"(there_bar) : "memory");
-        }
-        __syncwarp();
-        here = wait_for(jn.half(half), (turn >> 1) & 1, &jn.late);
-        if (threadIdx.x == 0) expect_bytes(jn.half(half), W * R * (uint32_t)sizeof(float));      // for the call after the next
-    } else {
-        if (l == 0)
-#pragma unroll
-            for (int r = 0; r < R; ++r) b[r * W + warp] = v[r];
-        if constexpr (TPR == kRowBlock) __syncthreads();
-        else asm volatile("bar.sync %0, %1;" ::"r"(g + 1), "n"(TPR) : "memory");
+        for (int r = 0; r < R; ++r)
+            asm volatile("st.async.shared::cluster.mbarrier::complete_tx::bytes.b32 [%0], %1, [%2];"
+                         ::"r"(there + (uint32_t)(r * W * sizeof(float))), "r"(__float_as_uint(v[r])), "r"(there_bar) : "memory");
     }
-    ++turn;
+    __syncwarp();
+}
+
+template <int R, typename J>
+__device__ __forceinline__ void join_read(const float* b, bool here, float (&out)[R][2], J&)
+{
+    constexpr int W = J::W;
+    const int l = threadIdx.x & 31;
 #pragma unroll
     for (int r = 0; r < R; ++r) {
         out[r][0] = here ? b[r * W + (l & (W - 1))] : __int_as_float(0x7fffffff);
         out[r][1] = W == 64 ? b[r * W + (W == 64 ? 32 + l : 0)] : 0.0f;
     }
+}
+
+template <int R, typename J>
+__device__ __forceinline__ void join_wait(float (&out)[R][2], J& jn, uint32_t turn)
+{
+    const int p = turn % J::PARTS;
+    const bool here = wait_for(jn.part(p), (turn / J::PARTS) & 1, &jn.late);
+    if (threadIdx.x == 0) expect_bytes(jn.part(p), J::W * R * (uint32_t)sizeof(float));          // for the part's next use
+    join_read(jn.v + p * R * J::W, here, out, jn);
+}
+
+template <int TPR, int C, int R, typename J>
+__device__ __forceinline__ void group_join(const float (&v)[R], float (&out)[R][2], J& jn, uint32_t& turn)
+{
+    if constexpr (C > 1) {
+        join_send<TPR, C>(v, jn, turn);
+        join_wait(out, jn, turn);
+    } else {
+        constexpr int W = J::W;
+        const int g = threadIdx.x / TPR, warp = (threadIdx.x % TPR) >> 5;
+        float* b = jn.v + (g * J::PARTS + turn % J::PARTS) * R * W;
+        if ((threadIdx.x & 31) == 0)
+#pragma unroll
+            for (int r = 0; r < R; ++r) b[r * W + warp] = v[r];
+        if constexpr (TPR == kRowBlock) __syncthreads();
+        else asm volatile("bar.sync %0, %1;" ::"r"(g + 1), "n"(TPR) : "memory");
+        join_read(b, true, out, jn);
+    }
+    ++turn;
 }
 
 // Sum (or maximum) of what group_join left in the lanes.
