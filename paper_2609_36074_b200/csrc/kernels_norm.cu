@@ -105,13 +105,17 @@ k_norm_dw_sum(const float* __restrict__ part, int records, int d, W* __restrict_
 
 // ---- streamed rows -----------------------------------------------------------------------------------------------
 
-// Rows that a group works on at a time: two or four of the narrow ones, so that their sums over the group run side by side.
-__host__ __device__ constexpr int fwd_rows(int tpr, int epl) { return tpr >= 32 ? 1 : epl <= 8 ? 4 : 2; }
+// Rows that a group works on at a time, so that their sums over the group run side by side: as many as the registers hold
+// next to the weights, up to a warp a row.
+__host__ __device__ constexpr int fwd_rows(int mode, int tpr, int epl)
+{
+    return tpr > 32 || epl > 24 || (epl > 16 && mode != 0) ? 1 : epl <= 8 ? 4 : 2;
+}
 
 template <typename T, int MODE, int TPR, int EPL, int C>
 struct NormShape {
     using S0 = Source<T, MODE, TPR, EPL, C>;
-    static constexpr int ROWS = fwd_rows(TPR, EPL), ROW = S0::stage_bytes(), STAGE = ROWS * ROW;
+    static constexpr int ROWS = fwd_rows(MODE, TPR, EPL), ROW = S0::stage_bytes(), STAGE = ROWS * ROW;
     static constexpr int MASKS = S0::L::mask_bytes(), STAGES = ring_stages(STAGE, MASKS), SHARED = STAGE * STAGES + MASKS;
 };
 
@@ -149,12 +153,20 @@ k_norm_rows(const T* __restrict__ x, int64_t ldx, const void* __restrict__ w, co
     // the rows of the iteration that begins at `base`
     const auto send = [&](int64_t base, int stage) {
         if constexpr (L::BULK) {
-            const int64_t row = base + ln.g;
-            if (lead && row < n) {
-                int skip;
-                const uint32_t bytes = xs.window(ln, row, usual, skip), bar = jn.stage(ln, stage);
-                expect_bytes(bar, bytes);
-                xs.send_bulk(ln, row, skip, bytes, ring0 + (uint32_t)(stage * H::STAGE), bar);
+            if (lead && base + ln.g < n) {
+                const uint32_t bar = jn.stage(ln, stage);
+                int skip[R];
+                uint32_t bytes[R], all = 0;
+#pragma unroll
+                for (int r = 0; r < R; ++r) {
+                    const int64_t row = base + r * step + ln.g;
+                    bytes[r] = row < n ? xs.window(ln, row, usual, skip[r]) : 0u;
+                    all += bytes[r];
+                }
+                expect_bytes(bar, all);
+#pragma unroll
+                for (int r = 0; r < R; ++r)
+                    xs.template send_bulk<true>(ln, base + r * step + ln.g, skip[r], bytes[r], ring0 + (uint32_t)(stage * H::STAGE + r * H::ROW), bar);
             }
         } else if constexpr (MODE != 2) {
             if (base < n)
@@ -238,7 +250,7 @@ k_norm_rows(const T* __restrict__ x, int64_t ldx, const void* __restrict__ w, co
             join_all<SumOp, TPR, C>(t);
             s[0] = t;
         }
-        if constexpr (L::BULK) send(base + S * step, at);        // every thread of the group has its part of the row
+        if constexpr (L::BULK) send(base + S * R * step, at);    // every thread of the group has its part of the rows
         if (++at == S) { at = 0; phase ^= 1; }
 #pragma unroll
         for (int r = 0; r < R; ++r) {
@@ -248,7 +260,7 @@ k_norm_rows(const T* __restrict__ x, int64_t ldx, const void* __restrict__ w, co
 #pragma unroll
             for (int q = 0; q < L::PAIRS; ++q)
                 xv[r].set_pair(q, __ffma2_rn(__fmul2_rn(__fadd2_rn(xv[r].pair(q), m2), r2), w2[q], b2[q]));
-            xv[r].store(ln, y, row, ldy, row < n, n, ed);
+            xv[r].template store<true>(ln, y, row, ldy, row < n, n, ed);
             if (ln.l == 0 && ln.rank == 0 && row < n) {
                 if (mean) mean[row] = mu[r];
                 if (rstd) rstd[row] = rs;
@@ -305,8 +317,8 @@ k_norm_grad_rows(const T* __restrict__ dy, int64_t lddy, const T* __restrict__ x
                 int sx, sg;
                 const uint32_t bx = xs.window(ln, row, usual, sx), bg = gs.window(ln, row, usual, sg), bar = jn.stage(ln, stage);
                 expect_bytes(bar, bx + bg);
-                xs.send_bulk(ln, row, sx, bx, o, bar);
-                gs.send_bulk(ln, row, sg, bg, o + H::ROW, bar);
+                xs.template send_bulk<true>(ln, row, sx, bx, o, bar);
+                gs.template send_bulk<true>(ln, row, sg, bg, o + H::ROW, bar);
             }
         } else if constexpr (MODE != 2) {
             if (row - ln.g < n) {
@@ -378,7 +390,7 @@ k_norm_grad_rows(const T* __restrict__ dy, int64_t lddy, const T* __restrict__ x
                 const float2 gw = __fmul2_rn(gv.pair(q), w2[q]);
                 xv.set_pair(q, __ffma2_rn(__fadd2_rn(xv.pair(q), m2), c2, __ffma2_rn(gw, r2, c1)));
             }
-            xv.store(ln, dx, row, lddx, row < n, n, ed);
+            xv.template store<false>(ln, dx, row, lddx, row < n, n, ed);
         }
         if (++at == S) { at = 0; phase ^= 1; }
     }
@@ -541,7 +553,7 @@ extern "C" int gem_nlr_layer_norm(const void* x_dev, int32_t type, int64_t ld_x,
         held = by_width<mode.value != 2 && sizeof(T) == 2 ? 16 : 8, mode.value != 2 && sizeof(T) == 2 ? 24 : 16, mode.value != 2 && sizeof(T) == 2 ? 32 : 24>(lie.mode == 1 ? (int64_t)d + 16 / tb - 1 : d, [&](auto tpr, auto epl, auto c) {
             constexpr auto k = k_norm_rows<T, mode.value, tpr.value, epl.value, c.value>;
             constexpr int shared = NormShape<T, mode.value, tpr.value, epl.value, c.value>::SHARED;
-            const int cl = spread(n, kRowBlock / tpr.value, fwd_rows(tpr.value, epl.value), lie.period, resident_clusters<k, c.value>(shared));
+            const int cl = spread(n, kRowBlock / tpr.value, fwd_rows(mode.value, tpr.value, epl.value), lie.period, resident_clusters<k, c.value>(shared));
             rc = launch_rows(k, cl * c.value, c.value, shared, false, st, (const T*)x_dev, ld_x, weight_dev, bias_dev, (int)wtype, n, (int)d, eps,
                              (T*)y_dev, ld_y, mean_dev, rstd_dev);
         });

@@ -212,7 +212,7 @@ k_xent_rows(const T* z, int64_t ld, const int32_t* __restrict__ labels, int64_t 
                 int skip;
                 const uint32_t bytes = zs.window(ln, row, usual, skip), bar = jn.stage(ln, stage);
                 expect_bytes(bar, bytes);
-                zs.send_bulk(ln, row, skip, bytes, ring0 + (uint32_t)(stage * H::STAGE), bar);
+                zs.template send_bulk<false>(ln, row, skip, bytes, ring0 + (uint32_t)(stage * H::STAGE), bar);
             }
         } else if constexpr (MODE != 2) {
             if (base < n)
@@ -359,7 +359,7 @@ k_xent_rows(const T* z, int64_t ld, const int32_t* __restrict__ labels, int64_t 
 #pragma unroll
             for (int p = 0; p < L::PAIRS; ++p) o.set_pair(p, __fmul2_rn(w.e[r][p], q2));
             if (!counts) o.zero();
-            o.store(ln, dz, row, ldd, row < n, n, ed);       // (ends with the warp's lanes in step: no store of theirs comes after)
+            o.template store<true>(ln, dz, row, ldd, row < n, n, ed);       // (ends with the warp's lanes in step: no store of theirs comes after)
             if (w.owner[r]) dz[row * ldd + w.lab[r]] = one_hot;
         }
     };

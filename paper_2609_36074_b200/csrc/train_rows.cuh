@@ -122,8 +122,17 @@ __device__ __forceinline__ void copies_end() { asm volatile("cp.async.commit_gro
 template <int LEFT> __device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(LEFT) : "memory"); }
 
 // One contiguous piece from global to shared memory; arrives at the barrier.  16-byte aligned, a multiple of 16 bytes.
+// ONCE: what is read is the first to leave L2.
+template <bool ONCE>
 __device__ __forceinline__ void bulk_ahead(uint32_t to, const void* from, uint32_t bytes, uint32_t bar)
 {
+    if constexpr (ONCE) {
+        uint64_t policy;
+        asm volatile("createpolicy.fractional.L2::evict_first.b64 %0, 1.0;" : "=l"(policy));
+        asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes.L2::cache_hint [%0], [%1], %2, [%3], %4;"
+                     ::"r"(to), "l"(from), "r"(bytes), "r"(bar), "l"(policy) : "memory");
+        return;
+    }
     asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
                  ::"r"(to), "l"(from), "r"(bytes), "r"(bar) : "memory");
 }
@@ -278,8 +287,9 @@ struct Row {
     struct One { T e; };
     typename std::conditional<MODE == 2, One, V>::type v[NV];
 
-    // By all lanes of the warp, `ok` or not.  (A lane's row is at most 31 rows from another's in its warp.)
-    template <typename LN>
+    // By all lanes of the warp, `ok` or not.  (A lane's row is at most 31 rows from another's in its warp.)  STREAM: what is
+    // written is the first to leave L2.
+    template <bool STREAM, typename LN>
     __device__ __forceinline__ void store(const LN& ln, T* base, int64_t row, int64_t ld, bool ok, int64_t n, Edges<LN>& ed) const
     {
         T* p = base + row * ld;
@@ -290,7 +300,9 @@ struct Row {
                 if constexpr (MODE == 2) {
                     if (ln.any(k)) mine[k * LN::STRIDE] = v[k].e;
                 } else {
-                    if (ln.whole(k)) v[k].store_streaming(mine + k * LN::STRIDE);
+                    if (ln.whole(k)) {
+                        if constexpr (STREAM) v[k].store_streaming(mine + k * LN::STRIDE); else v[k].store(mine + k * LN::STRIDE);
+                    }
                 }
             }
             if constexpr (LN::EDGED) {
@@ -434,10 +446,11 @@ struct Source {
         }
         return usual;
     }
+    template <bool ONCE>
     __device__ __forceinline__ void send_bulk(const L& ln, int64_t row, int skip, uint32_t bytes, uint32_t stage, uint32_t bar) const
     {
         const T* from = base + (row * ld - ln.s + ln.rank * (NV * TPR * N) + skip);
-        if (bytes) bulk_ahead(stage + (uint32_t)(ln.g * NV * TPR * 16 + skip * (int)sizeof(T)), from, bytes, bar);
+        if (bytes) bulk_ahead<ONCE>(stage + (uint32_t)(ln.g * NV * TPR * 16 + skip * (int)sizeof(T)), from, bytes, bar);
     }
     // What every thread of a narrower group sends for.
     __device__ __forceinline__ void send_own(const L& ln, int64_t row, uint32_t stage) const
