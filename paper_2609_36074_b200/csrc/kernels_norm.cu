@@ -317,8 +317,8 @@ k_norm_grad_rows(const T* __restrict__ dy, int64_t lddy, const T* __restrict__ x
                 int sx, sg;
                 const uint32_t bx = xs.window(ln, row, usual, sx), bg = gs.window(ln, row, usual, sg), bar = jn.stage(ln, stage);
                 expect_bytes(bar, bx + bg);
-                xs.template send_bulk<true>(ln, row, sx, bx, o, bar);
-                gs.template send_bulk<true>(ln, row, sg, bg, o + H::ROW, bar);
+                xs.template send_bulk<MODE == 0>(ln, row, sx, bx, o, bar);
+                gs.template send_bulk<MODE == 0>(ln, row, sg, bg, o + H::ROW, bar);
             }
         } else if constexpr (MODE != 2) {
             if (row - ln.g < n) {
@@ -390,7 +390,7 @@ k_norm_grad_rows(const T* __restrict__ dy, int64_t lddy, const T* __restrict__ x
                 const float2 gw = __fmul2_rn(gv.pair(q), w2[q]);
                 xv.set_pair(q, __ffma2_rn(__fadd2_rn(xv.pair(q), m2), c2, __ffma2_rn(gw, r2, c1)));
             }
-            xv.template store<false>(ln, dx, row, lddx, row < n, n, ed);
+            xv.template store<MODE != 0>(ln, dx, row, lddx, row < n, n, ed);
         }
         if (++at == S) { at = 0; phase ^= 1; }
     }
