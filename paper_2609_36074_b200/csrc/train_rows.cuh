@@ -487,7 +487,6 @@ struct Source {
         }
         if constexpr (MODE == 1) {
             if (row < n && near_end(row)) {          // vectors that reach over the matrix's own ends came through no copy
-
 #pragma unroll
                 for (int k = 0; k < NV; ++k)
                     if (((k == 0 && ln.head) || (ln.tail >> k & 1)) && !within(ln, row, k)) {
