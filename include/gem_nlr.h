@@ -335,8 +335,9 @@ int gem_nlr_column_sums_static(const float *U_dev, int64_t n, int32_t r, float *
  * between is held in FP32 or FP64 and rounded once when stored.  Outputs overlap neither each other nor an input,
  * except where a call says so.  Results are the same bits on every call (no floating-point atomics).
  * Work is enqueued on cuda_stream, whose device must be current; nothing is allocated and no call synchronizes,
- * so all of them can be captured into a graph (after a first call of the same kind, which loads the kernel).  scratch_dev (256-byte aligned, at least the bytes that the
- * matching *_scratch_bytes call names, which is 0 for small calls; contents never matter) is used until the work has run.
+ * so all of them can be captured into a graph (after a first call of the same kind, which loads the kernel).
+ * scratch_dev (256-byte aligned, at least the bytes that the matching *_scratch_bytes call names, which is 0 for small
+ * calls; contents never matter) is used until the work has run.
  * Rows have at most 2^30 columns.  Device-side waits are bounded as everywhere in this library; one that runs out, which no
  * healthy run sees, leaves NaN in the results that depend on it.
  * They return GEM_NLR_OK, GEM_NLR_E_INVALID, GEM_NLR_E_WORKSPACE (scratch missing, misaligned or too small) or

@@ -89,8 +89,8 @@ def _rows(t, name):
         shape = t.shape
     n, d = shape
     ld, one = t.stride()
-    if d < 1:
-        raise ValueError(f"{name} has no columns")
+    if not 0 < d <= 1 << 30:
+        raise ValueError(f"{name} has {d} columns")
     if one != 1 and d > 1 and n > 0:
         raise ValueError(f"the columns of {name} are not contiguous")
     return n, d, ld if n > 1 or ld > d else d
@@ -306,7 +306,8 @@ def _dense(t):
 
 def clip_grad_norm(grads, max_norm, out=None, eps=1e-6, stream=None):
     """gem_nlr_clip_grad_norm: scales all tensors by min(1, max_norm / (norm + eps)), in place or into `out` (tensors of
-    the same sizes, in the same order of elements, of the same types or float32), and returns the norm before it, a float32 scalar on the GPU."""
+    the same sizes, in the same order of elements, of the same types or float32), and returns the norm before it, a float32
+    scalar on the GPU."""
     grads = list(grads)
     return _norm_and_clip(grads, max_norm, grads if out is None else list(out), eps, stream)
 
