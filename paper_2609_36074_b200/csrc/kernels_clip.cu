@@ -20,7 +20,8 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kBlocks = kTrainSMs * 4;
 constexpr int kChunk = 2048;           // elements: the grain in which tensors are dealt out
-constexpr int kOneChunks = 64;         // a call of no more is one launch of one cluster: 16384 elements a block
+constexpr int kOneChunks = 64;         // a call of no more is one launch of one cluster: 16384 elements a block.  (258 chunks that
+                                       // way: 17 us on the device against 5.7 in two launches of the whole GPU)
 constexpr int kMaxRecords = 1000;      // 32 bytes a record: within the 32764 bytes of a kernel's parameters
 
 struct Record {

@@ -124,7 +124,9 @@ __device__ __forceinline__ void copies_end() { asm volatile("cp.async.commit_gro
 template <int LEFT> __device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(LEFT) : "memory"); }
 
 // One contiguous piece from global to shared memory; arrives at the barrier.  16-byte aligned, a multiple of 16 bytes.
-// ONCE: what is read is the first to leave L2.
+// ONCE: what is read is the first to leave L2.  Layer norm's aligned rows: 151 us without, 146 with (262144 x 768 bf16); rows
+// that begin anywhere share sectors with their neighbours and lose (gradient 60000 x 1001 89 to 93 us), and so does the cross
+// entropy (131072 x 1000 bf16 93 to 104 us).
 template <bool ONCE>
 __device__ __forceinline__ void bulk_ahead(uint32_t to, const void* from, uint32_t bytes, uint32_t bar)
 {
@@ -786,6 +788,9 @@ inline int spread(int64_t n, int groups, int at_once, int period, int64_t most)
 
 // Whether a call is small enough for one launch of one cluster of up to kOneBlocks blocks that join their sums themselves: at
 // most kOneRows rows a group, by the shape with the fewest groups that any layout of rows of d elements gets.
+// A launch and a scratch allocation cost the caller 3 to 4 us: cross entropy 128 x 1000 bf16 12.4 us a call against 16.1 (5.8
+// on the device against 7.5), layer norm's gradient 128 x 768 14.8 against 18.3.  With eight rows a group eight SMs take
+// longer than that saves (cross entropy 4000 x 33: 12.4 us on the device against 8.0).
 constexpr int kOneBlocks = 8, kOneRows = 4;
 inline bool one_cluster(int64_t n, int64_t d)
 {
