@@ -163,7 +163,7 @@ k_norm_rows(const T* __restrict__ x, int64_t ldx, const void* __restrict__ w, co
     // the rows of the iteration that begins at `base`
     const auto send = [&](int64_t base, int stage) {
         if constexpr (L::BULK) {
-            if (lead && base + ln.g < n) {
+            if (lead && (phase & 6) == 0 && base + ln.g < n) {
                 const uint32_t bar = jn.stage(ln, stage);
                 int skip[R];
                 uint32_t bytes[R], all = 0;
@@ -199,7 +199,7 @@ k_norm_rows(const T* __restrict__ x, int64_t ldx, const void* __restrict__ w, co
         float s[R], mu[R];
         bool here = true;
         if constexpr (L::BULK) {
-            if (base + ln.g < n) here = wait_for(jn.stage(ln, at), phase, &jn.late);
+            if (base + ln.g < n) here = jn.row_ready(ln, at, phase);
         } else if constexpr (MODE != 2) {
             send(base + (S - 1) * R * step, at == 0 ? S - 1 : at - 1);
             copies_wait<S - 1>();
@@ -251,7 +251,7 @@ k_norm_rows(const T* __restrict__ x, int64_t ldx, const void* __restrict__ w, co
             // warp's own and count (warp's mean - mean)^2.  One meeting of the group a row, and no cancellation.
             float v[3][2];
             const float mine[3] = {warp_n, mu[0], s[0]};
-            group_join<TPR, C>(mine, v, jn, turn);
+            group_join<TPR, C>(mine, v, jn, turn, phase);
             float t = v[0][0] * v[1][0] + v[0][1] * v[1][1];
             join_all<SumOp, TPR, C>(t);
             mu[0] = t * inv_d;
@@ -277,6 +277,7 @@ k_norm_rows(const T* __restrict__ x, int64_t ldx, const void* __restrict__ w, co
             }
         }
     }
+    jn.land(ln, phase);
     leave_cluster<C>();
 }
 
@@ -327,7 +328,7 @@ k_norm_grad_rows(const T* __restrict__ dy, int64_t lddy, const T* __restrict__ x
     const auto send = [&](int64_t row, int stage) {
         const uint32_t o = ring0 + (uint32_t)(stage * H::STAGE);
         if constexpr (L::BULK) {
-            if (lead && row < n) {
+            if (lead && (phase & 6) == 0 && row < n) {
                 int sx, sg;
                 const uint32_t bx = xs.window(ln, row, usual, sx), bg = gs.window(ln, row, usual, sg), bar = jn.stage(ln, stage);
                 expect_bytes(bar, bx + bg);
@@ -362,7 +363,7 @@ k_norm_grad_rows(const T* __restrict__ dy, int64_t lddy, const T* __restrict__ x
         float mu = mu_next, rs = rs_next;
         bool here = true;
         if constexpr (L::BULK) {
-            if (row < n) here = wait_for(jn.stage(ln, at), phase, &jn.late);
+            if (row < n) here = jn.row_ready(ln, at, phase);
         } else if constexpr (MODE != 2) {
             send(row + (S - 1) * step, at == 0 ? S - 1 : at - 1);
             copies_wait<S - 1>();
@@ -386,7 +387,7 @@ k_norm_grad_rows(const T* __restrict__ dy, int64_t lddy, const T* __restrict__ x
             s1 = __ffma2_rn(t, w2[q], s1);
         }
         float s[2] = {s0.x + s0.y, (s1.x + s1.y) * rs};
-        group_sum<TPR, C>(s, jn, turn);
+        group_sum<TPR, C>(s, jn, turn, phase);
         // every thread of the group is done with this row's stage, or (where it reads it again) with the one before
         if constexpr (L::BULK && !AGAIN) send(row + S * step, at);
         if constexpr (AGAIN) {
@@ -408,6 +409,7 @@ k_norm_grad_rows(const T* __restrict__ dy, int64_t lddy, const T* __restrict__ x
         }
         if (++at == S) { at = 0; phase ^= 1; }
     }
+    jn.land(ln, phase);
     leave_cluster<C>();
     if (!part && !one) return;
     next_may_start();

@@ -217,7 +217,7 @@ k_xent_rows(const T* z, int64_t ld, const int32_t* __restrict__ labels, int64_t 
     const auto send = [&](int64_t base, int stage) {
         if constexpr (L::BULK) {
             const int64_t row = base + ln.g;
-            if (lead && row < n) {
+            if (lead && (phase & 6) == 0 && row < n) {
                 int skip;
                 const uint32_t bytes = zs.window(ln, row, usual, skip), bar = jn.stage(ln, stage);
                 expect_bytes(bar, bytes);
@@ -274,7 +274,7 @@ k_xent_rows(const T* z, int64_t ld, const int32_t* __restrict__ labels, int64_t 
         if constexpr (L::BULK) {
             w.lab[0] = base + ln.g < n ? next : -1;
             if (base + step + ln.g < n) next = labels[base + step + ln.g];
-            if (base + ln.g < n) here = wait_for(jn.stage(ln, at), phase, &jn.late);
+            if (base + ln.g < n) here = jn.row_ready(ln, at, phase);
         } else if constexpr (MODE != 2) {
             send(base + (S - 1) * R * step, at == 0 ? S - 1 : at - 1);
             copies_wait<S - 1>();
@@ -317,7 +317,7 @@ k_xent_rows(const T* z, int64_t ld, const int32_t* __restrict__ labels, int64_t 
         warp_all<SumOp, TPR>(w.s);
         if constexpr (C > 1) {
             const float mine[2] = {w.bare ? -INFINITY : w.m[0], w.s[0]};
-            join_send<TPR, C>(mine, jn, sent++);
+            join_send<TPR, C>(mine, jn, sent++, phase);
         }
         if (++at == S) { at = 0; phase ^= 1; }
     };
@@ -329,8 +329,8 @@ k_xent_rows(const T* z, int64_t ld, const int32_t* __restrict__ labels, int64_t 
             // each warp's maximum and sum to the row's, at one meeting of the group a row
             float v[2][2];
             const float mine[2] = {w.bare ? -INFINITY : w.m[0], w.s[0]}, m_warp = w.m[0];
-            if constexpr (C > 1) join_wait(v, jn, turn++);
-            else group_join<TPR, C>(mine, v, jn, turn);
+            if constexpr (C > 1) join_wait(v, jn, turn++, phase);
+            else group_join<TPR, C>(mine, v, jn, turn, phase);
             constexpr bool MANY = TPR / 32 * C == 64;
             float t = MANY ? fmaxf(v[0][0], v[0][1]) : v[0][0];
             join_all<MaxOp, TPR, C>(t);
@@ -392,6 +392,7 @@ k_xent_rows(const T* z, int64_t ld, const int32_t* __restrict__ labels, int64_t 
         }
     }
     if (!scaled) grid_ready();
+    jn.land(ln, phase);
     leave_cluster<C>();
     if (C == 1 && one) finish_loss_one(sum, mean, counted, &slot, loss);
     else finish_loss<kRowBlock>(sum, mean, sc, loss);

@@ -149,22 +149,19 @@ __device__ __forceinline__ void barrier_init(uint32_t bar, uint32_t count)
     asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count) : "memory");
 }
 
-// Polls of one wait.  A healthy one ends within microseconds.  One that runs out raises the block's `late` flag: its row's
-// results become NaN, and later waits poll a little only (their copies still have to land), so that the kernel ends whatever
-// has happened.
-constexpr uint32_t kPolls = 1u << 20, kLatePolls = 1u << 12;
+// Polls of a wait.  A healthy one ends within microseconds.  One that runs out leaves NaN in the results that depend on it, and
+// its thread waits for nothing of that kind again, so that the kernel ends whatever has happened.  Messages are waited for
+// longer than rows: a block that gives a row up still sends its messages (NaN) in time, and the cluster's blocks stay in step.
+constexpr uint32_t kPolls = 1u << 20, kLandPolls = 1u << 12, kMessagePolls = 4 * kPolls;
 
-__device__ __forceinline__ bool wait_for(uint32_t bar, uint32_t parity, volatile uint32_t* late)
+__device__ __forceinline__ bool wait_for(uint32_t bar, uint32_t parity, uint32_t polls)
 {
-    uint32_t limit = kPolls;
-    for (uint32_t i = 0; i < limit; ++i) {
+    for (uint32_t i = 0; i < polls; ++i) {
         uint32_t ok;
         asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
                      : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
         if (ok) return true;
-        if ((i & 63u) == 63u && *late) limit = kLatePolls;
     }
-    *late = 1;
     return false;
 }
 
@@ -532,9 +529,34 @@ struct Join {
     float    v[TPR <= 32 ? 1 : PARTS * R * C * kRowBlock / 32];
     uint64_t bar[C > 1 ? PARTS : 1];                             // the parts' arrivals from the cluster's blocks
     uint64_t full[FULLS];                                        // the ring's stages
-    uint32_t late;                                               // a wait has run out
     __device__ __forceinline__ uint32_t part(int h) { return (uint32_t)__cvta_generic_to_shared(&bar[h]); }
     __device__ __forceinline__ uint32_t stage(const LN& ln, int at) { return (uint32_t)__cvta_generic_to_shared(&full[at * LN::GROUPS + ln.g]); }
+    // The group's row in stage `at`, whose turn is at bit 0 of `phase`: whether its copies are complete.  Bit 1 of `phase` says that
+    // a wait of this thread for a row has run out (and bits 3 and on where that was), bit 2 that one for messages has.  After
+    // the first it waits for no row, and after either it sends for none: the stage's barrier has an arrival that was not answered
+    // and takes no second one, and without messages nobody tells when all warps are done with a stage.
+    __device__ __forceinline__ bool row_ready(const LN& ln, int at, uint32_t& phase)
+    {
+        if (phase & 2) return false;
+        if (wait_for(stage(ln, at), phase & 1, kPolls)) return true;
+        phase |= 2 | (phase & 1) << 3 | (uint32_t)at << 4;
+        return false;
+    }
+    // After the last row: what is still on its way is given time to land, so that no copy meets whatever the memory is used for
+    // next.
+    __device__ __forceinline__ void land(const LN& ln, uint32_t phase)
+    {
+        if constexpr (LN::BULK) {
+            if (phase & 2) {
+                uint32_t parity = phase >> 3 & 1;
+#pragma unroll 1
+                for (int i = 0, at = (int)(phase >> 4); i < S; ++i) {
+                    wait_for(stage(ln, at), parity, kLandPolls);
+                    if (++at == S) { at = 0; parity ^= 1; }
+                }
+            }
+        }
+    }
     // before the first use, by all threads
     __device__ __forceinline__ void begin()
     {
@@ -545,7 +567,6 @@ struct Join {
                 if constexpr (C > 1)
                     for (int h = 0; h < PARTS; ++h) barrier_init(part(h), 1);
                 asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-                late = 0;
                 if constexpr (C > 1)
 #pragma unroll
                     for (int h = 0; h < PARTS; ++h) expect_bytes(part(h), W * R * (uint32_t)sizeof(float));
@@ -575,11 +596,11 @@ __device__ __forceinline__ void warp_all(float (&v)[R])
 // of that part.  A warp that sends once more before it waits needs four: it has then seen values of two calls before, sent
 // after the reads of four calls before.
 template <int TPR, int C, int R, typename J>
-__device__ __forceinline__ void join_send(const float (&v)[R], J& jn, uint32_t turn)
+__device__ __forceinline__ void join_send(const float (&v)[R], J& jn, uint32_t turn, uint32_t phase)
 {
     constexpr int W = J::W;
     const int warp = threadIdx.x >> 5, l = threadIdx.x & 31, p = turn % J::PARTS;
-    if (l < C) {
+    if (l < C && (phase & 4) == 0) {
         const uint32_t mine = (uint32_t)__cvta_generic_to_shared(jn.v + p * R * W + cluster_rank() * (TPR / 32) + warp);
         const uint32_t bar = jn.part(p);
         uint32_t there, there_bar;
@@ -605,21 +626,25 @@ __device__ __forceinline__ void join_read(const float* b, bool here, float (&out
     }
 }
 
+// A wait that runs out is the thread's last (bit 2 of `phase`, see row_ready): its part is not complete, and its next turn would
+// seem to be.  The first thread, which arms the parts, then arms no more (an incomplete part takes no second arrival), and
+// the warp sends no more, which lets all others run out at their next waits: every row from here on is NaN.
 template <int R, typename J>
-__device__ __forceinline__ void join_wait(float (&out)[R][2], J& jn, uint32_t turn)
+__device__ __forceinline__ void join_wait(float (&out)[R][2], J& jn, uint32_t turn, uint32_t& phase)
 {
     const int p = turn % J::PARTS;
-    const bool here = wait_for(jn.part(p), (turn / J::PARTS) & 1, &jn.late);
-    if (threadIdx.x == 0) expect_bytes(jn.part(p), J::W * R * (uint32_t)sizeof(float));          // for the part's next use
+    const bool here = (phase & 4) == 0 && wait_for(jn.part(p), (turn / J::PARTS) & 1, kMessagePolls);
+    if (!here) phase |= 4;
+    else if (threadIdx.x == 0) expect_bytes(jn.part(p), J::W * R * (uint32_t)sizeof(float));          // for the part's next use
     join_read(jn.v + p * R * J::W, here, out, jn);
 }
 
 template <int TPR, int C, int R, typename J>
-__device__ __forceinline__ void group_join(const float (&v)[R], float (&out)[R][2], J& jn, uint32_t& turn)
+__device__ __forceinline__ void group_join(const float (&v)[R], float (&out)[R][2], J& jn, uint32_t& turn, uint32_t& phase)
 {
     if constexpr (C > 1) {
-        join_send<TPR, C>(v, jn, turn);
-        join_wait(out, jn, turn);
+        join_send<TPR, C>(v, jn, turn, phase);
+        join_wait(out, jn, turn, phase);
     } else {
         constexpr int W = J::W;
         const int g = threadIdx.x / TPR, warp = (threadIdx.x % TPR) >> 5;
@@ -645,12 +670,12 @@ __device__ __forceinline__ void join_all(float& t)
 
 // Sums of R values over a group.
 template <int TPR, int C, int R, typename J>
-__device__ __forceinline__ void group_sum(float (&v)[R], J& jn, uint32_t& turn)
+__device__ __forceinline__ void group_sum(float (&v)[R], J& jn, uint32_t& turn, uint32_t& phase)
 {
     warp_all<SumOp, TPR>(v);
     if constexpr (TPR > 32) {
         float o[R][2];
-        group_join<TPR, C>(v, o, jn, turn);
+        group_join<TPR, C>(v, o, jn, turn, phase);
 #pragma unroll
         for (int r = 0; r < R; ++r) {
             v[r] = o[r][0] + o[r][1];

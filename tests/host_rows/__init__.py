@@ -51,7 +51,7 @@ class Rows:
         L = self.L = C.CDLL(path)
         vp, i32, i64, f32, size = C.c_void_p, C.c_int32, C.c_int64, C.c_float, C.c_size_t
         self.dtype, self.type = TYPES[kind]
-        L.emu_begin.argtypes = [i32, C.c_uint64, i32]
+        L.emu_begin.argtypes = [i32, C.c_uint64, i32, i32]
         L.emu_region.argtypes = [vp, size]
         L.emu_report.restype = C.c_char_p
         if name == "norm":
@@ -64,9 +64,9 @@ class Rows:
             L.gem_nlr_label_cross_entropy_scratch_bytes.argtypes = [i64, i32]
             L.gem_nlr_label_cross_entropy_scratch_bytes.restype = size
 
-    def run(self, fn, *args, reads=(), resident=2, seed=1, lost=0):
+    def run(self, fn, *args, reads=(), resident=2, seed=1, lost=0, lost_message=0):
         """The return code; what the emulation recorded is in `report`."""
-        self.L.emu_begin(resident, seed, lost)
+        self.L.emu_begin(resident, seed, lost, lost_message)
         for m in reads:
             if m is not None and m.numel():
                 last = sum((n - 1) * s for n, s in zip(m.shape, m.stride()))

@@ -63,7 +63,7 @@ struct Grid {
 extern Grid* grid;
 extern Fiber* self;
 extern int resident;                             // clusters that a launch may have at most
-extern int lost;                                 // number of the bulk copy that never lands; 0: none
+extern int lost, lost_message;                   // number of the bulk copy, the message, that never lands; 0: none
 extern uint64_t state;
 extern char report[200];
 extern std::vector<std::pair<const char*, size_t>> regions;
@@ -218,6 +218,7 @@ inline void op_st_async_shared__cluster_mbarrier__complete_tx__bytes_b32(uint32_
 {
     int b;
     unsigned char* p = at(to, b);
+    if (lost_message > 0 && --lost_message == 0) return;
     grid->on_their_way.push_back({2, nullptr, p, 4, b, bar & 0xffffff, v, -1, 0});
 }
 inline void op_ld_shared__cluster_f64(double& v, uint32_t a) { memcpy(&v, at(a), 8); }

@@ -124,7 +124,7 @@ def _cut(s, begin, end, instead):
 
 
 def translate(csrc, header, out, only, polls=None):
-    """Writes the translated sources of one element type to the folder `out`; polls: limits of a wait and of one after it."""
+    """Writes the translated sources of one element type to the folder `out`; polls: the limit of a wait for a row and of the one after it."""
     shared = _Shared()
     for name in FILES:
         with open(os.path.join(csrc, name)) as f:
@@ -135,7 +135,7 @@ def translate(csrc, header, out, only, polls=None):
                      "template <auto K, int C> int resident_clusters(int) { return emu::resident; }\n")
             s = _cut(s, "// Launch of `blocks` blocks", "}  // namespace gemnlr", "using emu::launch_rows;\nusing emu::launch_early;\n")
             if polls:
-                s, n = re.subn(r"kPolls = [^,]+, kLatePolls = [^;]+;", f"kPolls = {polls[0]}, kLatePolls = {polls[1]};", s)
+                s, n = re.subn(r"kPolls = [^,]+, kLandPolls = [^,]+,", f"kPolls = {polls[0]}, kLandPolls = {polls[1]},", s)
                 assert n == 1
         if name == "train_common.cuh":
             s = _cut(s, "template <typename F> inline int by_type", "constexpr int kTrainSMs",

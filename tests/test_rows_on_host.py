@@ -85,3 +85,80 @@ def test_rows(libs, case, kind):
             if g is not None:
                 ref.assert_within(g, v, e, name)
         assert dz is None or dz.kept()
+
+
+# A copy that never lands, as no healthy run sees it: shapes of a warp, two, four and eight warps a row, and clusters of two, four
+# and eight blocks; rows enough that the ring comes round after it.
+LATE = [("f32", 60, 520, 5), ("f32", 40, 777, 9), ("f32", 40, 1000, 7), ("f32", 30, 1500, 6), ("f32", 30, 4096, 3), ("f32", 20, 6200, 2),
+        ("f32", 18, 8200, 4), ("f32", 14, 16400, 9), ("f32", 12, 25003, 11), ("bf16", 90, 768, 30), ("bf16", 40, 1001, 11),
+        ("bf16", 30, 4096, 5), ("bf16", 20, 9000, 3), ("bf16", 12, 24576, 12)]
+
+
+def late_inputs(kind, n, d):
+    dtype = host_rows.TYPES[kind][0]
+    return given(n, d, dtype, d, 0, d, 1.0, 0.5).m, given(n, d, dtype, d, 0, d + 1, 0.1).m, dtype
+
+
+def healthy_or_nan(got, want):
+    """Rows of `got` that hold a NaN; every other element has to be what it is without the loss."""
+    bad = got.isnan()
+    assert torch.equal(got[~bad], want[~bad])
+    rows = bad.any(1) if got.dim() > 1 else bad
+    if got.dim() > 1:
+        assert bad[rows].all()
+    return rows
+
+
+@pytest.mark.parametrize("kind,n,d,lost", LATE)
+def test_a_copy_that_never_lands(libs, kind, n, d, lost):
+    """Rows that depend on it are NaN, no barrier gets an arrival too many, no block ends while copies are on their way."""
+    x, dy, dtype = late_inputs(kind, n, d)
+    norm, xent = libs["norm", kind], libs["xent", kind]
+    w, b = torch.ones(d), torch.zeros(d)
+    got = []
+    for k in (0, lost):
+        y, mean, rstd = torch.zeros(n, d, dtype=dtype), torch.empty(n), torch.empty(n)
+        assert norm.layer_norm(x, w, b, y, mean, rstd, resident=1, seed=d, lost=k) == 0 and norm.report == ""
+        got.append((y, mean, rstd))
+    rows = healthy_or_nan(got[1][0], got[0][0])
+    assert rows.any() and torch.equal(healthy_or_nan(got[1][1], got[0][1]), rows) and torch.equal(healthy_or_nan(got[1][2], got[0][2]), rows)
+    _, mean, rstd = got[0]
+    got = []
+    for k in (0, lost):
+        dx, dw, db = torch.zeros(n, d, dtype=dtype), torch.zeros(d), torch.zeros(d)
+        assert norm.layer_norm_backward(dy, x, mean, rstd, w, dx, dw, db, resident=1, seed=d, lost=k) == 0 and norm.report == ""
+        got.append(dx)
+    assert healthy_or_nan(got[1], got[0]).any()
+    labels = (torch.arange(n) % d).to(torch.int32)
+    got = []
+    for k in (0, min(lost, n)):
+        loss, row, dz = torch.zeros(()), torch.zeros(n), torch.zeros(n, d, dtype=dtype)
+        assert xent.label_cross_entropy(x, labels, True, loss, row, dz, resident=1, seed=d, lost=k) == 0 and xent.report == ""
+        got.append((loss, row, dz))
+    rows = healthy_or_nan(got[1][2], got[0][2])
+    assert rows.any() and torch.equal(healthy_or_nan(got[1][1], got[0][1]), rows) and got[1][0].isnan()
+
+
+@pytest.mark.parametrize("kind,n,d,lost", [("f32", 20, 6200, 9), ("f32", 14, 24576, 300), ("f32", 12, 32768, 2000), ("bf16", 20, 9000, 100)])
+def test_a_message_that_never_lands(libs, kind, n, d, lost):
+    """What the cluster works out after it is NaN; nothing is wrong, and nothing waits for ever."""
+    x, dy, dtype = late_inputs(kind, n, d)
+    norm, xent = libs["norm", kind], libs["xent", kind]
+    w, b = torch.ones(d), torch.zeros(d)
+    labels = (torch.arange(n) % d).to(torch.int32)
+    got = []
+    for k in (0, lost):
+        y, mean, rstd = torch.zeros(n, d, dtype=dtype), torch.empty(n), torch.empty(n)
+        assert norm.layer_norm(x, w, b, y, mean, rstd, resident=1, seed=d, lost_message=k) == 0 and norm.report == ""
+        if not got:
+            stats = mean, rstd
+        dx, dw, db = torch.zeros(n, d, dtype=dtype), torch.zeros(d), torch.zeros(d)
+        assert norm.layer_norm_backward(dy, x, *stats, w, dx, dw, db, resident=1, seed=d, lost_message=k) == 0 and norm.report == ""
+        loss, row, dz = torch.zeros(()), torch.zeros(n), torch.zeros(n, d, dtype=dtype)
+        assert xent.label_cross_entropy(x, labels, True, loss, row, dz, resident=1, seed=d, lost_message=k) == 0 and xent.report == ""
+        got.append((y, dx, dz, mean, rstd, row))
+    for i, (a, c) in enumerate(zip(got[1], got[0])):
+        bad = a.isnan()
+        assert torch.equal(a[~bad], c[~bad]), i
+        if i < 3:
+            assert bad.any() and not bad.all(), i
