@@ -416,6 +416,12 @@ k_norm_grad_rows(const T* __restrict__ dy, int64_t lddy, const T* __restrict__ x
     copies_wait<0>();
     float* sums = reinterpret_cast<float*>(ring);
     float* rec = one ? sums + kRowBlock * EPL : part + (int64_t)(blockIdx.x / C) * record_stride(d);
+    // whether one of the block's rows never came (after a meeting of the block): its sums are NaN then
+    const auto lost = [&] {
+        if constexpr (L::BULK) return *(volatile uint32_t*)&jn.row_lost != 0;
+        else return false;
+    };
+    const float nan = __int_as_float(0x7fffffff);
     // the records of a grid that is one cluster, joined by its blocks (in block order, FP64)
     const auto join_one = [&] {
         if constexpr (C == 1) {
@@ -448,9 +454,10 @@ k_norm_grad_rows(const T* __restrict__ dy, int64_t lddy, const T* __restrict__ x
                 else { sums[p] = a.x; sums[p + kRowBlock] = a.y; }
             }
             __syncthreads();
+            const bool none = lost();
             for (int p = threadIdx.x; p < kRowBlock * EPL; p += kRowBlock) {
                 const int e = from + p;
-                if (e >= 0 && e < d) rec[which * d + e] = sums[p];
+                if (e >= 0 && e < d) rec[which * d + e] = none ? nan : sums[p];
             }
         }
         if (one) join_one();
@@ -471,6 +478,7 @@ k_norm_grad_rows(const T* __restrict__ dy, int64_t lddy, const T* __restrict__ x
         // in two steps where a row is narrower than the block: its threads share a column's groups
         constexpr int SPLIT = W < kRowBlock ? kRowBlock / W : 1, EACH = L::GROUPS / SPLIT;
         __syncthreads();
+        const bool none = lost();
         for (int e = threadIdx.x % W; e < W; e += kRowBlock) {
             const int q0 = SPLIT > 1 ? (int)threadIdx.x / W * EACH : 0;
             float t = 0.0f;
@@ -478,7 +486,7 @@ k_norm_grad_rows(const T* __restrict__ dy, int64_t lddy, const T* __restrict__ x
 #pragma unroll
                 for (int q = 0; q < EACH; ++q) t += sums[(q0 + q) * W + e];
             if constexpr (SPLIT > 1) sums[q0 * W + e] = t;               // (only this thread reads that place)
-            else if (e < d) rec[which * d + e] = t;
+            else if (e < d) rec[which * d + e] = none ? nan : t;
         }
         if constexpr (SPLIT > 1) {
             __syncthreads();
@@ -486,7 +494,7 @@ k_norm_grad_rows(const T* __restrict__ dy, int64_t lddy, const T* __restrict__ x
                 float t = 0.0f;
 #pragma unroll
                 for (int q = 0; q < SPLIT; ++q) t += sums[q * EACH * W + threadIdx.x];
-                rec[which * d + threadIdx.x] = t;
+                rec[which * d + threadIdx.x] = none ? nan : t;
             }
         }
     }

@@ -529,6 +529,7 @@ struct Join {
     float    v[TPR <= 32 ? 1 : PARTS * R * C * kRowBlock / 32];
     uint64_t bar[C > 1 ? PARTS : 1];                             // the parts' arrivals from the cluster's blocks
     uint64_t full[FULLS];                                        // the ring's stages
+    uint32_t row_lost;                                           // whether a thread's wait for a row has run out (BULK)
     __device__ __forceinline__ uint32_t part(int h) { return (uint32_t)__cvta_generic_to_shared(&bar[h]); }
     __device__ __forceinline__ uint32_t stage(const LN& ln, int at) { return (uint32_t)__cvta_generic_to_shared(&full[at * LN::GROUPS + ln.g]); }
     // The group's row in stage `at`, whose turn is at bit 0 of `phase`: whether its copies are complete.  Bit 1 of `phase` says that
@@ -543,7 +544,7 @@ struct Join {
         return false;
     }
     // After the last row: what is still on its way is given time to land, so that no copy meets whatever the memory is used for
-    // next.
+    // next, and sums over the rows are told (row_lost is theirs to read after a meeting of the block).
     __device__ __forceinline__ void land(const LN& ln, uint32_t phase)
     {
         if constexpr (LN::BULK) {
@@ -554,6 +555,7 @@ struct Join {
                     wait_for(stage(ln, at), parity, kLandPolls);
                     if (++at == S) { at = 0; parity ^= 1; }
                 }
+                *(volatile uint32_t*)&row_lost = 1;
             }
         }
     }
@@ -567,6 +569,7 @@ struct Join {
                 if constexpr (C > 1)
                     for (int h = 0; h < PARTS; ++h) barrier_init(part(h), 1);
                 asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+                row_lost = 0;
                 if constexpr (C > 1)
 #pragma unroll
                     for (int h = 0; h < PARTS; ++h) expect_bytes(part(h), W * R * (uint32_t)sizeof(float));

@@ -162,3 +162,22 @@ def test_a_message_that_never_lands(libs, kind, n, d, lost):
         assert torch.equal(a[~bad], c[~bad]), i
         if i < 3:
             assert bad.any() and not bad.all(), i
+
+
+@pytest.mark.parametrize("need_dx", [True, False])
+@pytest.mark.parametrize("kind,n,d,lost", LATE)
+def test_sums_over_rows_that_never_came(libs, kind, n, d, lost, need_dx):
+    """The weight's and the bias's gradient are NaN in every column of which a row was lost, and right in the others."""
+    x, dy, dtype = late_inputs(kind, n, d)
+    norm = libs["norm", kind]
+    mean, rstd = torch.full((n,), 0.5), torch.ones(n)
+    w = torch.ones(d)
+    want, bound = ref.norm_grad(dy, x, mean, rstd, w, torch.float32)
+    dx, dw, db = torch.zeros(n, d, dtype=dtype) if need_dx else None, torch.zeros(d), torch.zeros(d)
+    assert norm.layer_norm_backward(dy, x, mean, rstd, w, dx, dw, db, resident=1, seed=d, lost=lost) == 0 and norm.report == ""
+    bad = dw.isnan()
+    assert torch.equal(bad, db.isnan()) and bad.any()
+    if d <= 4096:
+        assert bad.all()                                  # one block a row
+    for g, v, e in ((dw, want[1], bound[1]), (db, want[2], bound[2])):
+        ref.assert_within(g[~bad], v[~bad], e[~bad])
