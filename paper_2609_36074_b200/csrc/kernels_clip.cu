@@ -222,7 +222,7 @@ k_clip_one(const __grid_constant__ Table<CAP> tb, int scale, float max_norm, flo
     if (scale) all_scaled(tb, q0, q1, clip_factor(norm, max_norm, eps));
 }
 
-__device__ __forceinline__ double norm_of(const double* __restrict__ part, int parts, double* sred)
+__device__ __forceinline__ double norm_of(const double* part, int parts, double* sred)
 {
     double v = 0.0;
     for (int i = threadIdx.x; i < parts; i += kThreads) v += part[i];
@@ -230,7 +230,7 @@ __device__ __forceinline__ double norm_of(const double* __restrict__ part, int p
 }
 
 __global__ void __launch_bounds__(kThreads)
-k_clip_norm(const double* __restrict__ part, int parts, float* __restrict__ norm)
+k_clip_norm(const double* part, int parts, float* __restrict__ norm)
 {
     __shared__ double sred[kThreads / 32];
     grid_ready();
@@ -240,7 +240,7 @@ k_clip_norm(const double* __restrict__ part, int parts, float* __restrict__ norm
 
 template <int CAP>
 __global__ void __launch_bounds__(kThreads, 4)
-k_clip_scale(const __grid_constant__ Table<CAP> tb, const double* __restrict__ part, int parts, float max_norm, float eps,
+k_clip_scale(const __grid_constant__ Table<CAP> tb, const double* part, int parts, float max_norm, float eps,
              float* __restrict__ norm_out)
 {
     __shared__ double sred[kThreads / 32];

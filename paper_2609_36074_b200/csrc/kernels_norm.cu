@@ -504,7 +504,7 @@ k_norm_grad_rows(const T* __restrict__ dy, int64_t lddy, const T* __restrict__ x
 // dw, db: 128 columns a block, four to a lane; the block's 32 warps share the records out.  Fixed order, FP64.
 template <typename W>
 __global__ void __launch_bounds__(1024)
-k_norm_dw_join(const float* __restrict__ part, int records, int d, W* __restrict__ dw, W* __restrict__ db)
+k_norm_dw_join(const float* part, int records, int d, W* __restrict__ dw, W* __restrict__ db)
 {
     __shared__ double s[32][128];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, e = blockIdx.x * 128 + lane * 4;

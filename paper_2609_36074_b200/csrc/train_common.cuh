@@ -65,7 +65,9 @@ template <typename F> inline int by_type(int32_t type, F f)
 constexpr int kTrainSMs = 148, kTrainDevices = 64;
 
 // Programmatic launches: the kernel before says that the next one may begin; that one waits for the kernel before to be
-// complete (every block of it has to, or the kernel after it might begin before the first one is done).
+// complete (every block of it has to, or the kernel after it might begin before the first one is done).  What the kernel
+// before writes is read through plain pointers: const __restrict__ says that nobody writes it while this kernel runs, and lets
+// the compiler read it before the wait.
 __device__ __forceinline__ void next_may_start() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 __device__ __forceinline__ void grid_ready() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 
