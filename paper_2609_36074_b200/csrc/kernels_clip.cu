@@ -270,7 +270,7 @@ bool fill(Table<CAP>& tb, const gem_nlr_tensor* ts, int count)
 template <int CAP>
 int clip_all(const gem_nlr_tensor* ts, int32_t count, bool scale, float max_norm, float eps, float* norm, double* part, cudaStream_t st)
 {
-    static thread_local Table<CAP> tb;               // 32 KB: not on the caller's stack
+    static thread_local Table<CAP> tb;               // 32 KB: not on the caller's stack, nor copied there by the launches
     const int launches = clip_launches(count) < 1 ? 1 : clip_launches(count);
     int parts = 0;
     if (launches == 1) {
@@ -284,25 +284,23 @@ int clip_all(const gem_nlr_tensor* ts, int32_t count, bool scale, float max_norm
         const int first = l * kMaxRecords, m = count - first < kMaxRecords ? count - first : kMaxRecords;
         if (!fill(tb, ts + first, m)) return GEM_NLR_E_INVALID;
         const int blocks = tb.chunks < 1 ? 1 : tb.chunks < (uint32_t)kBlocks ? (int)tb.chunks : kBlocks;
-        k_clip_squares<CAP><<<blocks, kThreads, 0, st>>>(tb, part + parts);
+        const int rc = told(launch(k_clip_squares<CAP>, dim3((unsigned)blocks), kThreads, 1, 0, false, st, tb, part + parts));
+        if (rc != GEM_NLR_OK) return rc;
         parts += blocks;
     }
-    if (launched() != GEM_NLR_OK) return GEM_NLR_E_CUDA;
     if (!scale)
-        return told(launch_early(k_clip_norm, dim3(1), kThreads, st, (const double*)part, parts, norm));
+        return told(launch_early(k_clip_norm, dim3(1), kThreads, st, part, parts, norm));
     for (int l = launches - 1; l >= 0; --l) {
         const int first = l * kMaxRecords, m = count - first < kMaxRecords ? count - first : kMaxRecords;
         if (launches > 1) fill(tb, ts + first, m);
         const int blocks = tb.chunks < 1 ? 1 : tb.chunks < (uint32_t)kBlocks ? (int)tb.chunks : kBlocks;
         // only the first one may begin early: it waits for the squares, the others for it
-        if (l == launches - 1) {
-            const int rc = told(launch_early(k_clip_scale<CAP>, dim3((unsigned)blocks), kThreads, st, tb, (const double*)part, parts, max_norm, eps, norm));
-            if (rc != GEM_NLR_OK) return rc;
-        } else {
-            k_clip_scale<CAP><<<blocks, kThreads, 0, st>>>(tb, part, parts, max_norm, eps, nullptr);
-        }
+        const bool early = l == launches - 1;
+        const int rc = told(launch(k_clip_scale<CAP>, dim3((unsigned)blocks), kThreads, 1, 0, early, st, tb, part, parts, max_norm, eps,
+                                   early ? norm : nullptr));
+        if (rc != GEM_NLR_OK) return rc;
     }
-    return launched();
+    return GEM_NLR_OK;
 }
 
 }  // namespace

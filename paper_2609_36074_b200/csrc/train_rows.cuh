@@ -866,14 +866,16 @@ inline int told(cudaError_t e)
     return GEM_NLR_E_CUDA;
 }
 
-// Launch of `blocks` blocks of kRowBlock threads with `shared` bytes of dynamic shared memory in clusters of c; `early`: it may begin while the stream's last kernel ends
-// (and waits for its results with grid_ready()).
-template <typename... P, typename... A>
-cudaError_t launch_rows(void (*k)(P...), int blocks, int c, int shared, bool early, cudaStream_t st, A... args)
+// Launch of `blocks` blocks of kRowBlock threads with `shared` bytes of dynamic shared memory in clusters of c; `early`: it may
+// begin while the stream's last kernel ends (and waits for its results with grid_ready()).  Arguments go to the driver by
+// address: a table of records is 32 KB, and copies of it on the way would be on the caller's stack, which may be small.
+template <typename P> struct Same { using type = P; };
+template <typename... P>
+cudaError_t launch(void (*k)(P...), dim3 grid, int threads, int c, int shared, bool early, cudaStream_t st, const typename Same<P>::type&... args)
 {
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)blocks);
-    cfg.blockDim = dim3(kRowBlock);
+    cfg.gridDim = grid;
+    cfg.blockDim = dim3((unsigned)threads);
     cfg.dynamicSmemBytes = (size_t)shared;
     cfg.stream = st;
     cudaLaunchAttribute at[2] = {};
@@ -890,23 +892,20 @@ cudaError_t launch_rows(void (*k)(P...), int blocks, int c, int shared, bool ear
     }
     cfg.attrs = at;
     cfg.numAttrs = (unsigned)m;
-    return cudaLaunchKernelEx(&cfg, k, (P)args...);
+    void* list[] = {const_cast<void*>(static_cast<const void*>(&args))...};
+    return cudaLaunchKernelExC(&cfg, reinterpret_cast<const void*>(k), list);
+}
+template <typename... P>
+cudaError_t launch_rows(void (*k)(P...), int blocks, int c, int shared, bool early, cudaStream_t st, const typename Same<P>::type&... args)
+{
+    return launch(k, dim3((unsigned)blocks), kRowBlock, c, shared, early, st, args...);
 }
 
 // Launch behind `st`'s last kernel that may begin while it ends.
-template <typename... P, typename... A>
-cudaError_t launch_early(void (*k)(P...), dim3 grid, int threads, cudaStream_t st, A... args)
+template <typename... P>
+cudaError_t launch_early(void (*k)(P...), dim3 grid, int threads, cudaStream_t st, const typename Same<P>::type&... args)
 {
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = grid;
-    cfg.blockDim = dim3((unsigned)threads);
-    cfg.stream = st;
-    cudaLaunchAttribute at = {};
-    at.id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    at.val.programmaticStreamSerializationAllowed = 1;
-    cfg.attrs = &at;
-    cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, k, (P)args...);
+    return launch(k, grid, threads, 1, 0, true, st, args...);
 }
 
 }  // namespace gemnlr
