@@ -21,17 +21,16 @@ __global__ void __launch_bounds__(kRowThreads)
 k_norm_any(const T* __restrict__ x, int64_t ldx, const W* __restrict__ w, const W* __restrict__ b, int64_t n, int d,
            float eps, T* __restrict__ y, int64_t ldy, float* __restrict__ mean, float* __restrict__ rstd)
 {
-    __shared__ float sred[kRowThreads / 32];
-    const float inv_d = 1.0f / (float)d;
+    __shared__ double sred[kRowThreads / 32];
+    const double inv_d = 1.0 / (double)d;
     for (int64_t row = blockIdx.x; row < n; row += gridDim.x) {
         const T* xr = x + row * ldx;
         T* yr = y + row * ldy;
-        float s = 0.0f;
-        for (int j = threadIdx.x; j < d; j += kRowThreads) s += to_f(xr[j]);
-        const float mu = block_sum_f<kRowThreads>(s, sred) * inv_d;
-        s = 0.0f;
-        for (int j = threadIdx.x; j < d; j += kRowThreads) { const float c = to_f(xr[j]) - mu; s += c * c; }
-        const float r = 1.0f / sqrtf(block_sum_f<kRowThreads>(s, sred) * inv_d + eps);
+        double s[1];
+        thread_sums<kRowThreads>(d, s, [&](int j, float (&p)[1]) { p[0] += to_f(xr[j]); });
+        const float mu = (float)(block_sum<kRowThreads>(s[0], sred) * inv_d);
+        thread_sums<kRowThreads>(d, s, [&](int j, float (&p)[1]) { const float c = to_f(xr[j]) - mu; p[0] += c * c; });
+        const float r = 1.0f / sqrtf((float)(block_sum<kRowThreads>(s[0], sred) * inv_d) + eps);
         for (int j = threadIdx.x; j < d; j += kRowThreads) {
             const float h = (to_f(xr[j]) - mu) * r;
             yr[j] = from_f<T>(h * (w ? to_f(w[j]) : 1.0f) + (b ? to_f(b[j]) : 0.0f));
@@ -48,19 +47,19 @@ __global__ void __launch_bounds__(kRowThreads)
 k_norm_dx_any(const T* __restrict__ dy, int64_t lddy, const T* __restrict__ x, int64_t ldx, const float* __restrict__ mean,
               const float* __restrict__ rstd, const W* __restrict__ w, int64_t n, int d, T* __restrict__ dx, int64_t lddx)
 {
-    __shared__ float sred[kRowThreads / 32];
-    const float inv_d = 1.0f / (float)d;
+    __shared__ double sred[kRowThreads / 32];
+    const double inv_d = 1.0 / (double)d;
     for (int64_t row = blockIdx.x; row < n; row += gridDim.x) {
         const T *xr = x + row * ldx, *gr = dy + row * lddy;
         const float mu = mean[row], r = rstd[row];
-        float s1 = 0.0f, s2 = 0.0f;
-        for (int j = threadIdx.x; j < d; j += kRowThreads) {
+        double s[2];
+        thread_sums<kRowThreads>(d, s, [&](int j, float (&p)[2]) {
             const float g = to_f(gr[j]) * (w ? to_f(w[j]) : 1.0f);
-            s1 += g;
-            s2 += g * ((to_f(xr[j]) - mu) * r);
-        }
-        const float c1 = block_sum_f<kRowThreads>(s1, sred) * inv_d;
-        const float c2 = block_sum_f<kRowThreads>(s2, sred) * inv_d;
+            p[0] += g;
+            p[1] += g * ((to_f(xr[j]) - mu) * r);
+        });
+        const float c1 = (float)(block_sum<kRowThreads>(s[0], sred) * inv_d);
+        const float c2 = (float)(block_sum<kRowThreads>(s[1], sred) * inv_d);
         for (int j = threadIdx.x; j < d; j += kRowThreads) {
             const float g = to_f(gr[j]) * (w ? to_f(w[j]) : 1.0f);
             dx[row * lddx + j] = from_f<T>(r * (g - c1 - (to_f(xr[j]) - mu) * r * c2));

@@ -107,6 +107,7 @@ k_xent_any(const T* z, int64_t ld, const int32_t* __restrict__ labels, int64_t n
            Scratch* sc, float* __restrict__ loss, float* __restrict__ row_loss, T* dz, int64_t ldd)
 {
     __shared__ float sred[kRowThreads / 32];
+    __shared__ double dred[kRowThreads / 32];
     grid_ready();
     const float scale = loss_scale(sc, mean);
     double sum = 0.0;
@@ -123,9 +124,9 @@ k_xent_any(const T* z, int64_t ld, const int32_t* __restrict__ labels, int64_t n
         for (int j = threadIdx.x; j < k; j += kRowThreads) m = fmaxf(m, to_f(zr[j]));
         m = block_max_f<kRowThreads>(m, sred);
         const float base = m == -INFINITY ? 0.0f : m;           // nothing but -inf (or NaN): no -inf - -inf below
-        float s = 0.0f;
-        for (int j = threadIdx.x; j < k; j += kRowThreads) s += expf(to_f(zr[j]) - base);
-        s = block_sum_f<kRowThreads>(s, sred);
+        double total[1];
+        thread_sums<kRowThreads>(k, total, [&](int j, float (&p)[1]) { p[0] += expf(to_f(zr[j]) - base); });
+        const float s = (float)block_sum<kRowThreads>(total[0], dred);
         const float nan = __int_as_float(0x7fffffff);
         const float zl = lab < k ? to_f(zr[lab]) : nan;
         if (threadIdx.x == 0) {

@@ -26,20 +26,24 @@ template <> __device__ __forceinline__ __nv_bfloat16 from_f<__nv_bfloat16>(float
 inline int type_bytes(int32_t type) { return type == GEM_NLR_F32 ? 4 : (type == GEM_NLR_F16 || type == GEM_NLR_BF16) ? 2 : 0; }
 inline bool aligned_to(const void* p, size_t bytes) { return (reinterpret_cast<uintptr_t>(p) & (bytes - 1)) == 0; }
 
-// Sum over the block (fixed order), the same value in every thread; sred: NT / 32 floats, reusable at once.
-template <int NT>
-__device__ __forceinline__ float block_sum_f(float v, float* sred)
+// Sums over a thread's terms of a row that a block of NT threads shares: in FP32 over 32 terms at a time, in FP64 beyond.
+// (Terms that are alike round the same way: 2^17 of them in one FP32 sum are off by parts in a thousand.  It costs nothing:
+// layer norm 64 x 70000 FP32 118 -> 110 us, cross entropy 64 x 131073 196 -> 186.)
+template <int NT, int N, typename F>
+__device__ __forceinline__ void thread_sums(int d, double (&sum)[N], F term)
 {
-    v = warp_sum(v);
-    __syncthreads();
-    if ((threadIdx.x & 31) == 0) sred[threadIdx.x >> 5] = v;
-    __syncthreads();
-    float t = 0.0f;
 #pragma unroll
-    for (int w = 0; w < NT / 32; ++w) t += sred[w];
-    return t;
+    for (int i = 0; i < N; ++i) sum[i] = 0.0;
+    for (int j0 = threadIdx.x; j0 < d; j0 += 32 * NT) {
+        float part[N] = {};
+        const int end = d - j0 > 32 * NT ? j0 + 32 * NT : d;
+        for (int j = j0; j < end; j += NT) term(j, part);
+#pragma unroll
+        for (int i = 0; i < N; ++i) sum[i] += (double)part[i];
+    }
 }
 
+// Maximum over the block, the same value in every thread; sred: NT / 32 floats, reusable at once.
 template <int NT>
 __device__ __forceinline__ float block_max_f(float v, float* sred)
 {
