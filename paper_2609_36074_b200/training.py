@@ -2,6 +2,11 @@
 clipping.  Argument marshalling only, like binding.py; the functions have the C entry points' names and return torch
 tensors.  None of them synchronizes.
 
+They take no part in autograd: what they return has no graph, whatever their inputs require, and the backward pass of a
+model that uses them is written with layer_norm_backward and the dlogits of label_cross_entropy.  A tensor that the caller
+gives to be written to (out, dlogits, the gradients that are clipped) counts as changed in place, so that autograd refuses a
+backward pass for which it had saved it.
+
 `stream`: the torch stream to work on; None is the current one.  With a stream of its own, a call allocates there and
 tells the allocator that the inputs are in use there; ordering it after the work that wrote the inputs (and the outputs'
 readers after it) stays with the caller, as for any torch operation."""
@@ -26,14 +31,16 @@ class Tensor(C.Structure):
 _fn = None          # the entry points, by name
 _types = None       # torch dtype -> GEM_NLR_F32, ...
 _torch = None
+_written = None     # tells autograd that tensors were written to (0.3 us, 3 us for a list of 61)
 _device = None      # the current device's number, and the current stream of a device as a pointer: torch's own
 _stream = None      # accessors without the objects that torch.cuda.current_stream() builds (2 us of a 15 us call)
 
 
 def _load():
     """The entry points with their argument types, and torch, on the first call."""
-    global _fn, _types, _torch, _device, _stream
+    global _fn, _types, _torch, _written, _device, _stream
     import torch
+    from torch.autograd.graph import increment_version
     L = lib()
     vp, i32, i64, f32, size = C.c_void_p, C.c_int32, C.c_int64, C.c_float, C.c_size_t
     sig = {
@@ -52,6 +59,7 @@ def _load():
         f.restype = size if name.endswith("_bytes") else C.c_int
         fn[name] = f
     _device, _stream = torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream
+    _written = increment_version
     _torch, _types, _fn = torch, {torch.float32: F32, torch.float16: F16, torch.bfloat16: BF16}, fn
     return fn
 
@@ -164,6 +172,8 @@ def layer_norm(x, weight=None, bias=None, eps=1e-5, out=None, stream=None):
     rstd = torch.empty_like(mean)
     _check(fn["layer_norm"](x.data_ptr(), t, ld, wp, bp, wt, n, d, eps, y.data_ptr(), ldy, mean.data_ptr(), rstd.data_ptr(),
                             _stream(at)), "layer_norm")
+    if out is not None:
+        _written(out)
     return y, mean, rstd
 
 
@@ -227,14 +237,14 @@ def label_cross_entropy(logits, labels, mean=True, dlogits=None, need_grad=True,
     lead = logits.shape[:-1]
     if labels.dtype != torch.int32 or labels.shape != lead or not labels.is_contiguous() or labels.get_device() != at:
         raise ValueError(f"labels have to be {tuple(lead)} contiguous int32 on GPU {at}")
-    ldd, dp = k, None
+    ldd, dp, given = k, None, None
     if not need_grad:
         dlogits = None
     else:
         if dlogits is None:
             dlogits = torch.empty_like(logits) if logits.is_contiguous() else logits.new_empty(logits.shape)
         else:
-            ldd = _given(dlogits, logits, "dlogits")
+            given, ldd = dlogits, _given(dlogits, logits, "dlogits")
         dp = dlogits.data_ptr()
     row = _floats(logits, n)
     loss = torch.empty_strided((), (), dtype=torch.float32, device=logits.device)
@@ -242,6 +252,8 @@ def label_cross_entropy(logits, labels, mean=True, dlogits=None, need_grad=True,
     scratch = labels.new_empty(size, dtype=torch.uint8) if size else labels          # (none is needed then)
     _check(fn["label_cross_entropy"](logits.data_ptr(), t, ld, labels.data_ptr(), n, k, 1 if mean else 0, loss.data_ptr(), row.data_ptr(),
                                      dp, ldd, scratch.data_ptr(), size, _stream(at)), "label_cross_entropy")
+    if given is not None:
+        _written(given)
     return loss, row, dlogits
 
 
@@ -290,6 +302,8 @@ def _norm_and_clip(grads, max_norm, out, eps, stream):
     size = _scratch("clip_grad_norm_scratch_bytes", count)
     scratch = norm.new_empty(size // 4)
     _check(fn["clip_grad_norm"](table.buffer_info()[0], count, max_norm, eps, norm.data_ptr(), scratch.data_ptr(), size, _stream(at)), "clip_grad_norm")
+    if out is not None:
+        _written(out)
     return norm
 
 
