@@ -186,10 +186,11 @@ __device__ __forceinline__ void all_scaled(const Table<CAP>& tb, uint32_t q0, ui
 template <int CAP>
 __device__ __forceinline__ uint32_t first_chunk(const Table<CAP>& tb, unsigned block) { return (uint32_t)((uint64_t)tb.chunks * block / gridDim.x); }
 
+// c.  A NaN stays one; an infinite norm gives 0 whatever the limit (infinity by infinity would be a NaN of no tensor's).
 __device__ __forceinline__ float clip_factor(double norm, float max_norm, float eps)
 {
-    const double ratio = (double)max_norm / (norm + (double)eps);
-    return ratio >= 1.0 || norm == 0.0 ? 1.0f : (float)ratio;            // a NaN stays one
+    const double below = norm + (double)eps, ratio = (double)max_norm / below;
+    return norm == 0.0 || ratio >= 1.0 ? 1.0f : isinf(below) ? 0.0f : (float)ratio;
 }
 
 template <int CAP>
