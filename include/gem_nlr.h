@@ -384,7 +384,8 @@ int gem_nlr_label_cross_entropy(const void *logits_dev, int32_t type, int64_t ld
  * numel elements of out_type, which is `type` or FP32.  out may be in itself (same type); then nothing is written
  * when c == 1.  out NULL in every record: the norm alone (max_norm is not looked at).  norm: one float.  The squares
  * are summed in FP64 over the whole range of the types (no overflow or underflow inside); the stored norm is +inf
- * when it passes FP32.  A NaN anywhere makes norm and every output NaN; an infinite norm gives c = 0, a norm of 0 c = 1.
+ * when it passes FP32.  A NaN anywhere makes norm and every output NaN; an infinite norm gives c = 0, with max_norm = +inf
+ * too; a norm of 0 gives c = 1.
  * count >= 0, max_norm >= 0, eps >= 0; no two records' outputs overlap.                                         */
 typedef struct {
     const void *in_dev;

@@ -6,9 +6,10 @@
 // The variance is taken about the mean (a second look at the row in registers), so an offset far above the spread costs
 // nothing.  Statistics and sums are FP32 within a row and a block, FP64 across blocks; y, dx, dw, db are rounded once.
 //
-// Rows of up to 49152 elements (FP32 gradient: 32768) are streamed through shared memory and read from HBM once
-// (train_rows.cuh); wider ones, and calls without rows, take the plain kernels that come first here, which read a row
-// two to three times, from L2 but for the first.
+// Rows that eight blocks hold are streamed through shared memory and read from HBM once (train_rows.cuh): forward, up to 65536
+// elements of 2 bytes and 49152 of 4, or 49152 of any type read element by element (mode 2); gradient, up to 49152 aligned
+// ones of 2 bytes (mode 0), else 32768.  Rows that begin anywhere (mode 1) lose up to 7 of these.  Wider ones, and calls without
+// rows, take the plain kernels that come first here, which read a row two to three times, from L2 but for the first.
 #include "train_rows.cuh"
 
 namespace gemnlr {
@@ -127,7 +128,7 @@ struct NormShape {
 // (packed FP32 pairs; weights in registers).  More rows in flight than two blocks' registers hold come from the ring (four
 // stages).  What is read once leaves L2 first (262144 x 768: 151 us without, 144 us with the hints).
 // Measured, 262144 x 768 bf16: 144 us, 5.6 TB/s (a device copy of the same bytes: 126 us); 60000 x 1001 bf16, rows that begin
-// anywhere: 56 us, 4.3 TB/s, bound by issue (570 instructions a row and warp, 360 where rows are aligned).
+// anywhere: 50 us, 4.8 TB/s, bound by issue (530 instructions a row and warp, 360 where rows are aligned).
 template <typename T, int MODE, int TPR, int EPL, int C>
 __global__ void __launch_bounds__(kRowBlock, 2)
 k_norm_rows(const T* __restrict__ x, int64_t ldx, const void* __restrict__ w, const void* __restrict__ b, int wtype, int64_t n, int d,
@@ -287,8 +288,8 @@ __host__ __device__ inline int64_t record_stride(int d) { return (2 * (int64_t)d
 // groups' sums and writes one record; k_norm_dw_join adds the records (small calls: the blocks of the one cluster read each
 // other's).  A row's mean and rstd are read a row ahead.  With 24 elements a thread the row is read from the ring a second
 // time instead of being kept: sums and weights fill the registers (262144 x 768 bf16: 246 us when it was kept and spilled).
-// Measured: 262144 x 768 bf16 199 us, 6.1 TB/s, HBM; 1021 x 16384 FP32, clusters of four blocks a row: 40.4 us, of which the
-// rows take 33 and the join of 71 records of 131 KB 7; 60000 x 1001 bf16 90 us, bound by issue.
+// Measured: 262144 x 768 bf16 198 us, 6.1 TB/s, HBM; 1021 x 16384 FP32, clusters of four blocks a row: 41.5 us, of which the
+// rows take 33 and the join of 71 records of 131 KB 8; 60000 x 1001 bf16 85 us, bound by issue.
 template <typename T, int MODE, int TPR, int EPL, int C>
 struct GradShape {
     using S0 = Source<T, MODE, TPR, EPL, C>;

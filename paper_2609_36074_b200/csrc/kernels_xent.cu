@@ -7,7 +7,8 @@
 // exponentials about its own maximum, so that the warps of a wide row have to meet once, with a maximum and a sum each,
 // and not once for the maximum and once for the sum.  The mean's divisor is counted by a small kernel before, whose end the
 // first rows do not wait for; the loss is added up in FP64 by the last block, in block order.  Rows wider than eight blocks
-// hold (65536 elements of 2 bytes, 49152 of 4) take the plain kernel, which reads them three times.
+// hold (65536 elements of 2 bytes, 49152 of 4 or of any type read element by element; rows that begin anywhere lose up to 7 of
+// these) take the plain kernel, which reads them three times.
 #include "train_rows.cuh"
 
 namespace gemnlr {
@@ -189,9 +190,9 @@ __device__ __forceinline__ float row_max(const Row<T, MODE, EPL>& z)
     }
 }
 
-// Measured: 131072 x 1000 bf16 93 us, 5.6 TB/s (issue 60 %, 13 instructions an element); 2053 x 32768 f16, four blocks a row:
-// 64 us, 4.2 TB/s, bound by the chain of a row (maximum, sum, meeting, output) at two blocks an SM: a block begins the
-// next row before it ends one (67 us without); 16 x 100 FP32, one launch: 3.5 us on the device.
+// Measured: 131072 x 1000 bf16 92 us, 5.7 TB/s (issue 60 %, 13 instructions an element); 2053 x 32768 f16, four blocks a row:
+// 64.5 us, 4.2 TB/s, bound by the chain of a row (maximum, sum, meeting, output) at two blocks an SM: a block begins the
+// next row before it ends one (67 us without); 16 x 100 FP32, one launch: 3.6 us on the device.
 template <typename T, int MODE, int TPR, int EPL, int C>
 __global__ void __launch_bounds__(kRowBlock, 2)
 k_xent_rows(const T* z, int64_t ld, const int32_t* __restrict__ labels, int64_t n, int k, int mean, Scratch* sc, float* __restrict__ loss,

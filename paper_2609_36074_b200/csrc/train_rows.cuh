@@ -12,7 +12,7 @@
 //      neighbouring rows (or of the padding) too, which are replaced after loading and left alone in storing
 //   2  element by element, where the matrices of one call lie differently to 16 bytes
 // Measured, bf16, 60000 rows of 1000 in mode 0, of 1001 in mode 1, of 1000 out of 1013 (with dense outputs) in mode 2: layer norm
-// forward 46, 56, 78 us, its gradient 69, 90, 92 us, cross entropy 48, 54, 89 us.
+// forward 45, 50, 77 us, its gradient 68, 85, 90 us, cross entropy 48, 53, 88 us.
 //
 // In modes 0 and 1 rows come through a ring of stages in shared memory, S rows ahead: registers alone hold too few bytes in
 // flight for HBM.  From a warp a row on (BULK), one thread sends for the whole row by one bulk copy, which arrives at a
@@ -700,6 +700,16 @@ template <int V> struct Const { static constexpr int value = V; };
 // Narrower rows: E0, two vectors to a thread, so that neighbouring threads read whole sectors of 32 bytes.
 // Rows wider than 256 E2 go to clusters of blocks, so that every SM still has two blocks, one of which loads while the
 // other adds.
+// The triples of the callers.  E0 is two vectors of 16 bytes: 16 elements of 2 bytes, 8 of 4 (8 too where single elements are
+// read).  E1, E2 are 24 and 32 (2-byte vectors) or 16 and 24 in the forward norm and the loss: with 16 at most, norm 262144 x
+// 768 bf16 187 us instead of 144, 60000 x 1001 65 instead of 51, 2048 x 24000 FP32 83 instead of 69, loss 131072 x 1000 135 instead
+// of 92, 2053 x 32768 f16 103 instead of 64 (the other way: norm 16384 x 4096 bf16 46 instead of 49, loss 65536 x 768 FP32 73
+// instead of 76).  The gradient keeps two sums a column in registers and takes 16 (FP32: 12 and 16), and 24 only for 2-byte
+// elements in mode 0, where it reads the row a second time instead of keeping it (262144 x 768 bf16 198 us, 236 with 16).
+// In mode 1 the masks of that second time spill (up to 216 bytes a thread): 24 there measured 60000 x 701 88 us against 84,
+// 16384 x 2501 94 against 84, though 8000 x 5001 81 against 93.
+// Not all shapes stay within the registers: -Xptxas -v reports spills for 46 of 502 row kernels, 4 to 120 bytes a thread, most in
+// the forward norm of clusters in modes 1 and 2 (96 to 120, where each thread holds 24 or 32 elements beside two weight vectors).
 template <int E0, int E1, int E2, typename F>
 bool by_width(int64_t width, F f)
 {
