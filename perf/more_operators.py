@@ -210,7 +210,8 @@ def plain_route(s):
     key = z if s["bias"] is None else torch.where(none, z, score + s["bias"].double())
     if groups > 1:
         by = (key if c["best"] == 1 else torch.where(none, z, score) if s["bias"] is None else key).view(n, groups, e // groups)
-        best = by.sort(dim=2, descending=True).values[:, :, :c["best"]].sum(2)
+        best = by.sort(dim=2, descending=True).values[:, :, :c["best"]]
+        best = best[:, :, 0] + torch.where(best[:, :, 1:] == -math.inf, 0.0, best[:, :, 1:]).sum(2)
         at = best.sort(dim=1, descending=True, stable=True).indices[:, :c["kept"]]
         stays = torch.zeros(n, groups, dtype=torch.bool, device=z.device).scatter_(1, at, True)
         key = torch.where(stays[:, :, None], key.view(n, groups, -1), -math.inf).view(n, e)
