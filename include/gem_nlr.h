@@ -398,6 +398,101 @@ size_t gem_nlr_clip_grad_norm_scratch_bytes(int32_t count);
 int gem_nlr_clip_grad_norm(const gem_nlr_tensor *tensors_host, int32_t count, float max_norm, float eps,
                            float *norm_dev, void *scratch_dev, size_t scratch_bytes, void *cuda_stream);
 
+/* ---- Layers of experts in such an encoder -----------------------------------------------------------------
+ * A router sends each row to k of several experts, each expert multiplies its rows by its own weights, and the
+ * results come back to the rows as weighted sums; between the products stand activations, whose inputs are kept
+ * in 8 bits for the backward pass.  What the section above says of matrices, pointers, sums, repeated calls,
+ * streams, capture, scratch and waits holds here too.
+ *
+ * The experts' rows lie side by side: with `places` = n k, place p in [offset[e], offset[e + 1]) is a row of
+ * expert e, row[p] is the row of the router's input that it came from, place[t k + j] the place of row t's j-th
+ * expert.  Rows without an expert leave the last places unused.  offset[0] is 0; offsets outside [0, places]
+ * or falling ones are taken as if cut to what is possible; entries of row and place outside their ranges as if they were -1.      */
+#define GEM_NLR_SOFTMAX 0
+#define GEM_NLR_SIGMOID 1
+#define GEM_NLR_MAX_EXPERTS 512
+
+/* s_ij = softmax(z_i)_j or 1 / (1 + exp(-z_ij));  c_ij = s_ij + b_j (the bias balances the load; it takes part in
+ * the choice alone).  Row i goes to the k experts of largest c_ij, in falling order, the lowest index first among
+ * equals; without a bias the choice is by z_ij.  With groups > 1 the experts are that many groups of neighbours,
+ * and only those of the kept_groups best groups can be chosen: a group is as good as the sum of its group_best (1
+ * or 2) largest c (without a bias s; with group_best 1 then z), again the lowest index first.  Which of two scores is the larger is
+ * decided as in 64 bits.  weight = scale s / sum of the chosen s (renormalize == 1) or scale s (0).
+ * logits: n x experts of `type`; bias: experts floats or NULL; expert, weight, place: n x k; offset: experts + 1;
+ * row: n k.  1 <= k <= 32, k <= kept_groups experts / groups, experts <= GEM_NLR_MAX_EXPERTS, groups <= 32 and a
+ * divisor of experts, n k < 2^31, scale finite.
+ * A logit (or bias) of -inf leaves its expert out; where none is left, expert and place are -1 and the weight 0.  A row with a
+ * NaN (with softmax: or +inf) goes to no expert and its weights are NaN.  row is -1 behind offset[experts].    */
+size_t gem_nlr_route_scratch_bytes(int64_t n, int32_t experts);
+int gem_nlr_route(const void *logits_dev, int32_t type, int64_t ld, const float *bias_dev, int64_t n, int32_t experts,
+                  int32_t k, int32_t score, int32_t groups, int32_t kept_groups, int32_t group_best, int32_t renormalize,
+                  float scale, int32_t *expert_dev, float *weight_dev, int32_t *offset_dev, int32_t *row_dev,
+                  int32_t *place_dev, void *scratch_dev, size_t scratch_bytes, void *cuda_stream);
+
+/* The gradient of the weights in the logits, for the choice that was made: with v_j = dweight_ij scale,
+ *   softmax, renormalized: p_j (v_j - sum_l p_l v_l), p the softmax over the chosen logits; others 0
+ *   sigmoid, renormalized: the same times 1 - s_j with p_j = s_j / sum_l s_l;             others 0
+ *   softmax alone: s_j ([chosen] v_j - sum over the chosen of s_l v_l);  sigmoid alone: v_j s_j (1 - s_j), others 0.
+ * dweight, expert: n x k; dlogits: n x experts of `type`.  Slots whose expert is -1 take no part; their dweight is not looked
+ * at.  A row without an expert has gradient 0; a NaN (softmax: or +inf) among the logits that a row's gradient needs makes it NaN.  */
+int gem_nlr_route_backward(const float *dweight_dev, const void *logits_dev, int32_t type, int64_t ld,
+                           const int32_t *expert_dev, int64_t n, int32_t experts, int32_t k, int32_t score,
+                           int32_t renormalize, float scale, void *dlogits_dev, int64_t ld_d, void *cuda_stream);
+
+/* y_p = x_row(p) W_e for every place p of expert e;  rows of y behind offset[experts] are set to 0.
+ * x: x_rows x d_in; row: places entries, NULL when place p's row is x's row p (then x_rows >= places); W_e: d_in x
+ * d_out at w + e stride_w, rows ld_w apart, or with w_turned == 1 its transpose (d_out x d_in); y: places x d_out.
+ * x, w, y: GEM_NLR_F16 or GEM_NLR_BF16; products are summed in FP32 and rounded once.  A place whose row entry is -1 has
+ * a row of zeros for x.  16-byte aligned rows (and stride_w) take the fast loads.                              */
+int gem_nlr_expert_product(const void *x_dev, int32_t type, int64_t ld_x, int64_t x_rows, const void *w_dev,
+                           int64_t ld_w, int64_t stride_w, int32_t w_turned, const int32_t *offset_dev,
+                           const int32_t *row_dev, int64_t places, int32_t experts, int32_t d_in, int32_t d_out,
+                           void *y_dev, int64_t ld_y, void *cuda_stream);
+
+/* Its gradients: dx_p = dy_p W_e^T for every place (places x d_in; where row is given, the gradient of a row of x is the
+ * sum over its places: gem_nlr_combine without weights), dW_e = sum over e's places of x_row(p)^T dy_p, in w's
+ * layout with rows ld_dw and experts stride_dw apart (0 for an expert without rows).  dx and dw may each be NULL, not both.  */
+int gem_nlr_expert_product_backward(const void *dy_dev, int64_t ld_dy, const void *x_dev, int32_t type, int64_t ld_x,
+                                    int64_t x_rows, const void *w_dev, int64_t ld_w, int64_t stride_w, int32_t w_turned,
+                                    const int32_t *offset_dev, const int32_t *row_dev, int64_t places, int32_t experts,
+                                    int32_t d_in, int32_t d_out, void *dx_dev, int64_t ld_dx, void *dw_dev, int64_t ld_dw,
+                                    int64_t stride_dw, void *cuda_stream);
+
+/* out_t = sum_j weight_tj y_place(t,j) over the slots with a place (weight NULL: 1).  y: places x d, out: n x d, of `type`;
+ * place, weight: n x k, 1 <= k <= 32.  A slot without a place adds nothing, unless its weight is NaN.           */
+int gem_nlr_combine(const void *y_dev, int32_t type, int64_t ld_y, int64_t places, const int32_t *place_dev,
+                    const float *weight_dev, int64_t n, int32_t k, int32_t d, void *out_dev, int64_t ld_out,
+                    void *cuda_stream);
+
+/* Its gradients: dy_place(t,j) = weight_tj dout_t and dweight_tj = sum_c dout_tc y_place(t,j)c (0 without a place).  Rows of dy
+ * behind offset[experts] are set to 0.  No place is named twice.  dy and dweight may each be NULL, not both.   */
+int gem_nlr_combine_backward(const void *dout_dev, int64_t ld_dout, const void *y_dev, int32_t type, int64_t ld_y,
+                             int64_t places, const int32_t *place_dev, const float *weight_dev, const int32_t *offset_dev,
+                             int32_t experts, int64_t n, int32_t k, int32_t d, void *dy_dev, int64_t ld_dy,
+                             float *dweight_dev, void *cuda_stream);
+
+/* Activations: y = f(z), or for gated units y = f(g) u with z = [g u] (n x 2d).  f: z / (1 + exp(-z)) (GEM_NLR_SILU), z
+ * Phi(z) with the normal distribution Phi (GEM_NLR_GELU), tanh (GEM_NLR_TANH), z (GEM_NLR_IDENTITY).
+ * The 8-bit checkpoint of z: each 32 neighbouring columns (counted from 0 in each half of gated units; fewer at the end)
+ * share 2^e, e the smallest number >= -127 with their largest magnitude below 127.5 2^e, and are held as q = z 2^-e rounded to the nearest whole
+ * number, ties to even (e at most 121, GEM_NLR_F16: 9, so that 127 2^e is within the type; magnitudes beyond become that).
+ * q: n rows of gem_nlr_checkpoint_blocks(d, gated) blocks of 32 signed bytes (0 behind the last
+ * column), scale: n rows of as many bytes, e + 127; 255 where the columns hold an infinity or a NaN: they all stand for NaN.
+ * q 16-byte aligned.  y, or q and scale, may be NULL, not both.                                                */
+#define GEM_NLR_IDENTITY 0
+#define GEM_NLR_SILU 1
+#define GEM_NLR_GELU 2
+#define GEM_NLR_TANH 3
+int64_t gem_nlr_checkpoint_blocks(int32_t d, int32_t gated);
+int gem_nlr_activation(const void *z_dev, int32_t type, int64_t ld_z, int64_t n, int32_t d, int32_t kind, int32_t gated,
+                       void *y_dev, int64_t ld_y, int8_t *q_dev, uint8_t *scale_dev, void *cuda_stream);
+
+/* dz = dy f'(z) (gated: [dy u f'(g), dy f(g)]) and, where y is not NULL, y again, with z as the checkpoint holds it (z_dev
+ * NULL) or as it was (q_dev and scale_dev NULL).  With dy and dz NULL y alone; the kind GEM_NLR_IDENTITY then restores z.  */
+int gem_nlr_activation_backward(const void *dy_dev, int32_t type, int64_t ld_dy, const void *z_dev, int64_t ld_z,
+                                const int8_t *q_dev, const uint8_t *scale_dev, int64_t n, int32_t d, int32_t kind,
+                                int32_t gated, void *dz_dev, int64_t ld_dz, void *y_dev, int64_t ld_y, void *cuda_stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -25,3 +25,17 @@ from .training import (  # noqa: F401
     clip_grad_norm,
     grad_norm,
 )
+from .experts import (  # noqa: F401
+    Checkpoint,
+    Routing,
+    activation,
+    activation_backward,
+    checkpoint,
+    combine,
+    combine_backward,
+    expert_product,
+    expert_product_backward,
+    restore,
+    route,
+    route_backward,
+)

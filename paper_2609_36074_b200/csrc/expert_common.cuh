@@ -1,0 +1,44 @@
+// Shared by the expert layer's memory-bound kernels: eight neighbouring elements of a row at a time.
+#pragma once
+#include "train_common.cuh"
+
+namespace gemnlr {
+
+// Eight elements from p, as FP32; `many` of them are there (the others read as 0).  WIDE: all eight are, on 16 bytes.
+template <bool WIDE, typename T>
+__device__ __forceinline__ void load8(const T* __restrict__ p, int many, float (&v)[8])
+{
+    if constexpr (WIDE) {
+        uint4 w[sizeof(T) / 2];
+#pragma unroll
+        for (int i = 0; i < (int)sizeof(T) / 2; ++i) w[i] = __ldg(reinterpret_cast<const uint4*>(p) + i);
+        const T* t = reinterpret_cast<const T*>(w);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = to_f(t[i]);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = i < many ? to_f(p[i]) : 0.f;
+    }
+}
+
+template <bool WIDE, typename T>
+__device__ __forceinline__ void store8(T* __restrict__ p, int many, const float (&v)[8])
+{
+    if constexpr (WIDE) {
+        uint4 w[sizeof(T) / 2];
+        T* t = reinterpret_cast<T*>(w);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) t[i] = from_f<T>(v[i]);
+#pragma unroll
+        for (int i = 0; i < (int)sizeof(T) / 2; ++i) reinterpret_cast<uint4*>(p)[i] = w[i];
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (i < many) p[i] = from_f<T>(v[i]);
+    }
+}
+
+// Whether every row of a matrix begins on 16 bytes (absent ones count as such).
+inline bool wide_rows(const void* p, int64_t ld, int bytes) { return !p || (aligned_to(p, 16) && ld % (16 / bytes) == 0); }
+
+}  // namespace gemnlr

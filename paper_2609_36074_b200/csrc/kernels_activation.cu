@@ -1,0 +1,275 @@
+// Activations whose inputs are kept in 8 bits for the backward pass.
+//
+//   forward    y = f(z), or f(g) u for gated units, and per 32 columns of z: e the smallest number >= -127 with max |z| < 127.5 2^e,
+//              q = z 2^-e rounded to the nearest whole number
+//   backward   dz = dy f'(z) (gated: dy u f'(g), dy f(g)) and y again, from q 2^e
+//
+// A scale that is a power of two makes q and q 2^e exact FP32 operations, so that the 8 bits do not hang on how a division
+// rounds; it costs up to one of the 8 bits against max / 127.  The error of a column is at most 2^(e-1), a 127th of the
+// largest magnitude among its 32 neighbours.  127.5 = 64 (1 + 127/128): adding 2^16 to the bits of the largest magnitude
+// carries into its exponent exactly when it is at or above 127.5 2^e for the e of its own binade.
+//
+// Bound by HBM: one pass each way, eight columns a thread (four threads share a scale), values in FP32 in between.
+#include "expert_common.cuh"
+
+namespace gemnlr {
+namespace {
+
+constexpr int kThreads = 256;
+
+// e^x: FP32 outputs take the exact function, 16-bit ones the fast one (2 units of FP32 for |x| < 1, 2^-20 relative at |x| = 16:
+// a tenth of a 16-bit step at most).
+template <typename T> __device__ __forceinline__ float exp_of(float x) { return sizeof(T) == 4 ? expf(x) : __expf(x); }
+
+// f(z) and f'(z).
+template <typename T, int KIND>
+__device__ __forceinline__ void act(float z, float& value, float& slope)
+{
+    if constexpr (KIND == GEM_NLR_SILU) {
+        const float t = exp_of<T>(-fabsf(z)), over = z < 0.0f ? t : 1.0f;               // no overflow far below 0
+        const float p = sizeof(T) == 4 ? over / (1.0f + t) : __fdividef(over, 1.0f + t);
+        value = z * p;
+        slope = fmaf(value, 1.0f - p, p);
+    } else if constexpr (KIND == GEM_NLR_GELU) {
+        const float p = 0.5f * erfcf(z * -0.70710678118654752f);
+        value = z * p;
+        slope = fmaf(z * 0.39894228040143268f, exp_of<T>(-0.5f * z * z), p);
+    } else if constexpr (KIND == GEM_NLR_TANH) {
+        value = tanhf(z);
+        slope = fmaf(-value, value, 1.0f);
+    } else {
+        value = z;
+        slope = 1.0f;
+    }
+}
+
+// The 8 bits of this thread's eight values and the scale that the four threads of 32 columns share.
+// (e stops where 127 2^e is the last below T's largest number; magnitudes beyond are held as that.)
+template <typename T>
+__device__ __forceinline__ uint32_t to_8_bits(const float (&v)[8], uint2& q)
+{
+    constexpr int last = (std::is_same_v<T, __half> ? 9 : 121) + 127;
+    uint32_t top = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) top = max(top, __float_as_uint(v[i]) & 0x7fffffffu);
+    top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
+    top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
+    q = make_uint2(0, 0);
+    if (top >= 0x7f800000u) return 255u;
+    const int field = (int)((top + 0x10000u) >> 23) - 6;           // e + 127
+    const uint32_t scale = (uint32_t)min(max(field, 0), last);
+    const float up = __uint_as_float((254u - scale) << 23);        // 2^-e
+    uint32_t w[2] = {0, 0};
+#pragma unroll
+    for (int i = 0; i < 8; ++i) w[i >> 2] |= ((uint32_t)__float2int_rn(fminf(fmaxf(v[i] * up, -127.0f), 127.0f)) & 0xffu) << (8 * (i & 3));
+    q = make_uint2(w[0], w[1]);
+    return scale;
+}
+
+__device__ __forceinline__ void from_8_bits(uint2 q, uint32_t scale, float (&v)[8])
+{
+    // 2^e for e >= -126; -127 is a subnormal
+    const float unit = scale == 255u ? __uint_as_float(0x7fc00000u) : scale ? __uint_as_float(scale << 23) : __uint_as_float(0x00400000u);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = (float)(int8_t)(((i < 4 ? q.x : q.y) >> (8 * (i & 3))) & 0xffu) * unit;
+}
+
+// Threads (x: eight columns each, y: rows) over the columns of one half, then over rows.  The columns go in whole steps of
+// blockDim.x, a multiple of four, so that the four threads of a scale stay together and every lane takes part in the exchange.
+template <typename T, int KIND, bool GATED, bool WIDE>
+__global__ void __launch_bounds__(kThreads)
+k_activation(const T* __restrict__ z, int64_t ldz, int64_t n, int d, T* __restrict__ y, int64_t ldy, int8_t* __restrict__ q,
+             uint8_t* __restrict__ scale, int blocks)
+{
+    const int vecs = blocks * 4;                                    // of one half
+    const int64_t ldq = (int64_t)blocks * 32 * (GATED ? 2 : 1), lds = (int64_t)blocks * (GATED ? 2 : 1);
+    const int64_t steps = (n + blockDim.y - 1) / blockDim.y;
+    for (int64_t s = blockIdx.x; s < steps; s += gridDim.x) {
+        const int64_t row = s * blockDim.y + threadIdx.y;
+        for (int c0 = 0; c0 < vecs; c0 += blockDim.x) {
+            const int c = c0 + threadIdx.x, col = c * 8;
+            const bool on = row < n && col < d;
+            float a[8] = {}, b[8] = {}, o[8];
+            if (on) {
+                load8<WIDE>(z + row * ldz + col, d - col, a);
+                if (GATED) load8<WIDE>(z + row * ldz + d + col, d - col, b);
+            }
+            if (q) {
+                uint2 w;
+                const uint32_t sa = to_8_bits<T>(a, w);
+                const bool in = row < n && c < vecs;
+                if (in) *reinterpret_cast<uint2*>(q + row * ldq + col) = w;
+                if (in && (c & 3) == 0) scale[row * lds + (c >> 2)] = (uint8_t)sa;
+                if (GATED) {
+                    const uint32_t sb = to_8_bits<T>(b, w);
+                    if (in) *reinterpret_cast<uint2*>(q + row * ldq + (int64_t)blocks * 32 + col) = w;
+                    if (in && (c & 3) == 0) scale[row * lds + blocks + (c >> 2)] = (uint8_t)sb;
+                }
+            }
+            if (y && on) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    float slope;
+                    act<T, KIND>(a[i], o[i], slope);
+                    if (GATED) o[i] *= b[i];
+                }
+                store8<WIDE>(y + row * ldy + col, d - col, o);
+            }
+        }
+    }
+}
+
+template <typename T, int KIND, bool GATED, bool WIDE>
+__global__ void __launch_bounds__(kThreads)
+k_activation_backward(const T* __restrict__ dy, int64_t lddy, const T* __restrict__ z, int64_t ldz, const int8_t* __restrict__ q,
+                      const uint8_t* __restrict__ scale, int64_t n, int d, T* __restrict__ dz, int64_t lddz, T* __restrict__ y,
+                      int64_t ldy, int blocks)
+{
+    const int vecs = blocks * 4;
+    const int64_t ldq = (int64_t)blocks * 32 * (GATED ? 2 : 1), lds = (int64_t)blocks * (GATED ? 2 : 1);
+    const int64_t steps = (n + blockDim.y - 1) / blockDim.y;
+    for (int64_t s = blockIdx.x; s < steps; s += gridDim.x) {
+        const int64_t row = s * blockDim.y + threadIdx.y;
+        if (row >= n) continue;
+        for (int c = threadIdx.x; c < vecs; c += blockDim.x) {
+            const int col = c * 8;
+            if (col >= d) break;
+            float a[8], b[8], g[8];
+            if (q) {
+                const uint2 wa = __ldg(reinterpret_cast<const uint2*>(q + row * ldq + col));
+                const uint32_t sa = __ldg(scale + row * lds + (c >> 2));
+                if (GATED) {
+                    const uint2 wb = __ldg(reinterpret_cast<const uint2*>(q + row * ldq + (int64_t)blocks * 32 + col));
+                    const uint32_t sb = __ldg(scale + row * lds + blocks + (c >> 2));
+                    if (dz) load8<WIDE>(dy + row * lddy + col, d - col, g);
+                    from_8_bits(wb, sb, b);
+                } else if (dz) {
+                    load8<WIDE>(dy + row * lddy + col, d - col, g);
+                }
+                from_8_bits(wa, sa, a);
+            } else {
+                load8<WIDE>(z + row * ldz + col, d - col, a);
+                if (GATED) load8<WIDE>(z + row * ldz + d + col, d - col, b);
+                if (dz) load8<WIDE>(dy + row * lddy + col, d - col, g);
+            }
+            float o[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                float value, slope;
+                act<T, KIND>(a[i], value, slope);
+                if (GATED) {
+                    o[i] = value * b[i];
+                    if (dz) {
+                        b[i] *= g[i] * slope;
+                        g[i] *= value;
+                    }
+                } else {
+                    o[i] = value;
+                    if (dz) g[i] *= slope;
+                }
+            }
+            if (dz) {
+                if (GATED) {
+                    store8<WIDE>(dz + row * lddz + col, d - col, b);
+                    store8<WIDE>(dz + row * lddz + d + col, d - col, g);
+                } else {
+                    store8<WIDE>(dz + row * lddz + col, d - col, g);
+                }
+            }
+            if (y) store8<WIDE>(y + row * ldy + col, d - col, o);
+        }
+    }
+}
+
+struct Shape { dim3 grid, block; };
+
+// Blocks of 256 threads: as many along a row as it has vectors, up to 256, the rest rows.
+Shape shape_of(int64_t n, int vecs)
+{
+    int x = 4;
+    while (x < vecs && x < kThreads) x *= 2;
+    const int rows = kThreads / x;
+    const int64_t steps = (n + rows - 1) / rows, most = (int64_t)kTrainSMs * 64;
+    return {dim3((unsigned)(steps < most ? steps : most)), dim3(x, rows)};
+}
+
+template <typename F> int by_kind(int32_t kind, F f)
+{
+    switch (kind) {
+        case GEM_NLR_SILU: return f(std::integral_constant<int, GEM_NLR_SILU>{});
+        case GEM_NLR_GELU: return f(std::integral_constant<int, GEM_NLR_GELU>{});
+        case GEM_NLR_TANH: return f(std::integral_constant<int, GEM_NLR_TANH>{});
+        default: return f(std::integral_constant<int, GEM_NLR_IDENTITY>{});
+    }
+}
+
+template <typename F> int by_flags(bool gated, bool wide, F f)
+{
+    if (gated) return wide ? f(std::true_type{}, std::true_type{}) : f(std::true_type{}, std::false_type{});
+    return wide ? f(std::false_type{}, std::true_type{}) : f(std::false_type{}, std::false_type{});
+}
+
+bool fine(const void* p, int tb, int64_t ld, int64_t columns) { return p && aligned_to(p, tb) && ld >= columns; }
+
+}  // namespace
+}  // namespace gemnlr
+
+using namespace gemnlr;
+
+extern "C" int64_t gem_nlr_checkpoint_blocks(int32_t d, int32_t gated)
+{
+    return d < 1 || d > kMaxColumns || (gated != 0 && gated != 1) ? 0 : (int64_t)((d + 31) / 32) * (gated ? 2 : 1);
+}
+
+extern "C" int gem_nlr_activation(const void* z_dev, int32_t type, int64_t ld_z, int64_t n, int32_t d, int32_t kind, int32_t gated,
+                                  void* y_dev, int64_t ld_y, int8_t* q_dev, uint8_t* scale_dev, void* cuda_stream)
+{
+    const int tb = type_bytes(type);
+    if (!tb || n < 0 || d < 1 || kind < GEM_NLR_IDENTITY || kind > GEM_NLR_TANH || (gated != 0 && gated != 1) || d > kMaxColumns / (1 + gated) || ld_z < 0)
+        return GEM_NLR_E_INVALID;
+    if (n == 0) return GEM_NLR_OK;
+    if (!fine(z_dev, tb, ld_z, 0) || (y_dev && !fine(y_dev, tb, ld_y, d)) || (!y_dev && !q_dev) || !q_dev != !scale_dev || !aligned_to(q_dev, 16) ||
+        y_dev == z_dev)
+        return GEM_NLR_E_INVALID;
+    const int blocks = (d + 31) / 32;
+    const bool wide = d % 8 == 0 && wide_rows(z_dev, ld_z, tb) && wide_rows(y_dev, ld_y, tb);
+    const Shape sh = shape_of(n, blocks * 4);
+    return by_type(type, [&](auto t) {
+        using T = decltype(t);
+        return by_kind(kind, [&](auto f) {
+            return by_flags(gated, wide, [&](auto g, auto w) {
+                k_activation<T, f.value, g.value, w.value><<<sh.grid, sh.block, 0, (cudaStream_t)cuda_stream>>>(
+                    (const T*)z_dev, ld_z, n, (int)d, (T*)y_dev, ld_y, q_dev, scale_dev, blocks);
+                return launched();
+            });
+        });
+    });
+}
+
+extern "C" int gem_nlr_activation_backward(const void* dy_dev, int32_t type, int64_t ld_dy, const void* z_dev, int64_t ld_z,
+                                           const int8_t* q_dev, const uint8_t* scale_dev, int64_t n, int32_t d, int32_t kind,
+                                           int32_t gated, void* dz_dev, int64_t ld_dz, void* y_dev, int64_t ld_y, void* cuda_stream)
+{
+    const int tb = type_bytes(type);
+    if (!tb || n < 0 || d < 1 || kind < GEM_NLR_IDENTITY || kind > GEM_NLR_TANH || (gated != 0 && gated != 1) || d > kMaxColumns / (1 + gated))
+        return GEM_NLR_E_INVALID;
+    if (n == 0) return GEM_NLR_OK;
+    const int64_t columns = (int64_t)d * (1 + gated);
+    if (!q_dev != !scale_dev || !z_dev == !q_dev || !aligned_to(q_dev, 16) || (z_dev && !fine(z_dev, tb, ld_z, 0)) || !dy_dev != !dz_dev ||
+        (!dz_dev && !y_dev) || (dy_dev && (!fine(dy_dev, tb, ld_dy, 0) || !fine(dz_dev, tb, ld_dz, columns))) || (y_dev && !fine(y_dev, tb, ld_y, d)) ||
+        (dz_dev && (dz_dev == y_dev || dz_dev == z_dev || dz_dev == dy_dev)) || (y_dev && (y_dev == z_dev || y_dev == dy_dev)))
+        return GEM_NLR_E_INVALID;
+    const int blocks = (d + 31) / 32;
+    const bool wide = d % 8 == 0 && wide_rows(z_dev, ld_z, tb) && wide_rows(dy_dev, ld_dy, tb) && wide_rows(dz_dev, ld_dz, tb) && wide_rows(y_dev, ld_y, tb);
+    const Shape sh = shape_of(n, blocks * 4);
+    return by_type(type, [&](auto t) {
+        using T = decltype(t);
+        return by_kind(kind, [&](auto f) {
+            return by_flags(gated, wide, [&](auto g, auto w) {
+                k_activation_backward<T, f.value, g.value, w.value><<<sh.grid, sh.block, 0, (cudaStream_t)cuda_stream>>>(
+                    (const T*)dy_dev, ld_dy, (const T*)z_dev, ld_z, q_dev, scale_dev, n, (int)d, (T*)dz_dev, ld_dz, (T*)y_dev, ld_y, blocks);
+                return launched();
+            });
+        });
+    });
+}

@@ -1,0 +1,197 @@
+// The experts' rows back to the rows they came from, and the gradient of that.
+//
+//   forward    out_t = sum_j w_tj y_place(t,j)
+//   backward   dy_place(t,j) = w_tj dout_t,  dw_tj = <dout_t, y_place(t,j)>
+//
+// Bound by HBM: y is read once, in rows; a row of dout is read once for all its slots.  Sums in FP32, in a fixed order.
+#include "expert_common.cuh"
+
+namespace gemnlr {
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kSlots = 8;                 // slots whose loads are in flight together
+
+// Eight columns a thread: x along a row, y over rows.
+template <typename T, bool WIDE>
+__global__ void __launch_bounds__(kThreads)
+k_combine(const T* __restrict__ y, int64_t ldy, int64_t places, const int32_t* __restrict__ place, const float* __restrict__ weight,
+          int64_t n, int k, int d, T* __restrict__ out, int64_t ldo)
+{
+    const int vecs = (d + 7) / 8;
+    const int64_t steps = (n + blockDim.y - 1) / blockDim.y;
+    for (int64_t s = blockIdx.x; s < steps; s += gridDim.x) {
+        const int64_t t = s * blockDim.y + threadIdx.y;
+        if (t >= n) continue;
+        for (int c = threadIdx.x; c < vecs; c += blockDim.x) {
+            const int col = c * 8;
+            float sum[8] = {};
+            for (int j0 = 0; j0 < k; j0 += kSlots) {
+                int p[kSlots];
+                float w[kSlots];
+#pragma unroll
+                for (int j = 0; j < kSlots; ++j) {
+                    p[j] = j0 + j < k ? __ldg(place + t * k + j0 + j) : -1;
+                    w[j] = j0 + j < k ? weight ? __ldg(weight + t * k + j0 + j) : 1.0f : 0.0f;
+                    if (p[j] >= places) p[j] = -1;
+                }
+#pragma unroll
+                for (int j = 0; j < kSlots; ++j) {
+                    if (p[j] >= 0) {
+                        float v[8];
+                        load8<WIDE>(y + p[j] * ldy + col, d - col, v);
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) sum[i] = fmaf(w[j], v[i], sum[i]);
+                    } else if (w[j] != w[j]) {
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) sum[i] = w[j];
+                    }
+                }
+            }
+            store8<WIDE>(out + t * ldo + col, d - col, sum);
+        }
+    }
+}
+
+// TPR threads share a row t; NT threads a block.
+template <typename T, bool WIDE, int TPR>
+__global__ void __launch_bounds__(kThreads)
+k_combine_backward(const T* __restrict__ dout, int64_t ldo, const T* __restrict__ y, int64_t ldy, int64_t places,
+                   const int32_t* __restrict__ place, const float* __restrict__ weight, const int32_t* __restrict__ offset, int experts,
+                   int64_t n, int k, int d, T* __restrict__ dy, int64_t lddy, float* __restrict__ dweight)
+{
+    constexpr int ROWS = kThreads / TPR;
+    __shared__ float sred[kThreads / 32][kSlots];
+    const int vecs = (d + 7) / 8;
+    const int me = threadIdx.x % TPR, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int64_t steps = (n + ROWS - 1) / ROWS;
+    for (int64_t s = blockIdx.x; s < steps; s += gridDim.x) {
+        const int64_t t = s * ROWS + threadIdx.x / TPR;
+        for (int j0 = 0; j0 < k; j0 += kSlots) {
+            int p[kSlots];
+            float w[kSlots], dot[kSlots];
+#pragma unroll
+            for (int j = 0; j < kSlots; ++j) {
+                const bool in = t < n && j0 + j < k;
+                p[j] = in ? __ldg(place + t * k + j0 + j) : -1;
+                w[j] = in ? weight ? __ldg(weight + t * k + j0 + j) : 1.0f : 0.0f;
+                if (p[j] >= places) p[j] = -1;
+                dot[j] = 0.0f;
+            }
+            for (int c = me; t < n && c < vecs; c += TPR) {
+                const int col = c * 8;
+                float g[8];
+                load8<WIDE>(dout + t * ldo + col, d - col, g);
+#pragma unroll
+                for (int j = 0; j < kSlots; ++j) {
+                    if (p[j] < 0) continue;
+                    if (dweight) {
+                        float v[8];
+                        load8<WIDE>(y + p[j] * ldy + col, d - col, v);
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) dot[j] = fmaf(g[i], v[i], dot[j]);
+                    }
+                    if (dy) {
+                        float v[8];
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) v[i] = w[j] * g[i];
+                        store8<WIDE>(dy + p[j] * lddy + col, d - col, v);
+                    }
+                }
+            }
+            if (dweight) {
+#pragma unroll
+                for (int j = 0; j < kSlots; ++j) dot[j] = warp_sum(dot[j]);
+                if constexpr (TPR > 32) {
+                    __syncthreads();
+                    if (lane == 0)
+                        for (int j = 0; j < kSlots; ++j) sred[warp][j] = dot[j];
+                    __syncthreads();
+                    if (t < n && me < kSlots && j0 + me < k) {
+                        float sum = 0.0f;
+                        for (int x = 0; x < TPR / 32; ++x) sum += sred[warp / (TPR / 32) * (TPR / 32) + x][me];
+                        dweight[t * k + j0 + me] = sum;
+                    }
+                } else if (t < n && lane == 0) {
+#pragma unroll
+                    for (int j = 0; j < kSlots; ++j)
+                        if (j0 + j < k) dweight[t * k + j0 + j] = dot[j];
+                }
+            }
+        }
+    }
+    // places without an expert
+    if (dy) {
+        int64_t used = __ldg(offset + experts);
+        used = used < 0 ? 0 : used;
+        const float zero[8] = {};
+        for (int64_t p = used + blockIdx.x; p < places; p += gridDim.x)
+            for (int c = threadIdx.x; c < vecs; c += kThreads) store8<WIDE>(dy + p * lddy + c * 8, d - c * 8, zero);
+    }
+}
+
+template <typename F> int by_wide(bool wide, F f) { return wide ? f(std::true_type{}) : f(std::false_type{}); }
+
+bool rows_fine(const void* p, int tb, int64_t ld, int64_t columns) { return p && aligned_to(p, tb) && ld >= columns; }
+
+}  // namespace
+}  // namespace gemnlr
+
+using namespace gemnlr;
+
+extern "C" int gem_nlr_combine(const void* y_dev, int32_t type, int64_t ld_y, int64_t places, const int32_t* place_dev,
+                               const float* weight_dev, int64_t n, int32_t k, int32_t d, void* out_dev, int64_t ld_out, void* cuda_stream)
+{
+    const int tb = type_bytes(type);
+    if (!tb || n < 0 || k < 1 || k > 32 || d < 1 || d > kMaxColumns || places < 0 || places > INT32_MAX || ld_y < 0) return GEM_NLR_E_INVALID;
+    if (n == 0) return GEM_NLR_OK;
+    if ((places > 0 && !rows_fine(y_dev, tb, ld_y, 0)) || !place_dev || !aligned_to(place_dev, 4) || !aligned_to(weight_dev, 4) ||
+        !rows_fine(out_dev, tb, ld_out, d) || out_dev == y_dev)
+        return GEM_NLR_E_INVALID;
+    const int vecs = (d + 7) / 8;
+    int x = 1;
+    while (x < vecs && x < kThreads) x *= 2;
+    const int64_t steps = (n + kThreads / x - 1) / (kThreads / x), most = (int64_t)kTrainSMs * 64;
+    const dim3 grid((unsigned)(steps < most ? steps : most)), block(x, kThreads / x);
+    return by_type(type, [&](auto t) {
+        using T = decltype(t);
+        return by_wide(d % 8 == 0 && wide_rows(y_dev, ld_y, tb) && wide_rows(out_dev, ld_out, tb), [&](auto w) {
+            k_combine<T, w.value><<<grid, block, 0, (cudaStream_t)cuda_stream>>>((const T*)y_dev, ld_y, places, place_dev, weight_dev, n, (int)k, (int)d, (T*)out_dev, ld_out);
+            return launched();
+        });
+    });
+}
+
+extern "C" int gem_nlr_combine_backward(const void* dout_dev, int64_t ld_dout, const void* y_dev, int32_t type, int64_t ld_y, int64_t places,
+                                        const int32_t* place_dev, const float* weight_dev, const int32_t* offset_dev, int32_t experts, int64_t n,
+                                        int32_t k, int32_t d, void* dy_dev, int64_t ld_dy, float* dweight_dev, void* cuda_stream)
+{
+    const int tb = type_bytes(type);
+    if (!tb || n < 0 || k < 1 || k > 32 || d < 1 || d > kMaxColumns || places < 0 || places > INT32_MAX || experts < 1 || ld_dout < 0 || ld_y < 0 ||
+        (!dy_dev && !dweight_dev))
+        return GEM_NLR_E_INVALID;
+    if (n > 0 && (!rows_fine(dout_dev, tb, ld_dout, 0) || !place_dev || !aligned_to(place_dev, 4) || !aligned_to(weight_dev, 4) ||
+                  (dweight_dev && (!aligned_to(dweight_dev, 4) || (places > 0 && !rows_fine(y_dev, tb, ld_y, 0))))))
+        return GEM_NLR_E_INVALID;
+    if (dy_dev && places > 0 && (!rows_fine(dy_dev, tb, ld_dy, d) || !offset_dev || !aligned_to(offset_dev, 4) || dy_dev == dout_dev || dy_dev == y_dev))
+        return GEM_NLR_E_INVALID;
+    if (n == 0 && (!dy_dev || places == 0)) return GEM_NLR_OK;
+    void* dy = places > 0 ? dy_dev : nullptr;
+    if (!dy && !dweight_dev) return GEM_NLR_OK;
+    // A warp a row; where that leaves SMs without work, a block.
+    const bool few = n < (int64_t)kTrainSMs * 8 && d > 256;
+    const int64_t steps = few ? n : (n + 7) / 8, most = (int64_t)kTrainSMs * 32;
+    const unsigned grid = (unsigned)(steps < 1 ? 1 : steps < most ? steps : most);
+    const bool wide = d % 8 == 0 && wide_rows(y_dev, ld_y, tb) && wide_rows(dout_dev, ld_dout, tb) && wide_rows(dy, ld_dy, tb);
+    return by_type(type, [&](auto t) {
+        using T = decltype(t);
+        return by_wide(wide, [&](auto w) {
+            return by_wide(few, [&](auto f) {
+                k_combine_backward<T, w.value, f.value ? kThreads : 32><<<grid, kThreads, 0, (cudaStream_t)cuda_stream>>>(
+                    (const T*)dout_dev, ld_dout, (const T*)y_dev, ld_y, places, place_dev, weight_dev, offset_dev, experts, n, (int)k, (int)d, (T*)dy, ld_dy,
+                    dweight_dev);
+                return launched();
+            });
+        });
+    });
+}

@@ -1,0 +1,430 @@
+"""Layers of experts in an encoder that is trained on the cluster labels: routing and its gradient, the experts' products and
+theirs, the weighted sum of the experts' rows, and activations whose inputs are kept in 8 bits for the backward pass.
+
+Argument marshalling only, like training.py, whose rules on autograd, streams and tensors that are written to hold here too.
+
+A layer's forward and backward pass:
+
+    r = route(x @ router, k)                                    # expert, weight, offset, row, place
+    z = expert_product(x, w1, r.offset, r.row)                  # one row a place
+    h, saved = activation(z, "silu")                            # z in 8 bits; z itself can go
+    y = expert_product(h, w2, r.offset)
+    out = combine(y, r.place, r.weight)
+
+    dy, dweight = combine_backward(dout, y, r.place, r.weight, r.offset)
+    h = activation_backward(None, saved, "silu", need_y=True)[1]        # h again, from the 8 bits
+    dh, dw2 = expert_product_backward(dy, h, w2, r.offset)
+    dz, _ = activation_backward(dh, saved, "silu")
+    dplace, dw1 = expert_product_backward(dz, x, w1, r.offset, r.row)
+    dx = combine(dplace, r.place)                               # and dlogits @ router.T:
+    dlogits = route_backward(dweight, logits, r.expert)
+"""
+from __future__ import annotations
+
+import ctypes as C
+from typing import NamedTuple
+
+from . import training as _t
+from .binding import lib
+from .training import _check, _given, _rows, _type
+
+_SCORES = {"softmax": 0, "sigmoid": 1}
+_KINDS = {"identity": 0, "silu": 1, "gelu": 2, "tanh": 3}
+MAX_EXPERTS = 512
+
+
+class Routing(NamedTuple):
+    """Where each row goes.  expert, weight, place: (n, k) int32, float32, int32; offset: experts + 1 int32; row: n k int32."""
+    expert: object
+    weight: object
+    offset: object
+    row: object
+    place: object
+
+
+class Checkpoint(NamedTuple):
+    """A matrix in 8 bits: q (n, 32 blocks) int8, scale (n, blocks) uint8; shape and dtype are the matrix's; gated: its halves
+    have blocks of their own."""
+    q: object
+    scale: object
+    shape: tuple
+    dtype: object
+    gated: bool
+
+
+_fn = None
+
+
+def _load():
+    global _fn
+    if _t._fn is None:
+        _t._load()
+    L = lib()
+    vp, i32, i64, f32, size = C.c_void_p, C.c_int32, C.c_int64, C.c_float, C.c_size_t
+    sig = {
+        "route": [vp, i32, i64, vp, i64, i32, i32, i32, i32, i32, i32, i32, f32, vp, vp, vp, vp, vp, vp, size, vp],
+        "route_scratch_bytes": [i64, i32],
+        "route_backward": [vp, vp, i32, i64, vp, i64, i32, i32, i32, i32, f32, vp, i64, vp],
+        "expert_product": [vp, i32, i64, i64, vp, i64, i64, i32, vp, vp, i64, i32, i32, i32, vp, i64, vp],
+        "expert_product_backward": [vp, i64, vp, i32, i64, i64, vp, i64, i64, i32, vp, vp, i64, i32, i32, i32, vp, i64, vp, i64, i64, vp],
+        "combine": [vp, i32, i64, i64, vp, vp, i64, i32, i32, vp, i64, vp],
+        "combine_backward": [vp, i64, vp, i32, i64, i64, vp, vp, vp, i32, i64, i32, i32, vp, i64, vp, vp],
+        "activation": [vp, i32, i64, i64, i32, i32, i32, vp, i64, vp, vp, vp],
+        "activation_backward": [vp, i32, i64, vp, i64, vp, vp, i64, i32, i32, i32, vp, i64, vp, i64, vp],
+        "checkpoint_blocks": [i32, i32],
+    }
+    fn = {}
+    for name, args in sig.items():
+        f = getattr(L, "gem_nlr_" + name)
+        f.argtypes = args
+        f.restype = size if name.endswith("_bytes") else i64 if name.endswith("_blocks") else C.c_int
+        fn[name] = f
+    _fn = fn
+    return fn
+
+
+def _elsewhere(at, stream):
+    return stream is not None or at != _t._device()
+
+
+def _there(fn, stream, inputs, *args):
+    return _t._there(fn, stream, [t for t in inputs if t is not None], *args)
+
+
+def _new(like, shape, dtype):
+    return _t._torch.empty(shape, dtype=dtype, device=like.device)
+
+
+def _ints(t, shape, at, name):
+    torch = _t._torch
+    if t.dtype != torch.int32 or t.shape != shape or not t.is_contiguous() or t.get_device() != at:
+        raise ValueError(f"{name} has to be {tuple(shape)} contiguous int32 on GPU {at}")
+    return t.data_ptr()
+
+
+def _floats(t, shape, at, name):
+    torch = _t._torch
+    if t.dtype != torch.float32 or t.shape != shape or not t.is_contiguous() or t.get_device() != at:
+        raise ValueError(f"{name} has to be {tuple(shape)} contiguous float32 on GPU {at}")
+    return t.data_ptr()
+
+
+def _matrix(t, name):
+    if t.dim() != 2:
+        raise ValueError(f"{name} has to be a matrix")
+    return _rows(t, name)
+
+
+def _score(score):
+    if score not in _SCORES:
+        raise ValueError(f"score is {score!r}: 'softmax' or 'sigmoid'")
+    return _SCORES[score]
+
+
+def route(logits, k, score="softmax", bias=None, groups=1, kept_groups=None, group_best=1, renormalize=True, scale=1.0, stream=None):
+    """gem_nlr_route of (n, experts) logits: a Routing.  bias: float32, one an expert, in the choice alone.  Logits of -inf leave
+    experts out.  kept_groups: all by default."""
+    fn = _fn or _load()
+    n, experts, ld = _matrix(logits, "logits")
+    at = logits.get_device()
+    if _elsewhere(at, stream):
+        return _there(route, stream, (logits, bias), logits, k, score, bias, groups, kept_groups, group_best, renormalize, scale)
+    torch = _t._torch
+    kind, how = _type(logits, "logits"), _score(score)
+    if kept_groups is None:
+        kept_groups = groups
+    if not 1 <= experts <= MAX_EXPERTS:
+        raise ValueError(f"{experts} experts: 1 to {MAX_EXPERTS}")
+    if not (1 <= groups <= 32 and experts % groups == 0 and 1 <= kept_groups <= groups and group_best in (1, 2)):
+        raise ValueError(f"{experts} experts in {groups} groups, {kept_groups} of them kept by their {group_best} best")
+    if not 1 <= k <= min(32, kept_groups * (experts // groups)):
+        raise ValueError(f"k is {k}: 1 to 32 and at most the experts that are kept")
+    if n * k >= 1 << 31:
+        raise ValueError(f"{n} rows to {k} experts each: places are int32")
+    if not abs(scale) < float("inf"):
+        raise ValueError(f"scale is {scale}")
+    bp = None if bias is None else _floats(bias, (experts,), at, "bias")
+    got = Routing(_new(logits, (n, k), torch.int32), _new(logits, (n, k), torch.float32), _new(logits, (experts + 1,), torch.int32),
+                  _new(logits, (n * k,), torch.int32), _new(logits, (n, k), torch.int32))
+    size = fn["route_scratch_bytes"](n, experts)
+    scratch = _new(logits, (size,), torch.uint8) if size else got.offset
+    _check(fn["route"](logits.data_ptr(), kind, ld, bp, n, experts, k, how, groups, kept_groups, group_best, 1 if renormalize else 0, scale,
+                       *(t.data_ptr() for t in got), scratch.data_ptr(), size, _t._stream(at)), "route")
+    return got
+
+
+def route_backward(dweight, logits, expert, score="softmax", renormalize=True, scale=1.0, stream=None):
+    """gem_nlr_route_backward: the gradient of route's weights in the logits, of the logits' type and shape, for the choice
+    `expert` that it made."""
+    fn = _fn or _load()
+    n, experts, ld = _matrix(logits, "logits")
+    at = logits.get_device()
+    if _elsewhere(at, stream):
+        return _there(route_backward, stream, (logits, dweight, expert), dweight, logits, expert, score, renormalize, scale)
+    torch = _t._torch
+    kind, how = _type(logits, "logits"), _score(score)
+    if experts > MAX_EXPERTS:
+        raise ValueError(f"{experts} experts: 1 to {MAX_EXPERTS}")
+    if expert.dim() != 2 or not 1 <= expert.shape[1] <= 32 or n * expert.shape[1] >= 1 << 31:
+        raise ValueError(f"expert has to be ({n}, k) with k from 1 to 32")
+    if not abs(scale) < float("inf"):
+        raise ValueError(f"scale is {scale}")
+    k = expert.shape[1]
+    ep, dp = _ints(expert, (n, k), at, "expert"), _floats(dweight, (n, k), at, "dweight")
+    out = _new(logits, (n, experts), logits.dtype)
+    _check(fn["route_backward"](dp, logits.data_ptr(), kind, ld, ep, n, experts, k, how, 1 if renormalize else 0, scale, out.data_ptr(), experts,
+                                _t._stream(at)), "route_backward")
+    return out
+
+
+def _weights(w, at, name="w"):
+    """(experts, d_in, d_out, row distance, expert distance, turned) of (experts, d_in, d_out) weights, of which either of the last two
+    dimensions may be the contiguous one."""
+    if w.dim() != 3:
+        raise ValueError(f"{name} has to be (experts, d_in, d_out)")
+    experts, d_in, d_out = w.shape
+    if not 1 <= experts <= MAX_EXPERTS or d_in < 1 or d_out < 1:
+        raise ValueError(f"{name} is {tuple(w.shape)}: 1 to {MAX_EXPERTS} experts, and no empty dimension")
+    if w.get_device() != at:
+        raise ValueError(f"{name} is not on GPU {at}")
+    es, si, so = w.stride()
+    if so == 1 or d_out == 1 and si == 1 and d_in == 1:
+        return experts, d_in, d_out, si if d_in > 1 else d_out, es, 0
+    if si == 1:
+        return experts, d_in, d_out, so if d_out > 1 else d_in, es, 1
+    if d_out == 1:
+        return experts, d_in, d_out, si, es, 0
+    if d_in == 1:
+        return experts, d_in, d_out, so, es, 1
+    raise ValueError(f"{name} has neither contiguous rows nor contiguous columns")
+
+
+def _places(x, d_in, offset, experts, row, at):
+    """(rows of x, their distance, places, row's address) of a call on x."""
+    torch = _t._torch
+    x_rows, d, ld = _matrix(x, "x")
+    if x.dtype not in (torch.float16, torch.bfloat16):
+        raise ValueError(f"x is {x.dtype}: float16 or bfloat16 is needed")
+    if d != d_in:
+        raise ValueError(f"x has {d} columns, the weights {d_in} rows")
+    _ints(offset, (experts + 1,), at, "offset")
+    if row is None:
+        return x_rows, ld, x_rows, None
+    if row.dim() != 1:
+        raise ValueError("row has to be a vector")
+    return x_rows, ld, row.shape[0], _ints(row, row.shape, at, "row")
+
+
+def expert_product(x, w, offset, row=None, out=None, stream=None):
+    """gem_nlr_expert_product: y (places, d_out) with y[p] = x[row[p]] @ w[e] for the places p from offset[e] to offset[e + 1], zeros
+    behind the last; without row y[p] = x[p] @ w[e].  x: float16 or bfloat16; w: (experts, d_in, d_out) of its type, either of
+    the last two dimensions contiguous."""
+    fn = _fn or _load()
+    if not x.is_cuda:
+        raise ValueError("x is not on a GPU")
+    at = x.get_device()
+    if _elsewhere(at, stream):
+        return _there(expert_product, stream, (x, w, offset, row, out), x, w, offset, row, out)
+    experts, d_in, d_out, ldw, es, turned = _weights(w, at)
+    x_rows, ld, places, rp = _places(x, d_in, offset, experts, row, at)
+    if w.dtype != x.dtype:
+        raise ValueError(f"w is {w.dtype}, x {x.dtype}")
+    y, ldy = out, d_out
+    if out is None:
+        y = _new(x, (places, d_out), x.dtype)
+    else:
+        if out.shape != (places, d_out) or out.dtype != x.dtype or out.device != x.device:
+            raise ValueError(f"out has to be {(places, d_out)} {x.dtype} on {x.device}")
+        ldy = _rows(out, "out")[2]
+    _check(fn["expert_product"](x.data_ptr(), _type(x, "x"), ld, x_rows, w.data_ptr(), ldw, es, turned, offset.data_ptr(), rp, places, experts, d_in, d_out,
+                                y.data_ptr(), ldy, _t._stream(at)), "expert_product")
+    if out is not None:
+        _t._written(out)
+    return y
+
+
+def expert_product_backward(dy, x, w, offset, row=None, need_dx=True, need_dw=True, stream=None):
+    """gem_nlr_expert_product_backward: (dx, dw), None for each that is not needed.  dx: (places, d_in), one row a place (combine without
+    weights takes the sum over a row's places); dw: of w's shape and type, in its order of dimensions."""
+    fn = _fn or _load()
+    if not x.is_cuda:
+        raise ValueError("x is not on a GPU")
+    at = x.get_device()
+    if _elsewhere(at, stream):
+        return _there(expert_product_backward, stream, (x, dy, w, offset, row), dy, x, w, offset, row, need_dx, need_dw)
+    experts, d_in, d_out, ldw, es, turned = _weights(w, at)
+    x_rows, ld, places, rp = _places(x, d_in, offset, experts, row, at)
+    if w.dtype != x.dtype:
+        raise ValueError(f"w is {w.dtype}, x {x.dtype}")
+    if dy.shape != (places, d_out) or dy.dtype != x.dtype or dy.get_device() != at:
+        raise ValueError(f"dy has to be {(places, d_out)} {x.dtype} on GPU {at}")
+    ldg = _rows(dy, "dy")[2]
+    if not (need_dx or need_dw):
+        return None, None
+    dx = _new(x, (places, d_in), x.dtype) if need_dx else None
+    dw, dwp, ldd = None, None, 0
+    if need_dw:
+        made = _new(w, (experts, d_out, d_in) if turned else (experts, d_in, d_out), w.dtype)
+        dw, dwp, ldd = made.transpose(1, 2) if turned else made, made.data_ptr(), d_in if turned else d_out
+    _check(fn["expert_product_backward"](dy.data_ptr(), ldg, x.data_ptr(), _type(x, "x"), ld, x_rows, w.data_ptr(), ldw, es, turned, offset.data_ptr(), rp, places,
+                                         experts, d_in, d_out, None if dx is None else dx.data_ptr(), d_in, dwp, ldd, d_in * d_out, _t._stream(at)),
+           "expert_product_backward")
+    return dx, dw
+
+
+def _slots(place, n, at):
+    if place.dim() != 2 or not 1 <= place.shape[1] <= 32:
+        raise ValueError("place has to be (rows, k) with k from 1 to 32")
+    return place.shape[1], _ints(place, place.shape if n is None else (n, place.shape[1]), at, "place")
+
+
+def combine(y, place, weight=None, out=None, stream=None):
+    """gem_nlr_combine: out[t] = sum over j of weight[t, j] y[place[t, j]], of y's type; weight: float32 or None for ones."""
+    fn = _fn or _load()
+    places, d, ld = _matrix(y, "y")
+    at = y.get_device()
+    if _elsewhere(at, stream):
+        return _there(combine, stream, (y, place, weight, out), y, place, weight, out)
+    k, pp = _slots(place, None, at)
+    n = place.shape[0]
+    wp = None if weight is None else _floats(weight, place.shape, at, "weight")
+    to, ldo = out, d
+    if out is None:
+        to = _new(y, (n, d), y.dtype)
+    else:
+        if out.shape != (n, d) or out.dtype != y.dtype or out.device != y.device:
+            raise ValueError(f"out has to be {(n, d)} {y.dtype} on {y.device}")
+        ldo = _rows(out, "out")[2]
+    _check(fn["combine"](y.data_ptr(), _type(y, "y"), ld, places, pp, wp, n, k, d, to.data_ptr(), ldo, _t._stream(at)), "combine")
+    if out is not None:
+        _t._written(out)
+    return to
+
+
+def combine_backward(dout, y, place, weight, offset, need_dy=True, need_dweight=True, stream=None):
+    """gem_nlr_combine_backward: (dy, dweight), None for each that is not needed; dy has y's shape and type, dweight is float32 (n, k).
+    weight None: ones."""
+    fn = _fn or _load()
+    places, d, ld = _matrix(y, "y")
+    at = y.get_device()
+    if _elsewhere(at, stream):
+        return _there(combine_backward, stream, (y, dout, place, weight, offset), dout, y, place, weight, offset, need_dy, need_dweight)
+    k, pp = _slots(place, dout.shape[0] if dout.dim() else 0, at)
+    n = place.shape[0]
+    if dout.shape != (n, d) or dout.dtype != y.dtype or dout.get_device() != at:
+        raise ValueError(f"dout has to be {(n, d)} {y.dtype} on GPU {at}")
+    ldo = _rows(dout, "dout")[2]
+    wp = None if weight is None else _floats(weight, place.shape, at, "weight")
+    if offset.dim() != 1 or offset.shape[0] < 2:
+        raise ValueError("offset has to be a vector of experts + 1")
+    op = _ints(offset, offset.shape, at, "offset")
+    if not (need_dy or need_dweight):
+        return None, None
+    dy = _new(y, (places, d), y.dtype) if need_dy else None
+    dw = _new(y, (n, k), _t._torch.float32) if need_dweight else None
+    _check(fn["combine_backward"](dout.data_ptr(), ldo, y.data_ptr(), _type(y, "y"), ld, places, pp, wp, op, offset.shape[0] - 1, n, k, d,
+                                  None if dy is None else dy.data_ptr(), d, None if dw is None else dw.data_ptr(), _t._stream(at)), "combine_backward")
+    return dy, dw
+
+
+def _kind(kind):
+    if kind not in _KINDS:
+        raise ValueError(f"the activation is {kind!r}: one of {', '.join(_KINDS)}")
+    return _KINDS[kind]
+
+
+def _halves(columns, gated, name):
+    if gated and columns % 2:
+        raise ValueError(f"{name} has {columns} columns: gated units have an even number")
+    return columns // 2 if gated else columns
+
+
+def activation(z, kind, gated=False, checkpoint=True, need_y=True, out=None, stream=None):
+    """gem_nlr_activation: (y, saved), y = f(z), or f(left half) times right half (gated); saved: z in 8 bits for
+    activation_backward, None without checkpoint.  kind: 'silu', 'gelu', 'tanh' or 'identity'."""
+    fn = _fn or _load()
+    n, wide, ld = _rows(z, "z")
+    at = z.get_device()
+    if _elsewhere(at, stream):
+        return _there(activation, stream, (z, out), z, kind, gated, checkpoint, need_y, out)
+    torch = _t._torch
+    d, f, t = _halves(wide, gated, "z"), _kind(kind), _type(z, "z")
+    if not (checkpoint or need_y):
+        return None, None
+    y = saved = None
+    yp, ldy, qp, sp = None, d, None, None
+    if need_y:
+        shape = (*z.shape[:-1], d)
+        y = out
+        if out is None:
+            y = _new(z, shape, z.dtype)
+        else:
+            if out.shape != shape or out.dtype != z.dtype or out.device != z.device:
+                raise ValueError(f"out has to be {shape} {z.dtype} on {z.device}")
+            ldy = _rows(out, "out")[2]
+        yp = y.data_ptr()
+    if checkpoint:
+        blocks = fn["checkpoint_blocks"](d, 1 if gated else 0)
+        saved = Checkpoint(_new(z, (n, blocks * 32), torch.int8), _new(z, (n, blocks), torch.uint8), tuple(z.shape), z.dtype, bool(gated))
+        qp, sp = saved.q.data_ptr(), saved.scale.data_ptr()
+    _check(fn["activation"](z.data_ptr(), t, ld, n, d, f, 1 if gated else 0, yp, ldy, qp, sp, _t._stream(at)), "activation")
+    if need_y and out is not None:
+        _t._written(out)
+    return y, saved
+
+
+def activation_backward(dy, saved, kind, gated=False, need_y=False, stream=None):
+    """gem_nlr_activation_backward: (dz, y), from z in 8 bits (a Checkpoint) or z itself.  dy None: y alone; need_y: y again."""
+    fn = _fn or _load()
+    packed = isinstance(saved, Checkpoint)
+    first = saved.q if packed else saved
+    if not first.is_cuda:
+        raise ValueError("what was saved is not on a GPU")
+    at = first.get_device()
+    if _elsewhere(at, stream):
+        inputs = (saved.q, saved.scale, dy) if packed else (saved, dy)
+        return _there(activation_backward, stream, inputs, dy, saved, kind, gated, need_y)
+    torch = _t._torch
+    f, qp, sp, zp, ldz = _kind(kind), None, None, None, 0
+    if packed:
+        shape, dtype, n = saved.shape, saved.dtype, saved.q.shape[0]
+        wide = shape[-1]
+        if bool(gated) != saved.gated:
+            raise ValueError("gated has to be as it was when the checkpoint was made")
+        d = _halves(wide, gated, "z")
+        blocks = fn["checkpoint_blocks"](d, 1 if gated else 0)
+        for t, like, name in ((saved.q, (torch.int8, (n, blocks * 32)), "q"), (saved.scale, (torch.uint8, (n, blocks)), "scale")):
+            if t.dtype != like[0] or t.shape != like[1] or not t.is_contiguous() or t.get_device() != at:
+                raise ValueError(f"the checkpoint's {name} has to be {like[1]} contiguous {like[0]} on GPU {at}")
+        qp, sp = saved.q.data_ptr(), saved.scale.data_ptr()
+        kinds = _t._types.get(dtype)
+    else:
+        n, wide, ldz = _rows(saved, "z")
+        shape, dtype, zp, kinds, d = tuple(saved.shape), saved.dtype, saved.data_ptr(), _type(saved, "z"), _halves(wide, gated, "z")
+    lead = (*shape[:-1], d)
+    dz = y = None
+    gp, ldg = None, 0
+    if dy is not None:
+        if dy.shape != lead or dy.dtype != dtype or dy.get_device() != at:
+            raise ValueError(f"dy has to be {lead} {dtype} on GPU {at}")
+        ldg, gp = _rows(dy, "dy")[2], dy.data_ptr()
+        dz = _new(first, shape, dtype)
+    if need_y:
+        y = _new(first, lead, dtype)
+    if dz is None and y is None:
+        return None, None
+    _check(fn["activation_backward"](gp, kinds, ldg, zp, ldz, qp, sp, n, d, f, 1 if gated else 0, None if dz is None else dz.data_ptr(), wide,
+                                     None if y is None else y.data_ptr(), d, _t._stream(at)), "activation_backward")
+    return dz, y
+
+
+def checkpoint(x, stream=None):
+    """x in 8 bits, as activation keeps its input."""
+    return activation(x, "identity", need_y=False, stream=stream)[1]
+
+
+def restore(saved, stream=None):
+    """What a Checkpoint stands for, in the type and shape of what it was made from."""
+    if saved.gated:
+        raise ValueError("the checkpoint of gated units is restored by activation_backward")
+    return activation_backward(None, saved, "identity", need_y=True, stream=stream)[1]
