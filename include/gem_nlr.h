@@ -443,7 +443,7 @@ int gem_nlr_route_backward(const float *dweight_dev, const void *logits_dev, int
  * x: x_rows x d_in; row: places entries, NULL when place p's row is x's row p (then x_rows >= places); W_e: d_in x
  * d_out at w + e stride_w, rows ld_w apart, or with w_turned == 1 its transpose (d_out x d_in); y: places x d_out.
  * x, w, y: GEM_NLR_F16 or GEM_NLR_BF16; products are summed in FP32 and rounded once.  A place whose row entry is -1 has
- * a row of zeros for x.  16-byte aligned rows (and stride_w) take the fast loads.                              */
+ * a row of zeros for x.  places < 2^31 - 2^16.  16-byte aligned rows (and stride_w) take the fast loads.        */
 int gem_nlr_expert_product(const void *x_dev, int32_t type, int64_t ld_x, int64_t x_rows, const void *w_dev,
                            int64_t ld_w, int64_t stride_w, int32_t w_turned, const int32_t *offset_dev,
                            const int32_t *row_dev, int64_t places, int32_t experts, int32_t d_in, int32_t d_out,

@@ -34,7 +34,7 @@ enum Mode { kRowsTimesPlain = 0, kRowsTimesTurned = 1, kWeights = 2 };
 template <int BN> struct Shape {
     static constexpr int A = kTileM * kRow, B = BN * kRow, STAGE = A + B;
     static constexpr int STAGES = BN == 256 ? 4 : BN == 128 ? 6 : 8;
-    static constexpr int STAGING = 4 * 32 * kRow; // a warp's 32 rows of 64 columns
+    static constexpr int STAGING = 4 * 2048;      // a warp's 32 rows of 32 columns
     static constexpr int BARRIERS = 2 * STAGES + 5;
     static constexpr int TABLES = (2 * GEM_NLR_MAX_EXPERTS + 4) * 4;
     static constexpr int SHARED = 1024 + STAGES * STAGE + STAGING + TABLES + BARRIERS * 8 + 16;
@@ -63,11 +63,12 @@ struct Product {
     int bf16;
 };
 
+// (C is in memory, and a tile has at least 32 of its elements: tiles are counted in 32 bits.)
 struct Tile {
     int expert;
-    int64_t c_row, stop;      // first row of C and the one behind the last (rows: places; weights: of C_e)
+    int c_row, stop;          // first row of C and the one behind the last (rows: places; weights: of C_e)
     int n0;
-    int64_t k_first;          // weights: first place
+    int k_first;              // weights: first place
     int k;                    // length of the sum
 };
 
@@ -103,7 +104,8 @@ __device__ __forceinline__ void load_rows(uint32_t dst, const CUtensorMap* map, 
 }
 
 // first[e]: e's first place (falling or wild offsets cut to what is possible), tile0[e]: its first row of tiles; behind the
-// experts the places without one.  By one warp.
+// experts the places without one.  HEIGHT: of a tile.  By one warp.
+template <int HEIGHT>
 __device__ __forceinline__ void make_tables(const Product& q, int32_t* first, int32_t* tile0, int lane)
 {
     int32_t reached = 0, tiles = 0, before = 0;
@@ -119,7 +121,7 @@ __device__ __forceinline__ void make_tables(const Product& q, int32_t* first, in
         v = max(v, reached);
         int32_t prev = __shfl_up_sync(0xffffffffu, v, 1);
         if (lane == 0) prev = before;
-        int32_t t = e == 0 ? 0 : (int32_t)(((int64_t)v - prev + kTileM - 1) / kTileM);   // row tiles of e - 1
+        int32_t t = e == 0 ? 0 : (int32_t)(((int64_t)v - prev + HEIGHT - 1) / HEIGHT);   // row tiles of e - 1
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
             const int32_t u = __shfl_up_sync(0xffffffffu, t, o);
@@ -135,17 +137,17 @@ __device__ __forceinline__ void make_tables(const Product& q, int32_t* first, in
     }
 }
 
-template <int MODE, int BN>
-__device__ __forceinline__ Tile tile_at(const Product& q, const int32_t* first, const int32_t* tile0, int64_t t)
+template <int MODE, int BN, int HEIGHT = kTileM>
+__device__ __forceinline__ Tile tile_at(const Product& q, const int32_t* first, const int32_t* tile0, int t)
 {
     Tile w;
     const int nt = (q.n + BN - 1) / BN;
-    const int64_t row_tile = t / nt;
-    w.n0 = (int)(t - row_tile * nt) * BN;
+    const int row_tile = t / nt;
+    w.n0 = (t - row_tile * nt) * BN;
     if (MODE == kWeights) {
-        const int mt = (q.m + kTileM - 1) / kTileM;
-        w.expert = (int)(row_tile / mt);
-        w.c_row = (row_tile - (int64_t)w.expert * mt) * kTileM;
+        const int mt = (q.m + HEIGHT - 1) / HEIGHT;
+        w.expert = row_tile / mt;
+        w.c_row = (row_tile - w.expert * mt) * HEIGHT;
         w.stop = q.m;
         w.k_first = first[w.expert];
         w.k = first[w.expert + 1] - first[w.expert];
@@ -156,7 +158,7 @@ __device__ __forceinline__ Tile tile_at(const Product& q, const int32_t* first, 
             if (tile0[mid] <= row_tile) lo = mid; else hi = mid - 1;
         }
         w.expert = lo;
-        w.c_row = first[lo] + (row_tile - tile0[lo]) * kTileM;
+        w.c_row = first[lo] + (row_tile - tile0[lo]) * HEIGHT;
         w.stop = first[lo + 1];
         w.k_first = 0;
         w.k = lo == q.experts ? 0 : q.k;                             // places without an expert: zeros
@@ -224,6 +226,64 @@ __device__ __forceinline__ void load_ordinary(const Operand& o, const int32_t* r
     }
 }
 
+// A warp's 32 rows of `steps` times 32 columns of a tile, from accumulator column `acc` (the warp's lanes) into C from (row0, col0) on;
+// zeros where no sum was taken, NaN where a wait ran out.  32 columns at a time go through the warp's 2 KB of shared memory, so
+// that rows are stored in pieces of 64 bytes.
+template <int MODE>
+__device__ __forceinline__ void store_tile(const Product& q, const Tile& w, int row0, int col0, int steps, uint32_t acc, uint32_t mine, int lane, bool on)
+{
+    uint16_t* c = q.c + (MODE == kWeights ? w.expert * q.stride_c : 0) + row0 * q.ldc;
+    const int rows = min(32, w.stop - row0);
+    const uint32_t to_stage = mine + (uint32_t)(lane * 64), phase = (uint32_t)(lane >> 1) & 3u;
+    const uint32_t from_stage = mine + (uint32_t)((lane >> 2) * 64 + (((lane & 3) ^ ((lane >> 3) & 3)) << 4));
+#pragma unroll 1
+    for (int g = 0; g < steps && col0 < q.n; ++g, col0 += 32) {
+        float v[32];
+        if (w.k && on) {
+            tmem_ld32(acc + (uint32_t)(g * 32), v);
+        } else {
+            const float fill = on ? 0.0f : __uint_as_float(0x7fc00000u);
+#pragma unroll
+            for (int x = 0; x < 32; ++x) v[x] = fill;
+        }
+#pragma unroll
+        for (int x = 0; x < 4; ++x) {
+            uint32_t h[4];
+#pragma unroll
+            for (int y = 0; y < 4; ++y) {
+                const float lo = v[x * 8 + 2 * y], hi = v[x * 8 + 2 * y + 1];
+                if (q.bf16) {
+                    const __nv_bfloat162 p = __floats2bfloat162_rn(lo, hi);
+                    h[y] = *reinterpret_cast<const uint32_t*>(&p);
+                } else {
+                    const __half2 p = __floats2half2_rn(lo, hi);
+                    h[y] = *reinterpret_cast<const uint32_t*>(&p);
+                }
+            }
+            sts128u(to_stage + (((uint32_t)x ^ phase) << 4), make_uint4(h[0], h[1], h[2], h[3]));
+        }
+        __syncwarp();
+        const int col = col0 + (lane & 3) * 8;
+        uint16_t* to = c + (int64_t)(lane >> 2) * q.ldc + col;
+#pragma unroll
+        for (int x = 0; x < 4; ++x) {
+            const float4 f = lds128(from_stage + (uint32_t)(x * 512));
+            if (8 * x + (lane >> 2) < rows && col < q.n) {
+                uint16_t* at = to + (int64_t)(8 * x) * q.ldc;
+                const uint32_t h[4] = {__float_as_uint(f.x), __float_as_uint(f.y), __float_as_uint(f.z), __float_as_uint(f.w)};
+                if (q.c_wide && col + 8 <= q.n) {
+                    *reinterpret_cast<uint4*>(at) = make_uint4(h[0], h[1], h[2], h[3]);
+                } else {
+#pragma unroll
+                    for (int y = 0; y < 8; ++y)
+                        if (col + y < q.n) at[y] = (uint16_t)(h[y >> 1] >> (16 * (y & 1)));
+                }
+            }
+        }
+        __syncwarp();
+    }
+}
+
 template <int MODE, int BN, bool TMA>
 __global__ void __launch_bounds__(TMA ? 256 : 384, 1)
 k_expert(const __grid_constant__ Product q)
@@ -261,27 +321,27 @@ k_expert(const __grid_constant__ Product q)
         fence_barrier_init();
     }
     if (warp == 2) tmem_alloc(smem_u32((const void*)tmem_at), 2 * BN);
-    if (warp == 3) make_tables(q, first, tile0, lane);
+    if (warp == 3) make_tables<kTileM>(q, first, tile0, lane);
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem = *tmem_at;
 
     const int nt = (q.n + BN - 1) / BN;
-    const int64_t tiles = (MODE == kWeights ? (int64_t)q.experts * ((q.m + kTileM - 1) / kTileM) : tile0[q.experts + 1]) * nt;
+    const int tiles = (MODE == kWeights ? q.experts * ((q.m + kTileM - 1) / kTileM) : tile0[q.experts + 1]) * nt;
 
     if (TMA && warp == 0) {
         int s = 0;
         uint32_t parity = 1;                                  // the first round finds every stage free
         int64_t issued = 0;
         bool on = true;
-        for (int64_t t = blockIdx.x; t < tiles && on; t += gridDim.x) {
+        for (int t = blockIdx.x; t < tiles && on; t += gridDim.x) {
             const Tile w = tile_at<MODE, BN>(q, first, tile0, t);
             const int chunks = (w.k + kChunk - 1) / kChunk;
             int4 named = make_int4(0, 0, 0, 0);
             if (A_K && q.a.gather && chunks) named = four_rows(q.row, w.c_row + 4 * lane, w.stop, q.a.rows);
             for (int c = 0; c < chunks; ++c) {
-                const int64_t p0 = w.k_first + (int64_t)c * kChunk;        // weights: the chunk's first place
+                const int p0 = w.k_first + c * kChunk;        // weights: the chunk's first place
                 if (MODE == kWeights && (q.a.gather || q.b.gather))
                     named = four_rows(q.row, p0 + 4 * (lane & 15), w.k_first + w.k, q.a.gather ? q.a.rows : q.b.rows);
                 on = wait_for(free_(s), parity, dead);
@@ -292,11 +352,11 @@ k_expert(const __grid_constant__ Product q)
                 __syncwarp();
                 if (A_K) {
                     if (q.a.gather) load_rows(a + lane * 512, &q.ta, c * kChunk, named, bar);
-                    else if (lane == 0) tma_load_2d(a, &q.ta, c * kChunk, (int)w.c_row, bar);
+                    else if (lane == 0) tma_load_2d(a, &q.ta, c * kChunk, w.c_row, bar);
                 } else if (q.a.gather) {
-                    load_rows(a + lane * 512, &q.ta, (int)w.c_row + 64 * (lane >> 4), named, bar);
+                    load_rows(a + lane * 512, &q.ta, w.c_row + 64 * (lane >> 4), named, bar);
                 } else if (lane < 2) {
-                    tma_load_2d(a + lane * 8192, &q.ta, (int)w.c_row + 64 * lane, (int)p0, bar);
+                    tma_load_2d(a + lane * 8192, &q.ta, w.c_row + 64 * lane, p0, bar);
                 }
                 if (MODE == kRowsTimesTurned) {
                     if (lane == 0) load_3d(b, &q.tb, c * kChunk, w.n0, w.expert, bar);
@@ -309,7 +369,7 @@ k_expert(const __grid_constant__ Product q)
                         if (box < BN / 64) load_rows(b + box * 8192 + (lane & 15) * 512, &q.tb, w.n0 + 64 * box, named, bar);
                     }
                 } else if (lane < BN / 64) {
-                    tma_load_2d(b + lane * 8192, &q.tb, w.n0 + 64 * lane, (int)p0, bar);
+                    tma_load_2d(b + lane * 8192, &q.tb, w.n0 + 64 * lane, p0, bar);
                 }
                 ++issued;
                 if (++s == S::STAGES) { s = 0; parity ^= 1u; }
@@ -326,7 +386,7 @@ k_expert(const __grid_constant__ Product q)
         uint32_t parity = 0;
         int64_t i = 0;                                        // accumulators handed over
         bool on = true;
-        for (int64_t t = blockIdx.x; t < tiles && on; t += gridDim.x) {
+        for (int t = blockIdx.x; t < tiles && on; t += gridDim.x) {
             const Tile w = tile_at<MODE, BN>(q, first, tile0, t);
             if (w.k == 0) continue;
             const int chunks = (w.k + kChunk - 1) / kChunk;
@@ -373,10 +433,10 @@ k_expert(const __grid_constant__ Product q)
         }
     } else if (warp >= 4 && warp < 8) {
         const int quarter = warp & 3;
-        const uint32_t mine = smem_u32(staging) + (uint32_t)quarter * (32 * kRow);
+        const uint32_t mine = smem_u32(staging) + (uint32_t)quarter * 2048u;
         int64_t i = 0;
         bool on = true;
-        for (int64_t t = blockIdx.x; t < tiles; t += gridDim.x) {
+        for (int t = blockIdx.x; t < tiles; t += gridDim.x) {
             const Tile w = tile_at<MODE, BN>(q, first, tile0, t);
             const int a = (int)(i & 1);
             if (w.k && on) {
@@ -384,58 +444,7 @@ k_expert(const __grid_constant__ Product q)
                 on = __all_sync(0xffffffffu, on);
                 tc_fence_after();
             }
-            uint16_t* c = q.c + (MODE == kWeights ? w.expert * q.stride_c : 0);
-#pragma unroll 1
-            for (int g = 0; g < BN / 64; ++g) {
-                const int col0 = w.n0 + g * 64;
-                if (col0 < q.n) {
-                    float v[64];
-                    if (w.k && on) {
-                        tmem_ld32(tmem + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(a * BN + g * 64), v);
-                        tmem_ld32(tmem + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(a * BN + g * 64 + 32), v + 32);
-                    } else {
-                        const float fill = on ? 0.0f : __uint_as_float(0x7fc00000u);
-#pragma unroll
-                        for (int x = 0; x < 64; ++x) v[x] = fill;
-                    }
-#pragma unroll
-                    for (int x = 0; x < 8; ++x) {
-                        uint32_t h[4];
-#pragma unroll
-                        for (int y = 0; y < 4; ++y) {
-                            const float lo = v[x * 8 + 2 * y], hi = v[x * 8 + 2 * y + 1];
-                            if (q.bf16) {
-                                const __nv_bfloat162 p = __floats2bfloat162_rn(lo, hi);
-                                h[y] = *reinterpret_cast<const uint32_t*>(&p);
-                            } else {
-                                const __half2 p = __floats2half2_rn(lo, hi);
-                                h[y] = *reinterpret_cast<const uint32_t*>(&p);
-                            }
-                        }
-                        sts128u(mine + (uint32_t)(lane * kRow + ((x ^ (lane & 7)) << 4)), make_uint4(h[0], h[1], h[2], h[3]));
-                    }
-                    __syncwarp();
-#pragma unroll
-                    for (int x = 0; x < 8; ++x) {
-                        const int r = 4 * x + (lane >> 3), ch = lane & 7;
-                        const float4 f = lds128(mine + (uint32_t)(r * kRow + ((ch ^ (r & 7)) << 4)));
-                        const int64_t row = w.c_row + quarter * 32 + r;
-                        const int col = col0 + ch * 8;
-                        if (row < w.stop && col < q.n) {
-                            uint16_t* to = c + row * q.ldc + col;
-                            const uint32_t h[4] = {__float_as_uint(f.x), __float_as_uint(f.y), __float_as_uint(f.z), __float_as_uint(f.w)};
-                            if (q.c_wide && col + 8 <= q.n) {
-                                *reinterpret_cast<uint4*>(to) = make_uint4(h[0], h[1], h[2], h[3]);
-                            } else {
-#pragma unroll
-                                for (int y = 0; y < 8; ++y)
-                                    if (col + y < q.n) to[y] = (uint16_t)(h[y >> 1] >> (16 * (y & 1)));
-                            }
-                        }
-                    }
-                    __syncwarp();
-                }
-            }
+            store_tile<MODE>(q, w, w.c_row + quarter * 32, w.n0, BN / 32, tmem + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(a * BN), mine, lane, on);
             if (w.k) {
                 tc_fence_before();
                 __syncwarp();
@@ -448,16 +457,16 @@ k_expert(const __grid_constant__ Product q)
         int s = 0;
         uint32_t parity = 1;
         bool on = true;
-        for (int64_t t = blockIdx.x; t < tiles && on; t += gridDim.x) {
+        for (int t = blockIdx.x; t < tiles && on; t += gridDim.x) {
             const Tile w = tile_at<MODE, BN>(q, first, tile0, t);
             const int chunks = (w.k + kChunk - 1) / kChunk;
             for (int c = 0; c < chunks; ++c) {
                 on = wait_for(free_(s), parity, dead);
                 if (!on) break;
                 const uint32_t a = stages + (uint32_t)s * S::STAGE, b = a + S::A;
-                const int64_t p0 = w.k_first + (int64_t)c * kChunk, end = w.k_first + w.k;
+                const int p0 = w.k_first + c * kChunk, end = w.k_first + w.k;
                 if (MODE == kWeights) {
-                    load_ordinary<false, kTileM>(q.a, q.row, 0, p0, end, true, (int)w.c_row, q.a.columns, a, thread);
+                    load_ordinary<false, kTileM>(q.a, q.row, 0, p0, end, true, w.c_row, q.a.columns, a, thread);
                     load_ordinary<false, BN>(q.b, q.row, 0, p0, end, true, w.n0, q.b.columns, b, thread);
                 } else {
                     load_ordinary<true, kTileM>(q.a, q.row, 0, w.c_row, w.stop, true, c * kChunk, q.a.columns, a, thread);
@@ -473,6 +482,357 @@ k_expert(const __grid_constant__ Product q)
     tc_fence_before();
     __syncthreads();
     if (warp == 2) tmem_dealloc(tmem, 2 * BN);
+}
+
+// ---- two SMs on one tile of 256 x 256 ------------------------------------------------------------------------------------------
+// A stage costs 48 KB of loads a 128 x 256 tile of one SM, and 32 KB an SM here: each SM of a pair holds 128 rows of A and 128
+// columns of B, the MMA reads both SMs' shared memory, and each keeps 128 rows of accumulators.  The first SM issues the MMAs for
+// both; the second's loads and epilogue signal the first's barriers.
+//
+//   warp 0         TMA loads, each SM its own
+//   warp 1         (first SM) issues the MMAs
+//   warps 4-11     epilogue: a quarter of the rows and a half of the columns each
+//   warps 12-15    load what TMA boxes cannot: rows gathered by index, and an expert's last, cut rows where they are the K dimension
+//                  (16-byte asynchronous copies, zeros where nothing is)
+//   warp 3         waits for these copies, makes them visible to the tensor cores and signals
+// COPIES: 0 none, 1 the cut rows alone, 2 gathered rows too.
+
+constexpr int kPairN = 256;
+struct Pair {
+    static constexpr int A = kTileM * kRow, B = kTileM * kRow, STAGE = A + B;
+    static constexpr int STAGES = 6;
+    static constexpr int STAGING = 8 * 2048;
+    static constexpr int BARRIERS = 4 * STAGES + 5;
+    static constexpr int TABLES = (2 * GEM_NLR_MAX_EXPERTS + 4) * 4;
+    static constexpr int SHARED = 1024 + STAGES * STAGE + STAGING + TABLES + BARRIERS * 8 + 16;
+};
+
+// One thread of a converged warp.  What it runs alone takes its operands from uniform registers, which the MMAs and TMA copies read.
+__device__ __forceinline__ bool one_thread()
+{
+    uint32_t r;
+    asm volatile("{\n\t.reg .pred p;\n\t"
+                 "elect.sync _|p, 0xffffffff;\n\t"
+                 "selp.u32 %0, 1, 0, p;\n\t}" : "=r"(r));
+    return r != 0;
+}
+
+__device__ __forceinline__ uint32_t pair_rank()
+{
+    uint32_t r;
+    asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+    return r;
+}
+// The address of the first SM's copy of a shared variable.
+__device__ __forceinline__ uint32_t of_first(uint32_t addr)
+{
+    uint32_t r;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, 0;" : "=r"(r) : "r"(addr));
+    return r;
+}
+__device__ __forceinline__ void pair_barrier()
+{
+    asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+__device__ __forceinline__ void arrive_at(uint32_t bar)              // a barrier of either SM
+{
+    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
+}
+__device__ __forceinline__ bool pair_wait(uint32_t bar, uint32_t parity, volatile uint32_t* dead, uint32_t limit = kSpinLimit << 4)
+{
+    for (uint32_t i = 0; i < limit; ++i) {
+        uint32_t ok;
+        asm volatile("{\n\t.reg .pred p;\n\t"
+                     "mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+                     "selp.u32 %0, 1, 0, p;\n\t}" : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
+        if (ok) return true;
+        if ((i & 63u) == 63u && *dead) return false;
+    }
+    *dead = 1u;
+    return false;
+}
+__device__ __forceinline__ void pair_mma(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate)
+{
+    asm volatile("{\n\t.reg .pred p;\n\t"
+                 "setp.ne.b32 p, %4, 0;\n\t"
+                 "tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+                 ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
+}
+// Arrives at the barrier of this address in both SMs once the MMAs issued so far are complete.
+__device__ __forceinline__ void pair_commit(uint32_t bar)
+{
+    asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(bar), "h"((uint16_t)3) : "memory");
+}
+__device__ __forceinline__ void pair_load_2d(uint32_t dst, const CUtensorMap* map, int x, int y, uint32_t bar)
+{
+    asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes.cta_group::2 [%0], [%1, {%2, %3}], [%4];"
+                 ::"r"(dst), "l"((uint64_t)map), "r"(x), "r"(y), "r"(bar) : "memory");
+}
+__device__ __forceinline__ void pair_load_3d(uint32_t dst, const CUtensorMap* map, int x, int y, int z, uint32_t bar)
+{
+    asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes.cta_group::2 [%0], [%1, {%2, %3, %4}], [%5];"
+                 ::"r"(dst), "l"((uint64_t)map), "r"(x), "r"(y), "r"(z), "r"(bar) : "memory");
+}
+// 16 bytes of which `bytes` are read and the rest are zeros.
+__device__ __forceinline__ void copy_16(uint32_t dst, const void* src, int bytes)
+{
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
+}
+
+// 64 places from p0 on, up to `stop`, by 128 columns from column0 on: two boxes of 64 columns, rows along K.
+__device__ __forceinline__ void copy_places(const Operand& o, const int32_t* row, int p0, int stop, int column0, uint32_t dst, int thread)
+{
+    const int c = thread & 7;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int r = (thread >> 3) + 16 * i;
+        const int64_t from = p0 + r < stop ? row_of(o, row, p0 + r) : -1;
+#pragma unroll
+        for (int box = 0; box < 2; ++box) {
+            const int col = column0 + box * 64 + c * 8;
+            const int many = from < 0 ? 0 : max(0, min(8, o.columns - col));
+            copy_16(dst + (uint32_t)(box * 8192 + r * kRow + ((c ^ (r & 7)) << 4)), many ? o.p + from * o.ld + col : o.p, many * 2);
+        }
+    }
+}
+
+template <int MODE, int COPIES>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(COPIES ? 512 : 384, 1)
+k_expert_pair(const __grid_constant__ Product q)
+{
+    using S = Pair;
+    constexpr bool A_K = MODE != kWeights, B_K = MODE == kRowsTimesTurned;
+    extern __shared__ unsigned char raw[];
+    unsigned char* smem = (unsigned char*)(((uintptr_t)raw + 1023) & ~(uintptr_t)1023);
+    const uint32_t stages = smem_u32(smem);
+    unsigned char* staging = smem + S::STAGES * S::STAGE;
+    int32_t* first = reinterpret_cast<int32_t*>(staging + S::STAGING);
+    int32_t* tile0 = first + GEM_NLR_MAX_EXPERTS + 2;
+    uint64_t* bars = reinterpret_cast<uint64_t*>(staging + S::STAGING + S::TABLES);
+    volatile uint32_t* dead = reinterpret_cast<uint32_t*>(bars + S::BARRIERS);
+    volatile uint32_t* tmem_at = dead + 1;
+    const uint32_t bar0 = smem_u32(bars);
+    const auto full = [&](int s) { return bar0 + 8u * s; };                               // the first SM's count
+    const auto free_ = [&](int s) { return bar0 + 8u * (S::STAGES + s); };                // each SM's own
+    const auto landed = [&](int s) { return bar0 + 8u * (2 * S::STAGES + s); };           // copies; the first SM's counts the second's too
+    const auto acc_full = [&](int a) { return bar0 + 8u * (3 * S::STAGES + a); };         // each SM's own
+    const auto acc_free = [&](int a) { return bar0 + 8u * (3 * S::STAGES + 2 + a); };     // the first SM's count
+    const auto go = [&](int s) { return bar0 + 8u * (3 * S::STAGES + 4 + s); };           // COPIES 1: the stage is free for a cut chunk
+    const uint32_t drained = bar0 + 8u * (4 * S::STAGES + 4);
+
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int rank = (int)pair_rank();
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < S::STAGES; ++s) {
+            mbar_init(full(s), COPIES == 2 ? 2 : 1);
+            mbar_init(free_(s), 1);
+            mbar_init(landed(s), kLoaders + (rank == 0));
+            mbar_init(go(s), 1);
+        }
+        for (int a = 0; a < 2; ++a) {
+            mbar_init(acc_full(a), 1);
+            mbar_init(acc_free(a), 16);
+        }
+        mbar_init(drained, 1);
+        *dead = 0;
+        fence_barrier_init();
+    }
+    if (warp == 2) {
+        asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32((const void*)tmem_at)), "r"(512u) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+    }
+    if (warp == 3) make_tables<2 * kTileM>(q, first, tile0, lane);
+    tc_fence_before();
+    __syncthreads();
+    pair_barrier();
+    tc_fence_after();
+    const uint32_t tmem = *tmem_at;
+
+    const int nt = (q.n + kPairN - 1) / kPairN;
+    const int tiles = (MODE == kWeights ? q.experts * ((q.m + 2 * kTileM - 1) / (2 * kTileM)) : tile0[q.experts + 1]) * nt;
+    const int pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
+    const auto tile = [&](int t) { return tile_at<MODE, kPairN, 2 * kTileM>(q, first, tile0, t); };
+    // Chunks are counted through all tiles: chunk g is in stage g mod STAGES, for the (g / STAGES)-th time.
+    const auto stage_of = [](uint32_t g) { return (int)(g % S::STAGES); };
+    const auto round_of = [](uint32_t g) { return g / S::STAGES; };
+
+    if (warp == 0) {
+        if (one_thread()) {
+            int s = 0;
+            uint32_t parity = 1, g = 0;
+            bool on = true;
+            for (int t = pair; t < tiles && on; t += pairs) {
+                const Tile w = tile(t);
+                const int chunks = (w.k + kChunk - 1) / kChunk;
+                const int a_row = w.c_row + rank * kTileM, b_col = w.n0 + rank * kTileM;
+                for (int c = 0; c < chunks; ++c) {
+                    on = pair_wait(free_(s), parity, dead);
+                    if (!on) break;
+                    const uint32_t a = stages + (uint32_t)s * S::STAGE, b = a + S::A, bar = of_first(full(s));
+                    const bool cut = MODE == kWeights && w.k - c * kChunk < kChunk;          // copied
+                    const bool box_a = !cut && !(COPIES == 2 && q.a.gather), box_b = !cut && !(COPIES == 2 && q.b.gather);
+                    if (rank == 0) {
+                        const uint32_t bytes = 2u * ((box_a ? S::A : 0) + (box_b ? S::B : 0));
+                        if (bytes) mbar_expect_tx(full(s), bytes);
+                        else if (COPIES == 2) mbar_arrive(full(s));
+                    }
+                    if (COPIES == 1 && cut) mbar_arrive(go(s));
+                    const int p0 = w.k_first + c * kChunk;                                   // weights: the chunk's first place
+                    if (box_a) {
+                        if (A_K) {
+                            pair_load_2d(a, &q.ta, c * kChunk, a_row, bar);
+                        } else {
+                            pair_load_2d(a, &q.ta, a_row, p0, bar);
+                            pair_load_2d(a + 8192, &q.ta, a_row + 64, p0, bar);
+                        }
+                    }
+                    if (box_b) {
+                        if (MODE == kRowsTimesTurned) {
+                            pair_load_3d(b, &q.tb, c * kChunk, b_col, w.expert, bar);
+                        } else if (MODE == kRowsTimesPlain) {
+                            pair_load_3d(b, &q.tb, b_col, c * kChunk, w.expert, bar);
+                            pair_load_3d(b + 8192, &q.tb, b_col + 64, c * kChunk, w.expert, bar);
+                        } else {
+                            pair_load_2d(b, &q.tb, b_col, p0, bar);
+                            pair_load_2d(b + 8192, &q.tb, b_col + 64, p0, bar);
+                        }
+                    }
+                    ++g;
+                    if (++s == S::STAGES) { s = 0; parity ^= 1u; }
+                }
+            }
+            if (!on && rank == 0) {
+                // copies on their way land before the block ends
+                uint32_t none = 0;
+                for (uint32_t i = g > S::STAGES ? g - S::STAGES : 0; i < g; ++i) pair_wait(full(stage_of(i)), round_of(i) & 1u, &none, kSpinLimit);
+            }
+        }
+    } else if (warp == 1 && rank == 0) {
+        if (one_thread()) {
+            const uint64_t da0 = A_K ? umma_desc_sw128(stages, 16, 1024) : umma_desc_sw128(stages, 8192, 1024);
+            const uint64_t db0 = B_K ? umma_desc_sw128(stages + S::A, 16, 1024) : umma_desc_sw128(stages + S::A, 8192, 1024);
+            int s = 0;
+            uint32_t parity = 0, i = 0;
+            bool on = true;
+            for (int t = pair; t < tiles && on; t += pairs) {
+                const int k = tile(t).k;
+                if (k == 0) continue;
+                const uint32_t acc = tmem + (i & 1u) * kPairN;
+                on = pair_wait(acc_free(i & 1), ((i >> 1) + 1) & 1, dead);
+                for (int left = k; left > 0 && on; left -= kChunk) {
+                    on = pair_wait(full(s), parity, dead);
+                    if (!on) break;
+                    tc_fence_after();
+                    const uint64_t da = da0 + (uint64_t)(uint32_t)(s * (S::STAGE >> 4)), db = db0 + (uint64_t)(uint32_t)(s * (S::STAGE >> 4));
+#pragma unroll
+                    for (int x = 0; x < 4; ++x)
+                        if (x == 0 || x * 16 < left)
+                            pair_mma(acc, da + (uint64_t)(x * (A_K ? 2 : 128)), db + (uint64_t)(x * (B_K ? 2 : 128)), q.idesc, x || left < k);
+                    pair_commit(free_(s));
+                    if (++s == S::STAGES) { s = 0; parity ^= 1u; }
+                }
+                if (on) pair_commit(acc_full(i & 1));
+                ++i;
+            }
+            if (!on) {
+                uint32_t none = 0;
+                pair_commit(drained);
+                pair_wait(drained, 0, &none, kSpinLimit);
+            }
+        }
+    } else if (COPIES && warp == 3) {
+        if (one_thread()) {
+            uint32_t g = 0, parity = 0;                    // a bit a stage
+            bool on = true;
+            for (int t = pair; t < tiles && on; t += pairs) {
+                const Tile w = tile(t);
+                const uint32_t chunks = (uint32_t)(w.k + kChunk - 1) / kChunk;
+                uint32_t c = COPIES == 2 || chunks == 0 ? 0 : w.k % kChunk ? chunks - 1 : chunks;
+                for (; c < chunks && on; ++c) {
+                    const int s = stage_of(g + c);
+                    on = pair_wait(landed(s), parity >> s & 1u, dead);
+                    if (!on) break;
+                    parity ^= 1u << s;
+                    fence_proxy_async();
+                    if (rank == 0) mbar_arrive(full(s));
+                    else arrive_at(of_first(landed(s)));
+                }
+                g += chunks;
+            }
+        }
+    } else if (warp >= 4 && warp < 12) {
+        const int quarter = warp & 3, half = (warp - 4) >> 2;
+        const uint32_t mine = smem_u32(staging) + (uint32_t)(warp - 4) * 2048u;
+        uint32_t i = 0;
+        bool on = true;
+        for (int t = pair; t < tiles; t += pairs) {
+            const Tile w = tile(t);
+            if (w.k && on) {
+                on = wait_for(acc_full(i & 1), (i >> 1) & 1, dead);
+                on = __all_sync(0xffffffffu, on);
+                tc_fence_after();
+            }
+            store_tile<MODE>(q, w, w.c_row + rank * kTileM + quarter * 32, w.n0 + half * 128, 4,
+                             tmem + ((uint32_t)(quarter * 32) << 16) + (i & 1u) * kPairN + (uint32_t)(half * 128), mine, lane, on);
+            if (w.k) {
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0 && on) arrive_at(of_first(acc_free(i & 1)));
+                ++i;
+            }
+        }
+    } else if (COPIES && warp >= 12) {
+        const int thread = threadIdx.x - 384;
+        uint32_t g = 0, parity = 0;                        // (a bit a stage)
+        bool on = true;
+        for (int t = pair; t < tiles && on; t += pairs) {
+            const Tile w = tile(t);
+            const int chunks = (w.k + kChunk - 1) / kChunk;
+            const int a_row = w.c_row + rank * kTileM, b_col = w.n0 + rank * kTileM;
+            const uint16_t* from[8];                        // rows: this thread's eight rows of A
+            if (A_K && chunks) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const int p = a_row + (thread >> 3) + 16 * i;
+                    const int64_t r = p < w.stop ? row_of(q.a, q.row, p) : -1;
+                    from[i] = r < 0 ? nullptr : q.a.p + r * q.a.ld;
+                }
+            }
+            int c = COPIES == 2 || chunks == 0 ? 0 : w.k % kChunk ? chunks - 1 : chunks;
+            for (; c < chunks; ++c) {
+                const int s = stage_of(g + c);
+                // A stage's rounds differ by their parity alone.  Where every chunk waits for these threads they are never a
+                // round ahead or behind; where only cut chunks do they could be, and are told of each by warp 0.
+                if (COPIES == 2) on = wait_for(free_(s), (round_of(g + c) & 1u) ^ 1u, dead);
+                else on = wait_for(go(s), parity >> s & 1u, dead);
+                if (!on) break;
+                parity ^= 1u << s;
+                const uint32_t a = stages + (uint32_t)s * S::STAGE, b = a + S::A;
+                if (A_K) {
+                    const int col = c * kChunk + (thread & 7) * 8;
+                    const int many = max(0, min(8, q.a.columns - col));
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        const int r = (thread >> 3) + 16 * i;
+                        const bool there = from[i] && many;
+                        copy_16(a + (uint32_t)(r * kRow + (((thread & 7) ^ (r & 7)) << 4)), there ? from[i] + col : q.a.p, there ? many * 2 : 0);
+                    }
+                } else {
+                    const bool cut = w.k - c * kChunk < kChunk;
+                    const int p0 = w.k_first + c * kChunk, end = w.k_first + w.k;
+                    if (cut || q.a.gather) copy_places(q.a, q.row, p0, end, a_row, a, thread);
+                    if (cut || q.b.gather) copy_places(q.b, q.row, p0, end, b_col, b, thread);
+                }
+                asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(landed(s)) : "memory");
+            }
+            g += (uint32_t)chunks;
+        }
+        asm volatile("cp.async.wait_all;" ::: "memory");
+    }
+    tc_fence_before();
+    __syncthreads();
+    pair_barrier();
+    if (warp == 2) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512u));
 }
 
 PFN_cuTensorMapEncodeTiled_v12000 encoder()
@@ -523,6 +883,19 @@ int prepare(Product& q, int64_t tiles, bool bf16, cudaStream_t st)
     return launch<MODE, BN, false>(q, tiles, st);
 }
 
+template <int MODE, int COPIES>
+int launch_pair(const Product& q, int64_t tiles, cudaStream_t st)
+{
+    constexpr auto kern = k_expert_pair<MODE, COPIES>;
+    static_assert(Pair::SHARED <= 232448, "shared memory of a block");
+    if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, Pair::SHARED) != cudaSuccess) {
+        cudaGetLastError();
+        return GEM_NLR_E_CUDA;
+    }
+    kern<<<2 * (unsigned)(tiles < kTrainSMs / 2 ? tiles : kTrainSMs / 2), COPIES ? 512 : 384, Pair::SHARED, st>>>(q);
+    return launched();
+}
+
 // The widest tile that gives every SM one: a narrower one reads its rows (or the left operand) more often.
 template <int MODE>
 int run(Product& q, bool bf16, cudaStream_t st)
@@ -534,6 +907,17 @@ int run(Product& q, bool bf16, cudaStream_t st)
     const auto idesc = [&](int bn) {
         return umma_idesc_f16(kTileM, bn, MODE == kWeights, MODE != kRowsTimesTurned) | (bf16 ? 1u << 7 | 1u << 10 : 0u);
     };
+    const int64_t tall_tiles = (MODE == kWeights ? (int64_t)q.experts * ((q.m + 255) / 256) : q.places / 256 + (q.places < q.experts + 1 ? q.places : q.experts + 1)) *
+                               ((q.n + kPairN - 1) / kPairN);
+    if (q.a.wide && q.b.wide && (MODE == kWeights ? q.m : q.places / q.experts) >= 256 && tall_tiles >= kTrainSMs / 2) {
+        constexpr bool A_K = MODE != kWeights, B_K = MODE == kRowsTimesTurned;
+        q.idesc = idesc(256) & ~(31u << 24) | (uint32_t)(2 * kTileM >> 4) << 24;
+        if ((q.a.gather || encode(&q.ta, q.a, 0, A_K ? kTileM : kChunk, bf16)) &&
+            (q.b.gather || encode(&q.tb, q.b, MODE == kWeights ? 0 : q.experts, B_K ? kTileM : kChunk, bf16))) {
+            if (q.a.gather || q.b.gather) return launch_pair<MODE, 2>(q, tall_tiles, st);
+            return launch_pair<MODE, MODE == kWeights ? 1 : 0>(q, tall_tiles, st);
+        }
+    }
     if (tiles(256) >= kTrainSMs) {
         q.idesc = idesc(256);
         return prepare<MODE, 256>(q, tiles(256), bf16, st);
@@ -559,11 +943,12 @@ Operand weights_of(const void* p, int64_t ld, int64_t stride, int experts, int r
     return {(const uint16_t*)p, ld, stride, rows, columns, 0, on_16(p, ld) && ld > 0 && stride % 8 == 0 && stride > 0};
 }
 
+constexpr int64_t kMaxPlaces = INT32_MAX - (1 << 16);            // int arithmetic on places, tiles included, stays far from its end
 bool half_type(int32_t type) { return type == GEM_NLR_F16 || type == GEM_NLR_BF16; }
 bool halves(const void* p) { return p && aligned_to(p, 2); }
 bool sizes_fine(int32_t type, int64_t x_rows, int64_t places, int32_t experts, int32_t d_in, int32_t d_out, int32_t turned, const int32_t* row)
 {
-    return half_type(type) && x_rows >= 0 && x_rows <= INT32_MAX && places >= 0 && places <= INT32_MAX && experts >= 1 && experts <= GEM_NLR_MAX_EXPERTS && d_in >= 1 &&
+    return half_type(type) && x_rows >= 0 && x_rows <= INT32_MAX && places >= 0 && places <= kMaxPlaces && experts >= 1 && experts <= GEM_NLR_MAX_EXPERTS && d_in >= 1 &&
            d_in <= kMaxColumns && d_out >= 1 && d_out <= kMaxColumns && (turned == 0 || turned == 1) && aligned_to(row, 4) && (row || x_rows >= places);
 }
 

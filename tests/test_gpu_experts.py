@@ -100,6 +100,14 @@ def test_many_tiles(places, experts, d_in, d_out, turned):
     check(places, experts, d_in, d_out, BF16, turned, gather=places // 2, uneven=True)
 
 
+@pytest.mark.parametrize("dtype", [F16, BF16], ids=name)
+@pytest.mark.parametrize("gather", [0, 1500], ids=["as they are", "gathered"])
+@pytest.mark.parametrize("turned", [False, True], ids=["plain", "turned"])
+@pytest.mark.parametrize("places,experts,d_in,d_out", [(6000, 6, 520, 1160), (9000, 16, 768, 328), (4097, 2, 1544, 2056)])
+def test_large_tiles(places, experts, d_in, d_out, turned, gather, dtype):
+    check(places, experts, d_in, d_out, dtype, turned, gather, uneven=True, seed=places + turned)
+
+
 @pytest.mark.parametrize("d_in", [64, 65])
 def test_wild_offsets(d_in):
     for o in ([0, 0, 0, 0], [0, 100, 100, 100], [5, 20, 60, 90], [0, 50, 30, 100], [-7, 40, 400, 100], [100, 100, 100, 100], [0, 1, 2, 3]):
