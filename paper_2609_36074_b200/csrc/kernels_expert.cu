@@ -50,7 +50,8 @@ struct Operand {
 };
 
 struct Product {
-    CUtensorMap ta, tb;
+    CUtensorMap ta, tb;       // boxes of rows
+    CUtensorMap ra, rb;       // two SMs: single rows, for loads by index
     Operand a, b;
     const int32_t* offset;
     const int32_t* row;
@@ -489,20 +490,18 @@ k_expert(const __grid_constant__ Product q)
 // columns of B, the MMA reads both SMs' shared memory, and each keeps 128 rows of accumulators.  The first SM issues the MMAs for
 // both; the second's loads and epilogue signal the first's barriers.
 //
-//   warp 0         TMA loads, each SM its own
+//   warps 0, 2      TMA loads of A and of B, each SM its own
 //   warp 1         (first SM) issues the MMAs
 //   warps 4-11     epilogue: a quarter of the rows and a half of the columns each
-//   warps 12-15    load what TMA boxes cannot: rows gathered by index, and an expert's last, cut rows where they are the K dimension
-//                  (16-byte asynchronous copies, zeros where nothing is)
-//   warp 3         waits for these copies, makes them visible to the tensor cores and signals
-// COPIES: 0 none, 1 the cut rows alone, 2 gathered rows too.
+//   warps 12-15    (GATHER) rows that are named by index, four at a time: a box cannot; one thread each
+// An expert's last, cut rows where they are the K dimension are loaded by warps 0 and 2 in the same way, rows behind the last as zeros.
 
 constexpr int kPairN = 256;
 struct Pair {
     static constexpr int A = kTileM * kRow, B = kTileM * kRow, STAGE = A + B;
     static constexpr int STAGES = 6;
     static constexpr int STAGING = 8 * 2048;
-    static constexpr int BARRIERS = 4 * STAGES + 5;
+    static constexpr int BARRIERS = 2 * STAGES + 5;
     static constexpr int TABLES = (2 * GEM_NLR_MAX_EXPERTS + 4) * 4;
     static constexpr int SHARED = 1024 + STAGES * STAGE + STAGING + TABLES + BARRIERS * 8 + 16;
 };
@@ -573,31 +572,22 @@ __device__ __forceinline__ void pair_load_3d(uint32_t dst, const CUtensorMap* ma
     asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes.cta_group::2 [%0], [%1, {%2, %3, %4}], [%5];"
                  ::"r"(dst), "l"((uint64_t)map), "r"(x), "r"(y), "r"(z), "r"(bar) : "memory");
 }
-// 16 bytes of which `bytes` are read and the rest are zeros.
-__device__ __forceinline__ void copy_16(uint32_t dst, const void* src, int bytes)
+__device__ __forceinline__ void pair_load_rows(uint32_t dst, const CUtensorMap* map, int x, int4 y, uint32_t bar)
 {
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
+    asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.tile::gather4.mbarrier::complete_tx::bytes.cta_group::2 [%0], [%1, {%2, %3, %4, %5, %6}], [%7];"
+                 ::"r"(dst), "l"((uint64_t)map), "r"(x), "r"(y.x), "r"(y.y), "r"(y.z), "r"(y.w), "r"(bar) : "memory");
 }
 
-// 64 places from p0 on, up to `stop`, by 128 columns from column0 on: two boxes of 64 columns, rows along K.
-__device__ __forceinline__ void copy_places(const Operand& o, const int32_t* row, int p0, int stop, int column0, uint32_t dst, int thread)
+// The rows of places p to p + 3 of an operand, in the form that a load of rows takes: for none, the one behind the last.
+__device__ __forceinline__ int4 rows_at(const Operand& o, const int32_t* row, int p, int stop)
 {
-    const int c = thread & 7;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const int r = (thread >> 3) + 16 * i;
-        const int64_t from = p0 + r < stop ? row_of(o, row, p0 + r) : -1;
-#pragma unroll
-        for (int box = 0; box < 2; ++box) {
-            const int col = column0 + box * 64 + c * 8;
-            const int many = from < 0 ? 0 : max(0, min(8, o.columns - col));
-            copy_16(dst + (uint32_t)(box * 8192 + r * kRow + ((c ^ (r & 7)) << 4)), many ? o.p + from * o.ld + col : o.p, many * 2);
-        }
-    }
+    if (o.gather) return four_rows(row, p, stop, o.rows);
+    const int none = (int)o.rows;
+    return make_int4(p < stop ? p : none, p + 1 < stop ? p + 1 : none, p + 2 < stop ? p + 2 : none, p + 3 < stop ? p + 3 : none);
 }
 
-template <int MODE, int COPIES>
-__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(COPIES ? 512 : 384, 1)
+template <int MODE, bool GATHER>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(GATHER ? 512 : 384, 1)
 k_expert_pair(const __grid_constant__ Product q)
 {
     using S = Pair;
@@ -614,20 +604,16 @@ k_expert_pair(const __grid_constant__ Product q)
     const uint32_t bar0 = smem_u32(bars);
     const auto full = [&](int s) { return bar0 + 8u * s; };                               // the first SM's count
     const auto free_ = [&](int s) { return bar0 + 8u * (S::STAGES + s); };                // each SM's own
-    const auto landed = [&](int s) { return bar0 + 8u * (2 * S::STAGES + s); };           // copies; the first SM's counts the second's too
-    const auto acc_full = [&](int a) { return bar0 + 8u * (3 * S::STAGES + a); };         // each SM's own
-    const auto acc_free = [&](int a) { return bar0 + 8u * (3 * S::STAGES + 2 + a); };     // the first SM's count
-    const auto go = [&](int s) { return bar0 + 8u * (3 * S::STAGES + 4 + s); };           // COPIES 1: the stage is free for a cut chunk
-    const uint32_t drained = bar0 + 8u * (4 * S::STAGES + 4);
+    const auto acc_full = [&](int a) { return bar0 + 8u * (2 * S::STAGES + a); };         // each SM's own
+    const auto acc_free = [&](int a) { return bar0 + 8u * (2 * S::STAGES + 2 + a); };     // the first SM's count
+    const uint32_t drained = bar0 + 8u * (2 * S::STAGES + 4);
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int rank = (int)pair_rank();
     if (threadIdx.x == 0) {
         for (int s = 0; s < S::STAGES; ++s) {
-            mbar_init(full(s), COPIES == 2 ? 2 : 1);
+            mbar_init(full(s), 1);
             mbar_init(free_(s), 1);
-            mbar_init(landed(s), kLoaders + (rank == 0));
-            mbar_init(go(s), 1);
         }
         for (int a = 0; a < 2; ++a) {
             mbar_init(acc_full(a), 1);
@@ -652,59 +638,59 @@ k_expert_pair(const __grid_constant__ Product q)
     const int tiles = (MODE == kWeights ? q.experts * ((q.m + 2 * kTileM - 1) / (2 * kTileM)) : tile0[q.experts + 1]) * nt;
     const int pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
     const auto tile = [&](int t) { return tile_at<MODE, kPairN, 2 * kTileM>(q, first, tile0, t); };
-    // Chunks are counted through all tiles: chunk g is in stage g mod STAGES, for the (g / STAGES)-th time.
-    const auto stage_of = [](uint32_t g) { return (int)(g % S::STAGES); };
-    const auto round_of = [](uint32_t g) { return g / S::STAGES; };
-
-    if (warp == 0) {
+    if (warp == 0 || warp == 2) {
         if (one_thread()) {
+            const bool left_one = warp == 0;                // A; the other warp loads B
+            const Operand& o = left_one ? q.a : q.b;
+            const CUtensorMap* by_index = left_one ? &q.ra : &q.rb;
+            const bool others = GATHER && o.gather;         // warps 12 to 15 load it
             int s = 0;
             uint32_t parity = 1, g = 0;
             bool on = true;
             for (int t = pair; t < tiles && on; t += pairs) {
                 const Tile w = tile(t);
-                const int chunks = (w.k + kChunk - 1) / kChunk;
                 const int a_row = w.c_row + rank * kTileM, b_col = w.n0 + rank * kTileM;
-                for (int c = 0; c < chunks; ++c) {
+                const int x = left_one ? a_row : b_col;     // weights: the operand's first column
+                int p0 = w.k_first;                         // weights: the chunk's first place
+                for (int k = 0; k < w.k; k += kChunk, p0 += kChunk) {
                     on = pair_wait(free_(s), parity, dead);
                     if (!on) break;
-                    const uint32_t a = stages + (uint32_t)s * S::STAGE, b = a + S::A, bar = of_first(full(s));
-                    const bool cut = MODE == kWeights && w.k - c * kChunk < kChunk;          // copied
-                    const bool box_a = !cut && !(COPIES == 2 && q.a.gather), box_b = !cut && !(COPIES == 2 && q.b.gather);
-                    if (rank == 0) {
-                        const uint32_t bytes = 2u * ((box_a ? S::A : 0) + (box_b ? S::B : 0));
-                        if (bytes) mbar_expect_tx(full(s), bytes);
-                        else if (COPIES == 2) mbar_arrive(full(s));
-                    }
-                    if (COPIES == 1 && cut) mbar_arrive(go(s));
-                    const int p0 = w.k_first + c * kChunk;                                   // weights: the chunk's first place
-                    if (box_a) {
-                        if (A_K) {
-                            pair_load_2d(a, &q.ta, c * kChunk, a_row, bar);
-                        } else {
-                            pair_load_2d(a, &q.ta, a_row, p0, bar);
-                            pair_load_2d(a + 8192, &q.ta, a_row + 64, p0, bar);
-                        }
-                    }
-                    if (box_b) {
-                        if (MODE == kRowsTimesTurned) {
-                            pair_load_3d(b, &q.tb, c * kChunk, b_col, w.expert, bar);
-                        } else if (MODE == kRowsTimesPlain) {
-                            pair_load_3d(b, &q.tb, b_col, c * kChunk, w.expert, bar);
-                            pair_load_3d(b + 8192, &q.tb, b_col + 64, c * kChunk, w.expert, bar);
-                        } else {
-                            pair_load_2d(b, &q.tb, b_col, p0, bar);
-                            pair_load_2d(b + 8192, &q.tb, b_col + 64, p0, bar);
+                    const uint32_t to = stages + (uint32_t)s * S::STAGE + (left_one ? 0 : S::A), bar = of_first(full(s));
+                    if (MODE == kWeights && w.k - k < kChunk) {
+                        // 16 rows an MMA; what is behind those stays
+                        const int quads = (w.k - k + 15) / 16 * 4, end = w.k_first + w.k;
+                        if (left_one && rank == 0) mbar_expect_tx(full(s), 8 * 512 * quads);
+                        if (!others)
+#pragma unroll 4
+                            for (int i = 0; i < quads; ++i) {
+                                const int4 named = rows_at(o, q.row, p0 + 4 * i, end);
+                                pair_load_rows(to + i * 512, by_index, x, named, bar);
+                                pair_load_rows(to + 8192 + i * 512, by_index, x + 64, named, bar);
+                            }
+                    } else {
+                        if (left_one && rank == 0) mbar_expect_tx(full(s), 2 * S::STAGE);
+                        if (!others) {
+                            if (MODE == kWeights) {
+                                pair_load_2d(to, left_one ? &q.ta : &q.tb, x, p0, bar);
+                                pair_load_2d(to + 8192, left_one ? &q.ta : &q.tb, x + 64, p0, bar);
+                            } else if (left_one) {
+                                pair_load_2d(to, &q.ta, k, a_row, bar);
+                            } else if (MODE == kRowsTimesTurned) {
+                                pair_load_3d(to, &q.tb, k, b_col, w.expert, bar);
+                            } else {
+                                pair_load_3d(to, &q.tb, b_col, k, w.expert, bar);
+                                pair_load_3d(to + 8192, &q.tb, b_col + 64, k, w.expert, bar);
+                            }
                         }
                     }
                     ++g;
                     if (++s == S::STAGES) { s = 0; parity ^= 1u; }
                 }
             }
-            if (!on && rank == 0) {
+            if (!on && rank == 0 && left_one) {
                 // copies on their way land before the block ends
                 uint32_t none = 0;
-                for (uint32_t i = g > S::STAGES ? g - S::STAGES : 0; i < g; ++i) pair_wait(full(stage_of(i)), round_of(i) & 1u, &none, kSpinLimit);
+                for (uint32_t i = g > S::STAGES ? g - S::STAGES : 0; i < g; ++i) pair_wait(full((int)(i % S::STAGES)), i / S::STAGES & 1u, &none, kSpinLimit);
             }
         }
     } else if (warp == 1 && rank == 0) {
@@ -740,26 +726,6 @@ k_expert_pair(const __grid_constant__ Product q)
                 pair_wait(drained, 0, &none, kSpinLimit);
             }
         }
-    } else if (COPIES && warp == 3) {
-        if (one_thread()) {
-            uint32_t g = 0, parity = 0;                    // a bit a stage
-            bool on = true;
-            for (int t = pair; t < tiles && on; t += pairs) {
-                const Tile w = tile(t);
-                const uint32_t chunks = (uint32_t)(w.k + kChunk - 1) / kChunk;
-                uint32_t c = COPIES == 2 || chunks == 0 ? 0 : w.k % kChunk ? chunks - 1 : chunks;
-                for (; c < chunks && on; ++c) {
-                    const int s = stage_of(g + c);
-                    on = pair_wait(landed(s), parity >> s & 1u, dead);
-                    if (!on) break;
-                    parity ^= 1u << s;
-                    fence_proxy_async();
-                    if (rank == 0) mbar_arrive(full(s));
-                    else arrive_at(of_first(landed(s)));
-                }
-                g += chunks;
-            }
-        }
     } else if (warp >= 4 && warp < 12) {
         const int quarter = warp & 3, half = (warp - 4) >> 2;
         const uint32_t mine = smem_u32(staging) + (uint32_t)(warp - 4) * 2048u;
@@ -781,53 +747,69 @@ k_expert_pair(const __grid_constant__ Product q)
                 ++i;
             }
         }
-    } else if (COPIES && warp >= 12) {
-        const int thread = threadIdx.x - 384;
-        uint32_t g = 0, parity = 0;                        // (a bit a stage)
+    } else if (GATHER && warp >= 12) {
+        const int part = warp - 12;
+        int s = 0;
+        uint32_t parity = 1;
         bool on = true;
         for (int t = pair; t < tiles && on; t += pairs) {
             const Tile w = tile(t);
-            const int chunks = (w.k + kChunk - 1) / kChunk;
             const int a_row = w.c_row + rank * kTileM, b_col = w.n0 + rank * kTileM;
-            const uint16_t* from[8];                        // rows: this thread's eight rows of A
-            if (A_K && chunks) {
+            if (A_K) {
+                if (one_thread()) {
+                    int4 named[8];                          // a quarter of A's rows
+                    if (w.k)
 #pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const int p = a_row + (thread >> 3) + 16 * i;
-                    const int64_t r = p < w.stop ? row_of(q.a, q.row, p) : -1;
-                    from[i] = r < 0 ? nullptr : q.a.p + r * q.a.ld;
-                }
-            }
-            int c = COPIES == 2 || chunks == 0 ? 0 : w.k % kChunk ? chunks - 1 : chunks;
-            for (; c < chunks; ++c) {
-                const int s = stage_of(g + c);
-                // A stage's rounds differ by their parity alone.  Where every chunk waits for these threads they are never a
-                // round ahead or behind; where only cut chunks do they could be, and are told of each by warp 0.
-                if (COPIES == 2) on = wait_for(free_(s), (round_of(g + c) & 1u) ^ 1u, dead);
-                else on = wait_for(go(s), parity >> s & 1u, dead);
-                if (!on) break;
-                parity ^= 1u << s;
-                const uint32_t a = stages + (uint32_t)s * S::STAGE, b = a + S::A;
-                if (A_K) {
-                    const int col = c * kChunk + (thread & 7) * 8;
-                    const int many = max(0, min(8, q.a.columns - col));
+                        for (int i = 0; i < 8; ++i) named[i] = rows_at(q.a, q.row, a_row + 32 * part + 4 * i, w.stop);
+                    for (int k = 0; k < w.k; k += kChunk) {
+                        on = pair_wait(free_(s), parity, dead);
+                        if (!on) break;
+                        const uint32_t to = stages + (uint32_t)s * S::STAGE + (uint32_t)(32 * part * kRow), bar = of_first(full(s));
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        const int r = (thread >> 3) + 16 * i;
-                        const bool there = from[i] && many;
-                        copy_16(a + (uint32_t)(r * kRow + (((thread & 7) ^ (r & 7)) << 4)), there ? from[i] + col : q.a.p, there ? many * 2 : 0);
+                        for (int i = 0; i < 8; ++i) pair_load_rows(to + (uint32_t)(4 * i * kRow), &q.ra, k, named[i], bar);
+                        if (++s == S::STAGES) { s = 0; parity ^= 1u; }
                     }
-                } else {
-                    const bool cut = w.k - c * kChunk < kChunk;
-                    const int p0 = w.k_first + c * kChunk, end = w.k_first + w.k;
-                    if (cut || q.a.gather) copy_places(q.a, q.row, p0, end, a_row, a, thread);
-                    if (cut || q.b.gather) copy_places(q.b, q.row, p0, end, b_col, b, thread);
                 }
-                asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(landed(s)) : "memory");
+                on = __all_sync(0xffffffffu, on);
+            } else {
+                // A quarter of a chunk's places: lane i has the i-th's row, read four chunks ahead.
+                constexpr int AHEAD = 4;
+                const Operand& o = q.a.gather ? q.a : q.b;
+                const CUtensorMap* map = q.a.gather ? &q.ra : &q.rb;
+                const int x = q.a.gather ? a_row : b_col, end = w.k_first + w.k, mine = w.k_first + 16 * part + (lane & 15);
+                int ahead[AHEAD];
+#pragma unroll
+                for (int u = 0; u < AHEAD; ++u) ahead[u] = mine + u * kChunk < end ? __ldg(q.row + mine + u * kChunk) : -1;
+                for (int k0 = 0; k0 < w.k && on; k0 += AHEAD * kChunk) {
+#pragma unroll
+                    for (int u = 0; u < AHEAD; ++u) {
+                        const int k = k0 + u * kChunk;
+                        if (k >= w.k || !on) break;
+                        on = pair_wait(free_(s), parity, dead);
+                        on = __all_sync(0xffffffffu, on);
+                        if (!on) break;
+                        const int r = (uint32_t)ahead[u] < (uint32_t)o.rows ? ahead[u] : (int)o.rows;
+                        const int next = mine + k + AHEAD * kChunk;
+                        ahead[u] = next < end ? __ldg(q.row + next) : -1;
+                        int4 named[4];
+#pragma unroll
+                        for (int i = 0; i < 4; ++i)
+                            named[i] = make_int4(__shfl_sync(0xffffffffu, r, 4 * i), __shfl_sync(0xffffffffu, r, 4 * i + 1), __shfl_sync(0xffffffffu, r, 4 * i + 2),
+                                                 __shfl_sync(0xffffffffu, r, 4 * i + 3));
+                        if (one_thread() && 16 * part < w.k - k) {          // (a cut chunk has only the rows that an MMA takes)
+                            const uint32_t to = stages + (uint32_t)s * S::STAGE + (q.a.gather ? 0 : S::A) + (uint32_t)(16 * part * kRow), bar = of_first(full(s));
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) {
+                                pair_load_rows(to + (uint32_t)(i * 512), map, x, named[i], bar);
+                                pair_load_rows(to + (uint32_t)(8192 + i * 512), map, x + 64, named[i], bar);
+                            }
+                        }
+                        __syncwarp();
+                        if (++s == S::STAGES) { s = 0; parity ^= 1u; }
+                    }
+                }
             }
-            g += (uint32_t)chunks;
         }
-        asm volatile("cp.async.wait_all;" ::: "memory");
     }
     tc_fence_before();
     __syncthreads();
@@ -883,16 +865,16 @@ int prepare(Product& q, int64_t tiles, bool bf16, cudaStream_t st)
     return launch<MODE, BN, false>(q, tiles, st);
 }
 
-template <int MODE, int COPIES>
+template <int MODE, bool GATHER>
 int launch_pair(const Product& q, int64_t tiles, cudaStream_t st)
 {
-    constexpr auto kern = k_expert_pair<MODE, COPIES>;
+    constexpr auto kern = k_expert_pair<MODE, GATHER>;
     static_assert(Pair::SHARED <= 232448, "shared memory of a block");
     if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, Pair::SHARED) != cudaSuccess) {
         cudaGetLastError();
         return GEM_NLR_E_CUDA;
     }
-    kern<<<2 * (unsigned)(tiles < kTrainSMs / 2 ? tiles : kTrainSMs / 2), COPIES ? 512 : 384, Pair::SHARED, st>>>(q);
+    kern<<<2 * (unsigned)(tiles < kTrainSMs / 2 ? tiles : kTrainSMs / 2), GATHER ? 512 : 384, Pair::SHARED, st>>>(q);
     return launched();
 }
 
@@ -912,11 +894,11 @@ int run(Product& q, bool bf16, cudaStream_t st)
     if (q.a.wide && q.b.wide && (MODE == kWeights ? q.m : q.places / q.experts) >= 256 && tall_tiles >= kTrainSMs / 2) {
         constexpr bool A_K = MODE != kWeights, B_K = MODE == kRowsTimesTurned;
         q.idesc = idesc(256) & ~(31u << 24) | (uint32_t)(2 * kTileM >> 4) << 24;
+        const bool cut = MODE == kWeights;                          // rows of both operands by index
         if ((q.a.gather || encode(&q.ta, q.a, 0, A_K ? kTileM : kChunk, bf16)) &&
-            (q.b.gather || encode(&q.tb, q.b, MODE == kWeights ? 0 : q.experts, B_K ? kTileM : kChunk, bf16))) {
-            if (q.a.gather || q.b.gather) return launch_pair<MODE, 2>(q, tall_tiles, st);
-            return launch_pair<MODE, MODE == kWeights ? 1 : 0>(q, tall_tiles, st);
-        }
+            (q.b.gather || encode(&q.tb, q.b, MODE == kWeights ? 0 : q.experts, B_K ? kTileM : kChunk, bf16)) &&
+            (!(cut || q.a.gather) || encode(&q.ra, q.a, 0, 1, bf16)) && (!cut || encode(&q.rb, q.b, 0, 1, bf16)))
+            return q.a.gather || q.b.gather ? launch_pair<MODE, true>(q, tall_tiles, st) : launch_pair<MODE, false>(q, tall_tiles, st);
     }
     if (tiles(256) >= kTrainSMs) {
         q.idesc = idesc(256);
