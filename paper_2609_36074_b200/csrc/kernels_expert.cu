@@ -537,19 +537,6 @@ __device__ __forceinline__ void arrive_at(uint32_t bar)              // a barrie
 {
     asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
 }
-__device__ __forceinline__ bool pair_wait(uint32_t bar, uint32_t parity, volatile uint32_t* dead, uint32_t limit = kSpinLimit << 4)
-{
-    for (uint32_t i = 0; i < limit; ++i) {
-        uint32_t ok;
-        asm volatile("{\n\t.reg .pred p;\n\t"
-                     "mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
-                     "selp.u32 %0, 1, 0, p;\n\t}" : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
-        if (ok) return true;
-        if ((i & 63u) == 63u && *dead) return false;
-    }
-    *dead = 1u;
-    return false;
-}
 __device__ __forceinline__ void pair_mma(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate)
 {
     asm volatile("{\n\t.reg .pred p;\n\t"
@@ -653,7 +640,7 @@ k_expert_pair(const __grid_constant__ Product q)
                 const int x = left_one ? a_row : b_col;     // weights: the operand's first column
                 int p0 = w.k_first;                         // weights: the chunk's first place
                 for (int k = 0; k < w.k; k += kChunk, p0 += kChunk) {
-                    on = pair_wait(free_(s), parity, dead);
+                    on = wait_for(free_(s), parity, dead);
                     if (!on) break;
                     const uint32_t to = stages + (uint32_t)s * S::STAGE + (left_one ? 0 : S::A), bar = of_first(full(s));
                     if (MODE == kWeights && w.k - k < kChunk) {
@@ -690,7 +677,7 @@ k_expert_pair(const __grid_constant__ Product q)
             if (!on && rank == 0 && left_one) {
                 // copies on their way land before the block ends
                 uint32_t none = 0;
-                for (uint32_t i = g > S::STAGES ? g - S::STAGES : 0; i < g; ++i) pair_wait(full((int)(i % S::STAGES)), i / S::STAGES & 1u, &none, kSpinLimit);
+                for (uint32_t i = g > S::STAGES ? g - S::STAGES : 0; i < g; ++i) wait_for(full((int)(i % S::STAGES)), i / S::STAGES & 1u, &none, kSpinLimit);
             }
         }
     } else if (warp == 1 && rank == 0) {
@@ -704,9 +691,9 @@ k_expert_pair(const __grid_constant__ Product q)
                 const int k = tile(t).k;
                 if (k == 0) continue;
                 const uint32_t acc = tmem + (i & 1u) * kPairN;
-                on = pair_wait(acc_free(i & 1), ((i >> 1) + 1) & 1, dead);
+                on = wait_for(acc_free(i & 1), ((i >> 1) + 1) & 1, dead);
                 for (int left = k; left > 0 && on; left -= kChunk) {
-                    on = pair_wait(full(s), parity, dead);
+                    on = wait_for(full(s), parity, dead);
                     if (!on) break;
                     tc_fence_after();
                     const uint64_t da = da0 + (uint64_t)(uint32_t)(s * (S::STAGE >> 4)), db = db0 + (uint64_t)(uint32_t)(s * (S::STAGE >> 4));
@@ -723,7 +710,7 @@ k_expert_pair(const __grid_constant__ Product q)
             if (!on) {
                 uint32_t none = 0;
                 pair_commit(drained);
-                pair_wait(drained, 0, &none, kSpinLimit);
+                wait_for(drained, 0, &none, kSpinLimit);
             }
         }
     } else if (warp >= 4 && warp < 12) {
@@ -762,7 +749,7 @@ k_expert_pair(const __grid_constant__ Product q)
 #pragma unroll
                         for (int i = 0; i < 8; ++i) named[i] = rows_at(q.a, q.row, a_row + 32 * part + 4 * i, w.stop);
                     for (int k = 0; k < w.k; k += kChunk) {
-                        on = pair_wait(free_(s), parity, dead);
+                        on = wait_for(free_(s), parity, dead);
                         if (!on) break;
                         const uint32_t to = stages + (uint32_t)s * S::STAGE + (uint32_t)(32 * part * kRow), bar = of_first(full(s));
 #pragma unroll
@@ -785,7 +772,7 @@ k_expert_pair(const __grid_constant__ Product q)
                     for (int u = 0; u < AHEAD; ++u) {
                         const int k = k0 + u * kChunk;
                         if (k >= w.k || !on) break;
-                        on = pair_wait(free_(s), parity, dead);
+                        on = wait_for(free_(s), parity, dead);
                         on = __all_sync(0xffffffffu, on);
                         if (!on) break;
                         const int r = (uint32_t)ahead[u] < (uint32_t)o.rows ? ahead[u] : (int)o.rows;
