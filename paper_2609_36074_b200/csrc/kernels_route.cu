@@ -3,12 +3,13 @@
 //   s = softmax(z) or 1 / (1 + exp(-z));  c = s + b;  the k largest c of the kept groups (without b: the k largest z)
 //   w_j = scale s_j / sum_l s_l (or scale s_j)
 //
-// A warp a row, up to 16 neighbouring logits a lane.  Scores become unsigned keys in their order, so that the largest of 32 lanes is
-// one warp reduction; the lowest lane among equals, and in it the lowest logit, is the lowest index.  A round of the choice is that
-// reduction, a vote and the owner's next best.  The FP32 scores of the choice are right to about 2^-20, which does not tell
-// neighbours apart: where two scores that follow one another in the choice are nearer than that (and are not the same logit with
-// the same bias, which are equal in any precision), the row is chosen again in FP64.  One row in a hundred is, at 128 experts with
-// sigmoid scores.  Weights are taken from the chosen logits anew, one a lane.
+// Part-warps a row: up to 16 neighbouring logits a lane, 4 to 32 lanes a row.  A candidate is one 32-bit key, its score above its
+// index (the lowest index largest), so that the best of a row is a butterfly of maxima and no two are equal: each lane sorts
+// its own once, and a round of the choice is the butterfly and a step of the owner's list.  The score in the key is the logit's upper
+// bits, or with a bias a fixed-point number from an FP32 score that is right to about 2^-20.  Neither tells neighbours apart: where
+// two that follow one another in the choice are too near (and are not the same logit with the same bias, which are equal in any
+// precision), the warp chooses that row again in FP64.  One row in a hundred is, at 128 experts with sigmoid scores.  Weights are
+// taken from the chosen logits anew.
 //
 // The order is a counting sort that keeps the rows of an expert in order, without atomics whose order shows: blocks own
 // consecutive rows and count their experts; the second kernel adds the counts of the blocks before (each block reads all of
@@ -19,9 +20,8 @@
 namespace gemnlr {
 namespace {
 
-// Threads of a block: 1024 where 64 registers a thread suffice.  (Fewer, larger blocks: fewer counts to add.)
-template <int V> constexpr int kBlockThreads = V <= 4 ? 1024 : 512;
-constexpr int kBlocks = kTrainSMs * 2;             // at most
+constexpr int kThreads = 512, kWarps = kThreads / 32;
+constexpr int kBlocks = kTrainSMs;                 // at most
 constexpr int kMaxChosen = 32, kMaxGroups = 32;
 constexpr unsigned kAll = 0xffffffffu;
 
@@ -32,7 +32,6 @@ struct Route {
     int64_t n;
     int experts, k, score, groups, kept, best, renorm;
     int wide;               // a lane's logits are one vector
-    int group_lanes;        // lanes that hold a group's experts; 0 where groups end inside a lane's or are not a power of two of lanes
     float scale;
     int32_t* expert;
     float* weight;
@@ -40,28 +39,23 @@ struct Route {
     int32_t* row;
     int32_t* place;
     int32_t* counts;        // blocks x experts
-    int64_t rows_per_warp;
+    int64_t rows_per_warp;  // a multiple of the rows that a warp takes at a time
 };
 
-// Keys: whole numbers in the order of the scores; 0 is no candidate.
+// Whole numbers in the order of the scores.
 __device__ __forceinline__ uint32_t key_of(float c)
 {
     const uint32_t u = __float_as_uint(c + 0.0f);
     return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
-__device__ __forceinline__ float score_of(uint32_t k) { return __uint_as_float(k & 0x80000000u ? k & 0x7fffffffu : ~k); }
 __device__ __forceinline__ uint64_t key_of(double c)
 {
     const uint64_t u = (uint64_t)__double_as_longlong(c + 0.0);
     return u >> 63 ? ~u : u | 1ull << 63;
 }
-__device__ __forceinline__ double score_of(uint64_t k) { return __longlong_as_double((long long)(k >> 63 ? k & ~(1ull << 63) : ~k)); }
 constexpr uint32_t kNone32 = 0x007fffffu;                   // -inf
 constexpr uint64_t kNone64 = 0x000fffffffffffffull;
-__device__ __forceinline__ bool is_none(uint32_t k) { return k <= kNone32; }
-__device__ __forceinline__ bool is_none(uint64_t k) { return k <= kNone64; }
 
-__device__ __forceinline__ uint32_t warp_max(uint32_t k) { return __reduce_max_sync(kAll, k); }
 __device__ __forceinline__ uint64_t warp_max(uint64_t k)
 {
     const uint32_t hi = __reduce_max_sync(kAll, (uint32_t)(k >> 32));
@@ -77,326 +71,381 @@ __device__ __forceinline__ float warp_top(float v)
     return t;
 }
 
-// How far the choice's FP32 scores can be off: 2^-18 of a score that is at most 1 (the exponential is off by 2^-21 of itself and by
-// its argument's rounding, x exp(-x) <= 0.37; a sum of 16 and 5 steps, a quotient and the sum with the bias add 30 units of 2^-24), and a
-// rounding of the bias.
-__device__ __forceinline__ float margin_of(float c) { return 0x1p-18f + 0x1p-21f * fabsf(c); }
-
-// A lane's candidates: experts lane * V + v.  `at` are their v, in the order of `key` where they are kept sorted (the same v first
-// among equals).
-template <int V, typename K> struct Candidates {
-    static constexpr bool SORTED = V <= 4;              // more are searched anew when the best is taken
-    K key[V], top;
-    int at[V], best;
-    int lane;
-    __device__ __forceinline__ void search()
-    {
-        top = key[0];
-        best = 0;
-#pragma unroll
-        for (int v = 1; v < V; ++v)
-            if (key[v] > top) { top = key[v]; best = v; }
-    }
-    __device__ __forceinline__ void begin()
-    {
-        if constexpr (SORTED) {
-#pragma unroll
-            for (int v = 0; v < V; ++v) at[v] = v;
-#pragma unroll
-            for (int round = 0; round < V; ++round)
-#pragma unroll
-                for (int v = round & 1; v + 1 < V; v += 2)
-                    if (key[v + 1] > key[v]) {
-                        const K k = key[v]; key[v] = key[v + 1]; key[v + 1] = k;
-                        const int a = at[v]; at[v] = at[v + 1]; at[v + 1] = a;
-                    }
-            top = key[0];
-            best = at[0];
-        } else {
-            search();
-        }
-    }
-    __device__ __forceinline__ void take()
-    {
-        if constexpr (SORTED) {
-#pragma unroll
-            for (int v = 0; v + 1 < V; ++v) { key[v] = key[v + 1]; at[v] = at[v + 1]; }
-            key[V - 1] = 0;
-            top = key[0];
-            best = at[0];
-        } else {
-#pragma unroll
-            for (int v = 0; v < V; ++v)
-                if (v == best) key[v] = 0;
-            search();
-        }
-    }
-};
-
-// The k best keys into `got` (lane j: the j-th's index, -1 for none).  near(key, index, key, index) is told of each two that follow one
-// another, and of the last and the one after it.  Returns whether it ever said that they are too near.
-template <int V, typename K, typename N>
-__device__ __forceinline__ bool choose(Candidates<V, K>& c, int k, int& got, N near)
+template <int LANES> __device__ __forceinline__ float lanes_sum(float v)
 {
-    const int lane = c.lane;
-    K last = 0;
-    int before = -1;
-    bool unsure = false;
-    got = -1;
-    c.begin();
-    for (int j = 0; j <= k; ++j) {
-        const K best = warp_max(c.top);
-        if (is_none(best)) break;
-        const int owner = __ffs(__ballot_sync(kAll, c.top == best)) - 1;
-        const int index = owner * V + __shfl_sync(kAll, c.best, owner);
-        if (j > 0 && near(last, before, best, index)) unsure = true;
-        if (j == k) break;
-        if (lane == j) got = index;
-        last = best;
-        before = index;
-        if (lane == owner) c.take();
-    }
-    return unsure;
+#pragma unroll
+    for (int o = LANES / 2; o > 0; o >>= 1) v += __shfl_xor_sync(kAll, v, o);
+    return v;
+}
+template <int LANES> __device__ __forceinline__ float lanes_top(float v)
+{
+#pragma unroll
+    for (int o = LANES / 2; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor_sync(kAll, v, o));
+    return v;
 }
 
-// Leaves only the kept groups' keys.  S: float or double; by[v]: the score of the lane's v-th expert that its group is judged by
-// (-inf: none).  Returns whether the border between kept groups and others is nearer than FP32 tells (`scored`).
-template <int V, typename S, typename K>
-__device__ __forceinline__ bool keep_groups(Candidates<V, K>& c, const Route& r, const S (&by)[V], bool scored)
+// ---- the choice in FP64, a row by a warp: experts lane * V + v -------------------------------------------------------------------
+// Lane j returns the j-th chosen expert, -1 for none.
+template <int V, typename T>
+__device__ __noinline__ int choose_in_64_bits(const Route& r, int64_t row, int lane)
 {
-    const int size = r.experts / r.groups, lane = c.lane;
-    const S none = -(S)INFINITY;
-    S mine = none;                                       // the score of the group `me`
-    int me = r.groups, every = 1;                        // groups' scores are held by lanes 0, every, 2 every, ...
-    if (r.group_lanes) {
-        S first = none, second = none;
+    const T* zr = reinterpret_cast<const T*>(r.z) + row * r.ld;
+    const bool soft = r.score == GEM_NLR_SOFTMAX;
+    const double none = -(double)INFINITY;
+    float z[V], m = -INFINITY;
+    double s[V], sum = 0.0;
 #pragma unroll
-        for (int v = 0; v < V; ++v) {
-            const S x = lane * V + v < r.experts ? by[v] : none;
-            second = fmax(second, fmin(first, x));
-            first = fmax(first, x);
-        }
-        for (int o = 1; o < r.group_lanes; o *= 2) {
-            const S a = __shfl_xor_sync(kAll, first, o), b = __shfl_xor_sync(kAll, second, o);
-            second = fmax(fmin(first, a), fmax(second, b));
-            first = fmax(first, a);
-        }
-        every = r.group_lanes;
-        if (lane / every < r.groups) {
-            me = lane / every;
-            mine = r.best == 2 && second != none ? first + second : first;
-        }
-    } else {
+    for (int v = 0; v < V; ++v) {
+        z[v] = lane * V + v < r.experts ? to_f(zr[lane * V + v]) : -INFINITY;
+        m = fmaxf(m, z[v]);
+    }
+    m = warp_top(m);
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+        s[v] = z[v] == -INFINITY ? 0.0 : soft ? exp((double)z[v] - (double)m) : 1.0 / (1.0 + exp(-(double)z[v]));
+        sum += s[v];
+    }
+    sum = warp_sum(sum);
+    uint64_t key[V];
+    double by[V];                                        // what a group is judged by
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+        const int i = lane * V + v;
+        if (soft) s[v] /= sum;
+        double x = r.bias ? s[v] + (double)(i < r.experts ? __ldg(r.bias + i) : 0.f) : (double)z[v];
+        if (z[v] == -INFINITY) x = none;
+        key[v] = i < r.experts ? key_of(x) : 0;
+        by[v] = z[v] == -INFINITY ? none : r.bias || r.best == 1 ? x : s[v];
+    }
+    if (r.groups > 1) {
+        const int size = r.experts / r.groups;
+        double mine = none;                              // lane g: group g's score
         for (int g = 0; g < r.groups; ++g) {
-            S first = none, second = none;
+            double first = none, second = none;
 #pragma unroll
             for (int v = 0; v < V; ++v) {
                 const int i = lane * V + v;
-                const S x = i >= g * size && i < (g + 1) * size ? by[v] : none;
+                const double x = i >= g * size && i < (g + 1) * size ? by[v] : none;
                 second = fmax(second, fmin(first, x));
                 first = fmax(first, x);
             }
 #pragma unroll
             for (int o = 1; o < 32; o *= 2) {
-                const S a = __shfl_xor_sync(kAll, first, o), b = __shfl_xor_sync(kAll, second, o);
+                const double a = __shfl_xor_sync(kAll, first, o), b = __shfl_xor_sync(kAll, second, o);
                 second = fmax(fmin(first, a), fmax(second, b));
                 first = fmax(first, a);
             }
-            if (lane == g) {
-                me = g;
-                mine = r.best == 2 && second != none ? first + second : first;
-            }
+            if (lane == g) mine = r.best == 2 && second != none ? first + second : first;
         }
-    }
-    int rank = 0;
-    for (int g = 0; g < r.groups; ++g) {
-        const S other = __shfl_sync(kAll, mine, g * every);
-        rank += other > mine || (other == mine && g < me);
-    }
-    const bool kept = me < r.groups && rank < r.kept;
-    if (r.group_lanes) {
+        int rank = 0;
+        for (int g = 0; g < r.groups; ++g) {
+            const double other = __shfl_sync(kAll, mine, g);
+            rank += other > mine || (other == mine && g < lane);
+        }
+        const unsigned stays = __ballot_sync(kAll, lane < r.groups && rank < r.kept);
 #pragma unroll
         for (int v = 0; v < V; ++v)
-            if (!kept) c.key[v] = 0;
-    } else {
-        const unsigned stays = __ballot_sync(kAll, kept);
+            if (!(stays >> min((lane * V + v) / size, 31) & 1u)) key[v] = 0;
+    }
+    int got = -1;
+    for (int j = 0; j < r.k; ++j) {
+        uint64_t top = key[0];
+        int at = 0;
 #pragma unroll
-        for (int v = 0; v < V; ++v) {
-            const int g = min((lane * V + v) / size, 31);
-            if (!(stays >> g & 1u)) c.key[v] = 0;
+        for (int v = 1; v < V; ++v)
+            if (key[v] > top) { top = key[v]; at = v; }
+        const uint64_t best = warp_max(top);
+        if (best <= kNone64) break;
+        const int owner = __ffs(__ballot_sync(kAll, top == best)) - 1;
+        const int index = owner * V + __shfl_sync(kAll, at, owner);
+        if (lane == j) got = index;
+        if (lane == owner) {
+#pragma unroll
+            for (int v = 0; v < V; ++v)
+                if (v == at) key[v] = 0;
         }
     }
-    if (!scored) return false;
-    // the lowest of those kept and the highest of the others
-    const K low = ~warp_max((K)~key_of(kept ? mine : (S)INFINITY)), high = warp_max(key_of(me < r.groups && !kept ? mine : none));
-    const float x = (float)score_of(low), y = (float)score_of(high);
-    return !is_none(high) && !(x - y > 2.0f * margin_of(x));
-}
-
-// The choice in FP64, for rows whose FP32 scores do not decide it.
-template <int V>
-__device__ __noinline__ int choose_in_64_bits(const Route& r, const float (&z)[V], int lane)
-{
-    double s[V], sum = 0.0;
-    float m = -INFINITY;
-#pragma unroll
-    for (int v = 0; v < V; ++v) m = fmaxf(m, z[v]);
-    m = warp_top(m);
-#pragma unroll
-    for (int v = 0; v < V; ++v) {
-        s[v] = z[v] == -INFINITY ? 0.0 : r.score == GEM_NLR_SOFTMAX ? exp((double)z[v] - (double)m) : 1.0 / (1.0 + exp(-(double)z[v]));
-        sum += s[v];
-    }
-    sum = warp_sum(sum);
-    Candidates<V, uint64_t> c;
-    c.lane = lane;
-#pragma unroll
-    for (int v = 0; v < V; ++v) {
-        const int i = lane * V + v;
-        if (r.score == GEM_NLR_SOFTMAX) s[v] /= sum;
-        double x = r.bias ? s[v] + (double)(i < r.experts ? __ldg(r.bias + i) : 0.f) : (double)z[v];
-        if (z[v] == -INFINITY) x = -(double)INFINITY;
-        c.key[v] = i < r.experts ? key_of(x) : 0;
-        if (!r.bias && r.best == 1) s[v] = (double)z[v];
-        else if (r.bias) s[v] = x;
-        if (z[v] == -INFINITY) s[v] = -(double)INFINITY;
-    }
-    if (r.groups > 1) keep_groups<V, double>(c, r, s, false);
-    int got;
-    choose(c, r.k, got, [](uint64_t, int, uint64_t, int) { return false; });
     return got;
 }
 
-// A lane's V logits.
+// ---- the choice by keys -----------------------------------------------------------------------------------------------------------
+
+// How far the choice's FP32 scores can be off: 2^-19 of a score that is at most 1 (the exponential is off by 2^-21 of itself and by
+// its argument's rounding, x exp(-x) <= 0.37; a sum of 16 and 5 steps, a quotient and the sum with the bias add 30 units of 2^-24).
+// Two of them, and what a bias of up to 2^4 adds in rounding, are told apart from 2^-17 on.
+constexpr float kMargin = 0x1p-17f;
+
+// Largest first.  (Batcher's merge exchange; a network for a power of two.)
+template <int V>
+__device__ __forceinline__ void sort_keys(uint32_t (&key)[V])
+{
+#pragma unroll
+    for (int p = V / 2; p > 0; p /= 2) {
+#pragma unroll
+        for (int q = V / 2, r = 0, d = p; d > 0;) {
+#pragma unroll
+            for (int i = 0; i + d < V; ++i)
+                if ((i & p) == r) {
+                    const uint32_t a = key[i], b = key[i + d];
+                    key[i] = max(a, b);
+                    key[i + d] = min(a, b);
+                }
+            d = q > p ? q - p : 0;
+            q /= 2;
+            r = p;
+        }
+    }
+}
+
+// A lane's V logits, experts me * V + v.
 template <int V, typename T>
-__device__ __forceinline__ void load_logits(const T* zr, const Route& r, int lane, float (&z)[V])
+__device__ __forceinline__ void load_logits(const T* zr, const Route& r, int me, float (&z)[V])
 {
     constexpr int BYTES = V * (int)sizeof(T);
-    if (BYTES >= 4 && r.wide && lane * V + V <= r.experts) {
-        uint32_t w[(BYTES + 3) / 4];
+    if (r.wide && me * V + V <= r.experts) {
+        uint32_t w[BYTES / 4];
         if constexpr (BYTES >= 16) {
 #pragma unroll
-            for (int i = 0; i < BYTES / 16; ++i) *reinterpret_cast<uint4*>(w + 4 * i) = *(reinterpret_cast<const uint4*>(zr + lane * V) + i);
-        } else if constexpr (BYTES == 8) {
-            *reinterpret_cast<uint2*>(w) = *reinterpret_cast<const uint2*>(zr + lane * V);
-        } else if constexpr (BYTES == 4) {
-            w[0] = *reinterpret_cast<const uint32_t*>(zr + lane * V);
+            for (int i = 0; i < BYTES / 16; ++i) *reinterpret_cast<uint4*>(w + 4 * i) = __ldg(reinterpret_cast<const uint4*>(zr + me * V) + i);
+        } else {
+            *reinterpret_cast<uint2*>(w) = __ldg(reinterpret_cast<const uint2*>(zr + me * V));
         }
 #pragma unroll
         for (int v = 0; v < V; ++v) z[v] = to_f(reinterpret_cast<const T*>(w)[v]);
     } else {
 #pragma unroll
-        for (int v = 0; v < V; ++v) z[v] = lane * V + v < r.experts ? to_f(zr[lane * V + v]) : -INFINITY;
+        for (int v = 0; v < V; ++v) z[v] = me * V + v < r.experts ? to_f(zr[me * V + v]) : -INFINITY;
     }
 }
 
-// One row by one warp.
-template <int V, typename T>
-__device__ __forceinline__ void route_row(const Route& r, int64_t row, int lane, const float (&bias)[V], int& chosen)
+// A warp's shared memory: chosen experts, and where there are groups scores and groups' scores.
+template <int LANES, int V> struct Space {
+    static constexpr int ROWS = 32 / LANES, PITCH = LANES * V + 4;
+    int32_t chosen[ROWS][kMaxChosen];
+    float group[ROWS][kMaxGroups];
+    float score[ROWS][PITCH];
+};
+
+// 32 / LANES rows from `row` on by one warp; rows from `end` on are not there.  The chosen experts are left in sp.chosen.
+template <int LANES, int V, typename T>
+__device__ __forceinline__ void route_rows(const Route& r, int64_t row0, int64_t end, int lane, const float (&bias)[V], Space<LANES, V>& sp)
 {
-    const T* zr = reinterpret_cast<const T*>(r.z) + row * r.ld;
-    const bool soft = r.score == GEM_NLR_SOFTMAX;
-    float z[V], m = -INFINITY;
-    load_logits<V>(zr, r, lane, z);
+    constexpr int PAD = LANES * V;
+    constexpr uint32_t INDEX = PAD - 1;                   // the key's lower bits: PAD - 1 - index
+    constexpr int BITS = PAD == 16 ? 4 : PAD == 32 ? 5 : PAD == 64 ? 6 : PAD == 128 ? 7 : PAD == 256 ? 8 : 9;
+    const int me = lane % LANES, mine = lane / LANES;
+    const int64_t row = row0 + mine;
+    const bool in = row < end;
+    const T* zr = reinterpret_cast<const T*>(r.z) + (in ? row : row0) * r.ld;
+    const bool soft = r.score == GEM_NLR_SOFTMAX, biased = r.bias;
+    const bool scored = biased || (r.groups > 1 && r.best == 2);          // the choice needs the scores
+    const unsigned row_lanes = (LANES == 32 ? kAll : (1u << (LANES & 31)) - 1u) << (lane - me);
+    float z[V], m = -INFINITY, sum = 0.0f;
+    load_logits<V>(zr, r, me, z);
     bool bad = false;
 #pragma unroll
     for (int v = 0; v < V; ++v) {
-        bad |= z[v] != z[v] || (soft && z[v] == INFINITY);
+        bad |= !(z[v] < INFINITY) && (soft || z[v] != INFINITY);
         m = fmaxf(m, z[v]);
     }
-    const bool scored = r.bias || (r.groups > 1 && r.best == 2);          // the choice needs the scores
-    float sum = 0.0f;
-    Candidates<V, uint32_t> c;
-    c.lane = lane;
-    float by[V];
+    if (soft && (scored || !r.renorm)) m = lanes_top<LANES>(m);
+    float c[V];                                          // scores with their biases, or logits
     if (scored) {
-        // exponentials to 2^-21: close neighbours are chosen in FP64
-        float e[V];
         if (soft) {
-            m = warp_top(m);
 #pragma unroll
-            for (int v = 0; v < V; ++v) { e[v] = z[v] == -INFINITY ? 0.0f : __expf(z[v] - m); sum += e[v]; }
-            sum = warp_sum(sum);
+            for (int v = 0; v < V; ++v) {
+                c[v] = z[v] == -INFINITY ? 0.0f : __expf(z[v] - m);
+                sum += c[v];
+            }
+            const float over = __fdividef(1.0f, lanes_sum<LANES>(sum));
+#pragma unroll
+            for (int v = 0; v < V; ++v) c[v] *= over;
+        } else {
+#pragma unroll
+            for (int v = 0; v < V; ++v) c[v] = __fdividef(1.0f, 1.0f + __expf(-z[v]));
         }
 #pragma unroll
         for (int v = 0; v < V; ++v) {
-            const float s = soft ? __fdividef(e[v], sum) : __fdividef(1.0f, 1.0f + __expf(-z[v]));
-            const float x = s + bias[v];
-            const bool there = z[v] != -INFINITY;
-            bad |= there && x != x;
-            c.key[v] = lane * V + v < r.experts ? key_of(!there ? -INFINITY : r.bias ? x : z[v]) : 0;
-            by[v] = there ? x : -INFINITY;
+            c[v] = z[v] == -INFINITY ? -INFINITY : c[v] + bias[v];
+            bad |= c[v] != c[v];
+        }
+    } else {
+#pragma unroll
+        for (int v = 0; v < V; ++v) c[v] = z[v];
+    }
+    bool unsure = false;
+    unsigned stays = kAll;                               // groups that can be chosen
+    if (r.groups > 1) {
+        const int size = r.experts / r.groups;
+#pragma unroll
+        for (int v = 0; v < V; v += 4) *reinterpret_cast<float4*>(&sp.score[mine][me * V + v]) = make_float4(c[v], c[v + 1], c[v + 2], c[v + 3]);
+        __syncwarp();
+        for (int g = me; g < r.groups; g += LANES) {
+            float first = -INFINITY, second = -INFINITY;
+            const float* of = &sp.score[mine][g * size];
+#pragma unroll 4
+            for (int i = 0; i < size; ++i) {
+                const float x = of[i];
+                second = fmaxf(second, fminf(first, x));
+                first = fmaxf(first, x);
+            }
+            sp.group[mine][g] = (r.best == 2 && second != -INFINITY ? first + second : first) + 0.0f;
+        }
+        __syncwarp();
+        unsigned kept = 0;
+        float low = INFINITY, high = -INFINITY;          // the lowest group kept and the highest of the others
+        for (int g = me; g < r.groups; g += LANES) {
+            const float x = sp.group[mine][g];
+            int rank = 0;
+#pragma unroll 4
+            for (int o = 0; o < r.groups; ++o) {
+                const float y = sp.group[mine][o];
+                rank += y > x || (y == x && o < g);
+            }
+            if (rank < r.kept) {
+                kept |= 1u << g;
+                low = fminf(low, x);
+            } else {
+                high = fmaxf(high, x);
+            }
+        }
+#pragma unroll
+        for (int o = LANES / 2; o > 0; o >>= 1) {
+            kept |= __shfl_xor_sync(kAll, kept, o);
+            low = fminf(low, __shfl_xor_sync(kAll, low, o));
+            high = fmaxf(high, __shfl_xor_sync(kAll, high, o));
+        }
+        stays = kept;
+        unsure = scored && high != -INFINITY && !(low - high > 2.0f * kMargin + 0x1p-20f * fabsf(low));
+    }
+    uint32_t key[V];
+    if (biased) {
+        // in steps of 2^(BITS - 30) from two below the largest on; lower ones come out equal
+        float top = -INFINITY;
+#pragma unroll
+        for (int v = 0; v < V; ++v) top = fmaxf(top, c[v]);
+        top = lanes_top<LANES>(top);
+        const float from = top - 2.0f;
+        unsure |= fabsf(top) > 16.0f && top != -INFINITY;
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            const uint32_t q = (uint32_t)__float2uint_rn(fmaxf(c[v] - from, 0.0f) * (float)(1u << (31 - BITS - 1)));
+            key[v] = c[v] == -INFINITY ? 0u : (q + 1u) << BITS | (INDEX - (uint32_t)(me * V + v));
         }
     } else {
 #pragma unroll
         for (int v = 0; v < V; ++v) {
-            c.key[v] = lane * V + v < r.experts ? key_of(z[v]) : 0;
-            by[v] = z[v];
+            const uint32_t k = key_of(z[v]);
+            key[v] = k <= kNone32 ? 0u : (k & ~INDEX) | (INDEX - (uint32_t)(me * V + v));
         }
     }
-    int got = -1;
-    bad = __any_sync(kAll, bad);
-    if (!bad) {
-        // the same logit with the same bias is equal in any precision; other neighbours within the margin are not decided
-        const auto near = [&](uint32_t a, int i, uint32_t b, int j) {
-            if (!r.bias) return false;
-            const float x = score_of(a), y = score_of(b);
-            if (x - y > margin_of(x)) return false;
-            return !(to_f(zr[i]) == to_f(zr[j]) && __ldg(r.bias + i) == __ldg(r.bias + j));
-        };
-        bool unsure = false;
-        if (r.groups > 1) unsure = keep_groups<V, float>(c, r, by, scored);
-        unsure |= choose(c, r.k, got, near);
-        if (unsure) got = choose_in_64_bits<V>(r, z, lane);
-    }
-    // weights: lane j has the j-th chosen expert
-    float w = 0.0f;
-    if (bad) {
-        w = __uint_as_float(0x7fc00000u);
-    } else {
-        const float x = got >= 0 ? to_f(zr[got]) : -INFINITY;
-        const auto logistic = [](float v) { return 1.0f / (1.0f + expf(-v)); };
-        if (r.renorm) {
-            float e = 0.0f, total;
-            if (!soft) {
-                if (got >= 0) e = logistic(x);
-                total = warp_sum(e);
-            }
-            if (soft || total < 1e-30f) {
-                // a softmax over the chosen logits, or the logarithms of their scores: neither underflows
-                const float l = got < 0 ? -INFINITY : soft ? x : fminf(x, 0.0f) - log1pf(expf(-fabsf(x)));
-                const float top = warp_top(l);
-                e = got >= 0 ? expf(l - top) : 0.0f;
-                total = warp_sum(e);
-            }
-            if (got >= 0) w = e / total * r.scale;
-        } else if (soft) {
-            m = warp_top(m);
-            sum = 0.0f;
+    if (r.groups > 1) {
+        const int size = r.experts / r.groups;
+        int g = me * V / size, next = (g + 1) * size - me * V;               // the group of v, and the v where the next begins
 #pragma unroll
-            for (int v = 0; v < V; ++v) sum += z[v] == -INFINITY ? 0.0f : expf(z[v] - m);
-            sum = warp_sum(sum);
-            if (got >= 0) w = expf(x - m) / sum * r.scale;
-        } else if (got >= 0) {
-            w = logistic(x) * r.scale;
+        for (int v = 0; v < V; ++v) {
+            if (v == next) { ++g; next += size; }
+            if (!(stays >> (g & 31) & 1u)) key[v] = 0u;
         }
     }
-    if (lane < r.k) {
-        r.expert[row * r.k + lane] = got;
-        r.weight[row * r.k + lane] = w;
+    sort_keys<V>(key);
+    const bool few = r.k < 8;                            // entries of a list that can be reached
+    uint32_t last = 0;
+    for (int j = 0; j <= r.k; ++j) {
+        uint32_t best = key[0];
+#pragma unroll
+        for (int o = LANES / 2; o > 0; o >>= 1) best = max(best, __shfl_xor_sync(kAll, best, o));
+        const int index = best ? (int)(INDEX - (best & INDEX)) : -1;
+        if (best && j > 0) {
+            const uint32_t a = last >> BITS, b = best >> BITS;
+            if (biased ? a - b <= (uint32_t)(kMargin * (float)(1u << (31 - BITS - 1))) : a == b) {
+                const int before = (int)(INDEX - (last & INDEX));
+                unsure |= !(to_f(zr[before]) == to_f(zr[index]) && (!biased || __ldg(r.bias + before) == __ldg(r.bias + index)));
+            }
+        }
+        last = best;
+        if (j == r.k) break;
+        if (me == 0) sp.chosen[mine][j] = index;
+        if (key[0] == best) {
+            if (few) {
+#pragma unroll
+                for (int v = 0; v + 1 < (V < 8 ? V : 8); ++v) key[v] = key[v + 1];
+                if (V <= 8) key[V < 8 ? V - 1 : 7] = 0u;
+            } else {
+#pragma unroll
+                for (int v = 0; v + 1 < V; ++v) key[v] = key[v + 1];
+                key[V - 1] = 0u;
+            }
+        }
     }
-    chosen = got;
+    bad = (__ballot_sync(kAll, bad) & row_lanes) != 0;
+    unsure = unsure && !bad && in;
+    __syncwarp();
+    for (unsigned rows = __ballot_sync(kAll, unsure && me == 0); rows; rows &= rows - 1) {
+        const int which = (__ffs(rows) - 1) / LANES;
+        const int got = choose_in_64_bits<(PAD > 32 ? PAD / 32 : 1), T>(r, row0 + which, lane);
+        if (lane < r.k) sp.chosen[which][lane] = got;
+    }
+    __syncwarp();
+    // weights: slot j by lane j mod LANES of its row
+    const auto logistic = [](float x) { return 1.0f / (1.0f + expf(-x)); };
+    float top = -INFINITY, total = 0.0f;
+    if (!soft && r.renorm) {
+        for (int j = me; j < r.k; j += LANES) {
+            const int e = sp.chosen[mine][j];
+            if (e >= 0) total += logistic(to_f(zr[e]));
+        }
+        total = lanes_sum<LANES>(total);
+    }
+    // s_j / sum s as a softmax over the chosen logits, or where the scores underflow over their logarithms
+    const bool far = !soft && total < 1e-30f;
+    const auto log_score = [&](float x) { return soft ? x : fminf(x, 0.0f) - log1pf(expf(-fabsf(x))); };
+    if (r.renorm && __any_sync(kAll, soft || far)) {
+        for (int j = me; j < r.k; j += LANES) {
+            const int e = sp.chosen[mine][j];
+            if (e >= 0) top = fmaxf(top, log_score(to_f(zr[e])));
+        }
+        top = lanes_top<LANES>(top);
+        float t = 0.0f;
+        for (int j = me; j < r.k; j += LANES) {
+            const int e = sp.chosen[mine][j];
+            if (e >= 0) t += expf(log_score(to_f(zr[e])) - top);
+        }
+        t = lanes_sum<LANES>(t);
+        if (soft || far) total = t;
+    }
+    if (soft && !r.renorm) {
+        sum = 0.0f;
+#pragma unroll
+        for (int v = 0; v < V; ++v) sum += z[v] == -INFINITY ? 0.0f : expf(z[v] - m);
+        total = lanes_sum<LANES>(sum);
+        top = m;
+    }
+    for (int j = me; j < r.k; j += LANES) {
+        const int e = bad ? -1 : sp.chosen[mine][j];
+        float w = bad ? __uint_as_float(0x7fc00000u) : 0.0f;
+        if (e >= 0) {
+            const float x = to_f(zr[e]);
+            const float s = soft || (r.renorm && far) ? expf(log_score(x) - top) : logistic(x);
+            w = (soft || r.renorm ? s / total : s) * r.scale;
+        }
+        if (in) {
+            r.expert[row * r.k + j] = e;
+            r.weight[row * r.k + j] = w;
+        }
+        sp.chosen[mine][j] = in ? e : -1;
+    }
+    __syncwarp();
 }
 
 // Places for the rows of this block's warps.  at: warps x experts, each warp's counts, replaced by the place of its next row of
 // each expert; first: the place of the block's first row of each expert.
-template <int NT>
 __device__ __forceinline__ void give_places(const Route& r, int32_t* at, const int32_t* first, int64_t begin, int64_t end)
 {
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    for (int e = threadIdx.x; e < r.experts; e += NT) {
+    for (int e = threadIdx.x; e < r.experts; e += kThreads) {
         int32_t next = first[e];
-        for (int w = 0; w < (NT / 32); ++w) {
+        for (int w = 0; w < kWarps; ++w) {
             const int32_t c = at[w * r.experts + e];
             at[w * r.experts + e] = next;
             next += c;
@@ -420,11 +469,10 @@ __device__ __forceinline__ void give_places(const Route& r, int32_t* at, const i
     }
 }
 
-// Exclusive sums of total[experts] into first[experts + 1], by one block.  (experts <= NT)
-template <int NT>
+// Exclusive sums of total[experts] into first[experts + 1], by one block.  (experts <= kThreads)
 __device__ __forceinline__ void sums_over_experts(const int32_t* total, int32_t* first, int experts)
 {
-    __shared__ int32_t of_warp[(NT / 32)];
+    __shared__ int32_t of_warp[kWarps];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, e = threadIdx.x;
     const int32_t own = e < experts ? total[e] : 0;
     int32_t v = own;
@@ -442,73 +490,76 @@ __device__ __forceinline__ void sums_over_experts(const int32_t* total, int32_t*
     __syncthreads();
 }
 
-template <int NT>
 __device__ __forceinline__ void leave_rest(const Route& r, int32_t used)
 {
-    for (int64_t p = used + (int64_t)blockIdx.x * NT + threadIdx.x; p < r.n * r.k; p += (int64_t)gridDim.x * NT) r.row[p] = -1;
+    for (int64_t p = used + (int64_t)blockIdx.x * kThreads + threadIdx.x; p < r.n * r.k; p += (int64_t)gridDim.x * kThreads) r.row[p] = -1;
 }
 
-// Shared memory: warps x experts counts; ONE: and experts + 1 sums and experts totals.
-template <int V, typename T, bool ONE>
-__global__ void __launch_bounds__(kBlockThreads<V>)
+// Shared memory: warps x experts counts; ONE: and experts + 1 sums and experts totals; then the warps' space.
+template <int LANES, int V, typename T, bool ONE>
+__global__ void __launch_bounds__(kThreads)
 k_route(const __grid_constant__ Route r)
 {
-    constexpr int NT = kBlockThreads<V>;
+    using Sp = Space<LANES, V>;
     extern __shared__ int32_t at[];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    for (int i = threadIdx.x; i < (NT / 32) * r.experts; i += NT) at[i] = 0;
+    const int before = kWarps * r.experts + (ONE ? 2 * r.experts + 1 : 0);
+    char* space = reinterpret_cast<char*>(at) + ((size_t)before * 4 + 15) / 16 * 16;
+    Sp& sp = *reinterpret_cast<Sp*>(space + (size_t)warp * (r.groups > 1 ? sizeof(Sp) : offsetof(Sp, group)));
+    for (int i = threadIdx.x; i < kWarps * r.experts; i += kThreads) at[i] = 0;
     __syncthreads();
-    const int64_t begin = min(r.n, ((int64_t)blockIdx.x * (NT / 32) + warp) * r.rows_per_warp), end = min(r.n, begin + r.rows_per_warp);
+    const int64_t begin = min(r.n, ((int64_t)blockIdx.x * kWarps + warp) * r.rows_per_warp), end = min(r.n, begin + r.rows_per_warp);
     int32_t* mine = at + warp * r.experts;
     float bias[V];
 #pragma unroll
-    for (int v = 0; v < V; ++v) bias[v] = r.bias && lane * V + v < r.experts ? __ldg(r.bias + lane * V + v) : 0.0f;
-    for (int64_t row = begin; row < end; ++row) {
-        int got;
-        route_row<V, T>(r, row, lane, bias, got);
-        if (got >= 0) mine[got] += 1;                    // a row's experts differ
+    for (int v = 0; v < V; ++v) bias[v] = r.bias && lane % LANES * V + v < r.experts ? __ldg(r.bias + lane % LANES * V + v) : 0.0f;
+    for (int64_t row = begin; row < end; row += Sp::ROWS) {
+        route_rows<LANES, V, T>(r, row, end, lane, bias, sp);
+        for (int j = lane; j < Sp::ROWS * r.k; j += 32) {
+            const int e = sp.chosen[j / r.k][j % r.k];
+            if (e >= 0) atomicAdd(mine + e, 1);
+        }
         __syncwarp();
     }
     __syncthreads();
     next_may_start();
-    int32_t* first = at + (NT / 32) * r.experts;
+    int32_t* first = at + kWarps * r.experts;
     int32_t* total = ONE ? first + r.experts + 1 : r.counts + (int64_t)blockIdx.x * r.experts;
-    for (int e = threadIdx.x; e < r.experts; e += NT) {
+    for (int e = threadIdx.x; e < r.experts; e += kThreads) {
         int32_t c = 0;
-        for (int w = 0; w < (NT / 32); ++w) c += at[w * r.experts + e];
+        for (int w = 0; w < kWarps; ++w) c += at[w * r.experts + e];
         total[e] = c;
     }
     if constexpr (ONE) {
         __syncthreads();
-        sums_over_experts<NT>(total, first, r.experts);
-        for (int e = threadIdx.x; e <= r.experts; e += NT) r.offset[e] = first[e];
-        give_places<NT>(r, at, first, begin, end);
-        leave_rest<NT>(r, first[r.experts]);
+        sums_over_experts(total, first, r.experts);
+        for (int e = threadIdx.x; e <= r.experts; e += kThreads) r.offset[e] = first[e];
+        give_places(r, at, first, begin, end);
+        leave_rest(r, first[r.experts]);
     }
 }
 
 // Shared memory: warps x experts counts, then experts + 1 sums, experts totals, experts counts of the blocks before.
-template <int NT>
-__global__ void __launch_bounds__(NT)
+__global__ void __launch_bounds__(kThreads)
 k_route_places(const __grid_constant__ Route r, int blocks)
 {
     extern __shared__ int32_t at[];
-    int32_t* first = at + (NT / 32) * r.experts;
+    int32_t* first = at + kWarps * r.experts;
     int32_t* total = first + r.experts + 1;
     int32_t* before = total + r.experts;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    for (int i = threadIdx.x; i < (NT / 32) * r.experts + 3 * r.experts + 1; i += NT) at[i] = 0;
+    for (int i = threadIdx.x; i < kWarps * r.experts + 3 * r.experts + 1; i += kThreads) at[i] = 0;
     __syncthreads();
-    const int64_t begin = min(r.n, ((int64_t)blockIdx.x * (NT / 32) + warp) * r.rows_per_warp), end = min(r.n, begin + r.rows_per_warp);
+    const int64_t begin = min(r.n, ((int64_t)blockIdx.x * kWarps + warp) * r.rows_per_warp), end = min(r.n, begin + r.rows_per_warp);
     grid_ready();
     for (int64_t i = begin * r.k + lane; i < end * r.k; i += 32) {
         const int e = r.expert[i];
         if (e >= 0) atomicAdd(at + warp * r.experts + e, 1);
     }
     // threads in pairs (expert, share of the blocks); whole numbers: the order of the additions does not show
-    const int shares = max(1, NT / r.experts), share = threadIdx.x / r.experts;
+    const int shares = max(1, kThreads / r.experts), share = threadIdx.x / r.experts;
     if (share < shares)
-        for (int e = threadIdx.x % r.experts; e < r.experts; e += NT) {
+        for (int e = threadIdx.x % r.experts; e < r.experts; e += kThreads) {
             int32_t all = 0, low = 0;
 #pragma unroll 8
             for (int b = share; b < blocks; b += shares) {
@@ -520,13 +571,13 @@ k_route_places(const __grid_constant__ Route r, int blocks)
             atomicAdd(before + e, low);
         }
     __syncthreads();
-    sums_over_experts<NT>(total, first, r.experts);
+    sums_over_experts(total, first, r.experts);
     if (blockIdx.x == 0)
-        for (int e = threadIdx.x; e <= r.experts; e += NT) r.offset[e] = first[e];
-    for (int e = threadIdx.x; e < r.experts; e += NT) before[e] += first[e];
+        for (int e = threadIdx.x; e <= r.experts; e += kThreads) r.offset[e] = first[e];
+    for (int e = threadIdx.x; e < r.experts; e += kThreads) before[e] += first[e];
     __syncthreads();
-    give_places<NT>(r, at, before, begin, end);
-    leave_rest<NT>(r, first[r.experts]);
+    give_places(r, at, before, begin, end);
+    leave_rest(r, first[r.experts]);
 }
 
 struct RouteGrad {
@@ -541,19 +592,6 @@ struct RouteGrad {
     void* dz;
     int64_t ldd;
 };
-
-template <int LANES> __device__ __forceinline__ float lanes_sum(float v)
-{
-#pragma unroll
-    for (int o = LANES / 2; o > 0; o >>= 1) v += __shfl_xor_sync(kAll, v, o);
-    return v;
-}
-template <int LANES> __device__ __forceinline__ float lanes_top(float v)
-{
-#pragma unroll
-    for (int o = LANES / 2; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor_sync(kAll, v, o));
-    return v;
-}
 
 // LANES lanes a row, V neighbouring logits a lane.  Slots are taken LANES at a time, a slot a lane; each lane then picks up the shares of
 // its own experts.
@@ -601,6 +639,7 @@ k_route_backward(const __grid_constant__ RouteGrad r)
             }
             sum = lanes_sum<LANES>(sum);
         }
+        const float over = 1.0f / sum;
         // the slots: weights' shares first (their sum over all slots), then each lane's own
         const int rounds = (r.k + LANES - 1) / LANES;
         float top = -INFINITY, total = 0.0f, t = 0.0f;
@@ -640,7 +679,7 @@ k_route_backward(const __grid_constant__ RouteGrad r)
                 int e; float v, x;
                 slot(q, e, v, x);
                 if (q == 0) { e0 = e; v0 = v; x0 = x; }
-                if (whole && e >= 0 && x != -INFINITY) t += expf(x - m) / sum * v;
+                if (whole && e >= 0 && x != -INFINITY) t += expf(x - m) * over * v;
             }
             if (whole) t = lanes_sum<LANES>(t);
         }
@@ -649,7 +688,7 @@ k_route_backward(const __grid_constant__ RouteGrad r)
             unsigned has = __ballot_sync(kAll, any);
             any = has >> (lane - me) & (LANES == 32 ? kAll : (1u << (LANES & 31)) - 1u);
 #pragma unroll
-            for (int i = 0; i < V; ++i) out[i] = any && sum > 0.0f ? -(z[i] / sum) * t : any && sum != sum ? sum : 0.0f;
+            for (int i = 0; i < V; ++i) out[i] = any && sum > 0.0f ? -(z[i] * over) * t : any && sum != sum ? sum : 0.0f;
         } else {
 #pragma unroll
             for (int i = 0; i < V; ++i) out[i] = 0.0f;
@@ -659,7 +698,7 @@ k_route_backward(const __grid_constant__ RouteGrad r)
             if (q > 0) { slot(q, e, v, x); l = r.renorm ? log_score(x) : 0.0f; }
             float g;
             if (whole) {
-                g = expf(x - m) / sum * v;
+                g = expf(x - m) * over * v;
             } else {
                 const float rest = soft ? 1.0f : 1.0f / (1.0f + expf(x));          // 1 - s
                 g = r.renorm ? (total != 0.0f ? expf(l - top) / total : 0.0f) * (v - t) * rest : v * rest / (1.0f + expf(-x));
@@ -694,13 +733,16 @@ k_route_backward(const __grid_constant__ RouteGrad r)
     }
 }
 
+// Lanes a row and logits a lane.
 template <typename F> int by_experts(int experts, F f)
 {
-    if (experts <= 32) return f(std::integral_constant<int, 1>{});
-    if (experts <= 64) return f(std::integral_constant<int, 2>{});
-    if (experts <= 128) return f(std::integral_constant<int, 4>{});
-    if (experts <= 256) return f(std::integral_constant<int, 8>{});
-    return f(std::integral_constant<int, 16>{});
+    using std::integral_constant;
+    if (experts <= 16) return f(integral_constant<int, 4>{}, integral_constant<int, 4>{});
+    if (experts <= 32) return f(integral_constant<int, 4>{}, integral_constant<int, 8>{});
+    if (experts <= 64) return f(integral_constant<int, 4>{}, integral_constant<int, 16>{});
+    if (experts <= 128) return f(integral_constant<int, 8>{}, integral_constant<int, 16>{});
+    if (experts <= 256) return f(integral_constant<int, 16>{}, integral_constant<int, 16>{});
+    return f(integral_constant<int, 32>{}, integral_constant<int, 16>{});
 }
 
 // Up to this many rows one block routes and sorts.
@@ -720,6 +762,10 @@ cudaError_t launch_route(F kern, int grid, int threads, int shared, bool early, 
     at[0].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = at;
     cfg.numAttrs = early;
+    if (shared > 48 * 1024) {
+        const cudaError_t rc = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, shared);
+        if (rc != cudaSuccess) return rc;
+    }
     return cudaLaunchKernelEx(&cfg, kern, args...);
 }
 
@@ -757,20 +803,22 @@ extern "C" int gem_nlr_route(const void* logits_dev, int32_t type, int64_t ld, c
     const bool one = one_block(n);
     if (!one && (!scratch_dev || !aligned_to(scratch_dev, 256) || scratch_bytes < gem_nlr_route_scratch_bytes(n, experts))) return GEM_NLR_E_WORKSPACE;
     return by_type(type, [&](auto t) {
-        return by_experts(experts, [&](auto v) {
+        return by_experts(experts, [&](auto lanes, auto v) {
             using T = decltype(t);
-            constexpr int V = v.value, NT = kBlockThreads<V>, WARPS = NT / 32, BYTES = V * (int)sizeof(T) < 16 ? V * (int)sizeof(T) : 16;
-            const int64_t slots = (int64_t)(kBlocks * 512 / NT) * WARPS, per_warp = one ? (n + WARPS - 1) / WARPS : (n + slots - 1) / slots;
-            const int blocks = one ? 1 : (int)((n + per_warp * WARPS - 1) / (per_warp * WARPS));
-            const int size = experts / groups, lanes = size % V ? 0 : size / V;
+            constexpr int LANES = lanes.value, V = v.value, BYTES = V * (int)sizeof(T) < 16 ? V * (int)sizeof(T) : 16;
+            using Sp = Space<LANES, V>;
+            const int64_t slots = (int64_t)kBlocks * kWarps;
+            int64_t per_warp = one ? (n + kWarps - 1) / kWarps : (n + slots - 1) / slots;
+            per_warp = (per_warp + Sp::ROWS - 1) / Sp::ROWS * Sp::ROWS;
+            const int blocks = one ? 1 : (int)((n + per_warp * kWarps - 1) / (per_warp * kWarps));
             const bool wide = aligned_to(logits_dev, BYTES) && ld * (int64_t)sizeof(T) % BYTES == 0;
-            const Route r = {logits_dev, ld, bias_dev, n, experts, k, score, groups, kept_groups, group_best, renormalize, wide, lanes & (lanes - 1) ? 0 : lanes, scale,
-                             expert_dev, weight_dev, offset_dev, row_dev, place_dev, (int32_t*)scratch_dev, per_warp};
-            const int counts = WARPS * experts * 4;
+            const Route r = {logits_dev, ld, bias_dev, n, experts, k, score, groups, kept_groups, group_best, renormalize, wide, scale, expert_dev, weight_dev,
+                             offset_dev, row_dev, place_dev, (int32_t*)scratch_dev, per_warp};
+            const int counts = kWarps * experts * 4, sums = (2 * experts + 1) * 4, space = kWarps * (int)(groups > 1 ? sizeof(Sp) : offsetof(Sp, group)) + 16;
             cudaStream_t st = (cudaStream_t)cuda_stream;
-            if (one) return told(launch_route(k_route<V, T, true>, 1, NT, counts + (2 * experts + 1) * 4, false, st, r));
-            cudaError_t rc = launch_route(k_route<V, T, false>, blocks, NT, counts, false, st, r);
-            if (rc == cudaSuccess) rc = launch_route(k_route_places<NT>, blocks, NT, counts + (3 * experts + 1) * 4, true, st, r, blocks);
+            if (one) return told(launch_route(k_route<LANES, V, T, true>, 1, kThreads, counts + sums + space, false, st, r));
+            cudaError_t rc = launch_route(k_route<LANES, V, T, false>, blocks, kThreads, counts + space, false, st, r);
+            if (rc == cudaSuccess) rc = launch_route(k_route_places, blocks, kThreads, counts + (3 * experts + 1) * 4, true, st, r, blocks);
             return told(rc);
         });
     });
