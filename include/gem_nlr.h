@@ -422,7 +422,7 @@ int gem_nlr_clip_grad_norm(const gem_nlr_tensor *tensors_host, int32_t count, fl
  * row: n k.  1 <= k <= 32, k <= kept_groups experts / groups, experts <= GEM_NLR_MAX_EXPERTS, groups <= 32 and a
  * divisor of experts, n k < 2^31, scale finite.
  * A logit (or bias) of -inf leaves its expert out; where none is left, expert and place are -1 and the weight 0.  A row with a
- * NaN (with softmax: or +inf) goes to no expert and its weights are NaN.  row is -1 behind offset[experts].    */
+ * NaN (with softmax: or +inf) goes to no expert and its weights are NaN; with a NaN in the bias every row does.  row is -1 behind offset[experts].    */
 size_t gem_nlr_route_scratch_bytes(int64_t n, int32_t experts);
 int gem_nlr_route(const void *logits_dev, int32_t type, int64_t ld, const float *bias_dev, int64_t n, int32_t experts,
                   int32_t k, int32_t score, int32_t groups, int32_t kept_groups, int32_t group_best, int32_t renormalize,

@@ -20,7 +20,7 @@
 namespace gemnlr {
 namespace {
 
-constexpr int kThreads = 512, kWarps = kThreads / 32;
+constexpr int kThreads = 1024, kWarps = kThreads / 32;
 constexpr int kBlocks = kTrainSMs;                 // at most
 constexpr int kMaxChosen = 32, kMaxGroups = 32;
 constexpr unsigned kAll = 0xffffffffu;
@@ -168,10 +168,25 @@ __device__ __noinline__ int choose_in_64_bits(const Route& r, int64_t row, int l
     return got;
 }
 
+// 2^x and 1 / x in one instruction each, off by 2^-22 of themselves; subnormal results are 0.
+__device__ __forceinline__ float fast_exp2(float x)
+{
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+__device__ __forceinline__ float fast_inverse(float x)
+{
+    float y;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+constexpr float kLog2E = 1.4426950408889634f;
+
 // ---- the choice by keys -----------------------------------------------------------------------------------------------------------
 
-// How far the choice's FP32 scores can be off: 2^-19 of a score that is at most 1 (the exponential is off by 2^-21 of itself and by
-// its argument's rounding, x exp(-x) <= 0.37; a sum of 16 and 5 steps, a quotient and the sum with the bias add 30 units of 2^-24).
+// How far the choice's FP32 scores can be off: 2^-19 of a score that is at most 1 (the exponential is off by 2^-22 of itself and by
+// its argument's two roundings, x exp(-x) <= 0.37; a sum of 16 and 5 steps, a reciprocal and the sum with the bias add 30 units of 2^-24).
 // Two of them, and what a bias of up to 2^4 adds in rounding, are told apart from 2^-17 on.
 constexpr float kMargin = 0x1p-17f;
 
@@ -218,7 +233,7 @@ __device__ __forceinline__ void load_logits(const T* zr, const Route& r, int me,
     }
 }
 
-// A warp's shared memory: chosen experts, and where there are groups scores and groups' scores.
+// A warp's shared memory: chosen experts, and where there are groups their scores and the experts'.
 template <int LANES, int V> struct Space {
     static constexpr int ROWS = 32 / LANES, PITCH = LANES * V + 4;
     int32_t chosen[ROWS][kMaxChosen];
@@ -226,57 +241,26 @@ template <int LANES, int V> struct Space {
     float score[ROWS][PITCH];
 };
 
-// 32 / LANES rows from `row` on by one warp; rows from `end` on are not there.  The chosen experts are left in sp.chosen.
-template <int LANES, int V, typename T>
-__device__ __forceinline__ void route_rows(const Route& r, int64_t row0, int64_t end, int lane, const float (&bias)[V], Space<LANES, V>& sp)
+// Which groups can be chosen from, a bit each.  c: what the lane's experts' groups are judged by (-inf: none).  close: the border
+// between kept groups and others is nearer than FP32 scores tell.
+template <int LANES, int V>
+__device__ __forceinline__ unsigned kept_groups(const Route& r, const float (&c)[V], int size, int me, int mine, Space<LANES, V>& sp, bool scored, bool& close)
 {
-    constexpr int PAD = LANES * V;
-    constexpr uint32_t INDEX = PAD - 1;                   // the key's lower bits: PAD - 1 - index
-    constexpr int BITS = PAD == 16 ? 4 : PAD == 32 ? 5 : PAD == 64 ? 6 : PAD == 128 ? 7 : PAD == 256 ? 8 : 9;
-    const int me = lane % LANES, mine = lane / LANES;
-    const int64_t row = row0 + mine;
-    const bool in = row < end;
-    const T* zr = reinterpret_cast<const T*>(r.z) + (in ? row : row0) * r.ld;
-    const bool soft = r.score == GEM_NLR_SOFTMAX, biased = r.bias;
-    const bool scored = biased || (r.groups > 1 && r.best == 2);          // the choice needs the scores
-    const unsigned row_lanes = (LANES == 32 ? kAll : (1u << (LANES & 31)) - 1u) << (lane - me);
-    float z[V], m = -INFINITY, sum = 0.0f;
-    load_logits<V>(zr, r, me, z);
-    bool bad = false;
+    const int lanes = size / V;                          // that hold a group
+    if (size % V == 0 && (lanes & (lanes - 1)) == 0) {
+        float first = c[0], second = -INFINITY;
 #pragma unroll
-    for (int v = 0; v < V; ++v) {
-        bad |= !(z[v] < INFINITY) && (soft || z[v] != INFINITY);
-        m = fmaxf(m, z[v]);
-    }
-    if (soft && (scored || !r.renorm)) m = lanes_top<LANES>(m);
-    float c[V];                                          // scores with their biases, or logits
-    if (scored) {
-        if (soft) {
-#pragma unroll
-            for (int v = 0; v < V; ++v) {
-                c[v] = z[v] == -INFINITY ? 0.0f : __expf(z[v] - m);
-                sum += c[v];
-            }
-            const float over = __fdividef(1.0f, lanes_sum<LANES>(sum));
-#pragma unroll
-            for (int v = 0; v < V; ++v) c[v] *= over;
-        } else {
-#pragma unroll
-            for (int v = 0; v < V; ++v) c[v] = __fdividef(1.0f, 1.0f + __expf(-z[v]));
+        for (int v = 1; v < V; ++v) {
+            second = fmaxf(second, fminf(first, c[v]));
+            first = fmaxf(first, c[v]);
         }
-#pragma unroll
-        for (int v = 0; v < V; ++v) {
-            c[v] = z[v] == -INFINITY ? -INFINITY : c[v] + bias[v];
-            bad |= c[v] != c[v];
+        for (int o = 1; o < lanes; o *= 2) {
+            const float a = __shfl_xor_sync(kAll, first, o), b = __shfl_xor_sync(kAll, second, o);
+            second = fmaxf(fminf(first, a), fmaxf(second, b));
+            first = fmaxf(first, a);
         }
+        if (me % lanes == 0 && me / lanes < r.groups) sp.group[mine][me / lanes] = (r.best == 2 && second != -INFINITY ? first + second : first) + 0.0f;
     } else {
-#pragma unroll
-        for (int v = 0; v < V; ++v) c[v] = z[v];
-    }
-    bool unsure = false;
-    unsigned stays = kAll;                               // groups that can be chosen
-    if (r.groups > 1) {
-        const int size = r.experts / r.groups;
 #pragma unroll
         for (int v = 0; v < V; v += 4) *reinterpret_cast<float4*>(&sp.score[mine][me * V + v]) = make_float4(c[v], c[v + 1], c[v + 2], c[v + 3]);
         __syncwarp();
@@ -291,48 +275,121 @@ __device__ __forceinline__ void route_rows(const Route& r, int64_t row0, int64_t
             }
             sp.group[mine][g] = (r.best == 2 && second != -INFINITY ? first + second : first) + 0.0f;
         }
-        __syncwarp();
-        unsigned kept = 0;
-        float low = INFINITY, high = -INFINITY;          // the lowest group kept and the highest of the others
-        for (int g = me; g < r.groups; g += LANES) {
-            const float x = sp.group[mine][g];
-            int rank = 0;
-#pragma unroll 4
-            for (int o = 0; o < r.groups; ++o) {
-                const float y = sp.group[mine][o];
-                rank += y > x || (y == x && o < g);
-            }
-            if (rank < r.kept) {
-                kept |= 1u << g;
-                low = fminf(low, x);
-            } else {
-                high = fmaxf(high, x);
-            }
-        }
-#pragma unroll
-        for (int o = LANES / 2; o > 0; o >>= 1) {
-            kept |= __shfl_xor_sync(kAll, kept, o);
-            low = fminf(low, __shfl_xor_sync(kAll, low, o));
-            high = fmaxf(high, __shfl_xor_sync(kAll, high, o));
-        }
-        stays = kept;
-        unsure = scored && high != -INFINITY && !(low - high > 2.0f * kMargin + 0x1p-20f * fabsf(low));
     }
+    __syncwarp();
+    unsigned kept = 0;
+    float low = INFINITY, high = -INFINITY;              // the lowest group kept and the highest of the others
+    for (int g = me; g < r.groups; g += LANES) {
+        const float x = sp.group[mine][g];
+        int rank = 0;
+#pragma unroll 4
+        for (int o = 0; o < r.groups; ++o) {
+            const float y = sp.group[mine][o];
+            rank += y > x || (y == x && o < g);
+        }
+        if (rank < r.kept) {
+            kept |= 1u << g;
+            low = fminf(low, x);
+        } else {
+            high = fmaxf(high, x);
+        }
+    }
+#pragma unroll
+    for (int o = LANES / 2; o > 0; o >>= 1) {
+        kept |= __shfl_xor_sync(kAll, kept, o);
+        low = fminf(low, __shfl_xor_sync(kAll, low, o));
+        high = fmaxf(high, __shfl_xor_sync(kAll, high, o));
+    }
+    close = scored && high != -INFINITY && !(low - high > 2.0f * kMargin + 0x1p-20f * fabsf(low));
+    return kept;
+}
+
+// 32 / LANES rows from `row0` on by one warp; rows from `end` on are not there.  bias: LANES * V in shared memory (0 behind the last);
+// counts: of the warp's rows by expert.
+template <int LANES, int V, typename T>
+__device__ __forceinline__ void route_rows(const Route& r, int64_t row0, int64_t end, int lane, const float* bias, bool bias_fine, int32_t* counts, Space<LANES, V>& sp)
+{
+    constexpr int PAD = LANES * V;
+    constexpr uint32_t INDEX = PAD - 1;                   // the key's lower bits: PAD - 1 - index
+    constexpr int BITS = PAD == 16 ? 4 : PAD == 32 ? 5 : PAD == 64 ? 6 : PAD == 128 ? 7 : PAD == 256 ? 8 : 9;
+    constexpr float STEP = (float)(1u << (30 - BITS));    // a biased score's steps of its key in one
+    const int me = lane % LANES, mine = lane / LANES;
+    const int64_t row = row0 + mine;
+    const bool in = row < end;
+    const T* zr = reinterpret_cast<const T*>(r.z) + (in ? row : row0) * r.ld;
+    const bool soft = r.score == GEM_NLR_SOFTMAX, biased = r.bias;
+    const bool scored = biased || (r.groups > 1 && r.best == 2);          // the choice needs the scores
+    const unsigned row_lanes = (LANES == 32 ? kAll : (1u << (LANES & 31)) - 1u) << (lane - me);
+    float z[V], m = -INFINITY, sum = 0.0f;
+    load_logits<V>(zr, r, me, z);
+    if (soft && (scored || !r.renorm)) {
+#pragma unroll
+        for (int v = 0; v < V; ++v) m = fmaxf(m, z[v]);
+        m = lanes_top<LANES>(m);
+    }
+    float whole = 1.0f;                                  // softmax without renormalization: the sum of the exponentials
+    if (soft && !r.renorm) {
+        whole = 0.0f;
+#pragma unroll
+        for (int v = 0; v < V; ++v) whole += z[v] == -INFINITY ? 0.0f : expf(z[v] - m);
+        whole = lanes_sum<LANES>(whole);
+    }
+    bool bad = false;
     uint32_t key[V];
-    if (biased) {
-        // in steps of 2^(BITS - 30) from two below the largest on; lower ones come out equal
-        float top = -INFINITY;
+    bool unsure = false;
+    unsigned stays = kAll;                               // groups that can be chosen
+    const int size = r.experts / r.groups;
+    bool nothing = false;                                // no expert is left
+    if (scored) {
+        float c[V];                                      // scores; a NaN (softmax: an infinity) comes out in their sum
+        if (soft) {
 #pragma unroll
-        for (int v = 0; v < V; ++v) top = fmaxf(top, c[v]);
-        top = lanes_top<LANES>(top);
-        const float from = top - 2.0f;
-        unsure |= fabsf(top) > 16.0f && top != -INFINITY;
+            for (int v = 0; v < V; ++v) {
+                c[v] = z[v] == -INFINITY ? 0.0f : fast_exp2((z[v] - m) * kLog2E);
+                sum += c[v];
+            }
+            sum = lanes_sum<LANES>(sum);
+            const float over = fast_inverse(sum);
 #pragma unroll
-        for (int v = 0; v < V; ++v) {
-            const uint32_t q = (uint32_t)__float2uint_rn(fmaxf(c[v] - from, 0.0f) * (float)(1u << (31 - BITS - 1)));
-            key[v] = c[v] == -INFINITY ? 0u : (q + 1u) << BITS | (INDEX - (uint32_t)(me * V + v));
+            for (int v = 0; v < V; ++v) c[v] *= over;
+        } else {
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                c[v] = fast_inverse(1.0f + fast_exp2(z[v] * -kLog2E));
+                sum += c[v];
+            }
+        }
+        bad = sum != sum || !bias_fine;
+#pragma unroll
+        for (int v = 0; v < V; v += 4) {
+            const float4 b = *reinterpret_cast<const float4*>(bias + me * V + v);
+            c[v] = z[v] == -INFINITY ? -INFINITY : c[v] + b.x;
+            c[v + 1] = z[v + 1] == -INFINITY ? -INFINITY : c[v + 1] + b.y;
+            c[v + 2] = z[v + 2] == -INFINITY ? -INFINITY : c[v + 2] + b.z;
+            c[v + 3] = z[v + 3] == -INFINITY ? -INFINITY : c[v + 3] + b.w;
+        }
+        if (r.groups > 1) stays = kept_groups<LANES, V>(r, c, size, me, mine, sp, true, unsure);
+        if (biased) {
+            // Fixed point from two below the largest on.  Step 0 is what lies lower, or cannot be chosen: where the choice
+            // comes to it, it is made in FP64.
+            float top = c[0];
+#pragma unroll
+            for (int v = 1; v < V; ++v) top = fmaxf(top, c[v]);
+            top = lanes_top<LANES>(top);
+            nothing = top == -INFINITY;
+            unsure |= fabsf(top) > 16.0f;
+            const float from = (2.0f - top) * STEP;
+            const uint32_t own = INDEX - (uint32_t)(me * V);
+#pragma unroll
+            for (int v = 0; v < V; ++v) key[v] = (__float2uint_rn(fmaf(c[v], STEP, from)) << BITS) + own - v;
         }
     } else {
+#pragma unroll
+        for (int v = 0; v < V; ++v) bad |= soft ? !(z[v] < INFINITY) : z[v] != z[v];
+        if (r.groups > 1) stays = kept_groups<LANES, V>(r, z, size, me, mine, sp, false, unsure);
+    }
+    if (!biased) {
+        // the logit's upper bits: of 16-bit types all of them
 #pragma unroll
         for (int v = 0; v < V; ++v) {
             const uint32_t k = key_of(z[v]);
@@ -340,12 +397,18 @@ __device__ __forceinline__ void route_rows(const Route& r, int64_t row0, int64_t
         }
     }
     if (r.groups > 1) {
-        const int size = r.experts / r.groups;
-        int g = me * V / size, next = (g + 1) * size - me * V;               // the group of v, and the v where the next begins
+        if (size % V == 0) {
+            if (!(stays >> (me * V / size & 31) & 1u)) {
 #pragma unroll
-        for (int v = 0; v < V; ++v) {
-            if (v == next) { ++g; next += size; }
-            if (!(stays >> (g & 31) & 1u)) key[v] = 0u;
+                for (int v = 0; v < V; ++v) key[v] = 0u;
+            }
+        } else {
+            int g = me * V / size, next = (g + 1) * size - me * V;           // the group of v, and the v where the next begins
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                if (v == next) { ++g; next += size; }
+                if (!(stays >> (g & 31) & 1u)) key[v] = 0u;
+            }
         }
     }
     sort_keys<V>(key);
@@ -355,17 +418,15 @@ __device__ __forceinline__ void route_rows(const Route& r, int64_t row0, int64_t
         uint32_t best = key[0];
 #pragma unroll
         for (int o = LANES / 2; o > 0; o >>= 1) best = max(best, __shfl_xor_sync(kAll, best, o));
-        const int index = best ? (int)(INDEX - (best & INDEX)) : -1;
-        if (best && j > 0) {
-            const uint32_t a = last >> BITS, b = best >> BITS;
-            if (biased ? a - b <= (uint32_t)(kMargin * (float)(1u << (31 - BITS - 1))) : a == b) {
-                const int before = (int)(INDEX - (last & INDEX));
-                unsure |= !(to_f(zr[before]) == to_f(zr[index]) && (!biased || __ldg(r.bias + before) == __ldg(r.bias + index)));
-            }
+        const uint32_t a = last >> BITS, b = best >> BITS;
+        if (j > 0 && a - b <= (biased ? (uint32_t)(kMargin * STEP) : 0u) && b) {
+            const int before = (int)(INDEX - (last & INDEX)), index = (int)(INDEX - (best & INDEX));
+            unsure |= !(to_f(zr[before]) == to_f(zr[index]) && (!biased || bias[before] == bias[index]));
         }
-        last = best;
         if (j == r.k) break;
-        if (me == 0) sp.chosen[mine][j] = index;
+        unsure |= biased && b == 0u;
+        if (me == 0) sp.chosen[mine][j] = b ? (int)(INDEX - (best & INDEX)) : -1;
+        last = best;
         if (key[0] == best) {
             if (few) {
 #pragma unroll
@@ -379,7 +440,7 @@ __device__ __forceinline__ void route_rows(const Route& r, int64_t row0, int64_t
         }
     }
     bad = (__ballot_sync(kAll, bad) & row_lanes) != 0;
-    unsure = unsure && !bad && in;
+    unsure = unsure && !bad && in && !nothing;
     __syncwarp();
     for (unsigned rows = __ballot_sync(kAll, unsure && me == 0); rows; rows &= rows - 1) {
         const int which = (__ffs(rows) - 1) / LANES;
@@ -387,53 +448,65 @@ __device__ __forceinline__ void route_rows(const Route& r, int64_t row0, int64_t
         if (lane < r.k) sp.chosen[which][lane] = got;
     }
     __syncwarp();
-    // weights: slot j by lane j mod LANES of its row
+    // Weights: slot j by lane j mod LANES of its row.  The first of a lane's slots, which mostly is its only one, stays in registers.
+    const auto slot = [&](int j, int& e, float& x) {
+        e = j < r.k && !bad ? sp.chosen[mine][j] : -1;
+        x = e >= 0 ? to_f(zr[e]) : 0.0f;
+    };
     const auto logistic = [](float x) { return 1.0f / (1.0f + expf(-x)); };
-    float top = -INFINITY, total = 0.0f;
-    if (!soft && r.renorm) {
-        for (int j = me; j < r.k; j += LANES) {
-            const int e = sp.chosen[mine][j];
-            if (e >= 0) total += logistic(to_f(zr[e]));
-        }
-        total = lanes_sum<LANES>(total);
-    }
-    // s_j / sum s as a softmax over the chosen logits, or where the scores underflow over their logarithms
-    const bool far = !soft && total < 1e-30f;
     const auto log_score = [&](float x) { return soft ? x : fminf(x, 0.0f) - log1pf(expf(-fabsf(x))); };
-    if (r.renorm && __any_sync(kAll, soft || far)) {
-        for (int j = me; j < r.k; j += LANES) {
-            const int e = sp.chosen[mine][j];
-            if (e >= 0) top = fmaxf(top, log_score(to_f(zr[e])));
+    int e0;
+    float x0, s0, total = 1.0f, top = m;
+    slot(me, e0, x0);
+    s0 = !soft && e0 >= 0 ? logistic(x0) : 0.0f;
+    bool logs = soft;                                    // scores from their logarithms (softmax: from the logits), relative to `top`
+    if (r.renorm) {
+        if (!soft) {
+            total = s0;
+            for (int j = me + LANES; j < r.k; j += LANES) {
+                int e; float x;
+                slot(j, e, x);
+                if (e >= 0) total += logistic(x);
+            }
+            total = lanes_sum<LANES>(total);
+            logs = total < 1e-30f;                       // they underflow
         }
-        top = lanes_top<LANES>(top);
-        float t = 0.0f;
-        for (int j = me; j < r.k; j += LANES) {
-            const int e = sp.chosen[mine][j];
-            if (e >= 0) t += expf(log_score(to_f(zr[e])) - top);
+        if (__any_sync(kAll, logs)) {
+            const float l0 = e0 >= 0 ? log_score(x0) : -INFINITY;
+            top = l0;
+            for (int j = me + LANES; j < r.k; j += LANES) {
+                int e; float x;
+                slot(j, e, x);
+                if (e >= 0) top = fmaxf(top, log_score(x));
+            }
+            top = lanes_top<LANES>(top);
+            float t = e0 >= 0 ? expf(l0 - top) : 0.0f;
+            if (logs) s0 = t;
+            for (int j = me + LANES; j < r.k; j += LANES) {
+                int e; float x;
+                slot(j, e, x);
+                if (e >= 0) t += expf(log_score(x) - top);
+            }
+            t = lanes_sum<LANES>(t);
+            if (logs) total = t;
         }
-        t = lanes_sum<LANES>(t);
-        if (soft || far) total = t;
-    }
-    if (soft && !r.renorm) {
-        sum = 0.0f;
-#pragma unroll
-        for (int v = 0; v < V; ++v) sum += z[v] == -INFINITY ? 0.0f : expf(z[v] - m);
-        total = lanes_sum<LANES>(sum);
-        top = m;
+    } else if (soft) {
+        total = whole;
+        if (e0 >= 0) s0 = expf(x0 - m);
     }
     for (int j = me; j < r.k; j += LANES) {
-        const int e = bad ? -1 : sp.chosen[mine][j];
-        float w = bad ? __uint_as_float(0x7fc00000u) : 0.0f;
-        if (e >= 0) {
-            const float x = to_f(zr[e]);
-            const float s = soft || (r.renorm && far) ? expf(log_score(x) - top) : logistic(x);
-            w = (soft || r.renorm ? s / total : s) * r.scale;
+        int e = e0;
+        float s = s0;
+        if (j != me) {
+            float x;
+            slot(j, e, x);
+            s = logs ? expf(log_score(x) - top) : logistic(x);
         }
         if (in) {
             r.expert[row * r.k + j] = e;
-            r.weight[row * r.k + j] = w;
+            r.weight[row * r.k + j] = bad ? __uint_as_float(0x7fc00000u) : e < 0 ? 0.0f : s / total * r.scale;
+            if (e >= 0) atomicAdd(counts + e, 1);
         }
-        sp.chosen[mine][j] = in ? e : -1;
     }
     __syncwarp();
 }
@@ -495,7 +568,7 @@ __device__ __forceinline__ void leave_rest(const Route& r, int32_t used)
     for (int64_t p = used + (int64_t)blockIdx.x * kThreads + threadIdx.x; p < r.n * r.k; p += (int64_t)gridDim.x * kThreads) r.row[p] = -1;
 }
 
-// Shared memory: warps x experts counts; ONE: and experts + 1 sums and experts totals; then the warps' space.
+// Shared memory: warps x experts counts; ONE: and experts + 1 sums and experts totals; then the biases and the warps' space.
 template <int LANES, int V, typename T, bool ONE>
 __global__ void __launch_bounds__(kThreads)
 k_route(const __grid_constant__ Route r)
@@ -504,23 +577,17 @@ k_route(const __grid_constant__ Route r)
     extern __shared__ int32_t at[];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int before = kWarps * r.experts + (ONE ? 2 * r.experts + 1 : 0);
-    char* space = reinterpret_cast<char*>(at) + ((size_t)before * 4 + 15) / 16 * 16;
-    Sp& sp = *reinterpret_cast<Sp*>(space + (size_t)warp * (r.groups > 1 ? sizeof(Sp) : offsetof(Sp, group)));
+    float* bias = reinterpret_cast<float*>(at) + (before + 3) / 4 * 4;
+    Sp& sp = *reinterpret_cast<Sp*>(reinterpret_cast<char*>(bias + LANES * V) + (size_t)warp * (r.groups > 1 ? sizeof(Sp) : offsetof(Sp, group)));
     for (int i = threadIdx.x; i < kWarps * r.experts; i += kThreads) at[i] = 0;
-    __syncthreads();
     const int64_t begin = min(r.n, ((int64_t)blockIdx.x * kWarps + warp) * r.rows_per_warp), end = min(r.n, begin + r.rows_per_warp);
-    int32_t* mine = at + warp * r.experts;
-    float bias[V];
-#pragma unroll
-    for (int v = 0; v < V; ++v) bias[v] = r.bias && lane % LANES * V + v < r.experts ? __ldg(r.bias + lane % LANES * V + v) : 0.0f;
-    for (int64_t row = begin; row < end; row += Sp::ROWS) {
-        route_rows<LANES, V, T>(r, row, end, lane, bias, sp);
-        for (int j = lane; j < Sp::ROWS * r.k; j += 32) {
-            const int e = sp.chosen[j / r.k][j % r.k];
-            if (e >= 0) atomicAdd(mine + e, 1);
-        }
-        __syncwarp();
+    bool fine = true;
+    for (int i = threadIdx.x; i < LANES * V; i += kThreads) {
+        bias[i] = r.bias && i < r.experts ? __ldg(r.bias + i) : 0.0f;
+        fine = bias[i] == bias[i];
     }
+    fine = __syncthreads_and(fine);
+    for (int64_t row = begin; row < end; row += Sp::ROWS) route_rows<LANES, V, T>(r, row, end, lane, bias, fine, at + warp * r.experts, sp);
     __syncthreads();
     next_may_start();
     int32_t* first = at + kWarps * r.experts;
@@ -552,16 +619,12 @@ k_route_places(const __grid_constant__ Route r, int blocks)
     __syncthreads();
     const int64_t begin = min(r.n, ((int64_t)blockIdx.x * kWarps + warp) * r.rows_per_warp), end = min(r.n, begin + r.rows_per_warp);
     grid_ready();
-    for (int64_t i = begin * r.k + lane; i < end * r.k; i += 32) {
-        const int e = r.expert[i];
-        if (e >= 0) atomicAdd(at + warp * r.experts + e, 1);
-    }
     // threads in pairs (expert, share of the blocks); whole numbers: the order of the additions does not show
     const int shares = max(1, kThreads / r.experts), share = threadIdx.x / r.experts;
     if (share < shares)
         for (int e = threadIdx.x % r.experts; e < r.experts; e += kThreads) {
             int32_t all = 0, low = 0;
-#pragma unroll 8
+#pragma unroll 16
             for (int b = share; b < blocks; b += shares) {
                 const int32_t c = r.counts[(int64_t)b * r.experts + e];
                 all += c;
@@ -570,6 +633,10 @@ k_route_places(const __grid_constant__ Route r, int blocks)
             atomicAdd(total + e, all);
             atomicAdd(before + e, low);
         }
+    for (int64_t i = begin * r.k + lane; i < end * r.k; i += 32) {
+        const int e = r.expert[i];
+        if (e >= 0) atomicAdd(at + warp * r.experts + e, 1);
+    }
     __syncthreads();
     sums_over_experts(total, first, r.experts);
     if (blockIdx.x == 0)
@@ -814,7 +881,7 @@ extern "C" int gem_nlr_route(const void* logits_dev, int32_t type, int64_t ld, c
             const bool wide = aligned_to(logits_dev, BYTES) && ld * (int64_t)sizeof(T) % BYTES == 0;
             const Route r = {logits_dev, ld, bias_dev, n, experts, k, score, groups, kept_groups, group_best, renormalize, wide, scale, expert_dev, weight_dev,
                              offset_dev, row_dev, place_dev, (int32_t*)scratch_dev, per_warp};
-            const int counts = kWarps * experts * 4, sums = (2 * experts + 1) * 4, space = kWarps * (int)(groups > 1 ? sizeof(Sp) : offsetof(Sp, group)) + 16;
+            const int counts = kWarps * experts * 4, sums = (2 * experts + 1) * 4, space = LANES * V * 4 + kWarps * (int)(groups > 1 ? sizeof(Sp) : offsetof(Sp, group)) + 16;
             cudaStream_t st = (cudaStream_t)cuda_stream;
             if (one) return told(launch_route(k_route<LANES, V, T, true>, 1, kThreads, counts + sums + space, false, st, r));
             cudaError_t rc = launch_route(k_route<LANES, V, T, false>, blocks, kThreads, counts + space, false, st, r);
