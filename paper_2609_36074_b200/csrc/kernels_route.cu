@@ -12,9 +12,8 @@
 // taken from the chosen logits anew.
 //
 // The order is a counting sort that keeps the rows of an expert in order, without atomics whose order shows: blocks own
-// consecutive rows and count their experts; the second kernel adds the counts of the blocks before (each block reads all of
-// them, 148 x experts numbers), takes sums over the experts, and gives out places in order, a warp's 32 entries at a time by
-// matching equal experts.  Few rows are one block and one launch.
+// consecutive rows, count their experts and rank their entries; the second kernel adds the counts of the blocks before (each
+// block reads all of them, 148 x experts numbers) and the sums over the experts.  Few rows are one block and one launch.
 #include "expert_common.cuh"
 
 namespace gemnlr {
@@ -54,7 +53,6 @@ __device__ __forceinline__ uint64_t key_of(double c)
     return u >> 63 ? ~u : u | 1ull << 63;
 }
 constexpr uint32_t kNone32 = 0x007fffffu;                   // -inf
-constexpr uint64_t kNone64 = 0x000fffffffffffffull;
 
 __device__ __forceinline__ uint64_t warp_max(uint64_t k)
 {
@@ -71,6 +69,7 @@ __device__ __forceinline__ float warp_top(float v)
     return t;
 }
 
+// Over LANES neighbouring lanes.
 template <int LANES> __device__ __forceinline__ float lanes_sum(float v)
 {
 #pragma unroll
@@ -84,373 +83,15 @@ template <int LANES> __device__ __forceinline__ float lanes_top(float v)
     return v;
 }
 
-// ---- the choice in FP64, a row by a warp: experts lane * V + v -------------------------------------------------------------------
-// Lane j returns the j-th chosen expert, -1 for none.
-template <int V, typename T>
-__device__ __noinline__ int choose_in_64_bits(const Route& r, int64_t row, int lane)
+// A row's weights, by LANES lanes; the expert counts take the row in where `in`.  m, whole: softmax without renormalization, the
+// largest logit and the sum of the exponentials.
+template <int LANES, typename T>
+__device__ __forceinline__ void take_weights(const Route& r, int64_t row, bool in, bool bad, const T* zr, float m, float whole, const int32_t* chosen, int me, int32_t* counts)
 {
-    const T* zr = reinterpret_cast<const T*>(r.z) + row * r.ld;
     const bool soft = r.score == GEM_NLR_SOFTMAX;
-    const double none = -(double)INFINITY;
-    float z[V], m = -INFINITY;
-    double s[V], sum = 0.0;
-#pragma unroll
-    for (int v = 0; v < V; ++v) {
-        z[v] = lane * V + v < r.experts ? to_f(zr[lane * V + v]) : -INFINITY;
-        m = fmaxf(m, z[v]);
-    }
-    m = warp_top(m);
-#pragma unroll
-    for (int v = 0; v < V; ++v) {
-        s[v] = z[v] == -INFINITY ? 0.0 : soft ? exp((double)z[v] - (double)m) : 1.0 / (1.0 + exp(-(double)z[v]));
-        sum += s[v];
-    }
-    sum = warp_sum(sum);
-    uint64_t key[V];
-    double by[V];                                        // what a group is judged by
-#pragma unroll
-    for (int v = 0; v < V; ++v) {
-        const int i = lane * V + v;
-        if (soft) s[v] /= sum;
-        double x = r.bias ? s[v] + (double)(i < r.experts ? __ldg(r.bias + i) : 0.f) : (double)z[v];
-        if (z[v] == -INFINITY) x = none;
-        key[v] = i < r.experts ? key_of(x) : 0;
-        by[v] = z[v] == -INFINITY ? none : r.bias || r.best == 1 ? x : s[v];
-    }
-    if (r.groups > 1) {
-        const int size = r.experts / r.groups;
-        double mine = none;                              // lane g: group g's score
-        for (int g = 0; g < r.groups; ++g) {
-            double first = none, second = none;
-#pragma unroll
-            for (int v = 0; v < V; ++v) {
-                const int i = lane * V + v;
-                const double x = i >= g * size && i < (g + 1) * size ? by[v] : none;
-                second = fmax(second, fmin(first, x));
-                first = fmax(first, x);
-            }
-#pragma unroll
-            for (int o = 1; o < 32; o *= 2) {
-                const double a = __shfl_xor_sync(kAll, first, o), b = __shfl_xor_sync(kAll, second, o);
-                second = fmax(fmin(first, a), fmax(second, b));
-                first = fmax(first, a);
-            }
-            if (lane == g) mine = r.best == 2 && second != none ? first + second : first;
-        }
-        int rank = 0;
-        for (int g = 0; g < r.groups; ++g) {
-            const double other = __shfl_sync(kAll, mine, g);
-            rank += other > mine || (other == mine && g < lane);
-        }
-        const unsigned stays = __ballot_sync(kAll, lane < r.groups && rank < r.kept);
-#pragma unroll
-        for (int v = 0; v < V; ++v)
-            if (!(stays >> min((lane * V + v) / size, 31) & 1u)) key[v] = 0;
-    }
-    int got = -1;
-    for (int j = 0; j < r.k; ++j) {
-        uint64_t top = key[0];
-        int at = 0;
-#pragma unroll
-        for (int v = 1; v < V; ++v)
-            if (key[v] > top) { top = key[v]; at = v; }
-        const uint64_t best = warp_max(top);
-        if (best <= kNone64) break;
-        const int owner = __ffs(__ballot_sync(kAll, top == best)) - 1;
-        const int index = owner * V + __shfl_sync(kAll, at, owner);
-        if (lane == j) got = index;
-        if (lane == owner) {
-#pragma unroll
-            for (int v = 0; v < V; ++v)
-                if (v == at) key[v] = 0;
-        }
-    }
-    return got;
-}
-
-// 2^x and 1 / x in one instruction each, off by 2^-22 of themselves; subnormal results are 0.
-__device__ __forceinline__ float fast_exp2(float x)
-{
-    float y;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-    return y;
-}
-__device__ __forceinline__ float fast_inverse(float x)
-{
-    float y;
-    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-    return y;
-}
-constexpr float kLog2E = 1.4426950408889634f;
-
-// ---- the choice by keys -----------------------------------------------------------------------------------------------------------
-
-// How far the choice's FP32 scores can be off: 2^-19 of a score that is at most 1 (the exponential is off by 2^-22 of itself and by
-// its argument's two roundings, x exp(-x) <= 0.37; a sum of 16 and 5 steps, a reciprocal and the sum with the bias add 30 units of 2^-24).
-// Two of them, and what a bias of up to 2^4 adds in rounding, are told apart from 2^-17 on.
-constexpr float kMargin = 0x1p-17f;
-
-// Largest first.  (Batcher's merge exchange; a network for a power of two.)
-template <int V>
-__device__ __forceinline__ void sort_keys(uint32_t (&key)[V])
-{
-#pragma unroll
-    for (int p = V / 2; p > 0; p /= 2) {
-#pragma unroll
-        for (int q = V / 2, r = 0, d = p; d > 0;) {
-#pragma unroll
-            for (int i = 0; i + d < V; ++i)
-                if ((i & p) == r) {
-                    const uint32_t a = key[i], b = key[i + d];
-                    key[i] = max(a, b);
-                    key[i + d] = min(a, b);
-                }
-            d = q > p ? q - p : 0;
-            q /= 2;
-            r = p;
-        }
-    }
-}
-
-// A lane's V logits, experts me * V + v.
-template <int V, typename T>
-__device__ __forceinline__ void load_logits(const T* zr, const Route& r, int me, float (&z)[V])
-{
-    constexpr int BYTES = V * (int)sizeof(T);
-    if (r.wide && me * V + V <= r.experts) {
-        uint32_t w[BYTES / 4];
-        if constexpr (BYTES >= 16) {
-#pragma unroll
-            for (int i = 0; i < BYTES / 16; ++i) *reinterpret_cast<uint4*>(w + 4 * i) = __ldg(reinterpret_cast<const uint4*>(zr + me * V) + i);
-        } else {
-            *reinterpret_cast<uint2*>(w) = __ldg(reinterpret_cast<const uint2*>(zr + me * V));
-        }
-#pragma unroll
-        for (int v = 0; v < V; ++v) z[v] = to_f(reinterpret_cast<const T*>(w)[v]);
-    } else {
-#pragma unroll
-        for (int v = 0; v < V; ++v) z[v] = me * V + v < r.experts ? to_f(zr[me * V + v]) : -INFINITY;
-    }
-}
-
-// A warp's shared memory: chosen experts, and where there are groups their scores and the experts'.
-template <int LANES, int V> struct Space {
-    static constexpr int ROWS = 32 / LANES, PITCH = LANES * V + 4;
-    int32_t chosen[ROWS][kMaxChosen];
-    float group[ROWS][kMaxGroups];
-    float score[ROWS][PITCH];
-};
-
-// Which groups can be chosen from, a bit each.  c: what the lane's experts' groups are judged by (-inf: none).  close: the border
-// between kept groups and others is nearer than FP32 scores tell.
-template <int LANES, int V>
-__device__ __forceinline__ unsigned kept_groups(const Route& r, const float (&c)[V], int size, int me, int mine, Space<LANES, V>& sp, bool scored, bool& close)
-{
-    const int lanes = size / V;                          // that hold a group
-    if (size % V == 0 && (lanes & (lanes - 1)) == 0) {
-        float first = c[0], second = -INFINITY;
-#pragma unroll
-        for (int v = 1; v < V; ++v) {
-            second = fmaxf(second, fminf(first, c[v]));
-            first = fmaxf(first, c[v]);
-        }
-        for (int o = 1; o < lanes; o *= 2) {
-            const float a = __shfl_xor_sync(kAll, first, o), b = __shfl_xor_sync(kAll, second, o);
-            second = fmaxf(fminf(first, a), fmaxf(second, b));
-            first = fmaxf(first, a);
-        }
-        if (me % lanes == 0 && me / lanes < r.groups) sp.group[mine][me / lanes] = (r.best == 2 && second != -INFINITY ? first + second : first) + 0.0f;
-    } else {
-#pragma unroll
-        for (int v = 0; v < V; v += 4) *reinterpret_cast<float4*>(&sp.score[mine][me * V + v]) = make_float4(c[v], c[v + 1], c[v + 2], c[v + 3]);
-        __syncwarp();
-        for (int g = me; g < r.groups; g += LANES) {
-            float first = -INFINITY, second = -INFINITY;
-            const float* of = &sp.score[mine][g * size];
-#pragma unroll 4
-            for (int i = 0; i < size; ++i) {
-                const float x = of[i];
-                second = fmaxf(second, fminf(first, x));
-                first = fmaxf(first, x);
-            }
-            sp.group[mine][g] = (r.best == 2 && second != -INFINITY ? first + second : first) + 0.0f;
-        }
-    }
-    __syncwarp();
-    unsigned kept = 0;
-    float low = INFINITY, high = -INFINITY;              // the lowest group kept and the highest of the others
-    for (int g = me; g < r.groups; g += LANES) {
-        const float x = sp.group[mine][g];
-        int rank = 0;
-#pragma unroll 4
-        for (int o = 0; o < r.groups; ++o) {
-            const float y = sp.group[mine][o];
-            rank += y > x || (y == x && o < g);
-        }
-        if (rank < r.kept) {
-            kept |= 1u << g;
-            low = fminf(low, x);
-        } else {
-            high = fmaxf(high, x);
-        }
-    }
-#pragma unroll
-    for (int o = LANES / 2; o > 0; o >>= 1) {
-        kept |= __shfl_xor_sync(kAll, kept, o);
-        low = fminf(low, __shfl_xor_sync(kAll, low, o));
-        high = fmaxf(high, __shfl_xor_sync(kAll, high, o));
-    }
-    close = scored && high != -INFINITY && !(low - high > 2.0f * kMargin + 0x1p-20f * fabsf(low));
-    return kept;
-}
-
-// 32 / LANES rows from `row0` on by one warp; rows from `end` on are not there.  bias: LANES * V in shared memory (0 behind the last);
-// counts: of the warp's rows by expert.
-template <int LANES, int V, typename T>
-__device__ __forceinline__ void route_rows(const Route& r, int64_t row0, int64_t end, int lane, const float* bias, bool bias_fine, int32_t* counts, Space<LANES, V>& sp)
-{
-    constexpr int PAD = LANES * V;
-    constexpr uint32_t INDEX = PAD - 1;                   // the key's lower bits: PAD - 1 - index
-    constexpr int BITS = PAD == 16 ? 4 : PAD == 32 ? 5 : PAD == 64 ? 6 : PAD == 128 ? 7 : PAD == 256 ? 8 : 9;
-    constexpr float STEP = (float)(1u << (30 - BITS));    // a biased score's steps of its key in one
-    const int me = lane % LANES, mine = lane / LANES;
-    const int64_t row = row0 + mine;
-    const bool in = row < end;
-    const T* zr = reinterpret_cast<const T*>(r.z) + (in ? row : row0) * r.ld;
-    const bool soft = r.score == GEM_NLR_SOFTMAX, biased = r.bias;
-    const bool scored = biased || (r.groups > 1 && r.best == 2);          // the choice needs the scores
-    const unsigned row_lanes = (LANES == 32 ? kAll : (1u << (LANES & 31)) - 1u) << (lane - me);
-    float z[V], m = -INFINITY, sum = 0.0f;
-    load_logits<V>(zr, r, me, z);
-    if (soft && (scored || !r.renorm)) {
-#pragma unroll
-        for (int v = 0; v < V; ++v) m = fmaxf(m, z[v]);
-        m = lanes_top<LANES>(m);
-    }
-    float whole = 1.0f;                                  // softmax without renormalization: the sum of the exponentials
-    if (soft && !r.renorm) {
-        whole = 0.0f;
-#pragma unroll
-        for (int v = 0; v < V; ++v) whole += z[v] == -INFINITY ? 0.0f : expf(z[v] - m);
-        whole = lanes_sum<LANES>(whole);
-    }
-    bool bad = false;
-    uint32_t key[V];
-    bool unsure = false;
-    unsigned stays = kAll;                               // groups that can be chosen
-    const int size = r.experts / r.groups;
-    bool nothing = false;                                // no expert is left
-    if (scored) {
-        float c[V];                                      // scores; a NaN (softmax: an infinity) comes out in their sum
-        if (soft) {
-#pragma unroll
-            for (int v = 0; v < V; ++v) {
-                c[v] = z[v] == -INFINITY ? 0.0f : fast_exp2((z[v] - m) * kLog2E);
-                sum += c[v];
-            }
-            sum = lanes_sum<LANES>(sum);
-            const float over = fast_inverse(sum);
-#pragma unroll
-            for (int v = 0; v < V; ++v) c[v] *= over;
-        } else {
-#pragma unroll
-            for (int v = 0; v < V; ++v) {
-                c[v] = fast_inverse(1.0f + fast_exp2(z[v] * -kLog2E));
-                sum += c[v];
-            }
-        }
-        bad = sum != sum || !bias_fine;
-#pragma unroll
-        for (int v = 0; v < V; v += 4) {
-            const float4 b = *reinterpret_cast<const float4*>(bias + me * V + v);
-            c[v] = z[v] == -INFINITY ? -INFINITY : c[v] + b.x;
-            c[v + 1] = z[v + 1] == -INFINITY ? -INFINITY : c[v + 1] + b.y;
-            c[v + 2] = z[v + 2] == -INFINITY ? -INFINITY : c[v + 2] + b.z;
-            c[v + 3] = z[v + 3] == -INFINITY ? -INFINITY : c[v + 3] + b.w;
-        }
-        if (r.groups > 1) stays = kept_groups<LANES, V>(r, c, size, me, mine, sp, true, unsure);
-        if (biased) {
-            // Fixed point from two below the largest on.  Step 0 is what lies lower, or cannot be chosen: where the choice
-            // comes to it, it is made in FP64.
-            float top = c[0];
-#pragma unroll
-            for (int v = 1; v < V; ++v) top = fmaxf(top, c[v]);
-            top = lanes_top<LANES>(top);
-            nothing = top == -INFINITY;
-            unsure |= fabsf(top) > 16.0f;
-            const float from = (2.0f - top) * STEP;
-            const uint32_t own = INDEX - (uint32_t)(me * V);
-#pragma unroll
-            for (int v = 0; v < V; ++v) key[v] = (__float2uint_rn(fmaf(c[v], STEP, from)) << BITS) + own - v;
-        }
-    } else {
-#pragma unroll
-        for (int v = 0; v < V; ++v) bad |= soft ? !(z[v] < INFINITY) : z[v] != z[v];
-        if (r.groups > 1) stays = kept_groups<LANES, V>(r, z, size, me, mine, sp, false, unsure);
-    }
-    if (!biased) {
-        // the logit's upper bits: of 16-bit types all of them
-#pragma unroll
-        for (int v = 0; v < V; ++v) {
-            const uint32_t k = key_of(z[v]);
-            key[v] = k <= kNone32 ? 0u : (k & ~INDEX) | (INDEX - (uint32_t)(me * V + v));
-        }
-    }
-    if (r.groups > 1) {
-        if (size % V == 0) {
-            if (!(stays >> (me * V / size & 31) & 1u)) {
-#pragma unroll
-                for (int v = 0; v < V; ++v) key[v] = 0u;
-            }
-        } else {
-            int g = me * V / size, next = (g + 1) * size - me * V;           // the group of v, and the v where the next begins
-#pragma unroll
-            for (int v = 0; v < V; ++v) {
-                if (v == next) { ++g; next += size; }
-                if (!(stays >> (g & 31) & 1u)) key[v] = 0u;
-            }
-        }
-    }
-    sort_keys<V>(key);
-    const bool few = r.k < 8;                            // entries of a list that can be reached
-    uint32_t last = 0;
-    for (int j = 0; j <= r.k; ++j) {
-        uint32_t best = key[0];
-#pragma unroll
-        for (int o = LANES / 2; o > 0; o >>= 1) best = max(best, __shfl_xor_sync(kAll, best, o));
-        const uint32_t a = last >> BITS, b = best >> BITS;
-        if (j > 0 && a - b <= (biased ? (uint32_t)(kMargin * STEP) : 0u) && b) {
-            const int before = (int)(INDEX - (last & INDEX)), index = (int)(INDEX - (best & INDEX));
-            unsure |= !(to_f(zr[before]) == to_f(zr[index]) && (!biased || bias[before] == bias[index]));
-        }
-        if (j == r.k) break;
-        unsure |= biased && b == 0u;
-        if (me == 0) sp.chosen[mine][j] = b ? (int)(INDEX - (best & INDEX)) : -1;
-        last = best;
-        if (key[0] == best) {
-            if (few) {
-#pragma unroll
-                for (int v = 0; v + 1 < (V < 8 ? V : 8); ++v) key[v] = key[v + 1];
-                if (V <= 8) key[V < 8 ? V - 1 : 7] = 0u;
-            } else {
-#pragma unroll
-                for (int v = 0; v + 1 < V; ++v) key[v] = key[v + 1];
-                key[V - 1] = 0u;
-            }
-        }
-    }
-    bad = (__ballot_sync(kAll, bad) & row_lanes) != 0;
-    unsure = unsure && !bad && in && !nothing;
-    __syncwarp();
-    for (unsigned rows = __ballot_sync(kAll, unsure && me == 0); rows; rows &= rows - 1) {
-        const int which = (__ffs(rows) - 1) / LANES;
-        const int got = choose_in_64_bits<(PAD > 32 ? PAD / 32 : 1), T>(r, row0 + which, lane);
-        if (lane < r.k) sp.chosen[which][lane] = got;
-    }
-    __syncwarp();
     // Weights: slot j by lane j mod LANES of its row.  The first of a lane's slots, which mostly is its only one, stays in registers.
     const auto slot = [&](int j, int& e, float& x) {
-        e = j < r.k && !bad ? sp.chosen[mine][j] : -1;
+        e = j < r.k && !bad ? chosen[j] : -1;
         x = e >= 0 ? to_f(zr[e]) : 0.0f;
     };
     const auto logistic = [](float x) { return 1.0f / (1.0f + expf(-x)); };
@@ -508,27 +149,400 @@ __device__ __forceinline__ void route_rows(const Route& r, int64_t row0, int64_t
             if (e >= 0) atomicAdd(counts + e, 1);
         }
     }
+}
+
+// ---- the choice in FP64, a row by a warp: lane's experts are lane, lane + 32, ... ------------------------------------------------------
+// Short rather than fast: few rows come here, and what they wait for is the code.  chosen: shared memory of a row.
+template <typename T>
+__device__ __noinline__ void route_in_64_bits(const Route& r, int64_t row, int lane, int32_t* chosen, int32_t* counts)
+{
+    constexpr int MOST = GEM_NLR_MAX_EXPERTS / 32;
+    const T* zr = reinterpret_cast<const T*>(r.z) + row * r.ld;
+    const bool soft = r.score == GEM_NLR_SOFTMAX;
+    const double none = -(double)INFINITY;
+    const int size = r.experts / r.groups;
+    double c[MOST], by[MOST];                            // what is chosen by, and what groups are judged by; NaN: taken
+    float m = -INFINITY, whole = 0.0f;
+    double sum = 0.0;
+#pragma unroll 1
+    for (int i = lane; i < r.experts; i += 32) m = fmaxf(m, to_f(zr[i]));
+    m = warp_top(m);
+#pragma unroll 1
+    for (int i = lane; i < r.experts; i += 32) {
+        const float z = to_f(zr[i]);
+        const double e = exp(soft ? (double)z - (double)m : -(double)z);
+        if (z != -INFINITY) sum += e;
+        by[i >> 5] = soft ? e : 1.0 / (1.0 + e);
+        if (soft && z != -INFINITY) whole += expf(z - m);
+    }
+    sum = warp_sum(sum);
+    whole = warp_sum(whole);
+#pragma unroll 1
+    for (int i = lane; i < r.experts; i += 32) {
+        const float z = to_f(zr[i]);
+        const double s = soft ? by[i >> 5] / sum : by[i >> 5];
+        const double x = z == -INFINITY ? none : r.bias ? s + (double)__ldg(r.bias + i) : (double)z;
+        c[i >> 5] = x;
+        by[i >> 5] = z == -INFINITY ? none : r.bias || r.best == 1 ? x : s;
+    }
+    unsigned stays = kAll;
+    if (r.groups > 1) {
+        double mine = none;                              // lane g: group g's score
+#pragma unroll 1
+        for (int g = 0; g < r.groups; ++g) {
+            double first = none, second = none;
+#pragma unroll 1
+            for (int i = g * size + (lane - g * size & 31); i < (g + 1) * size; i += 32) {
+                const double x = by[i >> 5];
+                second = fmax(second, fmin(first, x));
+                first = fmax(first, x);
+            }
+#pragma unroll 1
+            for (int o = 1; o < 32; o *= 2) {
+                const double a = __shfl_xor_sync(kAll, first, o), b = __shfl_xor_sync(kAll, second, o);
+                second = fmax(fmin(first, a), fmax(second, b));
+                first = fmax(first, a);
+            }
+            if (lane == g) mine = r.best == 2 && second != none ? first + second : first;
+        }
+        int rank = 0;
+#pragma unroll 1
+        for (int g = 0; g < r.groups; ++g) {
+            const double other = __shfl_sync(kAll, mine, g);
+            rank += other > mine || (other == mine && g < lane);
+        }
+        stays = __ballot_sync(kAll, lane < r.groups && rank < r.kept);
+    }
+#pragma unroll 1
+    for (int j = 0; j < r.k; ++j) {
+        double top = none;
+        unsigned at = kAll;
+#pragma unroll 1
+        for (int i = lane; i < r.experts; i += 32)
+            if ((r.groups == 1 || stays >> (i / size) & 1u) && c[i >> 5] > top) { top = c[i >> 5]; at = i; }
+        const uint64_t key = at == kAll ? 0 : key_of(top), best = warp_max(key);
+        const unsigned index = __reduce_min_sync(kAll, key == best ? at : kAll);
+        if (lane == 0) chosen[j] = best ? (int)index : -1;
+        if (best && (index & 31u) == (unsigned)lane) c[index >> 5] = none;
+    }
+    __syncwarp();
+    take_weights<32>(r, row, true, false, zr, m, whole, chosen, lane, counts);
     __syncwarp();
 }
 
-// Places for the rows of this block's warps.  at: warps x experts, each warp's counts, replaced by the place of its next row of
-// each expert; first: the place of the block's first row of each expert.
-__device__ __forceinline__ void give_places(const Route& r, int32_t* at, const int32_t* first, int64_t begin, int64_t end)
+// 2^x and 1 / x in one instruction each, off by 2^-22 of themselves; subnormal results are 0.
+__device__ __forceinline__ float fast_exp2(float x)
 {
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    for (int e = threadIdx.x; e < r.experts; e += kThreads) {
-        int32_t next = first[e];
-        for (int w = 0; w < kWarps; ++w) {
-            const int32_t c = at[w * r.experts + e];
-            at[w * r.experts + e] = next;
-            next += c;
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+__device__ __forceinline__ float fast_inverse(float x)
+{
+    float y;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+constexpr float kLog2E = 1.4426950408889634f;
+
+// ---- the choice by keys -----------------------------------------------------------------------------------------------------------
+
+// How far apart two FP32 scores of the choice have to be for their order to be right.  A logistic score is off by 2^-22: the
+// exponential by 2^-22 of itself and by its argument's roundings (s (1 - s) <= 1/4, times |z| <= 0.23), the reciprocal by 2^-23.
+// A softmax score is off by 2^-19 of the largest: its sum has up to 21 steps.  The bias adds a rounding of the sum, the key a step.
+__device__ __forceinline__ float margin_of(bool soft, float largest, float top, float step)
+{
+    return (soft ? largest * 0x1p-17f : 0x1p-20f) + (fabsf(top) + 2.0f) * 0x1p-22f + 2.0f * step;
+}
+
+// Largest first.  (Batcher's merge exchange; a network for a power of two.)
+template <int V>
+__device__ __forceinline__ void sort_keys(uint32_t (&key)[V])
+{
+#pragma unroll
+    for (int p = V / 2; p > 0; p /= 2) {
+#pragma unroll
+        for (int q = V / 2, r = 0, d = p; d > 0;) {
+#pragma unroll
+            for (int i = 0; i + d < V; ++i)
+                if ((i & p) == r) {
+                    const uint32_t a = key[i], b = key[i + d];
+                    key[i] = max(a, b);
+                    key[i + d] = min(a, b);
+                }
+            d = q > p ? q - p : 0;
+            q /= 2;
+            r = p;
         }
     }
-    __syncthreads();
-    int32_t* mine = at + warp * r.experts;
-    const int64_t stop = end * r.k;
-    for (int64_t i0 = begin * r.k; i0 < stop; i0 += 32) {
-        const int64_t i = i0 + lane;
+}
+
+// A lane's V logits, experts me * V + v.
+template <int V, typename T>
+__device__ __forceinline__ void load_logits(const T* zr, const Route& r, int me, float (&z)[V])
+{
+    constexpr int BYTES = V * (int)sizeof(T);
+    if (r.wide && me * V + V <= r.experts) {
+        uint32_t w[BYTES / 4];
+        if constexpr (BYTES >= 16) {
+#pragma unroll
+            for (int i = 0; i < BYTES / 16; ++i) *reinterpret_cast<uint4*>(w + 4 * i) = __ldg(reinterpret_cast<const uint4*>(zr + me * V) + i);
+        } else {
+            *reinterpret_cast<uint2*>(w) = __ldg(reinterpret_cast<const uint2*>(zr + me * V));
+        }
+#pragma unroll
+        for (int v = 0; v < V; ++v) z[v] = to_f(reinterpret_cast<const T*>(w)[v]);
+    } else {
+#pragma unroll
+        for (int v = 0; v < V; ++v) z[v] = me * V + v < r.experts ? to_f(zr[me * V + v]) : -INFINITY;
+    }
+}
+
+// A warp's shared memory: chosen experts, and where there are groups their scores and the experts'.
+template <int LANES, int V> struct Space {
+    static constexpr int ROWS = 32 / LANES, PITCH = LANES * V + 4;
+    int32_t chosen[ROWS][kMaxChosen];
+    int32_t later[32];
+    float group[ROWS][kMaxGroups];
+    float score[ROWS][PITCH];
+};
+
+// Which groups can be chosen from, a bit each.  c: what the lane's experts' groups are judged by (-inf: none).  close: the border
+// between kept groups and others is nearer than FP32 scores tell.
+template <int LANES, int V>
+__device__ __forceinline__ unsigned kept_groups(const Route& r, const float (&c)[V], int size, int me, int mine, Space<LANES, V>& sp, bool scored, float largest, bool& close)
+{
+    const int lanes = size / V;                          // that hold a group
+    if (size % V == 0 && (lanes & (lanes - 1)) == 0) {
+        float first = c[0], second = -INFINITY;
+#pragma unroll
+        for (int v = 1; v < V; ++v) {
+            second = fmaxf(second, fminf(first, c[v]));
+            first = fmaxf(first, c[v]);
+        }
+        for (int o = 1; o < lanes; o *= 2) {
+            const float a = __shfl_xor_sync(kAll, first, o), b = __shfl_xor_sync(kAll, second, o);
+            second = fmaxf(fminf(first, a), fmaxf(second, b));
+            first = fmaxf(first, a);
+        }
+        if (me % lanes == 0 && me / lanes < r.groups) sp.group[mine][me / lanes] = (r.best == 2 && second != -INFINITY ? first + second : first) + 0.0f;
+    } else {
+#pragma unroll
+        for (int v = 0; v < V; v += 4) *reinterpret_cast<float4*>(&sp.score[mine][me * V + v]) = make_float4(c[v], c[v + 1], c[v + 2], c[v + 3]);
+        __syncwarp();
+        for (int g = me; g < r.groups; g += LANES) {
+            float first = -INFINITY, second = -INFINITY;
+            const float* of = &sp.score[mine][g * size];
+#pragma unroll 4
+            for (int i = 0; i < size; ++i) {
+                const float x = of[i];
+                second = fmaxf(second, fminf(first, x));
+                first = fmaxf(first, x);
+            }
+            sp.group[mine][g] = (r.best == 2 && second != -INFINITY ? first + second : first) + 0.0f;
+        }
+    }
+    __syncwarp();
+    unsigned kept = 0;
+    float low = INFINITY, high = -INFINITY;              // the lowest group kept and the highest of the others
+    for (int g = me; g < r.groups; g += LANES) {
+        const float x = sp.group[mine][g];
+        int rank = 0;
+#pragma unroll 4
+        for (int o = 0; o < r.groups; ++o) {
+            const float y = sp.group[mine][o];
+            rank += y > x || (y == x && o < g);
+        }
+        if (rank < r.kept) {
+            kept |= 1u << g;
+            low = fminf(low, x);
+        } else {
+            high = fmaxf(high, x);
+        }
+    }
+#pragma unroll
+    for (int o = LANES / 2; o > 0; o >>= 1) {
+        kept |= __shfl_xor_sync(kAll, kept, o);
+        low = fminf(low, __shfl_xor_sync(kAll, low, o));
+        high = fmaxf(high, __shfl_xor_sync(kAll, high, o));
+    }
+    close = scored && high != -INFINITY && !(low - high > 2.0f * margin_of(r.score == GEM_NLR_SOFTMAX, largest, low, 0.0f));
+    return kept;
+}
+
+// 32 / LANES rows from `row0` on by one warp; rows from `end` on are not there.  bias: LANES * V in shared memory (0 behind the last);
+// counts: of the warp's rows by expert.  Returns the lanes that begin rows which FP32 scores do not decide; nothing is written for these.
+template <int LANES, int V, typename T>
+__device__ __forceinline__ unsigned route_rows(const Route& r, int64_t row0, int64_t end, int lane, const float* bias, bool bias_fine, int32_t* counts, Space<LANES, V>& sp)
+{
+    constexpr int PAD = LANES * V;
+    constexpr uint32_t INDEX = PAD - 1;                   // the key's lower bits: PAD - 1 - index
+    constexpr int BITS = PAD == 16 ? 4 : PAD == 32 ? 5 : PAD == 64 ? 6 : PAD == 128 ? 7 : PAD == 256 ? 8 : 9;
+    constexpr float STEP = (float)(1u << (30 - BITS));    // a biased score's steps of its key in one
+    const int me = lane % LANES, mine = lane / LANES;
+    const int64_t row = row0 + mine;
+    const bool in = row < end;
+    const T* zr = reinterpret_cast<const T*>(r.z) + (in ? row : row0) * r.ld;
+    const bool soft = r.score == GEM_NLR_SOFTMAX, biased = r.bias;
+    const bool scored = biased || (r.groups > 1 && r.best == 2);          // the choice needs the scores
+    const unsigned row_lanes = (LANES == 32 ? kAll : (1u << (LANES & 31)) - 1u) << (lane - me);
+    float z[V], m = -INFINITY, sum = 0.0f;
+    load_logits<V>(zr, r, me, z);
+    if (soft && (scored || !r.renorm)) {
+#pragma unroll
+        for (int v = 0; v < V; ++v) m = fmaxf(m, z[v]);
+        m = lanes_top<LANES>(m);
+    }
+    float whole = 1.0f;                                  // softmax without renormalization: the sum of the exponentials
+    if (soft && !r.renorm) {
+        whole = 0.0f;
+#pragma unroll
+        for (int v = 0; v < V; ++v) whole += z[v] == -INFINITY ? 0.0f : expf(z[v] - m);
+        whole = lanes_sum<LANES>(whole);
+    }
+    bool bad = false;
+    uint32_t key[V];
+    bool unsure = false;
+    unsigned stays = kAll;                               // groups that can be chosen
+    const int size = r.experts / r.groups;
+    bool nothing = false;                                // no expert is left
+    uint32_t near = 0;                                   // steps of the key that do not tell two scores apart
+    if (scored) {
+        float over = 1.0f, c[V];                         // scores; a NaN (softmax: an infinity) comes out in their sum
+        if (soft) {
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                c[v] = z[v] == -INFINITY ? 0.0f : fast_exp2((z[v] - m) * kLog2E);
+                sum += c[v];
+            }
+            sum = lanes_sum<LANES>(sum);
+            over = fast_inverse(sum);
+#pragma unroll
+            for (int v = 0; v < V; ++v) c[v] *= over;
+        } else {
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                c[v] = fast_inverse(1.0f + fast_exp2(z[v] * -kLog2E));
+                sum += c[v];
+            }
+        }
+        bad = sum != sum || !bias_fine;
+#pragma unroll
+        for (int v = 0; v < V; v += 4) {
+            const float4 b = *reinterpret_cast<const float4*>(bias + me * V + v);
+            c[v] = z[v] == -INFINITY ? -INFINITY : c[v] + b.x;
+            c[v + 1] = z[v + 1] == -INFINITY ? -INFINITY : c[v + 1] + b.y;
+            c[v + 2] = z[v + 2] == -INFINITY ? -INFINITY : c[v + 2] + b.z;
+            c[v + 3] = z[v + 3] == -INFINITY ? -INFINITY : c[v + 3] + b.w;
+        }
+        if (r.groups > 1) stays = kept_groups<LANES, V>(r, c, size, me, mine, sp, true, over, unsure);
+        if (biased) {
+            // Fixed point from two below the largest on.  Step 0 is what lies lower, or cannot be chosen: where the choice
+            // comes to it, it is made in FP64.
+            float top = c[0];
+#pragma unroll
+            for (int v = 1; v < V; ++v) top = fmaxf(top, c[v]);
+            top = lanes_top<LANES>(top);
+            nothing = top == -INFINITY;
+            unsure |= fabsf(top) > 16.0f;
+            near = (uint32_t)(margin_of(soft, over, fminf(fabsf(top), 16.0f), 1.0f / STEP) * STEP);
+            const float from = (2.0f - top) * STEP;
+            const uint32_t own = INDEX - (uint32_t)(me * V);
+#pragma unroll
+            for (int v = 0; v < V; ++v) key[v] = (__float2uint_rn(fmaf(c[v], STEP, from)) << BITS) + own - v;
+        }
+    } else {
+#pragma unroll
+        for (int v = 0; v < V; ++v) bad |= soft ? !(z[v] < INFINITY) : z[v] != z[v];
+        if (r.groups > 1) stays = kept_groups<LANES, V>(r, z, size, me, mine, sp, false, 1.0f, unsure);
+    }
+    if (!biased) {
+        // the logit's upper bits: of 16-bit types all of them
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            const uint32_t k = key_of(z[v]);
+            key[v] = k <= kNone32 ? 0u : (k & ~INDEX) | (INDEX - (uint32_t)(me * V + v));
+        }
+    }
+    if (r.groups > 1) {
+        if (size % V == 0) {
+            if (!(stays >> (me * V / size & 31) & 1u)) {
+#pragma unroll
+                for (int v = 0; v < V; ++v) key[v] = 0u;
+            }
+        } else {
+            int g = me * V / size, next = (g + 1) * size - me * V;           // the group of v, and the v where the next begins
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                if (v == next) { ++g; next += size; }
+                if (!(stays >> (g & 31) & 1u)) key[v] = 0u;
+            }
+        }
+    }
+    sort_keys<V>(key);
+    const bool few = r.k < 8;                            // entries of a list that can be reached
+    uint32_t last = 0;
+    for (int j = 0; j <= r.k; ++j) {
+        uint32_t best = key[0];
+#pragma unroll
+        for (int o = LANES / 2; o > 0; o >>= 1) best = max(best, __shfl_xor_sync(kAll, best, o));
+        const uint32_t a = last >> BITS, b = best >> BITS;
+        if (j > 0 && a - b <= near && b) {
+            const int before = (int)(INDEX - (last & INDEX)), index = (int)(INDEX - (best & INDEX));
+            unsure |= !(to_f(zr[before]) == to_f(zr[index]) && (!biased || bias[before] == bias[index]));
+        }
+        if (j == r.k) break;
+        unsure |= biased && b == 0u;
+        if (me == 0) sp.chosen[mine][j] = b ? (int)(INDEX - (best & INDEX)) : -1;
+        last = best;
+        if (key[0] == best) {
+            if (few) {
+#pragma unroll
+                for (int v = 0; v + 1 < (V < 8 ? V : 8); ++v) key[v] = key[v + 1];
+                if (V <= 8) key[V < 8 ? V - 1 : 7] = 0u;
+            } else {
+#pragma unroll
+                for (int v = 0; v + 1 < V; ++v) key[v] = key[v + 1];
+                key[V - 1] = 0u;
+            }
+        }
+    }
+    bad = (__ballot_sync(kAll, bad) & row_lanes) != 0;
+    unsure = unsure && !bad && in && !nothing;
+    __syncwarp();
+    take_weights<LANES>(r, row, in && !unsure, bad, zr, m, whole, sp.chosen[mine], me, counts);
+    return __ballot_sync(kAll, unsure && me == 0);
+}
+
+// Counts by warp and expert lie `pitch` apart, an odd number, so that a warp reads all warps' counts of an expert without conflicts.
+__device__ __forceinline__ int pitch_of(int experts) { return experts | 1; }
+
+// at: each warp's counts, which become the sums over the warps before; total: over all of them.  By the whole block.
+__device__ __forceinline__ void sums_over_warps(int32_t* at, int32_t* total, int experts)
+{
+    const int lane = threadIdx.x & 31, pitch = pitch_of(experts);
+    for (int e = threadIdx.x >> 5; e < experts; e += kWarps) {
+        const int32_t own = at[lane * pitch + e];
+        int32_t v = own;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int32_t u = __shfl_up_sync(kAll, v, o);
+            if (lane >= o) v += u;
+        }
+        at[lane * pitch + e] = v - own;
+        if (lane == 31) total[e] = v;
+    }
+}
+
+// The rank of each entry among its expert's entries of the block, in order: a warp's 32 at a time by matching equal experts.
+// ONE: the places themselves, first[e] being expert e's first.
+template <bool ONE>
+__device__ __forceinline__ void rank_entries(const Route& r, int32_t* mine, const int32_t* first, int64_t begin, int64_t end)
+{
+    const int lane = threadIdx.x & 31;
+    const int stop = (int)(end * r.k);
+    for (int i0 = (int)(begin * r.k); i0 < stop; i0 += 32) {
+        const int i = i0 + lane;
         const int e = i < stop ? r.expert[i] : -1;
         const unsigned same = __match_any_sync(kAll, e);
         const int rank = __popc(same & ((1u << lane) - 1));
@@ -537,8 +551,11 @@ __device__ __forceinline__ void give_places(const Route& r, int32_t* at, const i
         __syncwarp();
         if (e >= 0 && rank == 0) mine[e] += __popc(same);
         __syncwarp();
+        if (ONE && e >= 0) {
+            p += first[e];
+            r.row[p] = (int32_t)((uint32_t)i / (uint32_t)r.k);
+        }
         if (i < stop) r.place[i] = p;
-        if (e >= 0) r.row[p] = (int32_t)(i / r.k);
     }
 }
 
@@ -565,10 +582,11 @@ __device__ __forceinline__ void sums_over_experts(const int32_t* total, int32_t*
 
 __device__ __forceinline__ void leave_rest(const Route& r, int32_t used)
 {
-    for (int64_t p = used + (int64_t)blockIdx.x * kThreads + threadIdx.x; p < r.n * r.k; p += (int64_t)gridDim.x * kThreads) r.row[p] = -1;
+    const int places = (int)(r.n * r.k);
+    for (int64_t p = used + (int64_t)blockIdx.x * kThreads + threadIdx.x; p < places; p += (int64_t)gridDim.x * kThreads) r.row[p] = -1;
 }
 
-// Shared memory: warps x experts counts; ONE: and experts + 1 sums and experts totals; then the biases and the warps' space.
+// Shared memory: counts by warp and expert, experts + 1 sums, experts totals, the biases, the warps' space.
 template <int LANES, int V, typename T, bool ONE>
 __global__ void __launch_bounds__(kThreads)
 k_route(const __grid_constant__ Route r)
@@ -576,10 +594,10 @@ k_route(const __grid_constant__ Route r)
     using Sp = Space<LANES, V>;
     extern __shared__ int32_t at[];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int before = kWarps * r.experts + (ONE ? 2 * r.experts + 1 : 0);
+    const int pitch = pitch_of(r.experts), before = kWarps * pitch + 2 * r.experts + 1;
     float* bias = reinterpret_cast<float*>(at) + (before + 3) / 4 * 4;
     Sp& sp = *reinterpret_cast<Sp*>(reinterpret_cast<char*>(bias + LANES * V) + (size_t)warp * (r.groups > 1 ? sizeof(Sp) : offsetof(Sp, group)));
-    for (int i = threadIdx.x; i < kWarps * r.experts; i += kThreads) at[i] = 0;
+    for (int i = threadIdx.x; i < kWarps * pitch; i += kThreads) at[i] = 0;
     const int64_t begin = min(r.n, ((int64_t)blockIdx.x * kWarps + warp) * r.rows_per_warp), end = min(r.n, begin + r.rows_per_warp);
     bool fine = true;
     for (int i = threadIdx.x; i < LANES * V; i += kThreads) {
@@ -587,38 +605,49 @@ k_route(const __grid_constant__ Route r)
         fine = bias[i] == bias[i];
     }
     fine = __syncthreads_and(fine);
-    for (int64_t row = begin; row < end; row += Sp::ROWS) route_rows<LANES, V, T>(r, row, end, lane, bias, fine, at + warp * r.experts, sp);
+    // Rows for FP64 wait in sp.later until there are many, or all others are done.
+    for (int64_t row = begin; row < end;) {
+        int waiting = 0;
+        for (; row < end && waiting <= 32 - Sp::ROWS; row += Sp::ROWS) {
+            const unsigned rows = route_rows<LANES, V, T>(r, row, end, lane, bias, fine, at + warp * pitch, sp);
+            if (rows >> lane & 1u) sp.later[waiting + __popc(rows & ((1u << lane) - 1))] = (int32_t)(row - begin) + lane / LANES;
+            waiting += __popc(rows);
+        }
+        __syncwarp();
+        for (int i = 0; i < waiting; ++i) route_in_64_bits<T>(r, begin + sp.later[i], lane, sp.chosen[0], at + warp * pitch);
+    }
     __syncthreads();
     next_may_start();
-    int32_t* first = at + kWarps * r.experts;
-    int32_t* total = ONE ? first + r.experts + 1 : r.counts + (int64_t)blockIdx.x * r.experts;
-    for (int e = threadIdx.x; e < r.experts; e += kThreads) {
-        int32_t c = 0;
-        for (int w = 0; w < kWarps; ++w) c += at[w * r.experts + e];
-        total[e] = c;
-    }
+    int32_t* first = at + kWarps * pitch;
+    int32_t* total = first + r.experts + 1;
+    sums_over_warps(at, total, r.experts);
+    __syncthreads();
     if constexpr (ONE) {
-        __syncthreads();
         sums_over_experts(total, first, r.experts);
         for (int e = threadIdx.x; e <= r.experts; e += kThreads) r.offset[e] = first[e];
-        give_places(r, at, first, begin, end);
+        rank_entries<true>(r, at + warp * pitch, first, begin, end);
         leave_rest(r, first[r.experts]);
+    } else {
+        for (int e = threadIdx.x; e < r.experts; e += kThreads) r.counts[(int64_t)blockIdx.x * r.experts + e] = total[e];
+        rank_entries<false>(r, at + warp * pitch, first, begin, end);
     }
 }
 
-// Shared memory: warps x experts counts, then experts + 1 sums, experts totals, experts counts of the blocks before.
+// Ranks to places.  Shared memory: experts + 1 sums, experts totals, experts counts of the blocks before.
 __global__ void __launch_bounds__(kThreads)
 k_route_places(const __grid_constant__ Route r, int blocks)
 {
-    extern __shared__ int32_t at[];
-    int32_t* first = at + kWarps * r.experts;
+    extern __shared__ int32_t first[];
     int32_t* total = first + r.experts + 1;
     int32_t* before = total + r.experts;
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    for (int i = threadIdx.x; i < kWarps * r.experts + 3 * r.experts + 1; i += kThreads) at[i] = 0;
+    for (int e = threadIdx.x; e < 2 * r.experts; e += kThreads) total[e] = 0;
     __syncthreads();
-    const int64_t begin = min(r.n, ((int64_t)blockIdx.x * kWarps + warp) * r.rows_per_warp), end = min(r.n, begin + r.rows_per_warp);
+    const int begin = (int)(min(r.n, (int64_t)blockIdx.x * kWarps * r.rows_per_warp) * r.k), end = (int)(min(r.n, ((int64_t)blockIdx.x + 1) * kWarps * r.rows_per_warp) * r.k);
     grid_ready();
+    // the first entries come with the counts
+    const int i0 = begin + threadIdx.x;
+    const int e0 = i0 < end ? r.expert[i0] : -1;
+    const int32_t p0 = i0 < end ? r.place[i0] : -1;
     // threads in pairs (expert, share of the blocks); whole numbers: the order of the additions does not show
     const int shares = max(1, kThreads / r.experts), share = threadIdx.x / r.experts;
     if (share < shares)
@@ -633,17 +662,17 @@ k_route_places(const __grid_constant__ Route r, int blocks)
             atomicAdd(total + e, all);
             atomicAdd(before + e, low);
         }
-    for (int64_t i = begin * r.k + lane; i < end * r.k; i += 32) {
-        const int e = r.expert[i];
-        if (e >= 0) atomicAdd(at + warp * r.experts + e, 1);
-    }
     __syncthreads();
     sums_over_experts(total, first, r.experts);
     if (blockIdx.x == 0)
         for (int e = threadIdx.x; e <= r.experts; e += kThreads) r.offset[e] = first[e];
-    for (int e = threadIdx.x; e < r.experts; e += kThreads) before[e] += first[e];
-    __syncthreads();
-    give_places(r, at, before, begin, end);
+    for (int64_t i = i0; i < end; i += kThreads) {
+        const int e = i == i0 ? e0 : r.expert[i];
+        if (e < 0) continue;
+        const int32_t p = (i == i0 ? p0 : r.place[i]) + before[e] + first[e];
+        r.place[i] = p;
+        r.row[p] = (int32_t)((uint32_t)i / (uint32_t)r.k);
+    }
     leave_rest(r, first[r.experts]);
 }
 
@@ -881,11 +910,11 @@ extern "C" int gem_nlr_route(const void* logits_dev, int32_t type, int64_t ld, c
             const bool wide = aligned_to(logits_dev, BYTES) && ld * (int64_t)sizeof(T) % BYTES == 0;
             const Route r = {logits_dev, ld, bias_dev, n, experts, k, score, groups, kept_groups, group_best, renormalize, wide, scale, expert_dev, weight_dev,
                              offset_dev, row_dev, place_dev, (int32_t*)scratch_dev, per_warp};
-            const int counts = kWarps * experts * 4, sums = (2 * experts + 1) * 4, space = LANES * V * 4 + kWarps * (int)(groups > 1 ? sizeof(Sp) : offsetof(Sp, group)) + 16;
+            const int counts = (kWarps * (experts | 1) + 2 * experts + 1) * 4, space = LANES * V * 4 + kWarps * (int)(groups > 1 ? sizeof(Sp) : offsetof(Sp, group)) + 16;
             cudaStream_t st = (cudaStream_t)cuda_stream;
-            if (one) return told(launch_route(k_route<LANES, V, T, true>, 1, kThreads, counts + sums + space, false, st, r));
+            if (one) return told(launch_route(k_route<LANES, V, T, true>, 1, kThreads, counts + space, false, st, r));
             cudaError_t rc = launch_route(k_route<LANES, V, T, false>, blocks, kThreads, counts + space, false, st, r);
-            if (rc == cudaSuccess) rc = launch_route(k_route_places, blocks, kThreads, counts + (3 * experts + 1) * 4, true, st, r, blocks);
+            if (rc == cudaSuccess) rc = launch_route(k_route_places, blocks, kThreads, (3 * experts + 1) * 4, true, st, r, blocks);
             return told(rc);
         });
     });
