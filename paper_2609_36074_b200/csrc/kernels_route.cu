@@ -152,48 +152,49 @@ __device__ __forceinline__ void take_weights(const Route& r, int64_t row, bool i
 }
 
 // ---- the choice in FP64, a row by a warp: lane's experts are lane, lane + 32, ... ------------------------------------------------------
-// Short rather than fast: few rows come here, and what they wait for is the code.  chosen: shared memory of a row.
+// Short: few rows come here, and what they wait for is the code and its chains.  stays: the groups to choose from, 0 where FP32 scores
+// do not decide them either.  chosen: shared memory of a row.
 template <typename T>
-__device__ __noinline__ void route_in_64_bits(const Route& r, int64_t row, int lane, int32_t* chosen, int32_t* counts)
+__device__ __noinline__ void route_in_64_bits(const Route& r, int64_t row, unsigned stays, int lane, int32_t* chosen, int32_t* counts)
 {
     constexpr int MOST = GEM_NLR_MAX_EXPERTS / 32;
     const T* zr = reinterpret_cast<const T*>(r.z) + row * r.ld;
     const bool soft = r.score == GEM_NLR_SOFTMAX;
     const double none = -(double)INFINITY;
     const int size = r.experts / r.groups;
-    double c[MOST], by[MOST];                            // what is chosen by, and what groups are judged by; NaN: taken
+    double c[MOST];                                      // what is chosen by
     float m = -INFINITY, whole = 0.0f;
-    double sum = 0.0;
+    double sum = 1.0;
+    if (soft) {
 #pragma unroll 1
-    for (int i = lane; i < r.experts; i += 32) m = fmaxf(m, to_f(zr[i]));
-    m = warp_top(m);
-#pragma unroll 1
-    for (int i = lane; i < r.experts; i += 32) {
-        const float z = to_f(zr[i]);
-        const double e = exp(soft ? (double)z - (double)m : -(double)z);
-        if (z != -INFINITY) sum += e;
-        by[i >> 5] = soft ? e : 1.0 / (1.0 + e);
-        if (soft && z != -INFINITY) whole += expf(z - m);
+        for (int i = lane; i < r.experts; i += 32) m = fmaxf(m, to_f(zr[i]));
+        m = warp_top(m);
+        sum = 0.0;
+#pragma unroll 2
+        for (int i = lane; i < r.experts; i += 32) {
+            const float z = to_f(zr[i]);
+            const double e = exp((double)z - (double)m);
+            c[i >> 5] = e;
+            sum += e;
+            whole += expf(z - m);
+        }
+        sum = warp_sum(sum);
+        whole = warp_sum(whole);
     }
-    sum = warp_sum(sum);
-    whole = warp_sum(whole);
-#pragma unroll 1
-    for (int i = lane; i < r.experts; i += 32) {
+    // what groups are judged by, then what is chosen by
+    const auto judged = [&](int i, bool group) {
         const float z = to_f(zr[i]);
-        const double s = soft ? by[i >> 5] / sum : by[i >> 5];
-        const double x = z == -INFINITY ? none : r.bias ? s + (double)__ldg(r.bias + i) : (double)z;
-        c[i >> 5] = x;
-        by[i >> 5] = z == -INFINITY ? none : r.bias || r.best == 1 ? x : s;
-    }
-    unsigned stays = kAll;
-    if (r.groups > 1) {
+        const double s = soft ? c[i >> 5] / sum : 1.0 / (1.0 + exp(-(double)z));
+        return z == -INFINITY ? none : r.bias ? s + (double)__ldg(r.bias + i) : group && r.best == 2 ? s : (double)z;
+    };
+    if (!stays) {
         double mine = none;                              // lane g: group g's score
 #pragma unroll 1
         for (int g = 0; g < r.groups; ++g) {
             double first = none, second = none;
 #pragma unroll 1
-            for (int i = g * size + (lane - g * size & 31); i < (g + 1) * size; i += 32) {
-                const double x = by[i >> 5];
+            for (int i = g * size + ((lane - g * size) & 31); i < (g + 1) * size; i += 32) {
+                const double x = judged(i, true);
                 second = fmax(second, fmin(first, x));
                 first = fmax(first, x);
             }
@@ -213,19 +214,29 @@ __device__ __noinline__ void route_in_64_bits(const Route& r, int64_t row, int l
         }
         stays = __ballot_sync(kAll, lane < r.groups && rank < r.kept);
     }
+    double top = none;
+    unsigned at = kAll;
+#pragma unroll 2
+    for (int i = lane; i < r.experts; i += 32) {
+        const double x = r.groups == 1 || stays >> (i / size) & 1u ? judged(i, false) : none;
+        c[i >> 5] = x;
+        if (x > top) { top = x; at = i; }
+    }
 #pragma unroll 1
     for (int j = 0; j < r.k; ++j) {
-        double top = none;
-        unsigned at = kAll;
-#pragma unroll 1
-        for (int i = lane; i < r.experts; i += 32)
-            if ((r.groups == 1 || stays >> (i / size) & 1u) && c[i >> 5] > top) { top = c[i >> 5]; at = i; }
         const uint64_t key = at == kAll ? 0 : key_of(top), best = warp_max(key);
         const unsigned index = __reduce_min_sync(kAll, key == best ? at : kAll);
         if (lane == 0) chosen[j] = best ? (int)index : -1;
-        if (best && (index & 31u) == (unsigned)lane) c[index >> 5] = none;
+        if (best && index == at) {
+            c[index >> 5] = none;
+            top = none;
+            at = kAll;
+#pragma unroll 1
+            for (int i = lane; i < r.experts; i += 32)
+                if (c[i >> 5] > top) { top = c[i >> 5]; at = i; }
+        }
+        __syncwarp();
     }
-    __syncwarp();
     take_weights<32>(r, row, true, false, zr, m, whole, chosen, lane, counts);
     __syncwarp();
 }
@@ -303,6 +314,7 @@ template <int LANES, int V> struct Space {
     static constexpr int ROWS = 32 / LANES, PITCH = LANES * V + 4;
     int32_t chosen[ROWS][kMaxChosen];
     int32_t later[32];
+    uint32_t later_groups[32];
     float group[ROWS][kMaxGroups];
     float score[ROWS][PITCH];
 };
@@ -371,9 +383,10 @@ __device__ __forceinline__ unsigned kept_groups(const Route& r, const float (&c)
 }
 
 // 32 / LANES rows from `row0` on by one warp; rows from `end` on are not there.  bias: LANES * V in shared memory (0 behind the last);
-// counts: of the warp's rows by expert.  Returns the lanes that begin rows which FP32 scores do not decide; nothing is written for these.
+// counts: of the warp's rows by expert.  Returns the lanes that begin rows which FP32 scores do not decide, for which nothing is written,
+// and the groups to choose from there (0: not decided).
 template <int LANES, int V, typename T>
-__device__ __forceinline__ unsigned route_rows(const Route& r, int64_t row0, int64_t end, int lane, const float* bias, bool bias_fine, int32_t* counts, Space<LANES, V>& sp)
+__device__ __forceinline__ unsigned route_rows(const Route& r, int64_t row0, int64_t end, int lane, const float* bias, bool bias_fine, int32_t* counts, Space<LANES, V>& sp, unsigned& groups)
 {
     constexpr int PAD = LANES * V;
     constexpr uint32_t INDEX = PAD - 1;                   // the key's lower bits: PAD - 1 - index
@@ -406,6 +419,7 @@ __device__ __forceinline__ unsigned route_rows(const Route& r, int64_t row0, int
     unsigned stays = kAll;                               // groups that can be chosen
     const int size = r.experts / r.groups;
     bool nothing = false;                                // no expert is left
+    bool close = false;                                  // the groups are not decided
     uint32_t near = 0;                                   // steps of the key that do not tell two scores apart
     if (scored) {
         float over = 1.0f, c[V];                         // scores; a NaN (softmax: an infinity) comes out in their sum
@@ -435,7 +449,7 @@ __device__ __forceinline__ unsigned route_rows(const Route& r, int64_t row0, int
             c[v + 2] = z[v + 2] == -INFINITY ? -INFINITY : c[v + 2] + b.z;
             c[v + 3] = z[v + 3] == -INFINITY ? -INFINITY : c[v + 3] + b.w;
         }
-        if (r.groups > 1) stays = kept_groups<LANES, V>(r, c, size, me, mine, sp, true, over, unsure);
+        if (r.groups > 1) stays = kept_groups<LANES, V>(r, c, size, me, mine, sp, true, over, close);
         if (biased) {
             // Fixed point from two below the largest on.  Step 0 is what lies lower, or cannot be chosen: where the choice
             // comes to it, it is made in FP64.
@@ -454,7 +468,7 @@ __device__ __forceinline__ unsigned route_rows(const Route& r, int64_t row0, int
     } else {
 #pragma unroll
         for (int v = 0; v < V; ++v) bad |= soft ? !(z[v] < INFINITY) : z[v] != z[v];
-        if (r.groups > 1) stays = kept_groups<LANES, V>(r, z, size, me, mine, sp, false, 1.0f, unsure);
+        if (r.groups > 1) stays = kept_groups<LANES, V>(r, z, size, me, mine, sp, false, 1.0f, close);
     }
     if (!biased) {
         // the logit's upper bits: of 16-bit types all of them
@@ -508,7 +522,8 @@ __device__ __forceinline__ unsigned route_rows(const Route& r, int64_t row0, int
         }
     }
     bad = (__ballot_sync(kAll, bad) & row_lanes) != 0;
-    unsure = unsure && !bad && in && !nothing;
+    unsure = (unsure || close) && !bad && in && !nothing;
+    groups = close ? 0u : stays;
     __syncwarp();
     take_weights<LANES>(r, row, in && !unsure, bad, zr, m, whole, sp.chosen[mine], me, counts);
     return __ballot_sync(kAll, unsure && me == 0);
@@ -609,12 +624,17 @@ k_route(const __grid_constant__ Route r)
     for (int64_t row = begin; row < end;) {
         int waiting = 0;
         for (; row < end && waiting <= 32 - Sp::ROWS; row += Sp::ROWS) {
-            const unsigned rows = route_rows<LANES, V, T>(r, row, end, lane, bias, fine, at + warp * pitch, sp);
-            if (rows >> lane & 1u) sp.later[waiting + __popc(rows & ((1u << lane) - 1))] = (int32_t)(row - begin) + lane / LANES;
+            unsigned groups;
+            const unsigned rows = route_rows<LANES, V, T>(r, row, end, lane, bias, fine, at + warp * pitch, sp, groups);
+            if (rows >> lane & 1u) {
+                const int i = waiting + __popc(rows & ((1u << lane) - 1));
+                sp.later[i] = (int32_t)(row - begin) + lane / LANES;
+                sp.later_groups[i] = groups;
+            }
             waiting += __popc(rows);
         }
         __syncwarp();
-        for (int i = 0; i < waiting; ++i) route_in_64_bits<T>(r, begin + sp.later[i], lane, sp.chosen[0], at + warp * pitch);
+        for (int i = 0; i < waiting; ++i) route_in_64_bits<T>(r, begin + sp.later[i], sp.later_groups[i], lane, sp.chosen[0], at + warp * pitch);
     }
     __syncthreads();
     next_may_start();
