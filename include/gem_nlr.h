@@ -443,20 +443,28 @@ int gem_nlr_route_backward(const float *dweight_dev, const void *logits_dev, int
  * x: x_rows x d_in; row: places entries, NULL when place p's row is x's row p (then x_rows >= places); W_e: d_in x
  * d_out at w + e stride_w, rows ld_w apart, or with w_turned == 1 its transpose (d_out x d_in); y: places x d_out.
  * x, w, y: GEM_NLR_F16 or GEM_NLR_BF16; products are summed in FP32 and rounded once.  A place whose row entry is -1 has
- * a row of zeros for x.  places < 2^31 - 2^16.  16-byte aligned rows (and stride_w) take the fast loads.        */
+ * a row of zeros for x.  places < 2^31 - 2^16.
+ * Operands whose rows (of w: and experts) do not begin on 16 bytes, lie closer than they are long or are shared are copied to scratch
+ * first; the *_scratch_bytes calls look at the addresses for their alignment alone.                            */
+size_t gem_nlr_expert_product_scratch_bytes(const void *x_dev, int64_t ld_x, int64_t x_rows, const void *w_dev, int64_t ld_w,
+                                            int64_t stride_w, int32_t w_turned, int32_t experts, int32_t d_in, int32_t d_out);
 int gem_nlr_expert_product(const void *x_dev, int32_t type, int64_t ld_x, int64_t x_rows, const void *w_dev,
                            int64_t ld_w, int64_t stride_w, int32_t w_turned, const int32_t *offset_dev,
                            const int32_t *row_dev, int64_t places, int32_t experts, int32_t d_in, int32_t d_out,
-                           void *y_dev, int64_t ld_y, void *cuda_stream);
+                           void *y_dev, int64_t ld_y, void *scratch_dev, size_t scratch_bytes, void *cuda_stream);
 
 /* Its gradients: dx_p = dy_p W_e^T for every place (places x d_in; where row is given, the gradient of a row of x is the
  * sum over its places: gem_nlr_combine without weights), dW_e = sum over e's places of x_row(p)^T dy_p, in w's
  * layout with rows ld_dw and experts stride_dw apart (0 for an expert without rows).  dx and dw may each be NULL, not both.  */
+size_t gem_nlr_expert_product_backward_scratch_bytes(const void *dy_dev, int64_t ld_dy, int64_t places, const void *x_dev,
+                                                     int64_t ld_x, int64_t x_rows, const void *w_dev, int64_t ld_w,
+                                                     int64_t stride_w, int32_t w_turned, int32_t experts, int32_t d_in,
+                                                     int32_t d_out);
 int gem_nlr_expert_product_backward(const void *dy_dev, int64_t ld_dy, const void *x_dev, int32_t type, int64_t ld_x,
                                     int64_t x_rows, const void *w_dev, int64_t ld_w, int64_t stride_w, int32_t w_turned,
                                     const int32_t *offset_dev, const int32_t *row_dev, int64_t places, int32_t experts,
                                     int32_t d_in, int32_t d_out, void *dx_dev, int64_t ld_dx, void *dw_dev, int64_t ld_dw,
-                                    int64_t stride_dw, void *cuda_stream);
+                                    int64_t stride_dw, void *scratch_dev, size_t scratch_bytes, void *cuda_stream);
 
 /* out_t = sum_j weight_tj y_place(t,j) over the slots with a place (weight NULL: 1).  y: places x d, out: n x d, of `type`;
  * place, weight: n x k, 1 <= k <= 32.  A slot without a place adds nothing, unless its weight is NaN.           */

@@ -65,8 +65,10 @@ def _load():
         "route": [vp, i32, i64, vp, i64, i32, i32, i32, i32, i32, i32, i32, f32, vp, vp, vp, vp, vp, vp, size, vp],
         "route_scratch_bytes": [i64, i32],
         "route_backward": [vp, vp, i32, i64, vp, i64, i32, i32, i32, i32, f32, vp, i64, vp],
-        "expert_product": [vp, i32, i64, i64, vp, i64, i64, i32, vp, vp, i64, i32, i32, i32, vp, i64, vp],
-        "expert_product_backward": [vp, i64, vp, i32, i64, i64, vp, i64, i64, i32, vp, vp, i64, i32, i32, i32, vp, i64, vp, i64, i64, vp],
+        "expert_product": [vp, i32, i64, i64, vp, i64, i64, i32, vp, vp, i64, i32, i32, i32, vp, i64, vp, size, vp],
+        "expert_product_scratch_bytes": [vp, i64, i64, vp, i64, i64, i32, i32, i32, i32],
+        "expert_product_backward": [vp, i64, vp, i32, i64, i64, vp, i64, i64, i32, vp, vp, i64, i32, i32, i32, vp, i64, vp, i64, i64, vp, size, vp],
+        "expert_product_backward_scratch_bytes": [vp, i64, i64, vp, i64, i64, vp, i64, i64, i32, i32, i32, i32],
         "combine": [vp, i32, i64, i64, vp, vp, i64, i32, i32, vp, i64, vp],
         "combine_backward": [vp, i64, vp, i32, i64, i64, vp, vp, vp, i32, i64, i32, i32, vp, i64, vp, vp],
         "activation": [vp, i32, i64, i64, i32, i32, i32, vp, i64, vp, vp, vp],
@@ -236,8 +238,11 @@ def expert_product(x, w, offset, row=None, out=None, stream=None):
         if out.shape != (places, d_out) or out.dtype != x.dtype or out.device != x.device:
             raise ValueError(f"out has to be {(places, d_out)} {x.dtype} on {x.device}")
         ldy = _rows(out, "out")[2]
-    _check(fn["expert_product"](x.data_ptr(), _type(x, "x"), ld, x_rows, w.data_ptr(), ldw, es, turned, offset.data_ptr(), rp, places, experts, d_in, d_out,
-                                y.data_ptr(), ldy, _t._stream(at)), "expert_product")
+    xp, wp = x.data_ptr(), w.data_ptr()
+    size = fn["expert_product_scratch_bytes"](xp, ld, x_rows, wp, ldw, es, turned, experts, d_in, d_out)
+    scratch = _new(x, (size,), _t._torch.uint8) if size else None
+    _check(fn["expert_product"](xp, _type(x, "x"), ld, x_rows, wp, ldw, es, turned, offset.data_ptr(), rp, places, experts, d_in, d_out, y.data_ptr(), ldy,
+                                scratch.data_ptr() if size else None, size, _t._stream(at)), "expert_product")
     if out is not None:
         _t._written(out)
     return y
@@ -266,9 +271,12 @@ def expert_product_backward(dy, x, w, offset, row=None, need_dx=True, need_dw=Tr
     if need_dw:
         made = _new(w, (experts, d_out, d_in) if turned else (experts, d_in, d_out), w.dtype)
         dw, dwp, ldd = made.transpose(1, 2) if turned else made, made.data_ptr(), d_in if turned else d_out
-    _check(fn["expert_product_backward"](dy.data_ptr(), ldg, x.data_ptr(), _type(x, "x"), ld, x_rows, w.data_ptr(), ldw, es, turned, offset.data_ptr(), rp, places,
-                                         experts, d_in, d_out, None if dx is None else dx.data_ptr(), d_in, dwp, ldd, d_in * d_out, _t._stream(at)),
-           "expert_product_backward")
+    gp, xp, wp = dy.data_ptr(), x.data_ptr(), w.data_ptr()
+    size = fn["expert_product_backward_scratch_bytes"](gp, ldg, places, xp, ld, x_rows, wp, ldw, es, turned, experts, d_in, d_out)
+    scratch = _new(x, (size,), _t._torch.uint8) if size else None
+    _check(fn["expert_product_backward"](gp, ldg, xp, _type(x, "x"), ld, x_rows, wp, ldw, es, turned, offset.data_ptr(), rp, places, experts, d_in, d_out,
+                                         None if dx is None else dx.data_ptr(), d_in, dwp, ldd, d_in * d_out, scratch.data_ptr() if size else None, size,
+                                         _t._stream(at)), "expert_product_backward")
     return dx, dw
 
 

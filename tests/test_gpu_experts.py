@@ -108,6 +108,16 @@ def test_large_tiles(places, experts, d_in, d_out, turned, gather, dtype):
     check(places, experts, d_in, d_out, dtype, turned, gather, uneven=True, seed=places + turned)
 
 
+@pytest.mark.parametrize("gather", [0, 4000], ids=["as they are", "gathered"])
+@pytest.mark.parametrize("experts", [1, 3, 40])
+def test_many_tiles_a_block(experts, gather):
+    """Dozens of tiles for each block, full ones and almost empty ones after one another."""
+    check(40000, experts, 392, 648, BF16, gather=gather, uneven=True, seed=experts)
+    offset = torch.arange(experts + 1, dtype=torch.int32, device="cuda") * (40000 // experts)
+    offset[1:-1:2] += 1 - 40000 // experts                       # every other expert has one row
+    check(40000, experts, 136, 1032, F16, True, gather, offset=offset)
+
+
 @pytest.mark.parametrize("d_in", [64, 65])
 def test_wild_offsets(d_in):
     for o in ([0, 0, 0, 0], [0, 100, 100, 100], [5, 20, 60, 90], [0, 50, 30, 100], [-7, 40, 400, 100], [100, 100, 100, 100], [0, 1, 2, 3]):
