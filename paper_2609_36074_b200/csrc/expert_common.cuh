@@ -38,6 +38,20 @@ __device__ __forceinline__ void store8(T* __restrict__ p, int many, const float 
     }
 }
 
+// Lets a kernel have `bytes` of shared memory, once on each device.
+template <auto kern> inline cudaError_t allow_shared(int bytes)
+{
+    static std::atomic<uint64_t> done{0};
+    int dev = 0;
+    cudaError_t rc = cudaGetDevice(&dev);
+    if (rc != cudaSuccess) return rc;
+    const uint64_t bit = dev < kTrainDevices ? 1ull << dev : 0;
+    if (done.load(std::memory_order_relaxed) & bit) return cudaSuccess;
+    rc = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    if (rc == cudaSuccess) done.fetch_or(bit, std::memory_order_relaxed);
+    return rc;
+}
+
 // Whether every row of a matrix begins on 16 bytes (absent ones count as such).
 inline bool wide_rows(const void* p, int64_t ld, int bytes) { return !p || (aligned_to(p, 16) && ld % (16 / bytes) == 0); }
 

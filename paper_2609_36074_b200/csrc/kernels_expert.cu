@@ -24,7 +24,7 @@
 // Every wait is bounded; after one that runs out the block issues nothing more and its remaining tiles are NaN.
 #include <cuda.h>
 #include <cudaTypedefs.h>
-#include "train_common.cuh"
+#include "expert_common.cuh"
 #include "pipeline.cuh"
 #include "tc_common.cuh"
 
@@ -636,7 +636,7 @@ bool encode(CUtensorMap* map, const Operand& o, int experts, int box_rows, bool 
 template <auto kern, int SHARED>
 int launch(const Product& q, int sms, int64_t tiles, bool by_index, cudaStream_t st)
 {
-    if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, SHARED) != cudaSuccess) {
+    if (allow_shared<kern>(SHARED) != cudaSuccess) {
         cudaGetLastError();
         return GEM_NLR_E_CUDA;
     }

@@ -878,10 +878,6 @@ cudaError_t launch_route(F kern, int grid, int threads, int shared, bool early, 
     at[0].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = at;
     cfg.numAttrs = early;
-    if (shared > 48 * 1024) {
-        const cudaError_t rc = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, shared);
-        if (rc != cudaSuccess) return rc;
-    }
     return cudaLaunchKernelEx(&cfg, kern, args...);
 }
 
@@ -932,6 +928,8 @@ extern "C" int gem_nlr_route(const void* logits_dev, int32_t type, int64_t ld, c
                              offset_dev, row_dev, place_dev, (int32_t*)scratch_dev, per_warp};
             const int counts = (kWarps * (experts | 1) + 2 * experts + 1) * 4, space = LANES * V * 4 + kWarps * (int)(groups > 1 ? sizeof(Sp) : offsetof(Sp, group)) + 16;
             cudaStream_t st = (cudaStream_t)cuda_stream;
+            constexpr int most = (kWarps * (LANES * V | 1) + 3 * LANES * V + 1) * 4 + kWarps * (int)sizeof(Sp) + 16;
+            if ((one ? allow_shared<k_route<LANES, V, T, true>>(most) : allow_shared<k_route<LANES, V, T, false>>(most)) != cudaSuccess) return told(cudaErrorInvalidValue);
             if (one) return told(launch_route(k_route<LANES, V, T, true>, 1, kThreads, counts + space, false, st, r));
             cudaError_t rc = launch_route(k_route<LANES, V, T, false>, blocks, kThreads, counts + space, false, st, r);
             if (rc == cudaSuccess) rc = launch_route(k_route_places, blocks, kThreads, (3 * experts + 1) * 4, true, st, r, blocks);

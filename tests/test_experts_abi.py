@@ -1,4 +1,5 @@
 """Host-only checks of the expert layer's entry points: what they refuse before anything is launched."""
+import ctypes as C
 import math
 
 import pytest
@@ -97,8 +98,11 @@ def test_combine_refuses():
 
 
 def test_activation_refuses():
-    fns = experts._load()
-    assert fns["checkpoint_blocks"](100, 0) == 4 and fns["checkpoint_blocks"](100, 1) == 8 and fns["checkpoint_blocks"](0, 0) == fns["checkpoint_blocks"](4, 2) == 0
+    blocks = gem.lib().gem_nlr_checkpoint_blocks
+    blocks.argtypes, blocks.restype = [C.c_int32, C.c_int32], C.c_int64
+    for d in (1, 31, 32, 33, 100, 4096):
+        assert blocks(d, 0) == experts._blocks(d, False) and blocks(d, 1) == experts._blocks(d, True)
+    assert blocks(100, 1) == 8 and blocks(0, 0) == blocks(4, 2) == 0
     good = dict(z=P, type=0, ldz=32, n=5, d=16, kind=1, gated=1, y=2 * P, ldy=16, q=P, scale=P)
     refuses("activation", good, (
         dict(z=None), dict(z=P + 1), dict(type=3), dict(ldz=-1), dict(n=-1), dict(d=0), dict(d=(1 << 29) + 1), dict(kind=4), dict(kind=-1), dict(gated=2), dict(y=P), dict(y=2 * P + 2),
