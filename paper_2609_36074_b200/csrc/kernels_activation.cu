@@ -21,13 +21,21 @@ constexpr int kThreads = 256;
 // a tenth of a 16-bit step at most).
 template <typename T> __device__ __forceinline__ float exp_of(float x) { return sizeof(T) == 4 ? expf(x) : __expf(x); }
 
+// 1 / x to 2^-23 of itself, for x from 1 to 2.
+__device__ __forceinline__ float inverse(float x)
+{
+    float y;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+
 // f(z) and f'(z).
 template <typename T, int KIND>
 __device__ __forceinline__ void act(float z, float& value, float& slope)
 {
     if constexpr (KIND == GEM_NLR_SILU) {
         const float t = exp_of<T>(-fabsf(z)), over = z < 0.0f ? t : 1.0f;               // no overflow far below 0
-        const float p = sizeof(T) == 4 ? over / (1.0f + t) : __fdividef(over, 1.0f + t);
+        const float p = sizeof(T) == 4 ? over / (1.0f + t) : over * inverse(1.0f + t);
         value = z * p;
         slope = fmaf(value, 1.0f - p, p);
     } else if constexpr (KIND == GEM_NLR_GELU) {
@@ -49,9 +57,10 @@ template <typename T>
 __device__ __forceinline__ uint32_t to_8_bits(const float (&v)[8], uint2& q)
 {
     constexpr int last = (std::is_same_v<T, __half> ? 9 : 121) + 127;
-    uint32_t top = 0;
+    float largest = v[0];                                          // by magnitude; a NaN stays
 #pragma unroll
-    for (int i = 0; i < 8; ++i) top = max(top, __float_as_uint(v[i]) & 0x7fffffffu);
+    for (int i = 1; i < 8; ++i) asm("max.NaN.xorsign.abs.f32 %0, %0, %1;" : "+f"(largest) : "f"(v[i]));
+    uint32_t top = __float_as_uint(largest) & 0x7fffffffu;
     top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
     top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
     q = make_uint2(0, 0);
@@ -59,10 +68,15 @@ __device__ __forceinline__ uint32_t to_8_bits(const float (&v)[8], uint2& q)
     const int field = (int)((top + 0x10000u) >> 23) - 6;           // e + 127
     const uint32_t scale = (uint32_t)min(max(field, 0), last);
     const float up = __uint_as_float((254u - scale) << 23);        // 2^-e
-    uint32_t w[2] = {0, 0};
+    // Added to 1.5 2^23 a number is rounded to a whole one, whose low byte is q.  Beyond the last scale it is held as 127.
+    uint32_t b[8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) w[i >> 2] |= ((uint32_t)__float2int_rn(fminf(fmaxf(v[i] * up, -127.0f), 127.0f)) & 0xffu) << (8 * (i & 3));
-    q = make_uint2(w[0], w[1]);
+    for (int i = 0; i < 8; ++i) b[i] = __float_as_uint(fmaf(v[i], up, 12582912.0f));
+    if (field > last)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) b[i] = __float_as_uint(fminf(fmaxf(v[i] * up, -127.0f), 127.0f) + 12582912.0f);
+    q = make_uint2(__byte_perm(__byte_perm(b[0], b[1], 0x0040), __byte_perm(b[2], b[3], 0x0040), 0x5410),
+                   __byte_perm(__byte_perm(b[4], b[5], 0x0040), __byte_perm(b[6], b[7], 0x0040), 0x5410));
     return scale;
 }
 
@@ -71,7 +85,8 @@ __device__ __forceinline__ void from_8_bits(uint2 q, uint32_t scale, float (&v)[
     // 2^e for e >= -126; -127 is a subnormal
     const float unit = scale == 255u ? __uint_as_float(0x7fc00000u) : scale ? __uint_as_float(scale << 23) : __uint_as_float(0x00400000u);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = (float)(int8_t)(((i < 4 ? q.x : q.y) >> (8 * (i & 3))) & 0xffu) * unit;
+    for (int i = 0; i < 8; ++i)          // 2^23 + 128 + q has q + 128 in its low byte
+        v[i] = (__uint_as_float(__byte_perm((i < 4 ? q.x : q.y) ^ 0x80808080u, 0x4b000000u, 0x7540 + (i & 3))) - 8388736.0f) * unit;
 }
 
 // Threads (x: eight columns each, y: rows) over the columns of one half, then over rows.  The columns go in whole steps of
