@@ -38,6 +38,22 @@ __device__ __forceinline__ void store8(T* __restrict__ p, int many, const float 
     }
 }
 
+// Blocks of up to 256 threads over the vectors of rows (x, in equal steps, whole warps where there are many) and over rows (y).
+struct RowBlocks { dim3 grid, block; };
+inline RowBlocks row_blocks(int64_t n, int vecs)
+{
+    int x = 4;
+    if (vecs > 16) {
+        const int steps = (vecs + 255) / 256;
+        x = ((vecs + steps - 1) / steps + 31) / 32 * 32;
+    } else {
+        while (x < vecs) x *= 2;
+    }
+    const int rows = 256 / x;
+    const int64_t steps = (n + rows - 1) / rows, most = (int64_t)kTrainSMs * 64;
+    return {dim3((unsigned)(steps < most ? steps : most)), dim3(x, rows)};
+}
+
 // Lets a kernel have `bytes` of shared memory, once on each device.
 template <auto kern> inline cudaError_t allow_shared(int bytes)
 {

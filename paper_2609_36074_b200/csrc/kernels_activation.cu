@@ -196,18 +196,6 @@ k_activation_backward(const T* __restrict__ dy, int64_t lddy, const T* __restric
     }
 }
 
-struct Shape { dim3 grid, block; };
-
-// Blocks of 256 threads: as many along a row as it has vectors, up to 256, the rest rows.
-Shape shape_of(int64_t n, int vecs)
-{
-    int x = 4;
-    while (x < vecs && x < kThreads) x *= 2;
-    const int rows = kThreads / x;
-    const int64_t steps = (n + rows - 1) / rows, most = (int64_t)kTrainSMs * 64;
-    return {dim3((unsigned)(steps < most ? steps : most)), dim3(x, rows)};
-}
-
 template <typename F> int by_kind(int32_t kind, F f)
 {
     switch (kind) {
@@ -248,7 +236,7 @@ extern "C" int gem_nlr_activation(const void* z_dev, int32_t type, int64_t ld_z,
         return GEM_NLR_E_INVALID;
     const int blocks = (d + 31) / 32;
     const bool wide = d % 8 == 0 && wide_rows(z_dev, ld_z, tb) && wide_rows(y_dev, ld_y, tb);
-    const Shape sh = shape_of(n, blocks * 4);
+    const RowBlocks sh = row_blocks(n, blocks * 4);
     return by_type(type, [&](auto t) {
         using T = decltype(t);
         return by_kind(kind, [&](auto f) {
@@ -276,7 +264,7 @@ extern "C" int gem_nlr_activation_backward(const void* dy_dev, int32_t type, int
         return GEM_NLR_E_INVALID;
     const int blocks = (d + 31) / 32;
     const bool wide = d % 8 == 0 && wide_rows(z_dev, ld_z, tb) && wide_rows(dy_dev, ld_dy, tb) && wide_rows(dz_dev, ld_dz, tb) && wide_rows(y_dev, ld_y, tb);
-    const Shape sh = shape_of(n, blocks * 4);
+    const RowBlocks sh = row_blocks(n, blocks * 4);
     return by_type(type, [&](auto t) {
         using T = decltype(t);
         return by_kind(kind, [&](auto f) {

@@ -3,17 +3,17 @@
 //   forward    out_t = sum_j w_tj y_place(t,j)
 //   backward   dy_place(t,j) = w_tj dout_t,  dw_tj = <dout_t, y_place(t,j)>
 //
-// Bound by HBM: y is read once, in rows; a row of dout is read once for all its slots.  Sums in FP32, in a fixed order.
+// Bound by HBM: y is read once, in rows; a row of dout is read once for all its slots, 2, 4 or 8 of which are taken together.  Sums in
+// FP32, in a fixed order.
 #include "expert_common.cuh"
 
 namespace gemnlr {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kSlots = 8;                 // slots whose loads are in flight together
 
 // Eight columns a thread: x along a row, y over rows.
-template <typename T, bool WIDE>
+template <typename T, bool WIDE, int SLOTS>
 __global__ void __launch_bounds__(kThreads)
 k_combine(const T* __restrict__ y, int64_t ldy, int64_t places, const int32_t* __restrict__ place, const float* __restrict__ weight,
           int64_t n, int k, int d, T* __restrict__ out, int64_t ldo)
@@ -26,17 +26,17 @@ k_combine(const T* __restrict__ y, int64_t ldy, int64_t places, const int32_t* _
         for (int c = threadIdx.x; c < vecs; c += blockDim.x) {
             const int col = c * 8;
             float sum[8] = {};
-            for (int j0 = 0; j0 < k; j0 += kSlots) {
-                int p[kSlots];
-                float w[kSlots];
+            for (int j0 = 0; j0 < k; j0 += SLOTS) {
+                int p[SLOTS];
+                float w[SLOTS];
 #pragma unroll
-                for (int j = 0; j < kSlots; ++j) {
+                for (int j = 0; j < SLOTS; ++j) {
                     p[j] = j0 + j < k ? __ldg(place + t * k + j0 + j) : -1;
                     w[j] = j0 + j < k ? weight ? __ldg(weight + t * k + j0 + j) : 1.0f : 0.0f;
                     if (p[j] >= places) p[j] = -1;
                 }
 #pragma unroll
-                for (int j = 0; j < kSlots; ++j) {
+                for (int j = 0; j < SLOTS; ++j) {
                     if (p[j] >= 0) {
                         float v[8];
                         load8<WIDE>(y + p[j] * ldy + col, d - col, v);
@@ -54,24 +54,24 @@ k_combine(const T* __restrict__ y, int64_t ldy, int64_t places, const int32_t* _
 }
 
 // TPR threads share a row t; NT threads a block.
-template <typename T, bool WIDE, int TPR>
+template <typename T, bool WIDE, int SLOTS, int TPR>
 __global__ void __launch_bounds__(kThreads)
 k_combine_backward(const T* __restrict__ dout, int64_t ldo, const T* __restrict__ y, int64_t ldy, int64_t places,
                    const int32_t* __restrict__ place, const float* __restrict__ weight, const int32_t* __restrict__ offset, int experts,
                    int64_t n, int k, int d, T* __restrict__ dy, int64_t lddy, float* __restrict__ dweight)
 {
     constexpr int ROWS = kThreads / TPR;
-    __shared__ float sred[kThreads / 32][kSlots];
+    __shared__ float sred[kThreads / 32][SLOTS];
     const int vecs = (d + 7) / 8;
     const int me = threadIdx.x % TPR, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int64_t steps = (n + ROWS - 1) / ROWS;
     for (int64_t s = blockIdx.x; s < steps; s += gridDim.x) {
         const int64_t t = s * ROWS + threadIdx.x / TPR;
-        for (int j0 = 0; j0 < k; j0 += kSlots) {
-            int p[kSlots];
-            float w[kSlots], dot[kSlots];
+        for (int j0 = 0; j0 < k; j0 += SLOTS) {
+            int p[SLOTS];
+            float w[SLOTS], dot[SLOTS];
 #pragma unroll
-            for (int j = 0; j < kSlots; ++j) {
+            for (int j = 0; j < SLOTS; ++j) {
                 const bool in = t < n && j0 + j < k;
                 p[j] = in ? __ldg(place + t * k + j0 + j) : -1;
                 w[j] = in ? weight ? __ldg(weight + t * k + j0 + j) : 1.0f : 0.0f;
@@ -83,7 +83,7 @@ k_combine_backward(const T* __restrict__ dout, int64_t ldo, const T* __restrict_
                 float g[8];
                 load8<WIDE>(dout + t * ldo + col, d - col, g);
 #pragma unroll
-                for (int j = 0; j < kSlots; ++j) {
+                for (int j = 0; j < SLOTS; ++j) {
                     if (p[j] < 0) continue;
                     if (dweight) {
                         float v[8];
@@ -101,20 +101,20 @@ k_combine_backward(const T* __restrict__ dout, int64_t ldo, const T* __restrict_
             }
             if (dweight) {
 #pragma unroll
-                for (int j = 0; j < kSlots; ++j) dot[j] = warp_sum(dot[j]);
+                for (int j = 0; j < SLOTS; ++j) dot[j] = warp_sum(dot[j]);
                 if constexpr (TPR > 32) {
                     __syncthreads();
                     if (lane == 0)
-                        for (int j = 0; j < kSlots; ++j) sred[warp][j] = dot[j];
+                        for (int j = 0; j < SLOTS; ++j) sred[warp][j] = dot[j];
                     __syncthreads();
-                    if (t < n && me < kSlots && j0 + me < k) {
+                    if (t < n && me < SLOTS && j0 + me < k) {
                         float sum = 0.0f;
                         for (int x = 0; x < TPR / 32; ++x) sum += sred[warp / (TPR / 32) * (TPR / 32) + x][me];
                         dweight[t * k + j0 + me] = sum;
                     }
                 } else if (t < n && lane == 0) {
 #pragma unroll
-                    for (int j = 0; j < kSlots; ++j)
+                    for (int j = 0; j < SLOTS; ++j)
                         if (j0 + j < k) dweight[t * k + j0 + j] = dot[j];
                 }
             }
@@ -128,6 +128,12 @@ k_combine_backward(const T* __restrict__ dout, int64_t ldo, const T* __restrict_
         for (int64_t p = used + blockIdx.x; p < places; p += gridDim.x)
             for (int c = threadIdx.x; c < vecs; c += kThreads) store8<WIDE>(dy + p * lddy + c * 8, d - c * 8, zero);
     }
+}
+
+template <typename F> int by_slots(int k, F f)
+{
+    using std::integral_constant;
+    return k <= 2 ? f(integral_constant<int, 2>{}) : k <= 4 ? f(integral_constant<int, 4>{}) : f(integral_constant<int, 8>{});
 }
 
 template <typename F> int by_wide(bool wide, F f) { return wide ? f(std::true_type{}) : f(std::false_type{}); }
@@ -148,16 +154,15 @@ extern "C" int gem_nlr_combine(const void* y_dev, int32_t type, int64_t ld_y, in
     if ((places > 0 && !rows_fine(y_dev, tb, ld_y, 0)) || !place_dev || !aligned_to(place_dev, 4) || !aligned_to(weight_dev, 4) ||
         !rows_fine(out_dev, tb, ld_out, d) || out_dev == y_dev)
         return GEM_NLR_E_INVALID;
-    const int vecs = (d + 7) / 8;
-    int x = 1;
-    while (x < vecs && x < kThreads) x *= 2;
-    const int64_t steps = (n + kThreads / x - 1) / (kThreads / x), most = (int64_t)kTrainSMs * 64;
-    const dim3 grid((unsigned)(steps < most ? steps : most)), block(x, kThreads / x);
+    const RowBlocks sh = row_blocks(n, (d + 7) / 8);
     return by_type(type, [&](auto t) {
         using T = decltype(t);
         return by_wide(d % 8 == 0 && wide_rows(y_dev, ld_y, tb) && wide_rows(out_dev, ld_out, tb), [&](auto w) {
-            k_combine<T, w.value><<<grid, block, 0, (cudaStream_t)cuda_stream>>>((const T*)y_dev, ld_y, places, place_dev, weight_dev, n, (int)k, (int)d, (T*)out_dev, ld_out);
-            return launched();
+            return by_slots(k, [&](auto s) {
+                k_combine<T, w.value, s.value><<<sh.grid, sh.block, 0, (cudaStream_t)cuda_stream>>>((const T*)y_dev, ld_y, places, place_dev, weight_dev, n, (int)k, (int)d,
+                                                                                                   (T*)out_dev, ld_out);
+                return launched();
+            });
         });
     });
 }
@@ -187,10 +192,12 @@ extern "C" int gem_nlr_combine_backward(const void* dout_dev, int64_t ld_dout, c
         using T = decltype(t);
         return by_wide(wide, [&](auto w) {
             return by_wide(few, [&](auto f) {
-                k_combine_backward<T, w.value, f.value ? kThreads : 32><<<grid, kThreads, 0, (cudaStream_t)cuda_stream>>>(
-                    (const T*)dout_dev, ld_dout, (const T*)y_dev, ld_y, places, place_dev, weight_dev, offset_dev, experts, n, (int)k, (int)d, (T*)dy, ld_dy,
-                    dweight_dev);
-                return launched();
+                return by_slots(k, [&](auto s) {
+                    k_combine_backward<T, w.value, s.value, f.value ? kThreads : 32><<<grid, kThreads, 0, (cudaStream_t)cuda_stream>>>(
+                        (const T*)dout_dev, ld_dout, (const T*)y_dev, ld_y, places, place_dev, weight_dev, offset_dev, experts, n, (int)k, (int)d, (T*)dy, ld_dy,
+                        dweight_dev);
+                    return launched();
+                });
             });
         });
     });
