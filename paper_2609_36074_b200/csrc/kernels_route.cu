@@ -709,8 +709,9 @@ struct RouteGrad {
     int64_t ldd;
 };
 
-// LANES lanes a row, V neighbouring logits a lane.  Slots are taken LANES at a time, a slot a lane; each lane then picks up the shares of
-// its own experts.
+// LANES lanes a row, V neighbouring logits a lane, a slot a lane.  Rows are stored as if nothing were chosen, then each slot's lane stores
+// the gradient of its expert over that.  Rows with more slots than lanes, or with an expert twice, give their shares to the
+// lanes that hold the experts first.
 template <int LANES, int V, typename T>
 __global__ void __launch_bounds__(256)
 k_route_backward(const __grid_constant__ RouteGrad r)
@@ -719,12 +720,28 @@ k_route_backward(const __grid_constant__ RouteGrad r)
     const int lane = threadIdx.x & 31, me = lane % LANES;
     const bool soft = r.score == GEM_NLR_SOFTMAX;
     const bool whole = soft && !r.renorm;                  // every logit has a share
+    const int rounds = (r.k + LANES - 1) / LANES;
     const int64_t steps = (r.n + ROWS - 1) / ROWS;
+    // e^(z - m): 16-bit gradients are off by a tenth of their rounding at most by the fast one (2^-21 of itself at 16 below m)
+    const auto power = [](float z, float m) { return sizeof(T) == 4 ? expf(z - m) : fast_exp2((z - m) * kLog2E); };
+    const auto log_score = [&](float x) { return soft || x == -INFINITY ? x : fminf(x, 0.0f) - log1pf(expf(-fabsf(x))); };
     for (int64_t step = blockIdx.x; step < steps; step += gridDim.x) {
         const int64_t row = step * ROWS + threadIdx.x / LANES;
         const bool in = row < r.n;
         const T* zr = reinterpret_cast<const T*>(r.z) + (in ? row : 0) * r.ld;
-        float z[V], m = -INFINITY, sum = 0.0f;
+        T* dr = reinterpret_cast<T*>(r.dz) + (in ? row : 0) * r.ldd;
+        const auto slot = [&](int round, int& e, float& v, float& x) {
+            const int j = round * LANES + me;
+            e = in && j < r.k ? __ldg(r.expert + row * r.k + j) : -1;
+            v = e >= 0 && e < r.experts ? __ldg(r.dweight + row * r.k + j) * r.scale : 0.0f;
+            if (e >= r.experts) e = -1;
+            x = e >= 0 ? to_f(zr[e]) : -INFINITY;
+        };
+        int e0;
+        float v0, x0;                                       // the first round's, which mostly is the only one
+        slot(0, e0, v0, x0);
+        float z[V], m = -INFINITY, sum = 0.0f, over = 0.0f, top = -INFINITY, total = 0.0f, t = 0.0f, coef = 0.0f;
+        bool any = e0 >= 0;
         if (whole) {
 #pragma unroll
             for (int i = 0; i < V; ++i) z[i] = -INFINITY;
@@ -750,87 +767,68 @@ k_route_backward(const __grid_constant__ RouteGrad r)
             // a NaN among the logits is lost in the maximum and comes back in the sum
 #pragma unroll
             for (int i = 0; i < V; ++i) {
-                z[i] = z[i] == -INFINITY ? 0.0f : expf(z[i] - m);
+                z[i] = z[i] == -INFINITY ? 0.0f : power(z[i], m);
                 sum += z[i];
             }
             sum = lanes_sum<LANES>(sum);
+            over = sum == 0.0f ? 0.0f : 1.0f / sum;
         }
-        const float over = 1.0f / sum;
-        // the slots: weights' shares first (their sum over all slots), then each lane's own
-        const int rounds = (r.k + LANES - 1) / LANES;
-        float top = -INFINITY, total = 0.0f, t = 0.0f;
-        bool any = false;
-        const auto slot = [&](int round, int& e, float& v, float& x) {
-            const int j = round * LANES + me;
-            e = in && j < r.k ? __ldg(r.expert + row * r.k + j) : -1;
-            if (e >= r.experts) e = -1;
-            v = e >= 0 ? __ldg(r.dweight + row * r.k + j) * r.scale : 0.0f;
-            x = e >= 0 ? to_f(zr[e]) : -INFINITY;
-            any |= e >= 0;
-        };
-        const auto log_score = [&](float x) { return soft || x == -INFINITY ? x : fminf(x, 0.0f) - log1pf(expf(-fabsf(x))); };
-        float l0 = 0.0f, v0 = 0.0f, x0 = 0.0f;              // the first round's, which mostly is the only one
-        int e0 = -1;
+        float l0 = 0.0f;
         if (r.renorm) {
-            for (int q = 0; q < rounds; ++q) {
+            l0 = log_score(x0);
+            top = l0;
+            for (int q = 1; q < rounds; ++q) {
                 int e; float v, x;
                 slot(q, e, v, x);
-                const float l = log_score(x);
-                if (q == 0) { e0 = e; v0 = v; x0 = x; l0 = l; }
-                top = fmaxf(top, l);
+                top = fmaxf(top, log_score(x));
             }
             top = lanes_top<LANES>(top);
-            for (int q = 0; q < rounds; ++q) {
-                int e = e0; float v = v0, x = x0, l = l0;
-                if (q > 0) { slot(q, e, v, x); l = log_score(x); }
-                const float p = e >= 0 && x != -INFINITY ? expf(l - top) : 0.0f;
-                total += p;
-                t += p * v;
-            }
+        }
+        for (int q = 0; q < rounds && (whole || r.renorm); ++q) {
+            int e = e0; float v = v0, x = x0, l = l0;
+            if (q > 0) { slot(q, e, v, x); l = r.renorm ? log_score(x) : 0.0f; any |= e >= 0; }
+            const float p = e < 0 || x == -INFINITY ? 0.0f : whole ? power(x, m) * over : expf(l - top);
+            total += p;
+            t += p * v;
+        }
+        if (r.renorm) {
             total = lanes_sum<LANES>(total);
             t = lanes_sum<LANES>(t);
             if (total != 0.0f) t /= total;
-        } else {
-            for (int q = 0; q < rounds; ++q) {
-                int e; float v, x;
-                slot(q, e, v, x);
-                if (q == 0) { e0 = e; v0 = v; x0 = x; }
-                if (whole && e >= 0 && x != -INFINITY) t += expf(x - m) * over * v;
-            }
-            if (whole) t = lanes_sum<LANES>(t);
+        } else if (whole) {
+            t = lanes_sum<LANES>(t);
+            any = (__ballot_sync(kAll, any) >> (lane - me) & (LANES == 32 ? kAll : (1u << (LANES & 31)) - 1u)) != 0;
+            coef = any ? -t * over : 0.0f;
         }
+        // the gradient of slot's expert beyond what every expert has
+        const auto share = [&](int e, float v, float x, float l) {
+            if (e < 0 || x == -INFINITY) return 0.0f;
+            if (whole) return power(x, m) * over * v;
+            const float rest = soft ? 1.0f : 1.0f / (1.0f + expf(x));              // 1 - s
+            return r.renorm ? (total != 0.0f ? expf(l - top) / total : 0.0f) * (v - t) * rest : v * rest / (1.0f + expf(-x));
+        };
         float out[V];
-        if (whole) {
-            unsigned has = __ballot_sync(kAll, any);
-            any = has >> (lane - me) & (LANES == 32 ? kAll : (1u << (LANES & 31)) - 1u);
 #pragma unroll
-            for (int i = 0; i < V; ++i) out[i] = any && sum > 0.0f ? -(z[i] * over) * t : any && sum != sum ? sum : 0.0f;
-        } else {
+        for (int i = 0; i < V; ++i) out[i] = whole ? z[i] * coef : 0.0f;
+        const float g0 = share(e0, v0, x0, l0);
+        const unsigned same = __match_any_sync(kAll, e0 < 0 ? -1 - lane : e0 | (lane / LANES) << 16);
+        const bool direct = rounds == 1 && !__any_sync(kAll, same & (same - 1));
+        if (!direct) {
+            for (int q = 0; q < rounds; ++q) {
+                int e = e0; float v = v0, x = x0, l = l0;
+                if (q > 0) { slot(q, e, v, x); l = r.renorm ? log_score(x) : 0.0f; }
+                const float g = share(e, v, x, l);
+                const int most = min(LANES, r.k - q * LANES);
+                for (int j = 0; j < most; ++j) {
+                    const int at = __shfl_sync(kAll, e, j, LANES) - me * V;
+                    const float add = __shfl_sync(kAll, g, j, LANES);
 #pragma unroll
-            for (int i = 0; i < V; ++i) out[i] = 0.0f;
-        }
-        for (int q = 0; q < rounds; ++q) {
-            int e = e0; float v = v0, x = x0, l = l0;
-            if (q > 0) { slot(q, e, v, x); l = r.renorm ? log_score(x) : 0.0f; }
-            float g;
-            if (whole) {
-                g = expf(x - m) * over * v;
-            } else {
-                const float rest = soft ? 1.0f : 1.0f / (1.0f + expf(x));          // 1 - s
-                g = r.renorm ? (total != 0.0f ? expf(l - top) / total : 0.0f) * (v - t) * rest : v * rest / (1.0f + expf(-x));
-            }
-            if (e < 0 || x == -INFINITY) g = 0.0f;
-            const int most = min(LANES, r.k - q * LANES);
-            for (int j = 0; j < most; ++j) {
-                const int at = __shfl_sync(kAll, e, j, LANES) - me * V;
-                const float add = __shfl_sync(kAll, g, j, LANES);
-#pragma unroll
-                for (int i = 0; i < V; ++i)
-                    if (i == at) out[i] += add;
+                    for (int i = 0; i < V; ++i)
+                        if (i == at) out[i] += add;
+                }
             }
         }
         if (in) {
-            T* dr = reinterpret_cast<T*>(r.dz) + row * r.ldd;
             if (r.wide) {
 #pragma unroll
                 for (int b = 0; b < V / 8; ++b) {
@@ -845,6 +843,11 @@ k_route_backward(const __grid_constant__ RouteGrad r)
                 for (int i = 0; i < V; ++i)
                     if (me * V + i < r.experts) dr[me * V + i] = from_f<T>(out[i]);
             }
+        }
+        __syncwarp();
+        if (direct && e0 >= 0) {
+            const float every = whole && x0 != -INFINITY ? power(x0, m) * coef : whole ? 0.0f * coef : 0.0f;
+            dr[e0] = from_f<T>(every + g0);
         }
     }
 }

@@ -163,6 +163,18 @@ def test_gradient_of_slots_that_are_not_there():
             assert (d[5] == 0).all()
 
 
+@pytest.mark.parametrize("e,k", [(8, 2), (40, 4), (300, 6), (20, 9)])
+def test_gradient_of_an_expert_named_twice_is_the_sum(e, k):
+    z = logits(60, e)
+    gen = torch.Generator(device="cuda").manual_seed(k)
+    twice = torch.randint(0, max(2, k - 1), (60, k), generator=gen, device="cuda", dtype=torch.int32)
+    v = torch.randn(60, k, generator=gen, device="cuda")
+    for score in ("softmax", "sigmoid"):
+        for renorm in (True, False):
+            grad, bound = ref.route_grad(v, z, twice, score, renorm, 1.0)
+            assert_within(gem.route_backward(v, z, twice, score, renorm), grad, bound, f"{score} {renorm}")
+
+
 def test_gradient_against_differences():
     z = logits(6, 10, F32).double()
     r = gem.route(z.float(), 3, "softmax")
