@@ -54,13 +54,6 @@ __device__ __forceinline__ uint64_t key_of(double c)
 }
 constexpr uint32_t kNone32 = 0x007fffffu;                   // -inf
 
-__device__ __forceinline__ uint64_t warp_max(uint64_t k)
-{
-    const uint32_t hi = __reduce_max_sync(kAll, (uint32_t)(k >> 32));
-    const uint32_t lo = __reduce_max_sync(kAll, (uint32_t)(k >> 32) == hi ? (uint32_t)k : 0u);
-    return (uint64_t)hi << 32 | lo;
-}
-
 // (NaNs are left out.)
 __device__ __forceinline__ float warp_top(float v)
 {
@@ -152,62 +145,58 @@ __device__ __forceinline__ void take_weights(const Route& r, int64_t row, bool i
 }
 
 // ---- the choice in FP64, a row by a warp: lane's experts are lane, lane + 32, ... ------------------------------------------------------
-// Short: few rows come here, and what they wait for is the code and its chains.  stays: the groups to choose from, 0 where FP32 scores
-// do not decide them either.  chosen: shared memory of a row.
+// Few rows come here, and what a block waits for is one row's chain of operations.  stays: the groups to choose from, 0 where FP32 scores
+// do not decide them either.  chosen: shared memory of a row; judged: of `experts` numbers where there are groups.
 template <typename T>
-__device__ __noinline__ void route_in_64_bits(const Route& r, int64_t row, unsigned stays, int lane, int32_t* chosen, int32_t* counts)
+__device__ __noinline__ void route_in_64_bits(const Route& r, int64_t row, unsigned stays, int lane, int32_t* chosen, double* judged, int32_t* counts)
 {
     constexpr int MOST = GEM_NLR_MAX_EXPERTS / 32;
     const T* zr = reinterpret_cast<const T*>(r.z) + row * r.ld;
     const bool soft = r.score == GEM_NLR_SOFTMAX;
     const double none = -(double)INFINITY;
     const int size = r.experts / r.groups;
-    double c[MOST];                                      // what is chosen by
-    float m = -INFINITY, whole = 0.0f;
-    double sum = 1.0;
+    double c[MOST];                                      // exponentials, then what is chosen by
+    float m = 0.0f, whole = 0.0f;
     if (soft) {
-#pragma unroll 1
+        m = -INFINITY;
         for (int i = lane; i < r.experts; i += 32) m = fmaxf(m, to_f(zr[i]));
         m = warp_top(m);
-        sum = 0.0;
-#pragma unroll 2
-        for (int i = lane; i < r.experts; i += 32) {
-            const float z = to_f(zr[i]);
-            const double e = exp((double)z - (double)m);
-            c[i >> 5] = e;
-            sum += e;
-            whole += expf(z - m);
-        }
+    }
+    double sum = 0.0;
+#pragma unroll 4
+    for (int i = lane; i < r.experts; i += 32) {
+        const float z = to_f(zr[i]);
+        const double e = exp(soft ? (double)z - (double)m : -(double)z);
+        c[i >> 5] = e;
+        sum += e;
+        if (soft && !r.renorm) whole += expf(z - m);
+    }
+    if (soft) {
         sum = warp_sum(sum);
         whole = warp_sum(whole);
     }
-    // what groups are judged by, then what is chosen by
-    const auto judged = [&](int i, bool group) {
-        const float z = to_f(zr[i]);
-        const double s = soft ? c[i >> 5] / sum : 1.0 / (1.0 + exp(-(double)z));
-        return z == -INFINITY ? none : r.bias ? s + (double)__ldg(r.bias + i) : group && r.best == 2 ? s : (double)z;
-    };
+    const auto score = [&](int i) { return soft ? c[i >> 5] / sum : 1.0 / (1.0 + c[i >> 5]); };
+    const auto by_choice = [&](int i, float z) { return z == -INFINITY ? none : r.bias ? score(i) + (double)__ldg(r.bias + i) : (double)z; };
     if (!stays) {
+#pragma unroll 4
+        for (int i = lane; i < r.experts; i += 32) {
+            const float z = to_f(zr[i]);
+            judged[i] = !r.bias && r.best == 2 && z != -INFINITY ? score(i) : by_choice(i, z);
+        }
+        __syncwarp();
         double mine = none;                              // lane g: group g's score
-#pragma unroll 1
-        for (int g = 0; g < r.groups; ++g) {
+        if (lane < r.groups) {
             double first = none, second = none;
-#pragma unroll 1
-            for (int i = g * size + ((lane - g * size) & 31); i < (g + 1) * size; i += 32) {
-                const double x = judged(i, true);
-                second = fmax(second, fmin(first, x));
-                first = fmax(first, x);
+#pragma unroll 4
+            for (int i = lane * size; i < (lane + 1) * size; ++i) {
+                const double x = judged[i];
+                second = x > first ? first : x > second ? x : second;
+                first = x > first ? x : first;
             }
-#pragma unroll 1
-            for (int o = 1; o < 32; o *= 2) {
-                const double a = __shfl_xor_sync(kAll, first, o), b = __shfl_xor_sync(kAll, second, o);
-                second = fmax(fmin(first, a), fmax(second, b));
-                first = fmax(first, a);
-            }
-            if (lane == g) mine = r.best == 2 && second != none ? first + second : first;
+            mine = r.best == 2 && second != none ? first + second : first;
         }
         int rank = 0;
-#pragma unroll 1
+#pragma unroll 4
         for (int g = 0; g < r.groups; ++g) {
             const double other = __shfl_sync(kAll, mine, g);
             rank += other > mine || (other == mine && g < lane);
@@ -216,27 +205,34 @@ __device__ __noinline__ void route_in_64_bits(const Route& r, int64_t row, unsig
     }
     double top = none;
     unsigned at = kAll;
-#pragma unroll 2
+#pragma unroll 4
     for (int i = lane; i < r.experts; i += 32) {
-        const double x = r.groups == 1 || stays >> (i / size) & 1u ? judged(i, false) : none;
+        const double x = r.groups == 1 || stays >> (i / size) & 1u ? by_choice(i, to_f(zr[i])) : none;
         c[i >> 5] = x;
         if (x > top) { top = x; at = i; }
     }
-#pragma unroll 1
     for (int j = 0; j < r.k; ++j) {
-        const uint64_t key = at == kAll ? 0 : key_of(top), best = warp_max(key);
-        const unsigned index = __reduce_min_sync(kAll, key == best ? at : kAll);
-        if (lane == 0) chosen[j] = best ? (int)index : -1;
-        if (best && index == at) {
-            c[index >> 5] = none;
+        const uint64_t key = at == kAll ? 0 : key_of(top);
+        const uint32_t high = __reduce_max_sync(kAll, (uint32_t)(key >> 32));
+        unsigned best = __ballot_sync(kAll, high && (uint32_t)(key >> 32) == high);
+        if (best & (best - 1)) {
+            // equal in the upper halves: by the lower ones, and among equals the lowest index
+            const uint32_t low = __reduce_max_sync(kAll, best >> lane & 1u ? (uint32_t)key : 0u);
+            best = __ballot_sync(kAll, (best >> lane & 1u) && (uint32_t)key == low);
+            const unsigned index = __reduce_min_sync(kAll, best >> lane & 1u ? at : kAll);
+            best &= 1u << (index & 31u);
+        }
+        const bool own = best >> lane & 1u;
+        if (best ? own : lane == 0) chosen[j] = best ? (int)at : -1;
+        if (own) {
+            c[at >> 5] = none;
             top = none;
             at = kAll;
-#pragma unroll 1
             for (int i = lane; i < r.experts; i += 32)
                 if (c[i >> 5] > top) { top = c[i >> 5]; at = i; }
         }
-        __syncwarp();
     }
+    __syncwarp();
     take_weights<32>(r, row, true, false, zr, m, whole, chosen, lane, counts);
     __syncwarp();
 }
@@ -316,7 +312,7 @@ template <int LANES, int V> struct Space {
     int32_t later[32];
     uint32_t later_groups[32];
     float group[ROWS][kMaxGroups];
-    float score[ROWS][PITCH];
+    alignas(16) float score[ROWS * PITCH > 2 * LANES * V ? ROWS * PITCH : 2 * LANES * V];        // by row; or by expert in FP64, of one row
 };
 
 // Which groups can be chosen from, a bit each.  c: what the lane's experts' groups are judged by (-inf: none).  close: the border
@@ -340,11 +336,11 @@ __device__ __forceinline__ unsigned kept_groups(const Route& r, const float (&c)
         if (me % lanes == 0 && me / lanes < r.groups) sp.group[mine][me / lanes] = (r.best == 2 && second != -INFINITY ? first + second : first) + 0.0f;
     } else {
 #pragma unroll
-        for (int v = 0; v < V; v += 4) *reinterpret_cast<float4*>(&sp.score[mine][me * V + v]) = make_float4(c[v], c[v + 1], c[v + 2], c[v + 3]);
+        for (int v = 0; v < V; v += 4) *reinterpret_cast<float4*>(&sp.score[mine * Space<LANES, V>::PITCH + me * V + v]) = make_float4(c[v], c[v + 1], c[v + 2], c[v + 3]);
         __syncwarp();
         for (int g = me; g < r.groups; g += LANES) {
             float first = -INFINITY, second = -INFINITY;
-            const float* of = &sp.score[mine][g * size];
+            const float* of = &sp.score[mine * Space<LANES, V>::PITCH + g * size];
 #pragma unroll 4
             for (int i = 0; i < size; ++i) {
                 const float x = of[i];
@@ -634,7 +630,8 @@ k_route(const __grid_constant__ Route r)
             waiting += __popc(rows);
         }
         __syncwarp();
-        for (int i = 0; i < waiting; ++i) route_in_64_bits<T>(r, begin + sp.later[i], sp.later_groups[i], lane, sp.chosen[0], at + warp * pitch);
+        for (int i = 0; i < waiting; ++i) route_in_64_bits<T>(r, begin + sp.later[i], sp.later_groups[i], lane, sp.chosen[0],
+                                                                    reinterpret_cast<double*>(sp.score), at + warp * pitch);
     }
     __syncthreads();
     next_may_start();
