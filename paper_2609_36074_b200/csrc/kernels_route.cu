@@ -38,7 +38,7 @@ struct Route {
     int32_t* row;
     int32_t* place;
     int32_t* counts;        // blocks x experts
-    int64_t rows_per_warp;  // a multiple of the rows that a warp takes at a time
+    int64_t block_rows;     // a multiple of the rows that a warp takes at a time
 };
 
 // Whole numbers in the order of the scores.
@@ -609,7 +609,9 @@ k_route(const __grid_constant__ Route r)
     float* bias = reinterpret_cast<float*>(at) + (before + 3) / 4 * 4;
     Sp& sp = *reinterpret_cast<Sp*>(reinterpret_cast<char*>(bias + LANES * V) + (size_t)warp * (r.groups > 1 ? sizeof(Sp) : offsetof(Sp, group)));
     for (int i = threadIdx.x; i < kWarps * pitch; i += kThreads) at[i] = 0;
-    const int64_t begin = min(r.n, ((int64_t)blockIdx.x * kWarps + warp) * r.rows_per_warp), end = min(r.n, begin + r.rows_per_warp);
+    // the block's rows in whole steps of a warp, as even as they go
+    const int64_t rows = blockIdx.x * r.block_rows, turns = r.block_rows / Sp::ROWS;
+    const int64_t begin = min(r.n, rows + turns * warp / kWarps * Sp::ROWS), end = min(r.n, rows + turns * (warp + 1) / kWarps * Sp::ROWS);
     bool fine = true;
     for (int i = threadIdx.x; i < LANES * V; i += kThreads) {
         bias[i] = r.bias && i < r.experts ? __ldg(r.bias + i) : 0.0f;
@@ -659,7 +661,7 @@ k_route_places(const __grid_constant__ Route r, int blocks)
     int32_t* before = total + r.experts;
     for (int e = threadIdx.x; e < 2 * r.experts; e += kThreads) total[e] = 0;
     __syncthreads();
-    const int begin = (int)(min(r.n, (int64_t)blockIdx.x * kWarps * r.rows_per_warp) * r.k), end = (int)(min(r.n, ((int64_t)blockIdx.x + 1) * kWarps * r.rows_per_warp) * r.k);
+    const int begin = (int)(min(r.n, blockIdx.x * r.block_rows) * r.k), end = (int)(min(r.n, (blockIdx.x + 1) * r.block_rows) * r.k);
     grid_ready();
     // the first entries come with the counts
     const int i0 = begin + threadIdx.x;
@@ -919,13 +921,11 @@ extern "C" int gem_nlr_route(const void* logits_dev, int32_t type, int64_t ld, c
             using T = decltype(t);
             constexpr int LANES = lanes.value, V = v.value, BYTES = V * (int)sizeof(T) < 16 ? V * (int)sizeof(T) : 16;
             using Sp = Space<LANES, V>;
-            const int64_t slots = (int64_t)kBlocks * kWarps;
-            int64_t per_warp = one ? (n + kWarps - 1) / kWarps : (n + slots - 1) / slots;
-            per_warp = (per_warp + Sp::ROWS - 1) / Sp::ROWS * Sp::ROWS;
-            const int blocks = one ? 1 : (int)((n + per_warp * kWarps - 1) / (per_warp * kWarps));
+            const int64_t turns = (n + Sp::ROWS - 1) / Sp::ROWS, block_rows = (one ? turns : (turns + kBlocks - 1) / kBlocks) * Sp::ROWS;
+            const int blocks = one ? 1 : (int)((n + block_rows - 1) / block_rows);
             const bool wide = aligned_to(logits_dev, BYTES) && ld * (int64_t)sizeof(T) % BYTES == 0;
             const Route r = {logits_dev, ld, bias_dev, n, experts, k, score, groups, kept_groups, group_best, renormalize, wide, scale, expert_dev, weight_dev,
-                             offset_dev, row_dev, place_dev, (int32_t*)scratch_dev, per_warp};
+                             offset_dev, row_dev, place_dev, (int32_t*)scratch_dev, block_rows};
             const int counts = (kWarps * (experts | 1) + 2 * experts + 1) * 4, space = LANES * V * 4 + kWarps * (int)(groups > 1 ? sizeof(Sp) : offsetof(Sp, group)) + 16;
             cudaStream_t st = (cudaStream_t)cuda_stream;
             constexpr int most = (kWarps * (LANES * V | 1) + 3 * LANES * V + 1) * 4 + kWarps * (int)sizeof(Sp) + 16;
