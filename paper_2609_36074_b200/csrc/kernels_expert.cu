@@ -1,4 +1,6 @@
-// The experts' products on the tensor cores (tcgen05 + TMEM): FP16 or BF16 operands, FP32 accumulators.
+// The experts' products on the tensor cores (tcgen05 + TMEM): FP16 or BF16 operands, FP32 accumulators.  FP32 operands are split
+// into three BF16 images each, x = x0 + x1 + x2 exactly (8 bits of the 24 apiece), and six of the nine products are summed, the
+// smallest first; the three left out are below 2^-24 of the largest.
 //
 //   rows      C_p = A_row(p) B_e  for the places p of expert e        (y = x W; dx = dy W^T)
 //   weights   C_e = sum over e's places of A_row(p)^T B_row(p)          (dW = x^T dy)
@@ -20,7 +22,8 @@
 //   warps 12-15     (BY_INDEX) rows that are named by index, four at a time: a box cannot; one thread each
 //
 // An expert's last, cut rows where they are the K dimension are loaded by warps 0 and 2 by index too, rows behind the last as zeros.
-// TMA wants rows that begin on 16 bytes; operands whose rows do not are copied first, into scratch (k_copy_rows).
+// TMA wants rows that begin on 16 bytes; operands whose rows do not are copied first, into scratch (k_copy_rows), as FP32 ones are
+// split (k_split_rows).
 // Every wait is bounded; after one that runs out the block issues nothing more and its remaining tiles are NaN.
 #include <cuda.h>
 #include <cudaTypedefs.h>
@@ -51,7 +54,7 @@ template <int BN, int SMS> struct Shape {
 struct Operand {
     const uint16_t* p;
     int64_t ld, stride;       // elements from one row to the next, from one expert to the next (0: not the experts')
-    int64_t rows;             // rows there are, of one expert where there are experts
+    int64_t rows;             // rows there are, of one expert where there are experts; images (FP32) lie behind one another
     int columns;
     int gather;               // rows are named by row[]
 };
@@ -64,12 +67,17 @@ struct Product {
     const int32_t* row;
     int64_t places;
     int experts, m, n, k;     // m: of C_e (weights); k: of the rows' products
-    uint16_t* c;
+    int terms;                // products of images: 1, or 6 of FP32's
+    void* c;
     int64_t ldc, stride_c;
     int c_wide;
     uint32_t idesc;
-    int bf16;
+    int bf16, f32;            // operands; C
 };
+
+// The images of the i-th of six products, smallest first: x2 w0, x0 w2, x1 w1, x1 w0, x0 w1, x0 w0.
+__device__ __forceinline__ int a_image(const Product& q, int i) { return q.terms == 1 ? 0 : 0x001102 >> (4 * i) & 3; }
+__device__ __forceinline__ int b_image(const Product& q, int i) { return q.terms == 1 ? 0 : 0x010120 >> (4 * i) & 3; }
 
 // (C is in memory, and a tile has at least 32 of its elements: tiles are counted in 32 bits.)
 struct Tile {
@@ -250,13 +258,16 @@ __device__ __forceinline__ Tile tile_at(const Product& q, const int32_t* first, 
 }
 
 // The rows of places p to p + 3 of an operand, in the form that a load of rows takes: for none, the one behind the last.
-__device__ __forceinline__ int4 rows_at(const Operand& o, const int32_t* row, int p, int stop)
+__device__ __forceinline__ int4 rows_at(const Product& q, const Operand& o, int image, int p, int stop)
 {
-    const uint32_t none = (uint32_t)o.rows;
+    const int32_t* row = q.row;
+    const uint32_t rows = (uint32_t)o.rows, none = q.terms == 1 ? rows : 3 * rows, base = rows * (uint32_t)image;
     uint32_t r[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) r[i] = p + i < stop ? o.gather ? (uint32_t)__ldg(row + p + i) : (uint32_t)(p + i) : none;
-    return make_int4((int)min(r[0], none), (int)min(r[1], none), (int)min(r[2], none), (int)min(r[3], none));
+#pragma unroll
+    for (int i = 0; i < 4; ++i) r[i] = r[i] < rows ? r[i] + base : none;
+    return make_int4((int)r[0], (int)r[1], (int)r[2], (int)r[3]);
 }
 
 // A warp's 32 rows of `steps` times 32 columns of a tile, from accumulator column `acc` (the warp's lanes) into C from (row0, col0) on;
@@ -265,7 +276,7 @@ __device__ __forceinline__ int4 rows_at(const Operand& o, const int32_t* row, in
 template <int MODE>
 __device__ __forceinline__ void store_tile(const Product& q, const Tile& w, int row0, int col0, int steps, uint32_t acc, uint32_t mine, int lane, bool on)
 {
-    uint16_t* c = q.c + (MODE == kWeights ? w.expert * q.stride_c : 0) + row0 * q.ldc;
+    uint16_t* c = (uint16_t*)q.c + (MODE == kWeights ? w.expert * q.stride_c : 0) + row0 * q.ldc;
     const int rows = min(32, w.stop - row0);
     const uint32_t to_stage = mine + (uint32_t)(lane * 64), phase = (uint32_t)(lane >> 1) & 3u;
     const uint32_t from_stage = mine + (uint32_t)((lane >> 2) * 64 + (((lane & 3) ^ ((lane >> 3) & 3)) << 4));
@@ -311,6 +322,48 @@ __device__ __forceinline__ void store_tile(const Product& q, const Tile& w, int 
                 uint16_t h;
                 asm volatile("ld.shared.u16 %0, [%1];" : "=h"(h) : "r"(mine + (uint32_t)(r * 64 + (((lane >> 3) ^ ((r >> 1) & 3)) << 4) + (lane & 7) * 2)));
                 if (in) *to = h;
+            }
+        }
+        __syncwarp();
+    }
+}
+
+// The same for FP32 results, 16 columns at a time.
+template <int MODE>
+__device__ __forceinline__ void store_tile_32(const Product& q, const Tile& w, int row0, int col0, int steps, uint32_t acc, uint32_t mine, int lane, bool on)
+{
+    float* c = (float*)q.c + (MODE == kWeights ? w.expert * q.stride_c : 0) + row0 * q.ldc;
+    const int rows = min(32, w.stop - row0);
+    const uint32_t to_stage = mine + (uint32_t)(lane * 64), phase = (uint32_t)(lane >> 1) & 3u;
+    const uint32_t from_stage = mine + (uint32_t)((lane >> 2) * 64 + (((lane & 3) ^ ((lane >> 3) & 3)) << 4));
+#pragma unroll 1
+    for (int g = 0; g < 2 * steps && col0 < q.n; ++g, col0 += 16) {
+        float v[16];
+        if (w.k && on) {
+            tmem_ld16(acc + (uint32_t)(g * 16), v);
+        } else {
+            const float fill = on ? 0.0f : __uint_as_float(0x7fc00000u);
+#pragma unroll
+            for (int x = 0; x < 16; ++x) v[x] = fill;
+        }
+#pragma unroll
+        for (int x = 0; x < 4; ++x) sts128(to_stage + (((uint32_t)x ^ phase) << 4), make_float4(v[4 * x], v[4 * x + 1], v[4 * x + 2], v[4 * x + 3]));
+        __syncwarp();
+        float* to = c + (int64_t)(lane >> 2) * q.ldc + col0 + (lane & 3) * 4;
+#pragma unroll
+        for (int x = 0; x < 4; ++x) {
+            const float4 f = lds128(from_stage + (uint32_t)(x * 512));
+            if (8 * x + (lane >> 2) < rows) {
+                float* at = to + (int64_t)(8 * x) * q.ldc;
+                const int left = q.n - col0 - (lane & 3) * 4;
+                if (q.c_wide && left >= 4) {
+                    *reinterpret_cast<float4*>(at) = f;
+                } else {
+                    if (left > 0) at[0] = f.x;
+                    if (left > 1) at[1] = f.y;
+                    if (left > 2) at[2] = f.z;
+                    if (left > 3) at[3] = f.w;
+                }
             }
         }
         __syncwarp();
@@ -392,38 +445,41 @@ __device__ __forceinline__ void products(const Product& q)
                     a_bytes = 0;
                     for (int i = 0; i < SMS; ++i) a_bytes += 16 * kRow * loads_of(w.stop - w.c_row - i * kTileM);
                 }
-                int p0 = w.k_first;                         // weights: the chunk's first place
-                for (int k = 0; k < w.k; k += kChunk, p0 += kChunk) {
-                    on = wait_for(free_(s), parity, dead);
-                    if (!on) break;
-                    const uint32_t to = stages + (uint32_t)s * S::STAGE + (is_a ? 0 : S::A), bar = of_first<SMS>(full(s));
-                    if (MODE == kWeights && w.k - k < kChunk) {
-                        const int quads = (w.k - k + 15) / 16 * 4, end = w.k_first + w.k;
-                        const int a_quads = BY_INDEX && q.a.gather ? 16 : quads, b_quads = BY_INDEX && q.b.gather ? 16 : quads;
-                        if (counts) mbar_expect_tx(full(s), SMS * 4 * kRow * (A_BOXES * a_quads + B_BOXES * b_quads));
-                        if (!others)
+                for (int term = 0; term < q.terms && on; ++term) {
+                    const int image = is_a ? a_image(q, term) : b_image(q, term), image_row = image * (int)o.rows;
+                    int p0 = w.k_first;                         // weights: the chunk's first place
+                    for (int k = 0; k < w.k; k += kChunk, p0 += kChunk) {
+                        on = wait_for(free_(s), parity, dead);
+                        if (!on) break;
+                        const uint32_t to = stages + (uint32_t)s * S::STAGE + (is_a ? 0 : S::A), bar = of_first<SMS>(full(s));
+                        if (MODE == kWeights && w.k - k < kChunk) {
+                            const int quads = (w.k - k + 15) / 16 * 4, end = w.k_first + w.k;
+                            const int a_quads = BY_INDEX && q.a.gather ? 16 : quads, b_quads = BY_INDEX && q.b.gather ? 16 : quads;
+                            if (counts) mbar_expect_tx(full(s), SMS * 4 * kRow * (A_BOXES * a_quads + B_BOXES * b_quads));
+                            if (!others)
 #pragma unroll 2
-                            for (int i = 0; i < quads; ++i) {
-                                const int4 named = rows_at(o, q.row, p0 + 4 * i, end);
-                                for (int b = 0; b < boxes; ++b) load_rows<SMS>(to + b * kBox + i * 4 * kRow, by_index, x + 64 * b, named, bar);
-                            }
-                    } else {
-                        if (counts) mbar_expect_tx(full(s), a_bytes + SMS * S::B);
-                        if (!others) {
-                            if (MODE == kWeights) {
-                                for (int b = 0; b < boxes; ++b) load_2d<SMS>(to + b * kBox, by_box, x + 64 * b, p0, bar);
-                            } else if (is_a) {
-                                load_2d<SMS>(to, by_box, k, a_row, bar);
-                            } else if (MODE == kRowsTimesTurned) {
-                                load_3d<SMS>(to, by_box, k, b_col, w.expert, bar);
-                            } else {
+                                for (int i = 0; i < quads; ++i) {
+                                    const int4 named = rows_at(q, o, image, p0 + 4 * i, end);
+                                    for (int b = 0; b < boxes; ++b) load_rows<SMS>(to + b * kBox + i * 4 * kRow, by_index, x + 64 * b, named, bar);
+                                }
+                        } else {
+                            if (counts) mbar_expect_tx(full(s), a_bytes + SMS * S::B);
+                            if (!others) {
+                                if (MODE == kWeights) {
+                                    for (int b = 0; b < boxes; ++b) load_2d<SMS>(to + b * kBox, by_box, x + 64 * b, image_row + p0, bar);
+                                } else if (is_a) {
+                                    load_2d<SMS>(to, by_box, k, image_row + a_row, bar);
+                                } else if (MODE == kRowsTimesTurned) {
+                                    load_3d<SMS>(to, by_box, k, b_col, image * q.experts + w.expert, bar);
+                                } else {
 #pragma unroll
-                                for (int b = 0; b < B_BOXES; ++b) load_3d<SMS>(to + b * kBox, by_box, b_col + 64 * b, k, w.expert, bar);
+                                    for (int b = 0; b < B_BOXES; ++b) load_3d<SMS>(to + b * kBox, by_box, b_col + 64 * b, k, image * q.experts + w.expert, bar);
+                                }
                             }
                         }
+                        ++g;
+                        if (++s == S::STAGES) { s = 0; parity ^= 1u; }
                     }
-                    ++g;
-                    if (++s == S::STAGES) { s = 0; parity ^= 1u; }
                 }
             }
             if (!on && counts) {
@@ -444,7 +500,9 @@ __device__ __forceinline__ void products(const Product& q)
                 if (k == 0) continue;
                 const uint32_t acc = tmem + (i & 1u) * BN;
                 on = wait_for(acc_free(i & 1), ((i >> 1) + 1) & 1, dead);
-                for (int left = k; left > 0 && on; left -= kChunk) {
+                bool begun = false;
+                int left = k;
+                for (int term = 0; term < q.terms;) {
                     on = wait_for(full(s), parity, dead);
                     if (!on) break;
                     tc_fence_after();
@@ -452,9 +510,12 @@ __device__ __forceinline__ void products(const Product& q)
 #pragma unroll
                     for (int x = 0; x < 4; ++x)
                         if (x == 0 || x * 16 < left)
-                            mma<SMS>(acc, da + (uint64_t)(x * (A_K ? 2 : 128)), db + (uint64_t)(x * (B_K ? 2 : 128)), q.idesc, x || left < k);
+                            mma<SMS>(acc, da + (uint64_t)(x * (A_K ? 2 : 128)), db + (uint64_t)(x * (B_K ? 2 : 128)), q.idesc, x || begun);
+                    begun = true;
                     commit<SMS>(free_(s));
                     if (++s == S::STAGES) { s = 0; parity ^= 1u; }
+                    left -= kChunk;
+                    if (left <= 0) { left = k; ++term; }
                 }
                 if (on) commit<SMS>(acc_full(i & 1));
                 ++i;
@@ -477,8 +538,10 @@ __device__ __forceinline__ void products(const Product& q)
                 on = __all_sync(0xffffffffu, on);
                 tc_fence_after();
             }
-            store_tile<MODE>(q, w, w.c_row + rank * kTileM + quarter * 32, w.n0 + half * (BN / 2), BN / 64,
-                             tmem + ((uint32_t)(quarter * 32) << 16) + (i & 1u) * BN + (uint32_t)(half * (BN / 2)), mine, lane, on);
+            const int row0 = w.c_row + rank * kTileM + quarter * 32, col0 = w.n0 + half * (BN / 2);
+            const uint32_t acc = tmem + ((uint32_t)(quarter * 32) << 16) + (i & 1u) * BN + (uint32_t)(half * (BN / 2));
+            if (q.f32) store_tile_32<MODE>(q, w, row0, col0, BN / 64, acc, mine, lane, on);
+            else store_tile<MODE>(q, w, row0, col0, BN / 64, acc, mine, lane, on);
             if (w.k) {
                 tc_fence_before();
                 __syncwarp();
@@ -497,28 +560,29 @@ __device__ __forceinline__ void products(const Product& q)
                 if (one_thread()) {
                     int4 named[8];                          // every fourth four of A's rows
                     const int loads = loads_of(w.stop - a_row);
-                    if (w.k)
-#pragma unroll
-                        for (int i = 0; i < 8; ++i) named[i] = rows_at(q.a, q.row, a_row + 4 * (4 * i + part), w.stop);
                     int s = (int)(g % S::STAGES);
                     uint32_t parity = (g / S::STAGES & 1u) ^ 1u;
-                    for (int k = 0; k < w.k; k += kChunk) {
-                        on = wait_for(free_(s), parity, dead);
-                        if (!on) break;
-                        const uint32_t to = stages + (uint32_t)s * S::STAGE + (uint32_t)(4 * part * kRow), bar = of_first<SMS>(full(s));
-                        if (loads == 8) {
+                    for (int term = 0; term < q.terms && on && w.k; ++term) {
 #pragma unroll
-                            for (int i = 0; i < 8; ++i) load_rows<SMS>(to + (uint32_t)(16 * i * kRow), &q.ra, k, named[i], bar);
-                        } else {
+                        for (int i = 0; i < 8; ++i) named[i] = rows_at(q, q.a, a_image(q, term), a_row + 4 * (4 * i + part), w.stop);
+                        for (int k = 0; k < w.k; k += kChunk) {
+                            on = wait_for(free_(s), parity, dead);
+                            if (!on) break;
+                            const uint32_t to = stages + (uint32_t)s * S::STAGE + (uint32_t)(4 * part * kRow), bar = of_first<SMS>(full(s));
+                            if (loads == 8) {
 #pragma unroll
-                            for (int i = 0; i < 7; ++i)
-                                if (i < loads) load_rows<SMS>(to + (uint32_t)(16 * i * kRow), &q.ra, k, named[i], bar);
+                                for (int i = 0; i < 8; ++i) load_rows<SMS>(to + (uint32_t)(16 * i * kRow), &q.ra, k, named[i], bar);
+                            } else {
+#pragma unroll
+                                for (int i = 0; i < 7; ++i)
+                                    if (i < loads) load_rows<SMS>(to + (uint32_t)(16 * i * kRow), &q.ra, k, named[i], bar);
+                            }
+                            if (++s == S::STAGES) { s = 0; parity ^= 1u; }
                         }
-                        if (++s == S::STAGES) { s = 0; parity ^= 1u; }
                     }
                 }
                 on = __all_sync(0xffffffffu, on);
-                g += (uint32_t)(w.k + kChunk - 1) / kChunk;
+                g += (uint32_t)(w.k + kChunk - 1) / kChunk * (uint32_t)q.terms;
             } else {
                 // A quarter of a chunk's places: lane i has the i-th's row, read four chunks ahead.
                 constexpr int AHEAD = 4;
@@ -526,34 +590,37 @@ __device__ __forceinline__ void products(const Product& q)
                 const CUtensorMap* map = q.a.gather ? &q.ra : &q.rb;
                 const int x = q.a.gather ? a_row : b_col, boxes = q.a.gather ? A_BOXES : B_BOXES;
                 const int end = w.k_first + w.k, mine = w.k_first + 16 * part + (lane & 15);
-                int ahead[AHEAD];
+                for (int term = 0; term < q.terms && on; ++term) {
+                    const uint32_t rows = (uint32_t)o.rows, none = q.terms == 1 ? rows : 3 * rows, base = rows * (uint32_t)(q.a.gather ? a_image(q, term) : b_image(q, term));
+                    int ahead[AHEAD];
 #pragma unroll
-                for (int u = 0; u < AHEAD; ++u) ahead[u] = mine + u * kChunk < end ? __ldg(q.row + mine + u * kChunk) : -1;
-                for (int k0 = 0; k0 < w.k && on; k0 += AHEAD * kChunk) {
+                    for (int u = 0; u < AHEAD; ++u) ahead[u] = mine + u * kChunk < end ? __ldg(q.row + mine + u * kChunk) : -1;
+                    for (int k0 = 0; k0 < w.k && on; k0 += AHEAD * kChunk) {
 #pragma unroll
-                    for (int u = 0; u < AHEAD; ++u) {
-                        const int k = k0 + u * kChunk;
-                        if (k >= w.k || !on) break;
-                        const int s = (int)(g % S::STAGES);
-                        on = wait_for(free_(s), (g / S::STAGES & 1u) ^ 1u, dead);
-                        on = __all_sync(0xffffffffu, on);
-                        if (!on) break;
-                        const int r = (int)min((uint32_t)ahead[u], (uint32_t)o.rows);
-                        const int next = mine + k + AHEAD * kChunk;
-                        ahead[u] = next < end ? __ldg(q.row + next) : -1;
-                        int4 named[4];
-#pragma unroll
-                        for (int i = 0; i < 4; ++i)
-                            named[i] = make_int4(__shfl_sync(0xffffffffu, r, 4 * i), __shfl_sync(0xffffffffu, r, 4 * i + 1), __shfl_sync(0xffffffffu, r, 4 * i + 2),
-                                                 __shfl_sync(0xffffffffu, r, 4 * i + 3));
-                        if (one_thread()) {
-                            const uint32_t to = stages + (uint32_t)s * S::STAGE + (q.a.gather ? 0 : S::A) + (uint32_t)(16 * part * kRow), bar = of_first<SMS>(full(s));
+                        for (int u = 0; u < AHEAD; ++u) {
+                            const int k = k0 + u * kChunk;
+                            if (k >= w.k || !on) break;
+                            const int s = (int)(g % S::STAGES);
+                            on = wait_for(free_(s), (g / S::STAGES & 1u) ^ 1u, dead);
+                            on = __all_sync(0xffffffffu, on);
+                            if (!on) break;
+                            const int r = (int)((uint32_t)ahead[u] < rows ? (uint32_t)ahead[u] + base : none);
+                            const int next = mine + k + AHEAD * kChunk;
+                            ahead[u] = next < end ? __ldg(q.row + next) : -1;
+                            int4 named[4];
 #pragma unroll
                             for (int i = 0; i < 4; ++i)
-                                for (int b = 0; b < boxes; ++b) load_rows<SMS>(to + (uint32_t)(b * kBox + i * 4 * kRow), map, x + 64 * b, named[i], bar);
+                                named[i] = make_int4(__shfl_sync(0xffffffffu, r, 4 * i), __shfl_sync(0xffffffffu, r, 4 * i + 1), __shfl_sync(0xffffffffu, r, 4 * i + 2),
+                                                     __shfl_sync(0xffffffffu, r, 4 * i + 3));
+                            if (one_thread()) {
+                                const uint32_t to = stages + (uint32_t)s * S::STAGE + (q.a.gather ? 0 : S::A) + (uint32_t)(16 * part * kRow), bar = of_first<SMS>(full(s));
+#pragma unroll
+                                for (int i = 0; i < 4; ++i)
+                                    for (int b = 0; b < boxes; ++b) load_rows<SMS>(to + (uint32_t)(b * kBox + i * 4 * kRow), map, x + 64 * b, named[i], bar);
+                            }
+                            __syncwarp();
+                            ++g;
                         }
-                        __syncwarp();
-                        ++g;
                     }
                 }
             }
@@ -607,6 +674,40 @@ k_copy_rows(const uint16_t* __restrict__ from, int64_t ld, int64_t stride, int64
     }
 }
 
+// FP32 rows to three images of BF16 rows that begin on 16 bytes, `image` elements from one to the next: the nearest, the nearest of what
+// is left, and the rest, which is exact.  (What rounds beyond BF16's range is cut instead; infinities and NaN have no rest.)
+__global__ void __launch_bounds__(256)
+k_split_rows(const float* __restrict__ from, int64_t ld, int64_t stride, int64_t rows, int64_t all_rows, int columns, uint16_t* __restrict__ to, int64_t to_ld, int64_t image)
+{
+    const int vecs = (columns + 7) / 8;
+    const int64_t steps = (all_rows + blockDim.y - 1) / blockDim.y;
+    for (int64_t s = blockIdx.x; s < steps; s += gridDim.x) {
+        const int64_t i = s * blockDim.y + threadIdx.y;
+        if (i >= all_rows) continue;
+        const int64_t e = rows == all_rows ? 0 : i / rows;
+        const float* row = from + e * stride + (i - e * rows) * ld;
+        for (int c = threadIdx.x; c < vecs; c += blockDim.x) {
+            const float* p = row + c * 8;
+            float v[8];
+            if (((uintptr_t)p & 15) == 0 && c * 8 + 8 <= columns) load8<true>(p, 8, v);
+            else load8<false>(p, columns - c * 8, v);
+#pragma unroll
+            for (int part = 0; part < 3; ++part) {
+                uint32_t h[4] = {0, 0, 0, 0};
+#pragma unroll
+                for (int x = 0; x < 8; ++x) {
+                    const uint32_t bits = __float_as_uint(v[x]), magnitude = bits & 0x7fffffffu;
+                    uint32_t near = (bits + 0x7fffu + (bits >> 16 & 1u)) >> 16;
+                    if (magnitude >= 0x7f7f8000u) near = magnitude > 0x7f800000u ? 0x7fffu : bits >> 16;
+                    h[x >> 1] |= near << (16 * (x & 1));
+                    v[x] = magnitude >= 0x7f800000u ? 0.0f : v[x] - __uint_as_float(near << 16);
+                }
+                *reinterpret_cast<uint4*>(to + part * image + i * to_ld + c * 8) = make_uint4(h[0], h[1], h[2], h[3]);
+            }
+        }
+    }
+}
+
 // ---- host ---------------------------------------------------------------------------------------------------------------------------
 
 PFN_cuTensorMapEncodeTiled_v12000 encoder()
@@ -622,11 +723,11 @@ PFN_cuTensorMapEncodeTiled_v12000 encoder()
 }
 
 // Boxes of box_rows rows of 128 bytes, 128-byte swizzle, zeros outside.  (experts 0: the operand is not the experts'.)
-bool encode(CUtensorMap* map, const Operand& o, int experts, int box_rows, bool bf16)
+bool encode(CUtensorMap* map, const Operand& o, int experts, int images, int box_rows, bool bf16)
 {
     const auto fn = encoder();
     if (!fn) return false;
-    const cuuint64_t dims[3] = {(cuuint64_t)o.columns, (cuuint64_t)o.rows, (cuuint64_t)(experts ? experts : 1)};
+    const cuuint64_t dims[3] = {(cuuint64_t)o.columns, (cuuint64_t)(o.rows * (experts ? 1 : images)), (cuuint64_t)((experts ? experts : 1) * images)};
     const cuuint64_t strides[2] = {(cuuint64_t)(o.ld * 2), (cuuint64_t)(o.stride * 2)};
     const cuuint32_t box[3] = {kChunk, (cuuint32_t)box_rows, 1}, unit[3] = {1, 1, 1};
     return fn(map, bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, experts ? 3 : 2, const_cast<uint16_t*>(o.p), dims, strides, box, unit,
@@ -651,8 +752,10 @@ int run_tiles(Product& q, int64_t tiles, bool by_index, cudaStream_t st)
     constexpr bool A_K = MODE != kWeights, B_K = MODE == kRowsTimesTurned;
     // boxes where an operand is read by boxes, rows where it is read by index (weights: an expert's last rows)
     const bool boxes_a = A_K ? !by_index : !q.a.gather, boxes_b = A_K || !q.b.gather;
-    if ((boxes_a && !encode(&q.ta, q.a, 0, A_K ? kTileM : kChunk, q.bf16)) || (boxes_b && !encode(&q.tb, q.b, A_K ? q.experts : 0, B_K ? BN / SMS : kChunk, q.bf16)) ||
-        (!(A_K && !by_index) && !encode(&q.ra, q.a, 0, 1, q.bf16)) || (!A_K && !encode(&q.rb, q.b, 0, 1, q.bf16)))
+    const int images = q.f32 ? 3 : 1;
+    if ((boxes_a && !encode(&q.ta, q.a, 0, images, A_K ? kTileM : kChunk, q.bf16)) ||
+        (boxes_b && !encode(&q.tb, q.b, A_K ? q.experts : 0, images, B_K ? BN / SMS : kChunk, q.bf16)) ||
+        (!(A_K && !by_index) && !encode(&q.ra, q.a, 0, images, 1, q.bf16)) || (!A_K && !encode(&q.rb, q.b, 0, images, 1, q.bf16)))
         return GEM_NLR_E_CUDA;
     q.idesc = umma_idesc_f16(SMS * kTileM, BN, !A_K, !B_K) | (q.bf16 ? 1u << 7 | 1u << 10 : 0u);
     constexpr int SHARED = Shape<BN, SMS>::SHARED;
@@ -682,34 +785,37 @@ int run(Product& q, cudaStream_t st)
     return run_tiles<MODE, 64, 1>(q, tiles(kTileM, 64), by_index, st);
 }
 
-bool on_16(const void* p, int64_t ld) { return aligned_to(p, 16) && ld % 8 == 0; }
+// Rows of C on 16 bytes.
+bool on_16(const void* p, int64_t ld, int64_t stride, int bytes) { return aligned_to(p, 16) && ld * bytes % 16 == 0 && stride * bytes % 16 == 0; }
 int64_t pitch_of(int columns) { return ((int64_t)columns + 7) / 8 * 8; }
 
-// Whether an operand's rows can be read where they are: on 16 bytes, and each with memory of its own.
-bool in_place(const Operand& o, int experts)
+// Whether an operand's rows can be read where they are: 16-bit ones on 16 bytes, and each with memory of its own.
+bool in_place(const Operand& o, int experts, int type)
 {
-    return o.rows == 0 || (on_16(o.p, o.ld) && o.ld >= o.columns && (experts < 2 || (o.stride % 8 == 0 && o.stride >= o.rows * o.ld)));
+    return o.rows == 0 || (type != GEM_NLR_F32 && on_16(o.p, o.ld, experts < 2 ? 0 : o.stride, 2) && o.ld >= o.columns && (experts < 2 || o.stride >= o.rows * o.ld));
 }
 
-size_t copy_bytes(const Operand& o, int experts)
+size_t copy_bytes(const Operand& o, int experts, int type)
 {
-    return in_place(o, experts) ? 0 : ((size_t)o.rows * experts * pitch_of(o.columns) * 2 + 255) / 256 * 256;
+    return in_place(o, experts, type) ? 0 : ((size_t)o.rows * experts * pitch_of(o.columns) * (type == GEM_NLR_F32 ? 6 : 2) + 255) / 256 * 256;
 }
 
-// The operand, copied to `scratch` where it has to be.
-bool bring(Operand& o, int experts, char*& scratch, cudaStream_t st)
+// The operand, copied or split into `scratch` where it has to be.
+bool bring(Operand& o, int experts, int type, char*& scratch, cudaStream_t st)
 {
     if (experts < 2) o.stride = o.rows * o.ld;
-    if (in_place(o, experts)) return true;
+    if (in_place(o, experts, type)) return true;
     const int64_t all = o.rows * experts, pitch = pitch_of(o.columns);
-    int x = 1;
-    while (x < pitch / 8 && x < 256) x *= 2;
-    const int64_t steps = (all + 256 / x - 1) / (256 / x), most = (int64_t)kTrainSMs * 64;
-    k_copy_rows<<<(unsigned)(steps < most ? steps : most), dim3(x, 256 / x), 0, st>>>(o.p, o.ld, o.stride, o.rows, all, o.columns, (uint16_t*)scratch, pitch);
-    o.p = (const uint16_t*)scratch;
+    const RowBlocks sh = row_blocks(all, (int)(pitch / 8));
+    char* here = scratch;
+    scratch += copy_bytes(o, experts, type);
+    if (type == GEM_NLR_F32)
+        k_split_rows<<<sh.grid, sh.block, 0, st>>>((const float*)o.p, o.ld, o.stride, o.rows, all, o.columns, (uint16_t*)here, pitch, all * pitch);
+    else
+        k_copy_rows<<<sh.grid, sh.block, 0, st>>>(o.p, o.ld, o.stride, o.rows, all, o.columns, (uint16_t*)here, pitch);
+    o.p = (const uint16_t*)here;
     o.ld = pitch;
     o.stride = o.rows * pitch;
-    scratch += ((size_t)all * pitch * 2 + 255) / 256 * 256;
     return launched() == GEM_NLR_OK;
 }
 
@@ -720,18 +826,19 @@ Operand weights_of(const void* p, int64_t ld, int64_t stride, int32_t turned, in
 }
 
 constexpr int64_t kMaxPlaces = INT32_MAX - (1 << 16);            // int arithmetic on places, tiles included, stays far from its end
-bool half_type(int32_t type) { return type == GEM_NLR_F16 || type == GEM_NLR_BF16; }
-bool halves(const void* p) { return p && aligned_to(p, 2); }
-bool sizes_fine(int64_t x_rows, int64_t places, int32_t experts, int32_t d_in, int32_t d_out, int32_t turned, bool rows_named)
+bool elements(const void* p, int type) { return p && aligned_to(p, type_bytes(type)); }
+bool sizes_fine(int type, int64_t x_rows, int64_t places, int32_t experts, int32_t d_in, int32_t d_out, int32_t turned, bool rows_named)
 {
-    return x_rows >= 0 && x_rows <= INT32_MAX && places >= 0 && places <= kMaxPlaces && experts >= 1 && experts <= GEM_NLR_MAX_EXPERTS && d_in >= 1 &&
-           d_in <= kMaxColumns && d_out >= 1 && d_out <= kMaxColumns && (turned == 0 || turned == 1) && (rows_named || x_rows >= places);
+    const int64_t images = type == GEM_NLR_F32 ? 3 : 1;
+    return type_bytes(type) && x_rows >= 0 && x_rows <= INT32_MAX / images && places >= 0 && places <= kMaxPlaces / images && experts >= 1 && experts <= GEM_NLR_MAX_EXPERTS &&
+           d_in >= 1 && d_in <= kMaxColumns && d_out >= 1 && d_out <= kMaxColumns && (turned == 0 || turned == 1) && (rows_named || x_rows >= places);
 }
+
 // `count` matrices of zeros.
-int clear(void* to, int64_t ld, int64_t stride, int64_t rows, int64_t columns, int count, cudaStream_t st)
+int clear(void* to, int bytes, int64_t ld, int64_t stride, int64_t rows, int64_t columns, int count, cudaStream_t st)
 {
     for (int i = 0; i < count; ++i)
-        if (cudaMemset2DAsync((uint16_t*)to + i * stride, (size_t)ld * 2, 0, (size_t)columns * 2, rows, st) != cudaSuccess) {
+        if (cudaMemset2DAsync((char*)to + i * stride * bytes, (size_t)ld * bytes, 0, (size_t)columns * bytes, rows, st) != cudaSuccess) {
             cudaGetLastError();
             return GEM_NLR_E_CUDA;
         }
@@ -744,50 +851,52 @@ bool scratch_fine(const void* p, size_t have, size_t need) { return need == 0 ||
 
 using namespace gemnlr;
 
-extern "C" size_t gem_nlr_expert_product_scratch_bytes(const void* x_dev, int64_t ld_x, int64_t x_rows, const void* w_dev, int64_t ld_w, int64_t stride_w,
+extern "C" size_t gem_nlr_expert_product_scratch_bytes(const void* x_dev, int32_t type, int64_t ld_x, int64_t x_rows, const void* w_dev, int64_t ld_w, int64_t stride_w,
                                                        int32_t w_turned, int32_t experts, int32_t d_in, int32_t d_out)
 {
-    if (!sizes_fine(x_rows, 0, experts, d_in, d_out, w_turned, true) || ld_x < 0 || ld_w < 0 || stride_w < 0) return 0;
-    return copy_bytes(places_of(x_dev, ld_x, x_rows, d_in, false), 1) + copy_bytes(weights_of(w_dev, ld_w, stride_w, w_turned, d_in, d_out), experts);
+    if (!sizes_fine(type, x_rows, 0, experts, d_in, d_out, w_turned, true) || ld_x < 0 || ld_w < 0 || stride_w < 0) return 0;
+    return copy_bytes(places_of(x_dev, ld_x, x_rows, d_in, false), 1, type) + copy_bytes(weights_of(w_dev, ld_w, stride_w, w_turned, d_in, d_out), experts, type);
 }
 
 extern "C" int gem_nlr_expert_product(const void* x_dev, int32_t type, int64_t ld_x, int64_t x_rows, const void* w_dev, int64_t ld_w, int64_t stride_w,
                                       int32_t w_turned, const int32_t* offset_dev, const int32_t* row_dev, int64_t places, int32_t experts, int32_t d_in,
                                       int32_t d_out, void* y_dev, int64_t ld_y, void* scratch_dev, size_t scratch_bytes, void* cuda_stream)
 {
-    if (!half_type(type) || !sizes_fine(x_rows, places, experts, d_in, d_out, w_turned, row_dev != nullptr) || !aligned_to(row_dev, 4) || ld_x < 0 || ld_w < 0 || stride_w < 0)
+    if (!sizes_fine(type, x_rows, places, experts, d_in, d_out, w_turned, row_dev != nullptr) || !aligned_to(row_dev, 4) || ld_x < 0 || ld_w < 0 || stride_w < 0)
         return GEM_NLR_E_INVALID;
     if (places == 0) return GEM_NLR_OK;
-    if ((x_rows > 0 && !halves(x_dev)) || !halves(w_dev) || !offset_dev || !aligned_to(offset_dev, 4) || !halves(y_dev) || ld_y < d_out || y_dev == x_dev || y_dev == w_dev)
+    if ((x_rows > 0 && !elements(x_dev, type)) || !elements(w_dev, type) || !offset_dev || !aligned_to(offset_dev, 4) || !elements(y_dev, type) || ld_y < d_out || y_dev == x_dev || y_dev == w_dev)
         return GEM_NLR_E_INVALID;
     cudaStream_t st = (cudaStream_t)cuda_stream;
     Product q = {};
     q.a = places_of(x_dev, ld_x, x_rows, d_in, row_dev != nullptr);
     q.b = weights_of(w_dev, ld_w, stride_w, w_turned, d_in, d_out);
-    if (!scratch_fine(scratch_dev, scratch_bytes, copy_bytes(q.a, 1) + copy_bytes(q.b, experts))) return GEM_NLR_E_WORKSPACE;
-    if (x_rows == 0) return clear(y_dev, ld_y, 0, places, d_out, 1, st);
+    if (!scratch_fine(scratch_dev, scratch_bytes, copy_bytes(q.a, 1, type) + copy_bytes(q.b, experts, type))) return GEM_NLR_E_WORKSPACE;
+    if (x_rows == 0) return clear(y_dev, type_bytes(type), ld_y, 0, places, d_out, 1, st);
     char* scratch = (char*)scratch_dev;
-    if (!bring(q.a, 1, scratch, st) || !bring(q.b, experts, scratch, st)) return GEM_NLR_E_CUDA;
+    if (!bring(q.a, 1, type, scratch, st) || !bring(q.b, experts, type, scratch, st)) return GEM_NLR_E_CUDA;
     q.offset = offset_dev;
     q.row = row_dev;
     q.places = places;
     q.experts = experts;
     q.n = d_out;
     q.k = d_in;
-    q.c = (uint16_t*)y_dev;
+    q.c = y_dev;
     q.ldc = ld_y;
-    q.c_wide = on_16(y_dev, ld_y);
-    q.bf16 = type == GEM_NLR_BF16;
+    q.c_wide = on_16(y_dev, ld_y, 0, type_bytes(type));
+    q.bf16 = type != GEM_NLR_F16;
+    q.f32 = type == GEM_NLR_F32;
+    q.terms = q.f32 ? 6 : 1;
     return w_turned ? run<kRowsTimesTurned>(q, st) : run<kRowsTimesPlain>(q, st);
 }
 
-extern "C" size_t gem_nlr_expert_product_backward_scratch_bytes(const void* dy_dev, int64_t ld_dy, int64_t places, const void* x_dev, int64_t ld_x, int64_t x_rows,
+extern "C" size_t gem_nlr_expert_product_backward_scratch_bytes(const void* dy_dev, int64_t ld_dy, int64_t places, const void* x_dev, int32_t type, int64_t ld_x, int64_t x_rows,
                                                                 const void* w_dev, int64_t ld_w, int64_t stride_w, int32_t w_turned, int32_t experts,
                                                                 int32_t d_in, int32_t d_out)
 {
-    if (!sizes_fine(x_rows, places, experts, d_in, d_out, w_turned, true) || ld_dy < 0 || ld_x < 0 || ld_w < 0 || stride_w < 0) return 0;
-    return copy_bytes(places_of(dy_dev, ld_dy, places, d_out, false), 1) + copy_bytes(places_of(x_dev, ld_x, x_rows, d_in, false), 1) +
-           copy_bytes(weights_of(w_dev, ld_w, stride_w, w_turned, d_in, d_out), experts);
+    if (!sizes_fine(type, x_rows, places, experts, d_in, d_out, w_turned, true) || ld_dy < 0 || ld_x < 0 || ld_w < 0 || stride_w < 0) return 0;
+    return copy_bytes(places_of(dy_dev, ld_dy, places, d_out, false), 1, type) + copy_bytes(places_of(x_dev, ld_x, x_rows, d_in, false), 1, type) +
+           copy_bytes(weights_of(w_dev, ld_w, stride_w, w_turned, d_in, d_out), experts, type);
 }
 
 extern "C" int gem_nlr_expert_product_backward(const void* dy_dev, int64_t ld_dy, const void* x_dev, int32_t type, int64_t ld_x, int64_t x_rows, const void* w_dev,
@@ -796,50 +905,52 @@ extern "C" int gem_nlr_expert_product_backward(const void* dy_dev, int64_t ld_dy
                                                int64_t ld_dw, int64_t stride_dw, void* scratch_dev, size_t scratch_bytes, void* cuda_stream)
 {
     const int64_t wide = w_turned ? d_in : d_out, tall = w_turned ? d_out : d_in;
-    if (!half_type(type) || !sizes_fine(x_rows, places, experts, d_in, d_out, w_turned, row_dev != nullptr) || !aligned_to(row_dev, 4) || ld_dy < 0 || ld_x < 0 || ld_w < 0 ||
+    if (!sizes_fine(type, x_rows, places, experts, d_in, d_out, w_turned, row_dev != nullptr) || !aligned_to(row_dev, 4) || ld_dy < 0 || ld_x < 0 || ld_w < 0 ||
         stride_w < 0 || (!dx_dev && !dw_dev))
         return GEM_NLR_E_INVALID;
-    if (places > 0 && (!halves(dy_dev) || !offset_dev || !aligned_to(offset_dev, 4))) return GEM_NLR_E_INVALID;
-    if (dx_dev && places > 0 && (!halves(dx_dev) || ld_dx < d_in || !halves(w_dev) || dx_dev == dy_dev || dx_dev == w_dev)) return GEM_NLR_E_INVALID;
-    if (dw_dev && (!halves(dw_dev) || ld_dw < wide || (experts > 1 && stride_dw < tall * ld_dw) || (places > 0 && x_rows > 0 && !halves(x_dev)) ||
+    if (places > 0 && (!elements(dy_dev, type) || !offset_dev || !aligned_to(offset_dev, 4))) return GEM_NLR_E_INVALID;
+    if (dx_dev && places > 0 && (!elements(dx_dev, type) || ld_dx < d_in || !elements(w_dev, type) || dx_dev == dy_dev || dx_dev == w_dev)) return GEM_NLR_E_INVALID;
+    if (dw_dev && (!elements(dw_dev, type) || ld_dw < wide || (experts > 1 && stride_dw < tall * ld_dw) || (places > 0 && x_rows > 0 && !elements(x_dev, type)) ||
                    dw_dev == dy_dev || dw_dev == x_dev || dw_dev == dx_dev))
         return GEM_NLR_E_INVALID;
     cudaStream_t st = (cudaStream_t)cuda_stream;
-    if (places == 0) return dw_dev ? clear(dw_dev, ld_dw, stride_dw, tall, wide, experts, st) : GEM_NLR_OK;
+    if (places == 0) return dw_dev ? clear(dw_dev, type_bytes(type), ld_dw, stride_dw, tall, wide, experts, st) : GEM_NLR_OK;
     Operand dy = places_of(dy_dev, ld_dy, places, d_out, false), x = places_of(x_dev, ld_x, x_rows, d_in, row_dev != nullptr);
     Operand weights = weights_of(w_dev, ld_w, stride_w, w_turned, d_in, d_out);
-    if (!scratch_fine(scratch_dev, scratch_bytes, copy_bytes(dy, 1) + (dw_dev ? copy_bytes(x, 1) : 0) + (dx_dev ? copy_bytes(weights, experts) : 0))) return GEM_NLR_E_WORKSPACE;
+    if (!scratch_fine(scratch_dev, scratch_bytes, copy_bytes(dy, 1, type) + (dw_dev ? copy_bytes(x, 1, type) : 0) + (dx_dev ? copy_bytes(weights, experts, type) : 0))) return GEM_NLR_E_WORKSPACE;
     char* scratch = (char*)scratch_dev;
-    if (!bring(dy, 1, scratch, st)) return GEM_NLR_E_CUDA;
+    if (!bring(dy, 1, type, scratch, st)) return GEM_NLR_E_CUDA;
     Product q = {};
     q.offset = offset_dev;
     q.row = row_dev;
     q.places = places;
     q.experts = experts;
-    q.bf16 = type == GEM_NLR_BF16;
+    q.bf16 = type != GEM_NLR_F16;
+    q.f32 = type == GEM_NLR_F32;
+    q.terms = q.f32 ? 6 : 1;
     if (dx_dev) {
-        if (!bring(weights, experts, scratch, st)) return GEM_NLR_E_CUDA;
+        if (!bring(weights, experts, type, scratch, st)) return GEM_NLR_E_CUDA;
         q.a = dy;
         q.b = weights;
         q.n = d_in;
         q.k = d_out;
-        q.c = (uint16_t*)dx_dev;
+        q.c = dx_dev;
         q.ldc = ld_dx;
-        q.c_wide = on_16(dx_dev, ld_dx);
+        q.c_wide = on_16(dx_dev, ld_dx, 0, type_bytes(type));
         const int rc = w_turned ? run<kRowsTimesPlain>(q, st) : run<kRowsTimesTurned>(q, st);
         if (rc != GEM_NLR_OK) return rc;
     }
     if (!dw_dev) return GEM_NLR_OK;
-    if (x_rows == 0) return clear(dw_dev, ld_dw, stride_dw, tall, wide, experts, st);
-    if (!bring(x, 1, scratch, st)) return GEM_NLR_E_CUDA;
+    if (x_rows == 0) return clear(dw_dev, type_bytes(type), ld_dw, stride_dw, tall, wide, experts, st);
+    if (!bring(x, 1, type, scratch, st)) return GEM_NLR_E_CUDA;
     q.a = w_turned ? dy : x;
     q.b = w_turned ? x : dy;
     q.m = (int)tall;
     q.n = (int)wide;
     q.k = 0;
-    q.c = (uint16_t*)dw_dev;
+    q.c = dw_dev;
     q.ldc = ld_dw;
     q.stride_c = stride_dw;
-    q.c_wide = on_16(dw_dev, ld_dw) && stride_dw % 8 == 0;
+    q.c_wide = on_16(dw_dev, ld_dw, stride_dw, type_bytes(type));
     return run<kWeights>(q, st);
 }

@@ -67,9 +67,9 @@ def _load():
         "route_scratch_bytes": [i64, i32],
         "route_backward": [vp, vp, i32, i64, vp, i64, i32, i32, i32, i32, f32, vp, i64, vp],
         "expert_product": [vp, i32, i64, i64, vp, i64, i64, i32, vp, vp, i64, i32, i32, i32, vp, i64, vp, size, vp],
-        "expert_product_scratch_bytes": [vp, i64, i64, vp, i64, i64, i32, i32, i32, i32],
+        "expert_product_scratch_bytes": [vp, i32, i64, i64, vp, i64, i64, i32, i32, i32, i32],
         "expert_product_backward": [vp, i64, vp, i32, i64, i64, vp, i64, i64, i32, vp, vp, i64, i32, i32, i32, vp, i64, vp, i64, i64, vp, size, vp],
-        "expert_product_backward_scratch_bytes": [vp, i64, i64, vp, i64, i64, vp, i64, i64, i32, i32, i32, i32],
+        "expert_product_backward_scratch_bytes": [vp, i64, i64, vp, i32, i64, i64, vp, i64, i64, i32, i32, i32, i32],
         "combine": [vp, i32, i64, i64, vp, vp, i64, i32, i32, vp, i64, vp],
         "combine_backward": [vp, i64, vp, i32, i64, i64, vp, vp, vp, i32, i64, i32, i32, vp, i64, vp, vp],
         "activation": [vp, i32, i64, i64, i32, i32, i32, vp, i64, vp, vp, vp],
@@ -214,10 +214,7 @@ def _weights(w, at, name="w"):
 
 def _places(x, d_in, offset, experts, row, at):
     """(rows of x, their distance, places, row's address) of a call on x."""
-    torch = _t._torch
     x_rows, d, ld = _matrix(x, "x")
-    if x.dtype not in (torch.float16, torch.bfloat16):
-        raise ValueError(f"x is {x.dtype}: float16 or bfloat16 is needed")
     if d != d_in:
         raise ValueError(f"x has {d} columns, the weights {d_in} rows")
     _ints(offset, (experts + 1,), at, "offset")
@@ -230,8 +227,8 @@ def _places(x, d_in, offset, experts, row, at):
 
 def expert_product(x, w, offset, row=None, out=None, stream=None):
     """gem_nlr_expert_product: y (places, d_out) with y[p] = x[row[p]] @ w[e] for the places p from offset[e] to offset[e + 1], zeros
-    behind the last; without row y[p] = x[p] @ w[e].  x: float16 or bfloat16; w: (experts, d_in, d_out) of its type, either of
-    the last two dimensions contiguous."""
+    behind the last; without row y[p] = x[p] @ w[e].  w: (experts, d_in, d_out) of x's type, either of the last two dimensions
+    contiguous.  float32 costs six times a 16-bit product."""
     fn = _fn or _load()
     if not x.is_cuda:
         raise ValueError("x is not on a GPU")
@@ -250,9 +247,10 @@ def expert_product(x, w, offset, row=None, out=None, stream=None):
             raise ValueError(f"out has to be {(places, d_out)} {x.dtype} on {x.device}")
         ldy = _rows(out, "out")[2]
     xp, wp = x.data_ptr(), w.data_ptr()
-    size = _scratch("expert_product_scratch_bytes", xp & 255, ld, x_rows, wp & 255, ldw, es, turned, experts, d_in, d_out)
+    kind = _type(x, "x")
+    size = _scratch("expert_product_scratch_bytes", xp & 255, kind, ld, x_rows, wp & 255, ldw, es, turned, experts, d_in, d_out)
     scratch = _new(x, (size,), _t._torch.uint8) if size else None
-    _check(fn["expert_product"](xp, _type(x, "x"), ld, x_rows, wp, ldw, es, turned, offset.data_ptr(), rp, places, experts, d_in, d_out, y.data_ptr(), ldy,
+    _check(fn["expert_product"](xp, kind, ld, x_rows, wp, ldw, es, turned, offset.data_ptr(), rp, places, experts, d_in, d_out, y.data_ptr(), ldy,
                                 scratch.data_ptr() if size else None, size, _t._stream(at)), "expert_product")
     if out is not None:
         _t._written(out)
@@ -283,9 +281,10 @@ def expert_product_backward(dy, x, w, offset, row=None, need_dx=True, need_dw=Tr
         made = _new(w, (experts, d_out, d_in) if turned else (experts, d_in, d_out), w.dtype)
         dw, dwp, ldd = made.transpose(1, 2) if turned else made, made.data_ptr(), d_in if turned else d_out
     gp, xp, wp = dy.data_ptr(), x.data_ptr(), w.data_ptr()
-    size = _scratch("expert_product_backward_scratch_bytes", gp & 255, ldg, places, xp & 255, ld, x_rows, wp & 255, ldw, es, turned, experts, d_in, d_out)
+    kind = _type(x, "x")
+    size = _scratch("expert_product_backward_scratch_bytes", gp & 255, ldg, places, xp & 255, kind, ld, x_rows, wp & 255, ldw, es, turned, experts, d_in, d_out)
     scratch = _new(x, (size,), _t._torch.uint8) if size else None
-    _check(fn["expert_product_backward"](gp, ldg, xp, _type(x, "x"), ld, x_rows, wp, ldw, es, turned, offset.data_ptr(), rp, places, experts, d_in, d_out,
+    _check(fn["expert_product_backward"](gp, ldg, xp, kind, ld, x_rows, wp, ldw, es, turned, offset.data_ptr(), rp, places, experts, d_in, d_out,
                                          None if dx is None else dx.data_ptr(), d_in, dwp, ldd, d_in * d_out, scratch.data_ptr() if size else None, size,
                                          _t._stream(at)), "expert_product_backward")
     return dx, dw

@@ -47,7 +47,7 @@ def test_route_backward_refuses():
 def test_expert_product_refuses():
     good = dict(x=P, type=2, ldx=64, x_rows=100, w=2 * P, ldw=32, sw=64 * 32, turned=0, offset=P, row=None, places=100, experts=4, d_in=64, d_out=32, y=3 * P, ldy=32, scratch=None, size=0)
     refuses("expert_product", good, (
-        dict(x=None), dict(x=P + 1), dict(type=0), dict(type=3), dict(ldx=-1), dict(x_rows=99), dict(x_rows=-1), dict(x_rows=1 << 31, places=5), dict(w=None), dict(w=P + 1),
+        dict(x=None), dict(x=P + 1), dict(type=-1), dict(type=3), dict(ldx=-1), dict(x_rows=99), dict(x_rows=-1), dict(x_rows=1 << 31, places=5), dict(w=None), dict(w=P + 1),
         dict(ldw=-1), dict(sw=-1), dict(turned=2), dict(offset=None), dict(offset=P + 2), dict(row=P + 2), dict(places=-1), dict(places=1 << 31, x_rows=1 << 31),
         dict(experts=0), dict(experts=513), dict(d_in=0), dict(d_out=0), dict(d_in=(1 << 30) + 1), dict(y=None), dict(y=P), dict(y=2 * P), dict(y=3 * P + 1), dict(ldy=31)),
         (dict(places=0, x=None, y=None),))
@@ -57,7 +57,7 @@ def test_expert_product_backward_refuses():
     good = dict(dy=P, lddy=32, x=2 * P, type=1, ldx=64, x_rows=100, w=3 * P, ldw=32, sw=64 * 32, turned=0, offset=P, row=None, places=100, experts=4, d_in=64, d_out=32,
                 dx=4 * P, lddx=64, dw=5 * P, lddw=32, sdw=64 * 32, scratch=None, size=0)
     refuses("expert_product_backward", good, (
-        dict(dy=None), dict(dy=P + 1), dict(lddy=-1), dict(x=None), dict(x=P + 1), dict(type=0), dict(ldx=-1), dict(x_rows=50), dict(w=None), dict(w=P + 1), dict(ldw=-1),
+        dict(dy=None), dict(dy=P + 1), dict(lddy=-1), dict(x=None), dict(x=P + 1), dict(type=3), dict(ldx=-1), dict(x_rows=50), dict(w=None), dict(w=P + 1), dict(ldw=-1),
         dict(sw=-1), dict(turned=-1), dict(offset=None), dict(row=P + 1), dict(places=-1), dict(experts=0), dict(experts=600), dict(d_in=0), dict(d_out=-1),
         dict(dx=None, dw=None), dict(dx=P), dict(dx=4 * P + 1), dict(lddx=63), dict(dw=P), dict(dw=2 * P), dict(dw=4 * P), dict(dw=5 * P + 1), dict(lddw=31), dict(sdw=64 * 32 - 1),
         dict(turned=1, lddw=63)),
@@ -67,22 +67,25 @@ def test_expert_product_backward_refuses():
 def test_products_want_scratch_where_rows_do_not_begin_on_16_bytes():
     fns = experts._load()
     size = fns["expert_product_scratch_bytes"]
-    assert size(P, 64, 100, P, 32, 64 * 32, 0, 4, 64, 32) == 0
+    assert size(P, 2, 64, 100, P, 32, 64 * 32, 0, 4, 64, 32) == 0
+    assert size(P, 0, 64, 100, P, 32, 64 * 32, 0, 4, 64, 32) == 3 * (100 * 64 * 2 + 4 * 64 * 32 * 2)
+    assert size(P, 5, 64, 100, P, 32, 64 * 32, 0, 4, 64, 32) == 0 and size(P, 0, 64, 1 << 30, P, 32, 64 * 32, 0, 4, 64, 32) == 0
     copy_x, copy_w = 100 * 64 * 2, 4 * 64 * 32 * 2
     for kw in (dict(x=P + 2), dict(ldx=65), dict(ldx=0)):
         a = {**dict(x=P, ldx=64), **kw}
-        assert size(a["x"], a["ldx"], 100, P, 32, 64 * 32, 0, 4, 64, 32) == copy_x, kw
+        assert size(a["x"], 1, a["ldx"], 100, P, 32, 64 * 32, 0, 4, 64, 32) == copy_x, kw
     for kw in (dict(w=P + 8), dict(ldw=33, sw=64 * 33), dict(sw=0), dict(sw=64 * 32 + 1)):
         a = {**dict(w=P, ldw=32, sw=64 * 32), **kw}
-        assert size(P, 64, 100, a["w"], a["ldw"], a["sw"], 0, 4, 64, 32) == copy_w, kw
-    assert size(P, 65, 0, P, 32, 65 * 32, 0, 4, 65, 32) == 0 and size(P, 64, -1, P, 32, 0, 0, 4, 64, 32) == 0
-    both = fns["expert_product_backward_scratch_bytes"](P, 33, 100, P, 65, 100, P, 33, 65 * 33, 0, 4, 65, 33)
+        assert size(P, 2, 64, 100, a["w"], a["ldw"], a["sw"], 0, 4, 64, 32) == copy_w, kw
+    assert size(P, 2, 65, 0, P, 32, 65 * 32, 0, 4, 65, 32) == 0 and size(P, 2, 64, -1, P, 32, 0, 0, 4, 64, 32) == 0
+    both = fns["expert_product_backward_scratch_bytes"](P, 33, 100, P, 2, 65, 100, P, 33, 65 * 33, 0, 4, 65, 33)
     assert both == sum(-(-n // 256) * 256 for n in (100 * 40 * 2, 100 * 72 * 2, 4 * 65 * 40 * 2))
     good = dict(x=P, type=2, ldx=65, x_rows=100, w=2 * P, ldw=32, sw=65 * 32, turned=0, offset=P, row=None, places=100, experts=4, d_in=65, d_out=32, y=3 * P, ldy=32,
                 scratch=P, size=-(-100 * 72 * 2 // 256) * 256)
     fn = fns["expert_product"]
-    for kw in (dict(scratch=None), dict(scratch=P + 16), dict(size=good["size"] - 1), dict(size=0)):
+    for kw in (dict(scratch=None), dict(scratch=P + 16), dict(size=good["size"] - 1), dict(size=0), dict(type=0)):
         assert fn(*{**good, **kw}.values(), None) == gem.E_WORKSPACE, kw
+    assert fn(*{**good, **dict(type=0, x_rows=1 << 30, row=P, places=1 << 30)}.values(), None) == gem.E_INVALID
 
 
 def test_combine_refuses():

@@ -67,20 +67,21 @@ def check(places, experts, d_in, d_out, dtype, turned=False, gather=0, pad=0, fi
 SHAPES = [(1, 1, 8, 8), (1, 4, 64, 64), (5, 3, 64, 72), (129, 2, 768, 128), (300, 5, 200, 264), (513, 7, 1000, 136), (1000, 3, 72, 1024), (2100, 11, 256, 520)]
 
 
-@pytest.mark.parametrize("dtype", [F16, BF16], ids=name)
+@pytest.mark.parametrize("dtype", [F32, F16, BF16], ids=name)
 @pytest.mark.parametrize("turned", [False, True], ids=["plain", "turned"])
 @pytest.mark.parametrize("shape", SHAPES, ids=lambda s: "x".join(map(str, s)))
 def test_aligned(shape, turned, dtype):
     check(*shape, dtype, turned, seed=sum(shape))
 
 
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=name)
 @pytest.mark.parametrize("turned", [False, True], ids=["plain", "turned"])
 @pytest.mark.parametrize("shape", SHAPES, ids=lambda s: "x".join(map(str, s)))
-def test_gathered(shape, turned):
-    check(*shape, BF16, turned, gather=max(1, shape[0] // 3), seed=sum(shape))
+def test_gathered(shape, turned, dtype):
+    check(*shape, dtype, turned, gather=max(1, shape[0] // 3), seed=sum(shape))
 
 
-@pytest.mark.parametrize("dtype", [F16, BF16], ids=name)
+@pytest.mark.parametrize("dtype", [F32, F16, BF16], ids=name)
 @pytest.mark.parametrize("gather", [0, 40], ids=["as they are", "gathered"])
 @pytest.mark.parametrize("turned", [False, True], ids=["plain", "turned"])
 @pytest.mark.parametrize("shape", [(1, 1, 1, 1), (3, 2, 5, 7), (130, 3, 33, 65), (257, 4, 1001, 131), (700, 5, 129, 515)], ids=lambda s: "x".join(map(str, s)))
@@ -92,6 +93,7 @@ def test_odd_widths(shape, turned, gather, dtype):
 @pytest.mark.parametrize("gather", [0, 50], ids=["as they are", "gathered"])
 def test_strides_and_alignment(pad, first, gather):
     check(200, 3, 136, 72, BF16, False, gather, pad, first)
+    check(200, 3, 136, 72, F32, True, gather, pad, first)
 
 
 @pytest.mark.parametrize("turned", [False, True], ids=["plain", "turned"])
@@ -100,7 +102,7 @@ def test_many_tiles(places, experts, d_in, d_out, turned):
     check(places, experts, d_in, d_out, BF16, turned, gather=places // 2, uneven=True)
 
 
-@pytest.mark.parametrize("dtype", [F16, BF16], ids=name)
+@pytest.mark.parametrize("dtype", [F32, F16, BF16], ids=name)
 @pytest.mark.parametrize("gather", [0, 1500], ids=["as they are", "gathered"])
 @pytest.mark.parametrize("turned", [False, True], ids=["plain", "turned"])
 @pytest.mark.parametrize("places,experts,d_in,d_out", [(6000, 6, 520, 1160), (9000, 16, 768, 328), (4097, 2, 1544, 2056)])
@@ -153,12 +155,34 @@ def test_nothing_to_do(d_in, d_out):
     assert (gem.expert_product_backward(matrix(5, d_out, BF16, 2), x, w, offset, row)[1] == 0).all()
 
 
+def test_float32_of_any_size():
+    """Columns from the smallest to the largest numbers: what is split into three parts is exact there too."""
+    x, w = matrix(90, 64, F32, 1), weights(2, 64, 72, F32, 2)
+    x *= torch.exp2(torch.arange(90, device="cuda") * 2.0 - 100)[:, None]
+    offset = torch.tensor([0, 40, 90], dtype=torch.int32, device="cuda")
+    y = gem.expert_product(x, w, offset)
+    assert_within(y, *ref.product(x, w, offset))
+    one = torch.eye(64, device="cuda").expand(2, 64, 64).contiguous()
+    big = torch.tensor([3.4028235e38, -3.4028235e38, 3.39e38, 1.5 * 2.0 ** -120], dtype=torch.float64).float().cuda().repeat(90, 16)
+    got = gem.expert_product(big, one, offset)
+    assert ((got.double() - big.double()).abs() <= 4 * 2.0 ** -24 * big.double().abs()).all()
+    x[7, 3] = float("inf")
+    y = gem.expert_product(x, w, offset)
+    assert not torch.isfinite(y[7]).any() and torch.isfinite(torch.cat([y[:7], y[8:]])).all()
+
+
 def test_outputs_given_and_parts_of_wider_ones():
     offset = split(300, 4, 1)
     x, w = matrix(300, 128, BF16, 1), weights(4, 128, 100, BF16, 2)
+    for dtype in (BF16, F32):
+        x, w = x.to(dtype), w.to(dtype)
+        outputs_given(x, w, offset, dtype)
+
+
+def outputs_given(x, w, offset, dtype):
     want = gem.expert_product(x, w, offset)
     for left, wide in ((8, 128), (5, 131)):
-        whole = torch.full((300, wide), 7.0, dtype=BF16, device="cuda")
+        whole = torch.full((300, wide), 7.0, dtype=dtype, device="cuda")
         out = whole[:, left:left + 100]
         assert gem.expert_product(x, w, offset, out=out) is out
         assert torch.equal(out, want) and (whole[:, :left] == 7).all() and (whole[:, left + 100:] == 7).all()

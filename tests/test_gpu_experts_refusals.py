@@ -36,7 +36,8 @@ def test_products():
     x, w = torch.randn(6, 16, device="cuda").to(BF16), torch.randn(3, 16, 8, device="cuda").to(BF16)
     o, row = torch.zeros(4, dtype=torch.int32, device="cuda"), torch.zeros(5, dtype=torch.int32, device="cuda")
     dy = torch.zeros(6, 8, device="cuda", dtype=BF16)
-    no(gem.expert_product, x.float(), w.float(), o)
+    no(gem.expert_product, x.float(), w, o)
+    no(gem.expert_product, x.double(), w.double(), o)
     no(gem.expert_product, x, w.half(), o)
     no(gem.expert_product, x[:, :15], w, o)
     no(gem.expert_product, x, w[:, :, ::2], o)
