@@ -19,7 +19,7 @@
 //   warps 0, 2      TMA loads of A and of B, each SM its own
 //   warp 1          (first SM) issues the MMAs
 //   warps 4-11      epilogue: a quarter of the rows and a half of the columns each; accumulators are double-buffered in TMEM
-//   warps 12-15     (BY_INDEX) rows that are named by index, four at a time: a box cannot; one thread each
+//   warps 12-19     (BY_INDEX) rows that are named by index, four at a time: a box cannot; one thread each
 //
 // An expert's last, cut rows where they are the K dimension are loaded by warps 0 and 2 by index too, rows behind the last as zeros.
 // TMA wants rows that begin on 16 bytes; operands whose rows do not are copied first, into scratch (k_copy_rows), as FP32 ones are
@@ -38,6 +38,9 @@ constexpr int kTileM = 128;                       // rows of a tile an SM
 constexpr int kChunk = 64;                        // of K a stage: 128 bytes
 constexpr int kRow = kChunk * 2;                  // bytes of a row in shared memory
 constexpr int kBox = 64 * kRow;                   // bytes of 64 rows
+
+constexpr int kParts = 8;                         // warps that load rows by index
+constexpr int threads_of(bool by_index) { return by_index ? 384 + 32 * kParts : 384; }
 
 enum Mode { kRowsTimesPlain = 0, kRowsTimesTurned = 1, kWeights = 2 };
 
@@ -423,13 +426,13 @@ __device__ __forceinline__ void products(const Product& q)
     const auto tile = [&](int t) { return tile_at<MODE, BN, HEIGHT>(q, first, tile0, t); };
     // A stage's rounds differ by their parity alone, so a thread that waits for free stages may not fall a round behind, nor run a
     // round ahead: each one loads something of every chunk (or counts its bytes), and a chunk is not full without it.
-    // Loads of four rows by each of the warps 12 to 15: of A's rows there are (rows).
-    const auto loads_of = [](int rows) { return max(1, (min(kTileM, rows) + 15) / 16); };
+    // Loads of four rows by each of the warps 12 to 19: of A's rows there are (rows).
+    const auto loads_of = [](int rows) { return max(1, (min(kTileM, rows) + 4 * kParts - 1) / (4 * kParts)); };
 
     if (warp == 0 || warp == 2) {
         const bool is_a = warp == 0, counts = is_a && rank == 0;                  // the bytes of a stage
         const Operand& o = is_a ? q.a : q.b;
-        const bool others = BY_INDEX && (A_K ? is_a : o.gather != 0);             // warps 12 to 15 load it
+        const bool others = BY_INDEX && (A_K ? is_a : o.gather != 0);             // warps 12 to 19 load it
         if ((counts || !others) && one_thread()) {
             const CUtensorMap* by_box = is_a ? &q.ta : &q.tb;
             const CUtensorMap* by_index = is_a ? &q.ra : &q.rb;
@@ -443,7 +446,7 @@ __device__ __forceinline__ void products(const Product& q)
                 uint32_t a_bytes = SMS * S::A;
                 if (A_K && BY_INDEX) {
                     a_bytes = 0;
-                    for (int i = 0; i < SMS; ++i) a_bytes += 16 * kRow * loads_of(w.stop - w.c_row - i * kTileM);
+                    for (int i = 0; i < SMS; ++i) a_bytes += 4 * kParts * kRow * loads_of(w.stop - w.c_row - i * kTileM);
                 }
                 for (int term = 0; term < q.terms && on; ++term) {
                     const int image = is_a ? a_image(q, term) : b_image(q, term), image_row = image * (int)o.rows;
@@ -558,24 +561,25 @@ __device__ __forceinline__ void products(const Product& q)
             const int a_row = w.c_row + rank * kTileM, b_col = w.n0 + rank * BC;
             if (A_K) {
                 if (one_thread()) {
-                    int4 named[8];                          // every fourth four of A's rows
+                    constexpr int LOADS = kTileM / (4 * kParts);
+                    int4 named[LOADS];                      // every eighth four of A's rows
                     const int loads = loads_of(w.stop - a_row);
                     int s = (int)(g % S::STAGES);
                     uint32_t parity = (g / S::STAGES & 1u) ^ 1u;
                     for (int term = 0; term < q.terms && on && w.k; ++term) {
 #pragma unroll
-                        for (int i = 0; i < 8; ++i) named[i] = rows_at(q, q.a, a_image(q, term), a_row + 4 * (4 * i + part), w.stop);
+                        for (int i = 0; i < LOADS; ++i) named[i] = rows_at(q, q.a, a_image(q, term), a_row + 4 * (kParts * i + part), w.stop);
                         for (int k = 0; k < w.k; k += kChunk) {
                             on = wait_for(free_(s), parity, dead);
                             if (!on) break;
                             const uint32_t to = stages + (uint32_t)s * S::STAGE + (uint32_t)(4 * part * kRow), bar = of_first<SMS>(full(s));
-                            if (loads == 8) {
+                            if (loads == LOADS) {
 #pragma unroll
-                                for (int i = 0; i < 8; ++i) load_rows<SMS>(to + (uint32_t)(16 * i * kRow), &q.ra, k, named[i], bar);
+                                for (int i = 0; i < LOADS; ++i) load_rows<SMS>(to + (uint32_t)(4 * kParts * i * kRow), &q.ra, k, named[i], bar);
                             } else {
 #pragma unroll
-                                for (int i = 0; i < 7; ++i)
-                                    if (i < loads) load_rows<SMS>(to + (uint32_t)(16 * i * kRow), &q.ra, k, named[i], bar);
+                                for (int i = 0; i < LOADS - 1; ++i)
+                                    if (i < loads) load_rows<SMS>(to + (uint32_t)(4 * kParts * i * kRow), &q.ra, k, named[i], bar);
                             }
                             if (++s == S::STAGES) { s = 0; parity ^= 1u; }
                         }
@@ -584,12 +588,12 @@ __device__ __forceinline__ void products(const Product& q)
                 on = __all_sync(0xffffffffu, on);
                 g += (uint32_t)(w.k + kChunk - 1) / kChunk * (uint32_t)q.terms;
             } else {
-                // A quarter of a chunk's places: lane i has the i-th's row, read four chunks ahead.
-                constexpr int AHEAD = 4;
+                // An eighth of a chunk's places: lane i has the i-th's row, read four chunks ahead.
+                constexpr int AHEAD = 4, OWN = kChunk / kParts;
                 const Operand& o = q.a.gather ? q.a : q.b;
                 const CUtensorMap* map = q.a.gather ? &q.ra : &q.rb;
                 const int x = q.a.gather ? a_row : b_col, boxes = q.a.gather ? A_BOXES : B_BOXES;
-                const int end = w.k_first + w.k, mine = w.k_first + 16 * part + (lane & 15);
+                const int end = w.k_first + w.k, mine = w.k_first + OWN * part + lane % OWN;
                 for (int term = 0; term < q.terms && on; ++term) {
                     const uint32_t rows = (uint32_t)o.rows, none = q.terms == 1 ? rows : 3 * rows, base = rows * (uint32_t)(q.a.gather ? a_image(q, term) : b_image(q, term));
                     int ahead[AHEAD];
@@ -607,15 +611,15 @@ __device__ __forceinline__ void products(const Product& q)
                             const int r = (int)((uint32_t)ahead[u] < rows ? (uint32_t)ahead[u] + base : none);
                             const int next = mine + k + AHEAD * kChunk;
                             ahead[u] = next < end ? __ldg(q.row + next) : -1;
-                            int4 named[4];
+                            int4 named[OWN / 4];
 #pragma unroll
-                            for (int i = 0; i < 4; ++i)
+                            for (int i = 0; i < OWN / 4; ++i)
                                 named[i] = make_int4(__shfl_sync(0xffffffffu, r, 4 * i), __shfl_sync(0xffffffffu, r, 4 * i + 1), __shfl_sync(0xffffffffu, r, 4 * i + 2),
                                                      __shfl_sync(0xffffffffu, r, 4 * i + 3));
                             if (one_thread()) {
-                                const uint32_t to = stages + (uint32_t)s * S::STAGE + (q.a.gather ? 0 : S::A) + (uint32_t)(16 * part * kRow), bar = of_first<SMS>(full(s));
+                                const uint32_t to = stages + (uint32_t)s * S::STAGE + (q.a.gather ? 0 : S::A) + (uint32_t)(OWN * part * kRow), bar = of_first<SMS>(full(s));
 #pragma unroll
-                                for (int i = 0; i < 4; ++i)
+                                for (int i = 0; i < OWN / 4; ++i)
                                     for (int b = 0; b < boxes; ++b) load_rows<SMS>(to + (uint32_t)(b * kBox + i * 4 * kRow), map, x + 64 * b, named[i], bar);
                             }
                             __syncwarp();
@@ -633,9 +637,9 @@ __device__ __forceinline__ void products(const Product& q)
 }
 
 template <int MODE, int BN, bool BY_INDEX>
-__global__ void __launch_bounds__(BY_INDEX ? 512 : 384, 1) k_expert(const __grid_constant__ Product q) { products<MODE, BN, 1, BY_INDEX>(q); }
+__global__ void __launch_bounds__(threads_of(BY_INDEX), 1) k_expert(const __grid_constant__ Product q) { products<MODE, BN, 1, BY_INDEX>(q); }
 template <int MODE, bool BY_INDEX>
-__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(BY_INDEX ? 512 : 384, 1) k_expert_pair(const __grid_constant__ Product q)
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(threads_of(BY_INDEX), 1) k_expert_pair(const __grid_constant__ Product q)
 {
     products<MODE, 256, 2, BY_INDEX>(q);
 }
@@ -742,7 +746,7 @@ int launch(const Product& q, int sms, int64_t tiles, bool by_index, cudaStream_t
         return GEM_NLR_E_CUDA;
     }
     const int64_t most = kTrainSMs / sms;
-    kern<<<(unsigned)(sms * (tiles < most ? tiles : most)), by_index ? 512 : 384, SHARED, st>>>(q);
+    kern<<<(unsigned)(sms * (tiles < most ? tiles : most)), threads_of(by_index), SHARED, st>>>(q);
     return launched();
 }
 
