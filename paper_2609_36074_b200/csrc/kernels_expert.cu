@@ -21,6 +21,9 @@
 //   warps 4-11      epilogue: a quarter of the rows and a half of the columns each; accumulators are double-buffered in TMEM
 //   warps 12-19     (BY_INDEX) rows that are named by index, four at a time: a box cannot; one thread each
 //
+// Few experts with many rows have few tiles of dW and long sums: these are taken in `splits` parts of an expert's rows, each its own
+// matrix of FP32 partial sums, which k_join_parts adds in order.
+//
 // An expert's last, cut rows where they are the K dimension are loaded by warps 0 and 2 by index too, rows behind the last as zeros.
 // TMA wants rows that begin on 16 bytes; operands whose rows do not are copied first, into scratch (k_copy_rows), as FP32 ones are
 // split (k_split_rows).
@@ -73,6 +76,7 @@ struct Product {
     int terms;                // products of images: 1, or 6 of FP32's
     void* c;
     int64_t ldc, stride_c;
+    int splits;               // weights: parts of an expert's rows, a matrix each, all experts' first parts first
     int c_wide;
     uint32_t idesc;
     int bf16, f32;            // operands; C
@@ -82,9 +86,9 @@ struct Product {
 __device__ __forceinline__ int a_image(const Product& q, int i) { return q.terms == 1 ? 0 : 0x001102 >> (4 * i) & 3; }
 __device__ __forceinline__ int b_image(const Product& q, int i) { return q.terms == 1 ? 0 : 0x010120 >> (4 * i) & 3; }
 
-// (C is in memory, and a tile has at least 32 of its elements: tiles are counted in 32 bits.)
+// (C, or its parts, is in memory, and a tile has at least 32 of its elements: tiles are counted in 32 bits.)
 struct Tile {
-    int expert;
+    int expert, matrix;       // matrix: of C (weights)
     int c_row, stop;          // first row of C and the one behind the last (rows: places; weights: of C_e)
     int n0;
     int k_first;              // weights: first place
@@ -93,9 +97,9 @@ struct Tile {
 
 // ---- barriers and instructions of one SM or a pair -----------------------------------------------------------------------------
 
-__device__ __forceinline__ bool wait_for(uint32_t bar, uint32_t parity, volatile uint32_t* dead)
+__device__ __forceinline__ bool wait_for(uint32_t bar, uint32_t parity, volatile uint32_t* dead, uint64_t limit = kSpinLimit)
 {
-    for (uint32_t i = 0; i < kSpinLimit; ++i) {
+    for (uint64_t i = 0; i < limit; ++i) {
         if (mbar_try_wait(bar, parity)) return true;
         if ((i & 63u) == 63u && *dead) return false;
     }
@@ -240,11 +244,16 @@ __device__ __forceinline__ Tile tile_at(const Product& q, const int32_t* first, 
     w.n0 = (t - row_tile * nt) * BN;
     if (MODE == kWeights) {
         const int mt = (q.m + HEIGHT - 1) / HEIGHT;
-        w.expert = row_tile / mt;
-        w.c_row = (row_tile - w.expert * mt) * HEIGHT;
+        w.matrix = row_tile / mt;
+        const int part = w.matrix / q.experts;
+        w.expert = w.matrix - part * q.experts;
+        w.c_row = (row_tile - w.matrix * mt) * HEIGHT;
         w.stop = q.m;
-        w.k_first = first[w.expert];
-        w.k = first[w.expert + 1] - first[w.expert];
+        const int rows = first[w.expert + 1] - first[w.expert];
+        const int each = (rows / q.splits + kChunk) / kChunk * kChunk;                   // of a part, in whole chunks
+        const int begin = q.splits == 1 ? 0 : min(rows, part * each);
+        w.k_first = first[w.expert] + begin;
+        w.k = q.splits == 1 ? rows : min(rows - begin, each);
     } else {
         int lo = 0, hi = q.experts;                                  // the last with tile0[e] <= row_tile
         while (lo < hi) {
@@ -279,7 +288,7 @@ __device__ __forceinline__ int4 rows_at(const Product& q, const Operand& o, int 
 template <int MODE>
 __device__ __forceinline__ void store_tile(const Product& q, const Tile& w, int row0, int col0, int steps, uint32_t acc, uint32_t mine, int lane, bool on)
 {
-    uint16_t* c = (uint16_t*)q.c + (MODE == kWeights ? w.expert * q.stride_c : 0) + row0 * q.ldc;
+    uint16_t* c = (uint16_t*)q.c + (MODE == kWeights ? w.matrix * q.stride_c : 0) + row0 * q.ldc;
     const int rows = min(32, w.stop - row0);
     const uint32_t to_stage = mine + (uint32_t)(lane * 64), phase = (uint32_t)(lane >> 1) & 3u;
     const uint32_t from_stage = mine + (uint32_t)((lane >> 2) * 64 + (((lane & 3) ^ ((lane >> 3) & 3)) << 4));
@@ -335,7 +344,7 @@ __device__ __forceinline__ void store_tile(const Product& q, const Tile& w, int 
 template <int MODE>
 __device__ __forceinline__ void store_tile_32(const Product& q, const Tile& w, int row0, int col0, int steps, uint32_t acc, uint32_t mine, int lane, bool on)
 {
-    float* c = (float*)q.c + (MODE == kWeights ? w.expert * q.stride_c : 0) + row0 * q.ldc;
+    float* c = (float*)q.c + (MODE == kWeights ? w.matrix * q.stride_c : 0) + row0 * q.ldc;
     const int rows = min(32, w.stop - row0);
     const uint32_t to_stage = mine + (uint32_t)(lane * 64), phase = (uint32_t)(lane >> 1) & 3u;
     const uint32_t from_stage = mine + (uint32_t)((lane >> 2) * 64 + (((lane & 3) ^ ((lane >> 3) & 3)) << 4));
@@ -421,7 +430,7 @@ __device__ __forceinline__ void products(const Product& q)
     const uint32_t tmem = *tmem_at;
 
     const int nt = (q.n + BN - 1) / BN;
-    const int tiles = (MODE == kWeights ? q.experts * ((q.m + HEIGHT - 1) / HEIGHT) : tile0[q.experts + 1]) * nt;
+    const int tiles = (MODE == kWeights ? q.splits * q.experts * ((q.m + HEIGHT - 1) / HEIGHT) : tile0[q.experts + 1]) * nt;
     const int begin = blockIdx.x / SMS, step = gridDim.x / SMS;
     const auto tile = [&](int t) { return tile_at<MODE, BN, HEIGHT>(q, first, tile0, t); };
     // A stage's rounds differ by their parity alone, so a thread that waits for free stages may not fall a round behind, nor run a
@@ -537,7 +546,8 @@ __device__ __forceinline__ void products(const Product& q)
         for (int t = begin; t < tiles; t += step) {
             const Tile w = tile(t);
             if (w.k && on) {
-                on = wait_for(acc_full(i & 1), (i >> 1) & 1, dead);
+                // (a sum takes its chunks' time: some 10 attempts each)
+                on = wait_for(acc_full(i & 1), (i >> 1) & 1, dead, kSpinLimit + (uint64_t)256 * q.terms * (uint32_t)(w.k / kChunk));
                 on = __all_sync(0xffffffffu, on);
                 tc_fence_after();
             }
@@ -678,6 +688,35 @@ k_copy_rows(const uint16_t* __restrict__ from, int64_t ld, int64_t stride, int64
     }
 }
 
+// The parts' sums, in their order: n columns of m rows of `experts` matrices.  Four columns a thread.
+template <typename T>
+__global__ void __launch_bounds__(256)
+k_join_parts(const float* __restrict__ part, int64_t ld_part, int64_t stride_part, int parts, int m, int n, int experts, T* __restrict__ to, int64_t ld, int64_t stride)
+{
+    const int vecs = (n + 3) / 4;
+    const int64_t all = (int64_t)experts * m, steps = (all + blockDim.y - 1) / blockDim.y;
+    for (int64_t s = blockIdx.x; s < steps; s += gridDim.x) {
+        const int64_t i = s * blockDim.y + threadIdx.y;
+        if (i >= all) continue;
+        const int64_t e = i / m, row = i - e * m;
+        for (int c = threadIdx.x; c < vecs; c += blockDim.x) {
+            const float* p = part + e * stride_part + row * ld_part + c * 4;
+            float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+            for (int x = 0; x < parts; ++x) {
+                const float4 v = __ldg(reinterpret_cast<const float4*>(p + x * experts * stride_part));
+                sum.x += v.x; sum.y += v.y; sum.z += v.z; sum.w += v.w;
+            }
+            T* at = to + e * stride + row * ld + c * 4;
+            const int left = n - c * 4;
+            at[0] = from_f<T>(sum.x);
+            if (left > 1) at[1] = from_f<T>(sum.y);
+            if (left > 2) at[2] = from_f<T>(sum.z);
+            if (left > 3) at[3] = from_f<T>(sum.w);
+        }
+    }
+}
+
 // FP32 rows to three images of BF16 rows that begin on 16 bytes, `image` elements from one to the next: the nearest, the nearest of what
 // is left, and the rest, which is exact.  (What rounds beyond BF16's range is cut instead; infinities and NaN have no rest.)
 __global__ void __launch_bounds__(256)
@@ -756,7 +795,7 @@ int run_tiles(Product& q, int64_t tiles, bool by_index, cudaStream_t st)
     constexpr bool A_K = MODE != kWeights, B_K = MODE == kRowsTimesTurned;
     // boxes where an operand is read by boxes, rows where it is read by index (weights: an expert's last rows)
     const bool boxes_a = A_K ? !by_index : !q.a.gather, boxes_b = A_K || !q.b.gather;
-    const int images = q.f32 ? 3 : 1;
+    const int images = q.terms == 1 ? 1 : 3;
     if ((boxes_a && !encode(&q.ta, q.a, 0, images, A_K ? kTileM : kChunk, q.bf16)) ||
         (boxes_b && !encode(&q.tb, q.b, A_K ? q.experts : 0, images, B_K ? BN / SMS : kChunk, q.bf16)) ||
         (!(A_K && !by_index) && !encode(&q.ra, q.a, 0, images, 1, q.bf16)) || (!A_K && !encode(&q.rb, q.b, 0, images, 1, q.bf16)))
@@ -776,16 +815,16 @@ int run(Product& q, cudaStream_t st)
 {
     // row tiles there can be: an expert's last one may be almost empty, and places without an expert have one more
     const auto tiles = [&](int height, int bn) {
-        const int64_t row_tiles = MODE == kWeights ? (int64_t)q.experts * ((q.m + height - 1) / height)
+        const int64_t row_tiles = MODE == kWeights ? (int64_t)q.splits * q.experts * ((q.m + height - 1) / height)
                                                    : q.places / height + (q.places < q.experts + 1 ? q.places : q.experts + 1);
         return row_tiles * ((q.n + bn - 1) / bn);
     };
     const int64_t rows = MODE == kWeights ? q.m : q.places / q.experts;
     // few rows of A a tile: those alone, by index, instead of boxes of 128
     const bool by_index = q.a.gather || q.b.gather || (MODE != kWeights && rows < 32);
-    if (rows >= 2 * kTileM && tiles(2 * kTileM, 256) >= kTrainSMs / 2) return run_tiles<MODE, 256, 2>(q, tiles(2 * kTileM, 256), by_index, st);
-    if (tiles(kTileM, 256) >= kTrainSMs) return run_tiles<MODE, 256, 1>(q, tiles(kTileM, 256), by_index, st);
-    if (tiles(kTileM, 128) >= kTrainSMs) return run_tiles<MODE, 128, 1>(q, tiles(kTileM, 128), by_index, st);
+    if (q.splits == 1 && rows >= 2 * kTileM && tiles(2 * kTileM, 256) >= kTrainSMs / 2) return run_tiles<MODE, 256, 2>(q, tiles(2 * kTileM, 256), by_index, st);
+    if (q.splits == 1 && tiles(kTileM, 256) >= kTrainSMs) return run_tiles<MODE, 256, 1>(q, tiles(kTileM, 256), by_index, st);
+    if (q.splits > 1 ? q.n > 64 : tiles(kTileM, 128) >= kTrainSMs) return run_tiles<MODE, 128, 1>(q, tiles(kTileM, 128), by_index, st);
     return run_tiles<MODE, 64, 1>(q, tiles(kTileM, 64), by_index, st);
 }
 
@@ -836,6 +875,21 @@ bool sizes_fine(int type, int64_t x_rows, int64_t places, int32_t experts, int32
     const int64_t images = type == GEM_NLR_F32 ? 3 : 1;
     return type_bytes(type) && x_rows >= 0 && x_rows <= INT32_MAX / images && places >= 0 && places <= kMaxPlaces / images && experts >= 1 && experts <= GEM_NLR_MAX_EXPERTS &&
            d_in >= 1 && d_in <= kMaxColumns && d_out >= 1 && d_out <= kMaxColumns && (turned == 0 || turned == 1) && (rows_named || x_rows >= places);
+}
+
+// Parts of the experts' sums in dW (m x n): as many as give every SM a tile of 128 x 128 where even 128 x 64 in one part do not, with
+// 256 rows each.
+int splits_of(int64_t places, int experts, int64_t m, int64_t n)
+{
+    const int64_t tall = experts * ((m + kTileM - 1) / kTileM);
+    if (tall * ((n + 63) / 64) >= kTrainSMs) return 1;
+    const int64_t most = kTrainSMs / (tall * ((n + 127) / 128)), rows = places / experts / 256;
+    return (int)(most < rows ? (most < 1 ? 1 : most) : rows < 1 ? 1 : rows);
+}
+size_t parts_bytes(int64_t places, int experts, int64_t m, int64_t n)
+{
+    const int splits = splits_of(places, experts, m, n);
+    return splits == 1 ? 0 : ((size_t)splits * experts * m * ((n + 3) / 4 * 4) * 4 + 255) / 256 * 256;
 }
 
 // `count` matrices of zeros.
@@ -891,6 +945,7 @@ extern "C" int gem_nlr_expert_product(const void* x_dev, int32_t type, int64_t l
     q.bf16 = type != GEM_NLR_F16;
     q.f32 = type == GEM_NLR_F32;
     q.terms = q.f32 ? 6 : 1;
+    q.splits = 1;
     return w_turned ? run<kRowsTimesTurned>(q, st) : run<kRowsTimesPlain>(q, st);
 }
 
@@ -900,7 +955,8 @@ extern "C" size_t gem_nlr_expert_product_backward_scratch_bytes(const void* dy_d
 {
     if (!sizes_fine(type, x_rows, places, experts, d_in, d_out, w_turned, true) || ld_dy < 0 || ld_x < 0 || ld_w < 0 || stride_w < 0) return 0;
     return copy_bytes(places_of(dy_dev, ld_dy, places, d_out, false), 1, type) + copy_bytes(places_of(x_dev, ld_x, x_rows, d_in, false), 1, type) +
-           copy_bytes(weights_of(w_dev, ld_w, stride_w, w_turned, d_in, d_out), experts, type);
+           copy_bytes(weights_of(w_dev, ld_w, stride_w, w_turned, d_in, d_out), experts, type) +
+           parts_bytes(places, experts, w_turned ? d_out : d_in, w_turned ? d_in : d_out);
 }
 
 extern "C" int gem_nlr_expert_product_backward(const void* dy_dev, int64_t ld_dy, const void* x_dev, int32_t type, int64_t ld_x, int64_t x_rows, const void* w_dev,
@@ -921,7 +977,7 @@ extern "C" int gem_nlr_expert_product_backward(const void* dy_dev, int64_t ld_dy
     if (places == 0) return dw_dev ? clear(dw_dev, type_bytes(type), ld_dw, stride_dw, tall, wide, experts, st) : GEM_NLR_OK;
     Operand dy = places_of(dy_dev, ld_dy, places, d_out, false), x = places_of(x_dev, ld_x, x_rows, d_in, row_dev != nullptr);
     Operand weights = weights_of(w_dev, ld_w, stride_w, w_turned, d_in, d_out);
-    if (!scratch_fine(scratch_dev, scratch_bytes, copy_bytes(dy, 1, type) + (dw_dev ? copy_bytes(x, 1, type) : 0) + (dx_dev ? copy_bytes(weights, experts, type) : 0))) return GEM_NLR_E_WORKSPACE;
+    if (!scratch_fine(scratch_dev, scratch_bytes, copy_bytes(dy, 1, type) + (dw_dev ? copy_bytes(x, 1, type) + parts_bytes(places, experts, tall, wide) : 0) + (dx_dev ? copy_bytes(weights, experts, type) : 0))) return GEM_NLR_E_WORKSPACE;
     char* scratch = (char*)scratch_dev;
     if (!bring(dy, 1, type, scratch, st)) return GEM_NLR_E_CUDA;
     Product q = {};
@@ -932,6 +988,7 @@ extern "C" int gem_nlr_expert_product_backward(const void* dy_dev, int64_t ld_dy
     q.bf16 = type != GEM_NLR_F16;
     q.f32 = type == GEM_NLR_F32;
     q.terms = q.f32 ? 6 : 1;
+    q.splits = 1;
     if (dx_dev) {
         if (!bring(weights, experts, type, scratch, st)) return GEM_NLR_E_CUDA;
         q.a = dy;
@@ -956,5 +1013,19 @@ extern "C" int gem_nlr_expert_product_backward(const void* dy_dev, int64_t ld_dy
     q.ldc = ld_dw;
     q.stride_c = stride_dw;
     q.c_wide = on_16(dw_dev, ld_dw, stride_dw, type_bytes(type));
-    return run<kWeights>(q, st);
+    q.splits = splits_of(places, experts, tall, wide);
+    if (q.splits == 1) return run<kWeights>(q, st);
+    q.c = scratch;
+    q.f32 = 1;
+    q.c_wide = 1;
+    q.ldc = (wide + 3) / 4 * 4;
+    q.stride_c = tall * q.ldc;
+    const int rc = run<kWeights>(q, st);
+    if (rc != GEM_NLR_OK) return rc;
+    const RowBlocks sh = row_blocks(experts * tall, (int)(q.ldc / 4));
+    return by_type(type, [&](auto t) {
+        using T = decltype(t);
+        k_join_parts<T><<<sh.grid, sh.block, 0, st>>>((const float*)q.c, q.ldc, q.stride_c, q.splits, q.m, q.n, experts, (T*)dw_dev, ld_dw, stride_dw);
+        return launched();
+    });
 }

@@ -21,6 +21,7 @@ namespace {
 
 constexpr int kThreads = 1024, kWarps = kThreads / 32;
 constexpr int kBlocks = kTrainSMs;                 // at most
+constexpr int64_t kMaxPlaces = INT32_MAX - (1 << 16);           // int arithmetic on places stays far from its end
 constexpr int kMaxChosen = 32, kMaxGroups = 32;
 constexpr unsigned kAll = 0xffffffffu;
 
@@ -910,7 +911,7 @@ extern "C" int gem_nlr_route(const void* logits_dev, int32_t type, int64_t ld, c
     if (!tb || n < 0 || experts < 1 || experts > GEM_NLR_MAX_EXPERTS || k < 1 || k > kMaxChosen || (score != GEM_NLR_SOFTMAX && score != GEM_NLR_SIGMOID) ||
         groups < 1 || groups > kMaxGroups || experts % groups || kept_groups < 1 || kept_groups > groups || k > kept_groups * (experts / groups) ||
         (group_best != 1 && group_best != 2) || (renormalize != 0 && renormalize != 1) || !isfinite(scale) || !aligned_to(bias_dev, 4) || !ints(offset_dev) ||
-        n > INT32_MAX / k)
+        n > kMaxPlaces / k)
         return GEM_NLR_E_INVALID;
     if (n > 0 && (!logits_dev || !aligned_to(logits_dev, tb) || ld < 0 || !ints(expert_dev) || !ints(weight_dev) || !ints(row_dev) || !ints(place_dev)))
         return GEM_NLR_E_INVALID;
@@ -944,7 +945,7 @@ extern "C" int gem_nlr_route_backward(const float* dweight_dev, const void* logi
 {
     const int tb = type_bytes(type);
     if (!tb || n < 0 || experts < 1 || experts > GEM_NLR_MAX_EXPERTS || k < 1 || k > kMaxChosen || (score != GEM_NLR_SOFTMAX && score != GEM_NLR_SIGMOID) ||
-        (renormalize != 0 && renormalize != 1) || !isfinite(scale) || n > INT32_MAX / k)
+        (renormalize != 0 && renormalize != 1) || !isfinite(scale) || n > kMaxPlaces / k)
         return GEM_NLR_E_INVALID;
     if (n == 0) return GEM_NLR_OK;
     if (!logits_dev || !aligned_to(logits_dev, tb) || ld < 0 || !ints(dweight_dev) || !ints(expert_dev) || !dlogits_dev || !aligned_to(dlogits_dev, tb) ||

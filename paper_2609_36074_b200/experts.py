@@ -32,6 +32,7 @@ from .training import _check, _given, _rows, _type
 _SCORES = {"softmax": 0, "sigmoid": 1}
 _KINDS = {"identity": 0, "silu": 1, "gelu": 2, "tanh": 3}
 MAX_EXPERTS = 512
+MAX_PLACES = (1 << 31) - (1 << 16)
 
 
 class Routing(NamedTuple):
@@ -152,7 +153,7 @@ def route(logits, k, score="softmax", bias=None, groups=1, kept_groups=None, gro
         raise ValueError(f"{experts} experts in {groups} groups, {kept_groups} of them kept by their {group_best} best")
     if not 1 <= k <= min(32, kept_groups * (experts // groups)):
         raise ValueError(f"k is {k}: 1 to 32 and at most the experts that are kept")
-    if n * k >= 1 << 31:
+    if n * k >= MAX_PLACES:
         raise ValueError(f"{n} rows to {k} experts each: places are int32")
     if not abs(scale) < float("inf"):
         raise ValueError(f"scale is {scale}")
@@ -178,7 +179,7 @@ def route_backward(dweight, logits, expert, score="softmax", renormalize=True, s
     kind, how = _type(logits, "logits"), _score(score)
     if experts > MAX_EXPERTS:
         raise ValueError(f"{experts} experts: 1 to {MAX_EXPERTS}")
-    if expert.dim() != 2 or not 1 <= expert.shape[1] <= 32 or n * expert.shape[1] >= 1 << 31:
+    if expert.dim() != 2 or not 1 <= expert.shape[1] <= 32 or n * expert.shape[1] >= MAX_PLACES:
         raise ValueError(f"expert has to be ({n}, k) with k from 1 to 32")
     if not abs(scale) < float("inf"):
         raise ValueError(f"scale is {scale}")

@@ -30,7 +30,7 @@ def test_route_refuses():
         dict(z=None), dict(z=P + 2), dict(type=3), dict(type=-1), dict(ld=-1), dict(bias=P + 1), dict(n=-1), dict(experts=0), dict(experts=513, groups=1, kept=1), dict(k=0),
         dict(k=9), dict(k=33, experts=64), dict(score=2), dict(score=-1), dict(groups=0), dict(groups=3), dict(groups=33, experts=66), dict(kept=0), dict(kept=5),
         dict(best=0), dict(best=3), dict(renorm=2), dict(scale=math.inf), dict(scale=math.nan), dict(expert=None), dict(weight=P + 2), dict(offset=None), dict(offset=P + 1),
-        dict(row=None), dict(place=P + 3), dict(n=1 << 29)))
+        dict(row=None), dict(place=P + 3), dict(n=1 << 29), dict(n=(1 << 29) - (1 << 14))))
     fn = fns["route"]
     for kw in (dict(scratch=None), dict(scratch=P + 16), dict(size=size - 1), dict(size=0)):
         assert fn(*{**good, **kw}.values(), None) == gem.E_WORKSPACE, kw

@@ -110,6 +110,14 @@ def test_large_tiles(places, experts, d_in, d_out, turned, gather, dtype):
     check(places, experts, d_in, d_out, dtype, turned, gather, uneven=True, seed=places + turned)
 
 
+@pytest.mark.parametrize("dtype", [F32, F16, BF16], ids=name)
+@pytest.mark.parametrize("gather", [0, 900], ids=["as they are", "gathered"])
+@pytest.mark.parametrize("places,experts,d_in,d_out", [(20000, 2, 64, 64), (9001, 1, 33, 200), (4096, 3, 256, 40), (70000, 4, 100, 130), (600, 1, 16, 16), (3000, 5, 130, 72)])
+def test_long_sums_in_parts(places, experts, d_in, d_out, gather, dtype):
+    check(places, experts, d_in, d_out, dtype, False, gather, seed=places)
+    check(places, experts, d_in, d_out, dtype, True, gather, uneven=True, seed=places + 1)
+
+
 @pytest.mark.parametrize("gather", [0, 4000], ids=["as they are", "gathered"])
 @pytest.mark.parametrize("experts", [1, 3, 40])
 def test_many_tiles_a_block(experts, gather):
