@@ -11,10 +11,13 @@ namespace gemnlr {
 namespace {
 
 constexpr int kThreads = 256;
+// Blocks an SM: threads enough for the latency of 16-bit rows, at 32 registers each (combine of 32768 x 4 rows of 768 BF16 48 us, with the
+// 39 registers it would take 55; two rows a thread, 60 registers, 74).
+template <typename T, bool WIDE, int SLOTS> constexpr int kBlocks = WIDE && sizeof(T) == 2 && SLOTS <= 4 ? 8 : 1;
 
 // Eight columns a thread: x along a row, y over rows.
 template <typename T, bool WIDE, int SLOTS>
-__global__ void __launch_bounds__(kThreads)
+__global__ void __launch_bounds__(kThreads, kBlocks<T, WIDE, SLOTS>)
 k_combine(const T* __restrict__ y, int64_t ldy, int64_t places, const int32_t* __restrict__ place, const float* __restrict__ weight,
           int64_t n, int k, int d, T* __restrict__ out, int64_t ldo)
 {
@@ -55,7 +58,7 @@ k_combine(const T* __restrict__ y, int64_t ldy, int64_t places, const int32_t* _
 
 // TPR threads share a row t; NT threads a block.
 template <typename T, bool WIDE, int SLOTS, int TPR>
-__global__ void __launch_bounds__(kThreads)
+__global__ void __launch_bounds__(kThreads, kBlocks<T, WIDE, SLOTS>)
 k_combine_backward(const T* __restrict__ dout, int64_t ldo, const T* __restrict__ y, int64_t ldy, int64_t places,
                    const int32_t* __restrict__ place, const float* __restrict__ weight, const int32_t* __restrict__ offset, int experts,
                    int64_t n, int k, int d, T* __restrict__ dy, int64_t lddy, float* __restrict__ dweight)
