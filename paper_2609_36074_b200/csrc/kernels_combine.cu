@@ -4,7 +4,8 @@
 //   backward   dy_place(t,j) = w_tj dout_t,  dw_tj = <dout_t, y_place(t,j)>
 //
 // Bound by HBM: y is read once, in rows; a row of dout is read once for all its slots, 2, 4 or 8 of which are taken together.  Sums in
-// FP32, in a fixed order.
+// FP32, in a fixed order.  32768 rows of 768 BF16 with 4 slots: 48.5 us forward (5.2 TB/s; 39 at the rate of a copy), 83 us back (5.5 TB/s; 70).
+// A row is a warp's in the gradient, or a block's where fewer rows than warps there are would leave SMs without work.
 #include "expert_common.cuh"
 
 namespace gemnlr {

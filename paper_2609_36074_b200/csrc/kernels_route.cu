@@ -11,6 +11,10 @@
 // precision), the warp chooses that row again in FP64.  One row in a hundred is, at 128 experts with sigmoid scores.  Weights are
 // taken from the chosen logits anew.
 //
+// Measured: 65536 rows to 6 of 128 experts in 8 groups 54 us with the plan (45 choosing, of which 6 wait for the few rows in FP64, and 9 for
+// the places), bound by issue: 390 instructions a row; a warp a row with a reduction a round took 148 + 15.  The gradient of
+// 131072 x 64 BF16 20.5 us (1.8 TB/s), bound by latency and issue; with every slot's share offered to every lane it was 32.
+//
 // The order is a counting sort that keeps the rows of an expert in order, without atomics whose order shows: blocks own
 // consecutive rows, count their experts and rank their entries; the second kernel adds the counts of the blocks before (each
 // block reads all of them, 148 x experts numbers) and the sums over the experts.  Few rows are one block and one launch.

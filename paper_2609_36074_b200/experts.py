@@ -96,6 +96,8 @@ def _there(fn, stream, inputs, *args):
 
 def _new(like, shape, dtype):
     """A contiguous tensor on like's device.  (empty_strided is torch's shortest way to one: 1.4 us, empty() 2.3.)"""
+    if len(shape) == 2:
+        return _t._torch.empty_strided(shape, (shape[1], 1), dtype=dtype, device=like.device)
     strides, step = [], 1
     for n in reversed(shape):
         strides.append(step)
