@@ -25,8 +25,8 @@
 // matrix of FP32 partial sums, which k_join_parts adds in order.
 //
 // An expert's last, cut rows where they are the K dimension are loaded by warps 0 and 2 by index too, rows behind the last as zeros.
-// TMA wants rows that begin on 16 bytes; operands whose rows do not are copied first, into scratch (k_copy_rows), as FP32 ones are
-// split (k_split_rows).
+// TMA wants rows that begin on 16 bytes; operands whose rows do not are copied first, into scratch (k_copy_rows), where FP32
+// ones are split.
 // Every wait is bounded; after one that runs out the block issues nothing more and its remaining tiles are NaN.
 //
 // Measured on 131072 rows of 32 experts, 768 x 2048 BF16 (412 GFLOP, a library's product of one matrix of these sizes takes 316 us): x W
@@ -660,37 +660,77 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(threads_of(BY_INDEX)
     products<MODE, 256, 2, BY_INDEX>(q);
 }
 
-// Rows of `columns` elements from anywhere to rows that begin on 16 bytes, `rows` of them for each expert.  Sixteen bytes a thread,
-// from two aligned vectors where they are inside the row and from single elements at its ends.
-__global__ void __launch_bounds__(256)
-k_copy_rows(const uint16_t* __restrict__ from, int64_t ld, int64_t stride, int64_t rows, int64_t all_rows, int columns, uint16_t* __restrict__ to, int64_t to_ld)
+// Operands that the loads cannot take, all in one launch: rows of `columns` elements from anywhere to rows that begin on 16 bytes,
+// `rows` of them for each expert.  Threads lie x along a row (eight elements each) and y over rows.
+struct Source {
+    const void* from;
+    int64_t ld, stride, rows, all, to_ld, image;          // all: rows of all experts; image: elements from one image to the next (FP32)
+    uint16_t* to;
+    int columns, x, y, blocks;
+};
+struct Sources {
+    Source s[3];
+    int count, blocks;
+};
+
+// 16 bytes from two aligned vectors where they are inside the row, from single elements at its ends.
+__device__ __forceinline__ void copy_8(const uint16_t* row, int c, int columns, uint16_t* to, int64_t)
 {
-    const int vecs = (columns + 7) / 8;
-    const int64_t steps = (all_rows + blockDim.y - 1) / blockDim.y;
-    for (int64_t s = blockIdx.x; s < steps; s += gridDim.x) {
-        const int64_t i = s * blockDim.y + threadIdx.y;
-        if (i >= all_rows) continue;
-        const int64_t e = rows == all_rows ? 0 : i / rows;
-        const uint16_t* row = from + e * stride + (i - e * rows) * ld;
-        for (int c = threadIdx.x; c < vecs; c += blockDim.x) {
-            const uint16_t* p = row + c * 8;
-            const int off = (int)(((uintptr_t)p & 15) >> 1);                  // elements behind a 16-byte boundary
-            uint32_t h[4] = {0, 0, 0, 0};
-            if (c > 0 && (c + 2) * 8 <= columns) {
-                const uint4 a = __ldg(reinterpret_cast<const uint4*>(p - off)), b = __ldg(reinterpret_cast<const uint4*>(p - off) + 1);
-                const uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
-                uint32_t v[5];
+    const uint16_t* p = row + c * 8;
+    const int off = (int)(((uintptr_t)p & 15) >> 1);                  // elements behind a 16-byte boundary
+    uint32_t h[4] = {0, 0, 0, 0};
+    if (c > 0 && (c + 2) * 8 <= columns) {
+        const uint4 a = __ldg(reinterpret_cast<const uint4*>(p - off)), b = __ldg(reinterpret_cast<const uint4*>(p - off) + 1);
+        const uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+        uint32_t v[5];
 #pragma unroll
-                for (int x = 0; x < 5; ++x) v[x] = off < 2 ? w[x] : off < 4 ? w[x + 1 < 8 ? x + 1 : 7] : off < 6 ? w[x + 2 < 8 ? x + 2 : 7] : w[x + 3 < 8 ? x + 3 : 7];
+        for (int x = 0; x < 5; ++x) v[x] = off < 2 ? w[x] : off < 4 ? w[x + 1] : off < 6 ? w[x + 2] : w[x + 3];
 #pragma unroll
-                for (int x = 0; x < 4; ++x) h[x] = off & 1 ? __funnelshift_r(v[x], v[x + 1], 16) : v[x];
-            } else {
+        for (int x = 0; x < 4; ++x) h[x] = off & 1 ? __funnelshift_r(v[x], v[x + 1], 16) : v[x];
+    } else {
 #pragma unroll
-                for (int x = 0; x < 8; ++x)
-                    if (c * 8 + x < columns) h[x >> 1] |= (uint32_t)__ldg(p + x) << (16 * (x & 1));
-            }
-            *reinterpret_cast<uint4*>(to + i * to_ld + c * 8) = make_uint4(h[0], h[1], h[2], h[3]);
+        for (int x = 0; x < 8; ++x)
+            if (c * 8 + x < columns) h[x >> 1] |= (uint32_t)__ldg(p + x) << (16 * (x & 1));
+    }
+    *reinterpret_cast<uint4*>(to) = make_uint4(h[0], h[1], h[2], h[3]);
+}
+
+// FP32 to three images of BF16: the nearest, the nearest of what is left, and the rest, which is exact.  (What rounds beyond BF16's
+// range is cut instead; infinities and NaN have no rest.)
+__device__ __forceinline__ void copy_8(const float* row, int c, int columns, uint16_t* to, int64_t image)
+{
+    const float* p = row + c * 8;
+    float v[8];
+    if (((uintptr_t)p & 15) == 0 && c * 8 + 8 <= columns) load8<true>(p, 8, v);
+    else load8<false>(p, columns - c * 8, v);
+#pragma unroll
+    for (int part = 0; part < 3; ++part) {
+        uint32_t h[4] = {0, 0, 0, 0};
+#pragma unroll
+        for (int x = 0; x < 8; ++x) {
+            const uint32_t bits = __float_as_uint(v[x]), magnitude = bits & 0x7fffffffu;
+            uint32_t near = (bits + 0x7fffu + (bits >> 16 & 1u)) >> 16;
+            if (magnitude >= 0x7f7f8000u) near = magnitude > 0x7f800000u ? 0x7fffu : bits >> 16;
+            h[x >> 1] |= near << (16 * (x & 1));
+            v[x] = magnitude >= 0x7f800000u ? 0.0f : v[x] - __uint_as_float(near << 16);
         }
+        *reinterpret_cast<uint4*>(to + part * image) = make_uint4(h[0], h[1], h[2], h[3]);
+    }
+}
+
+template <typename T>
+__global__ void __launch_bounds__(256)
+k_copy_rows(const __grid_constant__ Sources all)
+{
+    int b = blockIdx.x, which = 0;
+    while (b >= all.s[which].blocks) b -= all.s[which++].blocks;
+    const Source& o = all.s[which];
+    const int tx = threadIdx.x % o.x, ty = threadIdx.x / o.x, vecs = (o.columns + 7) / 8;
+    if (ty >= o.y) return;
+    for (int64_t i = (int64_t)b * o.y + ty; i < o.all; i += (int64_t)o.blocks * o.y) {
+        const int64_t e = o.rows == o.all ? 0 : i / o.rows;
+        const T* row = (const T*)o.from + e * o.stride + (i - e * o.rows) * o.ld;
+        for (int c = tx; c < vecs; c += o.x) copy_8(row, c, o.columns, o.to + i * o.to_ld + c * 8, o.image);
     }
 }
 
@@ -719,40 +759,6 @@ k_join_parts(const float* __restrict__ part, int64_t ld_part, int64_t stride_par
             if (left > 1) at[1] = from_f<T>(sum.y);
             if (left > 2) at[2] = from_f<T>(sum.z);
             if (left > 3) at[3] = from_f<T>(sum.w);
-        }
-    }
-}
-
-// FP32 rows to three images of BF16 rows that begin on 16 bytes, `image` elements from one to the next: the nearest, the nearest of what
-// is left, and the rest, which is exact.  (What rounds beyond BF16's range is cut instead; infinities and NaN have no rest.)
-__global__ void __launch_bounds__(256)
-k_split_rows(const float* __restrict__ from, int64_t ld, int64_t stride, int64_t rows, int64_t all_rows, int columns, uint16_t* __restrict__ to, int64_t to_ld, int64_t image)
-{
-    const int vecs = (columns + 7) / 8;
-    const int64_t steps = (all_rows + blockDim.y - 1) / blockDim.y;
-    for (int64_t s = blockIdx.x; s < steps; s += gridDim.x) {
-        const int64_t i = s * blockDim.y + threadIdx.y;
-        if (i >= all_rows) continue;
-        const int64_t e = rows == all_rows ? 0 : i / rows;
-        const float* row = from + e * stride + (i - e * rows) * ld;
-        for (int c = threadIdx.x; c < vecs; c += blockDim.x) {
-            const float* p = row + c * 8;
-            float v[8];
-            if (((uintptr_t)p & 15) == 0 && c * 8 + 8 <= columns) load8<true>(p, 8, v);
-            else load8<false>(p, columns - c * 8, v);
-#pragma unroll
-            for (int part = 0; part < 3; ++part) {
-                uint32_t h[4] = {0, 0, 0, 0};
-#pragma unroll
-                for (int x = 0; x < 8; ++x) {
-                    const uint32_t bits = __float_as_uint(v[x]), magnitude = bits & 0x7fffffffu;
-                    uint32_t near = (bits + 0x7fffu + (bits >> 16 & 1u)) >> 16;
-                    if (magnitude >= 0x7f7f8000u) near = magnitude > 0x7f800000u ? 0x7fffu : bits >> 16;
-                    h[x >> 1] |= near << (16 * (x & 1));
-                    v[x] = magnitude >= 0x7f800000u ? 0.0f : v[x] - __uint_as_float(near << 16);
-                }
-                *reinterpret_cast<uint4*>(to + part * image + i * to_ld + c * 8) = make_uint4(h[0], h[1], h[2], h[3]);
-            }
         }
     }
 }
@@ -849,23 +855,27 @@ size_t copy_bytes(const Operand& o, int experts, int type)
     return in_place(o, experts, type) ? 0 : ((size_t)o.rows * experts * pitch_of(o.columns) * (type == GEM_NLR_F32 ? 6 : 2) + 255) / 256 * 256;
 }
 
-// The operand, copied or split into `scratch` where it has to be.
-bool bring(Operand& o, int experts, int type, char*& scratch, cudaStream_t st)
+// Where the operand is to be read: where it is, or in `scratch`, with what has to be copied there added to `list`.
+void bring(Operand& o, int experts, int type, char*& scratch, Sources& list)
 {
     if (experts < 2) o.stride = o.rows * o.ld;
-    if (in_place(o, experts, type)) return true;
+    if (in_place(o, experts, type)) return;
     const int64_t all = o.rows * experts, pitch = pitch_of(o.columns);
     const RowBlocks sh = row_blocks(all, (int)(pitch / 8));
-    char* here = scratch;
+    list.s[list.count++] = {o.p, o.ld, o.stride, o.rows, all, pitch, all * pitch, (uint16_t*)scratch, o.columns, (int)sh.block.x, (int)sh.block.y, (int)sh.grid.x};
+    list.blocks += (int)sh.grid.x;
     scratch += copy_bytes(o, experts, type);
-    if (type == GEM_NLR_F32)
-        k_split_rows<<<sh.grid, sh.block, 0, st>>>((const float*)o.p, o.ld, o.stride, o.rows, all, o.columns, (uint16_t*)here, pitch, all * pitch);
-    else
-        k_copy_rows<<<sh.grid, sh.block, 0, st>>>(o.p, o.ld, o.stride, o.rows, all, o.columns, (uint16_t*)here, pitch);
-    o.p = (const uint16_t*)here;
+    o.p = list.s[list.count - 1].to;
     o.ld = pitch;
     o.stride = o.rows * pitch;
-    return launched() == GEM_NLR_OK;
+}
+
+int copy(const Sources& list, int type, cudaStream_t st)
+{
+    if (!list.count) return GEM_NLR_OK;
+    if (type == GEM_NLR_F32) k_copy_rows<float><<<list.blocks, 256, 0, st>>>(list);
+    else k_copy_rows<uint16_t><<<list.blocks, 256, 0, st>>>(list);
+    return launched();
 }
 
 Operand places_of(const void* p, int64_t ld, int64_t rows, int columns, bool gather) { return {(const uint16_t*)p, ld, 0, rows, columns, gather}; }
@@ -938,7 +948,10 @@ extern "C" int gem_nlr_expert_product(const void* x_dev, int32_t type, int64_t l
     if (!scratch_fine(scratch_dev, scratch_bytes, copy_bytes(q.a, 1, type) + copy_bytes(q.b, experts, type))) return GEM_NLR_E_WORKSPACE;
     if (x_rows == 0) return clear(y_dev, type_bytes(type), ld_y, 0, places, d_out, 1, st);
     char* scratch = (char*)scratch_dev;
-    if (!bring(q.a, 1, type, scratch, st) || !bring(q.b, experts, type, scratch, st)) return GEM_NLR_E_CUDA;
+    Sources list = {};
+    bring(q.a, 1, type, scratch, list);
+    bring(q.b, experts, type, scratch, list);
+    if (copy(list, type, st) != GEM_NLR_OK) return GEM_NLR_E_CUDA;
     q.offset = offset_dev;
     q.row = row_dev;
     q.places = places;
@@ -985,7 +998,11 @@ extern "C" int gem_nlr_expert_product_backward(const void* dy_dev, int64_t ld_dy
     Operand weights = weights_of(w_dev, ld_w, stride_w, w_turned, d_in, d_out);
     if (!scratch_fine(scratch_dev, scratch_bytes, copy_bytes(dy, 1, type) + (dw_dev ? copy_bytes(x, 1, type) + parts_bytes(places, experts, tall, wide) : 0) + (dx_dev ? copy_bytes(weights, experts, type) : 0))) return GEM_NLR_E_WORKSPACE;
     char* scratch = (char*)scratch_dev;
-    if (!bring(dy, 1, type, scratch, st)) return GEM_NLR_E_CUDA;
+    Sources list = {};
+    bring(dy, 1, type, scratch, list);
+    if (dx_dev) bring(weights, experts, type, scratch, list);
+    if (dw_dev && x_rows > 0) bring(x, 1, type, scratch, list);
+    if (copy(list, type, st) != GEM_NLR_OK) return GEM_NLR_E_CUDA;
     Product q = {};
     q.offset = offset_dev;
     q.row = row_dev;
@@ -996,7 +1013,6 @@ extern "C" int gem_nlr_expert_product_backward(const void* dy_dev, int64_t ld_dy
     q.terms = q.f32 ? 6 : 1;
     q.splits = 1;
     if (dx_dev) {
-        if (!bring(weights, experts, type, scratch, st)) return GEM_NLR_E_CUDA;
         q.a = dy;
         q.b = weights;
         q.n = d_in;
@@ -1009,7 +1025,6 @@ extern "C" int gem_nlr_expert_product_backward(const void* dy_dev, int64_t ld_dy
     }
     if (!dw_dev) return GEM_NLR_OK;
     if (x_rows == 0) return clear(dw_dev, type_bytes(type), ld_dw, stride_dw, tall, wide, experts, st);
-    if (!bring(x, 1, type, scratch, st)) return GEM_NLR_E_CUDA;
     q.a = w_turned ? dy : x;
     q.b = w_turned ? x : dy;
     q.m = (int)tall;

@@ -100,6 +100,50 @@ def test_scores_that_32_bits_do_not_tell_apart(score):
     check(z, 8, score, bias, 8, 4, 2)
 
 
+@pytest.mark.parametrize("score", ["softmax", "sigmoid"])
+@pytest.mark.parametrize("e", [12, 40, 128, 300])
+def test_biases_of_any_size(e, score):
+    """Biases beyond the scores, beyond the keys' range, of both signs, and experts put out of reach."""
+    z = logits(120, e)
+    for scale in (0.5, 3.0, 40.0, 1e6):
+        check(z, min(6, e), score, biases(e, 3) * 20 * scale)
+    out = biases(e, 4)
+    out[::3] = -1e9
+    check(z, 4, score, out)
+    check(z, e // 2 + 1 if e < 60 else 9, score, out)
+    out[1], out[2] = INF, -INF
+    check(z, 4, score, out)
+    out[:] = 0.25
+    check(z, 4, score, out, 4, 2, 2)
+
+
+def test_a_bias_that_is_not_a_number():
+    z, bias = logits(20, 16), biases(16)
+    bias[3] = NAN
+    r = gem.route(z, 2, "sigmoid", bias)
+    assert (r.expert == -1).all() and torch.isnan(r.weight).all() and r.offset.sum() == 0
+
+
+def test_two_streams_at_once():
+    """Two plans and two products at a time, each on a stream of its own."""
+    z = [logits(3000, 32, seed=i) for i in range(2)]
+    x = torch.randn(3000, 96, device="cuda").bfloat16()
+    w = torch.randn(32, 96, 64, device="cuda").bfloat16()
+    want = [gem.route(v, 4) for v in z]
+    y = [gem.expert_product(x, w, r.offset, r.row) for r in want]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in z]
+    for _ in range(10):
+        got = []
+        for v, s in zip(z, streams):
+            with torch.cuda.stream(s):
+                r = gem.route(v, 4)
+                got.append((r, gem.expert_product(x, w, r.offset, r.row)))
+        torch.cuda.synchronize()
+        for (r, p), a, b in zip(got, want, y):
+            assert all(torch.equal(u, v) for u, v in zip(r, a)) and torch.equal(p, b)
+
+
 def test_saturated_scores():
     z = logits(300, 32, F32, spread=30.0)
     check(z, 4, "sigmoid", biases(32))
