@@ -666,6 +666,7 @@ struct Source {
     const void* from;
     int64_t ld, stride, rows, all, to_ld, image;          // all: rows of all experts; image: elements from one image to the next (FP32)
     uint16_t* to;
+    const void* end;                                      // behind the last element of all
     int columns, x, y, blocks;
 };
 struct Sources {
@@ -673,14 +674,15 @@ struct Sources {
     int count, blocks;
 };
 
-// 16 bytes from two aligned vectors where they are inside the row, from single elements at its ends.  (A word a thread instead, from the
-// two that hold it: 3001 x 1001 and 6180 x 1001 elements 22 us, so 13.5.)
-__device__ __forceinline__ void copy_8(const uint16_t* row, int c, int columns, uint16_t* to, int64_t)
+// 16 bytes from two aligned vectors, which may hold other rows' elements too (behind the last column anything may stand), from single
+// elements at the matrix's ends.  (A word a thread instead, from the
+// two that hold it: 3001 x 1001 and 6180 x 1001 elements 22 us, so 11.4.)
+__device__ __forceinline__ void copy_8(const Source& o, const uint16_t* row, int c, uint16_t* to)
 {
     const uint16_t* p = row + c * 8;
     const int off = (int)(((uintptr_t)p & 15) >> 1);                  // elements behind a 16-byte boundary
     uint32_t h[4] = {0, 0, 0, 0};
-    if (c > 0 && (c + 2) * 8 <= columns) {
+    if (p - off >= (const uint16_t*)o.from && p - off + 16 <= (const uint16_t*)o.end) {
         const uint4 a = __ldg(reinterpret_cast<const uint4*>(p - off)), b = __ldg(reinterpret_cast<const uint4*>(p - off) + 1);
         const uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
         uint32_t v[5];
@@ -691,15 +693,17 @@ __device__ __forceinline__ void copy_8(const uint16_t* row, int c, int columns, 
     } else {
 #pragma unroll
         for (int x = 0; x < 8; ++x)
-            if (c * 8 + x < columns) h[x >> 1] |= (uint32_t)__ldg(p + x) << (16 * (x & 1));
+            if (c * 8 + x < o.columns) h[x >> 1] |= (uint32_t)__ldg(p + x) << (16 * (x & 1));
     }
     *reinterpret_cast<uint4*>(to) = make_uint4(h[0], h[1], h[2], h[3]);
 }
 
 // FP32 to three images of BF16: the nearest, the nearest of what is left, and the rest, which is exact.  (What rounds beyond BF16's
 // range is cut instead; infinities and NaN have no rest.)
-__device__ __forceinline__ void copy_8(const float* row, int c, int columns, uint16_t* to, int64_t image)
+__device__ __forceinline__ void copy_8(const Source& o, const float* row, int c, uint16_t* to)
 {
+    const int columns = o.columns;
+    const int64_t image = o.image;
     const float* p = row + c * 8;
     float v[8];
     if (((uintptr_t)p & 15) == 0 && c * 8 + 8 <= columns) load8<true>(p, 8, v);
@@ -731,7 +735,7 @@ k_copy_rows(const __grid_constant__ Sources all)
     for (int64_t i = (int64_t)b * o.y + ty; i < o.all; i += (int64_t)o.blocks * o.y) {
         const int64_t e = o.rows == o.all ? 0 : i / o.rows;
         const T* row = (const T*)o.from + e * o.stride + (i - e * o.rows) * o.ld;
-        for (int c = tx; c < vecs; c += o.x) copy_8(row, c, o.columns, o.to + i * o.to_ld + c * 8, o.image);
+        for (int c = tx; c < vecs; c += o.x) copy_8(o, row, c, o.to + i * o.to_ld + c * 8);
     }
 }
 
@@ -864,7 +868,8 @@ void bring(Operand& o, int experts, int type, char*& scratch, Sources& list)
     if (in_place(o, experts, type)) return;
     const int64_t all = o.rows * experts, pitch = pitch_of(o.columns);
     const RowBlocks sh = row_blocks(all, (int)(pitch / 8));
-    list.s[list.count++] = {o.p, o.ld, o.stride, o.rows, all, pitch, all * pitch, (uint16_t*)scratch, o.columns, (int)sh.block.x, (int)sh.block.y, (int)sh.grid.x};
+    const void* end = (const char*)o.p + ((experts - 1) * o.stride + (o.rows - 1) * o.ld + o.columns) * type_bytes(type);
+    list.s[list.count++] = {o.p, o.ld, o.stride, o.rows, all, pitch, all * pitch, (uint16_t*)scratch, end, o.columns, (int)sh.block.x, (int)sh.block.y, (int)sh.grid.x};
     list.blocks += (int)sh.grid.x;
     scratch += copy_bytes(o, experts, type);
     o.p = list.s[list.count - 1].to;
