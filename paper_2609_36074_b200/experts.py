@@ -27,7 +27,7 @@ from typing import NamedTuple
 
 from . import training as _t
 from .binding import lib
-from .training import _check, _given, _rows, _type
+from .training import _INF, _check, _rows, _type
 
 _SCORES = {"softmax": 0, "sigmoid": 1}
 _KINDS = {"identity": 0, "silu": 1, "gelu": 2, "tanh": 3}
@@ -157,16 +157,18 @@ def route(logits, k, score="softmax", bias=None, groups=1, kept_groups=None, gro
         raise ValueError(f"k is {k}: 1 to 32 and at most the experts that are kept")
     if n * k >= MAX_PLACES:
         raise ValueError(f"{n} rows to {k} experts each: places are int32")
-    if not abs(scale) < float("inf"):
+    if not abs(scale) < _INF:
         raise ValueError(f"scale is {scale}")
     bp = None if bias is None else _floats(bias, (experts,), at, "bias")
-    got = Routing(_new(logits, (n, k), torch.int32), _new(logits, (n, k), torch.float32), _new(logits, (experts + 1,), torch.int32),
-                  _new(logits, (n * k,), torch.int32), _new(logits, (n, k), torch.int32))
+    new, at_gpu, i32 = torch.empty_strided, logits.device, torch.int32            # (written out: five of _new's calls are 2 us)
+    expert, weight = new((n, k), (k, 1), dtype=i32, device=at_gpu), new((n, k), (k, 1), dtype=torch.float32, device=at_gpu)
+    offset, row = new((experts + 1,), (1,), dtype=i32, device=at_gpu), new((n * k,), (1,), dtype=i32, device=at_gpu)
+    place = new((n, k), (k, 1), dtype=i32, device=at_gpu)
     size = _scratch("route_scratch_bytes", n, experts)
-    scratch = _new(logits, (size,), torch.uint8) if size else got.offset
-    _check(fn["route"](logits.data_ptr(), kind, ld, bp, n, experts, k, how, groups, kept_groups, group_best, 1 if renormalize else 0, scale,
-                       *(t.data_ptr() for t in got), scratch.data_ptr(), size, _t._stream(at)), "route")
-    return got
+    scratch = new((size,), (1,), dtype=torch.uint8, device=at_gpu) if size else offset
+    _check(fn["route"](logits.data_ptr(), kind, ld, bp, n, experts, k, how, groups, kept_groups, group_best, 1 if renormalize else 0, scale, expert.data_ptr(),
+                       weight.data_ptr(), offset.data_ptr(), row.data_ptr(), place.data_ptr(), scratch.data_ptr(), size, _t._stream(at)), "route")
+    return Routing(expert, weight, offset, row, place)
 
 
 def route_backward(dweight, logits, expert, score="softmax", renormalize=True, scale=1.0, stream=None):
@@ -183,7 +185,7 @@ def route_backward(dweight, logits, expert, score="softmax", renormalize=True, s
         raise ValueError(f"{experts} experts: 1 to {MAX_EXPERTS}")
     if expert.dim() != 2 or not 1 <= expert.shape[1] <= 32 or n * expert.shape[1] >= MAX_PLACES:
         raise ValueError(f"expert has to be ({n}, k) with k from 1 to 32")
-    if not abs(scale) < float("inf"):
+    if not abs(scale) < _INF:
         raise ValueError(f"scale is {scale}")
     k = expert.shape[1]
     ep, dp = _ints(expert, (n, k), at, "expert"), _floats(dweight, (n, k), at, "dweight")
