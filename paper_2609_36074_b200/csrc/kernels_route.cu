@@ -727,7 +727,7 @@ k_route_backward(const __grid_constant__ RouteGrad r)
     const int rounds = (r.k + LANES - 1) / LANES;
     const int64_t steps = (r.n + ROWS - 1) / ROWS;
     // e^(z - m): 16-bit gradients are off by a tenth of their rounding at most by the fast one (2^-21 of itself at 16 below m)
-    const auto power = [](float z, float m) { return sizeof(T) == 4 ? expf(z - m) : fast_exp2((z - m) * kLog2E); };
+    const auto power = [](float z, float m) { return sizeof(T) == 4 ? expf(z - m) : __expf(z - m); };
     const auto log_score = [&](float x) { return soft || x == -INFINITY ? x : fminf(x, 0.0f) - log1pf(expf(-fabsf(x))); };
     for (int64_t step = blockIdx.x; step < steps; step += gridDim.x) {
         const int64_t row = step * ROWS + threadIdx.x / LANES;

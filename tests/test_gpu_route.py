@@ -240,6 +240,17 @@ def test_gradient_against_differences():
                     assert abs(((loss(a) - loss(b)) / (2 * h)).item() - d[i, j].item()) <= 6 * h * h * v[i].abs().sum().item() + 1e-5
 
 
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=name)
+def test_gradients_next_to_the_smallest_numbers(dtype):
+    z = torch.linspace(-95.0, 0.0, 64, device="cuda").to(dtype).expand(20, 64).contiguous()
+    chosen = torch.tensor([[0, 5, 9, 63]], dtype=torch.int32, device="cuda").expand(20, 4).contiguous()
+    v = logits(20, 4, F32, 3) * 40
+    for score in ("softmax", "sigmoid"):
+        for renorm in (True, False):
+            grad, bound = ref.route_grad(v, z, chosen, score, renorm, 1.0)
+            assert_within(gem.route_backward(v, z, chosen, score, renorm), grad, bound, f"{score} {renorm}")
+
+
 def test_nothing_to_route_and_large_plans():
     r = gem.route(torch.empty(0, 8, device="cuda"), 2)
     assert r.offset.tolist() == [0] * 9 and r.row.numel() == 0
