@@ -416,8 +416,10 @@ int gem_nlr_clip_grad_norm(const gem_nlr_tensor *tensors_host, int32_t count, fl
  * the choice alone).  Row i goes to the k experts of largest c_ij, in falling order, the lowest index first among
  * equals; without a bias the choice is by z_ij.  With groups > 1 the experts are that many groups of neighbours,
  * and only those of the kept_groups best groups can be chosen: a group is as good as the sum of its group_best (1
- * or 2) largest c (without a bias s; with group_best 1 then z), again the lowest index first.  Which of two scores is the larger is
- * decided as in 64 bits (there too, what rounds to the same number is equal).  weight = scale s / sum of the chosen s (renormalize == 1) or scale s (0).
+ * or 2) largest c (without a bias s; with group_best 1 then z), again the lowest index first.  Which of two scores is
+ * the larger is decided as in 64 bits: two that differ there by a rounding or two, made of different terms, may come in
+ * either order.  Equal logits with equal biases are equal.
+ * weight = scale s / sum of the chosen s (renormalize == 1) or scale s (0).
  * logits: n x experts of `type`; bias: experts floats or NULL; expert, weight, place: n x k; offset: experts + 1;
  * row: n k.  1 <= k <= 32, k <= kept_groups experts / groups, experts <= GEM_NLR_MAX_EXPERTS, groups <= 32 and a
  * divisor of experts, n k < 2^31 - 2^16, scale finite.

@@ -497,16 +497,29 @@ __device__ __forceinline__ unsigned route_rows(const Route& r, int64_t row0, int
     sort_keys<V>(key);
     const bool few = r.k < 8;                            // entries of a list that can be reached
     uint32_t last = 0;
+    const auto differs = [&](uint32_t one, uint32_t two) {            // not the same logit with the same bias
+        const int a = (int)(INDEX - (one & INDEX)), b = (int)(INDEX - (two & INDEX));
+        return !(to_f(zr[a]) == to_f(zr[b]) && (!biased || bias[a] == bias[b]));
+    };
     for (int j = 0; j <= r.k; ++j) {
         uint32_t best = key[0];
 #pragma unroll
         for (int o = LANES / 2; o > 0; o >>= 1) best = max(best, __shfl_xor_sync(kAll, best, o));
-        const uint32_t a = last >> BITS, b = best >> BITS;
-        if (j > 0 && a - b <= near && b) {
-            const int before = (int)(INDEX - (last & INDEX)), index = (int)(INDEX - (best & INDEX));
-            unsure |= !(to_f(zr[before]) == to_f(zr[index]) && (!biased || bias[before] == bias[index]));
+        const uint32_t b = best >> BITS;
+        const bool beside = j > 0 && (last >> BITS) - b <= near && b;
+        if (beside) unsure |= differs(last, best);
+        if (j == r.k) {
+            // Behind the border only the next one's key is known to be near.  Where that one is the last one's equal, one that
+            // differs may lie behind it, by its score in 64 bits before both: the last one is compared with all that are near.
+            if ((biased || sizeof(T) == 4) && __any_sync(kAll, beside)) {
+                bool other = false;
+#pragma unroll
+                for (int v = 0; v < V; ++v)
+                    if (beside && (last >> BITS) - (key[v] >> BITS) <= near && key[v] >> BITS) other |= differs(last, key[v]);
+                unsure |= (__ballot_sync(kAll, other) & row_lanes) != 0;
+            }
+            break;
         }
-        if (j == r.k) break;
         unsure |= biased && b == 0u;
         if (me == 0) sp.chosen[mine][j] = b ? (int)(INDEX - (best & INDEX)) : -1;
         last = best;

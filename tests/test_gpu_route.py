@@ -101,6 +101,39 @@ def test_scores_that_32_bits_do_not_tell_apart(score):
 
 
 @pytest.mark.parametrize("score", ["softmax", "sigmoid"])
+@pytest.mark.parametrize("k,equals", [(1, 2), (2, 3), (4, 5), (7, 9), (9, 12)])
+@pytest.mark.parametrize("e", [16, 40, 300])
+def test_equals_at_the_border_before_a_larger_one(e, k, equals, score):
+    """More equals than are chosen, and behind them one that 32 bits do not tell from them and that 64 bits do."""
+    low = 14.0 if score == "sigmoid" else -17.0          # scores of about 1 and 0, apart by some 2^-26
+    step = 0.125
+    z = torch.full((60, e), -30.0, device="cuda")
+    for i in range(60):
+        z[i, :equals] = low
+        z[i, equals + i % (e - equals)] = low + (step if i % 3 else -step)
+        z[i, equals + (i + 1) % (e - equals)] = low + (2 * step if i % 5 else 0.0)
+    bias = torch.full((e,), 0.125, device="cuda")
+    if score == "softmax":
+        z[:, e - 1], bias[e - 1] = 0.0, -0.5             # the largest score, chosen by none
+    for dtype in (F32, F16, BF16):
+        check(z.to(dtype), k, score, bias)
+        check(z.to(dtype), k, score, bias, 4, 4, 2)
+    near = z.clone()                                     # logits apart in their last bits, without a bias
+    near[:, :equals] = 1.0
+    for i in range(60):
+        near[i, equals + i % (e - equals)] = 1.0 + (2.0 ** -22 if i % 3 else -(2.0 ** -22))
+    check(near, k, score)
+
+
+@pytest.mark.parametrize("score", ["softmax", "sigmoid"])
+def test_rows_of_one_score(score):
+    for e, k in ((16, 1), (40, 7), (300, 9)):
+        z = torch.full((500, e), 0.25, device="cuda")
+        got = check(z, k, score, torch.full((e,), 0.125, device="cuda"))
+        assert torch.equal(got.expert, torch.arange(k, device="cuda", dtype=torch.int32).expand(500, k))
+
+
+@pytest.mark.parametrize("score", ["softmax", "sigmoid"])
 @pytest.mark.parametrize("e", [12, 40, 128, 300])
 def test_biases_of_any_size(e, score):
     """Biases beyond the scores, beyond the keys' range, of both signs, and experts put out of reach."""
