@@ -7,11 +7,11 @@
 // index (the lowest index largest), so that the best of a row is a butterfly of maxima and no two are equal: each lane sorts
 // its own once, and a round of the choice is the butterfly and a step of the owner's list.  The score in the key is the logit's upper
 // bits, or with a bias a fixed-point number from an FP32 score that is right to about 2^-20.  Neither tells neighbours apart: where
-// two that follow one another in the choice are too near (and are not the same logit with the same bias, which are equal in any
-// precision), the warp chooses that row again in FP64, after its others.  One row in two thousand is, at 128 experts with sigmoid
+// two that follow one another in the choice, or the last one chosen and any left, are too near (and are not the same logit with the
+// same bias, which are equal in any precision), the warp chooses that row again in FP64, after its others.  One row in two thousand is, at 128 experts with sigmoid
 // scores.  Weights are taken from the chosen logits anew.
 //
-// Measured: 65536 rows to 6 of 128 experts in 8 groups 54 us with the plan (45 choosing, of which 6 wait for the few rows in FP64, and 9 for
+// Measured: 65536 rows to 6 of 128 experts in 8 groups 56.4 us with the plan (47 choosing, of which 6 wait for the few rows in FP64, and 9 for
 // the places), bound by issue: 390 instructions a row; a warp a row with a reduction a round took 148 + 15.  The gradient of
 // 131072 x 64 BF16 20.5 us (1.8 TB/s), bound by latency and issue; with every slot's share offered to every lane it was 32.
 //
